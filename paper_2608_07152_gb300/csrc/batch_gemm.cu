@@ -451,12 +451,14 @@ __global__ void __launch_bounds__(kBatchThreads, 1)
 }
 
 // ---- host side ---------------------------------------------------------------
-bool tensor_map_2d(CUtensorMap* m, CUtensorMapDataType type, int elem, const void* base,
-                   uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
-    typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                      const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                      const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+namespace {
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder, null where it has none.
+EncodeTiledFn encode_tiled() {
     static std::once_flag once;
     static EncodeTiledFn fn = nullptr;
     std::call_once(once, [] {
@@ -469,12 +471,34 @@ bool tensor_map_2d(CUtensorMap* m, CUtensorMapDataType type, int elem, const voi
         else
             cudaGetLastError();
     });
+    return fn;
+}
+}  // namespace
+
+bool tensor_map_2d(CUtensorMap* m, CUtensorMapDataType type, int elem, const void* base,
+                   uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
+    const EncodeTiledFn fn = encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[2] = {cols, rows};
     const cuuint64_t strides[1] = {cols * (uint64_t)elem};
     const cuuint32_t box[2] = {box_cols, box_rows};
     const cuuint32_t estr[2] = {1, 1};
     return fn(m, type, 2, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
+}
+
+bool tensor_map_3d(CUtensorMap* m, CUtensorMapDataType type, int elem, const void* base,
+                   uint64_t parts, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t part_stride,
+                   uint32_t box_cols, uint32_t box_rows) {
+    const EncodeTiledFn fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {cols, rows, parts};
+    const cuuint64_t strides[2] = {ld * (uint64_t)elem, part_stride * (uint64_t)elem};
+    const cuuint32_t box[3] = {box_cols, box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, type, 3, const_cast<void*>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
            CUDA_SUCCESS;

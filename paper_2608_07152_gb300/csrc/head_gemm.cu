@@ -1,0 +1,696 @@
+// Persistent tcgen05 product of the projection head's operators (head_gemm.h).
+//
+// One CTA per SM, 10 warps.  A unit of work is a tile of D (128 x bn) over a
+// range of k; unit u goes to CTA u mod grid.
+//   warp 0     TMA producer: A (128 x 64) and B (bn x 64) chunks into a ring of
+//              four stages, 128-byte swizzle;
+//   warp 1     one thread issues the MMAs (M = 128, N = bn, K = 16, four to
+//              a chunk) into one of two TMEM accumulators;
+//   warps 2-9  epilogue: a TMEM lane (a row of D) per thread; the two warps
+//              that share a lane quarter take every other chunk of 32 columns.
+// Two accumulators let the epilogue of a unit run under the MMAs of the next.
+//
+// Operands.  K contiguous: a box is 64 elements of k (128 bytes) by the tile's
+// rows.  M or N contiguous (gradients contract over rows): a box is 64 of m by
+// 64 of k, so that the operand is never transposed in memory; the matrix
+// descriptor's major bit and its strides say so.
+//
+// Softmax arithmetic is in powers of two: l = acc (a log2 e) + b log2 e, one FMA
+// and one ex2 an entry; sums are float32 of at most 2^7 terms a thread and
+// tile, joined in a fixed order, so a call's results do not depend on timing.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <mutex>
+
+#include "../../include/head.h"
+#include "head_gemm.h"
+#include "kernels.h"
+#include "pvs_common.cuh"
+#include "tc.cuh"
+#include "tensor_map.h"
+
+namespace pvs {
+namespace head {
+
+constexpr int kStageA = kTileM * kTileK * 2;     // 16 KB
+constexpr int kStageB = kTileN * kTileK * 2;     // 32 KB
+constexpr int kStageBytes = kStageA + kStageB;
+constexpr int kStages = 4;
+constexpr int kEpiWarps = 8;
+constexpr int kEpiThreads = kEpiWarps * 32;
+constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr uint32_t kTmemCols = 512;
+constexpr float kLog2e = 1.4426950408889634f;
+
+static_assert(kEpiThreads == kTileN, "an epilogue thread stages one column's bias");
+
+struct Shared {
+    uint64_t full[kStages];
+    uint64_t empty[kStages];
+    uint64_t tfull[2];
+    uint64_t tempty[2];
+    uint32_t tmem_base;
+    int abort;
+    uint32_t masked[2][kTileN / 32];     // items of the tile outside the softmax
+    alignas(16) float b2[2][kTileN];     // their biases, in powers of two
+};
+
+constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + sizeof(Shared);
+static_assert(kSmemBytes <= 227 * 1024, "smem");
+
+__device__ __forceinline__ bool abort_set(Shared& sh) {
+    return *reinterpret_cast<volatile int*>(&sh.abort) != 0;
+}
+__device__ __forceinline__ void raise_abort(Shared& sh, int* status) {
+    *reinterpret_cast<volatile int*>(&sh.abort) = 1;
+    *reinterpret_cast<volatile int*>(status) = PVS_ERR_TIMEOUT;
+}
+
+// M or N contiguous with 128-byte swizzle: 64 elements of m (128 bytes) by 8 of
+// k are an atom of 1024 bytes; SBO is the step to the next 8 of k, LBO to the
+// next 64 of m (the boxes of 64 of k, 8 KB each, lie one after another).
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t smem_addr) {
+    return tc::smem_desc_sw128_kmajor(smem_addr) | ((uint64_t)((kTileK * 128) >> 4) << 16);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const void* tmap, int x, int y, int z,
+                                            uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// 32 bytes to global memory, a whole sector.
+__device__ __forceinline__ void store_32b(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]),
+                 "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ void load_32b(const void* p, uint32_t* v) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]),
+                   "=r"(v[6]), "=r"(v[7])
+                 : "l"(p)
+                 : "memory");
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// The leading 8 bits of two values as bf16, and what is left of them.  Cutting
+// (not rounding) makes the parts exact: three hold a float32's 24 bits, and no
+// finite value becomes an infinity.
+__device__ __forceinline__ uint32_t cut_bf16(float& lo, float& hi) {
+    uint32_t l = __float_as_uint(lo) & 0xffff0000u, h = __float_as_uint(hi) & 0xffff0000u;
+    if (lo != lo) l |= 0x00400000u;   // a NaN stays one
+    if (hi != hi) h |= 0x00400000u;
+    lo = isfinite(lo) ? lo - __uint_as_float(l) : 0.0f;
+    hi = isfinite(hi) ? hi - __uint_as_float(h) : 0.0f;
+    return (l >> 16) | h;
+}
+
+// A unit's tile and range of k.
+struct Unit {
+    int prob, mt, nt, split, k0, k1;
+};
+__device__ __forceinline__ Unit unit_of(const Args& a, int u) {
+    Unit w;
+    w.prob = a.nprob > 1 && u >= a.p[0].units ? 1 : 0;
+    const Problem& p = a.p[w.prob];
+    if (w.prob) u -= a.p[0].units;
+    if (p.m_fast) {
+        w.mt = u % p.mtiles;
+        u /= p.mtiles;
+        w.nt = u % p.ntiles;
+        w.split = u / p.ntiles;
+    } else {
+        w.nt = u % p.ntiles;
+        u /= p.ntiles;
+        w.mt = u % p.mtiles;
+        w.split = u / p.mtiles;
+    }
+    w.k0 = (int)((int64_t)p.kchunks * w.split / p.splits);
+    w.k1 = (int)((int64_t)p.kchunks * (w.split + 1) / p.splits);
+    return w;
+}
+
+// 32 float32 values of one row to `out` of any type: whole sectors where the
+// row is aligned, else one by one.  `valid` of them exist.
+__device__ __forceinline__ void store_row(void* out, int type, int64_t at, const float (&v)[32],
+                                          int valid) {
+    if (type == PVS_F32) {
+        float* o = static_cast<float*>(out) + at;
+        if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 31u) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+                store_32b(o + i, reinterpret_cast<const uint32_t*>(&v[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < valid) o[i] = v[i];
+        }
+        return;
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        w[i] = type == PVS_BF16 ? pack_bf16(v[2 * i], v[2 * i + 1])
+                                : pack_f16(v[2 * i], v[2 * i + 1]);
+    uint16_t* o = static_cast<uint16_t*>(out) + at;
+    if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 31u) == 0) {
+        store_32b(o, w);
+        store_32b(o + 16, w + 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < valid) o[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
+template <int EPI>
+__global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ Args a,
+                                                                int total) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    uint8_t* stages = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
+    Shared& sh = *reinterpret_cast<Shared*>(stages + kStages * kStageBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&sh.full[s], 1);
+            mbar_init(&sh.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sh.tfull[b], 1);
+            mbar_init(&sh.tempty[b], kEpiWarps);
+        }
+        sh.abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        tc::tmem_alloc(&sh.tmem_base, kTmemCols);
+        tc::fence_before_sync();
+    }
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = sh.tmem_base;
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        if (lane == 0) {
+            uint32_t g = 0;
+            for (int u = blockIdx.x; u < total && !abort_set(sh); u += gridDim.x) {
+                const Unit w = unit_of(a, u);
+                const Problem& p = a.p[w.prob];
+                const bool alt = p.alt_flag && *p.alt_flag;
+                const CUtensorMap* mb = alt ? &p.b_alt : &p.b;
+                const int am = p.a_mo + w.mt * kTileM;
+                const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn;
+                const int bk = alt ? p.alt_ko : p.b_ko;
+                const int nbox = (p.bn + 63) / 64;
+                const uint32_t bytes =
+                    kStageA + (uint32_t)(p.b_mn ? nbox * 64 : p.bn) * kTileK * 2u;
+                for (int q = 0; q < a.npairs && !abort_set(sh); ++q) {
+                    const int pa = a.pa[q], pb = a.pb[q];
+                    for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
+                        const int s = g % kStages;
+                        if (!mbar_wait(&sh.empty[s], ((g / kStages) & 1u) ^ 1u)) {
+                            raise_abort(sh, a.status);
+                            break;
+                        }
+                        uint8_t* sa = stages + s * kStageBytes;
+                        uint8_t* sb = sa + kStageA;
+                        uint64_t* bar = &sh.full[s];
+                        mbar_arrive_expect_tx(bar, bytes);
+                        const int ka = p.a_ko + kc * kTileK, kb = bk + kc * kTileK;
+                        if (p.a_mn) {
+                            tma_load_3d(sa, &p.a, am, ka, pa, bar);
+                            tma_load_3d(sa + kTileK * 128, &p.a, am + 64, ka, pa, bar);
+                        } else {
+                            tma_load_3d(sa, &p.a, ka, am, pa, bar);
+                        }
+                        if (p.b_mn) {
+                            for (int i = 0; i < nbox; ++i)
+                                tma_load_3d(sb + i * kTileK * 128, mb, bnc + 64 * i, kb, pb, bar);
+                        } else {
+                            tma_load_3d(sb, mb, kb, bnc, pb, bar);
+                        }
+                    }
+                }
+            }
+            // the MMAs have consumed the last fill of every stage used: no copy
+            // into this CTA is still in flight when it ends
+            for (int s = 0; s < kStages && (uint32_t)s < g; ++s) {
+                const uint32_t last = g - 1 - ((g - 1 - s) % kStages);
+                if (!mbar_wait(&sh.empty[s], (last / kStages) & 1u)) raise_abort(sh, a.status);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        if (lane == 0) {
+            uint32_t g = 0;
+            int it = 0;
+            for (int u = blockIdx.x; u < total && !abort_set(sh); u += gridDim.x, ++it) {
+                const Unit w = unit_of(a, u);
+                const Problem& p = a.p[w.prob];
+                const uint32_t idesc = (a.f16 ? tc::idesc_f16_f32(kTileM, p.bn)
+                                              : tc::idesc_bf16_f32(kTileM, p.bn)) |
+                                       ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16);
+                const int b = it & 1;
+                if (!mbar_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u)) {
+                    raise_abort(sh, a.status);
+                    break;
+                }
+                tc::fence_after_sync();
+                const uint32_t d = tmem + (uint32_t)(b * kTileN);
+                uint32_t acc = 0;
+                const int chunks = a.npairs * (w.k1 - w.k0);
+                for (int kc = 0; kc < chunks; ++kc, ++g) {
+                    const int s = g % kStages;
+                    if (!mbar_wait(&sh.full[s], (g / kStages) & 1u)) {
+                        raise_abort(sh, a.status);
+                        break;
+                    }
+                    tc::fence_after_sync();
+                    const uint32_t sa = smem_u32(stages + s * kStageBytes);
+                    const uint32_t sb = sa + kStageA;
+#pragma unroll
+                    for (int k = 0; k < kTileK / 16; ++k) {
+                        const uint64_t ad = p.a_mn ? smem_desc_sw128_mn(sa + k * 2048)
+                                                   : tc::smem_desc_sw128_kmajor(sa + k * 32);
+                        const uint64_t bd = p.b_mn ? smem_desc_sw128_mn(sb + k * 2048)
+                                                   : tc::smem_desc_sw128_kmajor(sb + k * 32);
+                        tc::mma_bf16(d, ad, bd, idesc, acc);
+                        acc = 1;
+                    }
+                    tc::commit(&sh.empty[s]);
+                }
+                if (abort_set(sh)) break;
+                tc::commit(&sh.tfull[b]);
+            }
+            // TMEM is released after the last unit's MMAs
+            if (it > 0) {
+                const int lb = (it - 1) & 1;
+                if (!mbar_wait(&sh.tfull[lb], (uint32_t)((it - 1) >> 1) & 1u))
+                    raise_abort(sh, a.status);
+            }
+        }
+    } else {
+        // ---------------- epilogue ----------------
+        const int quarter = warp & 3;            // TMEM lanes 32 * quarter ..
+        const int half = (warp - 2) >> 2;        // this warp's chunks of 32 columns
+        const int et = threadIdx.x - 64;
+        const int row_in_tile = quarter * 32 + lane;
+        const Softmax& sm = a.sm;
+        int it = 0;
+        for (int u = blockIdx.x; u < total; u += gridDim.x, ++it) {
+            const Unit w = unit_of(a, u);
+            const Problem& p = a.p[w.prob];
+            const int b = it & 1;
+            const int row = w.mt * kTileM + row_in_tile;
+            const int n0 = w.nt * p.bn;
+            const int ncols = min(p.bn, p.n - n0);      // columns of D in the tile
+            [[maybe_unused]] int64_t y = -1;
+            [[maybe_unused]] GradRow gr;
+            if constexpr (EPI != kOut) {
+                // the tile's biases, and which of its columns are in the softmax
+                const int item = sm.item0 + n0 + et;
+                float bv = 0.0f;
+                if (sm.bias && et < ncols) {
+                    bv = __ldg(sm.bias + item);
+                    // a finite bias stays one in powers of two
+                    if (isfinite(bv)) bv = fminf(fmaxf(bv * kLog2e, -3.402823466e38f), 3.402823466e38f);
+                }
+                if (et >= ncols) bv = -INFINITY;
+                sh.b2[b][et] = bv;
+                const uint32_t mask = __ballot_sync(0xffffffffu, bv == -INFINITY);
+                if (lane == 0) sh.masked[b][et >> 5] = mask;
+                if constexpr (EPI == kStats) {
+                    if (row < sm.rows) y = __ldg(sm.targets + row) - (sm.item0 + n0);
+                } else {
+                    gr = GradRow{0.0f, 0.0f, 0.0f, -1};
+                    if (row < sm.rows) {
+                        const float4 r4 = __ldg(reinterpret_cast<const float4*>(sm.row + row));
+                        gr = GradRow{r4.x, r4.y, r4.z, __float_as_int(r4.w)};
+                    }
+                    y = gr.y < 0 ? -1 : (int64_t)gr.y - (sm.item0 + n0);
+                }
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
+            }
+            if (!mbar_wait(&sh.tfull[b], (uint32_t)(it >> 1) & 1u)) {
+                raise_abort(sh, a.status);
+                break;
+            }
+            tc::fence_after_sync();
+            const uint32_t tcol =
+                tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * kTileN);
+            [[maybe_unused]] float mx = -INFINITY, sum = 0.0f;
+            for (int cc = half; cc * 32 < p.bn; cc += 2) {
+                uint32_t r[32];
+                __syncwarp();
+                // a tile's last chunk may be 16 columns wide; the columns past it are
+                // allocated, and what they hold is not used
+                tc::ld_32x32b_x32(tcol + (uint32_t)(cc * 32), r);
+                tc::wait_ld();
+                if constexpr (EPI == kOut) {
+                    const int valid = min(32, ncols - cc * 32);
+                    float v[32];
+                    if (row >= p.m || valid <= 0) {
+                        // nothing of D here
+                    } else if (p.to_slots) {
+                        float* o = p.slots + w.split * p.slot_stride + (int64_t)row * p.ldslot +
+                                   n0 + cc * 32;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+                        if (p.accumulate) {
+                            if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 31u) == 0) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 8) {
+                                    uint32_t old[8];
+                                    load_32b(o + i, old);
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) v[i + j] += __uint_as_float(old[j]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (i < valid) v[i] += o[i];
+                            }
+                        }
+                        store_row(o, PVS_F32, 0, v, valid);
+                    } else {
+                        const float alpha = p.alpha ? p.alpha0 * __ldg(p.alpha) : p.alpha0;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]) * alpha;
+                        store_row(p.out, p.out_type, (int64_t)row * p.ldout + n0 + cc * 32, v,
+                                  valid);
+                    }
+                } else {
+                    const uint32_t mask = sh.masked[b][cc];
+                    float v[32];
+                    [[maybe_unused]] bool bad = false;
+                    if (sm.bias || mask) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float l =
+                                fmaf(__uint_as_float(r[i]), sm.k2, sh.b2[b][cc * 32 + i]);
+                            const bool out = (mask >> i) & 1u;
+                            v[i] = out ? -INFINITY : l;
+                            // (a masked item's l is -inf unless its product is not finite)
+                            if (EPI == kGrad) bad |= out && !(l == -INFINITY);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]) * sm.k2;
+                    }
+                    const int64_t yr = y - cc * 32;
+                    const bool here = yr >= 0 && yr < 32;
+                    const bool any_here = __any_sync(0xffffffffu, here);
+                    if constexpr (EPI == kStats) {
+                        if (any_here && here) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i == (int)yr) v[i] = -INFINITY;
+                        }
+                        float cm = v[0];
+#pragma unroll
+                        for (int i = 1; i < 32; ++i) cm = fmaxf(cm, v[i]);
+                        const float nm = fmaxf(mx, cm);
+                        const float ref = nm == -INFINITY ? 0.0f : nm;
+                        float part = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) part += ex2(v[i] - ref);
+                        sum = sum * ex2(mx - ref) + part;
+                        mx = nm;
+                    } else {
+                        if (bad && row < sm.rows && sm.bad_masked)
+                            *reinterpret_cast<volatile int*>(sm.bad_masked) = 1;
+                        const bool none = gr.coef == 0.0f && gr.hit == 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            v[i] = none ? 0.0f : ex2(v[i] - gr.m) * gr.coef;
+                        if (any_here && here) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i == (int)yr) v[i] = gr.hit;
+                        }
+                        if (row < sm.rows) {
+                            uint16_t* o = sm.grad + (int64_t)row * sm.ldg + n0 + cc * 32;
+                            for (int part = 0; part < sm.grad_parts; ++part) {
+                                uint32_t h[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    h[i] = part + 1 < sm.grad_parts
+                                               ? cut_bf16(v[2 * i], v[2 * i + 1])
+                                           : sm.grad_f16 ? pack_f16(v[2 * i], v[2 * i + 1])
+                                                         : pack_bf16(v[2 * i], v[2 * i + 1]);
+                                store_32b(o, h);
+                                store_32b(o + 16, h + 8);
+                                o += sm.grad_part;
+                            }
+                        }
+                    }
+                }
+            }
+            if constexpr (EPI == kStats) {
+                if (row < sm.rows)
+                    sm.part[(int64_t)(sm.part0 + w.nt * 2 + half) * sm.rows + row] =
+                        make_float2(mx, sum);
+            }
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.tempty[b]);
+        }
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc::fence_after_sync();
+        tc::tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ---- sums over the splits ------------------------------------------------------
+__global__ void __launch_bounds__(256) sum_slots_kernel(const float* __restrict__ slots, int splits,
+                                                        int64_t slot_stride, int64_t ldslot,
+                                                        int64_t m, int n,
+                                                        const float* __restrict__ alpha,
+                                                        float alpha0, void* out, int64_t ldout,
+                                                        int out_type) {
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= m * n) return;
+    const int64_t row = i / n;
+    const int col = (int)(i - row * n);
+    const float* p = slots + row * ldslot + col;
+    float s = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) s += p[k * slot_stride];
+    s *= alpha ? alpha0 * __ldg(alpha) : alpha0;
+    const int64_t at = row * ldout + col;
+    if (out_type == PVS_F32)
+        static_cast<float*>(out)[at] = s;
+    else if (out_type == PVS_BF16)
+        static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(s);
+    else
+        static_cast<__half*>(out)[at] = __float2half_rn(s);
+}
+
+cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
+                             int64_t m, int n, const float* alpha, float alpha0, void* out,
+                             int64_t ldout, int out_type, cudaStream_t st) {
+    const int64_t blocks = (m * n + 255) / 256;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    count_launches(1);
+    sum_slots_kernel<<<(unsigned)blocks, 256, 0, st>>>(slots, splits, slot_stride, ldslot, m, n,
+                                                       alpha, alpha0, out, ldout, out_type);
+    return cudaGetLastError();
+}
+
+// ---- operands in 16-bit parts ----------------------------------------------------
+__device__ __forceinline__ float load_as_float(const void* p, int dtype, int64_t i) {
+    if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
+    if (dtype == PVS_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+    return __half2float(static_cast<const __half*>(p)[i]);
+}
+
+// Eight consecutive elements per thread.
+__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a) {
+    if (a.only_if && *a.only_if == 0) return;
+    const int64_t per_row = (a.cols + 7) / 8;
+    const int64_t total = a.rows * per_row, stride = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
+        const int64_t row = i / per_row;
+        const int col = (int)(i - row * per_row) * 8;
+        const bool zero = (a.zero_target && a.zero_target[row] == a.ignore_index) ||
+                          (a.zero_bias && a.zero_bias[row] == -INFINITY);
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = !zero && col + k < a.cols ? load_as_float(a.src, a.dtype, row * a.ld + col + k)
+                                             : 0.0f;
+        if (a.row_scale) {
+            const float s = a.row_scale[row];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = col + k < a.cols ? v[k] * s : 0.0f;
+        }
+        for (int part = 0; part < a.parts; ++part) {
+            uint32_t h[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                h[k] = part + 1 < a.parts ? cut_bf16(v[2 * k], v[2 * k + 1])
+                       : a.to_f16         ? pack_f16(v[2 * k], v[2 * k + 1])
+                                          : pack_bf16(v[2 * k], v[2 * k + 1]);
+            *reinterpret_cast<uint4*>(a.dst + part * a.part_stride + row * a.ldd + col) =
+                make_uint4(h[0], h[1], h[2], h[3]);
+        }
+    }
+}
+
+cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
+    const int64_t total = a.rows * ((a.cols + 7) / 8);
+    if (total <= 0) return cudaSuccess;
+    const int64_t blocks = (total + 255) / 256;
+    count_launches(1);
+    split_kernel<<<(unsigned)(blocks < 152 * 16 ? blocks : 152 * 16), 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+// Int8 codes as bf16 (exact).
+__global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restrict__ codes,
+                                                          int64_t ldc, int64_t rows, int cols,
+                                                          uint16_t* __restrict__ dst, int64_t ldd) {
+    const int64_t per_row = (cols + 7) / 8;
+    const int64_t total = rows * per_row, stride = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
+        const int64_t row = i / per_row;
+        const int col = (int)(i - row * per_row) * 8;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = col + k < cols ? (float)codes[row * ldc + col + k] : 0.0f;
+        *reinterpret_cast<uint4*>(dst + row * ldd + col) =
+            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+                       pack_bf16(v[6], v[7]));
+    }
+}
+
+cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, int64_t rows, int cols,
+                               uint16_t* dst, int64_t ldd, cudaStream_t st) {
+    const int64_t total = rows * ((cols + 7) / 8);
+    if (total <= 0) return cudaSuccess;
+    const int64_t blocks = (total + 255) / 256;
+    count_launches(1);
+    split_codes_kernel<<<(unsigned)(blocks < 152 * 16 ? blocks : 152 * 16), 256, 0, st>>>(
+        codes, ldc, rows, cols, dst, ldd);
+    return cudaGetLastError();
+}
+
+// ---- host side ---------------------------------------------------------------------
+bool operand_map(CUtensorMap* m, const Matrix& x, bool mn, int box_rows) {
+    return tensor_map_3d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x.p, (uint64_t)x.parts,
+                         (uint64_t)x.rows, (uint64_t)x.cols, (uint64_t)x.ld,
+                         (uint64_t)(x.parts > 1 ? x.part_stride : x.ld * x.rows), 64,
+                         (uint32_t)(mn ? kTileK : box_rows));
+}
+
+void part_pairs(Args& a, int pa, int pb) {
+    a.npairs = 0;
+    // parts are 2^-8 of one another; what is below the third of a float32's is left
+    // out.  Smallest first: the tensor cores cut each step's sum to 24 bits, so
+    // only the leading pair's steps may cost the sum its last bits
+    for (int level = 2; level >= 0; --level)
+        for (int i = 0; i <= level; ++i)
+            if (i < pa && level - i < pb) {
+                a.pa[a.npairs] = (uint8_t)i;
+                a.pb[a.npairs++] = (uint8_t)(level - i);
+            }
+}
+
+cudaError_t launch_gemm(int epilogue, Args& a, int num_sms, cudaStream_t st) {
+    int64_t total = 0;
+    for (int i = 0; i < a.nprob; ++i) {
+        Problem& p = a.p[i];
+        const int64_t u = (int64_t)p.mtiles * p.ntiles * p.splits;
+        if (p.kchunks < 1 || p.splits < 1 || p.splits > p.kchunks || u < 1 || u > (1 << 30))
+            return cudaErrorInvalidValue;
+        p.units = (int)u;
+        total += u;
+    }
+    const int grid = (int)(total < num_sms ? total : num_sms);
+    const void* fn = epilogue == kStats  ? (const void*)head_gemm_kernel<kStats>
+                     : epilogue == kGrad ? (const void*)head_gemm_kernel<kGrad>
+                                         : (const void*)head_gemm_kernel<kOut>;
+    cudaError_t e = raise_smem_limit(fn, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    count_launches(1);
+    if (epilogue == kStats)
+        head_gemm_kernel<kStats><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
+    else if (epilogue == kGrad)
+        head_gemm_kernel<kGrad><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
+    else
+        head_gemm_kernel<kOut><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
+    return cudaGetLastError();
+}
+
+namespace {
+constexpr int kMaxDevices = 64;
+std::mutex g_device_mutex;
+Device g_devices[kMaxDevices];
+}  // namespace
+
+cudaError_t device(Device* d) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    Device& g = g_devices[dev];
+    if (!g.status) {
+        int sms = 0;
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return e;
+        void* p = nullptr;
+        e = cudaHostAlloc(&p, 256, cudaHostAllocPortable | cudaHostAllocMapped);
+        if (e != cudaSuccess) return e;
+        *static_cast<volatile int*>(p) = 0;
+        g.sms = sms;
+        g.status = static_cast<int*>(p);
+    }
+    *d = g;
+    return cudaSuccess;
+}
+
+int take_status(const Device& d) {
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    volatile int* p = d.status;
+    const int s = *p;
+    if (s != 0) *p = 0;
+    return s;
+}
+
+}  // namespace head
+}  // namespace pvs
+
+extern "C" pvs_status pvs_head_status(void) {
+    pvs::head::Device d;
+    if (pvs::head::device(&d) != cudaSuccess) {
+        cudaGetLastError();
+        return PVS_ERR_CUDA;
+    }
+    return (pvs_status)pvs::head::take_status(d);
+}

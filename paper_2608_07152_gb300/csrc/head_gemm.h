@@ -1,0 +1,183 @@
+// The tensor-core product of the projection head's operators (internal).
+//
+//   D[m, n] = sum_k A[m, k] B[n, k], float32 accumulators in TMEM,
+//
+// over operands of 16-bit elements in either order (K contiguous, or M / N
+// contiguous), each in up to three parts that add up to it: the product then
+// runs over a list of part pairs.  What becomes of D is the kernel's choice:
+//   kStats   softmax statistics of D's rows, tile by tile (forward);
+//   kGrad    the softmax gradient of each entry, kept in 16 bits (backward);
+//   kOut     D itself, split over k where that fills the GPU.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+namespace pvs {
+namespace head {
+
+constexpr int kTileM = 128;
+constexpr int kTileN = 256;     // at most; a product may use fewer columns (bn)
+constexpr int kTileK = 64;      // 128 bytes: one swizzle row
+constexpr int kMaxParts = 3;
+constexpr int kMaxPairs = 6;
+
+enum Epilogue { kStats = 0, kGrad = 1, kOut = 2 };
+
+// An operand in memory: `parts` matrices [rows x cols] of 16-bit elements,
+// leading dimension ld, part_stride elements apart.  Base 16-byte aligned, ld and
+// part_stride multiples of 8.
+struct Matrix {
+    const void* p;
+    int64_t rows, cols, ld;
+    int parts;
+    int64_t part_stride;
+};
+
+struct Problem {
+    CUtensorMap a, b, b_alt;     // b_alt in place of b where *alt_flag is set
+    const int* alt_flag;
+    int a_mn, b_mn;              // 1: M (N) is the contiguous index
+    int m, n;                    // extents of D
+    int bn;                      // columns per tile: a multiple of 16, <= kTileN
+    int mtiles, ntiles, splits;
+    int kchunks;                 // chunks of kTileK for one pair of parts
+    int a_mo, a_ko, b_no, b_ko;  // where D's corner lies in the operands
+    int alt_no, alt_ko;          // the same in b_alt
+    int m_fast;                  // units run over m first (else n first)
+    int units;                   // mtiles * ntiles * splits
+    // kOut: splits > 1 or accumulate: float32 sums slots[split][m][n];
+    // else out = alpha D, rounded once
+    float* slots;
+    int64_t slot_stride, ldslot;
+    int accumulate, to_slots;
+    void* out;
+    int64_t ldout;
+    int out_type;                // pvs_dtype
+    const float* alpha;          // device, null: 1
+    float alpha0;
+};
+
+// A row of the backward pass: G = coef 2^(l - m), and `hit` at item y.
+struct alignas(16) GradRow {
+    float m, coef, hit;
+    int y;                       // -1: none
+};
+
+struct Softmax {
+    float k2;                    // scale log2(e): logits are powers of two
+    const float* bias;           // of the whole vocabulary, or null
+    int64_t items;               // bias entries
+    int item0;                   // the piece's first item
+    int rows;
+    // kStats
+    float2* part;                // [tile column half][rows]
+    int part0;                   // the piece's first tile column half
+    const int64_t* targets;      // a row's own target is left out of its statistics
+    // kGrad
+    const GradRow* row;
+    uint16_t* grad;              // [parts][rows][ldg]
+    int64_t ldg, grad_part;
+    int grad_parts, grad_f16;
+    int* bad_masked;             // set where a masked item's logit is not finite
+};
+
+struct Args {
+    Problem p[2];
+    int nprob;
+    int npairs;
+    uint8_t pa[kMaxPairs], pb[kMaxPairs];
+    int f16;
+    Softmax sm;
+    int* status;
+};
+
+// Tensor map of an operand: boxes of kTileK x rows (K contiguous) or
+// 64 x kTileK (M / N contiguous).
+bool operand_map(CUtensorMap* m, const Matrix& x, bool mn, int box_rows);
+
+// Columns per tile for n columns: the fewest tiles, evenly wide.
+inline int tile_columns(int64_t n) {
+    const int64_t t = (n + kTileN - 1) / kTileN;
+    const int64_t w = (n + t - 1) / t;
+    return (int)((w + 15) / 16 * 16);
+}
+
+// Columns per tile of n logits: whole tiles but for the last (a tile's 16-bit
+// gradient is stored 32 columns at a time, and must not reach into the next).
+inline int logit_columns(int64_t n) { return n >= kTileN ? kTileN : tile_columns(n); }
+
+// The part pairs of a product of operands in `pa` and `pb` parts: those whose
+// product is not below the last kept bit.
+void part_pairs(Args& a, int pa, int pb);
+
+cudaError_t launch_gemm(int epilogue, Args& a, int num_sms, cudaStream_t st);
+
+// out = alpha sum_s slots[s], rounded once.
+cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
+                             int64_t m, int n, const float* alpha, float alpha0, void* out,
+                             int64_t ldout, int out_type, cudaStream_t st);
+
+// src [rows x cols] of `dtype` to `parts` 16-bit matrices [rows x ldd] (f16 where
+// to_f16, else bf16), rows that `zero_target` ignores (or whose zero_bias is
+// -inf) as zeros, every row times row_scale where given.  With only_if, nothing
+// happens unless *only_if is set.
+struct SplitArgs {
+    const void* src;
+    int64_t ld, rows;
+    int cols, dtype;
+    const float* row_scale;
+    const int64_t* zero_target;
+    int64_t ignore_index;
+    const float* zero_bias;
+    const int* only_if;
+    uint16_t* dst;
+    int64_t ldd, part_stride;
+    int parts, to_f16;
+};
+cudaError_t launch_split(const SplitArgs& a, cudaStream_t st);
+cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, int64_t rows, int cols,
+                               uint16_t* dst, int64_t ldd, cudaStream_t st);
+
+// The current device: its SM count and the status word that its kernels set
+// (pinned host memory); status is what an earlier kernel left there.
+struct Device {
+    int sms;
+    int* status;
+};
+cudaError_t device(Device* d);
+int take_status(const Device& d);
+
+// A product's tiles; splits and everything else are the caller's.
+inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k) {
+    p.m = (int)m;
+    p.n = (int)n;
+    p.bn = bn;
+    p.mtiles = (int)((m + kTileM - 1) / kTileM);
+    p.ntiles = (int)((n + bn - 1) / bn);
+    p.kchunks = (int)((k + kTileK - 1) / kTileK);
+    p.splits = 1;
+}
+
+// Scratch of one call, carved from the caller's workspace in 256-byte steps.
+struct Carver {
+    uint8_t* base;
+    size_t used = 0;
+    template <typename T>
+    T* take(int64_t count) {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += ((size_t)count * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+// Rows of any matrix here: coordinates of tiles past the end still fit an int.
+constexpr int64_t kMaxRows = 0x7fff0000;
+inline int element_bytes(int dtype) { return dtype == 2 ? 4 : 2; }
+inline int parts_of(int dtype) { return dtype == 2 ? 3 : 1; }
+
+}  // namespace head
+}  // namespace pvs

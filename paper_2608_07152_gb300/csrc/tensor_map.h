@@ -1,4 +1,4 @@
-// 2-D TMA tensor maps, encoded by the driver on the host.
+// TMA tensor maps, encoded by the driver on the host.
 #pragma once
 
 #include <cstdint>
@@ -11,5 +11,11 @@ namespace pvs {
 // swizzle, elements past the matrix read as zero; false when the driver refuses it.
 bool tensor_map_2d(CUtensorMap* m, CUtensorMapDataType type, int elem, const void* base,
                    uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows);
+
+// The same for `parts` matrices with leading dimension ld, part_stride elements
+// apart, a box within one of them.
+bool tensor_map_3d(CUtensorMap* m, CUtensorMapDataType type, int elem, const void* base,
+                   uint64_t parts, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t part_stride,
+                   uint32_t box_cols, uint32_t box_rows);
 
 }  // namespace pvs

@@ -1,0 +1,552 @@
+// Softmax cross entropy over a large vocabulary and its gradients (head.h), by
+// the product of head_gemm.cu.
+//
+//   forward    l = a x w^T + b, tile by tile; each tile's rows leave a maximum and
+//              a sum of 2^(l - max), which a second launch joins; no logit is kept
+//   backward   for each piece of the vocabulary: the logits again, and from them
+//              G = g (2^(l - m) / s - [j = y]) in 16 bits; then, in one launch,
+//              dx += G w and dw = G^T x
+//
+// Every logit costs 2 d operations in the forward pass and 6 d in the backward
+// pass: bound by the tensor cores unless there are few rows, when w (and dw) bound
+// it.  G of a piece is written once and read twice.
+#include <algorithm>
+#include <cmath>
+#include <limits>
+
+#include <cuda_fp16.h>
+
+#include "../../include/head.h"
+#include "head_gemm.h"
+#include "kernels.h"
+#include "pvs_common.cuh"
+
+namespace pvs {
+namespace head {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
+constexpr size_t kGradBytes = (size_t)256 << 20;    // G of a piece, at most about
+constexpr size_t kPartsBytes = (size_t)256 << 20;   // copies of a piece of w, at most about
+
+__device__ __forceinline__ float element(const void* p, int dtype, int64_t i) {
+    if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
+    const uint16_t u = static_cast<const uint16_t*>(p)[i];
+    return dtype == PVS_BF16 ? __uint_as_float((uint32_t)u << 16) : __half2float(__ushort_as_half(u));
+}
+
+// ---- rows of the forward pass ------------------------------------------------------
+struct JoinArgs {
+    const float2* part;          // [n][rows]: the tiles' (m, s), the target left out
+    int64_t n;
+    pvs_xent_args a;
+    float k2;
+    float* loss;
+    float4* stats;
+};
+
+__device__ __forceinline__ void join(float& m, float& s, float2 p) {
+    const float nm = fmaxf(m, p.x), ref = nm == -INFINITY ? 0.0f : nm;
+    s = s * exp2f(m - ref) + p.y * exp2f(p.x - ref);
+    m = nm;
+}
+
+// A row's statistics from its tiles', joined in a fixed order, and its loss.
+// The target's logit is a float32 product of its own: the tensor cores cut each
+// step's sum, which takes about d / 16 times 2^-25 of a logit, and the target's is
+// the largest and the one that the loss subtracts.  Left out of the tiles' sums, it
+// also leaves 1 - p exact where p is near 1.
+// R rows a block; a warp's lanes run over the rows first (the tiles' statistics
+// are stored by rows).
+template <int R>
+__global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
+    constexpr int kLanes = 256 / R;
+    __shared__ float2 sh[kLanes][R];
+    __shared__ float dots[R];
+    const pvs_xent_args& a = j.a;
+    const int r = threadIdx.x % R, lane = threadIdx.x / R;
+    const int64_t row = (int64_t)blockIdx.x * R + r;
+    float m = -INFINITY, s = 0.0f;
+    if (row < a.rows) {
+#pragma unroll 4
+        for (int64_t i = lane; i < j.n; i += kLanes) join(m, s, j.part[i * a.rows + row]);
+    }
+    sh[lane][r] = make_float2(m, s);
+    for (int i = threadIdx.x >> 5; i < R; i += 8) {
+        const int64_t at = (int64_t)blockIdx.x * R + i;
+        const int64_t y = at < a.rows ? a.targets[at] : -1;
+        float dot = 0.0f;
+        if (y >= 0 && y < a.items)
+            for (int k = threadIdx.x & 31; k < a.dim; k += 32)
+                dot = fmaf(element(a.x, a.dtype, at * a.ldx + k),
+                           element(a.w, a.dtype, y * a.ldw + k), dot);
+        dot = warp_sum(dot);
+        if ((threadIdx.x & 31) == 0) dots[i] = dot;
+    }
+    __syncthreads();
+    for (int w = kLanes / 2; w > 0; w >>= 1) {
+        if (lane < w) {
+            join(m, s, sh[lane + w][r]);
+            sh[lane][r] = make_float2(m, s);
+        }
+        __syncthreads();
+    }
+    if (lane != 0 || row >= a.rows) return;
+    const int64_t y = a.targets[row];
+    const float nan = __int_as_float(0x7fffffff);
+    float loss = 0.0f, hit = 0.0f, t = -INFINITY;
+    const bool target = y >= 0 && y < a.items;
+    if (target) {
+        float b = a.bias ? a.bias[y] : 0.0f;
+        if (b != -INFINITY) {
+            const float b2 = isfinite(b) ? fminf(fmaxf(b * kLog2e, -3.402823466e38f), 3.402823466e38f) : b;
+            t = fmaf(dots[r], j.k2, b2);
+        }
+    }
+    if (y == a.ignore_index) {
+    } else if (!target) {
+        loss = hit = nan;
+    } else if (t == -INFINITY) {
+        // the target is not in the softmax; nothing else is either: no loss
+        loss = m == -INFINITY && s == 0.0f ? 0.0f : INFINITY;
+    } else if (m == -INFINITY && s == 0.0f) {
+        m = t;                                  // the target alone
+        s = 1.0f;
+        if (t != t) loss = hit = nan;
+    } else {
+        const float d = m - t;                  // others against the target
+        if (d < 64.0f) {
+            const float rest = s * exp2f(d);
+            loss = log1pf(rest);
+            hit = -rest / (1.0f + rest);
+            if (isinf(rest)) hit = -1.0f;
+        } else if (t < -1e38f && a.bias) {
+            // a bias near the type's lowest value was cut to stay finite here
+            loss = (float)((double)m * kLn2 - (double)a.bias[y]) + logf(s);
+            hit = -1.0f;
+        } else {
+            loss = fmaf(d, (float)kLn2, logf(s));
+            hit = d != d ? nan : -1.0f;
+        }
+        join(m, s, make_float2(t, 1.0f));
+    }
+    j.loss[row] = loss;
+    j.stats[row] = make_float4(m, s, hit, t);
+}
+
+// ---- rows of the backward pass -----------------------------------------------------
+// The largest finite |grad_loss| (its bits; an order-free maximum).
+__global__ void __launch_bounds__(256) xent_grad_max_kernel(const float* __restrict__ grad,
+                                                            const int64_t* __restrict__ targets,
+                                                            int64_t ignore_index, int64_t rows,
+                                                            unsigned int* top) {
+    float v = 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows;
+         i += (int64_t)gridDim.x * blockDim.x) {
+        const float g = fabsf(grad[i]);
+        if (targets[i] != ignore_index && isfinite(g)) v = fmaxf(v, g);
+    }
+    v = warp_max(v);
+    if ((threadIdx.x & 31) == 0) atomicMax(top, __float_as_uint(v));
+}
+
+// f16 gradients keep G times a power of two that puts the largest |grad_loss|
+// at 2^13 .. 2^14: entries down to 2^-38 of it stay above f16's last bit, which
+// is below what an f16 gradient can hold.  `undo` gets the inverse.
+__global__ void __launch_bounds__(256) xent_rows_kernel(const float4* __restrict__ stats,
+                                                        const float* __restrict__ grad,
+                                                        const int64_t* __restrict__ targets,
+                                                        int64_t items, int64_t ignore_index,
+                                                        int64_t rows,
+                                                        const unsigned int* __restrict__ top,
+                                                        float* undo, GradRow* out) {
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    float up = 1.0f;
+    if (top) {
+        const float t = __uint_as_float(*top);
+        if (t > 0.0f) {
+            const int e = min(max(14 - (ilogbf(t) + 1), -126), 126);
+            up = exp2f((float)e);
+            if (i == 0) *undo = exp2f((float)-e);
+        } else if (i == 0) {
+            *undo = 1.0f;
+        }
+    }
+    if (i >= rows) return;
+    const float4 st = stats[i];
+    const int64_t y = targets[i];
+    GradRow r{0.0f, 0.0f, 0.0f, -1};
+    if (y != ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
+        const float g = grad[i] * up;
+        r.m = st.x;
+        if (y < 0 || y >= items) {
+            r.coef = r.hit = __int_as_float(0x7fffffff);
+        } else {
+            r.coef = g / st.y;
+            r.hit = g * st.z;
+            // (a masked target has no logit, and no gradient of its own)
+            if (st.w != -INFINITY) r.y = (int)y;
+        }
+    }
+    out[i] = r;
+}
+
+// ---- the plan of a call --------------------------------------------------------------
+struct Plan {
+    int parts = 1, f16 = 0;
+    int64_t ldp = 0;            // leading dimension of copied operands
+    bool copy_x = false, copy_w = false;
+    int64_t piece = 0;          // items per piece, a multiple of kTileN (or all)
+    int64_t pieces = 0;
+    int64_t ldg = 0;
+    int bnd = 0;                // columns per tile of the gradients
+    int xsplits = 1, wsplits = 1;
+    // workspace
+    uint16_t *x = nullptr, *w = nullptr, *g = nullptr;
+    float2* part = nullptr;
+    GradRow* row = nullptr;
+    unsigned int* words = nullptr;   // [0] top |grad|, [1] undo, [2] bad masked
+    float *xslots = nullptr, *wslots = nullptr;
+    size_t bytes = 0;
+};
+
+bool aligned(const void* p, int64_t ld, int dtype) {
+    return dtype != PVS_F32 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0;
+}
+
+bool valid(const pvs_xent_args* a) {
+    if (!a || a->rows < 0 || a->rows > kMaxRows || a->items < 1 || a->items > kMaxRows ||
+        a->dim < 1 || a->dim > kMaxDim || a->dtype < PVS_BF16 || a->dtype > PVS_F32 ||
+        a->reserved != 0 || !(a->scale > 0.0f) || !std::isfinite(a->scale) || a->ldx < a->dim ||
+        a->ldw < a->dim)
+        return false;
+    return a->w && (a->rows == 0 || (a->x && a->targets));
+}
+
+// splits of a product's k so that a unit is about `target` chunks long
+int splits_of(int64_t kchunks, int64_t target) {
+    const int64_t s = (kchunks + target - 1) / target;
+    return (int)(s < 1 ? 1 : s > kchunks ? kchunks : s);
+}
+
+Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace) {
+    Plan p;
+    const int64_t T = a.rows, V = a.items;
+    p.parts = parts_of(a.dtype);
+    p.f16 = a.dtype == PVS_F16;
+    p.ldp = round_up(a.dim, 8);
+    p.copy_x = !aligned(a.x, a.ldx, a.dtype);
+    p.copy_w = !aligned(a.w, a.ldw, a.dtype);
+    int64_t piece = round_up(V, kTileN);
+    const bool w_buffer = p.copy_w || (backward && a.bias);
+    if (w_buffer) {
+        const int64_t most = (int64_t)(kPartsBytes / ((size_t)p.parts * p.ldp * 2)) / kTileN * kTileN;
+        piece = std::min(piece, std::max<int64_t>(most, 4 * kTileN));
+    }
+    if (backward) {
+        const int64_t most = (int64_t)(kGradBytes / ((size_t)p.parts * T * 2)) / kTileN * kTileN;
+        piece = std::min(piece, std::max<int64_t>(most, 4 * kTileN));
+    }
+    p.piece = piece;
+    p.pieces = (V + piece - 1) / piece;
+    Carver c{static_cast<uint8_t*>(workspace)};
+    if (p.copy_x || backward) p.x = c.take<uint16_t>((int64_t)p.parts * T * p.ldp);
+    if (w_buffer) p.w = c.take<uint16_t>((int64_t)p.parts * piece * p.ldp);
+    if (!backward) {
+        p.part = c.take<float2>((V + kTileN - 1) / kTileN * 2 * T);
+    } else {
+        p.row = c.take<GradRow>(T);
+        p.words = c.take<unsigned int>(64);
+        p.ldg = piece;
+        p.g = c.take<uint16_t>((int64_t)p.parts * T * p.ldg);
+        p.bnd = tile_columns(a.dim);
+        const int64_t first = std::min(piece, V);
+        const int64_t nt = (a.dim + p.bnd - 1) / p.bnd;
+        const int64_t ux = (T + kTileM - 1) / kTileM * nt, kx = (first + kTileK - 1) / kTileK;
+        const int64_t uw = (first + kTileM - 1) / kTileM * nt, kw = (T + kTileK - 1) / kTileK;
+        // units about a quarter of an SM's share, and not under 16 chunks
+        int64_t target = std::max<int64_t>(16, (ux * kx + uw * kw) / (4 * dev.sms));
+        // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 128
+        // steps at most before the splits are added with rounding
+        if (a.dtype == PVS_F32) target = std::min<int64_t>(target, 32);
+        p.xsplits = splits_of(kx, target);
+        p.wsplits = kw > 2 * target ? splits_of(kw, target) : 1;
+        if (p.xsplits > 1 || p.pieces > 1)
+            p.xslots = c.take<float>((int64_t)p.xsplits * T * p.ldp);
+        if (p.wsplits > 1) p.wslots = c.take<float>((int64_t)p.wsplits * first * p.ldp);
+    }
+    p.bytes = c.used;
+    return p;
+}
+
+// Logits of the piece [v0, v0 + n): x in a.p[0].a, w in .b.
+cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a,
+                   const Matrix& x, const Matrix& w, int64_t v0, int64_t n, const Device& dev,
+                   cudaStream_t st) {
+    Problem& q = g.p[0];
+    q = Problem{};
+    g.nprob = 1;
+    set_tiles(q, a.rows, n, logit_columns(n), a.dim);
+    if (!operand_map(&q.a, x, false, kTileM) || !operand_map(&q.b, w, false, q.bn))
+        return cudaErrorInvalidValue;
+    q.b_no = p.copy_w ? 0 : (int)v0;
+    q.m_fast = 1;
+    g.sm.item0 = (int)v0;
+    part_pairs(g, p.parts, p.parts);
+    return launch_gemm(epilogue, g, dev.sms, st);
+}
+
+SplitArgs split_of(const pvs_xent_args& a, const Plan& p) {
+    SplitArgs s{};
+    s.cols = a.dim;
+    s.dtype = a.dtype;
+    s.ldd = p.ldp;
+    s.parts = p.parts;
+    s.to_f16 = p.f16;
+    s.ignore_index = a.ignore_index;
+    return s;
+}
+
+cudaError_t copy_rows(const pvs_xent_args& a, const Plan& p, bool zero_ignored, cudaStream_t st) {
+    SplitArgs s = split_of(a, p);
+    s.src = a.x;
+    s.ld = a.ldx;
+    s.rows = a.rows;
+    s.dst = p.x;
+    s.part_stride = a.rows * p.ldp;
+    if (zero_ignored) s.zero_target = a.targets;
+    return launch_split(s, st);
+}
+
+cudaError_t copy_items(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_t n,
+                       const int* only_if, cudaStream_t st) {
+    SplitArgs s = split_of(a, p);
+    s.src = static_cast<const uint8_t*>(a.w) + v0 * a.ldw * element_bytes(a.dtype);
+    s.ld = a.ldw;
+    s.rows = n;
+    s.dst = p.w;
+    s.part_stride = p.piece * p.ldp;
+    if (a.bias) s.zero_bias = a.bias + v0;
+    s.only_if = only_if;
+    return launch_split(s, st);
+}
+
+Softmax softmax_of(const pvs_xent_args& a) {
+    Softmax s{};
+    s.k2 = a.scale * kLog2e;
+    s.bias = a.bias;
+    s.items = a.items;
+    s.rows = (int)a.rows;
+    return s;
+}
+
+cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, float* loss,
+                    float* stats, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
+    const int64_t T = a.rows, V = a.items;
+    if (p.copy_x) e = copy_rows(a, p, false, st);
+    const Matrix x = p.copy_x ? Matrix{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp}
+                              : Matrix{a.x, T, a.dim, a.ldx, 1, 0};
+    Args g{};
+    g.status = dev.status;
+    g.f16 = p.f16;
+    g.sm = softmax_of(a);
+    g.sm.part = p.part;
+    g.sm.targets = a.targets;
+    for (int64_t v0 = 0; v0 < V && e == cudaSuccess; v0 += p.piece) {
+        const int64_t n = std::min(p.piece, V - v0);
+        Matrix w{a.w, V, a.dim, a.ldw, 1, 0};
+        if (p.copy_w) {
+            e = copy_items(a, p, v0, n, nullptr, st);
+            if (e != cudaSuccess) break;
+            w = Matrix{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
+        }
+        g.sm.part0 = (int)(v0 / kTileN * 2);
+        e = logits(kStats, g, p, a, x, w, v0, n, dev, st);
+    }
+    if (e != cudaSuccess) return e;
+    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN * 2, a, a.scale * kLog2e, loss,
+                     reinterpret_cast<float4*>(stats)};
+    count_launches(1);
+    if (T >= 32 * dev.sms)
+        xent_join_kernel<32><<<(unsigned)((T + 31) / 32), 256, 0, st>>>(j);
+    else if (T >= 8 * dev.sms)
+        xent_join_kernel<8><<<(unsigned)((T + 7) / 8), 256, 0, st>>>(j);
+    else
+        xent_join_kernel<1><<<(unsigned)T, 256, 0, st>>>(j);
+    return cudaGetLastError();
+}
+
+cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, const float* stats,
+                     const float* grad_loss, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                     cudaStream_t st) {
+    const int64_t T = a.rows, V = a.items;
+    cudaError_t e = cudaMemsetAsync(p.words, 0, 256, st);
+    if (e != cudaSuccess) return e;
+    float* undo = reinterpret_cast<float*>(p.words + 1);
+    int* bad_masked = reinterpret_cast<int*>(p.words + 2);
+    const unsigned blocks = (unsigned)((T + 255) / 256);
+    if (p.f16) {
+        count_launches(1);
+        xent_grad_max_kernel<<<std::min(blocks, (unsigned)dev.sms), 256, 0, st>>>(
+            grad_loss, a.targets, a.ignore_index, T, p.words);
+    }
+    count_launches(1);
+    xent_rows_kernel<<<blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(stats), grad_loss,
+                                             a.targets, V, a.ignore_index, T,
+                                             p.f16 ? p.words : nullptr, undo, p.row);
+    e = cudaGetLastError();
+    // x without the rows that have no gradient: what they hold must not meet G's zeros
+    if (e == cudaSuccess) e = copy_rows(a, p, true, st);
+    const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
+    const float* alpha = p.f16 ? undo : nullptr;
+    for (int64_t v0 = 0, i = 0; v0 < V && e == cudaSuccess; v0 += p.piece, ++i) {
+        const int64_t n = std::min(p.piece, V - v0);
+        const Matrix direct{a.w, V, a.dim, a.ldw, 1, 0};
+        const Matrix copied{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
+        if (p.copy_w) e = copy_items(a, p, v0, n, nullptr, st);
+        if (e != cudaSuccess) break;
+        Args g{};
+        g.status = dev.status;
+        g.f16 = p.f16;
+        g.sm = softmax_of(a);
+        g.sm.row = p.row;
+        g.sm.grad = p.g;
+        g.sm.ldg = p.ldg;
+        g.sm.grad_part = T * p.ldg;
+        g.sm.grad_parts = p.parts;
+        g.sm.grad_f16 = p.f16;
+        const bool alt = !p.copy_w && a.bias;
+        if (alt) g.sm.bad_masked = bad_masked;
+        e = logits(kGrad, g, p, a, x, p.copy_w ? copied : direct, v0, n, dev, st);
+        // a masked item that holds NaN or infinities: dx takes w from a copy with zeros there
+        if (e == cudaSuccess && alt && dx) e = copy_items(a, p, v0, n, bad_masked, st);
+        if (e != cudaSuccess) break;
+        const Matrix gm{p.g, T, n, p.ldg, p.parts, T * p.ldg};
+        g.nprob = 0;
+        if (dx) {
+            Problem& q = g.p[g.nprob++];
+            q = Problem{};
+            set_tiles(q, T, a.dim, p.bnd, n);
+            q.splits = std::min(p.xsplits, q.kchunks);
+            if (!operand_map(&q.a, gm, false, kTileM) ||
+                !operand_map(&q.b, p.copy_w ? copied : direct, true, 0))
+                return cudaErrorInvalidValue;
+            q.b_mn = 1;
+            q.b_ko = p.copy_w ? 0 : (int)v0;
+            if (alt) {
+                if (!operand_map(&q.b_alt, copied, true, 0)) return cudaErrorInvalidValue;
+                q.alt_flag = bad_masked;
+            }
+            q.to_slots = p.xslots != nullptr;
+            q.accumulate = i > 0;
+            q.slots = p.xslots;
+            q.slot_stride = T * p.ldp;
+            q.ldslot = p.ldp;
+            q.out = dx;
+            q.ldout = lddx;
+            q.out_type = a.dtype;
+            q.alpha = alpha;
+            q.alpha0 = a.scale;
+        }
+        Problem* qw = nullptr;
+        if (dw) {
+            Problem& q = g.p[g.nprob++];
+            q = Problem{};
+            set_tiles(q, n, a.dim, p.bnd, T);
+            q.splits = std::min(p.wsplits, q.kchunks);
+            if (!operand_map(&q.a, gm, true, 0) || !operand_map(&q.b, x, true, 0))
+                return cudaErrorInvalidValue;
+            q.a_mn = q.b_mn = 1;
+            q.to_slots = q.splits > 1;
+            q.slots = p.wslots;
+            q.slot_stride = std::min(p.piece, V) * p.ldp;
+            q.ldslot = p.ldp;
+            q.out = static_cast<uint8_t*>(dw) + v0 * lddw * element_bytes(a.dtype);
+            q.ldout = lddw;
+            q.out_type = a.dtype;
+            q.alpha = alpha;
+            q.alpha0 = a.scale;
+            qw = &q;
+        }
+        if (g.nprob == 0) break;
+        part_pairs(g, p.parts, p.parts);
+        e = launch_gemm(kOut, g, dev.sms, st);
+        if (e == cudaSuccess && qw && qw->to_slots)
+            e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.ldp, n, a.dim, alpha,
+                                 a.scale, qw->out, lddw, a.dtype, st);
+    }
+    if (e == cudaSuccess && dx && p.xslots)
+        e = launch_sum_slots(p.xslots, p.xsplits, T * p.ldp, p.ldp, T, a.dim, alpha, a.scale, dx,
+                             lddx, a.dtype, st);
+    return e;
+}
+
+}  // namespace
+}  // namespace head
+}  // namespace pvs
+
+using namespace pvs::head;
+
+extern "C" pvs_status pvs_xent_workspace(const pvs_xent_args* a, int32_t backward, size_t* bytes) {
+    if (!bytes || !valid(a)) return PVS_ERR_INVALID;
+    *bytes = 0;
+    if (a->rows == 0) return PVS_OK;
+    Device dev;
+    if (device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return PVS_ERR_CUDA;
+    }
+    *bytes = plan_of(*a, backward != 0, dev, nullptr).bytes;
+    return PVS_OK;
+}
+
+// The device, an earlier timeout, and the workspace of a call.
+static pvs_status begin(const void* workspace, size_t have, size_t want, const Device& dev) {
+    if (have < want || (want > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))))
+        return PVS_ERR_INVALID;
+    return (pvs_status)take_status(dev);
+}
+
+static pvs_status ended(cudaError_t e) {
+    if (e == cudaSuccess) return PVS_OK;
+    cudaGetLastError();
+    return PVS_ERR_CUDA;
+}
+
+extern "C" pvs_status pvs_xent_forward(const pvs_xent_args* a, float* loss, float* stats,
+                                       void* workspace, size_t workspace_bytes,
+                                       void* cuda_stream) {
+    if (!valid(a)) return PVS_ERR_INVALID;
+    if (a->rows == 0) return PVS_OK;
+    if (!loss || !stats || (reinterpret_cast<uintptr_t>(stats) & 15u)) return PVS_ERR_INVALID;
+    Device dev;
+    if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
+    const Plan p = plan_of(*a, false, dev, workspace);
+    const pvs_status s = begin(workspace, workspace_bytes, p.bytes, dev);
+    if (s != PVS_OK) return s;
+    return ended(forward(*a, p, dev, loss, stats, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+extern "C" pvs_status pvs_xent_backward(const pvs_xent_args* a, const float* stats,
+                                        const float* grad_loss, void* dx, int64_t lddx, void* dw,
+                                        int64_t lddw, void* workspace, size_t workspace_bytes,
+                                        void* cuda_stream) {
+    if (!valid(a) || (dx && lddx < a->dim) || (dw && lddw < a->dim)) return PVS_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (a->rows == 0) {
+        if (!dw) return PVS_OK;
+        const size_t es = (size_t)element_bytes(a->dtype);
+        return ended(cudaMemset2DAsync(dw, (size_t)lddw * es, 0, (size_t)a->dim * es,
+                                       (size_t)a->items, st));
+    }
+    if (!stats || !grad_loss || (reinterpret_cast<uintptr_t>(stats) & 15u)) return PVS_ERR_INVALID;
+    Device dev;
+    if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
+    const Plan p = plan_of(*a, true, dev, workspace);
+    const pvs_status s = begin(workspace, workspace_bytes, p.bytes, dev);
+    if (s != PVS_OK) return s;
+    if (!dx && !dw) return PVS_OK;
+    return ended(backward(*a, p, dev, stats, grad_loss, dx, lddx, dw, lddw, st));
+}
