@@ -61,31 +61,58 @@ def _bind(lib, check) -> None:
         f.argtypes = args
 
 
-def _torch():
-    import torch
-    return torch
+torch = None              # bound by the first call: the package imports without it
+_CODES = {}
+
+
+def _bind_torch() -> None:
+    global torch, _CODES
+    import torch as t
+    _CODES = {t.bfloat16: PVS_BF16, t.float16: PVS_F16, t.float32: PVS_F32}
+    torch = t
+
+
+class _Current:
+    """The device of an operator's tensors made current, where it is not (a few
+    microseconds that a lone GPU's callers need not spend)."""
+
+    def __init__(self, device):
+        self.to = device.index
+        self.back = None
+
+    def __enter__(self):
+        now = torch.cuda.current_device()
+        if now != self.to:
+            self.back = now
+            torch.cuda.set_device(self.to)
+        return torch._C._cuda_getCurrentRawStream(self.to)
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
 
 
 def _dtype_code(dtype) -> int:
-    t = _torch()
-    code = {t.bfloat16: PVS_BF16, t.float16: PVS_F16, t.float32: PVS_F32}.get(dtype)
+    code = _CODES.get(dtype)
     if code is None:
         raise TypeError(f"{dtype} is none of bfloat16, float16 and float32")
     return code
 
 
-def _on_gpu(**tensors):
+def _on_gpu(*tensors):
     """The device that all of them are on (None entries are left out)."""
-    t = _torch()
+    if torch is None:
+        _bind_torch()
     device = None
-    for name, x in tensors.items():
+    for x in tensors:
         if x is None:
             continue
-        if not isinstance(x, t.Tensor) or not x.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor")
-        if device is not None and x.device != device:
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise TypeError("the operators take CUDA tensors")
+        if device is None:
+            device = x.device
+        elif x.device != device:
             raise ValueError("the tensors must be on one device")
-        device = x.device
     return device
 
 
@@ -114,12 +141,7 @@ def _vector(x, name: str, n: int, dtype):
 
 
 def _ptr(x):
-    return ctypes.c_void_p(x.data_ptr()) if x is not None else None
-
-
-def _stream(device):
-    s = _torch().cuda.current_stream(device).cuda_stream
-    return ctypes.c_void_p(s) if s else None
+    return x.data_ptr() if x is not None else None
 
 
 def pvs_head_status() -> int:
@@ -129,8 +151,7 @@ def pvs_head_status() -> int:
 
 
 def _xent_args(x, w, targets, bias, scale, ignore_index):
-    t = _torch()
-    device = _on_gpu(x=x, w=w, targets=targets, bias=bias)
+    device = _on_gpu(x, w, targets, bias)
     x, ldx = _matrix(x, "x")
     w, ldw = _matrix(w, "w", x.dtype)
     if x.shape[1] != w.shape[1]:
@@ -139,9 +160,9 @@ def _xent_args(x, w, targets, bias, scale, ignore_index):
         raise ValueError("w must have a row at least")
     if not (0.0 < scale < float("inf")):
         raise ValueError("scale must be positive and finite")
-    targets = _vector(targets, "targets", x.shape[0], t.int64)
+    targets = _vector(targets, "targets", x.shape[0], torch.int64)
     if bias is not None:
-        bias = _vector(bias, "bias", w.shape[0], t.float32)
+        bias = _vector(bias, "bias", w.shape[0], torch.float32)
     a = pvs_xent_args(x.data_ptr(), w.data_ptr(), targets.data_ptr(),
                       bias.data_ptr() if bias is not None else None, x.shape[0], w.shape[0], ldx,
                       ldw, int(ignore_index), x.shape[1], _dtype_code(x.dtype), float(scale), 0)
@@ -149,7 +170,7 @@ def _xent_args(x, w, targets, bias, scale, ignore_index):
 
 
 def _workspace(n: int, device):
-    return _torch().empty(max(n, 1), dtype=_torch().uint8, device=device)
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
 
 
 def pvs_xent_forward(x, w, targets, bias=None, scale: float = 1.0, ignore_index: int = -100):
@@ -158,16 +179,15 @@ def pvs_xent_forward(x, w, targets, bias=None, scale: float = 1.0, ignore_index:
     bias float32 [V] or None (-inf: the item is not in the softmax).  Returns
     (loss float32 [T], stats float32 [T, 4]); the backward pass takes the stats.
     x and w are both bfloat16, float16 or float32.  No logit is kept."""
-    t = _torch()
     a, device, keep = _xent_args(x, w, targets, bias, scale, ignore_index)
-    with t.cuda.device(device):
-        loss = t.empty(a.rows, dtype=t.float32, device=device)
-        stats = t.empty(a.rows, 4, dtype=t.float32, device=device)
+    with _Current(device) as stream:
+        loss = torch.empty(a.rows, dtype=torch.float32, device=device)
+        stats = torch.empty(a.rows, 4, dtype=torch.float32, device=device)
         n = ctypes.c_size_t()
         _check(_lib.pvs_xent_workspace(ctypes.byref(a), 0, ctypes.byref(n)), "pvs_xent_workspace")
         ws = _workspace(n.value, device)
         _check(_lib.pvs_xent_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(ws), n.value,
-                                     _stream(device)), "pvs_xent_forward")
+                                     stream), "pvs_xent_forward")
     return loss, stats
 
 
@@ -176,80 +196,75 @@ def pvs_xent_backward(x, w, targets, stats, grad_loss, bias=None, scale: float =
     """The gradients (dx, dw) of ``(grad_loss * loss).sum()``, grad_loss float32
     [T], from the forward pass's stats; None for one that is not needed.  The
     logits are computed again, a piece of the items at a time."""
-    t = _torch()
     a, device, keep = _xent_args(x, w, targets, bias, scale, ignore_index)
-    _on_gpu(x=x, stats=stats, grad_loss=grad_loss)
-    if stats.dtype != t.float32 or tuple(stats.shape) != (a.rows, 4):
+    _on_gpu(x, stats, grad_loss)
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (a.rows, 4):
         raise ValueError("stats must be the forward pass's float32 [T, 4]")
     stats = stats.contiguous()
     if stats.data_ptr() % 16:
         stats = stats.clone()
-    grad_loss = _vector(grad_loss, "grad_loss", a.rows, t.float32)
-    with t.cuda.device(device):
-        dx = t.empty(a.rows, a.dim, dtype=x.dtype, device=device) if need_x else None
-        dw = t.empty(a.items, a.dim, dtype=x.dtype, device=device) if need_w else None
+    grad_loss = _vector(grad_loss, "grad_loss", a.rows, torch.float32)
+    with _Current(device) as stream:
+        dx = torch.empty(a.rows, a.dim, dtype=x.dtype, device=device) if need_x else None
+        dw = torch.empty(a.items, a.dim, dtype=x.dtype, device=device) if need_w else None
         n = ctypes.c_size_t()
         _check(_lib.pvs_xent_workspace(ctypes.byref(a), 1, ctypes.byref(n)), "pvs_xent_workspace")
         ws = _workspace(n.value, device)
         _check(_lib.pvs_xent_backward(ctypes.byref(a), _ptr(stats), _ptr(grad_loss), _ptr(dx),
-                                      a.dim, _ptr(dw), a.dim, _ptr(ws), n.value, _stream(device)),
+                                      a.dim, _ptr(dw), a.dim, _ptr(ws), n.value, stream),
                "pvs_xent_backward")
     return dx, dw
 
 
 def _codes(codes, scales):
-    t = _torch()
-    codes, ld = _matrix(codes, "codes", t.int8)
-    return codes, ld, _vector(scales, "scales", codes.shape[0], t.float32)
+    codes, ld = _matrix(codes, "codes", torch.int8)
+    return codes, ld, _vector(scales, "scales", codes.shape[0], torch.float32)
 
 
 def pvs_ckpt_store(x, act: int = PVS_ACT_NONE):
     """Rows of x [R, K] in 8 bits: (codes int8 [R, K], scales float32 [R], y) with
     y = act(x) in x's type, None for PVS_ACT_NONE.  Row r stands for
     ``scales[r] * codes[r]``."""
-    t = _torch()
-    device = _on_gpu(x=x)
+    device = _on_gpu(x)
     x, ldx = _matrix(x, "x")
     dt = _dtype_code(x.dtype)
     rows, cols = x.shape
-    with t.cuda.device(device):
-        codes = t.empty(rows, cols, dtype=t.int8, device=device)
-        scales = t.empty(rows, dtype=t.float32, device=device)
-        y = t.empty(rows, cols, dtype=x.dtype, device=device) if act != PVS_ACT_NONE else None
+    with _Current(device) as stream:
+        codes = torch.empty(rows, cols, dtype=torch.int8, device=device)
+        scales = torch.empty(rows, dtype=torch.float32, device=device)
+        y = torch.empty(rows, cols, dtype=x.dtype, device=device) if act != PVS_ACT_NONE else None
         _check(_lib.pvs_ckpt_store(_ptr(x), ldx, rows, cols, dt, int(act), _ptr(codes), cols,
-                                   _ptr(scales), _ptr(y), cols, _stream(device)),
+                                   _ptr(scales), _ptr(y), cols, stream),
                "pvs_ckpt_store")
     return codes, scales, y
 
 
 def pvs_ckpt_load(codes, scales, dtype):
     """What rows kept by ``pvs_ckpt_store`` stand for, as a tensor of `dtype`."""
-    t = _torch()
-    device = _on_gpu(codes=codes, scales=scales)
+    device = _on_gpu(codes, scales)
     codes, ld, scales = _codes(codes, scales)
     dt = _dtype_code(dtype)
     rows, cols = codes.shape
-    with t.cuda.device(device):
-        out = t.empty(rows, cols, dtype=dtype, device=device)
+    with _Current(device) as stream:
+        out = torch.empty(rows, cols, dtype=dtype, device=device)
         _check(_lib.pvs_ckpt_load(_ptr(codes), ld, _ptr(scales), rows, cols, _ptr(out), cols, dt,
-                                  _stream(device)), "pvs_ckpt_load")
+                                  stream), "pvs_ckpt_load")
     return out
 
 
 def pvs_ckpt_act_backward(dy, codes, scales, act: int = PVS_ACT_GELU):
     """``dy * act'(x)`` for the rows x that the codes stand for, in dy's type."""
-    t = _torch()
-    device = _on_gpu(dy=dy, codes=codes, scales=scales)
+    device = _on_gpu(dy, codes, scales)
     dy, lddy = _matrix(dy, "dy")
     dt = _dtype_code(dy.dtype)
     codes, ld, scales = _codes(codes, scales)
     if dy.shape != codes.shape:
         raise ValueError("dy and codes must have one shape")
     rows, cols = codes.shape
-    with t.cuda.device(device):
-        dx = t.empty(rows, cols, dtype=dy.dtype, device=device)
+    with _Current(device) as stream:
+        dx = torch.empty(rows, cols, dtype=dy.dtype, device=device)
         _check(_lib.pvs_ckpt_act_backward(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows,
-                                          cols, dt, int(act), _ptr(dx), cols, _stream(device)),
+                                          cols, dt, int(act), _ptr(dx), cols, stream),
                "pvs_ckpt_act_backward")
     return dx
 
@@ -257,22 +272,21 @@ def pvs_ckpt_act_backward(dy, codes, scales, act: int = PVS_ACT_GELU):
 def pvs_ckpt_grad_weight(dy, codes, scales):
     """The weight gradient ``dy.T @ x`` [N, K] of a linear layer, dy [R, N], from the
     rows x [R, K] that the codes stand for, in dy's type."""
-    t = _torch()
-    device = _on_gpu(dy=dy, codes=codes, scales=scales)
+    device = _on_gpu(dy, codes, scales)
     dy, lddy = _matrix(dy, "dy")
     dt = _dtype_code(dy.dtype)
     codes, ld, scales = _codes(codes, scales)
     if dy.shape[0] != codes.shape[0]:
         raise ValueError("dy and codes must have as many rows")
     rows, n, k = dy.shape[0], dy.shape[1], codes.shape[1]
-    with t.cuda.device(device):
-        dw = t.empty(n, k, dtype=dy.dtype, device=device)
+    with _Current(device) as stream:
+        dw = torch.empty(n, k, dtype=dy.dtype, device=device)
         size = ctypes.c_size_t()
         _check(_lib.pvs_ckpt_grad_workspace(rows, n, k, dt, ctypes.byref(size)),
                "pvs_ckpt_grad_workspace")
         ws = _workspace(size.value, device)
         _check(_lib.pvs_ckpt_grad_weight(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows, n, k,
-                                         dt, _ptr(dw), k, _ptr(ws), size.value, _stream(device)),
+                                         dt, _ptr(dw), k, _ptr(ws), size.value, stream),
                "pvs_ckpt_grad_weight")
     return dw
 
@@ -282,10 +296,9 @@ def _wq_padded(k: int) -> int:
 
 
 def _wq_weights(codes, scales, group: int):
-    t = _torch()
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
-    if codes.dtype != t.uint8 or scales.dtype != t.bfloat16:
+    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
         raise TypeError("codes must be uint8 and scales bfloat16")
     if codes.dim() != 2 or scales.dim() != 2 or codes.shape[1] % 64 != 0 or codes.shape[1] == 0:
         raise ValueError("codes must be [N, padded K / 2], padded K a multiple of 128")
@@ -304,43 +317,40 @@ def pvs_wq_pack(w, group: int):
     """Weights [N, K] in 4 bits with a bfloat16 scale for every `group` (32, 64 or
     128) of a row: (codes uint8 [N, Kp / 2], scales bfloat16 [N, Kp / group]), Kp
     = K padded to a multiple of 128."""
-    t = _torch()
-    device = _on_gpu(w=w)
+    device = _on_gpu(w)
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
     w, ldw = _matrix(w, "w")
     dt = _dtype_code(w.dtype)
     n, k = w.shape
     kp = _wq_padded(k)
-    with t.cuda.device(device):
-        codes = t.empty(n, kp // 2, dtype=t.uint8, device=device)
-        scales = t.empty(n, kp // group, dtype=t.bfloat16, device=device)
+    with _Current(device) as stream:
+        codes = torch.empty(n, kp // 2, dtype=torch.uint8, device=device)
+        scales = torch.empty(n, kp // group, dtype=torch.bfloat16, device=device)
         _check(_lib.pvs_wq_pack(_ptr(w), ldw, n, k, dt, int(group), _ptr(codes), _ptr(scales),
-                                _stream(device)), "pvs_wq_pack")
+                                stream), "pvs_wq_pack")
     return codes, scales
 
 
 def pvs_wq_unpack(codes, scales, group: int, cols: int, dtype):
     """The weights [N, cols] that packed ones stand for, as a tensor of `dtype`."""
-    t = _torch()
-    device = _on_gpu(codes=codes, scales=scales)
+    device = _on_gpu(codes, scales)
     codes, scales, kp = _wq_weights(codes, scales, group)
     dt = _dtype_code(dtype)
     if cols < 1 or _wq_padded(cols) != kp:
         raise ValueError(f"cols = {cols} does not pad to {kp}")
     n = codes.shape[0]
-    with t.cuda.device(device):
-        out = t.empty(n, cols, dtype=dtype, device=device)
+    with _Current(device) as stream:
+        out = torch.empty(n, cols, dtype=dtype, device=device)
         _check(_lib.pvs_wq_unpack(_ptr(codes), _ptr(scales), n, cols, int(group), _ptr(out), cols,
-                                  dt, _stream(device)), "pvs_wq_unpack")
+                                  dt, stream), "pvs_wq_unpack")
     return out
 
 
 def pvs_wq_matvec(x, codes, scales, group: int):
     """``x @ weights.T`` [B, N] in x's type, for a few rows x [B, K] (B <= 64) and
     packed weights."""
-    t = _torch()
-    device = _on_gpu(x=x, codes=codes, scales=scales)
+    device = _on_gpu(x, codes, scales)
     codes, scales, kp = _wq_weights(codes, scales, group)
     x, ldx = _matrix(x, "x")
     dt = _dtype_code(x.dtype)
@@ -350,8 +360,8 @@ def pvs_wq_matvec(x, codes, scales, group: int):
     if _wq_padded(k) != kp:
         raise ValueError(f"x has {k} columns, the packed weights {kp} after padding")
     n = codes.shape[0]
-    with t.cuda.device(device):
-        y = t.empty(b, n, dtype=x.dtype, device=device)
+    with _Current(device) as stream:
+        y = torch.empty(b, n, dtype=x.dtype, device=device)
         _check(_lib.pvs_wq_matvec(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), n, k, int(group), dt,
-                                  _ptr(y), n, _stream(device)), "pvs_wq_matvec")
+                                  _ptr(y), n, stream), "pvs_wq_matvec")
     return y
