@@ -20,93 +20,265 @@ namespace {
 
 template <int TYPE> struct Element;
 template <> struct Element<PVS_BF16> {
-    using T = __nv_bfloat16;
-    static __device__ float to(T x) { return __bfloat162float(x); }
-    static __device__ T from(float x) { return __float2bfloat16_rn(x); }
+    using T = uint16_t;
+    static __device__ __forceinline__ float to(uint32_t x) { return __uint_as_float(x << 16); }
+    static __device__ __forceinline__ uint32_t from(float x) {
+        return __bfloat16_as_ushort(__float2bfloat16_rn(x));
+    }
 };
 template <> struct Element<PVS_F16> {
-    using T = __half;
-    static __device__ float to(T x) { return __half2float(x); }
-    static __device__ T from(float x) { return __float2half_rn(x); }
+    using T = uint16_t;
+    static __device__ __forceinline__ float to(uint32_t x) {
+        return __half2float(__ushort_as_half((uint16_t)x));
+    }
+    static __device__ __forceinline__ uint32_t from(float x) {
+        return __half_as_ushort(__float2half_rn(x));
+    }
 };
 template <> struct Element<PVS_F32> {
-    using T = float;
-    static __device__ float to(T x) { return x; }
-    static __device__ T from(float x) { return x; }
+    using T = uint32_t;
+    static __device__ __forceinline__ float to(uint32_t x) { return __uint_as_float(x); }
+    static __device__ __forceinline__ uint32_t from(float x) { return __float_as_uint(x); }
 };
 
-__device__ __forceinline__ float gelu(float x) {
-    return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+// N consecutive elements (8, aligned to their size, or 1) as raw words.
+template <int TYPE, int N>
+__device__ __forceinline__ void load_elements(const void* p, int64_t at, float (&v)[N]) {
+    using E = Element<TYPE>;
+    if constexpr (N == 1) {
+        v[0] = E::to(__ldg(static_cast<const typename E::T*>(p) + at));
+    } else if constexpr (TYPE == PVS_F32) {
+        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+        const float4 a = __ldg(q), b = __ldg(q + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+        v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = E::to((w[i >> 1] >> (16 * (i & 1))) & 0xffffu);
+    }
 }
-__device__ __forceinline__ float gelu_slope(float x) {
-    return 0.5f * (1.0f + erff(x * 0.70710678118654752f)) +
-           x * __expf(-0.5f * x * x) * 0.39894228040143268f;
+template <int TYPE, int N>
+__device__ __forceinline__ void store_elements(void* p, int64_t at, const float (&v)[N]) {
+    using E = Element<TYPE>;
+    if constexpr (N == 1) {
+        static_cast<typename E::T*>(p)[at] = (typename E::T)E::from(v[0]);
+    } else if constexpr (TYPE == PVS_F32) {
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+        q[0] = make_float4(v[0], v[1], v[2], v[3]);
+        q[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = E::from(v[2 * i]) | (E::from(v[2 * i + 1]) << 16);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <int N>
+__device__ __forceinline__ void load_codes(const int8_t* p, int64_t at, float (&v)[N]) {
+    if constexpr (N == 1) {
+        v[0] = (float)__ldg(p + at);
+    } else {
+        const uint2 a = __ldg(reinterpret_cast<const uint2*>(p + at));
+        const uint32_t w[2] = {a.x, a.y};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
 }
 
-// A warp per row, which it reads twice (the second time from L1 or L2).
-template <int TYPE>
-__global__ void __launch_bounds__(256) ckpt_store_kernel(const void* x, int64_t ldx, int64_t rows,
-                                                         int cols, int act, int8_t* codes,
-                                                         int64_t ldc, float* scales, void* y,
-                                                         int64_t ldy) {
-    using E = Element<TYPE>;
-    const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const typename E::T* v = static_cast<const typename E::T*>(x) + row * ldx;
-    float top = 0.0f;
-    bool finite = true;
-    for (int j = lane; j < cols; j += 32) {
-        const float f = E::to(v[j]);
-        finite &= isfinite(f);
-        top = fmaxf(top, fabsf(f));
+// 1 - erf(z) for z >= 0 as a polynomial in t = 1 / (1 + p z) times 2^(-z^2 log2 e)
+// (Abramowitz and Stegun 7.1.26, Hastings 1955: off by at most 1.5e-7; erff takes
+// about three times the instructions, and made the store bound by them).
+// `e` gets exp(-z^2).
+__device__ __forceinline__ float erfc_positive(float z, float& e) {
+    const float t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
+    e = exp2f(z * z * -1.4426950408889634f);
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    return p * t * e;
+}
+// x Phi(x): for x < 0 the tail itself, without a difference from 1.
+__device__ __forceinline__ float gelu(float x) {
+    float e;
+    const float h = 0.5f * erfc_positive(fabsf(x) * 0.70710678118654752f, e);
+    return x * (x < 0.0f ? h : 1.0f - h);
+}
+__device__ __forceinline__ float gelu_slope(float x) {
+    float e;
+    const float h = 0.5f * erfc_positive(fabsf(x) * 0.70710678118654752f, e);
+    const float tail = x * e * 0.39894228040143268f;
+    return (x < 0.0f ? h : 1.0f - h) + (e == 0.0f ? 0.0f : tail);
+}
+
+// TPR threads per row hold it in registers: read once, the maximum, the codes, the
+// activation.  N elements (8 where rows are aligned, else 1) make a piece; a
+// thread holds NV pieces of 8 elements' worth.
+template <int TYPE, int N, int NV, int TPR>
+__global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict__ x, int64_t ldx,
+                                                         int64_t rows, int cols, int act,
+                                                         int8_t* __restrict__ codes, int64_t ldc,
+                                                         float* __restrict__ scales,
+                                                         void* __restrict__ y, int64_t ldy) {
+    constexpr int kPieces = NV * 8 / N;
+    constexpr int kRows = 256 / TPR;
+    const int lane = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    const bool live = row < rows;
+    const int pieces = (cols + N - 1) / N;      // cols is a multiple of N
+    float v[kPieces][N];
+    float top = 0.0f, nan = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int j = i * TPR + lane;
+        if (live && j < pieces) {
+            load_elements<TYPE, N>(x, row * ldx + (int64_t)j * N, v[i]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[i][k] = 0.0f;
+        }
     }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            top = fmaxf(top, fabsf(v[i][k]));
+            nan += v[i][k] * 0.0f;              // NaN for a NaN or an infinity
+        }
+    if (nan != 0.0f) top = INFINITY;            // (NaN != 0)
     top = warp_max(top);
-    finite = __all_sync(0xffffffffu, finite);
+    if constexpr (TPR > 32) {
+        __shared__ float tops[TPR / 32];
+        if (lane % 32 == 0) tops[lane / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TPR / 32; ++i) top = fmaxf(top, tops[i]);
+    }
+    if (!live) return;
+    const bool finite = top != INFINITY;
     float s = top == 0.0f ? 1.0f : __fmul_rn(top, 1.0f / 127.0f);
     if (s == 0.0f) s = __uint_as_float(1u);
     const float r = __fdiv_rn(1.0f, s);
+    const bool fast = s >= kFastScaleMin;
     if (lane == 0) scales[row] = finite ? s : __int_as_float(0x7fffffff);
-    for (int j = lane; j < cols; j += 32) {
-        const float f = E::to(v[j]);
-        uint32_t c = 0;
-        if (finite) {
-            if (s >= kFastScaleMin)
-                code_of(f, s, r, c);
-            else
-                c = (uint32_t)(int)fminf(fmaxf(roundf(__fdiv_rn(f, s)), -127.0f), 127.0f);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int j = i * TPR + lane;
+        if (j >= pieces) break;
+        uint32_t c[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            c[k] = 0;
+            if (finite) {
+                if (fast)
+                    code_of(v[i][k], s, r, c[k]);
+                else
+                    c[k] = (uint32_t)(int)fminf(fmaxf(roundf(__fdiv_rn(v[i][k], s)), -127.0f), 127.0f);
+            }
         }
-        codes[row * ldc + j] = (int8_t)c;
-        if (act == PVS_ACT_GELU) static_cast<typename E::T*>(y)[row * ldy + j] = E::from(gelu(f));
+        int8_t* out = codes + row * ldc + (int64_t)j * N;
+        if constexpr (N == 1) {
+            *out = (int8_t)c[0];
+        } else {
+            uint32_t w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                w[h] = __byte_perm(__byte_perm(c[4 * h], c[4 * h + 1], 0x0040),
+                                   __byte_perm(c[4 * h + 2], c[4 * h + 3], 0x0040), 0x5410);
+            *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+        }
+        if (act == PVS_ACT_GELU) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[i][k] = gelu(v[i][k]);
+            store_elements<TYPE, N>(y, row * ldy + (int64_t)j * N, v[i]);
+        }
     }
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(256) ckpt_load_kernel(const int8_t* codes, int64_t ldc,
-                                                        const float* scales, int64_t rows,
-                                                        int cols, void* out, int64_t ldo) {
-    using E = Element<TYPE>;
-    const int64_t total = rows * cols, stride = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
-        const int64_t row = i / cols, j = i - row * cols;
-        static_cast<typename E::T*>(out)[row * ldo + j] =
-            E::from(scales[row] * (float)codes[row * ldc + j]);
+// What the codes stand for (DY: times dy act').  A block takes `per_block` rows;
+// a thread's pieces of N elements run over them.  n / pieces by a product:
+// m = floor(2^40 / pieces) + 1 is exact for n < 2^23 and pieces < 2^16.
+template <int TYPE, int N, bool DY>
+__global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__ dy, int64_t lddy,
+                                                        const int8_t* __restrict__ codes,
+                                                        int64_t ldc,
+                                                        const float* __restrict__ scales,
+                                                        int64_t rows, int cols, int per_block,
+                                                        uint64_t m, void* __restrict__ out,
+                                                        int64_t ldo) {
+    const int pieces = cols / N;
+    const int64_t row0 = (int64_t)blockIdx.x * per_block;
+    const int here = (int)min((int64_t)per_block, rows - row0);
+    const uint32_t total = (uint32_t)(here * pieces);
+    constexpr int kAhead = N == 1 ? 8 : 2;
+    for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 256 * kAhead) {
+        float z[kAhead][N], g[kAhead][N], s[kAhead];
+        int64_t row[kAhead];
+        int col[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const uint32_t i = i0 + a * 256;
+            if (i >= total) continue;
+            const uint32_t r = (uint32_t)((i * m) >> 40);
+            row[a] = row0 + r;
+            col[a] = (int)(i - r * (uint32_t)pieces) * N;
+            load_codes<N>(codes, row[a] * ldc + col[a], z[a]);
+            if constexpr (DY) load_elements<TYPE, N>(dy, row[a] * lddy + col[a], g[a]);
+            s[a] = __ldg(scales + row[a]);
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (i0 + a * 256 >= total) continue;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                z[a][k] *= s[a];
+                if constexpr (DY) z[a][k] = g[a][k] * gelu_slope(z[a][k]);
+            }
+            store_elements<TYPE, N>(out, row[a] * ldo + col[a], z[a]);
+        }
     }
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(256) ckpt_act_kernel(const void* dy, int64_t lddy,
-                                                       const int8_t* codes, int64_t ldc,
-                                                       const float* scales, int64_t rows, int cols,
-                                                       void* dx, int64_t lddx) {
-    using E = Element<TYPE>;
-    const int64_t total = rows * cols, stride = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
-        const int64_t row = i / cols, j = i - row * cols;
-        const float g = E::to(static_cast<const typename E::T*>(dy)[row * lddy + j]);
-        static_cast<typename E::T*>(dx)[row * lddx + j] =
-            E::from(g * gelu_slope(scales[row] * (float)codes[row * ldc + j]));
-    }
+// Whether rows of `elem`-byte elements can be read and written eight at a time.
+bool by_eight(const void* p, int64_t ld, int elem) {
+    return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(std::min(8 * elem, 16) - 1)) == 0 && ld % 8 == 0;
+}
+
+template <int TYPE, int N, int NV, int TPR>
+void store_launch(const void* x, int64_t ldx, int64_t rows, int cols, int act, int8_t* codes,
+                  int64_t ldc, float* scales, void* y, int64_t ldy, cudaStream_t st) {
+    constexpr int kRows = 256 / TPR;
+    ckpt_store_kernel<TYPE, N, NV, TPR><<<(unsigned)((rows + kRows - 1) / kRows), 256, 0, st>>>(
+        x, ldx, rows, cols, act, codes, ldc, scales, y, ldy);
+}
+
+// The narrowest layout that holds a row: a warp up to 2048 elements, else a block.
+template <int TYPE, int N, typename... A>
+void store_rows(int cols, A... a) {
+    const int nv = (cols + 255) / 256;
+    if (nv <= 1) store_launch<TYPE, N, 1, 32>(a...);
+    else if (nv <= 2) store_launch<TYPE, N, 2, 32>(a...);
+    else if (nv <= 3) store_launch<TYPE, N, 3, 32>(a...);
+    else if (nv <= 4) store_launch<TYPE, N, 4, 32>(a...);
+    else if (nv <= 6) store_launch<TYPE, N, 6, 32>(a...);
+    else if (nv <= 8) store_launch<TYPE, N, 8, 32>(a...);
+    else if (nv <= 16) store_launch<TYPE, N, 2, 256>(a...);
+    else if (nv <= 32) store_launch<TYPE, N, 4, 256>(a...);
+    else store_launch<TYPE, N, 16, 256>(a...);
+}
+
+template <int TYPE, int N, bool DY>
+void load_launch(const void* dy, int64_t lddy, const int8_t* codes, int64_t ldc,
+                 const float* scales, int64_t rows, int cols, void* out, int64_t ldo,
+                 cudaStream_t st) {
+    const int pieces = cols / N;
+    // about 4096 elements a block; under 2^23 pieces in any case
+    const int per_block = std::max(1, 4096 / cols);
+    ckpt_load_kernel<TYPE, N, DY>
+        <<<(unsigned)((rows + per_block - 1) / per_block), 256, 0, st>>>(
+            dy, lddy, codes, ldc, scales, rows, cols, per_block, (1ull << 40) / pieces + 1, out, ldo);
 }
 
 bool rows_ok(int64_t rows, int32_t cols, int32_t dtype) {
@@ -119,10 +291,6 @@ pvs_status queued(cudaError_t e = cudaSuccess) {
     if (e == cudaSuccess) return PVS_OK;
     cudaGetLastError();
     return PVS_ERR_CUDA;
-}
-
-unsigned grid_for(int64_t total) {
-    return (unsigned)std::min<int64_t>((total + 255) / 256, 152 * 32);
 }
 
 struct GradPlan {
@@ -188,8 +356,15 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
     if (!x || !codes || !scales || (act != PVS_ACT_NONE && !y)) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
-    PVS_BY_TYPE(dtype, (ckpt_store_kernel<TYPE><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(
-                           x, ldx, rows, cols, act, codes, ldcodes, scales, y, ldy)));
+    const int es = element_bytes(dtype);
+    const bool eight = cols % 8 == 0 && by_eight(x, ldx, es) && by_eight(codes, ldcodes, 1) &&
+                       (act == PVS_ACT_NONE || by_eight(y, ldy, es));
+    if (eight)
+        PVS_BY_TYPE(dtype, (store_rows<TYPE, 8>(cols, x, ldx, rows, cols, act, codes, ldcodes,
+                                                scales, y, ldy, st)));
+    else
+        PVS_BY_TYPE(dtype, (store_rows<TYPE, 1>(cols, x, ldx, rows, cols, act, codes, ldcodes,
+                                                scales, y, ldy, st)));
     return queued();
 }
 
@@ -201,8 +376,12 @@ extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const 
     if (!codes || !scales || !out) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
-    PVS_BY_TYPE(dtype, (ckpt_load_kernel<TYPE><<<grid_for(rows * cols), 256, 0, st>>>(
-                           codes, ldcodes, scales, rows, cols, out, ldout)));
+    if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(out, ldout, element_bytes(dtype)))
+        PVS_BY_TYPE(dtype, (load_launch<TYPE, 8, false>(nullptr, 0, codes, ldcodes, scales, rows,
+                                                        cols, out, ldout, st)));
+    else
+        PVS_BY_TYPE(dtype, (load_launch<TYPE, 1, false>(nullptr, 0, codes, ldcodes, scales, rows,
+                                                        cols, out, ldout, st)));
     return queued();
 }
 
@@ -217,8 +396,14 @@ extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const 
     if (!dy || !codes || !scales || !dx) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
-    PVS_BY_TYPE(dtype, (ckpt_act_kernel<TYPE><<<grid_for(rows * cols), 256, 0, st>>>(
-                           dy, lddy, codes, ldcodes, scales, rows, cols, dx, lddx)));
+    const int es = element_bytes(dtype);
+    if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(dy, lddy, es) &&
+        by_eight(dx, lddx, es))
+        PVS_BY_TYPE(dtype, (load_launch<TYPE, 8, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
+                                                       dx, lddx, st)));
+    else
+        PVS_BY_TYPE(dtype, (load_launch<TYPE, 1, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
+                                                       dx, lddx, st)));
     return queued();
 }
 
