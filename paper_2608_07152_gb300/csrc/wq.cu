@@ -87,8 +87,37 @@ struct WqArgs {
     int chunk;               // blocks whose x fragments are in shared memory at once
 };
 
-// NT: 8 columns (parts of rows of x) each; GROUP: weights per scale.
-template <int NT, int GROUP>
+// 32 codes of each of two rows, and their scales, as they come from memory.
+template <int GROUP>
+struct RowPair {
+    uint4 w0, w1;
+    uint2 s0, s1;            // 128 / GROUP bf16 scales each
+
+    __device__ __forceinline__ void load(const uint8_t* c0, const uint8_t* c1, const uint16_t* f0,
+                                         const uint16_t* f1, int blk) {
+        w0 = __ldg(reinterpret_cast<const uint4*>(c0 + (int64_t)blk * 64));
+        w1 = __ldg(reinterpret_cast<const uint4*>(c1 + (int64_t)blk * 64));
+        if constexpr (GROUP == 32) {
+            s0 = __ldg(reinterpret_cast<const uint2*>(f0) + blk);
+            s1 = __ldg(reinterpret_cast<const uint2*>(f1) + blk);
+        } else if constexpr (GROUP == 64) {
+            s0.x = __ldg(reinterpret_cast<const uint32_t*>(f0) + blk);
+            s1.x = __ldg(reinterpret_cast<const uint32_t*>(f1) + blk);
+        } else {
+            s0.x = __ldg(f0 + blk);
+            s1.x = __ldg(f1 + blk);
+        }
+    }
+    static __device__ __forceinline__ float scale(uint2 s, int group) {
+        const uint32_t w = group < 2 ? s.x : s.y;
+        return __uint_as_float(group & 1 ? w & 0xffff0000u : w << 16);
+    }
+};
+
+// NT: 8 columns (parts of rows of x) each; GROUP: weights per scale; RT: tiles of 16
+// rows a warp takes at once, which share the x fragments it reads.
+// A warp's next block is loaded before it works on the present one.
+template <int NT, int GROUP, int RT>
 __global__ void __launch_bounds__(kWqThreads) wq_matvec_kernel(const WqArgs a) {
     extern __shared__ uint4 xf[];                     // [block][word][NT][lane]
     __shared__ float out[kWqWarps][16][NT * 8 + 1];
@@ -96,19 +125,35 @@ __global__ void __launch_bounds__(kWqThreads) wq_matvec_kernel(const WqArgs a) {
     const int g = lane >> 2, t = lane & 3;
     const int team = warp / a.kw, share = warp % a.kw;
     const int teams = kWqWarps / a.kw;
-    constexpr int kScales = 128 / GROUP;              // a block
-    const int64_t code_row = (int64_t)a.blocks * 64, scale_row = (int64_t)a.blocks * kScales;
-    const int64_t tiles = (a.rows + 15) / 16;
+    const int64_t code_row = (int64_t)a.blocks * 64;
+    const int64_t scale_row = (int64_t)a.blocks * (128 / GROUP);
+    const int64_t tiles = (a.rows + 16 * RT - 1) / (16 * RT);
     const bool reload = a.chunk < a.blocks;
     bool loaded = false;
     for (int64_t t0 = (int64_t)blockIdx.x * teams; t0 < tiles; t0 += (int64_t)gridDim.x * teams) {
         const int64_t tile = t0 + team;
-        const int64_t r0 = min(tile * 16 + g, a.rows - 1), r1 = min(tile * 16 + g + 8, a.rows - 1);
-        float acc[NT][4] = {};
+        const uint8_t* code[RT][2];
+        const uint16_t* scale[RT][2];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t row = min((tile * RT + r) * 16 + g + 8 * h, a.rows - 1);
+                code[r][h] = a.codes + row * code_row + t * 16;
+                scale[r][h] = a.scales + row * scale_row;
+            }
+        float acc[RT][NT][4] = {};
         for (int c0 = 0; c0 < a.blocks; c0 += a.chunk) {
             const int c1 = min(c0 + a.chunk, a.blocks);
+            RowPair<GROUP> next[RT];
+            const bool mine = tile < tiles && c0 + share < c1;
+            if (mine) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    next[r].load(code[r][0], code[r][1], scale[r][0], scale[r][1], c0 + share);
+            }
             if (reload || !loaded) {
-                __syncthreads();
+                if (reload) __syncthreads();
                 for (int i = threadIdx.x; i < (c1 - c0) * 4 * NT * 32; i += kWqThreads) {
                     const int l = i & 31, nt = (i >> 5) % NT, word = (i / (32 * NT)) & 3;
                     const int blk = c0 + i / (128 * NT);
@@ -126,166 +171,238 @@ __global__ void __launch_bounds__(kWqThreads) wq_matvec_kernel(const WqArgs a) {
                 __syncthreads();
                 loaded = true;
             }
-            if (tile < tiles) {
-                for (int blk = c0 + share; blk < c1; blk += a.kw) {
-                    const uint4 w0 = __ldg(reinterpret_cast<const uint4*>(
-                        a.codes + r0 * code_row + (int64_t)blk * 64 + t * 16));
-                    const uint4 w1 = __ldg(reinterpret_cast<const uint4*>(
-                        a.codes + r1 * code_row + (int64_t)blk * 64 + t * 16));
-                    const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w};
-                    const uint32_t a1[4] = {w1.x, w1.y, w1.z, w1.w};
-                    float s0[kScales], s1[kScales];
+            if (!mine) continue;
+            for (int blk = c0 + share; blk < c1; blk += a.kw) {
+                RowPair<GROUP> now[RT];
 #pragma unroll
-                    for (int i = 0; i < kScales; ++i) {
-                        s0[i] = __uint_as_float(
-                            (uint32_t)__ldg(a.scales + r0 * scale_row + blk * kScales + i) << 16);
-                        s1[i] = __uint_as_float(
-                            (uint32_t)__ldg(a.scales + r1 * scale_row + blk * kScales + i) << 16);
-                    }
-                    const uint4* xb = xf + (blk - c0) * 4 * NT * 32 + lane;
-                    float part[NT][4];
+                for (int r = 0; r < RT; ++r) now[r] = next[r];
+                const int after = min(blk + a.kw, c1 - 1);   // (past the end: read again, unused)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                for (int r = 0; r < RT; ++r)
+                    next[r].load(code[r][0], code[r][1], scale[r][0], scale[r][1], after);
+                const uint4* xb = xf + (blk - c0) * 4 * NT * 32 + lane;
+                float part[RT][NT][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint4 x[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) x[n] = xb[(i * NT + n) * 32];
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const uint32_t w0 = i == 0   ? now[r].w0.x
+                                            : i == 1 ? now[r].w0.y
+                                            : i == 2 ? now[r].w0.z
+                                                     : now[r].w0.w;
+                        const uint32_t w1 = i == 0   ? now[r].w1.x
+                                            : i == 1 ? now[r].w1.y
+                                            : i == 2 ? now[r].w1.z
+                                                     : now[r].w1.w;
                         if (i % (GROUP / 32) == 0) {
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
-                                part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+                                part[r][n][0] = part[r][n][1] = part[r][n][2] = part[r][n][3] = 0.0f;
                         }
                         uint32_t p0[4], p1[4];
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
-                            p0[m] = code_pair(a0[i], m);
-                            p1[m] = code_pair(a1[i], m);
+                            p0[m] = code_pair(w0, m);
+                            p1[m] = code_pair(w1, m);
                         }
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint4 x = xb[(i * NT + n) * 32];
-                            mma_16816(part[n], p0[0], p1[0], p0[1], p1[1], x.x, x.y);
-                            mma_16816(part[n], p0[2], p1[2], p0[3], p1[3], x.z, x.w);
+                            mma_16816(part[r][n], p0[0], p1[0], p0[1], p1[1], x[n].x, x[n].y);
+                            mma_16816(part[r][n], p0[2], p1[2], p0[3], p1[3], x[n].z, x[n].w);
                         }
                         if (i % (GROUP / 32) == GROUP / 32 - 1) {
-                            const float f0 = s0[i / (GROUP / 32)], f1 = s1[i / (GROUP / 32)];
+                            const float f0 = RowPair<GROUP>::scale(now[r].s0, i / (GROUP / 32));
+                            const float f1 = RowPair<GROUP>::scale(now[r].s1, i / (GROUP / 32));
 #pragma unroll
                             for (int n = 0; n < NT; ++n) {
-                                acc[n][0] = fmaf(f0, part[n][0], acc[n][0]);
-                                acc[n][1] = fmaf(f0, part[n][1], acc[n][1]);
-                                acc[n][2] = fmaf(f1, part[n][2], acc[n][2]);
-                                acc[n][3] = fmaf(f1, part[n][3], acc[n][3]);
+                                acc[r][n][0] = fmaf(f0, part[r][n][0], acc[r][n][0]);
+                                acc[r][n][1] = fmaf(f0, part[r][n][1], acc[r][n][1]);
+                                acc[r][n][2] = fmaf(f1, part[r][n][2], acc[r][n][2]);
+                                acc[r][n][3] = fmaf(f1, part[r][n][3], acc[r][n][3]);
                             }
                         }
                     }
                 }
             }
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            out[warp][g][n * 8 + 2 * t] = acc[n][0];
-            out[warp][g][n * 8 + 2 * t + 1] = acc[n][1];
-            out[warp][g + 8][n * 8 + 2 * t] = acc[n][2];
-            out[warp][g + 8][n * 8 + 2 * t + 1] = acc[n][3];
-        }
-        __syncthreads();
         // a row of y takes the sums of a team's warps, smallest parts first
-        for (int i = threadIdx.x; i < teams * 16 * a.batch; i += kWqThreads) {
-            const int r = i % (teams * 16), b = i / (teams * 16);
-            const int64_t row = t0 * 16 + r;
-            if (row >= a.rows) continue;
-            float v = 0.0f;
-            for (int p = a.parts - 1; p >= 0; --p)
-                for (int s = 0; s < a.kw; ++s)
-                    v += out[(r >> 4) * a.kw + s][r & 15][b * a.parts + p];
-            store_y(a.y, a.dtype, b * a.ldy + row, 8.0f * v);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                out[warp][g][n * 8 + 2 * t] = acc[r][n][0];
+                out[warp][g][n * 8 + 2 * t + 1] = acc[r][n][1];
+                out[warp][g + 8][n * 8 + 2 * t] = acc[r][n][2];
+                out[warp][g + 8][n * 8 + 2 * t + 1] = acc[r][n][3];
+            }
+            const bool alone = a.kw == 1;     // the warp's own sums: no other warp to wait for
+            if (alone) __syncwarp(); else __syncthreads();
+            const int first = alone ? lane : threadIdx.x, step = alone ? 32 : kWqThreads;
+            const int width = alone ? 16 : teams * 16;
+            for (int i = first; i < width * a.batch; i += step) {
+                const int q = i % width, b = i / width, tm = alone ? warp : q >> 4;
+                const int64_t row = ((t0 + tm) * RT + r) * 16 + (q & 15);
+                if (t0 + tm >= tiles || row >= a.rows) continue;
+                float v = 0.0f;
+                for (int p = a.parts - 1; p >= 0; --p)
+                    for (int s = 0; s < a.kw; ++s) v += out[tm * a.kw + s][q & 15][b * a.parts + p];
+                store_y(a.y, a.dtype, b * a.ldy + row, 8.0f * v);
+            }
+            if (alone) __syncwarp(); else __syncthreads();
         }
-        __syncthreads();
     }
 }
 
-template <int NT>
+template <int NT, int RT>
 cudaError_t launch_matvec(const WqArgs& a, int group, int grid, cudaStream_t st) {
     const size_t smem = (size_t)a.chunk * NT * kWqBlockBytes;
-    const void* fn = group == 32   ? (const void*)wq_matvec_kernel<NT, 32>
-                     : group == 64 ? (const void*)wq_matvec_kernel<NT, 64>
-                                   : (const void*)wq_matvec_kernel<NT, 128>;
+    const void* fn = group == 32   ? (const void*)wq_matvec_kernel<NT, 32, RT>
+                     : group == 64 ? (const void*)wq_matvec_kernel<NT, 64, RT>
+                                   : (const void*)wq_matvec_kernel<NT, 128, RT>;
     cudaError_t e = raise_smem_limit(fn, smem);
     if (e != cudaSuccess) return e;
     count_launches(1);
     if (group == 32)
-        wq_matvec_kernel<NT, 32><<<grid, kWqThreads, smem, st>>>(a);
+        wq_matvec_kernel<NT, 32, RT><<<grid, kWqThreads, smem, st>>>(a);
     else if (group == 64)
-        wq_matvec_kernel<NT, 64><<<grid, kWqThreads, smem, st>>>(a);
+        wq_matvec_kernel<NT, 64, RT><<<grid, kWqThreads, smem, st>>>(a);
     else
-        wq_matvec_kernel<NT, 128><<<grid, kWqThreads, smem, st>>>(a);
+        wq_matvec_kernel<NT, 128, RT><<<grid, kWqThreads, smem, st>>>(a);
     return cudaGetLastError();
 }
 
-// A warp per block of 128 weights, four to a lane.
+// Eight weights from column k, zeros past the row: 16-byte loads where WIDE.
+template <bool WIDE>
+__device__ __forceinline__ void load_eight(const void* w, int dtype, int64_t at, int k, int cols,
+                                           float (&v)[8]) {
+    if (WIDE && k + 8 <= cols) {
+        if (dtype == PVS_F32) {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + at + k);
+            const float4 a = __ldg(p), b = __ldg(p + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+            v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a =
+                __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + at + k));
+            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t h = (u[j >> 1] >> (16 * (j & 1))) & 0xffffu;
+                v[j] = dtype == PVS_BF16 ? __uint_as_float(h << 16)
+                                         : __half2float(__ushort_as_half((uint16_t)h));
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < cols ? load_x(w, dtype, at + k + j) : 0.0f;
+}
+
+// A word (8 weights) per lane, two blocks of 128 a warp and step; a warp runs
+// along a row.  Word l of a block holds k = 8 l ..: group l / 4, byte 16 (l % 4) + 4 (l / 4).
+template <bool WIDE>
 __global__ void __launch_bounds__(256) wq_pack_kernel(const void* w, int64_t ldw, int64_t rows,
                                                       int cols, int dtype, int group, int blocks,
                                                       uint8_t* codes, uint16_t* scales) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = rows * blocks;
-    const int64_t step = (int64_t)gridDim.x * 8;
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += step) {
-        const int64_t row = i / blocks;
-        const int blk = (int)(i - row * blocks);
-        const int k = blk * 128 + lane * 4;
-        float v[4], top = 0.0f;
-        bool finite = true;
+    const int lane = threadIdx.x & 31, l = lane & 15;
+    const int lanes = group / 8;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
+         row += (int64_t)gridDim.x * 8) {
+        const int64_t at = row * ldw;
+#pragma unroll 2
+        for (int b0 = 0; b0 < blocks; b0 += 2) {
+            const int blk = b0 + (lane >> 4);
+            float v[8], top = 0.0f, nan = 0.0f;
+            load_eight<WIDE>(w, dtype, at, blk * 128 + l * 8, cols, v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = k + j < cols ? load_x(w, dtype, row * ldw + k + j) : 0.0f;
-            finite &= isfinite(v[j]);
-            top = fmaxf(top, fabsf(v[j]));
-        }
-        const int lanes = group / 4;
-        for (int o = lanes / 2; o > 0; o >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            finite &= __shfl_xor_sync(0xffffffffu, finite ? 1 : 0, o) != 0;
-        }
-        uint16_t sb = 0x3f80;                       // 1
-        if (!finite) {
-            sb = 0x7fff;                            // NaN
-        } else if (top > 0.0f) {
-            const __nv_bfloat16 s = __float2bfloat16_rn(__fmul_rn(top, 1.0f / 7.0f));
-            sb = __bfloat16_as_ushort(s);
-            if (sb == 0) sb = 1;
-        }
-        const float s = __uint_as_float((uint32_t)sb << 16);
-        uint32_t bits = 0;
+            for (int j = 0; j < 8; ++j) {
+                nan += v[j] * 0.0f;                 // NaN for a NaN or an infinity
+                top = fmaxf(top, fabsf(v[j]));
+            }
+            if (nan != 0.0f) top = INFINITY;
+            for (int o = lanes / 2; o > 0; o >>= 1)
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (blk >= blocks) continue;            // (the shuffles are done: half a warp stops)
+            uint32_t sb = 0x3f80;                   // 1
+            if (top == INFINITY) {
+                sb = 0x7fff;                        // NaN
+            } else if (top > 0.0f) {
+                sb = __bfloat16_as_ushort(__float2bfloat16_rn(__fmul_rn(top, 1.0f / 7.0f)));
+                if (sb == 0) sb = 1;
+            }
+            const float s = __uint_as_float(sb << 16);
+            uint32_t bits = 0x88888888u;
+            if (top != INFINITY) {
+                bits = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            int q = 0;
-            if (finite) q = (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
-            bits |= (uint32_t)(q + 8) << (4 * j);
+                for (int j = 0; j < 8; ++j) {
+                    const int q = (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
+                    bits |= (uint32_t)(q + 8) << (4 * j);
+                }
+            }
+            const int64_t i = row * blocks + blk;
+            *reinterpret_cast<uint32_t*>(codes + i * 64 + 16 * (l & 3) + 4 * (l >> 2)) = bits;
+            if (l % lanes == 0) scales[i * (128 / group) + l / lanes] = (uint16_t)sb;
         }
-        const int word = lane >> 3, t = (lane & 7) >> 1;
-        *reinterpret_cast<uint16_t*>(codes + i * 64 + 16 * t + 4 * word + 2 * (lane & 1)) =
-            (uint16_t)bits;
-        if (lane % lanes == 0) scales[i * (128 / group) + lane / lanes] = sb;
+        __syncwarp();
     }
 }
 
+template <bool WIDE>
 __global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* codes,
                                                         const uint16_t* scales, int64_t rows,
                                                         int cols, int group, int blocks, void* out,
                                                         int64_t ldo, int dtype) {
-    const int lane = threadIdx.x & 31;
-    const int64_t total = rows * blocks;
-    const int64_t step = (int64_t)gridDim.x * 8;
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += step) {
-        const int64_t row = i / blocks;
-        const int blk = (int)(i - row * blocks);
-        const int word = lane >> 3, t = (lane & 7) >> 1;
-        const uint32_t bits = *reinterpret_cast<const uint16_t*>(codes + i * 64 + 16 * t +
-                                                                 4 * word + 2 * (lane & 1));
-        const float s = __uint_as_float(
-            (uint32_t)scales[i * (128 / group) + lane * 4 / group] << 16);
-        const int k = blk * 128 + lane * 4;
+    const int lane = threadIdx.x & 31, l = lane & 15;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
+         row += (int64_t)gridDim.x * 8) {
+#pragma unroll 4
+        for (int blk = lane >> 4; blk < blocks; blk += 2) {
+            const int64_t i = row * blocks + blk;
+            const uint32_t bits =
+                __ldg(reinterpret_cast<const uint32_t*>(codes + i * 64 + 16 * (l & 3) + 4 * (l >> 2)));
+            const float s =
+                __uint_as_float((uint32_t)__ldg(scales + i * (128 / group) + l * 8 / group) << 16);
+            const int k = blk * 128 + l * 8;
+            const int64_t at = row * ldo + k;
+            float v[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (k + j < cols)
-                store_y(out, dtype, row * ldo + k + j, s * (float)((int)((bits >> (4 * j)) & 15u) - 8));
+            for (int j = 0; j < 8; ++j) v[j] = s * (float)((int)((bits >> (4 * j)) & 15u) - 8);
+            if (WIDE && k + 8 <= cols) {
+                if (dtype == PVS_F32) {
+                    float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
+                    p[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    p[1] = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (dtype == PVS_BF16) {
+                            const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                            h[j] = *reinterpret_cast<const uint32_t*>(&p);
+                        } else {
+                            const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+                            h[j] = *reinterpret_cast<const uint32_t*>(&p);
+                        }
+                    }
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) =
+                        make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k + j < cols) store_y(out, dtype, at + j, v[j]);
+            }
+        }
     }
+}
+
+// Whether every eight elements of a row from a multiple of eight are aligned.
+bool wide(const void* p, int64_t ld) {
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0;
 }
 
 bool shape_ok(int64_t rows, int32_t cols, int32_t group, int32_t dtype) {
@@ -317,10 +434,14 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
     if (rows == 0) return PVS_OK;
     if (!w || !codes || !scales || !codes_aligned(codes, scales)) return PVS_ERR_INVALID;
     const int blocks = (cols + 127) / 128;
+    const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    uint16_t* s = static_cast<uint16_t*>(scales);
     count_launches(1);
-    wq_pack_kernel<<<(unsigned)std::min<int64_t>((rows * blocks + 7) / 8, 152 * 32), 256, 0,
-                     static_cast<cudaStream_t>(cuda_stream)>>>(
-        w, ldw, rows, cols, dtype, group, blocks, codes, static_cast<uint16_t*>(scales));
+    if (wide(w, ldw))
+        wq_pack_kernel<true><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group, blocks, codes, s);
+    else
+        wq_pack_kernel<false><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group, blocks, codes, s);
     return queued(cudaGetLastError());
 }
 
@@ -331,10 +452,16 @@ extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, in
     if (rows == 0) return PVS_OK;
     if (!out || !codes || !scales || !codes_aligned(codes, scales)) return PVS_ERR_INVALID;
     const int blocks = (cols + 127) / 128;
+    const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const uint16_t* s = static_cast<const uint16_t*>(scales);
     count_launches(1);
-    wq_unpack_kernel<<<(unsigned)std::min<int64_t>((rows * blocks + 7) / 8, 152 * 32), 256, 0,
-                       static_cast<cudaStream_t>(cuda_stream)>>>(
-        codes, static_cast<const uint16_t*>(scales), rows, cols, group, blocks, out, ldout, dtype);
+    if (wide(out, ldout))
+        wq_unpack_kernel<true><<<grid, 256, 0, st>>>(codes, s, rows, cols, group, blocks, out, ldout,
+                                                     dtype);
+    else
+        wq_unpack_kernel<false><<<grid, 256, 0, st>>>(codes, s, rows, cols, group, blocks, out, ldout,
+                                                      dtype);
     return queued(cudaGetLastError());
 }
 
@@ -362,8 +489,11 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
     a.ldy = ldy;
     // a pass takes what 16 columns hold; one tile of 8 where that is enough
     const int most = 16 / a.parts;
-    const int64_t tiles = (rows + 15) / 16;
-    // warps share k until there are about 8 warps for every SM
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    // 32 rows a warp where that still gives every SM 16 warps or more; else 16 rows, and
+    // warps share k until there are about 8 for every SM
+    const int rt = rows >= 16ll * 32 * dev.sms ? 2 : 1;
+    const int64_t tiles = (rows + 16 * rt - 1) / (16 * rt);
     a.kw = 1;
     while (a.kw < 8 && a.kw * 2 <= a.blocks && tiles * a.kw < 8ll * dev.sms) a.kw *= 2;
     const int64_t groups = (tiles * a.kw + kWqWarps - 1) / kWqWarps;
@@ -373,9 +503,11 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
         a.y = static_cast<uint8_t*>(y) + (int64_t)b * ldy * es;
         const int nt = a.batch * a.parts > 8 ? 2 : 1;
         a.chunk = std::min(a.blocks, kWqSmem / (nt * kWqBlockBytes));
-        const int grid = (int)std::min<int64_t>(groups, 2ll * dev.sms);
-        e = nt == 1 ? launch_matvec<1>(a, group, grid, static_cast<cudaStream_t>(cuda_stream))
-                    : launch_matvec<2>(a, group, grid, static_cast<cudaStream_t>(cuda_stream));
+        const int grid = (int)std::min<int64_t>(groups, 4ll * dev.sms);
+        e = nt == 1 ? (rt == 1 ? launch_matvec<1, 1>(a, group, grid, st)
+                               : launch_matvec<1, 2>(a, group, grid, st))
+                    : (rt == 1 ? launch_matvec<2, 1>(a, group, grid, st)
+                               : launch_matvec<2, 2>(a, group, grid, st));
     }
     return queued(e);
 }
