@@ -419,14 +419,15 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]) * sm.k2;
                     }
+                    // the column of the row's target, as a bit
                     const int64_t yr = y - cc * 32;
-                    const bool here = yr >= 0 && yr < 32;
-                    const bool any_here = __any_sync(0xffffffffu, here);
+                    const uint32_t here = yr >= 0 && yr < 32 ? 1u << (int)yr : 0u;
+                    const bool any_here = __any_sync(0xffffffffu, here != 0);
                     if constexpr (EPI == kStats) {
-                        if (any_here && here) {
+                        if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (i == (int)yr) v[i] = -INFINITY;
+                                v[i] = here & (1u << i) ? -INFINITY : v[i];
                         }
                         float cm = v[0];
 #pragma unroll
@@ -445,10 +446,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             v[i] = none ? 0.0f : ex2(v[i] - gr.m) * gr.coef;
-                        if (any_here && here) {
+                        if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (i == (int)yr) v[i] = gr.hit;
+                                v[i] = here & (1u << i) ? gr.hit : v[i];
                         }
                         if (row < sm.rows) {
                             uint16_t* o = sm.grad + (int64_t)row * sm.ldg + n0 + cc * 32;
