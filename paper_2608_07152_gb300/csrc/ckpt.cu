@@ -310,10 +310,12 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, const Device
     p.ldb = round_up(cols, 8);
     p.ldslot = round_up(cols, 8);
     const int bn = tile_columns(cols);
-    const int64_t units = (int64_t)((out_cols + kTileM - 1) / kTileM) * ((cols + bn - 1) / bn);
+    const int tile_m = kTileM * ctas_for(out_cols, dev);
+    const int64_t slots = tile_m > kTileM ? dev.pairs : dev.sms;
+    const int64_t units = (int64_t)((out_cols + tile_m - 1) / tile_m) * ((cols + bn - 1) / bn);
     const int64_t kc = (rows + kTileK - 1) / kTileK;
     // enough splits for every SM, none under 8 chunks
-    int64_t s = std::max<int64_t>(1, std::min<int64_t>(dev.sms / std::min<int64_t>(units, dev.sms), kc / 8));
+    int64_t s = std::max<int64_t>(1, std::min<int64_t>(slots / std::min<int64_t>(units, slots), kc / 8));
     // float32 sums: 128 steps at most before the splits are added with rounding
     if (dtype == PVS_F32) s = std::max<int64_t>(s, (kc + 31) / 32);
     p.splits = (int)s;
@@ -460,7 +462,8 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     g.status = dev.status;
     g.nprob = 1;
     Problem& q = g.p[0];
-    set_tiles(q, out_cols, cols, tile_columns(cols), rows);
+    g.cta = ctas_for(out_cols, dev);
+    set_tiles(q, out_cols, cols, tile_columns(cols), rows, g.cta);
     q.splits = p.splits;
     if (!operand_map(&q.a, Matrix{p.a, rows, out_cols, p.lda, p.parts, rows * p.lda}, true, 0) ||
         !operand_map(&q.b, Matrix{p.b, rows, cols, p.ldb, 1, 0}, true, 0))
@@ -475,7 +478,7 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     q.out_type = dtype;
     q.alpha0 = 1.0f;
     part_pairs(g, p.parts, 1);
-    e = launch_gemm(kOut, g, dev.sms, st);
+    e = launch_gemm(kOut, g, dev, st);
     if (e == cudaSuccess && q.to_slots)
         e = launch_sum_slots(p.slots, p.splits, q.slot_stride, p.ldslot, out_cols, cols, nullptr,
                              1.0f, dw, lddw, dtype, st);

@@ -1,14 +1,20 @@
 // Persistent tcgen05 product of the projection head's operators (head_gemm.h).
 //
-// One CTA per SM, 10 warps.  A unit of work is a tile of D (128 x bn) over a
-// range of k; unit u goes to CTA u mod grid.
-//   warp 0     TMA producer: A (128 x 64) and B (bn x 64) chunks into a ring of
-//              four stages, 128-byte swizzle;
-//   warp 1     one thread issues the MMAs (M = 128, N = bn, K = 16, four to
-//              a chunk) into one of two TMEM accumulators;
-//   warps 2-9  epilogue: a TMEM lane (a row of D) per thread; the two warps
-//              that share a lane quarter take every other chunk of 32 columns.
+// CTA pairs (the two SMs of a TPC, cta_group::2), one CTA per SM, 10 warps.  A unit
+// of work is a tile of D (256 x bn) over a range of k; each CTA holds its own 128
+// rows of A and half of B's rows, 32 KB a chunk.  A lone CTA needs 48 KB for 128 x
+// 256, and its shared memory (fills and the MMAs' reads, 192 bytes a cycle at
+// full rate where 128 are there) kept the tensor cores 62% busy; lone CTAs (kCta = 1)
+// serve the products of 128 rows or fewer, which memory bounds.
+//   warp 0     TMA producer (both CTAs): chunks of A (128 x 64) and B into a ring,
+//              128-byte swizzle, the pair's bytes counted on the even CTA's barrier;
+//   warp 1     one thread (of the even CTA) issues the MMAs (M = 128 or 256, N = bn,
+//              K = 16, four to a chunk) into one of two TMEM accumulators;
+//   warps 2-9  epilogue (both CTAs): a TMEM lane (a row of D) per thread; the two
+//              warps that share a lane quarter take every other chunk of 32 columns.
 // Two accumulators let the epilogue of a unit run under the MMAs of the next.
+// Of two problems in one launch each gets CTAs of its own, in proportion to its
+// work, so that units of unlike lengths do not wait for one another.
 //
 // Operands.  K contiguous: a box is 64 elements of k (128 bytes) by the tile's
 // rows.  M or N contiguous (gradients contract over rows): a box is 64 of m by
@@ -21,6 +27,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "../../include/head.h"
@@ -34,9 +41,12 @@ namespace pvs {
 namespace head {
 
 constexpr int kStageA = kTileM * kTileK * 2;     // 16 KB
-constexpr int kStageB = kTileN * kTileK * 2;     // 32 KB
-constexpr int kStageBytes = kStageA + kStageB;
-constexpr int kStages = 4;
+template <int kCta> struct Ring {
+    static constexpr int kStageB = kTileN / kCta * kTileK * 2;   // this CTA's share of B
+    static constexpr int kStageBytes = kStageA + kStageB;
+    static constexpr int kStages = kCta == 2 ? 6 : 4;
+};
+constexpr int kMaxStages = 6;
 constexpr int kEpiWarps = 8;
 constexpr int kEpiThreads = kEpiWarps * 32;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
@@ -46,8 +56,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 static_assert(kEpiThreads == kTileN, "an epilogue thread stages one column's bias");
 
 struct Shared {
-    uint64_t full[kStages];
-    uint64_t empty[kStages];
+    uint64_t full[kMaxStages];
+    uint64_t empty[kMaxStages];
     uint64_t tfull[2];
     uint64_t tempty[2];
     uint32_t tmem_base;
@@ -56,8 +66,11 @@ struct Shared {
     alignas(16) float b2[2][kTileN];     // their biases, in powers of two
 };
 
-constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + sizeof(Shared);
-static_assert(kSmemBytes <= 227 * 1024, "smem");
+template <int kCta>
+constexpr size_t smem_bytes() {
+    return 1024 + (size_t)Ring<kCta>::kStages * Ring<kCta>::kStageBytes + sizeof(Shared);
+}
+static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "smem");
 
 __device__ __forceinline__ bool abort_set(Shared& sh) {
     return *reinterpret_cast<volatile int*>(&sh.abort) != 0;
@@ -80,13 +93,23 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
+// A box into this CTA's shared memory, its bytes counted on the mbarrier at
+// shared::cluster address `bar` (this CTA's or, of a pair, its peer's).
+template <int kCta>
 __device__ __forceinline__ void tma_load_3d(void* dst, const void* tmap, int x, int y, int z,
-                                            uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-        : "memory");
+                                            uint32_t bar) {
+    if constexpr (kCta == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+            "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+            "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
 }
 
 // 32 bytes to global memory, a whole sector.
@@ -123,15 +146,22 @@ __device__ __forceinline__ uint32_t cut_bf16(float& lo, float& hi) {
     return (l >> 16) | h;
 }
 
+// The units of one slot (a CTA, or a pair): those of one problem, a stride apart.
+struct Walk {
+    int prob, first, step, end;
+};
+__device__ __forceinline__ Walk walk_of(const Args& a, int slot, int nslots) {
+    if (a.nprob == 1) return Walk{0, slot, nslots, a.p[0].units};
+    if (slot < a.slots0) return Walk{0, slot, a.slots0, a.p[0].units};
+    return Walk{1, slot - a.slots0, nslots - a.slots0, a.p[1].units};
+}
+
 // A unit's tile and range of k.
 struct Unit {
-    int prob, mt, nt, split, k0, k1;
+    int mt, nt, split, k0, k1;
 };
-__device__ __forceinline__ Unit unit_of(const Args& a, int u) {
+__device__ __forceinline__ Unit unit_of(const Problem& p, int u) {
     Unit w;
-    w.prob = a.nprob > 1 && u >= a.p[0].units ? 1 : 0;
-    const Problem& p = a.p[w.prob];
-    if (w.prob) u -= a.p[0].units;
     if (p.m_fast) {
         w.mt = u % p.mtiles;
         u /= p.mtiles;
@@ -181,32 +211,42 @@ __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const
     }
 }
 
-template <int EPI>
-__global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ Args a,
-                                                                int total) {
+template <int EPI, int kCta>
+__global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ Args a) {
+    using R = Ring<kCta>;
     extern __shared__ uint8_t smem_raw[];
+    // the layout is the same in both CTAs of a pair: barriers and the pair's MMAs are
+    // addressed by offset
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t* stages = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
-    Shared& sh = *reinterpret_cast<Shared*>(stages + kStages * kStageBytes);
+    Shared& sh = *reinterpret_cast<Shared*>(stages + R::kStages * R::kStageBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int crank = kCta == 2 ? (int)cluster_ctarank() : 0;
+    const bool leader = crank == 0;
+    const Walk walk = walk_of(a, blockIdx.x / kCta, gridDim.x / kCta);
+    const Problem& p = a.p[walk.prob];
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < R::kStages; ++s) {
             mbar_init(&sh.full[s], 1);
             mbar_init(&sh.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sh.tfull[b], 1);
-            mbar_init(&sh.tempty[b], kEpiWarps);
+            mbar_init(&sh.tempty[b], kCta * kEpiWarps);   // both CTAs' epilogue warps
         }
         sh.abort = 0;
         mbar_fence_init();
     }
     if (warp == 1) {
-        tc::tmem_alloc(&sh.tmem_base, kTmemCols);
+        if (kCta == 2)
+            tc::tmem_alloc_pair(&sh.tmem_base, kTmemCols);
+        else
+            tc::tmem_alloc(&sh.tmem_base, kTmemCols);
         tc::fence_before_sync();
     }
     __syncthreads();
+    if (kCta == 2) cluster_barrier();   // both CTAs' barriers and TMEM are ready
     tc::fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
 
@@ -214,63 +254,65 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         // ---------------- TMA producer ----------------
         if (lane == 0) {
             uint32_t g = 0;
-            for (int u = blockIdx.x; u < total && !abort_set(sh); u += gridDim.x) {
-                const Unit w = unit_of(a, u);
-                const Problem& p = a.p[w.prob];
-                const bool alt = p.alt_flag && *p.alt_flag;
-                const CUtensorMap* mb = alt ? &p.b_alt : &p.b;
-                const int am = p.a_mo + w.mt * kTileM;
-                const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn;
+            const bool alt = p.alt_flag && *p.alt_flag;
+            const CUtensorMap* mb = alt ? &p.b_alt : &p.b;
+            const int bhalf = p.bn / kCta;              // rows of B that this CTA supplies
+            const int nbox = (bhalf + 63) / 64;
+            // the bytes of a stage, of both CTAs
+            const uint32_t bytes =
+                kCta * (kStageA + (uint32_t)(p.b_mn ? nbox * 64 : bhalf) * kTileK * 2u);
+            for (int u = walk.first; u < walk.end && !abort_set(sh); u += walk.step) {
+                const Unit w = unit_of(p, u);
+                const int am = p.a_mo + (w.mt * kCta + crank) * kTileM;
+                const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn + crank * bhalf;
                 const int bk = alt ? p.alt_ko : p.b_ko;
-                const int nbox = (p.bn + 63) / 64;
-                const uint32_t bytes =
-                    kStageA + (uint32_t)(p.b_mn ? nbox * 64 : p.bn) * kTileK * 2u;
                 for (int q = 0; q < a.npairs && !abort_set(sh); ++q) {
                     const int pa = a.pa[q], pb = a.pb[q];
                     for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
-                        const int s = g % kStages;
-                        if (!mbar_wait(&sh.empty[s], ((g / kStages) & 1u) ^ 1u)) {
+                        const int s = g % R::kStages;
+                        if (!mbar_wait(&sh.empty[s], ((g / R::kStages) & 1u) ^ 1u)) {
                             raise_abort(sh, a.status);
                             break;
                         }
-                        uint8_t* sa = stages + s * kStageBytes;
+                        uint8_t* sa = stages + s * R::kStageBytes;
                         uint8_t* sb = sa + kStageA;
-                        uint64_t* bar = &sh.full[s];
-                        mbar_arrive_expect_tx(bar, bytes);
+                        if (leader) mbar_arrive_expect_tx(&sh.full[s], bytes);
+                        const uint32_t bar =
+                            kCta == 2 ? cluster_map(&sh.full[s], 0) : smem_u32(&sh.full[s]);
                         const int ka = p.a_ko + kc * kTileK, kb = bk + kc * kTileK;
                         if (p.a_mn) {
-                            tma_load_3d(sa, &p.a, am, ka, pa, bar);
-                            tma_load_3d(sa + kTileK * 128, &p.a, am + 64, ka, pa, bar);
+                            tma_load_3d<kCta>(sa, &p.a, am, ka, pa, bar);
+                            tma_load_3d<kCta>(sa + kTileK * 128, &p.a, am + 64, ka, pa, bar);
                         } else {
-                            tma_load_3d(sa, &p.a, ka, am, pa, bar);
+                            tma_load_3d<kCta>(sa, &p.a, ka, am, pa, bar);
                         }
                         if (p.b_mn) {
                             for (int i = 0; i < nbox; ++i)
-                                tma_load_3d(sb + i * kTileK * 128, mb, bnc + 64 * i, kb, pb, bar);
+                                tma_load_3d<kCta>(sb + i * kTileK * 128, mb, bnc + 64 * i, kb, pb,
+                                                  bar);
                         } else {
-                            tma_load_3d(sb, mb, kb, bnc, pb, bar);
+                            tma_load_3d<kCta>(sb, mb, kb, bnc, pb, bar);
                         }
                     }
                 }
             }
-            // the MMAs have consumed the last fill of every stage used: no copy
-            // into this CTA is still in flight when it ends
-            for (int s = 0; s < kStages && (uint32_t)s < g; ++s) {
-                const uint32_t last = g - 1 - ((g - 1 - s) % kStages);
-                if (!mbar_wait(&sh.empty[s], (last / kStages) & 1u)) raise_abort(sh, a.status);
+            // the MMAs have consumed the last fill of every stage used: no copy into
+            // this CTA and no commit to its barriers is still in flight when it ends
+            for (int s = 0; s < R::kStages && (uint32_t)s < g; ++s) {
+                const uint32_t last = g - 1 - ((g - 1 - s) % R::kStages);
+                if (!mbar_wait(&sh.empty[s], (last / R::kStages) & 1u)) raise_abort(sh, a.status);
             }
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
-        if (lane == 0) {
+        // ---------------- MMA issuer (the even CTA of a pair) ----------------
+        if (lane == 0 && leader) {
+            const uint32_t idesc = (a.f16 ? tc::idesc_f16_f32(kTileM * kCta, p.bn)
+                                          : tc::idesc_bf16_f32(kTileM * kCta, p.bn)) |
+                                   ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16);
             uint32_t g = 0;
             int it = 0;
-            for (int u = blockIdx.x; u < total && !abort_set(sh); u += gridDim.x, ++it) {
-                const Unit w = unit_of(a, u);
-                const Problem& p = a.p[w.prob];
-                const uint32_t idesc = (a.f16 ? tc::idesc_f16_f32(kTileM, p.bn)
-                                              : tc::idesc_bf16_f32(kTileM, p.bn)) |
-                                       ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16);
+            for (int u = walk.first; u < walk.end && !abort_set(sh); u += walk.step, ++it) {
+                const Unit w = unit_of(p, u);
                 const int b = it & 1;
                 if (!mbar_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u)) {
                     raise_abort(sh, a.status);
@@ -281,13 +323,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 uint32_t acc = 0;
                 const int chunks = a.npairs * (w.k1 - w.k0);
                 for (int kc = 0; kc < chunks; ++kc, ++g) {
-                    const int s = g % kStages;
-                    if (!mbar_wait(&sh.full[s], (g / kStages) & 1u)) {
+                    const int s = g % R::kStages;
+                    if (!mbar_wait(&sh.full[s], (g / R::kStages) & 1u)) {
                         raise_abort(sh, a.status);
                         break;
                     }
                     tc::fence_after_sync();
-                    const uint32_t sa = smem_u32(stages + s * kStageBytes);
+                    const uint32_t sa = smem_u32(stages + s * R::kStageBytes);
                     const uint32_t sb = sa + kStageA;
 #pragma unroll
                     for (int k = 0; k < kTileK / 16; ++k) {
@@ -295,13 +337,22 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                                                    : tc::smem_desc_sw128_kmajor(sa + k * 32);
                         const uint64_t bd = p.b_mn ? smem_desc_sw128_mn(sb + k * 2048)
                                                    : tc::smem_desc_sw128_kmajor(sb + k * 32);
-                        tc::mma_bf16(d, ad, bd, idesc, acc);
+                        if (kCta == 2)
+                            tc::mma_f16_pair(d, ad, bd, idesc, acc);
+                        else
+                            tc::mma_bf16(d, ad, bd, idesc, acc);
                         acc = 1;
                     }
-                    tc::commit(&sh.empty[s]);
+                    if (kCta == 2)
+                        tc::commit_pair(&sh.empty[s]);   // the stage is free in both CTAs
+                    else
+                        tc::commit(&sh.empty[s]);
                 }
                 if (abort_set(sh)) break;
-                tc::commit(&sh.tfull[b]);
+                if (kCta == 2)
+                    tc::commit_pair(&sh.tfull[b]);
+                else
+                    tc::commit(&sh.tfull[b]);
             }
             // TMEM is released after the last unit's MMAs
             if (it > 0) {
@@ -317,12 +368,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         const int et = threadIdx.x - 64;
         const int row_in_tile = quarter * 32 + lane;
         const Softmax& sm = a.sm;
+        const uint32_t tempty_at[2] = {kCta == 2 ? cluster_map(&sh.tempty[0], 0) : 0u,
+                                       kCta == 2 ? cluster_map(&sh.tempty[1], 0) : 0u};
         int it = 0;
-        for (int u = blockIdx.x; u < total; u += gridDim.x, ++it) {
-            const Unit w = unit_of(a, u);
-            const Problem& p = a.p[w.prob];
+        for (int u = walk.first; u < walk.end; u += walk.step, ++it) {
+            const Unit w = unit_of(p, u);
             const int b = it & 1;
-            const int row = w.mt * kTileM + row_in_tile;
+            const int row = (w.mt * kCta + crank) * kTileM + row_in_tile;
             const int n0 = w.nt * p.bn;
             const int ncols = min(p.bn, p.n - n0);      // columns of D in the tile
             [[maybe_unused]] int64_t y = -1;
@@ -364,8 +416,6 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             for (int cc = half; cc * 32 < p.bn; cc += 2) {
                 uint32_t r[32];
                 __syncwarp();
-                // a tile's last chunk may be 16 columns wide; the columns past it are
-                // allocated, and what they hold is not used
                 tc::ld_32x32b_x32(tcol + (uint32_t)(cc * 32), r);
                 tc::wait_ld();
                 if constexpr (EPI == kOut) {
@@ -476,13 +526,22 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             }
             tc::fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.tempty[b]);
+            if (lane == 0) {
+                if (kCta == 2)
+                    mbar_arrive_remote(tempty_at[b]);   // the even CTA's barrier (or its own)
+                else
+                    mbar_arrive(&sh.tempty[b]);
+            }
         }
     }
     __syncthreads();
+    if (kCta == 2) cluster_barrier();   // no CTA leaves while its peer may still address it
     if (warp == 1) {
         tc::fence_after_sync();
-        tc::tmem_dealloc(tmem, kTmemCols);
+        if (kCta == 2)
+            tc::tmem_dealloc_pair(tmem, kTmemCols);
+        else
+            tc::tmem_dealloc(tmem, kTmemCols);
     }
 }
 
@@ -622,7 +681,35 @@ void part_pairs(Args& a, int pa, int pb) {
             }
 }
 
-cudaError_t launch_gemm(int epilogue, Args& a, int num_sms, cudaStream_t st) {
+namespace {
+
+template <int kCta>
+const void* kernel_of(int epilogue) {
+    return epilogue == kStats  ? (const void*)head_gemm_kernel<kStats, kCta>
+           : epilogue == kGrad ? (const void*)head_gemm_kernel<kGrad, kCta>
+                               : (const void*)head_gemm_kernel<kOut, kCta>;
+}
+
+cudaLaunchConfig_t config(int cta, int grid, cudaStream_t st, cudaLaunchAttribute* attr) {
+    cudaLaunchConfig_t cfg{};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cta;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = cta == 2 ? smem_bytes<2>() : smem_bytes<1>();
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+}  // namespace
+
+cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t st) {
+    const int cta = a.cta;
+    const int slots = cta == 2 ? dev.pairs : dev.sms;
     int64_t total = 0;
     for (int i = 0; i < a.nprob; ++i) {
         Problem& p = a.p[i];
@@ -632,20 +719,24 @@ cudaError_t launch_gemm(int epilogue, Args& a, int num_sms, cudaStream_t st) {
         p.units = (int)u;
         total += u;
     }
-    const int grid = (int)(total < num_sms ? total : num_sms);
-    const void* fn = epilogue == kStats  ? (const void*)head_gemm_kernel<kStats>
-                     : epilogue == kGrad ? (const void*)head_gemm_kernel<kGrad>
-                                         : (const void*)head_gemm_kernel<kOut>;
-    cudaError_t e = raise_smem_limit(fn, kSmemBytes);
+    int used = (int)std::min<int64_t>(total, slots);
+    if (a.nprob == 2) {
+        // slots in proportion to the problems' work
+        used = std::max(used, 2);
+        if (a.slots0 < 1 || a.slots0 >= used) {
+            const double w0 = (double)a.p[0].units * a.p[0].kchunks / a.p[0].splits;
+            const double w1 = (double)a.p[1].units * a.p[1].kchunks / a.p[1].splits;
+            a.slots0 = std::min(std::max((int)(used * w0 / (w0 + w1) + 0.5), 1), used - 1);
+        }
+    }
+    const void* fn = cta == 2 ? kernel_of<2>(epilogue) : kernel_of<1>(epilogue);
+    cudaLaunchAttribute attr[1];
+    const cudaLaunchConfig_t cfg = config(cta, used * cta, st, attr);
+    cudaError_t e = raise_smem_limit(fn, cfg.dynamicSmemBytes);
     if (e != cudaSuccess) return e;
     count_launches(1);
-    if (epilogue == kStats)
-        head_gemm_kernel<kStats><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
-    else if (epilogue == kGrad)
-        head_gemm_kernel<kGrad><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
-    else
-        head_gemm_kernel<kOut><<<grid, kThreads, kSmemBytes, st>>>(a, (int)total);
-    return cudaGetLastError();
+    void* args[1] = {&a};
+    return cudaLaunchKernelExC(&cfg, fn, args);
 }
 
 namespace {
@@ -665,11 +756,21 @@ cudaError_t device(Device* d) {
         int sms = 0;
         e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;
+        // CTA pairs that run at once (0 where none can: lone CTAs serve then)
+        int pairs = 0;
+        cudaLaunchAttribute attr[1];
+        const cudaLaunchConfig_t cfg = config(2, 2 * sms, nullptr, attr);
+        if (raise_smem_limit(kernel_of<2>(kOut), cfg.dynamicSmemBytes) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&pairs, kernel_of<2>(kOut), &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            pairs = 0;
+        }
         void* p = nullptr;
         e = cudaHostAlloc(&p, 256, cudaHostAllocPortable | cudaHostAllocMapped);
         if (e != cudaSuccess) return e;
         *static_cast<volatile int*>(p) = 0;
         g.sms = sms;
+        g.pairs = pairs;
         g.status = static_cast<int*>(p);
     }
     *d = g;

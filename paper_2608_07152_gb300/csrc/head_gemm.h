@@ -18,8 +18,8 @@
 namespace pvs {
 namespace head {
 
-constexpr int kTileM = 128;
-constexpr int kTileN = 256;     // at most; a product may use fewer columns (bn)
+constexpr int kTileM = 128;     // a CTA; a pair's tile has 256 rows
+constexpr int kTileN = 256;     // at most; a product may use fewer columns (bn, in steps of 32)
 constexpr int kTileK = 64;      // 128 bytes: one swizzle row
 constexpr int kMaxParts = 3;
 constexpr int kMaxPairs = 6;
@@ -41,7 +41,7 @@ struct Problem {
     const int* alt_flag;
     int a_mn, b_mn;              // 1: M (N) is the contiguous index
     int m, n;                    // extents of D
-    int bn;                      // columns per tile: a multiple of 16, <= kTileN
+    int bn;                      // columns per tile: a multiple of 32, <= kTileN
     int mtiles, ntiles, splits;
     int kchunks;                 // chunks of kTileK for one pair of parts
     int a_mo, a_ko, b_no, b_ko;  // where D's corner lies in the operands
@@ -90,19 +90,31 @@ struct Args {
     int npairs;
     uint8_t pa[kMaxPairs], pb[kMaxPairs];
     int f16;
+    int cta;                     // CTAs to a tile: 1, or 2 (a pair)
+    int slots0;                  // of two problems, the CTAs (pairs) of the first; 0: by work
     Softmax sm;
     int* status;
 };
 
-// Tensor map of an operand: boxes of kTileK x rows (K contiguous) or
+// The current device: its SMs, the CTA pairs that run at once on them, and the
+// status word that its kernels set (pinned host memory).
+struct Device {
+    int sms, pairs;
+    int* status;
+};
+cudaError_t device(Device* d);
+int take_status(const Device& d);
+
+// Tensor map of an operand: boxes of kTileK x box_rows (K contiguous) or
 // 64 x kTileK (M / N contiguous).
 bool operand_map(CUtensorMap* m, const Matrix& x, bool mn, int box_rows);
 
-// Columns per tile for n columns: the fewest tiles, evenly wide.
+// Columns per tile for n columns: the fewest tiles, evenly wide, in the steps of 32
+// that a pair's MMA takes.
 inline int tile_columns(int64_t n) {
     const int64_t t = (n + kTileN - 1) / kTileN;
     const int64_t w = (n + t - 1) / t;
-    return (int)((w + 15) / 16 * 16);
+    return (int)((w + 31) / 32 * 32);
 }
 
 // Columns per tile of n logits: whole tiles but for the last (a tile's 16-bit
@@ -113,7 +125,10 @@ inline int logit_columns(int64_t n) { return n >= kTileN ? kTileN : tile_columns
 // product is not below the last kept bit.
 void part_pairs(Args& a, int pa, int pb);
 
-cudaError_t launch_gemm(int epilogue, Args& a, int num_sms, cudaStream_t st);
+cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t st);
+
+// Pairs where there are more rows than one CTA takes.
+inline int ctas_for(int64_t m, const Device& dev) { return m > kTileM && dev.pairs > 0 ? 2 : 1; }
 
 // out = alpha sum_s slots[s], rounded once.
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
@@ -141,21 +156,12 @@ cudaError_t launch_split(const SplitArgs& a, cudaStream_t st);
 cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, int64_t rows, int cols,
                                uint16_t* dst, int64_t ldd, cudaStream_t st);
 
-// The current device: its SM count and the status word that its kernels set
-// (pinned host memory); status is what an earlier kernel left there.
-struct Device {
-    int sms;
-    int* status;
-};
-cudaError_t device(Device* d);
-int take_status(const Device& d);
-
 // A product's tiles; splits and everything else are the caller's.
-inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k) {
+inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k, int cta) {
     p.m = (int)m;
     p.n = (int)n;
     p.bn = bn;
-    p.mtiles = (int)((m + kTileM - 1) / kTileM);
+    p.mtiles = (int)((m + kTileM * cta - 1) / (kTileM * cta));
     p.ntiles = (int)((n + bn - 1) / bn);
     p.kchunks = (int)((k + kTileK - 1) / kTileK);
     p.splits = 1;

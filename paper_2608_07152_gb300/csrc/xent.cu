@@ -287,14 +287,15 @@ cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a,
     Problem& q = g.p[0];
     q = Problem{};
     g.nprob = 1;
-    set_tiles(q, a.rows, n, logit_columns(n), a.dim);
-    if (!operand_map(&q.a, x, false, kTileM) || !operand_map(&q.b, w, false, q.bn))
+    g.cta = ctas_for(a.rows, dev);
+    set_tiles(q, a.rows, n, logit_columns(n), a.dim, g.cta);
+    if (!operand_map(&q.a, x, false, kTileM) || !operand_map(&q.b, w, false, q.bn / g.cta))
         return cudaErrorInvalidValue;
     q.b_no = p.copy_w ? 0 : (int)v0;
     q.m_fast = 1;
     g.sm.item0 = (int)v0;
     part_pairs(g, p.parts, p.parts);
-    return launch_gemm(epilogue, g, dev.sms, st);
+    return launch_gemm(epilogue, g, dev, st);
 }
 
 SplitArgs split_of(const pvs_xent_args& a, const Plan& p) {
@@ -425,10 +426,12 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         if (e != cudaSuccess) break;
         const Matrix gm{p.g, T, n, p.ldg, p.parts, T * p.ldg};
         g.nprob = 0;
+        // dw's tiles have items for rows: pairs unless all of it is one CTA's tile
+        g.cta = ctas_for(dw ? std::max(T, n) : T, dev);
         if (dx) {
             Problem& q = g.p[g.nprob++];
             q = Problem{};
-            set_tiles(q, T, a.dim, p.bnd, n);
+            set_tiles(q, T, a.dim, p.bnd, n, g.cta);
             q.splits = std::min(p.xsplits, q.kchunks);
             if (!operand_map(&q.a, gm, false, kTileM) ||
                 !operand_map(&q.b, p.copy_w ? copied : direct, true, 0))
@@ -454,7 +457,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         if (dw) {
             Problem& q = g.p[g.nprob++];
             q = Problem{};
-            set_tiles(q, n, a.dim, p.bnd, T);
+            set_tiles(q, n, a.dim, p.bnd, T, g.cta);
             q.splits = std::min(p.wsplits, q.kchunks);
             if (!operand_map(&q.a, gm, true, 0) || !operand_map(&q.b, x, true, 0))
                 return cudaErrorInvalidValue;
@@ -472,7 +475,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         }
         if (g.nprob == 0) break;
         part_pairs(g, p.parts, p.parts);
-        e = launch_gemm(kOut, g, dev.sms, st);
+        e = launch_gemm(kOut, g, dev, st);
         if (e == cudaSuccess && qw && qw->to_slots)
             e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.ldp, n, a.dim, alpha,
                                  a.scale, qw->out, lddw, a.dtype, st);
