@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "../../include/head.h"
+#include "f32x2.cuh"
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
@@ -25,6 +26,10 @@ template <> struct Element<PVS_BF16> {
     static __device__ __forceinline__ uint32_t from(float x) {
         return __bfloat16_as_ushort(__float2bfloat16_rn(x));
     }
+    static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
 };
 template <> struct Element<PVS_F16> {
     using T = uint16_t;
@@ -34,6 +39,10 @@ template <> struct Element<PVS_F16> {
     static __device__ __forceinline__ uint32_t from(float x) {
         return __half_as_ushort(__float2half_rn(x));
     }
+    static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
 };
 template <> struct Element<PVS_F32> {
     using T = uint32_t;
@@ -41,7 +50,7 @@ template <> struct Element<PVS_F32> {
     static __device__ __forceinline__ uint32_t from(float x) { return __float_as_uint(x); }
 };
 
-// N consecutive elements (8, aligned to their size, or 1) as raw words.
+// N consecutive elements (8, aligned to their size, or 1).
 template <int TYPE, int N>
 __device__ __forceinline__ void load_elements(const void* p, int64_t at, float (&v)[N]) {
     using E = Element<TYPE>;
@@ -71,7 +80,7 @@ __device__ __forceinline__ void store_elements(void* p, int64_t at, const float 
     } else {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = E::from(v[2 * i]) | (E::from(v[2 * i + 1]) << 16);
+        for (int i = 0; i < 4; ++i) w[i] = E::pair(v[2 * i], v[2 * i + 1]);
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
@@ -81,36 +90,116 @@ __device__ __forceinline__ void load_codes(const int8_t* p, int64_t at, float (&
         v[0] = (float)__ldg(p + at);
     } else {
         const uint2 a = __ldg(reinterpret_cast<const uint2*>(p + at));
-        const uint32_t w[2] = {a.x, a.y};
+        const uint32_t w[2] = {a.x ^ 0x80808080u, a.y ^ 0x80808080u};
+        // the byte code + 128 under the exponent of 2^23 reads as 2^23 + 128 + code
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3)));
+        for (int i = 0; i < 8; ++i)
+            v[i] = __uint_as_float(__byte_perm(w[i >> 2], 0x4b000000u, 0x7440 | (i & 3))) - 8388736.0f;
     }
 }
 
-// 1 - erf(z) for z >= 0 as a polynomial in t = 1 / (1 + p z) times 2^(-z^2 log2 e)
-// (Abramowitz and Stegun 7.1.26, Hastings 1955: off by at most 1.5e-7; erff takes
-// about three times the instructions, and made the store bound by them).
-// `e` gets exp(-z^2).
-__device__ __forceinline__ float erfc_positive(float z, float& e) {
-    const float t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
-    e = exp2f(z * z * -1.4426950408889634f);
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
-    return p * t * e;
+__device__ __forceinline__ float ex2_ftz(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
-// x Phi(x): for x < 0 the tail itself, without a difference from 1.
-__device__ __forceinline__ float gelu(float x) {
-    float e;
-    const float h = 0.5f * erfc_positive(fabsf(x) * 0.70710678118654752f, e);
-    return x * (x < 0.0f ? h : 1.0f - h);
+__device__ __forceinline__ float rcp_ftz(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
-__device__ __forceinline__ float gelu_slope(float x) {
-    float e;
-    const float h = 0.5f * erfc_positive(fabsf(x) * 0.70710678118654752f, e);
-    const float tail = x * e * 0.39894228040143268f;
-    return (x < 0.0f ? h : 1.0f - h) + (e == 0.0f ? 0.0f : tail);
+
+// 1 - Phi(|x|) of two values, and e = exp(-x^2 / 2): half of 1 - erf(z), z = |x| /
+// sqrt(2), as a polynomial in t = 1 / (1 + p z) times exp(-z^2) (Abramowitz and
+// Stegun 7.1.26, Hastings 1955: 1 - erf off by at most 1.5e-7).  With erff the
+// activation took three quarters of the store's instructions; this is 8 an element,
+// two elements an instruction where the operation has such a form.
+__device__ __forceinline__ uint64_t upper_tail(float x0, float x1, float& a0, float& a1, float& e0,
+                                               float& e1) {
+    a0 = fabsf(x0);
+    a1 = fabsf(x1);
+    const uint64_t a = f2_pack(a0, a1);
+    const float pz = 0.3275911f * 0.70710678118654752f;
+    float d0, d1, q0, q1;
+    f2_unpack(f2_fma(a, f2_pack(pz, pz), f2_pack(1.0f, 1.0f)), d0, d1);
+    const float el = -0.5f * 1.4426950408889634f;
+    f2_unpack(f2_mul(f2_mul(a, a), f2_pack(el, el)), q0, q1);
+    e0 = ex2_ftz(q0);
+    e1 = ex2_ftz(q1);
+    const uint64_t t = f2_pack(rcp_ftz(d0), rcp_ftz(d1));
+    auto two = [](float c) { return f2_pack(c, c); };
+    uint64_t p = f2_fma(two(0.5f * 1.061405429f), t, two(0.5f * -1.453152027f));
+    p = f2_fma(p, t, two(0.5f * 1.421413741f));
+    p = f2_fma(p, t, two(0.5f * -0.284496736f));
+    p = f2_fma(p, t, two(0.5f * 0.254829592f));
+    return f2_mul(f2_mul(p, t), f2_pack(e0, e1));
+}
+// x Phi(x) = max(x, 0) - |x| (1 - Phi(|x|)): the negative side is the tail itself,
+// without a difference from 1.
+__device__ __forceinline__ void gelu2(float& x0, float& x1) {
+    float a0, a1, e0, e1;
+    const uint64_t h = upper_tail(x0, x1, a0, a1, e0, e1);
+    // (-inf, whose tail is 0, gives NaN as the formula does; a NaN stays one through h)
+    f2_unpack(f2_fma(f2_pack(-a0, -a1), h, f2_pack(fmaxf(x0, 0.0f), fmaxf(x1, 0.0f))), x0, x1);
+}
+__device__ __forceinline__ void slope2(float x0, float x1, float& s0, float& s1) {
+    float a0, a1, e0, e1, h0, h1;
+    f2_unpack(upper_tail(x0, x1, a0, a1, e0, e1), h0, h1);
+    const float c = 0.39894228040143268f;
+    s0 = (x0 < 0.0f ? h0 : 1.0f - h0) + (e0 == 0.0f ? 0.0f : x0 * (e0 * c));
+    s1 = (x1 < 0.0f ? h1 : 1.0f - h1) + (e1 == 0.0f ? 0.0f : x1 * (e1 * c));
+}
+template <int N>
+__device__ __forceinline__ void gelu_all(float (&v)[N]) {
+    if constexpr (N == 1) {
+        float other = 0.0f;
+        gelu2(v[0], other);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 2) gelu2(v[k], v[k + 1]);
+    }
+}
+template <int N>
+__device__ __forceinline__ void times_slope(float (&z)[N], const float (&g)[N]) {
+    float s[N + 1];
+#pragma unroll
+    for (int k = 0; k < N; k += 2) slope2(z[k], N == 1 ? 0.0f : z[k + 1], s[k], s[k + 1]);
+#pragma unroll
+    for (int k = 0; k < N; ++k) z[k] = g[k] * s[k];
+}
+
+// Codes of N values against scale s (r = RN(1 / s)), a byte each in the low bits
+// of c.  v r is within 2^-15 of v / s, so a product further than 2^-14 from every
+// half-integer rounds as the quotient does; a piece with a nearer one (one warp in
+// thirty) divides.  The sum with 1.5 2^23 leaves the code in its low byte.
+template <int N>
+__device__ __forceinline__ void codes_of(const float (&v)[N], float s, float r, bool fast,
+                                         uint32_t (&c)[N]) {
+    const float k = 12582912.0f;
+    float far = 0.0f;
+    if constexpr (N == 1) {
+        const float t = v[0] * r, f = t + k;
+        far = fabsf(t - (f - k));
+        c[0] = __float_as_uint(f);
+    } else {
+        const uint64_t r2 = f2_pack(r, r), k2 = f2_pack(k, k), m2 = f2_pack(-k, -k);
+        const uint64_t minus = f2_pack(-1.0f, -1.0f);
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const uint64_t t = f2_mul(f2_pack(v[i], v[i + 1]), r2), f = f2_add(t, k2);
+            float d0, d1, f0, f1;
+            f2_unpack(f2_fma(f2_add(f, m2), minus, t), d0, d1);
+            f2_unpack(f, f0, f1);
+            far = fmaxf(far, fmaxf(fabsf(d0), fabsf(d1)));
+            c[i] = __float_as_uint(f0);
+            c[i + 1] = __float_as_uint(f1);
+        }
+    }
+    if (!fast || !(far < 0.5f - 0x1p-14f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            c[i] = (uint32_t)(int)fminf(fmaxf(roundf(__fdiv_rn(v[i], s)), -127.0f), 127.0f);
+    }
 }
 
 // TPR threads per row hold it in registers: read once, the maximum, the codes, the
@@ -129,7 +218,6 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
     const bool live = row < rows;
     const int pieces = (cols + N - 1) / N;      // cols is a multiple of N
     float v[kPieces][N];
-    float top = 0.0f, nan = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         const int j = i * TPR + lane;
@@ -140,25 +228,23 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
             for (int k = 0; k < N; ++k) v[i][k] = 0.0f;
         }
     }
+    // the largest magnitude by its bits: infinities and NaN are above every number
+    uint32_t bits = 0;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            top = fmaxf(top, fabsf(v[i][k]));
-            nan += v[i][k] * 0.0f;              // NaN for a NaN or an infinity
-        }
-    if (nan != 0.0f) top = INFINITY;            // (NaN != 0)
-    top = warp_max(top);
+        for (int k = 0; k < N; ++k) bits = max(bits, __float_as_uint(v[i][k]) & 0x7fffffffu);
+    bits = __reduce_max_sync(0xffffffffu, bits);
     if constexpr (TPR > 32) {
-        __shared__ float tops[TPR / 32];
-        if (lane % 32 == 0) tops[lane / 32] = top;
+        __shared__ uint32_t tops[TPR / 32];
+        if (lane % 32 == 0) tops[lane / 32] = bits;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < TPR / 32; ++i) top = fmaxf(top, tops[i]);
+        for (int i = 0; i < TPR / 32; ++i) bits = max(bits, tops[i]);
     }
     if (!live) return;
-    const bool finite = top != INFINITY;
-    float s = top == 0.0f ? 1.0f : __fmul_rn(top, 1.0f / 127.0f);
+    const bool finite = bits < 0x7f800000u;
+    float s = bits == 0u ? 1.0f : __fmul_rn(__uint_as_float(bits), 1.0f / 127.0f);
     if (s == 0.0f) s = __uint_as_float(1u);
     const float r = __fdiv_rn(1.0f, s);
     const bool fast = s >= kFastScaleMin;
@@ -168,15 +254,11 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
         const int j = i * TPR + lane;
         if (j >= pieces) break;
         uint32_t c[N];
+        if (finite) {
+            codes_of<N>(v[i], s, r, fast, c);
+        } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            c[k] = 0;
-            if (finite) {
-                if (fast)
-                    code_of(v[i][k], s, r, c[k]);
-                else
-                    c[k] = (uint32_t)(int)fminf(fmaxf(roundf(__fdiv_rn(v[i][k], s)), -127.0f), 127.0f);
-            }
+            for (int k = 0; k < N; ++k) c[k] = 0;
         }
         int8_t* out = codes + row * ldc + (int64_t)j * N;
         if constexpr (N == 1) {
@@ -190,8 +272,7 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
             *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
         }
         if (act == PVS_ACT_GELU) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[i][k] = gelu(v[i][k]);
+            gelu_all<N>(v[i]);
             store_elements<TYPE, N>(y, row * ldy + (int64_t)j * N, v[i]);
         }
     }
@@ -219,8 +300,8 @@ __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__
         int col[kAhead];
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            const uint32_t i = i0 + a * 256;
-            if (i >= total) continue;
+            // (past the end: the first piece again, not stored)
+            const uint32_t i = i0 + a * 256 < total ? i0 + a * 256 : i0;
             const uint32_t r = (uint32_t)((i * m) >> 40);
             row[a] = row0 + r;
             col[a] = (int)(i - r * (uint32_t)pieces) * N;
@@ -230,12 +311,10 @@ __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__
         }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            if (i0 + a * 256 >= total) continue;
+            if (i0 + a * 256 >= total) break;
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                z[a][k] *= s[a];
-                if constexpr (DY) z[a][k] = g[a][k] * gelu_slope(z[a][k]);
-            }
+            for (int k = 0; k < N; ++k) z[a][k] *= s[a];
+            if constexpr (DY) times_slope<N>(z[a], g[a]);
             store_elements<TYPE, N>(out, row[a] * ldo + col[a], z[a]);
         }
     }

@@ -546,38 +546,68 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
 }
 
 // ---- sums over the splits ------------------------------------------------------
+// Four columns a thread; a block takes `per_block` rows, n / pieces by a product
+// (m = floor(2^40 / pieces) + 1, exact for n < 2^23 and pieces < 2^16).
 __global__ void __launch_bounds__(256) sum_slots_kernel(const float* __restrict__ slots, int splits,
                                                         int64_t slot_stride, int64_t ldslot,
-                                                        int64_t m, int n,
+                                                        int64_t rows, int n, int per_block,
+                                                        uint64_t m,
                                                         const float* __restrict__ alpha,
-                                                        float alpha0, void* out, int64_t ldout,
-                                                        int out_type) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= m * n) return;
-    const int64_t row = i / n;
-    const int col = (int)(i - row * n);
-    const float* p = slots + row * ldslot + col;
-    float s = 0.0f;
+                                                        float alpha0, void* __restrict__ out,
+                                                        int64_t ldout, int out_type) {
+    const int pieces = (n + 3) / 4;
+    const int64_t row0 = (int64_t)blockIdx.x * per_block;
+    const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
+    const float f = alpha ? alpha0 * __ldg(alpha) : alpha0;
+    for (uint32_t i = threadIdx.x; i < total; i += 256) {
+        const uint32_t r = (uint32_t)((i * m) >> 40);
+        const int64_t row = row0 + r;
+        const int col = (int)(i - r * (uint32_t)pieces) * 4;
+        // (a slot's rows are padded to eight columns)
+        const float* p = slots + row * ldslot + col;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-    for (int k = 0; k < splits; ++k) s += p[k * slot_stride];
-    s *= alpha ? alpha0 * __ldg(alpha) : alpha0;
-    const int64_t at = row * ldout + col;
-    if (out_type == PVS_F32)
-        static_cast<float*>(out)[at] = s;
-    else if (out_type == PVS_BF16)
-        static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(s);
-    else
-        static_cast<__half*>(out)[at] = __float2half_rn(s);
+        for (int k = 0; k < splits; ++k) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(p + k * slot_stride));
+            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+        }
+        s.x *= f, s.y *= f, s.z *= f, s.w *= f;
+        const int64_t at = row * ldout + col;
+        if (out_type == PVS_F32) {
+            float* o = static_cast<float*>(out) + at;
+            if (col + 4 <= n && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
+                *reinterpret_cast<float4*>(o) = s;
+            } else {
+                o[0] = s.x;
+                if (col + 1 < n) o[1] = s.y;
+                if (col + 2 < n) o[2] = s.z;
+                if (col + 3 < n) o[3] = s.w;
+            }
+        } else {
+            uint16_t* o = static_cast<uint16_t*>(out) + at;
+            const uint32_t lo = out_type == PVS_BF16 ? pack_bf16(s.x, s.y) : pack_f16(s.x, s.y);
+            const uint32_t hi = out_type == PVS_BF16 ? pack_bf16(s.z, s.w) : pack_f16(s.z, s.w);
+            if (col + 4 <= n && (reinterpret_cast<uintptr_t>(o) & 7u) == 0) {
+                *reinterpret_cast<uint2*>(o) = make_uint2(lo, hi);
+            } else {
+                o[0] = (uint16_t)lo;
+                if (col + 1 < n) o[1] = (uint16_t)(lo >> 16);
+                if (col + 2 < n) o[2] = (uint16_t)hi;
+                if (col + 3 < n) o[3] = (uint16_t)(hi >> 16);
+            }
+        }
+    }
 }
 
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
                              int64_t ldout, int out_type, cudaStream_t st) {
-    const int64_t blocks = (m * n + 255) / 256;
-    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    const int pieces = (n + 3) / 4;
+    const int per_block = std::max(1, 512 / pieces);
     count_launches(1);
-    sum_slots_kernel<<<(unsigned)blocks, 256, 0, st>>>(slots, splits, slot_stride, ldslot, m, n,
-                                                       alpha, alpha0, out, ldout, out_type);
+    sum_slots_kernel<<<(unsigned)((m + per_block - 1) / per_block), 256, 0, st>>>(
+        slots, splits, slot_stride, ldslot, m, n, per_block, (1ull << 40) / pieces + 1, alpha, alpha0,
+        out, ldout, out_type);
     return cudaGetLastError();
 }
 

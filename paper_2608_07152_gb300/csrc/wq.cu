@@ -315,32 +315,44 @@ __global__ void __launch_bounds__(256) wq_pack_kernel(const void* w, int64_t ldw
 #pragma unroll 2
         for (int b0 = 0; b0 < blocks; b0 += 2) {
             const int blk = b0 + (lane >> 4);
-            float v[8], top = 0.0f, nan = 0.0f;
+            float v[8];
             load_eight<WIDE>(w, dtype, at, blk * 128 + l * 8, cols, v);
+            // the largest magnitude by its bits: infinities and NaN are above every number
+            uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                nan += v[j] * 0.0f;                 // NaN for a NaN or an infinity
-                top = fmaxf(top, fabsf(v[j]));
-            }
-            if (nan != 0.0f) top = INFINITY;
+            for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
             for (int o = lanes / 2; o > 0; o >>= 1)
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
             if (blk >= blocks) continue;            // (the shuffles are done: half a warp stops)
             uint32_t sb = 0x3f80;                   // 1
-            if (top == INFINITY) {
+            if (top >= 0x7f800000u) {
                 sb = 0x7fff;                        // NaN
-            } else if (top > 0.0f) {
-                sb = __bfloat16_as_ushort(__float2bfloat16_rn(__fmul_rn(top, 1.0f / 7.0f)));
+            } else if (top != 0u) {
+                sb = __bfloat16_as_ushort(
+                    __float2bfloat16_rn(__fmul_rn(__uint_as_float(top), 1.0f / 7.0f)));
                 if (sb == 0) sb = 1;
             }
             const float s = __uint_as_float(sb << 16);
             uint32_t bits = 0x88888888u;
-            if (top != INFINITY) {
+            if (top < 0x7f800000u) {
+                // as in the 8-bit quantizer: w / s by a product, rounded by a sum that
+                // leaves q + 8 in the low bits, unless that is near a tie
+                const float r = __fdiv_rn(1.0f, s), k = 12582912.0f + 8.0f;
+                float far = 0.0f;
                 bits = 0;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int q = (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
-                    bits |= (uint32_t)(q + 8) << (4 * j);
+                    const float t = __fmul_rn(v[j], r), f = __fadd_rn(t, k);
+                    far = fmaxf(far, fabsf(__fsub_rn(t, __fsub_rn(f, k))));
+                    bits |= (__float_as_uint(f) & 15u) << (4 * j);
+                }
+                if (!(far < 0.5f - 0x1p-14f) || s < kFastScaleMin) {
+                    bits = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int q = (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
+                        bits |= (uint32_t)(q + 8) << (4 * j);
+                    }
                 }
             }
             const int64_t i = row * blocks + blk;

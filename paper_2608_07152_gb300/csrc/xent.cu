@@ -36,12 +36,44 @@ __device__ __forceinline__ float element(const void* p, int dtype, int64_t i) {
     return dtype == PVS_BF16 ? __uint_as_float((uint32_t)u << 16) : __half2float(__ushort_as_half(u));
 }
 
+// A lane's part of <x_row, w_y>, element by element or eight 16-bit ones at a time.
+__device__ float dot_any(const pvs_xent_args& a, int64_t row, int64_t y) {
+    float dot = 0.0f;
+#pragma unroll 4
+    for (int k = threadIdx.x & 31; k < a.dim; k += 32)
+        dot = fmaf(element(a.x, a.dtype, row * a.ldx + k), element(a.w, a.dtype, y * a.ldw + k), dot);
+    return dot;
+}
+__device__ float dot_wide(const pvs_xent_args& a, int64_t row, int64_t y) {
+    const uint4* x = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.ldx);
+    const uint4* w = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.w) + y * a.ldw);
+    float lo = 0.0f, hi = 0.0f;
+    auto add = [&](uint32_t u, uint32_t v) {
+        if (a.dtype == PVS_BF16) {
+            lo = fmaf(__uint_as_float(u << 16), __uint_as_float(v << 16), lo);
+            hi = fmaf(__uint_as_float(u & 0xffff0000u), __uint_as_float(v & 0xffff0000u), hi);
+        } else {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u));
+            const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&v));
+            lo = fmaf(p.x, q.x, lo);
+            hi = fmaf(p.y, q.y, hi);
+        }
+    };
+#pragma unroll 4
+    for (int k = threadIdx.x & 31; k < a.dim / 8; k += 32) {
+        const uint4 u = __ldg(x + k), v = __ldg(w + k);
+        add(u.x, v.x), add(u.y, v.y), add(u.z, v.z), add(u.w, v.w);
+    }
+    return lo + hi;
+}
+
 // ---- rows of the forward pass ------------------------------------------------------
 struct JoinArgs {
     const float2* part;          // [n][rows]: the tiles' (m, s), the target left out
     int64_t n;
     pvs_xent_args a;
     float k2;
+    bool wide;                   // 16-bit rows of whole, aligned eights
     float* loss;
     float4* stats;
 };
@@ -77,10 +109,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
         const int64_t at = (int64_t)blockIdx.x * R + i;
         const int64_t y = at < a.rows ? a.targets[at] : -1;
         float dot = 0.0f;
-        if (y >= 0 && y < a.items)
-            for (int k = threadIdx.x & 31; k < a.dim; k += 32)
-                dot = fmaf(element(a.x, a.dtype, at * a.ldx + k),
-                           element(a.w, a.dtype, y * a.ldw + k), dot);
+        if (y >= 0 && y < a.items) dot = j.wide ? dot_wide(a, at, y) : dot_any(a, at, y);
         dot = warp_sum(dot);
         if ((threadIdx.x & 31) == 0) dots[i] = dot;
     }
@@ -367,12 +396,11 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
         e = logits(kStats, g, p, a, x, w, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
-    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN * 2, a, a.scale * kLog2e, loss,
+    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN * 2, a, a.scale * kLog2e,
+                     !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
-    if (T >= 32 * dev.sms)
-        xent_join_kernel<32><<<(unsigned)((T + 31) / 32), 256, 0, st>>>(j);
-    else if (T >= 8 * dev.sms)
+    if (T >= 4 * dev.sms)
         xent_join_kernel<8><<<(unsigned)((T + 7) / 8), 256, 0, st>>>(j);
     else
         xent_join_kernel<1><<<(unsigned)T, 256, 0, st>>>(j);
