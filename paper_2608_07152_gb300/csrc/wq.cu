@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "../../include/head.h"
+#include "f32x2.cuh"
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
@@ -42,17 +43,14 @@ __device__ __forceinline__ void store_y(void* p, int dtype, int64_t i, float v) 
         static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
 
-// The bits of one bf16 part of x: parts 0, 1, .. are its leading 8 bits, the
-// next 8, ..; cut, not rounded, so that they add up to x.
-__device__ __forceinline__ uint32_t part_bits(float x, int part) {
+// The leading 8 bits of x as a bf16's bits, and what is left of it: cut, not rounded,
+// so that the parts add up to x.  Nothing is left of an infinity or a NaN.
+__device__ __forceinline__ uint32_t cut_part(float& x) {
     uint32_t h = __float_as_uint(x) & 0xffff0000u;
-    for (int i = 0; i < part; ++i) {
-        x = isfinite(x) ? x - __uint_as_float(h) : 0.0f;
-        h = __float_as_uint(x) & 0xffff0000u;
-    }
-    // a NaN whose payload is in the low bits stays one
-    if (x != x) h |= 0x00400000u;
-    return h >> 16;
+    const bool finite = h < 0x7f800000u || (h >= 0x80000000u && h < 0xff800000u);
+    if (x != x) h |= 0x00400000u;   // a NaN whose payload is in the low bits stays one
+    x = finite ? x - __uint_as_float(h) : 0.0f;
+    return h;
 }
 
 // Pair `m` of a word's nibbles, m and m + 4, as two bf16 codes in eighths: no
@@ -65,12 +63,53 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w, int m) {
     return r;
 }
 
+// The same from zero sums.
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                                uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                           uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
         "{%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Eight elements of a row from column k, zeros past the row: 16-byte loads where WIDE.
+template <bool WIDE>
+__device__ __forceinline__ void load_eight(const void* w, int dtype, int64_t at, int k, int cols,
+                                           float (&v)[8]) {
+    if (WIDE && k + 8 <= cols) {
+        if (dtype == PVS_F32) {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + at + k);
+            const float4 a = __ldg(p), b = __ldg(p + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+            v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a =
+                __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + at + k));
+            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t h = (u[j >> 1] >> (16 * (j & 1))) & 0xffffu;
+                v[j] = dtype == PVS_BF16 ? __uint_as_float(h << 16)
+                                         : __half2float(__ushort_as_half((uint16_t)h));
+            }
+        }
+        return;
+    }
+    if (k >= cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < cols ? load_x(w, dtype, at + k + j) : 0.0f;
 }
 
 struct WqArgs {
@@ -114,17 +153,63 @@ struct RowPair {
     }
 };
 
+// acc += the products of 16 rows by a block's 128 columns; x: the block's fragments.
+template <int NT, int GROUP, int RT>
+__device__ __forceinline__ void multiply(const RowPair<GROUP> (&w)[RT], const uint4* x,
+                                         float (&acc)[RT][NT][4]) {
+    constexpr int kWords = GROUP / 32;                // words of a group
+    float part[RT][NT][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 f[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) f[n] = x[(i * NT + n) * 32];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const uint32_t w0 = i == 0 ? w[r].w0.x : i == 1 ? w[r].w0.y : i == 2 ? w[r].w0.z : w[r].w0.w;
+            const uint32_t w1 = i == 0 ? w[r].w1.x : i == 1 ? w[r].w1.y : i == 2 ? w[r].w1.z : w[r].w1.w;
+            uint32_t p0[4], p1[4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                p0[m] = code_pair(w0, m);
+                p1[m] = code_pair(w1, m);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (i % kWords == 0)
+                    mma_16816_first(part[r][n], p0[0], p1[0], p0[1], p1[1], f[n].x, f[n].y);
+                else
+                    mma_16816(part[r][n], p0[0], p1[0], p0[1], p1[1], f[n].x, f[n].y);
+                mma_16816(part[r][n], p0[2], p1[2], p0[3], p1[3], f[n].z, f[n].w);
+            }
+            if (i % kWords == kWords - 1) {
+                const float f0 = RowPair<GROUP>::scale(w[r].s0, i / kWords);
+                const float f1 = RowPair<GROUP>::scale(w[r].s1, i / kWords);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    acc[r][n][0] = fmaf(f0, part[r][n][0], acc[r][n][0]);
+                    acc[r][n][1] = fmaf(f0, part[r][n][1], acc[r][n][1]);
+                    acc[r][n][2] = fmaf(f1, part[r][n][2], acc[r][n][2]);
+                    acc[r][n][3] = fmaf(f1, part[r][n][3], acc[r][n][3]);
+                }
+            }
+        }
+    }
+}
+
 // NT: 8 columns (parts of rows of x) each; GROUP: weights per scale; RT: tiles of 16
 // rows a warp takes at once, which share the x fragments it reads.
 // A warp's next block is loaded before it works on the present one.
 template <int NT, int GROUP, int RT>
-__global__ void __launch_bounds__(kWqThreads) wq_matvec_kernel(const WqArgs a) {
+__global__ void __launch_bounds__(kWqThreads, 2) wq_matvec_kernel(const WqArgs a) {
+    constexpr int kRowsAhead = 36;                    // a column's rows, apart in the banks
     extern __shared__ uint4 xf[];                     // [block][word][NT][lane]
-    __shared__ float out[kWqWarps][16][NT * 8 + 1];
+    __shared__ float out[kWqWarps][NT * 8][kRowsAhead];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
-    const int team = warp / a.kw, share = warp % a.kw;
-    const int teams = kWqWarps / a.kw;
+    const int kw = RT == 2 ? 1 : a.kw;                // (two tiles a warp: rows abound)
+    const int team = warp / kw, share = warp % kw;
+    const int teams = kWqWarps / kw;
     const int64_t code_row = (int64_t)a.blocks * 64;
     const int64_t scale_row = (int64_t)a.blocks * (128 / GROUP);
     const int64_t tiles = (a.rows + 16 * RT - 1) / (16 * RT);
@@ -138,121 +223,88 @@ __global__ void __launch_bounds__(kWqThreads) wq_matvec_kernel(const WqArgs a) {
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t row = min((tile * RT + r) * 16 + g + 8 * h, a.rows - 1);
+                const int64_t row = min(tile * (16 * RT) + r * 16 + g + 8 * h, a.rows - 1);
                 code[r][h] = a.codes + row * code_row + t * 16;
                 scale[r][h] = a.scales + row * scale_row;
             }
         float acc[RT][NT][4] = {};
         for (int c0 = 0; c0 < a.blocks; c0 += a.chunk) {
             const int c1 = min(c0 + a.chunk, a.blocks);
-            RowPair<GROUP> next[RT];
-            const bool mine = tile < tiles && c0 + share < c1;
-            if (mine) {
+            RowPair<GROUP> even[RT], odd[RT];
+            auto load = [&](RowPair<GROUP>(&w)[RT], int blk) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
-                    next[r].load(code[r][0], code[r][1], scale[r][0], scale[r][1], c0 + share);
-            }
+                    w[r].load(code[r][0], code[r][1], scale[r][0], scale[r][1], blk);
+            };
+            const bool mine = tile < tiles && c0 + share < c1;
+            if (mine) load(even, c0 + share);
             if (reload || !loaded) {
                 if (reload) __syncthreads();
-                for (int i = threadIdx.x; i < (c1 - c0) * 4 * NT * 32; i += kWqThreads) {
-                    const int l = i & 31, nt = (i >> 5) % NT, word = (i / (32 * NT)) & 3;
-                    const int blk = c0 + i / (128 * NT);
-                    const int col = nt * 8 + (l >> 2), b = col / a.parts, part = col % a.parts;
-                    const int k = blk * 128 + word * 32 + (l & 3) * 8;
-                    uint32_t h[8];
+                // eight elements of a row of x make an entry in each of its columns; the
+                // columns past the last hold anything, and so do their sums
+                const int eights = (c1 - c0) * 16;
+                for (int i = threadIdx.x; i < eights * a.batch; i += kWqThreads) {
+                    const int b = i / eights, k8 = i - b * eights;
+                    float v[8];
+                    load_eight<false>(a.x, a.dtype, b * a.ldx, (c0 * 16 + k8) * 8, a.cols, v);
+                    const int at = (k8 >> 2) * NT * 32 + (k8 & 3);   // [block, word][0][lane]
+                    for (int part = 0; part < a.parts; ++part) {
+                        uint32_t h[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        h[j] = b < a.batch && k + j < a.cols
-                                   ? part_bits(load_x(a.x, a.dtype, b * a.ldx + k + j), part)
-                                   : 0u;
-                    xf[i] = make_uint4(h[0] | (h[4] << 16), h[1] | (h[5] << 16),
-                                       h[2] | (h[6] << 16), h[3] | (h[7] << 16));
+                        for (int j = 0; j < 8; ++j) h[j] = cut_part(v[j]);
+                        const int col = b * a.parts + part;
+                        xf[at + (col >> 3) * 32 + (col & 7) * 4] =
+                            make_uint4(__byte_perm(h[0], h[4], 0x7632), __byte_perm(h[1], h[5], 0x7632),
+                                       __byte_perm(h[2], h[6], 0x7632), __byte_perm(h[3], h[7], 0x7632));
+                    }
                 }
                 __syncthreads();
                 loaded = true;
             }
             if (!mine) continue;
-            for (int blk = c0 + share; blk < c1; blk += a.kw) {
-                RowPair<GROUP> now[RT];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) now[r] = next[r];
-                const int after = min(blk + a.kw, c1 - 1);   // (past the end: read again, unused)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    next[r].load(code[r][0], code[r][1], scale[r][0], scale[r][1], after);
-                const uint4* xb = xf + (blk - c0) * 4 * NT * 32 + lane;
-                float part[RT][NT][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 x[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) x[n] = xb[(i * NT + n) * 32];
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const uint32_t w0 = i == 0   ? now[r].w0.x
-                                            : i == 1 ? now[r].w0.y
-                                            : i == 2 ? now[r].w0.z
-                                                     : now[r].w0.w;
-                        const uint32_t w1 = i == 0   ? now[r].w1.x
-                                            : i == 1 ? now[r].w1.y
-                                            : i == 2 ? now[r].w1.z
-                                                     : now[r].w1.w;
-                        if (i % (GROUP / 32) == 0) {
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                part[r][n][0] = part[r][n][1] = part[r][n][2] = part[r][n][3] = 0.0f;
-                        }
-                        uint32_t p0[4], p1[4];
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) {
-                            p0[m] = code_pair(w0, m);
-                            p1[m] = code_pair(w1, m);
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            mma_16816(part[r][n], p0[0], p1[0], p0[1], p1[1], x[n].x, x[n].y);
-                            mma_16816(part[r][n], p0[2], p1[2], p0[3], p1[3], x[n].z, x[n].w);
-                        }
-                        if (i % (GROUP / 32) == GROUP / 32 - 1) {
-                            const float f0 = RowPair<GROUP>::scale(now[r].s0, i / (GROUP / 32));
-                            const float f1 = RowPair<GROUP>::scale(now[r].s1, i / (GROUP / 32));
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) {
-                                acc[r][n][0] = fmaf(f0, part[r][n][0], acc[r][n][0]);
-                                acc[r][n][1] = fmaf(f0, part[r][n][1], acc[r][n][1]);
-                                acc[r][n][2] = fmaf(f1, part[r][n][2], acc[r][n][2]);
-                                acc[r][n][3] = fmaf(f1, part[r][n][3], acc[r][n][3]);
-                            }
-                        }
-                    }
-                }
+            const uint4* x = xf + share * (4 * NT * 32) + lane;
+            const int step = kw * (4 * NT * 32);
+            int blk = c0 + share;
+            while (true) {
+                // two blocks a turn, so that no registers are copied
+                int after = blk + kw;
+                if (after < c1) load(odd, after);
+                multiply<NT, GROUP, RT>(even, x, acc);
+                if (after >= c1) break;
+                x += step;
+                blk = after + kw;
+                if (blk < c1) load(even, blk);
+                multiply<NT, GROUP, RT>(odd, x, acc);
+                if (blk >= c1) break;
+                x += step;
             }
         }
-        // a row of y takes the sums of a team's warps, smallest parts first
+        // a row of y takes the sums of a team's warps, each with its smallest part first; a
+        // lone warp waits for no other
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                out[warp][g][n * 8 + 2 * t] = acc[r][n][0];
-                out[warp][g][n * 8 + 2 * t + 1] = acc[r][n][1];
-                out[warp][g + 8][n * 8 + 2 * t] = acc[r][n][2];
-                out[warp][g + 8][n * 8 + 2 * t + 1] = acc[r][n][3];
-            }
-            const bool alone = a.kw == 1;     // the warp's own sums: no other warp to wait for
-            if (alone) __syncwarp(); else __syncthreads();
-            const int first = alone ? lane : threadIdx.x, step = alone ? 32 : kWqThreads;
-            const int width = alone ? 16 : teams * 16;
-            for (int i = first; i < width * a.batch; i += step) {
-                const int q = i % width, b = i / width, tm = alone ? warp : q >> 4;
-                const int64_t row = ((t0 + tm) * RT + r) * 16 + (q & 15);
-                if (t0 + tm >= tiles || row >= a.rows) continue;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    out[warp][n * 8 + 2 * t + (j & 1)][r * 16 + g + 8 * (j >> 1)] = acc[r][n][j];
+        if (kw == 1) __syncwarp(); else __syncthreads();
+        const int64_t row = tile * (16 * RT) + lane;
+        if (share == 0 && lane < 16 * RT && tile < tiles && row < a.rows) {
+            const float* o = &out[warp][0][lane];
+            for (int b = 0; b < a.batch; ++b) {
                 float v = 0.0f;
-                for (int p = a.parts - 1; p >= 0; --p)
-                    for (int s = 0; s < a.kw; ++s) v += out[tm * a.kw + s][q & 15][b * a.parts + p];
+                for (int s = 0; s < kw; ++s) {
+                    const float* q = o + s * (NT * 8 * kRowsAhead);
+                    if (a.parts == 3) v += q[2 * kRowsAhead];
+                    if (a.parts >= 2) v += q[kRowsAhead];
+                    v += q[0];
+                }
+                o += a.parts * kRowsAhead;
                 store_y(a.y, a.dtype, b * a.ldy + row, 8.0f * v);
             }
-            if (alone) __syncwarp(); else __syncthreads();
         }
+        if (kw == 1) __syncwarp(); else __syncthreads();
     }
 }
 
@@ -274,143 +326,158 @@ cudaError_t launch_matvec(const WqArgs& a, int group, int grid, cudaStream_t st)
     return cudaGetLastError();
 }
 
-// Eight weights from column k, zeros past the row: 16-byte loads where WIDE.
-template <bool WIDE>
-__device__ __forceinline__ void load_eight(const void* w, int dtype, int64_t at, int k, int cols,
-                                           float (&v)[8]) {
-    if (WIDE && k + 8 <= cols) {
-        if (dtype == PVS_F32) {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + at + k);
-            const float4 a = __ldg(p), b = __ldg(p + 1);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-            v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        } else {
-            const uint4 a =
-                __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + at + k));
-            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t h = (u[j >> 1] >> (16 * (j & 1))) & 0xffffu;
-                v[j] = dtype == PVS_BF16 ? __uint_as_float(h << 16)
-                                         : __half2float(__ushort_as_half((uint16_t)h));
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = k + j < cols ? load_x(w, dtype, at + k + j) : 0.0f;
-}
+constexpr int kPackAhead = 4;    // steps whose loads are in flight together
 
 // A word (8 weights) per lane, two blocks of 128 a warp and step; a warp runs
-// along a row.  Word l of a block holds k = 8 l ..: group l / 4, byte 16 (l % 4) + 4 (l / 4).
+// along a row.  Word l of a block holds k = 8 l ..: group l / 4 of 32, byte 16 (l % 4) +
+// 4 (l / 4).  gs: log2 of the group.
 template <bool WIDE>
-__global__ void __launch_bounds__(256) wq_pack_kernel(const void* w, int64_t ldw, int64_t rows,
-                                                      int cols, int dtype, int group, int blocks,
-                                                      uint8_t* codes, uint16_t* scales) {
-    const int lane = threadIdx.x & 31, l = lane & 15;
-    const int lanes = group / 8;
+__global__ void __launch_bounds__(256) wq_pack_kernel(const void* __restrict__ w, int64_t ldw,
+                                                      int64_t rows, int cols, int dtype, int gs,
+                                                      int blocks, uint8_t* __restrict__ codes,
+                                                      uint16_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
+    const int lanes = 1 << (gs - 3);                // of a group
+    const int at_code = 16 * (l & 3) + 4 * (l >> 2);
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
          row += (int64_t)gridDim.x * 8) {
-        const int64_t at = row * ldw;
-#pragma unroll 2
-        for (int b0 = 0; b0 < blocks; b0 += 2) {
-            const int blk = b0 + (lane >> 4);
-            float v[8];
-            load_eight<WIDE>(w, dtype, at, blk * 128 + l * 8, cols, v);
-            // the largest magnitude by its bits: infinities and NaN are above every number
-            uint32_t top = 0;
+        for (int first = 0; first < blocks; first += 2 * kPackAhead) {
+            float ahead[kPackAhead][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-            for (int o = lanes / 2; o > 0; o >>= 1)
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (blk >= blocks) continue;            // (the shuffles are done: half a warp stops)
-            uint32_t sb = 0x3f80;                   // 1
-            if (top >= 0x7f800000u) {
-                sb = 0x7fff;                        // NaN
-            } else if (top != 0u) {
-                sb = __bfloat16_as_ushort(
-                    __float2bfloat16_rn(__fmul_rn(__uint_as_float(top), 1.0f / 7.0f)));
-                if (sb == 0) sb = 1;
-            }
-            const float s = __uint_as_float(sb << 16);
-            uint32_t bits = 0x88888888u;
-            if (top < 0x7f800000u) {
-                // as in the 8-bit quantizer: w / s by a product, rounded by a sum that
-                // leaves q + 8 in the low bits, unless that is near a tie
-                const float r = __fdiv_rn(1.0f, s), k = 12582912.0f + 8.0f;
-                float far = 0.0f;
-                bits = 0;
+            for (int i = 0; i < kPackAhead; ++i)
+                load_eight<WIDE>(w, dtype, row * ldw, (first + 2 * i + side) * 128 + l * 8, cols,
+                                 ahead[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float t = __fmul_rn(v[j], r), f = __fadd_rn(t, k);
-                    far = fmaxf(far, fabsf(__fsub_rn(t, __fsub_rn(f, k))));
-                    bits |= (__float_as_uint(f) & 15u) << (4 * j);
+            for (int i = 0; i < kPackAhead; ++i) {
+                if (first + 2 * i >= blocks) break;
+                const int blk = first + 2 * i + side;
+                float(&v)[8] = ahead[i];
+                // the largest magnitude by its bits: infinities and NaN are above every number
+                uint32_t top = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+                for (int o = lanes / 2; o > 0; o >>= 1)
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                uint32_t sb = 0x3f80;               // 1
+                if (top >= 0x7f800000u) {
+                    sb = 0x7fff;                    // NaN
+                } else if (top != 0u) {
+                    sb = __bfloat16_as_ushort(
+                        __float2bfloat16_rn(__fmul_rn(__uint_as_float(top), 1.0f / 7.0f)));
+                    if (sb == 0) sb = 1;
                 }
-                if (!(far < 0.5f - 0x1p-14f) || s < kFastScaleMin) {
-                    bits = 0;
+                const float s = __uint_as_float(sb << 16);
+                uint32_t bits = 0x88888888u;
+                if (top < 0x7f800000u) {
+                    // as in the 8-bit quantizer: w / s by a product, rounded by a sum that
+                    // leaves q + 8 in the low bits, unless that is near a tie; the sums'
+                    // bits times powers of 16 add up to the word and a constant (modulo 2^32)
+                    float r;
+                    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+                    const float k = 12582912.0f + 8.0f;
+                    const uint64_t r2 = f2_pack(r, r), k2 = f2_pack(k, k), m2 = f2_pack(-k, -k);
+                    const uint64_t minus = f2_pack(-1.0f, -1.0f);
+                    float far = 0.0f;
+                    bits = 0u - 0x4b400000u * 0x11111111u;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int q = (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
-                        bits |= (uint32_t)(q + 8) << (4 * j);
+                    for (int j = 0; j < 8; j += 2) {
+                        const uint64_t t = f2_mul(f2_pack(v[j], v[j + 1]), r2), f = f2_add(t, k2);
+                        float d0, d1, f0, f1;
+                        f2_unpack(f2_fma(f2_add(f, m2), minus, t), d0, d1);
+                        f2_unpack(f, f0, f1);
+                        far = fmaxf(far, fmaxf(fabsf(d0), fabsf(d1)));
+                        bits += (__float_as_uint(f0) << (4 * j)) + (__float_as_uint(f1) << (4 * j + 4));
+                    }
+                    if (!(far < 0.5f - 0x1p-14f) || s < kFastScaleMin) {
+                        bits = 0;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int q =
+                                (int)fminf(fmaxf(roundf(__fdiv_rn(v[j], s)), -7.0f), 7.0f);
+                            bits |= (uint32_t)(q + 8) << (4 * j);
+                        }
                     }
                 }
+                if (blk < blocks) {
+                    const int64_t n = row * blocks + blk;
+                    *reinterpret_cast<uint32_t*>(codes + n * 64 + at_code) = bits;
+                    if ((l & (lanes - 1)) == 0) scales[(n << (7 - gs)) + (l >> (gs - 3))] = (uint16_t)sb;
+                }
+                __syncwarp();
             }
-            const int64_t i = row * blocks + blk;
-            *reinterpret_cast<uint32_t*>(codes + i * 64 + 16 * (l & 3) + 4 * (l >> 2)) = bits;
-            if (l % lanes == 0) scales[i * (128 / group) + l / lanes] = (uint16_t)sb;
         }
-        __syncwarp();
     }
 }
 
 template <bool WIDE>
-__global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* codes,
-                                                        const uint16_t* scales, int64_t rows,
-                                                        int cols, int group, int blocks, void* out,
-                                                        int64_t ldo, int dtype) {
-    const int lane = threadIdx.x & 31, l = lane & 15;
+__global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* __restrict__ codes,
+                                                        const uint16_t* __restrict__ scales,
+                                                        int64_t rows, int cols, int gs, int blocks,
+                                                        void* __restrict__ out, int64_t ldo,
+                                                        int dtype) {
+    const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
+    const int at_code = 16 * (l & 3) + 4 * (l >> 2), at_scale = l >> (gs - 3);
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
          row += (int64_t)gridDim.x * 8) {
-#pragma unroll 4
-        for (int blk = lane >> 4; blk < blocks; blk += 2) {
-            const int64_t i = row * blocks + blk;
-            const uint32_t bits =
-                __ldg(reinterpret_cast<const uint32_t*>(codes + i * 64 + 16 * (l & 3) + 4 * (l >> 2)));
-            const float s =
-                __uint_as_float((uint32_t)__ldg(scales + i * (128 / group) + l * 8 / group) << 16);
-            const int k = blk * 128 + l * 8;
-            const int64_t at = row * ldo + k;
-            float v[8];
+        for (int first = 0; first < blocks; first += 2 * kPackAhead) {
+            uint32_t word[kPackAhead], unit[kPackAhead];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = s * (float)((int)((bits >> (4 * j)) & 15u) - 8);
-            if (WIDE && k + 8 <= cols) {
-                if (dtype == PVS_F32) {
-                    float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
-                    p[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    p[1] = make_float4(v[4], v[5], v[6], v[7]);
-                } else {
-                    uint32_t h[4];
+            for (int i = 0; i < kPackAhead; ++i) {
+                const int64_t n = row * blocks + min(first + 2 * i + side, blocks - 1);
+                word[i] = __ldg(reinterpret_cast<const uint32_t*>(codes + n * 64 + at_code));
+                unit[i] = __ldg(scales + (n << (7 - gs)) + at_scale);
+            }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (dtype == PVS_BF16) {
-                            const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-                            h[j] = *reinterpret_cast<const uint32_t*>(&p);
-                        } else {
-                            const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
-                            h[j] = *reinterpret_cast<const uint32_t*>(&p);
+            for (int i = 0; i < kPackAhead; ++i) {
+                const int k = (first + 2 * i + side) * 128 + l * 8;
+                if (k >= cols) continue;
+                const float s = __uint_as_float(unit[i] << 16);
+                // u under the exponent of 2^23 reads as 2^23 + u
+                float v[8];
+                const uint64_t s2 = f2_pack(s, s), k2 = f2_pack(-8388616.0f, -8388616.0f);
+#pragma unroll
+                for (int j = 0; j < 8; j += 2)
+                    f2_unpack(f2_mul(f2_add(f2_pack(__uint_as_float(((word[i] >> (4 * j)) & 15u) |
+                                                                    0x4b000000u),
+                                                    __uint_as_float(((word[i] >> (4 * j + 4)) & 15u) |
+                                                                    0x4b000000u)),
+                                            k2),
+                                     s2),
+                              v[j], v[j + 1]);
+                const int64_t at = row * ldo + k;
+                if (WIDE && k + 8 <= cols) {
+                    if (dtype == PVS_F32) {
+                        float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
+                        p[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        p[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    } else {
+                        uint32_t h[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (dtype == PVS_BF16) {
+                                const __nv_bfloat162 p =
+                                    __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                                h[j] = *reinterpret_cast<const uint32_t*>(&p);
+                            } else {
+                                const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+                                h[j] = *reinterpret_cast<const uint32_t*>(&p);
+                            }
                         }
+                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) =
+                            make_uint4(h[0], h[1], h[2], h[3]);
                     }
-                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) =
-                        make_uint4(h[0], h[1], h[2], h[3]);
-                }
-            } else {
+                } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k + j < cols) store_y(out, dtype, at + j, v[j]);
+                    for (int j = 0; j < 8; ++j)
+                        if (k + j < cols) store_y(out, dtype, at + j, v[j]);
+                }
             }
         }
     }
 }
+
+// log2 of a group of 32, 64 or 128.
+int group_shift(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
 // Whether every eight elements of a row from a multiple of eight are aligned.
 bool wide(const void* p, int64_t ld) {
@@ -451,9 +518,11 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
     uint16_t* s = static_cast<uint16_t*>(scales);
     count_launches(1);
     if (wide(w, ldw))
-        wq_pack_kernel<true><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group, blocks, codes, s);
+        wq_pack_kernel<true><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group_shift(group), blocks,
+                                                codes, s);
     else
-        wq_pack_kernel<false><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group, blocks, codes, s);
+        wq_pack_kernel<false><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group_shift(group), blocks,
+                                                codes, s);
     return queued(cudaGetLastError());
 }
 
@@ -469,10 +538,10 @@ extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, in
     const uint16_t* s = static_cast<const uint16_t*>(scales);
     count_launches(1);
     if (wide(out, ldout))
-        wq_unpack_kernel<true><<<grid, 256, 0, st>>>(codes, s, rows, cols, group, blocks, out, ldout,
+        wq_unpack_kernel<true><<<grid, 256, 0, st>>>(codes, s, rows, cols, group_shift(group), blocks, out, ldout,
                                                      dtype);
     else
-        wq_unpack_kernel<false><<<grid, 256, 0, st>>>(codes, s, rows, cols, group, blocks, out, ldout,
+        wq_unpack_kernel<false><<<grid, 256, 0, st>>>(codes, s, rows, cols, group_shift(group), blocks, out, ldout,
                                                       dtype);
     return queued(cudaGetLastError());
 }
@@ -515,7 +584,8 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
         a.y = static_cast<uint8_t*>(y) + (int64_t)b * ldy * es;
         const int nt = a.batch * a.parts > 8 ? 2 : 1;
         a.chunk = std::min(a.blocks, kWqSmem / (nt * kWqBlockBytes));
-        const int grid = (int)std::min<int64_t>(groups, 4ll * dev.sms);
+        // (as many blocks as run at once: each makes the fragments of x for itself)
+        const int grid = (int)std::min<int64_t>(groups, 2ll * dev.sms);
         e = nt == 1 ? (rt == 1 ? launch_matvec<1, 1>(a, group, grid, st)
                                : launch_matvec<1, 2>(a, group, grid, st))
                     : (rt == 1 ? launch_matvec<2, 1>(a, group, grid, st)
