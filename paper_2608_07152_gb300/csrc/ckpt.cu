@@ -372,8 +372,12 @@ pvs_status queued(cudaError_t e = cudaSuccess) {
     return PVS_ERR_CUDA;
 }
 
+// bf16: dy is an operand as it lies, and the kept rows the other, each a bf16.  f16
+// and float32: dy s in two or three bf16 parts, and the codes as they are (exact).
 struct GradPlan {
     int parts;
+    bool scaled;             // the kept rows are the operand, dy has no scale
+    bool copy;               // dy is copied
     int64_t lda, ldb;
     int splits;
     uint16_t *a, *b;
@@ -381,9 +385,11 @@ struct GradPlan {
     int64_t ldslot;
     size_t bytes;
 };
-GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, const Device& dev,
-                   void* workspace) {
+GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_place,
+                   const Device& dev, void* workspace) {
     GradPlan p{};
+    p.scaled = dtype == PVS_BF16;
+    p.copy = !p.scaled || !in_place;
     p.parts = dtype == PVS_BF16 ? 1 : dtype == PVS_F16 ? 2 : 3;
     p.lda = round_up(out_cols, 8);
     p.ldb = round_up(cols, 8);
@@ -399,7 +405,7 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, const Device
     if (dtype == PVS_F32) s = std::max<int64_t>(s, (kc + 31) / 32);
     p.splits = (int)s;
     Carver c{static_cast<uint8_t*>(workspace)};
-    p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
+    if (p.copy) p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
     p.b = c.take<uint16_t>(rows * p.ldb);
     if (p.splits > 1) p.slots = c.take<float>((int64_t)p.splits * out_cols * p.ldslot);
     p.bytes = c.used;
@@ -497,7 +503,7 @@ extern "C" pvs_status pvs_ckpt_grad_workspace(int64_t rows, int32_t out_cols, in
     Device dev;
     const cudaError_t e = device(&dev);
     if (e != cudaSuccess) return queued(e);
-    *bytes = grad_plan(rows, out_cols, cols, dtype, dev, nullptr).bytes;
+    *bytes = grad_plan(rows, out_cols, cols, dtype, false, dev, nullptr).bytes;
     return PVS_OK;
 }
 
@@ -518,24 +524,29 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     Device dev;
     cudaError_t e = device(&dev);
     if (e != cudaSuccess) return queued(e);
-    const GradPlan p = grad_plan(rows, out_cols, cols, dtype, dev, workspace);
+    const bool in_place = (reinterpret_cast<uintptr_t>(dy) & 15u) == 0 && lddy % 8 == 0;
+    const GradPlan p = grad_plan(rows, out_cols, cols, dtype, in_place, dev, workspace);
     if (workspace_bytes < p.bytes || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return PVS_ERR_INVALID;
     const pvs_status before = (pvs_status)take_status(dev);
     if (before != PVS_OK) return before;
-    SplitArgs s{};
-    s.src = dy;
-    s.ld = lddy;
-    s.rows = rows;
-    s.cols = out_cols;
-    s.dtype = dtype;
-    s.row_scale = scales;
-    s.dst = p.a;
-    s.ldd = p.lda;
-    s.part_stride = rows * p.lda;
-    s.parts = p.parts;
-    e = launch_split(s, st);
-    if (e == cudaSuccess) e = launch_split_codes(codes, ldcodes, rows, cols, p.b, p.ldb, st);
+    if (p.copy) {
+        SplitArgs s{};
+        s.src = dy;
+        s.ld = lddy;
+        s.rows = rows;
+        s.cols = out_cols;
+        s.dtype = dtype;
+        s.row_scale = p.scaled ? nullptr : scales;
+        s.dst = p.a;
+        s.ldd = p.lda;
+        s.part_stride = rows * p.lda;
+        s.parts = p.parts;
+        e = launch_split(s, st);
+    }
+    if (e == cudaSuccess)
+        e = launch_split_codes(codes, ldcodes, p.scaled ? scales : nullptr, rows, cols, p.b, p.ldb,
+                               st);
     if (e != cudaSuccess) return queued(e);
     Args g{};
     g.status = dev.status;
@@ -544,7 +555,9 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     g.cta = ctas_for(out_cols, dev);
     set_tiles(q, out_cols, cols, tile_columns(cols), rows, g.cta);
     q.splits = p.splits;
-    if (!operand_map(&q.a, Matrix{p.a, rows, out_cols, p.lda, p.parts, rows * p.lda}, true, 0) ||
+    const Matrix a = p.copy ? Matrix{p.a, rows, out_cols, p.lda, p.parts, rows * p.lda}
+                            : Matrix{dy, rows, out_cols, lddy, 1, 0};
+    if (!operand_map(&q.a, a, true, 0) ||
         !operand_map(&q.b, Matrix{p.b, rows, cols, p.ldb, 1, 0}, true, 0))
         return PVS_ERR_CUDA;
     q.a_mn = q.b_mn = 1;

@@ -618,75 +618,130 @@ __device__ __forceinline__ float load_as_float(const void* p, int dtype, int64_t
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// Eight consecutive elements per thread.
-__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a) {
+// Eight consecutive elements a thread, in one load (two of float32) where rows are
+// aligned; n / pieces by a product as in sum_slots_kernel.
+__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, int per_block, uint64_t m,
+                                                    int wide) {
     if (a.only_if && *a.only_if == 0) return;
-    const int64_t per_row = (a.cols + 7) / 8;
-    const int64_t total = a.rows * per_row, stride = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
-        const int64_t row = i / per_row;
-        const int col = (int)(i - row * per_row) * 8;
-        const bool zero = (a.zero_target && a.zero_target[row] == a.ignore_index) ||
-                          (a.zero_bias && a.zero_bias[row] == -INFINITY);
-        float v[8];
+    const int pieces = (a.cols + 7) / 8;
+    const int64_t step = (int64_t)gridDim.x * per_block;
+    for (int64_t row0 = (int64_t)blockIdx.x * per_block; row0 < a.rows; row0 += step) {
+        const uint32_t total = (uint32_t)(min((int64_t)per_block, a.rows - row0) * pieces);
+        for (uint32_t i = threadIdx.x; i < total; i += 256) {
+            const uint32_t r = (uint32_t)((i * m) >> 40);
+            const int64_t row = row0 + r;
+            const int col = (int)(i - r * (uint32_t)pieces) * 8;
+            const bool zero = (a.zero_target && a.zero_target[row] == a.ignore_index) ||
+                              (a.zero_bias && a.zero_bias[row] == -INFINITY);
+            const int64_t at = row * a.ld + col;
+            float v[8];
+            if (wide && col + 8 <= a.cols) {
+                if (a.dtype == PVS_F32) {
+                    const float4* p =
+                        reinterpret_cast<const float4*>(static_cast<const float*>(a.src) + at);
+                    const float4 x = __ldg(p), y = __ldg(p + 1);
+                    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                    v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+                } else {
+                    const uint4 x = __ldg(
+                        reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.src) + at));
+                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = !zero && col + k < a.cols ? load_as_float(a.src, a.dtype, row * a.ld + col + k)
-                                             : 0.0f;
-        if (a.row_scale) {
-            const float s = a.row_scale[row];
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t h = (u[k >> 1] >> (16 * (k & 1))) & 0xffffu;
+                        v[k] = a.dtype == PVS_BF16 ? __uint_as_float(h << 16)
+                                                   : __half2float(__ushort_as_half((uint16_t)h));
+                    }
+                }
+            } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = col + k < a.cols ? v[k] * s : 0.0f;
-        }
-        for (int part = 0; part < a.parts; ++part) {
-            uint32_t h[4];
+                for (int k = 0; k < 8; ++k)
+                    v[k] = col + k < a.cols ? load_as_float(a.src, a.dtype, at + k) : 0.0f;
+            }
+            if (zero) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                h[k] = part + 1 < a.parts ? cut_bf16(v[2 * k], v[2 * k + 1])
-                       : a.to_f16         ? pack_f16(v[2 * k], v[2 * k + 1])
-                                          : pack_bf16(v[2 * k], v[2 * k + 1]);
-            *reinterpret_cast<uint4*>(a.dst + part * a.part_stride + row * a.ldd + col) =
-                make_uint4(h[0], h[1], h[2], h[3]);
+                for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+            }
+            if (a.row_scale) {
+                const float s = a.row_scale[row];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = col + k < a.cols ? v[k] * s : 0.0f;
+            }
+            for (int part = 0; part < a.parts; ++part) {
+                uint32_t h[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    h[k] = part + 1 < a.parts ? cut_bf16(v[2 * k], v[2 * k + 1])
+                           : a.to_f16         ? pack_f16(v[2 * k], v[2 * k + 1])
+                                              : pack_bf16(v[2 * k], v[2 * k + 1]);
+                *reinterpret_cast<uint4*>(a.dst + part * a.part_stride + row * a.ldd + col) =
+                    make_uint4(h[0], h[1], h[2], h[3]);
+            }
         }
     }
 }
 
 cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
-    const int64_t total = a.rows * ((a.cols + 7) / 8);
-    if (total <= 0) return cudaSuccess;
-    const int64_t blocks = (total + 255) / 256;
+    if (a.rows <= 0) return cudaSuccess;
+    const int pieces = (a.cols + 7) / 8;
+    const int per_block = std::max(1, 512 / pieces);
+    const int wide = (reinterpret_cast<uintptr_t>(a.src) & 15u) == 0 && a.ld % 8 == 0;
+    const int64_t blocks = (a.rows + per_block - 1) / per_block;
+    // (a conditional copy mostly does nothing: few blocks)
+    const int64_t most = a.only_if ? 152 * 4 : 1 << 20;
     count_launches(1);
-    split_kernel<<<(unsigned)(blocks < 152 * 16 ? blocks : 152 * 16), 256, 0, st>>>(a);
+    split_kernel<<<(unsigned)std::min(blocks, most), 256, 0, st>>>(a, per_block,
+                                                                    (1ull << 40) / pieces + 1, wide);
     return cudaGetLastError();
 }
 
-// Int8 codes as bf16 (exact).
+// Eight codes a thread, in one load where rows are aligned.
 __global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restrict__ codes,
-                                                          int64_t ldc, int64_t rows, int cols,
+                                                          int64_t ldc,
+                                                          const float* __restrict__ scales,
+                                                          int64_t rows, int cols, int per_block,
+                                                          uint64_t m, int wide,
                                                           uint16_t* __restrict__ dst, int64_t ldd) {
-    const int64_t per_row = (cols + 7) / 8;
-    const int64_t total = rows * per_row, stride = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
-        const int64_t row = i / per_row;
-        const int col = (int)(i - row * per_row) * 8;
+    const int pieces = (cols + 7) / 8;
+    const int64_t row0 = (int64_t)blockIdx.x * per_block;
+    const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
+#pragma unroll 2
+    for (uint32_t i = threadIdx.x; i < total; i += 256) {
+        const uint32_t r = (uint32_t)((i * m) >> 40);
+        const int64_t row = row0 + r;
+        const int col = (int)(i - r * (uint32_t)pieces) * 8;
+        const int8_t* p = codes + row * ldc + col;
+        const float s = scales ? __ldg(scales + row) : 1.0f;
         float v[8];
+        if (wide && col + 8 <= cols) {
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+            const uint32_t w[2] = {u.x ^ 0x80808080u, u.y ^ 0x80808080u};
+            // the byte code + 128 under the exponent of 2^23 reads as 2^23 + 128 + code
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = col + k < cols ? (float)codes[row * ldc + col + k] : 0.0f;
+            for (int k = 0; k < 8; ++k)
+                v[k] = __uint_as_float(__byte_perm(w[k >> 2], 0x4b000000u, 0x7440 | (k & 3))) -
+                       8388736.0f;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? (float)p[k] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? v[k] * s : 0.0f;
         *reinterpret_cast<uint4*>(dst + row * ldd + col) =
             make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
                        pack_bf16(v[6], v[7]));
     }
 }
 
-cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, int64_t rows, int cols,
-                               uint16_t* dst, int64_t ldd, cudaStream_t st) {
-    const int64_t total = rows * ((cols + 7) / 8);
-    if (total <= 0) return cudaSuccess;
-    const int64_t blocks = (total + 255) / 256;
+cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows,
+                               int cols, uint16_t* dst, int64_t ldd, cudaStream_t st) {
+    if (rows <= 0) return cudaSuccess;
+    const int pieces = (cols + 7) / 8;
+    const int per_block = std::max(1, 512 / pieces);
+    const int wide = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 8 == 0;
     count_launches(1);
-    split_codes_kernel<<<(unsigned)(blocks < 152 * 16 ? blocks : 152 * 16), 256, 0, st>>>(
-        codes, ldc, rows, cols, dst, ldd);
+    split_codes_kernel<<<(unsigned)((rows + per_block - 1) / per_block), 256, 0, st>>>(
+        codes, ldc, scales, rows, cols, per_block, (1ull << 40) / pieces + 1, wide, dst, ldd);
     return cudaGetLastError();
 }
 

@@ -153,8 +153,9 @@ struct SplitArgs {
     int parts, to_f16;
 };
 cudaError_t launch_split(const SplitArgs& a, cudaStream_t st);
-cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, int64_t rows, int cols,
-                               uint16_t* dst, int64_t ldd, cudaStream_t st);
+// Codes as bf16 (exact), or times their rows' scales, rounded to bf16.
+cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows,
+                               int cols, uint16_t* dst, int64_t ldd, cudaStream_t st);
 
 // A product's tiles; splits and everything else are the caller's.
 inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k, int cta) {
