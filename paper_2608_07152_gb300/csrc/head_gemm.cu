@@ -146,6 +146,15 @@ __device__ __forceinline__ uint32_t cut_bf16(float& lo, float& hi) {
     return (l >> 16) | h;
 }
 
+template <int kCta>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc,
+                                    uint32_t acc) {
+    if constexpr (kCta == 2)
+        tc::mma_f16_pair(d, ad, bd, idesc, acc);
+    else
+        tc::mma_bf16(d, ad, bd, idesc, acc);
+}
+
 // The units of one slot (a CTA, or a pair): those of one problem, a stride apart.
 struct Walk {
     int prob, first, step, end;
@@ -309,6 +318,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             const uint32_t idesc = (a.f16 ? tc::idesc_f16_f32(kTileM * kCta, p.bn)
                                           : tc::idesc_bf16_f32(kTileM * kCta, p.bn)) |
                                    ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16);
+            // the first stage's descriptors, and their steps of 16 of k (32 bytes, or two
+            // atoms): one thread issues every MMA, and has 128 cycles for each
+            const uint32_t s0 = smem_u32(stages);
+            const uint64_t a0 = p.a_mn ? smem_desc_sw128_mn(s0) : tc::smem_desc_sw128_kmajor(s0);
+            const uint64_t b0 = p.b_mn ? smem_desc_sw128_mn(s0 + kStageA)
+                                       : tc::smem_desc_sw128_kmajor(s0 + kStageA);
+            const uint64_t astep = p.a_mn ? 128 : 2, bstep = p.b_mn ? 128 : 2;
             uint32_t g = 0;
             int it = 0;
             for (int u = walk.first; u < walk.end && !abort_set(sh); u += walk.step, ++it) {
@@ -322,6 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 const uint32_t d = tmem + (uint32_t)(b * kTileN);
                 uint32_t acc = 0;
                 const int chunks = a.npairs * (w.k1 - w.k0);
+                int in_k = w.k0;
+                const bool tail = w.k1 == p.kchunks && p.ktail < kTileK / 16;
                 for (int kc = 0; kc < chunks; ++kc, ++g) {
                     const int s = g % R::kStages;
                     if (!mbar_wait(&sh.full[s], (g / R::kStages) & 1u)) {
@@ -329,19 +347,21 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                         break;
                     }
                     tc::fence_after_sync();
-                    const uint32_t sa = smem_u32(stages + s * R::kStageBytes);
-                    const uint32_t sb = sa + kStageA;
+                    const uint32_t off = (uint32_t)(s * R::kStageBytes) >> 4;
+                    uint64_t ad = a0 + off, bd = b0 + off;
+                    if (++in_k == w.k1) in_k = w.k0;
+                    if (tail && in_k == w.k0) {
+                        // the last chunk's steps past k multiply zeros: left out
+                        for (int k = 0; k < p.ktail; ++k, ad += astep, bd += bstep) {
+                            mma<kCta>(d, ad, bd, idesc, acc);
+                            acc = 1;
+                        }
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < kTileK / 16; ++k) {
-                        const uint64_t ad = p.a_mn ? smem_desc_sw128_mn(sa + k * 2048)
-                                                   : tc::smem_desc_sw128_kmajor(sa + k * 32);
-                        const uint64_t bd = p.b_mn ? smem_desc_sw128_mn(sb + k * 2048)
-                                                   : tc::smem_desc_sw128_kmajor(sb + k * 32);
-                        if (kCta == 2)
-                            tc::mma_f16_pair(d, ad, bd, idesc, acc);
-                        else
-                            tc::mma_bf16(d, ad, bd, idesc, acc);
-                        acc = 1;
+                        for (int k = 0; k < kTileK / 16; ++k, ad += astep, bd += bstep) {
+                            mma<kCta>(d, ad, bd, idesc, acc);
+                            acc = 1;
+                        }
                     }
                     if (kCta == 2)
                         tc::commit_pair(&sh.empty[s]);   // the stage is free in both CTAs

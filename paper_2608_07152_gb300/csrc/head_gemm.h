@@ -44,6 +44,7 @@ struct Problem {
     int bn;                      // columns per tile: a multiple of 32, <= kTileN
     int mtiles, ntiles, splits;
     int kchunks;                 // chunks of kTileK for one pair of parts
+    int ktail;                   // steps of 16 in the last of them
     int a_mo, a_ko, b_no, b_ko;  // where D's corner lies in the operands
     int alt_no, alt_ko;          // the same in b_alt
     int m_fast;                  // units run over m first (else n first)
@@ -165,6 +166,7 @@ inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k, int c
     p.mtiles = (int)((m + kTileM * cta - 1) / (kTileM * cta));
     p.ntiles = (int)((n + bn - 1) / bn);
     p.kchunks = (int)((k + kTileK - 1) / kTileK);
+    p.ktail = (int)((k - (int64_t)(p.kchunks - 1) * kTileK + 15) / 16);
     p.splits = 1;
 }
 

@@ -27,8 +27,11 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
-constexpr size_t kGradBytes = (size_t)256 << 20;    // G of a piece, at most about
-constexpr size_t kPartsBytes = (size_t)256 << 20;   // copies of a piece of w, at most about
+// G of a piece, and copies of a piece of w, at most about: a piece costs two launches and
+// their uneven ends, and the sums of dx one pass over its splits.  A step of 256 rows
+// over a million items took 2.5 ms in pieces of 32 K items, 1.6 ms in 256 K ones.
+constexpr size_t kGradBytes = (size_t)1 << 30;
+constexpr size_t kPartsBytes = (size_t)1 << 30;
 
 __device__ __forceinline__ float element(const void* p, int dtype, int64_t i) {
     if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
@@ -230,7 +233,7 @@ struct Plan {
     int64_t pieces = 0;
     int64_t ldg = 0;
     int bnd = 0;                // columns per tile of the gradients
-    int xsplits = 1, wsplits = 1;
+    int xsplits = 1, wsplits = 1, slots0 = 0;
     // workspace
     uint16_t *x = nullptr, *w = nullptr, *g = nullptr;
     float2* part = nullptr;
@@ -253,10 +256,48 @@ bool valid(const pvs_xent_args* a) {
     return a->w && (a->rows == 0 || (a->x && a->targets));
 }
 
-// splits of a product's k so that a unit is about `target` chunks long
-int splits_of(int64_t kchunks, int64_t target) {
-    const int64_t s = (kchunks + target - 1) / target;
-    return (int)(s < 1 ? 1 : s > kchunks ? kchunks : s);
+// How dx (u0 tiles, k0 chunks of k) and dw (u1, k1) share the `slots` CTAs or pairs
+// of one launch: each gets slots of its own, and its k is cut where that evens the
+// ends.  The cost of a choice, in the time of a chunk's MMAs (npairs of them a
+// chunk), is the longer side's rounds of units, a unit taking its chunks or its
+// epilogue, whichever is longer (measured: about 3 chunks' time, 6 for float32 sums
+// that splits leave), and what the splits' sums move.
+struct Division {
+    int xsplits = 1, wsplits = 1, slots0 = 1;
+};
+Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int npairs,
+                int64_t most_chunks, bool accumulate) {
+    Division best;
+    double least = 1e300;
+    const double sum = 2.0 * 6 / slots;           // a split tile's store and its later read
+    for (int64_t wsplits = 1; wsplits <= 16 && wsplits <= k1; wsplits *= 2) {
+        if (wsplits > 1 && u1 * wsplits > 8 * slots) break;
+        if (k1 > most_chunks * wsplits && 2 * wsplits <= 16 && 2 * wsplits <= k1) continue;
+        const double w1 = std::max<double>((double)((k1 + wsplits - 1) / wsplits) * npairs, wsplits > 1 ? 6 : 3);
+        const int64_t n1 = u1 * wsplits;
+        // (every split up to 8, then in steps of a quarter to an eighth)
+        for (int64_t xsplits = 1; xsplits <= k0 && (xsplits == 1 || u0 * xsplits <= 8 * slots);
+             xsplits += std::max<int64_t>(1, xsplits / 8)) {
+            const int64_t len = (k0 + xsplits - 1) / xsplits;
+            if (len > most_chunks && xsplits < k0 && u0 * (xsplits + 1) <= 8 * slots) continue;
+            const double w0 = std::max<double>((double)len * npairs, xsplits > 1 || accumulate ? 6 : 3);
+            const int64_t n0 = u0 * xsplits;
+            const int p = (int)(slots * (n0 * w0) / (n0 * w0 + n1 * w1) + 0.5);
+            for (int s0 = std::max(1, p - 1); s0 <= std::min(slots - 1, p + 1); ++s0) {
+                const double t0 = (double)((n0 + s0 - 1) / s0) * w0;
+                const double t1 = (double)((n1 + slots - s0 - 1) / (slots - s0)) * w1;
+                const double cost = std::max(t0, t1) +
+                                    sum * ((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0));
+                if (cost < least) {
+                    least = cost;
+                    best.xsplits = (int)xsplits;
+                    best.wsplits = (int)wsplits;
+                    best.slots0 = s0;
+                }
+            }
+        }
+    }
+    return best;
 }
 
 Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace) {
@@ -292,15 +333,17 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         p.bnd = tile_columns(a.dim);
         const int64_t first = std::min(piece, V);
         const int64_t nt = (a.dim + p.bnd - 1) / p.bnd;
-        const int64_t ux = (T + kTileM - 1) / kTileM * nt, kx = (first + kTileK - 1) / kTileK;
-        const int64_t uw = (first + kTileM - 1) / kTileM * nt, kw = (T + kTileK - 1) / kTileK;
-        // units about a quarter of an SM's share, and not under 16 chunks
-        int64_t target = std::max<int64_t>(16, (ux * kx + uw * kw) / (4 * dev.sms));
+        const int cta = ctas_for(std::max(T, first), dev);
+        const int tile = kTileM * cta;
         // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 128
         // steps at most before the splits are added with rounding
-        if (a.dtype == PVS_F32) target = std::min<int64_t>(target, 32);
-        p.xsplits = splits_of(kx, target);
-        p.wsplits = kw > 2 * target ? splits_of(kw, target) : 1;
+        const Division s = divide((T + tile - 1) / tile * nt, (first + kTileK - 1) / kTileK,
+                                  (first + tile - 1) / tile * nt, (T + kTileK - 1) / kTileK,
+                                  cta == 2 ? dev.pairs : dev.sms, a.dtype == PVS_F32 ? 6 : 1,
+                                  a.dtype == PVS_F32 ? 32 : INT64_MAX / 64, p.pieces > 1);
+        p.xsplits = s.xsplits;
+        p.wsplits = s.wsplits;
+        p.slots0 = s.slots0;
         if (p.xsplits > 1 || p.pieces > 1)
             p.xslots = c.take<float>((int64_t)p.xsplits * T * p.ldp);
         if (p.wsplits > 1) p.wslots = c.take<float>((int64_t)p.wsplits * first * p.ldp);
@@ -502,6 +545,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             qw = &q;
         }
         if (g.nprob == 0) break;
+        if (n == std::min(p.piece, V)) g.slots0 = p.slots0;   // (the last piece: by its work)
         part_pairs(g, p.parts, p.parts);
         e = launch_gemm(kOut, g, dev, st);
         if (e == cudaSuccess && qw && qw->to_slots)
