@@ -403,7 +403,7 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     int64_t s = std::max<int64_t>(1, std::min<int64_t>(slots / std::min<int64_t>(units, slots), kc / 8));
     // float32 sums: 128 steps at most before the splits are added with rounding
     if (dtype == PVS_F32) s = std::max<int64_t>(s, (kc + 31) / 32);
-    p.splits = (int)s;
+    p.splits = even_splits(kc, s);
     Carver c{static_cast<uint8_t*>(workspace)};
     if (p.copy) p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
     p.b = c.take<uint16_t>(rows * p.ldb);

@@ -47,13 +47,14 @@ template <int kCta> struct Ring {
     static constexpr int kStages = kCta == 2 ? 6 : 4;
 };
 constexpr int kMaxStages = 6;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 8;     // two to a TMEM lane quarter (four were no faster)
 constexpr int kEpiThreads = kEpiWarps * 32;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
-static_assert(kEpiThreads == kTileN, "an epilogue thread stages one column's bias");
+constexpr int kEpiGroups = kEpiWarps / 4;
+static_assert(kEpiThreads >= kTileN, "an epilogue thread stages one column's bias");
 
 struct Shared {
     uint64_t full[kMaxStages];
@@ -64,6 +65,7 @@ struct Shared {
     int abort;
     uint32_t masked[2][kTileN / 32];     // items of the tile outside the softmax
     alignas(16) float b2[2][kTileN];     // their biases, in powers of two
+    float2 rowstat[2][kEpiGroups][kTileM];   // a tile's statistics, by the warps' shares of it
 };
 
 template <int kCta>
@@ -155,37 +157,67 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t ad, uint64_t bd, uint32
         tc::mma_bf16(d, ad, bd, idesc, acc);
 }
 
-// The units of one slot (a CTA, or a pair): those of one problem, a stride apart.
-struct Walk {
-    int prob, first, step, end;
-};
-__device__ __forceinline__ Walk walk_of(const Args& a, int slot, int nslots) {
-    if (a.nprob == 1) return Walk{0, slot, nslots, a.p[0].units};
-    if (slot < a.slots0) return Walk{0, slot, a.slots0, a.p[0].units};
-    return Walk{1, slot - a.slots0, nslots - a.slots0, a.p[1].units};
-}
+// The units of one slot (a CTA, or a pair): those of one problem, `step` apart.  A unit
+// is a tile and a range of k; the next one is found by additions with carries (its
+// division by the tiles, in each of the three roles, cost a short unit as much as its
+// MMAs).
+struct Units {
+    int prob, left;              // units still to come, this one included
+    int mt, nt, split, k0, k1;   // this unit
+    int a, b;                    // the faster and the slower tile index
+    int na, nb, sa, sb, ss;      // their extents, and the step in them and in the splits
+    int length, chunks;
+    bool m_fast;
 
-// A unit's tile and range of k.
-struct Unit {
-    int mt, nt, split, k0, k1;
-};
-__device__ __forceinline__ Unit unit_of(const Problem& p, int u) {
-    Unit w;
-    if (p.m_fast) {
-        w.mt = u % p.mtiles;
-        u /= p.mtiles;
-        w.nt = u % p.ntiles;
-        w.split = u / p.ntiles;
-    } else {
-        w.nt = u % p.ntiles;
-        u /= p.ntiles;
-        w.mt = u % p.mtiles;
-        w.split = u / p.mtiles;
+    __device__ __forceinline__ Units(const Args& args, int slot, int nslots) {
+        prob = 0;
+        int step = nslots;
+        if (args.nprob > 1) {
+            if (slot < args.slots0) {
+                step = args.slots0;
+            } else {
+                prob = 1;
+                slot -= args.slots0;
+                step = nslots - args.slots0;
+            }
+        }
+        const Problem& p = args.p[prob];
+        left = slot < p.units ? (p.units - slot + step - 1) / step : 0;
+        m_fast = p.m_fast;
+        na = m_fast ? p.mtiles : p.ntiles;
+        nb = m_fast ? p.ntiles : p.mtiles;
+        a = slot % na;
+        b = slot / na % nb;
+        split = slot / na / nb;
+        sa = step % na;
+        sb = step / na % nb;
+        ss = step / na / nb;
+        length = p.klength;
+        chunks = p.kchunks;
+        place();
     }
-    w.k0 = (int)((int64_t)p.kchunks * w.split / p.splits);
-    w.k1 = (int)((int64_t)p.kchunks * (w.split + 1) / p.splits);
-    return w;
-}
+    __device__ __forceinline__ void place() {
+        mt = m_fast ? a : b;
+        nt = m_fast ? b : a;
+        k0 = split * length;
+        k1 = min(k0 + length, chunks);
+    }
+    __device__ __forceinline__ void next() {
+        --left;
+        a += sa;
+        b += sb;
+        split += ss;
+        if (a >= na) {
+            a -= na;
+            ++b;
+        }
+        if (b >= nb) {
+            b -= nb;
+            ++split;
+        }
+        place();
+    }
+};
 
 // 32 float32 values of one row to `out` of any type: whole sectors where the
 // row is aligned, else one by one.  `valid` of them exist.
@@ -220,6 +252,22 @@ __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const
     }
 }
 
+// A tile's statistics of one row, from its shares, in their order.
+__device__ __forceinline__ void write_stats(const float2 (&share)[kEpiGroups][kTileM],
+                                            const Softmax& sm, int at, int row, int row_in_tile) {
+    if (row >= sm.rows) return;
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kEpiGroups; ++g) m = fmaxf(m, share[g][row_in_tile].x);
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int g = 0; g < kEpiGroups; ++g) {
+        const float2 p = share[g][row_in_tile];
+        s += p.y * ex2(p.x - ref);
+    }
+    sm.part[(int64_t)at * sm.rows + row] = make_float2(m, s);
+}
+
 template <int EPI, int kCta>
 __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ Args a) {
     using R = Ring<kCta>;
@@ -232,8 +280,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int crank = kCta == 2 ? (int)cluster_ctarank() : 0;
     const bool leader = crank == 0;
-    const Walk walk = walk_of(a, blockIdx.x / kCta, gridDim.x / kCta);
-    const Problem& p = a.p[walk.prob];
+    Units w(a, blockIdx.x / kCta, gridDim.x / kCta);
+    const Problem& p = a.p[w.prob];
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < R::kStages; ++s) {
@@ -270,8 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             // the bytes of a stage, of both CTAs
             const uint32_t bytes =
                 kCta * (kStageA + (uint32_t)(p.b_mn ? nbox * 64 : bhalf) * kTileK * 2u);
-            for (int u = walk.first; u < walk.end && !abort_set(sh); u += walk.step) {
-                const Unit w = unit_of(p, u);
+            for (; w.left > 0 && !abort_set(sh); w.next()) {
                 const int am = p.a_mo + (w.mt * kCta + crank) * kTileM;
                 const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn + crank * bhalf;
                 const int bk = alt ? p.alt_ko : p.b_ko;
@@ -327,8 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             const uint64_t astep = p.a_mn ? 128 : 2, bstep = p.b_mn ? 128 : 2;
             uint32_t g = 0;
             int it = 0;
-            for (int u = walk.first; u < walk.end && !abort_set(sh); u += walk.step, ++it) {
-                const Unit w = unit_of(p, u);
+            for (; w.left > 0 && !abort_set(sh); w.next(), ++it) {
                 const int b = it & 1;
                 if (!mbar_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u)) {
                     raise_abort(sh, a.status);
@@ -384,15 +430,16 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     } else {
         // ---------------- epilogue ----------------
         const int quarter = warp & 3;            // TMEM lanes 32 * quarter ..
-        const int half = (warp - 2) >> 2;        // this warp's chunks of 32 columns
+        const int group = (warp - 2) >> 2;       // this warp's chunks of 32 columns
         const int et = threadIdx.x - 64;
         const int row_in_tile = quarter * 32 + lane;
         const Softmax& sm = a.sm;
         const uint32_t tempty_at[2] = {kCta == 2 ? cluster_map(&sh.tempty[0], 0) : 0u,
                                        kCta == 2 ? cluster_map(&sh.tempty[1], 0) : 0u};
         int it = 0;
-        for (int u = walk.first; u < walk.end; u += walk.step, ++it) {
-            const Unit w = unit_of(p, u);
+        [[maybe_unused]] int part_at = 0, row_before = 0;
+        bool dead = false;
+        for (; w.left > 0; w.next(), ++it) {
             const int b = it & 1;
             const int row = (w.mt * kCta + crank) * kTileM + row_in_tile;
             const int n0 = w.nt * p.bn;
@@ -409,9 +456,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     if (isfinite(bv)) bv = fminf(fmaxf(bv * kLog2e, -3.402823466e38f), 3.402823466e38f);
                 }
                 if (et >= ncols) bv = -INFINITY;
-                sh.b2[b][et] = bv;
                 const uint32_t mask = __ballot_sync(0xffffffffu, bv == -INFINITY);
-                if (lane == 0) sh.masked[b][et >> 5] = mask;
+                if (et < kTileN) {
+                    sh.b2[b][et] = bv;
+                    if (lane == 0) sh.masked[b][et >> 5] = mask;
+                }
                 if constexpr (EPI == kStats) {
                     if (row < sm.rows) y = __ldg(sm.targets + row) - (sm.item0 + n0);
                 } else {
@@ -424,16 +473,29 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 }
                 __syncwarp();
                 asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
+                if constexpr (EPI == kStats) {
+                    // the tile before this one: all its shares are in shared memory
+                    if (it > 0 && group == 0)
+                        write_stats(sh.rowstat[b ^ 1], sm, part_at, row_before, row_in_tile);
+                    part_at = sm.part0 + w.nt;
+                    row_before = row;
+                }
             }
-            if (!mbar_wait(&sh.tfull[b], (uint32_t)(it >> 1) & 1u)) {
-                raise_abort(sh, a.status);
-                break;
+            // after a wait that ran out, the warps still meet at every barrier
+            if (!dead) {
+                bool late = abort_set(sh);
+                if (!late && !mbar_wait(&sh.tfull[b], (uint32_t)(it >> 1) & 1u)) {
+                    raise_abort(sh, a.status);
+                    late = true;
+                }
+                dead = __any_sync(0xffffffffu, late);
             }
+            if (dead) continue;
             tc::fence_after_sync();
             const uint32_t tcol =
                 tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * kTileN);
             [[maybe_unused]] float mx = -INFINITY, sum = 0.0f;
-            for (int cc = half; cc * 32 < p.bn; cc += 2) {
+            for (int cc = group; cc * 32 < p.bn; cc += kEpiGroups) {
                 uint32_t r[32];
                 __syncwarp();
                 tc::ld_32x32b_x32(tcol + (uint32_t)(cc * 32), r);
@@ -539,11 +601,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     }
                 }
             }
-            if constexpr (EPI == kStats) {
-                if (row < sm.rows)
-                    sm.part[(int64_t)(sm.part0 + w.nt * 2 + half) * sm.rows + row] =
-                        make_float2(mx, sum);
-            }
+            if constexpr (EPI == kStats)
+                sh.rowstat[b][group][row_in_tile] = make_float2(mx, sum);
             tc::fence_before_sync();
             __syncwarp();
             if (lane == 0) {
@@ -552,6 +611,12 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 else
                     mbar_arrive(&sh.tempty[b]);
             }
+        }
+        if constexpr (EPI == kStats) {
+            __syncwarp();
+            asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
+            if (it > 0 && group == 0)
+                write_stats(sh.rowstat[(it - 1) & 1], sm, part_at, row_before, row_in_tile);
         }
     }
     __syncthreads();
@@ -821,6 +886,9 @@ cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t s
         const int64_t u = (int64_t)p.mtiles * p.ntiles * p.splits;
         if (p.kchunks < 1 || p.splits < 1 || p.splits > p.kchunks || u < 1 || u > (1 << 30))
             return cudaErrorInvalidValue;
+        // equal lengths but for the last: every split has a chunk
+        p.klength = (p.kchunks + p.splits - 1) / p.splits;
+        if ((int64_t)p.klength * (p.splits - 1) >= p.kchunks) return cudaErrorInvalidValue;
         p.units = (int)u;
         total += u;
     }

@@ -45,6 +45,7 @@ struct Problem {
     int mtiles, ntiles, splits;
     int kchunks;                 // chunks of kTileK for one pair of parts
     int ktail;                   // steps of 16 in the last of them
+    int klength;                 // launch_gemm: chunks of a split (the last may have fewer)
     int a_mo, a_ko, b_no, b_ko;  // where D's corner lies in the operands
     int alt_no, alt_ko;          // the same in b_alt
     int m_fast;                  // units run over m first (else n first)
@@ -74,8 +75,8 @@ struct Softmax {
     int item0;                   // the piece's first item
     int rows;
     // kStats
-    float2* part;                // [tile column half][rows]
-    int part0;                   // the piece's first tile column half
+    float2* part;                // [tile of columns][rows]
+    int part0;                   // the piece's first tile
     const int64_t* targets;      // a row's own target is left out of its statistics
     // kGrad
     const GradRow* row;
@@ -168,6 +169,14 @@ inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k, int c
     p.kchunks = (int)((k + kTileK - 1) / kTileK);
     p.ktail = (int)((k - (int64_t)(p.kchunks - 1) * kTileK + 15) / 16);
     p.splits = 1;
+}
+
+// The splits of k that `want` gives when all but the last are equally long.
+inline int even_splits(int64_t kchunks, int64_t want) {
+    if (want > kchunks) want = kchunks;
+    if (want < 1) want = 1;
+    const int64_t len = (kchunks + want - 1) / want;
+    return (int)((kchunks + len - 1) / len);
 }
 
 // Scratch of one call, carved from the caller's workspace in 256-byte steps.

@@ -324,7 +324,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     if (p.copy_x || backward) p.x = c.take<uint16_t>((int64_t)p.parts * T * p.ldp);
     if (w_buffer) p.w = c.take<uint16_t>((int64_t)p.parts * piece * p.ldp);
     if (!backward) {
-        p.part = c.take<float2>((V + kTileN - 1) / kTileN * 2 * T);
+        p.part = c.take<float2>((V + kTileN - 1) / kTileN * T);
     } else {
         p.row = c.take<GradRow>(T);
         p.words = c.take<unsigned int>(64);
@@ -341,8 +341,8 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
                                   (first + tile - 1) / tile * nt, (T + kTileK - 1) / kTileK,
                                   cta == 2 ? dev.pairs : dev.sms, a.dtype == PVS_F32 ? 6 : 1,
                                   a.dtype == PVS_F32 ? 32 : INT64_MAX / 64, p.pieces > 1);
-        p.xsplits = s.xsplits;
-        p.wsplits = s.wsplits;
+        p.xsplits = even_splits((first + kTileK - 1) / kTileK, s.xsplits);
+        p.wsplits = even_splits((T + kTileK - 1) / kTileK, s.wsplits);
         p.slots0 = s.slots0;
         if (p.xsplits > 1 || p.pieces > 1)
             p.xslots = c.take<float>((int64_t)p.xsplits * T * p.ldp);
@@ -435,11 +435,11 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
             if (e != cudaSuccess) break;
             w = Matrix{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
         }
-        g.sm.part0 = (int)(v0 / kTileN * 2);
+        g.sm.part0 = (int)(v0 / kTileN);
         e = logits(kStats, g, p, a, x, w, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
-    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN * 2, a, a.scale * kLog2e,
+    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN, a, a.scale * kLog2e,
                      !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
@@ -503,7 +503,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             Problem& q = g.p[g.nprob++];
             q = Problem{};
             set_tiles(q, T, a.dim, p.bnd, n, g.cta);
-            q.splits = std::min(p.xsplits, q.kchunks);
+            q.splits = even_splits(q.kchunks, p.xsplits);
             if (!operand_map(&q.a, gm, false, kTileM) ||
                 !operand_map(&q.b, p.copy_w ? copied : direct, true, 0))
                 return cudaErrorInvalidValue;
@@ -529,7 +529,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             Problem& q = g.p[g.nprob++];
             q = Problem{};
             set_tiles(q, n, a.dim, p.bnd, T, g.cta);
-            q.splits = std::min(p.wsplits, q.kchunks);
+            q.splits = even_splits(q.kchunks, p.wsplits);
             if (!operand_map(&q.a, gm, true, 0) || !operand_map(&q.b, x, true, 0))
                 return cudaErrorInvalidValue;
             q.a_mn = q.b_mn = 1;
