@@ -168,60 +168,59 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
 }
 
 // ---- rows of the backward pass -----------------------------------------------------
-// The largest finite |grad_loss| (its bits; an order-free maximum).
-__global__ void __launch_bounds__(256) xent_grad_max_kernel(const float* __restrict__ grad,
-                                                            const int64_t* __restrict__ targets,
-                                                            int64_t ignore_index, int64_t rows,
-                                                            unsigned int* top) {
+// f16 gradients keep G times a power of two that puts the largest finite
+// |grad_loss| at 2^13 .. 2^14: entries down to 2^-38 of it stay above f16's last
+// bit, which is below what an f16 gradient can hold.  up[0] is that power, up[1] its
+// inverse.  One block: a row's weight is 12 bytes of the thousands that it costs.
+__global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __restrict__ grad,
+                                                               const int64_t* __restrict__ targets,
+                                                               int64_t ignore_index, int64_t rows,
+                                                               float* up) {
+    __shared__ float tops[32];
     float v = 0.0f;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows;
-         i += (int64_t)gridDim.x * blockDim.x) {
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
         const float g = fabsf(grad[i]);
         if (targets[i] != ignore_index && isfinite(g)) v = fmaxf(v, g);
     }
     v = warp_max(v);
-    if ((threadIdx.x & 31) == 0) atomicMax(top, __float_as_uint(v));
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    v = warp_max(tops[threadIdx.x]);
+    if (threadIdx.x != 0) return;
+    const int e = v > 0.0f ? min(max(14 - (ilogbf(v) + 1), -126), 126) : 0;
+    up[0] = exp2f((float)e);
+    up[1] = exp2f((float)-e);
 }
 
-// f16 gradients keep G times a power of two that puts the largest |grad_loss|
-// at 2^13 .. 2^14: entries down to 2^-38 of it stay above f16's last bit, which
-// is below what an f16 gradient can hold.  `undo` gets the inverse.
-__global__ void __launch_bounds__(256) xent_rows_kernel(const float4* __restrict__ stats,
-                                                        const float* __restrict__ grad,
-                                                        const int64_t* __restrict__ targets,
-                                                        int64_t items, int64_t ignore_index,
-                                                        int64_t rows,
-                                                        const unsigned int* __restrict__ top,
-                                                        float* undo, GradRow* out) {
+struct RowArgs {
+    pvs_xent_args a;
+    const float4* stats;
+    const float* grad;
+    const float* up;             // or null
+    GradRow* out;
+    int* bad_masked;             // cleared
+};
+__global__ void __launch_bounds__(256) xent_rows_kernel(const RowArgs r) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    float up = 1.0f;
-    if (top) {
-        const float t = __uint_as_float(*top);
-        if (t > 0.0f) {
-            const int e = min(max(14 - (ilogbf(t) + 1), -126), 126);
-            up = exp2f((float)e);
-            if (i == 0) *undo = exp2f((float)-e);
-        } else if (i == 0) {
-            *undo = 1.0f;
-        }
-    }
-    if (i >= rows) return;
-    const float4 st = stats[i];
-    const int64_t y = targets[i];
-    GradRow r{0.0f, 0.0f, 0.0f, -1};
-    if (y != ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
-        const float g = grad[i] * up;
-        r.m = st.x;
-        if (y < 0 || y >= items) {
-            r.coef = r.hit = __int_as_float(0x7fffffff);
+    if (i == 0) *r.bad_masked = 0;
+    if (i >= r.a.rows) return;
+    const float4 st = r.stats[i];
+    const int64_t y = r.a.targets[i];
+    GradRow o{0.0f, 0.0f, 0.0f, -1};
+    if (y != r.a.ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
+        const float g = r.grad[i] * (r.up ? *r.up : 1.0f);
+        o.m = st.x;
+        if (y < 0 || y >= r.a.items) {
+            o.coef = o.hit = __int_as_float(0x7fffffff);
         } else {
-            r.coef = g / st.y;
-            r.hit = g * st.z;
+            o.coef = g / st.y;
+            o.hit = g * st.z;
             // (a masked target has no logit, and no gradient of its own)
-            if (st.w != -INFINITY) r.y = (int)y;
+            if (st.w != -INFINITY) o.y = (int)y;
         }
     }
-    out[i] = r;
+    r.out[i] = o;
 }
 
 // ---- the plan of a call --------------------------------------------------------------
@@ -238,7 +237,7 @@ struct Plan {
     uint16_t *x = nullptr, *w = nullptr, *g = nullptr;
     float2* part = nullptr;
     GradRow* row = nullptr;
-    unsigned int* words = nullptr;   // [0] top |grad|, [1] undo, [2] bad masked
+    unsigned int* words = nullptr;   // [0] up, [1] its inverse, [2] bad masked
     float *xslots = nullptr, *wslots = nullptr;
     size_t bytes = 0;
 };
@@ -286,7 +285,10 @@ Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int n
             for (int s0 = std::max(1, p - 1); s0 <= std::min(slots - 1, p + 1); ++s0) {
                 const double t0 = (double)((n0 + s0 - 1) / s0) * w0;
                 const double t1 = (double)((n1 + slots - s0 - 1) / (slots - s0)) * w1;
-                const double cost = std::max(t0, t1) +
+                // (dx alone, which a head trained against fixed items wants, takes the same
+                // splits over every slot: a quarter of its time counts too)
+                const double x_alone = (double)((n0 + slots - 1) / slots) * w0;
+                const double cost = std::max(t0, t1) + 0.25 * x_alone +
                                     sum * ((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0));
                 if (cost < least) {
                     least = cost;
@@ -454,21 +456,18 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
                      const float* grad_loss, void* dx, int64_t lddx, void* dw, int64_t lddw,
                      cudaStream_t st) {
     const int64_t T = a.rows, V = a.items;
-    cudaError_t e = cudaMemsetAsync(p.words, 0, 256, st);
-    if (e != cudaSuccess) return e;
-    float* undo = reinterpret_cast<float*>(p.words + 1);
+    float* up = reinterpret_cast<float*>(p.words);
+    const float* undo = up + 1;
     int* bad_masked = reinterpret_cast<int*>(p.words + 2);
-    const unsigned blocks = (unsigned)((T + 255) / 256);
     if (p.f16) {
         count_launches(1);
-        xent_grad_max_kernel<<<std::min(blocks, (unsigned)dev.sms), 256, 0, st>>>(
-            grad_loss, a.targets, a.ignore_index, T, p.words);
+        xent_grad_scale_kernel<<<1, 1024, 0, st>>>(grad_loss, a.targets, a.ignore_index, T, up);
     }
     count_launches(1);
-    xent_rows_kernel<<<blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(stats), grad_loss,
-                                             a.targets, V, a.ignore_index, T,
-                                             p.f16 ? p.words : nullptr, undo, p.row);
-    e = cudaGetLastError();
+    xent_rows_kernel<<<(unsigned)((T + 255) / 256), 256, 0, st>>>(
+        RowArgs{a, reinterpret_cast<const float4*>(stats), grad_loss, p.f16 ? up : nullptr, p.row,
+                bad_masked});
+    cudaError_t e = cudaGetLastError();
     // x without the rows that have no gradient: what they hold must not meet G's zeros
     if (e == cudaSuccess) e = copy_rows(a, p, true, st);
     const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
