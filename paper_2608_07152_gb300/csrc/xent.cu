@@ -258,9 +258,10 @@ bool valid(const pvs_xent_args* a) {
 // How dx (u0 tiles, k0 chunks of k) and dw (u1, k1) share the `slots` CTAs or pairs
 // of one launch: each gets slots of its own, and its k is cut where that evens the
 // ends.  The cost of a choice, in the time of a chunk's MMAs (npairs of them a
-// chunk), is the longer side's rounds of units, a unit taking its chunks or its
-// epilogue, whichever is longer (measured: about 3 chunks' time, 6 for float32 sums
-// that splits leave), and what the splits' sums move.
+// chunk), is the longer side's rounds of units, and what the splits' sums move.  A
+// unit takes 1.3 times its chunks and 7 more (10 where it leaves float32 sums): what
+// dw's tiles took with 1, 4 and 16 chunks (64, 256 and 1024 rows: 8, 10.5 and 27).
+double unit_cost(int64_t chunks, bool sums) { return 1.3 * (double)chunks + (sums ? 10 : 7); }
 struct Division {
     int xsplits = 1, wsplits = 1, slots0 = 1;
 };
@@ -272,14 +273,14 @@ Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int n
     for (int64_t wsplits = 1; wsplits <= 16 && wsplits <= k1; wsplits *= 2) {
         if (wsplits > 1 && u1 * wsplits > 8 * slots) break;
         if (k1 > most_chunks * wsplits && 2 * wsplits <= 16 && 2 * wsplits <= k1) continue;
-        const double w1 = std::max<double>((double)((k1 + wsplits - 1) / wsplits) * npairs, wsplits > 1 ? 6 : 3);
+        const double w1 = unit_cost((k1 + wsplits - 1) / wsplits * npairs, wsplits > 1);
         const int64_t n1 = u1 * wsplits;
         // (every split up to 8, then in steps of a quarter to an eighth)
         for (int64_t xsplits = 1; xsplits <= k0 && (xsplits == 1 || u0 * xsplits <= 8 * slots);
              xsplits += std::max<int64_t>(1, xsplits / 8)) {
             const int64_t len = (k0 + xsplits - 1) / xsplits;
             if (len > most_chunks && xsplits < k0 && u0 * (xsplits + 1) <= 8 * slots) continue;
-            const double w0 = std::max<double>((double)len * npairs, xsplits > 1 || accumulate ? 6 : 3);
+            const double w0 = unit_cost(len * npairs, xsplits > 1 || accumulate);
             const int64_t n0 = u0 * xsplits;
             const int p = (int)(slots * (n0 * w0) / (n0 * w0 + n1 * w1) + 0.5);
             for (int s0 = std::max(1, p - 1); s0 <= std::min(slots - 1, p + 1); ++s0) {
