@@ -871,7 +871,7 @@ cudaLaunchConfig_t config(int cta, int grid, cudaStream_t st, cudaLaunchAttribut
     cfg.dynamicSmemBytes = cta == 2 ? smem_bytes<2>() : smem_bytes<1>();
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cta == 2 ? 1 : 0;
     return cfg;
 }
 

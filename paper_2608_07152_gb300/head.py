@@ -72,26 +72,6 @@ def _bind_torch() -> None:
     torch = t
 
 
-class _Current:
-    """The device of an operator's tensors made current, where it is not (a few
-    microseconds that a lone GPU's callers need not spend)."""
-
-    def __init__(self, device):
-        self.to = device.index
-        self.back = None
-
-    def __enter__(self):
-        now = torch.cuda.current_device()
-        if now != self.to:
-            self.back = now
-            torch.cuda.set_device(self.to)
-        return torch._C._cuda_getCurrentRawStream(self.to)
-
-    def __exit__(self, *exc):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
-
-
 def _dtype_code(dtype) -> int:
     code = _CODES.get(dtype)
     if code is None:
@@ -99,21 +79,32 @@ def _dtype_code(dtype) -> int:
     return code
 
 
-def _on_gpu(*tensors):
-    """The device that all of them are on (None entries are left out)."""
+def _on_gpu(*tensors) -> int:
+    """The index of the device that all of them are on (None entries are left out).
+    The checks of a call cost as much as a small kernel: they stay plain."""
     if torch is None:
         _bind_torch()
-    device = None
+    device = -1
     for x in tensors:
         if x is None:
             continue
-        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        d = x.get_device() if isinstance(x, torch.Tensor) else -1
+        if d < 0:
             raise TypeError("the operators take CUDA tensors")
-        if device is None:
-            device = x.device
-        elif x.device != device:
+        if device < 0:
+            device = d
+        elif d != device:
             raise ValueError("the tensors must be on one device")
     return device
+
+
+def _elsewhere(device: int) -> bool:
+    """Whether another device is current: the call is then made again with this one."""
+    return torch._C._cuda_getDevice() != device
+
+
+def _stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _matrix(x, name: str, dtype=None):
@@ -127,8 +118,10 @@ def _matrix(x, name: str, dtype=None):
         raise ValueError(f"{name} has {cols} columns, outside [1, {_MAX_DIM}]")
     if rows > _MAX_ROWS:
         raise ValueError(f"{name} has more than {_MAX_ROWS} rows")
+    if x.is_contiguous():
+        return x, cols
     if (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
-        x = x.contiguous()
+        return x.contiguous(), cols
     return x, (x.stride(0) if rows > 1 else cols)
 
 
@@ -180,14 +173,16 @@ def pvs_xent_forward(x, w, targets, bias=None, scale: float = 1.0, ignore_index:
     (loss float32 [T], stats float32 [T, 4]); the backward pass takes the stats.
     x and w are both bfloat16, float16 or float32.  No logit is kept."""
     a, device, keep = _xent_args(x, w, targets, bias, scale, ignore_index)
-    with _Current(device) as stream:
-        loss = torch.empty(a.rows, dtype=torch.float32, device=device)
-        stats = torch.empty(a.rows, 4, dtype=torch.float32, device=device)
-        n = ctypes.c_size_t()
-        _check(_lib.pvs_xent_workspace(ctypes.byref(a), 0, ctypes.byref(n)), "pvs_xent_workspace")
-        ws = _workspace(n.value, device)
-        _check(_lib.pvs_xent_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(ws), n.value,
-                                     stream), "pvs_xent_forward")
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_xent_forward(x, w, targets, bias, scale, ignore_index)
+    loss = torch.empty(a.rows, dtype=torch.float32, device=device)
+    stats = torch.empty(a.rows, 4, dtype=torch.float32, device=device)
+    n = ctypes.c_size_t()
+    _check(_lib.pvs_xent_workspace(ctypes.byref(a), 0, ctypes.byref(n)), "pvs_xent_workspace")
+    ws = _workspace(n.value, device)
+    _check(_lib.pvs_xent_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(ws), n.value,
+                                 _stream(device)), "pvs_xent_forward")
     return loss, stats
 
 
@@ -197,6 +192,10 @@ def pvs_xent_backward(x, w, targets, stats, grad_loss, bias=None, scale: float =
     [T], from the forward pass's stats; None for one that is not needed.  The
     logits are computed again, a piece of the items at a time."""
     a, device, keep = _xent_args(x, w, targets, bias, scale, ignore_index)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_xent_backward(x, w, targets, stats, grad_loss, bias, scale, ignore_index,
+                                     need_x, need_w)
     _on_gpu(x, stats, grad_loss)
     if stats.dtype != torch.float32 or tuple(stats.shape) != (a.rows, 4):
         raise ValueError("stats must be the forward pass's float32 [T, 4]")
@@ -204,15 +203,14 @@ def pvs_xent_backward(x, w, targets, stats, grad_loss, bias=None, scale: float =
     if stats.data_ptr() % 16:
         stats = stats.clone()
     grad_loss = _vector(grad_loss, "grad_loss", a.rows, torch.float32)
-    with _Current(device) as stream:
-        dx = torch.empty(a.rows, a.dim, dtype=x.dtype, device=device) if need_x else None
-        dw = torch.empty(a.items, a.dim, dtype=x.dtype, device=device) if need_w else None
-        n = ctypes.c_size_t()
-        _check(_lib.pvs_xent_workspace(ctypes.byref(a), 1, ctypes.byref(n)), "pvs_xent_workspace")
-        ws = _workspace(n.value, device)
-        _check(_lib.pvs_xent_backward(ctypes.byref(a), _ptr(stats), _ptr(grad_loss), _ptr(dx),
-                                      a.dim, _ptr(dw), a.dim, _ptr(ws), n.value, stream),
-               "pvs_xent_backward")
+    dx = torch.empty(a.rows, a.dim, dtype=x.dtype, device=device) if need_x else None
+    dw = torch.empty(a.items, a.dim, dtype=x.dtype, device=device) if need_w else None
+    n = ctypes.c_size_t()
+    _check(_lib.pvs_xent_workspace(ctypes.byref(a), 1, ctypes.byref(n)), "pvs_xent_workspace")
+    ws = _workspace(n.value, device)
+    _check(_lib.pvs_xent_backward(ctypes.byref(a), _ptr(stats), _ptr(grad_loss), _ptr(dx),
+                                  a.dim, _ptr(dw), a.dim, _ptr(ws), n.value, _stream(device)),
+           "pvs_xent_backward")
     return dx, dw
 
 
@@ -226,46 +224,52 @@ def pvs_ckpt_store(x, act: int = PVS_ACT_NONE):
     y = act(x) in x's type, None for PVS_ACT_NONE.  Row r stands for
     ``scales[r] * codes[r]``."""
     device = _on_gpu(x)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_ckpt_store(x, act)
     x, ldx = _matrix(x, "x")
     dt = _dtype_code(x.dtype)
     rows, cols = x.shape
-    with _Current(device) as stream:
-        codes = torch.empty(rows, cols, dtype=torch.int8, device=device)
-        scales = torch.empty(rows, dtype=torch.float32, device=device)
-        y = torch.empty(rows, cols, dtype=x.dtype, device=device) if act != PVS_ACT_NONE else None
-        _check(_lib.pvs_ckpt_store(_ptr(x), ldx, rows, cols, dt, int(act), _ptr(codes), cols,
-                                   _ptr(scales), _ptr(y), cols, stream),
-               "pvs_ckpt_store")
+    codes = torch.empty(rows, cols, dtype=torch.int8, device=device)
+    scales = torch.empty(rows, dtype=torch.float32, device=device)
+    y = torch.empty(rows, cols, dtype=x.dtype, device=device) if act != PVS_ACT_NONE else None
+    _check(_lib.pvs_ckpt_store(_ptr(x), ldx, rows, cols, dt, int(act), _ptr(codes), cols,
+                               _ptr(scales), _ptr(y), cols, _stream(device)),
+           "pvs_ckpt_store")
     return codes, scales, y
 
 
 def pvs_ckpt_load(codes, scales, dtype):
     """What rows kept by ``pvs_ckpt_store`` stand for, as a tensor of `dtype`."""
     device = _on_gpu(codes, scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_ckpt_load(codes, scales, dtype)
     codes, ld, scales = _codes(codes, scales)
     dt = _dtype_code(dtype)
     rows, cols = codes.shape
-    with _Current(device) as stream:
-        out = torch.empty(rows, cols, dtype=dtype, device=device)
-        _check(_lib.pvs_ckpt_load(_ptr(codes), ld, _ptr(scales), rows, cols, _ptr(out), cols, dt,
-                                  stream), "pvs_ckpt_load")
+    out = torch.empty(rows, cols, dtype=dtype, device=device)
+    _check(_lib.pvs_ckpt_load(_ptr(codes), ld, _ptr(scales), rows, cols, _ptr(out), cols, dt,
+                              _stream(device)), "pvs_ckpt_load")
     return out
 
 
 def pvs_ckpt_act_backward(dy, codes, scales, act: int = PVS_ACT_GELU):
     """``dy * act'(x)`` for the rows x that the codes stand for, in dy's type."""
     device = _on_gpu(dy, codes, scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_ckpt_act_backward(dy, codes, scales, act)
     dy, lddy = _matrix(dy, "dy")
     dt = _dtype_code(dy.dtype)
     codes, ld, scales = _codes(codes, scales)
     if dy.shape != codes.shape:
         raise ValueError("dy and codes must have one shape")
     rows, cols = codes.shape
-    with _Current(device) as stream:
-        dx = torch.empty(rows, cols, dtype=dy.dtype, device=device)
-        _check(_lib.pvs_ckpt_act_backward(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows,
-                                          cols, dt, int(act), _ptr(dx), cols, stream),
-               "pvs_ckpt_act_backward")
+    dx = torch.empty(rows, cols, dtype=dy.dtype, device=device)
+    _check(_lib.pvs_ckpt_act_backward(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows,
+                                      cols, dt, int(act), _ptr(dx), cols, _stream(device)),
+           "pvs_ckpt_act_backward")
     return dx
 
 
@@ -273,21 +277,23 @@ def pvs_ckpt_grad_weight(dy, codes, scales):
     """The weight gradient ``dy.T @ x`` [N, K] of a linear layer, dy [R, N], from the
     rows x [R, K] that the codes stand for, in dy's type."""
     device = _on_gpu(dy, codes, scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_ckpt_grad_weight(dy, codes, scales)
     dy, lddy = _matrix(dy, "dy")
     dt = _dtype_code(dy.dtype)
     codes, ld, scales = _codes(codes, scales)
     if dy.shape[0] != codes.shape[0]:
         raise ValueError("dy and codes must have as many rows")
     rows, n, k = dy.shape[0], dy.shape[1], codes.shape[1]
-    with _Current(device) as stream:
-        dw = torch.empty(n, k, dtype=dy.dtype, device=device)
-        size = ctypes.c_size_t()
-        _check(_lib.pvs_ckpt_grad_workspace(rows, n, k, dt, ctypes.byref(size)),
-               "pvs_ckpt_grad_workspace")
-        ws = _workspace(size.value, device)
-        _check(_lib.pvs_ckpt_grad_weight(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows, n, k,
-                                         dt, _ptr(dw), k, _ptr(ws), size.value, stream),
-               "pvs_ckpt_grad_weight")
+    dw = torch.empty(n, k, dtype=dy.dtype, device=device)
+    size = ctypes.c_size_t()
+    _check(_lib.pvs_ckpt_grad_workspace(rows, n, k, dt, ctypes.byref(size)),
+           "pvs_ckpt_grad_workspace")
+    ws = _workspace(size.value, device)
+    _check(_lib.pvs_ckpt_grad_weight(_ptr(dy), lddy, _ptr(codes), ld, _ptr(scales), rows, n, k,
+                                     dt, _ptr(dw), k, _ptr(ws), size.value, _stream(device)),
+           "pvs_ckpt_grad_weight")
     return dw
 
 
@@ -300,9 +306,13 @@ def _wq_weights(codes, scales, group: int):
         raise ValueError("group must be 32, 64 or 128")
     if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
         raise TypeError("codes must be uint8 and scales bfloat16")
-    if codes.dim() != 2 or scales.dim() != 2 or codes.shape[1] % 64 != 0 or codes.shape[1] == 0:
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes and scales must be 2-D")
+    n, half = codes.shape
+    if half % 64 != 0 or half == 0:
         raise ValueError("codes must be [N, padded K / 2], padded K a multiple of 128")
-    if tuple(scales.shape) != (codes.shape[0], codes.shape[1] * 2 // group):
+    ns, groups = scales.shape
+    if ns != n or groups != half * 2 // group:
         raise ValueError("scales must be [N, padded K / group]")
     codes, scales = codes.contiguous(), scales.contiguous()
     # a view can start anywhere; the kernels read 16 (8) bytes at once
@@ -310,7 +320,7 @@ def _wq_weights(codes, scales, group: int):
         codes = codes.clone()
     if scales.data_ptr() % 8:
         scales = scales.clone()
-    return codes, scales, codes.shape[1] * 2
+    return codes, scales, half * 2
 
 
 def pvs_wq_pack(w, group: int):
@@ -318,32 +328,36 @@ def pvs_wq_pack(w, group: int):
     128) of a row: (codes uint8 [N, Kp / 2], scales bfloat16 [N, Kp / group]), Kp
     = K padded to a multiple of 128."""
     device = _on_gpu(w)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_wq_pack(w, group)
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
     w, ldw = _matrix(w, "w")
     dt = _dtype_code(w.dtype)
     n, k = w.shape
     kp = _wq_padded(k)
-    with _Current(device) as stream:
-        codes = torch.empty(n, kp // 2, dtype=torch.uint8, device=device)
-        scales = torch.empty(n, kp // group, dtype=torch.bfloat16, device=device)
-        _check(_lib.pvs_wq_pack(_ptr(w), ldw, n, k, dt, int(group), _ptr(codes), _ptr(scales),
-                                stream), "pvs_wq_pack")
+    codes = torch.empty(n, kp // 2, dtype=torch.uint8, device=device)
+    scales = torch.empty(n, kp // group, dtype=torch.bfloat16, device=device)
+    _check(_lib.pvs_wq_pack(_ptr(w), ldw, n, k, dt, int(group), _ptr(codes), _ptr(scales),
+                            _stream(device)), "pvs_wq_pack")
     return codes, scales
 
 
 def pvs_wq_unpack(codes, scales, group: int, cols: int, dtype):
     """The weights [N, cols] that packed ones stand for, as a tensor of `dtype`."""
     device = _on_gpu(codes, scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_wq_unpack(codes, scales, group, cols, dtype)
     codes, scales, kp = _wq_weights(codes, scales, group)
     dt = _dtype_code(dtype)
     if cols < 1 or _wq_padded(cols) != kp:
         raise ValueError(f"cols = {cols} does not pad to {kp}")
     n = codes.shape[0]
-    with _Current(device) as stream:
-        out = torch.empty(n, cols, dtype=dtype, device=device)
-        _check(_lib.pvs_wq_unpack(_ptr(codes), _ptr(scales), n, cols, int(group), _ptr(out), cols,
-                                  dt, stream), "pvs_wq_unpack")
+    out = torch.empty(n, cols, dtype=dtype, device=device)
+    _check(_lib.pvs_wq_unpack(_ptr(codes), _ptr(scales), n, cols, int(group), _ptr(out), cols,
+                              dt, _stream(device)), "pvs_wq_unpack")
     return out
 
 
@@ -351,6 +365,9 @@ def pvs_wq_matvec(x, codes, scales, group: int):
     """``x @ weights.T`` [B, N] in x's type, for a few rows x [B, K] (B <= 64) and
     packed weights."""
     device = _on_gpu(x, codes, scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_wq_matvec(x, codes, scales, group)
     codes, scales, kp = _wq_weights(codes, scales, group)
     x, ldx = _matrix(x, "x")
     dt = _dtype_code(x.dtype)
@@ -360,8 +377,7 @@ def pvs_wq_matvec(x, codes, scales, group: int):
     if _wq_padded(k) != kp:
         raise ValueError(f"x has {k} columns, the packed weights {kp} after padding")
     n = codes.shape[0]
-    with _Current(device) as stream:
-        y = torch.empty(b, n, dtype=x.dtype, device=device)
-        _check(_lib.pvs_wq_matvec(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), n, k, int(group), dt,
-                                  _ptr(y), n, stream), "pvs_wq_matvec")
+    y = torch.empty(b, n, dtype=x.dtype, device=device)
+    _check(_lib.pvs_wq_matvec(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), n, k, int(group), dt,
+                              _ptr(y), n, _stream(device)), "pvs_wq_matvec")
     return y
