@@ -583,7 +583,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                             for (int i = 0; i < 32; ++i)
                                 v[i] = here & (1u << i) ? gr.hit : v[i];
                         }
-                        if (row < sm.rows) {
+                        // (a row of grad has room for the chunk that its last column is in)
+                        if (row < sm.rows && cc * 32 < ncols) {
                             uint16_t* o = sm.grad + (int64_t)row * sm.ldg + n0 + cc * 32;
                             for (int part = 0; part < sm.grad_parts; ++part) {
                                 uint32_t h[16];

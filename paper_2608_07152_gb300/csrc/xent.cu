@@ -229,8 +229,9 @@ struct Plan {
     int64_t ldp = 0;            // leading dimension of copied operands
     bool copy_x = false, copy_w = false;
     int64_t piece = 0;          // items per piece, a multiple of kTileN (or all)
-    int64_t pieces = 0;
+    int64_t pieces = 0, piece_tiles = 0;
     int64_t ldg = 0;
+    int bnl = 0;                // columns per tile of the logits
     int bnd = 0;                // columns per tile of the gradients
     int xsplits = 1, wsplits = 1, slots0 = 0;
     // workspace
@@ -323,11 +324,16 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     }
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
+    const int rows_cta = ctas_for(T, dev);
+    p.bnl = logit_columns(std::min(piece, V), (T + kTileM * rows_cta - 1) / (kTileM * rows_cta),
+                          rows_cta == 2 ? dev.pairs : dev.sms);
+    // (a piece's tiles of logits: their statistics are numbered on from piece to piece)
+    p.piece_tiles = (piece + p.bnl - 1) / p.bnl;
     Carver c{static_cast<uint8_t*>(workspace)};
     if (p.copy_x || backward) p.x = c.take<uint16_t>((int64_t)p.parts * T * p.ldp);
     if (w_buffer) p.w = c.take<uint16_t>((int64_t)p.parts * piece * p.ldp);
     if (!backward) {
-        p.part = c.take<float2>((V + kTileN - 1) / kTileN * T);
+        p.part = c.take<float2>(p.pieces * p.piece_tiles * T);
     } else {
         p.row = c.take<GradRow>(T);
         p.words = c.take<unsigned int>(64);
@@ -363,7 +369,7 @@ cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a,
     q = Problem{};
     g.nprob = 1;
     g.cta = ctas_for(a.rows, dev);
-    set_tiles(q, a.rows, n, logit_columns(n), a.dim, g.cta);
+    set_tiles(q, a.rows, n, p.bnl, a.dim, g.cta);
     if (!operand_map(&q.a, x, false, kTileM) || !operand_map(&q.b, w, false, q.bn / g.cta))
         return cudaErrorInvalidValue;
     q.b_no = p.copy_w ? 0 : (int)v0;
@@ -438,11 +444,12 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
             if (e != cudaSuccess) break;
             w = Matrix{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
         }
-        g.sm.part0 = (int)(v0 / kTileN);
+        g.sm.part0 = (int)(v0 / p.piece * p.piece_tiles);
         e = logits(kStats, g, p, a, x, w, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
-    const JoinArgs j{p.part, (V + kTileN - 1) / kTileN, a, a.scale * kLog2e,
+    const int64_t last = V - (p.pieces - 1) * p.piece;
+    const JoinArgs j{p.part, (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl, a, a.scale * kLog2e,
                      !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
