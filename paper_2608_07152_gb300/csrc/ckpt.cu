@@ -391,8 +391,8 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     p.scaled = dtype == PVS_BF16;
     p.copy = !p.scaled || !in_place;
     p.parts = dtype == PVS_BF16 ? 1 : dtype == PVS_F16 ? 2 : 3;
-    p.lda = round_up(out_cols, 8);
-    p.ldb = round_up(cols, 8);
+    p.lda = copied_ld(out_cols);
+    p.ldb = copied_ld(cols);
     p.ldslot = round_up(cols, 8);
     const int bn = tile_columns(cols);
     const int tile_m = kTileM * ctas_for(out_cols, dev);

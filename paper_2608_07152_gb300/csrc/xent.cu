@@ -227,6 +227,7 @@ __global__ void __launch_bounds__(256) xent_rows_kernel(const RowArgs r) {
 struct Plan {
     int parts = 1, f16 = 0;
     int64_t ldp = 0;            // leading dimension of copied operands
+    int64_t lds = 0;            // and of float32 sums
     bool copy_x = false, copy_w = false;
     int64_t piece = 0;          // items per piece, a multiple of kTileN (or all)
     int64_t pieces = 0, piece_tiles = 0;
@@ -309,7 +310,8 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     const int64_t T = a.rows, V = a.items;
     p.parts = parts_of(a.dtype);
     p.f16 = a.dtype == PVS_F16;
-    p.ldp = round_up(a.dim, 8);
+    p.ldp = copied_ld(a.dim);
+    p.lds = round_up(a.dim, 8);
     p.copy_x = !aligned(a.x, a.ldx, a.dtype);
     p.copy_w = !aligned(a.w, a.ldw, a.dtype);
     int64_t piece = round_up(V, kTileN);
@@ -354,8 +356,8 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         p.wsplits = even_splits((T + kTileK - 1) / kTileK, s.wsplits);
         p.slots0 = s.slots0;
         if (p.xsplits > 1 || p.pieces > 1)
-            p.xslots = c.take<float>((int64_t)p.xsplits * T * p.ldp);
-        if (p.wsplits > 1) p.wslots = c.take<float>((int64_t)p.wsplits * first * p.ldp);
+            p.xslots = c.take<float>((int64_t)p.xsplits * T * p.lds);
+        if (p.wsplits > 1) p.wslots = c.take<float>((int64_t)p.wsplits * first * p.lds);
     }
     p.bytes = c.used;
     return p;
@@ -523,8 +525,8 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             q.to_slots = p.xslots != nullptr;
             q.accumulate = i > 0;
             q.slots = p.xslots;
-            q.slot_stride = T * p.ldp;
-            q.ldslot = p.ldp;
+            q.slot_stride = T * p.lds;
+            q.ldslot = p.lds;
             q.out = dx;
             q.ldout = lddx;
             q.out_type = a.dtype;
@@ -542,8 +544,8 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             q.a_mn = q.b_mn = 1;
             q.to_slots = q.splits > 1;
             q.slots = p.wslots;
-            q.slot_stride = std::min(p.piece, V) * p.ldp;
-            q.ldslot = p.ldp;
+            q.slot_stride = std::min(p.piece, V) * p.lds;
+            q.ldslot = p.lds;
             q.out = static_cast<uint8_t*>(dw) + v0 * lddw * element_bytes(a.dtype);
             q.ldout = lddw;
             q.out_type = a.dtype;
@@ -556,11 +558,11 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         part_pairs(g, p.parts, p.parts);
         e = launch_gemm(kOut, g, dev, st);
         if (e == cudaSuccess && qw && qw->to_slots)
-            e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.ldp, n, a.dim, alpha,
+            e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.lds, n, a.dim, alpha,
                                  a.scale, qw->out, lddw, a.dtype, st);
     }
     if (e == cudaSuccess && dx && p.xslots)
-        e = launch_sum_slots(p.xslots, p.xsplits, T * p.ldp, p.ldp, T, a.dim, alpha, a.scale, dx,
+        e = launch_sum_slots(p.xslots, p.xsplits, T * p.lds, p.lds, T, a.dim, alpha, a.scale, dx,
                              lddx, a.dtype, st);
     return e;
 }
