@@ -306,6 +306,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     if (kCta == 2) cluster_barrier();   // both CTAs' barriers and TMEM are ready
     tc::fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
+    next_early();
+    wait_before();
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
@@ -641,6 +643,8 @@ __global__ void __launch_bounds__(256) sum_slots_kernel(const float* __restrict_
                                                         const float* __restrict__ alpha,
                                                         float alpha0, void* __restrict__ out,
                                                         int64_t ldout, int out_type) {
+    next_early();
+    wait_before();
     const int pieces = (n + 3) / 4;
     const int64_t row0 = (int64_t)blockIdx.x * per_block;
     const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
@@ -691,10 +695,9 @@ cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride
     const int pieces = (n + 3) / 4;
     const int per_block = std::max(1, 512 / pieces);
     count_launches(1);
-    sum_slots_kernel<<<(unsigned)((m + per_block - 1) / per_block), 256, 0, st>>>(
-        slots, splits, slot_stride, ldslot, m, n, per_block, (1ull << 40) / pieces + 1, alpha, alpha0,
-        out, ldout, out_type);
-    return cudaGetLastError();
+    return launch_early(sum_slots_kernel, (m + per_block - 1) / per_block, 256, st, slots, splits,
+                        slot_stride, ldslot, m, n, per_block, (1ull << 40) / pieces + 1, alpha,
+                        alpha0, out, ldout, out_type);
 }
 
 // ---- operands in 16-bit parts ----------------------------------------------------
@@ -708,6 +711,8 @@ __device__ __forceinline__ float load_as_float(const void* p, int dtype, int64_t
 // aligned; n / pieces by a product as in sum_slots_kernel.
 __global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, int per_block, uint64_t m,
                                                     int wide) {
+    next_early();
+    wait_before();
     if (a.only_if && *a.only_if == 0) return;
     const int pieces = (a.cols + 7) / 8;
     const int64_t step = (int64_t)gridDim.x * per_block;
@@ -776,9 +781,8 @@ cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
     // (a conditional copy mostly does nothing: few blocks)
     const int64_t most = a.only_if ? 152 * 4 : 1 << 20;
     count_launches(1);
-    split_kernel<<<(unsigned)std::min(blocks, most), 256, 0, st>>>(a, per_block,
-                                                                    (1ull << 40) / pieces + 1, wide);
-    return cudaGetLastError();
+    return launch_early(split_kernel, std::min(blocks, most), 256, st, a, per_block,
+                        (1ull << 40) / pieces + 1, wide);
 }
 
 // Eight codes a thread, in one load where rows are aligned.
@@ -788,6 +792,8 @@ __global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restri
                                                           int64_t rows, int cols, int per_block,
                                                           uint64_t m, int wide,
                                                           uint16_t* __restrict__ dst, int64_t ldd) {
+    next_early();
+    wait_before();
     const int pieces = (cols + 7) / 8;
     const int64_t row0 = (int64_t)blockIdx.x * per_block;
     const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
@@ -826,9 +832,8 @@ cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* sc
     const int per_block = std::max(1, 512 / pieces);
     const int wide = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 8 == 0;
     count_launches(1);
-    split_codes_kernel<<<(unsigned)((rows + per_block - 1) / per_block), 256, 0, st>>>(
-        codes, ldc, scales, rows, cols, per_block, (1ull << 40) / pieces + 1, wide, dst, ldd);
-    return cudaGetLastError();
+    return launch_early(split_codes_kernel, (rows + per_block - 1) / per_block, 256, st, codes, ldc,
+                        scales, rows, cols, per_block, (1ull << 40) / pieces + 1, wide, dst, ldd);
 }
 
 // ---- host side ---------------------------------------------------------------------
@@ -861,18 +866,20 @@ const void* kernel_of(int epilogue) {
                                : (const void*)head_gemm_kernel<kOut, kCta>;
 }
 
-cudaLaunchConfig_t config(int cta, int grid, cudaStream_t st, cudaLaunchAttribute* attr) {
+cudaLaunchConfig_t config(int cta, int grid, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
     cudaLaunchConfig_t cfg{};
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cta;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cta;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = cta == 2 ? smem_bytes<2>() : smem_bytes<1>();
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = cta == 2 ? 1 : 0;
+    cfg.numAttrs = cta == 2 ? 2 : 1;
     return cfg;
 }
 
@@ -904,7 +911,7 @@ cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t s
         }
     }
     const void* fn = cta == 2 ? kernel_of<2>(epilogue) : kernel_of<1>(epilogue);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     const cudaLaunchConfig_t cfg = config(cta, used * cta, st, attr);
     cudaError_t e = raise_smem_limit(fn, cfg.dynamicSmemBytes);
     if (e != cudaSuccess) return e;
@@ -932,7 +939,7 @@ cudaError_t device(Device* d) {
         if (e != cudaSuccess) return e;
         // CTA pairs that run at once (0 where none can: lone CTAs serve then)
         int pairs = 0;
-        cudaLaunchAttribute attr[1];
+        cudaLaunchAttribute attr[2];
         const cudaLaunchConfig_t cfg = config(2, 2 * sms, nullptr, attr);
         if (raise_smem_limit(kernel_of<2>(kOut), cfg.dynamicSmemBytes) != cudaSuccess ||
             cudaOccupancyMaxActiveClusters(&pairs, kernel_of<2>(kOut), &cfg) != cudaSuccess) {

@@ -98,6 +98,32 @@ struct Args {
     int* status;
 };
 
+// A kernel of a call may be put on the SMs while the one before it ends: its setup then
+// costs nothing.  Every kernel launched with launch_early() first lets the next one
+// start (next_early) and, before it touches memory, waits for the one before it to be
+// complete and visible (wait_before); nothing before the wait depends on memory.
+#ifdef __CUDACC__
+__device__ __forceinline__ void next_early() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... Params, typename... Given>
+cudaError_t launch_early(void (*kernel)(Params...), int64_t grid, int block, cudaStream_t st,
+                         Given&&... given) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(given)...);
+}
+#endif
+
 // The current device: its SMs, the CTA pairs that run at once on them, and the
 // status word that its kernels set (pinned host memory).
 struct Device {

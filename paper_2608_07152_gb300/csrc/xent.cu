@@ -99,6 +99,8 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
     constexpr int kLanes = 256 / R;
     __shared__ float2 sh[kLanes][R];
     __shared__ float dots[R];
+    next_early();
+    wait_before();
     const pvs_xent_args& a = j.a;
     const int r = threadIdx.x % R, lane = threadIdx.x / R;
     const int64_t row = (int64_t)blockIdx.x * R + r;
@@ -176,6 +178,8 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
                                                                const int64_t* __restrict__ targets,
                                                                int64_t ignore_index, int64_t rows,
                                                                float* up) {
+    next_early();
+    wait_before();
     __shared__ float tops[32];
     float v = 0.0f;
     for (int64_t i = threadIdx.x; i < rows; i += 1024) {
@@ -202,6 +206,8 @@ struct RowArgs {
     int* bad_masked;             // cleared
 };
 __global__ void __launch_bounds__(256) xent_rows_kernel(const RowArgs r) {
+    next_early();
+    wait_before();
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i == 0) *r.bad_masked = 0;
     if (i >= r.a.rows) return;
@@ -455,11 +461,8 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
                      !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
-    if (T >= 4 * dev.sms)
-        xent_join_kernel<8><<<(unsigned)((T + 7) / 8), 256, 0, st>>>(j);
-    else
-        xent_join_kernel<1><<<(unsigned)T, 256, 0, st>>>(j);
-    return cudaGetLastError();
+    if (T >= 4 * dev.sms) return launch_early(xent_join_kernel<8>, (T + 7) / 8, 256, st, j);
+    return launch_early(xent_join_kernel<1>, T, 256, st, j);
 }
 
 cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, const float* stats,
@@ -469,15 +472,17 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
     float* up = reinterpret_cast<float*>(p.words);
     const float* undo = up + 1;
     int* bad_masked = reinterpret_cast<int*>(p.words + 2);
+    cudaError_t e = cudaSuccess;
     if (p.f16) {
         count_launches(1);
-        xent_grad_scale_kernel<<<1, 1024, 0, st>>>(grad_loss, a.targets, a.ignore_index, T, up);
+        e = launch_early(xent_grad_scale_kernel, 1, 1024, st, grad_loss, a.targets, a.ignore_index,
+                         T, up);
     }
+    if (e != cudaSuccess) return e;
     count_launches(1);
-    xent_rows_kernel<<<(unsigned)((T + 255) / 256), 256, 0, st>>>(
-        RowArgs{a, reinterpret_cast<const float4*>(stats), grad_loss, p.f16 ? up : nullptr, p.row,
-                bad_masked});
-    cudaError_t e = cudaGetLastError();
+    e = launch_early(xent_rows_kernel, (T + 255) / 256, 256, st,
+                     RowArgs{a, reinterpret_cast<const float4*>(stats), grad_loss,
+                             p.f16 ? up : nullptr, p.row, bad_masked});
     // x without the rows that have no gradient: what they hold must not meet G's zeros
     if (e == cudaSuccess) e = copy_rows(a, p, true, st);
     const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
