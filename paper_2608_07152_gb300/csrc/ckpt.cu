@@ -211,6 +211,8 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
                                                          int8_t* __restrict__ codes, int64_t ldc,
                                                          float* __restrict__ scales,
                                                          void* __restrict__ y, int64_t ldy) {
+    next_early();
+    wait_before();
     constexpr int kPieces = NV * 8 / N;
     constexpr int kRows = 256 / TPR;
     const int lane = threadIdx.x % TPR;
@@ -289,6 +291,8 @@ __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__
                                                         int64_t rows, int cols, int per_block,
                                                         uint64_t m, void* __restrict__ out,
                                                         int64_t ldo) {
+    next_early();
+    wait_before();
     const int pieces = cols / N;
     const int64_t row0 = (int64_t)blockIdx.x * per_block;
     const int here = (int)min((int64_t)per_block, rows - row0);
@@ -326,38 +330,38 @@ bool by_eight(const void* p, int64_t ld, int elem) {
 }
 
 template <int TYPE, int N, int NV, int TPR>
-void store_launch(const void* x, int64_t ldx, int64_t rows, int cols, int act, int8_t* codes,
+cudaError_t store_launch(const void* x, int64_t ldx, int64_t rows, int cols, int act, int8_t* codes,
                   int64_t ldc, float* scales, void* y, int64_t ldy, cudaStream_t st) {
     constexpr int kRows = 256 / TPR;
-    ckpt_store_kernel<TYPE, N, NV, TPR><<<(unsigned)((rows + kRows - 1) / kRows), 256, 0, st>>>(
-        x, ldx, rows, cols, act, codes, ldc, scales, y, ldy);
+    return launch_early(ckpt_store_kernel<TYPE, N, NV, TPR>, (rows + kRows - 1) / kRows, 256, 0, st, x,
+                        ldx, rows, cols, act, codes, ldc, scales, y, ldy);
 }
 
 // The narrowest layout that holds a row: a warp up to 2048 elements, else a block.
 template <int TYPE, int N, typename... A>
-void store_rows(int cols, A... a) {
+cudaError_t store_rows(int cols, A... a) {
     const int nv = (cols + 255) / 256;
-    if (nv <= 1) store_launch<TYPE, N, 1, 32>(a...);
-    else if (nv <= 2) store_launch<TYPE, N, 2, 32>(a...);
-    else if (nv <= 3) store_launch<TYPE, N, 3, 32>(a...);
-    else if (nv <= 4) store_launch<TYPE, N, 4, 32>(a...);
-    else if (nv <= 6) store_launch<TYPE, N, 6, 32>(a...);
-    else if (nv <= 8) store_launch<TYPE, N, 8, 32>(a...);
-    else if (nv <= 16) store_launch<TYPE, N, 2, 256>(a...);
-    else if (nv <= 32) store_launch<TYPE, N, 4, 256>(a...);
-    else store_launch<TYPE, N, 16, 256>(a...);
+    if (nv <= 1) return store_launch<TYPE, N, 1, 32>(a...);
+    if (nv <= 2) return store_launch<TYPE, N, 2, 32>(a...);
+    if (nv <= 3) return store_launch<TYPE, N, 3, 32>(a...);
+    if (nv <= 4) return store_launch<TYPE, N, 4, 32>(a...);
+    if (nv <= 6) return store_launch<TYPE, N, 6, 32>(a...);
+    if (nv <= 8) return store_launch<TYPE, N, 8, 32>(a...);
+    if (nv <= 16) return store_launch<TYPE, N, 2, 256>(a...);
+    if (nv <= 32) return store_launch<TYPE, N, 4, 256>(a...);
+    return store_launch<TYPE, N, 16, 256>(a...);
 }
 
 template <int TYPE, int N, bool DY>
-void load_launch(const void* dy, int64_t lddy, const int8_t* codes, int64_t ldc,
+cudaError_t load_launch(const void* dy, int64_t lddy, const int8_t* codes, int64_t ldc,
                  const float* scales, int64_t rows, int cols, void* out, int64_t ldo,
                  cudaStream_t st) {
     const int pieces = cols / N;
     // about 4096 elements a block; under 2^23 pieces in any case
     const int per_block = std::max(1, 4096 / cols);
-    ckpt_load_kernel<TYPE, N, DY>
-        <<<(unsigned)((rows + per_block - 1) / per_block), 256, 0, st>>>(
-            dy, lddy, codes, ldc, scales, rows, cols, per_block, (1ull << 40) / pieces + 1, out, ldo);
+    return launch_early(ckpt_load_kernel<TYPE, N, DY>, (rows + per_block - 1) / per_block, 256, 0, st, dy,
+                        lddy, codes, ldc, scales, rows, cols, per_block, (1ull << 40) / pieces + 1,
+                        out, ldo);
 }
 
 bool rows_ok(int64_t rows, int32_t cols, int32_t dtype) {
@@ -443,16 +447,17 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
     if (!x || !codes || !scales || (act != PVS_ACT_NONE && !y)) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
+    cudaError_t e = cudaSuccess;
     const int es = element_bytes(dtype);
     const bool eight = cols % 8 == 0 && by_eight(x, ldx, es) && by_eight(codes, ldcodes, 1) &&
                        (act == PVS_ACT_NONE || by_eight(y, ldy, es));
     if (eight)
-        PVS_BY_TYPE(dtype, (store_rows<TYPE, 8>(cols, x, ldx, rows, cols, act, codes, ldcodes,
+        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 8>(cols, x, ldx, rows, cols, act, codes, ldcodes,
                                                 scales, y, ldy, st)));
     else
-        PVS_BY_TYPE(dtype, (store_rows<TYPE, 1>(cols, x, ldx, rows, cols, act, codes, ldcodes,
+        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 1>(cols, x, ldx, rows, cols, act, codes, ldcodes,
                                                 scales, y, ldy, st)));
-    return queued();
+    return queued(e);
 }
 
 extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const float* scales,
@@ -463,13 +468,14 @@ extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const 
     if (!codes || !scales || !out) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
+    cudaError_t e = cudaSuccess;
     if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(out, ldout, element_bytes(dtype)))
-        PVS_BY_TYPE(dtype, (load_launch<TYPE, 8, false>(nullptr, 0, codes, ldcodes, scales, rows,
+        PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 8, false>(nullptr, 0, codes, ldcodes, scales, rows,
                                                         cols, out, ldout, st)));
     else
-        PVS_BY_TYPE(dtype, (load_launch<TYPE, 1, false>(nullptr, 0, codes, ldcodes, scales, rows,
+        PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 1, false>(nullptr, 0, codes, ldcodes, scales, rows,
                                                         cols, out, ldout, st)));
-    return queued();
+    return queued(e);
 }
 
 extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const int8_t* codes,
@@ -483,15 +489,16 @@ extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const 
     if (!dy || !codes || !scales || !dx) return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
+    cudaError_t e = cudaSuccess;
     const int es = element_bytes(dtype);
     if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(dy, lddy, es) &&
         by_eight(dx, lddx, es))
-        PVS_BY_TYPE(dtype, (load_launch<TYPE, 8, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
+        PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 8, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
                                                        dx, lddx, st)));
     else
-        PVS_BY_TYPE(dtype, (load_launch<TYPE, 1, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
+        PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 1, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
                                                        dx, lddx, st)));
-    return queued();
+    return queued(e);
 }
 
 extern "C" pvs_status pvs_ckpt_grad_workspace(int64_t rows, int32_t out_cols, int32_t cols,

@@ -695,7 +695,7 @@ cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride
     const int pieces = (n + 3) / 4;
     const int per_block = std::max(1, 512 / pieces);
     count_launches(1);
-    return launch_early(sum_slots_kernel, (m + per_block - 1) / per_block, 256, st, slots, splits,
+    return launch_early(sum_slots_kernel, (m + per_block - 1) / per_block, 256, 0, st, slots, splits,
                         slot_stride, ldslot, m, n, per_block, (1ull << 40) / pieces + 1, alpha,
                         alpha0, out, ldout, out_type);
 }
@@ -781,7 +781,7 @@ cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
     // (a conditional copy mostly does nothing: few blocks)
     const int64_t most = a.only_if ? 152 * 4 : 1 << 20;
     count_launches(1);
-    return launch_early(split_kernel, std::min(blocks, most), 256, st, a, per_block,
+    return launch_early(split_kernel, std::min(blocks, most), 256, 0, st, a, per_block,
                         (1ull << 40) / pieces + 1, wide);
 }
 
@@ -832,7 +832,7 @@ cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* sc
     const int per_block = std::max(1, 512 / pieces);
     const int wide = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 8 == 0;
     count_launches(1);
-    return launch_early(split_codes_kernel, (rows + per_block - 1) / per_block, 256, st, codes, ldc,
+    return launch_early(split_codes_kernel, (rows + per_block - 1) / per_block, 256, 0, st, codes, ldc,
                         scales, rows, cols, per_block, (1ull << 40) / pieces + 1, wide, dst, ldd);
 }
 

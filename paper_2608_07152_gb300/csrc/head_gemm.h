@@ -109,14 +109,15 @@ __device__ __forceinline__ void next_early() {
 __device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 template <typename... Params, typename... Given>
-cudaError_t launch_early(void (*kernel)(Params...), int64_t grid, int block, cudaStream_t st,
-                         Given&&... given) {
+cudaError_t launch_early(void (*kernel)(Params...), int64_t grid, int block, size_t smem,
+                         cudaStream_t st, Given&&... given) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;

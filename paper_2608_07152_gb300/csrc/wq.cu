@@ -202,6 +202,8 @@ __device__ __forceinline__ void multiply(const RowPair<GROUP> (&w)[RT], const ui
 // A warp's next block is loaded before it works on the present one.
 template <int NT, int GROUP, int RT>
 __global__ void __launch_bounds__(kWqThreads, 2) wq_matvec_kernel(const WqArgs a) {
+    next_early();
+    wait_before();
     constexpr int kRowsAhead = 36;                    // a column's rows, apart in the banks
     extern __shared__ uint4 xf[];                     // [block][word][NT][lane]
     __shared__ float out[kWqWarps][NT * 8][kRowsAhead];
@@ -308,22 +310,18 @@ __global__ void __launch_bounds__(kWqThreads, 2) wq_matvec_kernel(const WqArgs a
     }
 }
 
+using MatvecKernel = void (*)(const WqArgs);
+
 template <int NT, int RT>
 cudaError_t launch_matvec(const WqArgs& a, int group, int grid, cudaStream_t st) {
     const size_t smem = (size_t)a.chunk * NT * kWqBlockBytes;
-    const void* fn = group == 32   ? (const void*)wq_matvec_kernel<NT, 32, RT>
-                     : group == 64 ? (const void*)wq_matvec_kernel<NT, 64, RT>
-                                   : (const void*)wq_matvec_kernel<NT, 128, RT>;
-    cudaError_t e = raise_smem_limit(fn, smem);
+    const MatvecKernel fn = group == 32   ? wq_matvec_kernel<NT, 32, RT>
+                            : group == 64 ? wq_matvec_kernel<NT, 64, RT>
+                                          : wq_matvec_kernel<NT, 128, RT>;
+    const cudaError_t e = raise_smem_limit((const void*)fn, smem);
     if (e != cudaSuccess) return e;
     count_launches(1);
-    if (group == 32)
-        wq_matvec_kernel<NT, 32, RT><<<grid, kWqThreads, smem, st>>>(a);
-    else if (group == 64)
-        wq_matvec_kernel<NT, 64, RT><<<grid, kWqThreads, smem, st>>>(a);
-    else
-        wq_matvec_kernel<NT, 128, RT><<<grid, kWqThreads, smem, st>>>(a);
-    return cudaGetLastError();
+    return launch_early(fn, grid, kWqThreads, smem, st, a);
 }
 
 constexpr int kPackAhead = 4;    // steps whose loads are in flight together
@@ -336,6 +334,8 @@ __global__ void __launch_bounds__(256) wq_pack_kernel(const void* __restrict__ w
                                                       int64_t rows, int cols, int dtype, int gs,
                                                       int blocks, uint8_t* __restrict__ codes,
                                                       uint16_t* __restrict__ scales) {
+    next_early();
+    wait_before();
     const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
     const int lanes = 1 << (gs - 3);                // of a group
     const int at_code = 16 * (l & 3) + 4 * (l >> 2);
@@ -415,6 +415,8 @@ __global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* __restric
                                                         int64_t rows, int cols, int gs, int blocks,
                                                         void* __restrict__ out, int64_t ldo,
                                                         int dtype) {
+    next_early();
+    wait_before();
     const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
     const int at_code = 16 * (l & 3) + 4 * (l >> 2), at_scale = l >> (gs - 3);
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
@@ -517,13 +519,9 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     uint16_t* s = static_cast<uint16_t*>(scales);
     count_launches(1);
-    if (wide(w, ldw))
-        wq_pack_kernel<true><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group_shift(group), blocks,
-                                                codes, s);
-    else
-        wq_pack_kernel<false><<<grid, 256, 0, st>>>(w, ldw, rows, cols, dtype, group_shift(group), blocks,
-                                                codes, s);
-    return queued(cudaGetLastError());
+    return queued(launch_early(wide(w, ldw) ? wq_pack_kernel<true> : wq_pack_kernel<false>, grid, 256,
+                               0, st, w, ldw, rows, cols, dtype, group_shift(group), blocks, codes,
+                               s));
 }
 
 extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, int64_t rows,
@@ -537,13 +535,9 @@ extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, in
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const uint16_t* s = static_cast<const uint16_t*>(scales);
     count_launches(1);
-    if (wide(out, ldout))
-        wq_unpack_kernel<true><<<grid, 256, 0, st>>>(codes, s, rows, cols, group_shift(group), blocks, out, ldout,
-                                                     dtype);
-    else
-        wq_unpack_kernel<false><<<grid, 256, 0, st>>>(codes, s, rows, cols, group_shift(group), blocks, out, ldout,
-                                                      dtype);
-    return queued(cudaGetLastError());
+    return queued(launch_early(wide(out, ldout) ? wq_unpack_kernel<true> : wq_unpack_kernel<false>,
+                               grid, 256, 0, st, codes, s, rows, cols, group_shift(group), blocks,
+                               out, ldout, dtype));
 }
 
 extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,

@@ -461,8 +461,8 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
                      !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
-    if (T >= 4 * dev.sms) return launch_early(xent_join_kernel<8>, (T + 7) / 8, 256, st, j);
-    return launch_early(xent_join_kernel<1>, T, 256, st, j);
+    if (T >= 4 * dev.sms) return launch_early(xent_join_kernel<8>, (T + 7) / 8, 256, 0, st, j);
+    return launch_early(xent_join_kernel<1>, T, 256, 0, st, j);
 }
 
 cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, const float* stats,
@@ -475,12 +475,12 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
     cudaError_t e = cudaSuccess;
     if (p.f16) {
         count_launches(1);
-        e = launch_early(xent_grad_scale_kernel, 1, 1024, st, grad_loss, a.targets, a.ignore_index,
+        e = launch_early(xent_grad_scale_kernel, 1, 1024, 0, st, grad_loss, a.targets, a.ignore_index,
                          T, up);
     }
     if (e != cudaSuccess) return e;
     count_launches(1);
-    e = launch_early(xent_rows_kernel, (T + 255) / 256, 256, st,
+    e = launch_early(xent_rows_kernel, (T + 255) / 256, 256, 0, st,
                      RowArgs{a, reinterpret_cast<const float4*>(stats), grad_loss,
                              p.f16 ? up : nullptr, p.row, bad_masked});
     // x without the rows that have no gradient: what they hold must not meet G's zeros
