@@ -326,53 +326,123 @@ cudaError_t launch_matvec(const WqArgs& a, int group, int grid, cudaStream_t st)
 
 constexpr int kPackAhead = 4;    // steps whose loads are in flight together
 
+// Eight weights as they lie in memory: 16-bit ones two to a word, float32 ones a word each.
+template <int TYPE, bool WIDE>
+struct Eight {
+    static constexpr int kWords = TYPE == PVS_F32 ? 8 : 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void load(const void* p, int64_t at, int k, int cols) {
+        if (WIDE && k + 8 <= cols) {
+            const uint4* q = TYPE == PVS_F32
+                                 ? reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at + k)
+                                 : reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at + k);
+            const uint4 a = __ldg(q);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+            if constexpr (TYPE == PVS_F32) {
+                const uint4 c = __ldg(q + 1);
+                w[4] = c.x, w[5] = c.y, w[6] = c.z, w[7] = c.w;
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+        if (k >= cols) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (k + j >= cols) continue;
+            if constexpr (TYPE == PVS_F32)
+                w[j] = __ldg(static_cast<const uint32_t*>(p) + at + k + j);
+            else
+                w[j >> 1] |= (uint32_t)__ldg(static_cast<const uint16_t*>(p) + at + k + j)
+                             << (16 * (j & 1));
+        }
+    }
+    // the largest magnitude by its bits, in the type's own
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = 0;
+        if constexpr (TYPE == PVS_F32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+            m = max(m & 0xffffu, m >> 16);
+        }
+        return m;
+    }
+    // infinities and NaN are above every number
+    static __device__ __forceinline__ bool finite(uint32_t top) {
+        return top < (TYPE == PVS_F32 ? 0x7f800000u : TYPE == PVS_BF16 ? 0x7f80u : 0x7c00u);
+    }
+    static __device__ __forceinline__ float value(uint32_t bits) {
+        if constexpr (TYPE == PVS_F32) return __uint_as_float(bits);
+        if constexpr (TYPE == PVS_BF16) return __uint_as_float(bits << 16);
+        return __half2float(__ushort_as_half((uint16_t)bits));
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        if constexpr (TYPE == PVS_F32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+        } else if constexpr (TYPE == PVS_BF16) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                v[j] = __uint_as_float(w[j >> 1] << 16);
+                v[j + 1] = __uint_as_float(w[j >> 1] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j >> 1]));
+                v[j] = f.x;
+                v[j + 1] = f.y;
+            }
+        }
+    }
+};
+
 // A word (8 weights) per lane, two blocks of 128 a warp and step; a warp runs
 // along a row.  Word l of a block holds k = 8 l ..: group l / 4 of 32, byte 16 (l % 4) +
-// 4 (l / 4).  gs: log2 of the group.
-template <bool WIDE>
+// 4 (l / 4).  GS: log2 of the group.
+template <int TYPE, bool WIDE, int GS>
 __global__ void __launch_bounds__(256) wq_pack_kernel(const void* __restrict__ w, int64_t ldw,
-                                                      int64_t rows, int cols, int dtype, int gs,
-                                                      int blocks, uint8_t* __restrict__ codes,
+                                                      int64_t rows, int cols, int blocks,
+                                                      uint8_t* __restrict__ codes,
                                                       uint16_t* __restrict__ scales) {
     next_early();
     wait_before();
     const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
-    const int lanes = 1 << (gs - 3);                // of a group
+    constexpr int kLanes = 1 << (GS - 3);           // of a group
     const int at_code = 16 * (l & 3) + 4 * (l >> 2);
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
          row += (int64_t)gridDim.x * 8) {
         for (int first = 0; first < blocks; first += 2 * kPackAhead) {
-            float ahead[kPackAhead][8];
+            Eight<TYPE, WIDE> ahead[kPackAhead];
 #pragma unroll
             for (int i = 0; i < kPackAhead; ++i)
-                load_eight<WIDE>(w, dtype, row * ldw, (first + 2 * i + side) * 128 + l * 8, cols,
-                                 ahead[i]);
+                ahead[i].load(w, row * ldw, (first + 2 * i + side) * 128 + l * 8, cols);
 #pragma unroll
             for (int i = 0; i < kPackAhead; ++i) {
                 if (first + 2 * i >= blocks) break;
                 const int blk = first + 2 * i + side;
-                float(&v)[8] = ahead[i];
-                // the largest magnitude by its bits: infinities and NaN are above every number
-                uint32_t top = 0;
+                uint32_t top = ahead[i].top();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-                for (int o = lanes / 2; o > 0; o >>= 1)
+                for (int o = kLanes / 2; o > 0; o >>= 1)
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                uint32_t sb = 0x3f80;               // 1
-                if (top >= 0x7f800000u) {
-                    sb = 0x7fff;                    // NaN
-                } else if (top != 0u) {
-                    sb = __bfloat16_as_ushort(
-                        __float2bfloat16_rn(__fmul_rn(__uint_as_float(top), 1.0f / 7.0f)));
-                    if (sb == 0) sb = 1;
-                }
+                const bool finite = Eight<TYPE, WIDE>::finite(top);
+                uint32_t sb = __bfloat16_as_ushort(__float2bfloat16_rn(
+                    __fmul_rn(Eight<TYPE, WIDE>::value(top), 1.0f / 7.0f)));
+                if (sb == 0) sb = 1;
+                if (top == 0u) sb = 0x3f80;         // 1
+                if (!finite) sb = 0x7fff;           // NaN
                 const float s = __uint_as_float(sb << 16);
                 uint32_t bits = 0x88888888u;
-                if (top < 0x7f800000u) {
+                if (finite) {
                     // as in the 8-bit quantizer: w / s by a product, rounded by a sum that
                     // leaves q + 8 in the low bits, unless that is near a tie; the sums'
                     // bits times powers of 16 add up to the word and a constant (modulo 2^32)
-                    float r;
+                    float v[8], r;
+                    ahead[i].values(v);
                     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
                     const float k = 12582912.0f + 8.0f;
                     const uint64_t r2 = f2_pack(r, r), k2 = f2_pack(k, k), m2 = f2_pack(-k, -k);
@@ -401,12 +471,27 @@ __global__ void __launch_bounds__(256) wq_pack_kernel(const void* __restrict__ w
                 if (blk < blocks) {
                     const int64_t n = row * blocks + blk;
                     *reinterpret_cast<uint32_t*>(codes + n * 64 + at_code) = bits;
-                    if ((l & (lanes - 1)) == 0) scales[(n << (7 - gs)) + (l >> (gs - 3))] = (uint16_t)sb;
+                    if ((l & (kLanes - 1)) == 0)
+                        scales[(n << (7 - GS)) + (l >> (GS - 3))] = (uint16_t)sb;
                 }
                 __syncwarp();
             }
         }
     }
+}
+
+using PackKernel = void (*)(const void*, int64_t, int64_t, int, int, uint8_t*, uint16_t*);
+template <int TYPE, bool WIDE>
+PackKernel pack_kernel(int group) {
+    return group == 32   ? wq_pack_kernel<TYPE, WIDE, 5>
+           : group == 64 ? wq_pack_kernel<TYPE, WIDE, 6>
+                         : wq_pack_kernel<TYPE, WIDE, 7>;
+}
+template <bool WIDE>
+PackKernel pack_kernel(int dtype, int group) {
+    return dtype == PVS_BF16  ? pack_kernel<PVS_BF16, WIDE>(group)
+           : dtype == PVS_F16 ? pack_kernel<PVS_F16, WIDE>(group)
+                              : pack_kernel<PVS_F32, WIDE>(group);
 }
 
 template <bool WIDE>
@@ -519,9 +604,9 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     uint16_t* s = static_cast<uint16_t*>(scales);
     count_launches(1);
-    return queued(launch_early(wide(w, ldw) ? wq_pack_kernel<true> : wq_pack_kernel<false>, grid, 256,
-                               0, st, w, ldw, rows, cols, dtype, group_shift(group), blocks, codes,
-                               s));
+    return queued(launch_early(wide(w, ldw) ? pack_kernel<true>(dtype, group)
+                                            : pack_kernel<false>(dtype, group),
+                               grid, 256, 0, st, w, ldw, rows, cols, blocks, codes, s));
 }
 
 extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, int64_t rows,
