@@ -65,6 +65,7 @@ struct Shared {
     int abort;
     uint32_t masked[2][kTileN / 32];     // items of the tile outside the softmax
     alignas(16) float b2[2][kTileN];     // their biases, in powers of two
+    alignas(16) float unit[2][kTileN];   // what their logits are in units of
     float2 rowstat[2][kEpiGroups][kTileM];   // a tile's statistics, by the warps' shares of it
 };
 
@@ -447,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             const int n0 = w.nt * p.bn;
             const int ncols = min(p.bn, p.n - n0);      // columns of D in the tile
             [[maybe_unused]] int64_t y = -1;
+            [[maybe_unused]] float row_k2 = 0.0f;
             [[maybe_unused]] GradRow gr;
             if constexpr (EPI != kOut) {
                 // the tile's biases, and which of its columns are in the softmax
@@ -461,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 const uint32_t mask = __ballot_sync(0xffffffffu, bv == -INFINITY);
                 if (et < kTileN) {
                     sh.b2[b][et] = bv;
+                    if (sm.col_unit) sh.unit[b][et] = et < ncols ? __ldg(sm.col_unit + n0 + et) : 0.0f;
                     if (lane == 0) sh.masked[b][et >> 5] = mask;
                 }
                 if constexpr (EPI == kStats) {
@@ -473,6 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     }
                     y = gr.y < 0 ? -1 : (int64_t)gr.y - (sm.item0 + n0);
                 }
+                row_k2 = sm.row_unit && row < sm.rows ? sm.k2 * __ldg(sm.row_unit + row) : sm.k2;
                 __syncwarp();
                 asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
                 if constexpr (EPI == kStats) {
@@ -539,11 +543,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     const uint32_t mask = sh.masked[b][cc];
                     float v[32];
                     [[maybe_unused]] bool bad = false;
+                    if (sm.col_unit) {
+                        // (the powers of two first: neither may leave the range alone)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            r[i] = __float_as_uint(__uint_as_float(r[i]) *
+                                                   (row_k2 * sh.unit[b][cc * 32 + i]));
+                    }
                     if (sm.bias || mask) {
+                        const float f = sm.col_unit ? 1.0f : sm.k2;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            const float l =
-                                fmaf(__uint_as_float(r[i]), sm.k2, sh.b2[b][cc * 32 + i]);
+                            const float l = fmaf(__uint_as_float(r[i]), f, sh.b2[b][cc * 32 + i]);
                             const bool out = (mask >> i) & 1u;
                             v[i] = out ? -INFINITY : l;
                             // (a masked item's l is -inf unless its product is not finite)
@@ -551,7 +562,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                         }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]) * sm.k2;
+                        for (int i = 0; i < 32; ++i)
+                            v[i] = sm.col_unit ? __uint_as_float(r[i]) : __uint_as_float(r[i]) * sm.k2;
                     }
                     // the column of the row's target, as a bit
                     const int64_t yr = y - cc * 32;
@@ -785,6 +797,77 @@ cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
                         (1ull << 40) / pieces + 1, wide);
 }
 
+// A warp per row, which it reads twice (the second time from L1).
+__global__ void __launch_bounds__(256) split16_kernel(const Split16Args a, int wide) {
+    next_early();
+    wait_before();
+    const SplitArgs& s = a.s;
+    const int lane = threadIdx.x & 31;
+    const float* src = static_cast<const float*>(s.src);
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < s.rows;
+         row += (int64_t)gridDim.x * 8) {
+        const bool zero = (s.zero_target && s.zero_target[row] == s.ignore_index) ||
+                          (s.zero_bias && s.zero_bias[row] == -INFINITY);
+        const float* x = src + row * s.ld;
+        float top = 0.0f;
+        if (!zero) {
+            for (int k = lane; k < s.cols; k += 32) {
+                const float f = fabsf(__ldg(x + k));
+                if (f <= 3.402823466e38f) top = fmaxf(top, f);
+            }
+        }
+        top = warp_max(top);
+        const int e = top > 0.0f ? min(13 - ilogbf(top), 126) : 0;
+        const float up = exp2f((float)e);
+        if (lane == 0) a.units[row] = exp2f((float)-e);
+        for (int k = lane * 8; k < s.cols; k += 256) {
+            float v[8];
+            if (wide && k + 8 <= s.cols && !zero) {
+                const float4 p = __ldg(reinterpret_cast<const float4*>(x + k));
+                const float4 q = __ldg(reinterpret_cast<const float4*>(x + k) + 1);
+                v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
+                v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = !zero && k + j < s.cols ? __ldg(x + k + j) : 0.0f;
+            }
+            const int64_t at = row * s.ldd + k;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f0 = v[2 * j] * up, f1 = v[2 * j + 1] * up;
+                const __half h0 = __float2half_rn(f0), h1 = __float2half_rn(f1);
+                hi[j] = (uint32_t)__half_as_ushort(h0) | ((uint32_t)__half_as_ushort(h1) << 16);
+                // (nothing is left of an infinity or a NaN)
+                lo[j] = pack_f16(isfinite(f0) ? f0 - __half2float(h0) : 0.0f,
+                                 isfinite(f1) ? f1 - __half2float(h1) : 0.0f);
+            }
+            *reinterpret_cast<uint4*>(a.dst16 + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(a.dst16 + a.part16_stride + at) =
+                make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            if (!s.dst) continue;
+            for (int part = 0; part < s.parts; ++part) {
+                uint32_t h[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    h[j] = part + 1 < s.parts ? cut_bf16(v[2 * j], v[2 * j + 1])
+                                              : pack_bf16(v[2 * j], v[2 * j + 1]);
+                *reinterpret_cast<uint4*>(s.dst + part * s.part_stride + at) =
+                    make_uint4(h[0], h[1], h[2], h[3]);
+            }
+        }
+        __syncwarp();
+    }
+}
+
+cudaError_t launch_split16(const Split16Args& a, cudaStream_t st) {
+    if (a.s.rows <= 0) return cudaSuccess;
+    const int wide = (reinterpret_cast<uintptr_t>(a.s.src) & 15u) == 0 && a.s.ld % 4 == 0;
+    count_launches(1);
+    return launch_early(split16_kernel, std::min<int64_t>((a.s.rows + 7) / 8, 1 << 20), 256, 0, st, a,
+                        wide);
+}
+
 // Eight codes a thread, in one load where rows are aligned.
 __global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restrict__ codes,
                                                           int64_t ldc,
@@ -844,12 +927,12 @@ bool operand_map(CUtensorMap* m, const Matrix& x, bool mn, int box_rows) {
                          (uint32_t)(mn ? kTileK : box_rows));
 }
 
-void part_pairs(Args& a, int pa, int pb) {
+void part_pairs(Args& a, int pa, int pb, int levels) {
     a.npairs = 0;
-    // parts are 2^-8 of one another; what is below the third of a float32's is left
-    // out.  Smallest first: the tensor cores cut each step's sum to 24 bits, so
-    // only the leading pair's steps may cost the sum its last bits
-    for (int level = 2; level >= 0; --level)
+    // parts are 2^-8 (bf16) or 2^-11 (f16) of one another; what is below the last bits of
+    // a float32 is left out.  Smallest first: the tensor cores cut each step's sum to 24
+    // bits, so only the leading pair's steps may cost the sum its last bits
+    for (int level = levels; level >= 0; --level)
         for (int i = 0; i <= level; ++i)
             if (i < pa && level - i < pb) {
                 a.pa[a.npairs] = (uint8_t)i;

@@ -70,6 +70,8 @@ struct alignas(16) GradRow {
 
 struct Softmax {
     float k2;                    // scale log2(e): logits are powers of two
+    const float* row_unit;       // float32 operands: what D's rows and columns (the piece's
+    const float* col_unit;       // items) are in units of; else null
     const float* bias;           // of the whole vocabulary, or null
     int64_t items;               // bias entries
     int item0;                   // the piece's first item
@@ -162,9 +164,9 @@ inline int logit_columns(int64_t n, int64_t mtiles, int slots) {
     return n >= best ? best : tile_columns(n);
 }
 
-// The part pairs of a product of operands in `pa` and `pb` parts: those whose
-// product is not below the last kept bit.
-void part_pairs(Args& a, int pa, int pb);
+// The part pairs of a product of operands in `pa` and `pb` parts, i and j of one pair
+// adding up to `levels` at most.
+void part_pairs(Args& a, int pa, int pb, int levels = 2);
 
 cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t st);
 
@@ -194,6 +196,19 @@ struct SplitArgs {
     int parts, to_f16;
 };
 cudaError_t launch_split(const SplitArgs& a, cudaStream_t st);
+
+// float32 rows in two f16 parts for a product whose rows (or columns) undo a scale: each
+// row times a power of two that puts its largest finite magnitude at 2^13 .. 2^14,
+// rounded twice to 11 bits (what is left is 2^-24 of an element, 2^-39 of the row's
+// largest); units gets the powers' inverses.  In the same pass, where given, `parts`
+// bf16 parts as launch_split makes them.
+struct Split16Args {
+    SplitArgs s;                 // s.dst may be null
+    uint16_t* dst16;
+    int64_t part16_stride;
+    float* units;
+};
+cudaError_t launch_split16(const Split16Args& a, cudaStream_t st);
 // Codes as bf16 (exact), or times their rows' scales, rounded to bf16.
 cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows,
                                int cols, uint16_t* dst, int64_t ldd, cudaStream_t st);

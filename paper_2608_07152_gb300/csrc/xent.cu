@@ -230,8 +230,15 @@ __global__ void __launch_bounds__(256) xent_rows_kernel(const RowArgs r) {
 }
 
 // ---- the plan of a call --------------------------------------------------------------
+// float32 operands: the logits' product takes them in two f16 parts with a power of two
+// for each row and item, which its epilogue undoes (three products, the fourth is below
+// 2^-22 of an element); the gradients' products, whose sums run over those rows and
+// items, in three bf16 parts (six products).
 struct Plan {
-    int parts = 1, f16 = 0;
+    int parts = 1, f16 = 0;     // of the gradients' operands
+    bool two = false;           // the logits' operands are f16 pairs
+    uint16_t *x16 = nullptr, *w16 = nullptr;
+    float *xunit = nullptr, *wunit = nullptr;
     int64_t ldp = 0;            // leading dimension of copied operands
     int64_t lds = 0;            // and of float32 sums
     bool copy_x = false, copy_w = false;
@@ -316,6 +323,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     const int64_t T = a.rows, V = a.items;
     p.parts = parts_of(a.dtype);
     p.f16 = a.dtype == PVS_F16;
+    p.two = a.dtype == PVS_F32;
     p.ldp = copied_ld(a.dim);
     p.lds = round_up(a.dim, 8);
     p.copy_x = !aligned(a.x, a.ldx, a.dtype);
@@ -338,8 +346,14 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     // (a piece's tiles of logits: their statistics are numbered on from piece to piece)
     p.piece_tiles = (piece + p.bnl - 1) / p.bnl;
     Carver c{static_cast<uint8_t*>(workspace)};
-    if (p.copy_x || backward) p.x = c.take<uint16_t>((int64_t)p.parts * T * p.ldp);
-    if (w_buffer) p.w = c.take<uint16_t>((int64_t)p.parts * piece * p.ldp);
+    if (backward || (p.copy_x && !p.two)) p.x = c.take<uint16_t>((int64_t)p.parts * T * p.ldp);
+    if (w_buffer && (backward || !p.two)) p.w = c.take<uint16_t>((int64_t)p.parts * piece * p.ldp);
+    if (p.two) {
+        p.x16 = c.take<uint16_t>(2 * T * p.ldp);
+        p.w16 = c.take<uint16_t>(2 * piece * p.ldp);
+        p.xunit = c.take<float>(T);
+        p.wunit = c.take<float>(piece);
+    }
     if (!backward) {
         p.part = c.take<float2>(p.pieces * p.piece_tiles * T);
     } else {
@@ -352,12 +366,12 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         const int64_t nt = (a.dim + p.bnd - 1) / p.bnd;
         const int cta = ctas_for(std::max(T, first), dev);
         const int tile = kTileM * cta;
-        // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 128
+        // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 64
         // steps at most before the splits are added with rounding
         const Division s = divide((T + tile - 1) / tile * nt, (first + kTileK - 1) / kTileK,
                                   (first + tile - 1) / tile * nt, (T + kTileK - 1) / kTileK,
                                   cta == 2 ? dev.pairs : dev.sms, a.dtype == PVS_F32 ? 6 : 1,
-                                  a.dtype == PVS_F32 ? 32 : INT64_MAX / 64, p.pieces > 1);
+                                  a.dtype == PVS_F32 ? 16 : INT64_MAX / 64, p.pieces > 1);
         p.xsplits = even_splits((first + kTileK - 1) / kTileK, s.xsplits);
         p.wsplits = even_splits((T + kTileK - 1) / kTileK, s.wsplits);
         p.slots0 = s.slots0;
@@ -369,10 +383,19 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     return p;
 }
 
-// Logits of the piece [v0, v0 + n): x in a.p[0].a, w in .b.
-cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a,
-                   const Matrix& x, const Matrix& w, int64_t v0, int64_t n, const Device& dev,
-                   cudaStream_t st) {
+// Logits of the piece [v0, v0 + n).
+cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a, int64_t v0,
+                   int64_t n, const Device& dev, cudaStream_t st) {
+    const int64_t T = a.rows;
+    const Matrix x = p.two      ? Matrix{p.x16, T, a.dim, p.ldp, 2, T * p.ldp}
+                     : p.copy_x ? Matrix{p.x, T, a.dim, p.ldp, 1, 0}
+                                : Matrix{a.x, T, a.dim, a.ldx, 1, 0};
+    const Matrix w = p.two      ? Matrix{p.w16, n, a.dim, p.ldp, 2, p.piece * p.ldp}
+                     : p.copy_w ? Matrix{p.w, n, a.dim, p.ldp, 1, 0}
+                                : Matrix{a.w, a.items, a.dim, a.ldw, 1, 0};
+    g.f16 = a.dtype != PVS_BF16;
+    g.sm.row_unit = p.xunit;
+    g.sm.col_unit = p.wunit;
     Problem& q = g.p[0];
     q = Problem{};
     g.nprob = 1;
@@ -383,7 +406,7 @@ cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a,
     q.b_no = p.copy_w ? 0 : (int)v0;
     q.m_fast = 1;
     g.sm.item0 = (int)v0;
-    part_pairs(g, p.parts, p.parts);
+    part_pairs(g, x.parts, w.parts, 1);
     return launch_gemm(epilogue, g, dev, st);
 }
 
@@ -406,6 +429,7 @@ cudaError_t copy_rows(const pvs_xent_args& a, const Plan& p, bool zero_ignored, 
     s.dst = p.x;
     s.part_stride = a.rows * p.ldp;
     if (zero_ignored) s.zero_target = a.targets;
+    if (p.two) return launch_split16(Split16Args{s, p.x16, a.rows * p.ldp, p.xunit}, st);
     return launch_split(s, st);
 }
 
@@ -419,6 +443,7 @@ cudaError_t copy_items(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_
     s.part_stride = p.piece * p.ldp;
     if (a.bias) s.zero_bias = a.bias + v0;
     s.only_if = only_if;
+    if (p.two) return launch_split16(Split16Args{s, p.w16, p.piece * p.ldp, p.wunit}, st);
     return launch_split(s, st);
 }
 
@@ -436,24 +461,17 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     cudaError_t e = cudaSuccess;
     const int64_t T = a.rows, V = a.items;
     if (p.copy_x) e = copy_rows(a, p, false, st);
-    const Matrix x = p.copy_x ? Matrix{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp}
-                              : Matrix{a.x, T, a.dim, a.ldx, 1, 0};
     Args g{};
     g.status = dev.status;
-    g.f16 = p.f16;
     g.sm = softmax_of(a);
     g.sm.part = p.part;
     g.sm.targets = a.targets;
     for (int64_t v0 = 0; v0 < V && e == cudaSuccess; v0 += p.piece) {
         const int64_t n = std::min(p.piece, V - v0);
-        Matrix w{a.w, V, a.dim, a.ldw, 1, 0};
-        if (p.copy_w) {
-            e = copy_items(a, p, v0, n, nullptr, st);
-            if (e != cudaSuccess) break;
-            w = Matrix{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
-        }
+        if (p.copy_w) e = copy_items(a, p, v0, n, nullptr, st);
+        if (e != cudaSuccess) break;
         g.sm.part0 = (int)(v0 / p.piece * p.piece_tiles);
-        e = logits(kStats, g, p, a, x, w, v0, n, dev, st);
+        e = logits(kStats, g, p, a, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
     const int64_t last = V - (p.pieces - 1) * p.piece;
@@ -505,12 +523,13 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         g.sm.grad_f16 = p.f16;
         const bool alt = !p.copy_w && a.bias;
         if (alt) g.sm.bad_masked = bad_masked;
-        e = logits(kGrad, g, p, a, x, p.copy_w ? copied : direct, v0, n, dev, st);
+        e = logits(kGrad, g, p, a, v0, n, dev, st);
         // a masked item that holds NaN or infinities: dx takes w from a copy with zeros there
         if (e == cudaSuccess && alt && dx) e = copy_items(a, p, v0, n, bad_masked, st);
         if (e != cudaSuccess) break;
         const Matrix gm{p.g, T, n, p.ldg, p.parts, T * p.ldg};
         g.nprob = 0;
+        g.f16 = p.f16;
         // dw's tiles have items for rows: pairs unless all of it is one CTA's tile
         g.cta = ctas_for(dw ? std::max(T, n) : T, dev);
         if (dx) {

@@ -354,3 +354,16 @@ def test_refusals():
         pvs.pvs_xent_backward(x, w, y, stats, grad[:4])
     with pytest.raises(TypeError):
         pvs.pvs_xent_backward(x, w, y, stats, grad.half())
+
+
+def test_float32_rows_and_items_of_unlike_sizes():
+    # rows and items from 2^-60 to 2^60 of one another: each logit and gradient keeps the
+    # digits that its own products have
+    x, w, y, _, grad, scale = make(40, 300, 72, F32, spread=1.0)
+    up = torch.exp2(torch.randint(-60, 61, (40, 1), device="cuda").float())
+    down = torch.exp2(torch.randint(-60, 61, (300, 1), device="cuda").float())
+    check((x * up, w / up.max(), y, None, grad, scale))
+    check((x / down.max(), w * down, y, None, grad, scale))
+    # the largest and the smallest that float32 holds, with logits of order one
+    check((x * 2.0 ** 120, w * 2.0 ** -120, y, None, grad, scale))
+    check((x * 2.0 ** -100, w * 2.0 ** 100, y, None, grad, scale))
