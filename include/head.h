@@ -67,8 +67,9 @@ pvs_status pvs_head_status(void);
  *   - no item in the softmax: every loss is 0, and no gradient.
  *   - the target itself masked: loss +inf, and no gradient through the target.
  * NaN and overflows elsewhere reach the outputs as in that formula.
- * bf16 and f16 products are exact; float32 ones are made of three bf16 parts
- * for each operand (their six leading products, about 2^-24 each).
+ * bf16 and f16 products are exact.  float32 operands enter the logits as pairs
+ * of f16 with a power of two for each row and item, and the gradients as three
+ * bf16 parts; what is left out of a product is about 2^-22 of it.
  * ------------------------------------------------------------------------ */
 typedef struct pvs_xent_args {
     const void* x;            /* [rows x dim], leading dimension ldx           */
@@ -169,8 +170,8 @@ pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, int64_t rows,
 
 /* y [batch x rows] = x [batch x cols] times the transposed weights, in x's
  * type, 0 <= batch <= 64 (written for single queries and a few: the weights
- * are read once for 8 bf16 rows, 4 f16 rows or 2 float32 rows).  x enters as
- * one, two or three bf16 parts (exact), codes are exact, sums float32. */
+ * are read once for 32 bf16, 16 f16 or 10 float32 rows).  x enters as one, two
+ * or three bf16 parts (exact), codes are exact, sums float32. */
 pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch, const uint8_t* codes,
                          const void* scales, int64_t rows, int32_t cols, int32_t group,
                          int32_t dtype, void* y, int64_t ldy, void* cuda_stream);

@@ -27,7 +27,7 @@ namespace {
 constexpr int kWqThreads = 256;
 constexpr int kWqWarps = kWqThreads / 32;
 constexpr int kWqBlockBytes = 2048;      // x fragments of 128 of k and 8 columns
-constexpr int kWqSmem = 96 * 1024;       // of x fragments, at most
+constexpr int kWqSmem = 88 * 1024;       // of x fragments, at most (two blocks an SM)
 
 __device__ __forceinline__ float load_x(const void* p, int dtype, int64_t i) {
     if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
@@ -647,28 +647,30 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
     a.cols = cols;
     a.blocks = (cols + 127) / 128;
     a.ldy = ldy;
-    // a pass takes what 16 columns hold; one tile of 8 where that is enough
-    const int most = 16 / a.parts;
+    // a pass takes what 32 columns hold, in one, two or four tiles of 8
+    const int most = 32 / a.parts;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    // 32 rows a warp where that still gives every SM 16 warps or more; else 16 rows, and
-    // warps share k until there are about 8 for every SM
-    const int rt = rows >= 16ll * 32 * dev.sms ? 2 : 1;
-    const int64_t tiles = (rows + 16 * rt - 1) / (16 * rt);
-    a.kw = 1;
-    while (a.kw < 8 && a.kw * 2 <= a.blocks && tiles * a.kw < 8ll * dev.sms) a.kw *= 2;
-    const int64_t groups = (tiles * a.kw + kWqWarps - 1) / kWqWarps;
     for (int b = 0; b < batch && e == cudaSuccess; b += most) {
         a.batch = std::min(most, batch - b);
         a.x = static_cast<const uint8_t*>(x) + (int64_t)b * ldx * es;
         a.y = static_cast<uint8_t*>(y) + (int64_t)b * ldy * es;
-        const int nt = a.batch * a.parts > 8 ? 2 : 1;
+        const int columns = a.batch * a.parts;
+        const int nt = columns > 16 ? 4 : columns > 8 ? 2 : 1;
+        // 32 rows a warp where that still gives every SM 16 warps or more (and the sums fit
+        // the registers); else 16 rows, and warps share k until there are about 8 for every SM
+        const int rt = nt < 4 && rows >= 16ll * 32 * dev.sms ? 2 : 1;
+        const int64_t tiles = (rows + 16 * rt - 1) / (16 * rt);
+        a.kw = 1;
+        while (a.kw < 8 && a.kw * 2 <= a.blocks && tiles * a.kw < 8ll * dev.sms) a.kw *= 2;
+        const int64_t groups = (tiles * a.kw + kWqWarps - 1) / kWqWarps;
         a.chunk = std::min(a.blocks, kWqSmem / (nt * kWqBlockBytes));
         // (as many blocks as run at once: each makes the fragments of x for itself)
         const int grid = (int)std::min<int64_t>(groups, 2ll * dev.sms);
-        e = nt == 1 ? (rt == 1 ? launch_matvec<1, 1>(a, group, grid, st)
-                               : launch_matvec<1, 2>(a, group, grid, st))
-                    : (rt == 1 ? launch_matvec<2, 1>(a, group, grid, st)
-                               : launch_matvec<2, 2>(a, group, grid, st));
+        e = nt == 4   ? launch_matvec<4, 1>(a, group, grid, st)
+            : nt == 2 ? (rt == 1 ? launch_matvec<2, 1>(a, group, grid, st)
+                                 : launch_matvec<2, 2>(a, group, grid, st))
+                      : (rt == 1 ? launch_matvec<1, 1>(a, group, grid, st)
+                                 : launch_matvec<1, 2>(a, group, grid, st));
     }
     return queued(e);
 }
