@@ -202,8 +202,6 @@ __device__ __forceinline__ void multiply(const RowPair<GROUP> (&w)[RT], const ui
 // A warp's next block is loaded before it works on the present one.
 template <int NT, int GROUP, int RT>
 __global__ void __launch_bounds__(kWqThreads, 2) wq_matvec_kernel(const WqArgs a) {
-    next_early();
-    wait_before();
     constexpr int kRowsAhead = 36;                    // a column's rows, apart in the banks
     extern __shared__ uint4 xf[];                     // [block][word][NT][lane]
     __shared__ float out[kWqWarps][NT * 8][kRowsAhead];
@@ -321,7 +319,10 @@ cudaError_t launch_matvec(const WqArgs& a, int group, int grid, cudaStream_t st)
     const cudaError_t e = raise_smem_limit((const void*)fn, smem);
     if (e != cudaSuccess) return e;
     count_launches(1);
-    return launch_early(fn, grid, kWqThreads, smem, st, a);
+    // (not early: blocks that came before their turn share SMs unevenly, and 100,000 x 4096
+    // took 63 us behind another product, 55 on its own)
+    fn<<<grid, kWqThreads, smem, st>>>(a);
+    return cudaGetLastError();
 }
 
 constexpr int kPackAhead = 4;    // steps whose loads are in flight together
