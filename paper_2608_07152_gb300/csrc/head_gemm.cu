@@ -31,6 +31,7 @@
 #include <mutex>
 
 #include "../../include/head.h"
+#include "alloc.h"
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
@@ -1029,13 +1030,13 @@ cudaError_t device(Device* d) {
             cudaGetLastError();
             pairs = 0;
         }
-        void* p = nullptr;
-        e = cudaHostAlloc(&p, 256, cudaHostAllocPortable | cudaHostAllocMapped);
+        int* p = nullptr;
+        e = pinned_alloc(&p, 64);
         if (e != cudaSuccess) return e;
         *static_cast<volatile int*>(p) = 0;
         g.sms = sms;
         g.pairs = pairs;
-        g.status = static_cast<int*>(p);
+        g.status = p;
     }
     *d = g;
     return cudaSuccess;
