@@ -203,8 +203,10 @@ __device__ __forceinline__ void codes_of(const float (&v)[N], float s, float r, 
 }
 
 // TPR threads per row hold it in registers: read once, the maximum, the codes, the
-// activation.  N elements (8 where rows are aligned, else 1) make a piece; a
-// thread holds NV pieces of 8 elements' worth.
+// activation.  N elements (8, or 1 where nothing is aligned) make a piece; a thread
+// holds NV pieces of 8 elements' worth.  Rows without gaps of any width are cut into
+// the aligned eights of the whole matrix: a row's first and last piece may hold
+// elements of its neighbours, which are left out.
 template <int TYPE, int N, int NV, int TPR>
 __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict__ x, int64_t ldx,
                                                          int64_t rows, int cols, int act,
@@ -218,16 +220,22 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
     const bool live = row < rows;
-    const int pieces = (cols + N - 1) / N;      // cols is a multiple of N
+    // (the three leading dimensions agree modulo 8 where N is 8)
+    const int before = N == 1 ? 0 : (int)(row * ldx & 7);
+    const int pieces = (before + cols + N - 1) / N;
     float v[kPieces][N];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-        const int j = i * TPR + lane;
-        if (live && j < pieces) {
-            load_elements<TYPE, N>(x, row * ldx + (int64_t)j * N, v[i]);
+        const int j = i * TPR + lane, e = j * N - before;    // the piece's first element
+        if (live && j < pieces && e >= 0 && e + N <= cols) {
+            load_elements<TYPE, N>(x, row * ldx + e, v[i]);
         } else {
 #pragma unroll
-            for (int k = 0; k < N; ++k) v[i][k] = 0.0f;
+            for (int k = 0; k < N; ++k) {
+                float one[1] = {0.0f};
+                if (live && e + k >= 0 && e + k < cols) load_elements<TYPE, 1>(x, row * ldx + e + k, one);
+                v[i][k] = one[0];
+            }
         }
     }
     // the largest magnitude by its bits: infinities and NaN are above every number
@@ -253,8 +261,9 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
     if (lane == 0) scales[row] = finite ? s : __int_as_float(0x7fffffff);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-        const int j = i * TPR + lane;
+        const int j = i * TPR + lane, e = j * N - before;
         if (j >= pieces) break;
+        const bool whole = N == 1 || (e >= 0 && e + N <= cols);
         uint32_t c[N];
         if (finite) {
             codes_of<N>(v[i], s, r, fast, c);
@@ -262,9 +271,13 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
 #pragma unroll
             for (int k = 0; k < N; ++k) c[k] = 0;
         }
-        int8_t* out = codes + row * ldc + (int64_t)j * N;
+        int8_t* out = codes + row * ldc + e;
         if constexpr (N == 1) {
             *out = (int8_t)c[0];
+        } else if (!whole) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (e + k >= 0 && e + k < cols) out[k] = (int8_t)c[k];
         } else {
             uint32_t w[2];
 #pragma unroll
@@ -275,7 +288,15 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
         }
         if (act == PVS_ACT_GELU) {
             gelu_all<N>(v[i]);
-            store_elements<TYPE, N>(y, row * ldy + (int64_t)j * N, v[i]);
+            if (whole) {
+                store_elements<TYPE, N>(y, row * ldy + e, v[i]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float one[1] = {v[i][k]};
+                    if (e + k >= 0 && e + k < cols) store_elements<TYPE, 1>(y, row * ldy + e + k, one);
+                }
+            }
         }
     }
 }
@@ -324,6 +345,67 @@ __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__
     }
 }
 
+// The same for matrices without gaps of any width: the aligned eights of the whole
+// matrix, which may hold the end of one row and the start of the next (rows are 8
+// elements long at least).
+template <int TYPE, bool DY>
+__global__ void __launch_bounds__(256) ckpt_load_flat_kernel(const void* __restrict__ dy,
+                                                             const int8_t* __restrict__ codes,
+                                                             const float* __restrict__ scales,
+                                                             int64_t total, int cols, uint64_t m,
+                                                             void* __restrict__ out) {
+    next_early();
+    wait_before();
+    constexpr int kAhead = 2;
+    const int64_t e0 = (int64_t)blockIdx.x * (256 * 8 * kAhead);
+    const int64_t row0 = e0 / cols;
+    const uint32_t in_row = (uint32_t)(e0 - row0 * cols);
+    float z[kAhead][8], g[kAhead][8], s[kAhead], next[kAhead];
+    uint32_t left[kAhead];                       // elements up to the end of the row
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+        const uint32_t i = (a * 256 + threadIdx.x) * 8;
+        const int64_t e = e0 + i;
+        if (e >= total) continue;
+        const uint32_t r = (uint32_t)(((in_row + i) * m) >> 40);
+        left[a] = (r + 1) * (uint32_t)cols - (in_row + i);
+        s[a] = __ldg(scales + row0 + r);
+        next[a] = left[a] < 8 && e + left[a] < total ? __ldg(scales + row0 + r + 1) : 0.0f;
+        if (e + 8 <= total) {
+            load_codes<8>(codes, e, z[a]);
+            if constexpr (DY) load_elements<TYPE, 8>(dy, e, g[a]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float one[1] = {0.0f}, two[1] = {0.0f};
+                if (e + k < total) {
+                    load_codes<1>(codes, e + k, one);
+                    if constexpr (DY) load_elements<TYPE, 1>(dy, e + k, two);
+                }
+                z[a][k] = one[0];
+                g[a][k] = two[0];
+            }
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+        const int64_t e = e0 + (a * 256 + threadIdx.x) * 8;
+        if (e >= total) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[a][k] *= (uint32_t)k < left[a] ? s[a] : next[a];
+        if constexpr (DY) times_slope<8>(z[a], g[a]);
+        if (e + 8 <= total) {
+            store_elements<TYPE, 8>(out, e, z[a]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float one[1] = {z[a][k]};
+                if (e + k < total) store_elements<TYPE, 1>(out, e + k, one);
+            }
+        }
+    }
+}
+
 // Whether rows of `elem`-byte elements can be read and written eight at a time.
 bool by_eight(const void* p, int64_t ld, int elem) {
     return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(std::min(8 * elem, 16) - 1)) == 0 && ld % 8 == 0;
@@ -340,7 +422,8 @@ cudaError_t store_launch(const void* x, int64_t ldx, int64_t rows, int cols, int
 // The narrowest layout that holds a row: a warp up to 2048 elements, else a block.
 template <int TYPE, int N, typename... A>
 cudaError_t store_rows(int cols, A... a) {
-    const int nv = (cols + 255) / 256;
+    // (a row may reach into one piece more than its width makes)
+    const int nv = (cols + (N == 8 && cols % 8 != 0 ? 14 : 0) + 255) / 256;
     if (nv <= 1) return store_launch<TYPE, N, 1, 32>(a...);
     if (nv <= 2) return store_launch<TYPE, N, 2, 32>(a...);
     if (nv <= 3) return store_launch<TYPE, N, 3, 32>(a...);
@@ -350,6 +433,21 @@ cudaError_t store_rows(int cols, A... a) {
     if (nv <= 16) return store_launch<TYPE, N, 2, 256>(a...);
     if (nv <= 32) return store_launch<TYPE, N, 4, 256>(a...);
     return store_launch<TYPE, N, 16, 256>(a...);
+}
+
+// Matrices without gaps that start aligned.
+bool flat_ok(const void* dy, int64_t lddy, const int8_t* codes, int64_t ldc, int cols, const void* out,
+             int64_t ldo, int elem) {
+    return cols >= 8 && ldc == cols && ldo == cols && (!dy || lddy == cols) && by_eight(codes, 8, 1) &&
+           by_eight(out, 8, elem) && (!dy || by_eight(dy, 8, elem));
+}
+
+template <int TYPE, bool DY>
+cudaError_t flat_launch(const void* dy, const int8_t* codes, const float* scales, int64_t rows, int cols,
+                        void* out, cudaStream_t st) {
+    const int64_t total = rows * cols, per_block = 256 * 8 * 2;
+    return launch_early(ckpt_load_flat_kernel<TYPE, DY>, (total + per_block - 1) / per_block, 256, 0, st,
+                        dy, codes, scales, total, cols, (1ull << 40) / cols + 1, out);
 }
 
 template <int TYPE, int N, bool DY>
@@ -449,8 +547,12 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
     count_launches(1);
     cudaError_t e = cudaSuccess;
     const int es = element_bytes(dtype);
-    const bool eight = cols % 8 == 0 && by_eight(x, ldx, es) && by_eight(codes, ldcodes, 1) &&
-                       (act == PVS_ACT_NONE || by_eight(y, ldy, es));
+    // eights: aligned rows, or matrices without gaps that start aligned
+    const bool dense = ldx == cols && ldcodes == cols && (act == PVS_ACT_NONE || ldy == cols);
+    const bool eight = (cols % 8 == 0 || dense) && by_eight(x, dense ? 8 : ldx, es) &&
+                       by_eight(codes, dense ? 8 : ldcodes, 1) &&
+                       (act == PVS_ACT_NONE || by_eight(y, dense ? 8 : ldy, es)) &&
+                       cols <= 32767 - 8;
     if (eight)
         PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 8>(cols, x, ldx, rows, cols, act, codes, ldcodes,
                                                 scales, y, ldy, st)));
@@ -469,7 +571,10 @@ extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const 
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
-    if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(out, ldout, element_bytes(dtype)))
+    if (cols % 8 != 0 && flat_ok(nullptr, 0, codes, ldcodes, cols, out, ldout, element_bytes(dtype)) &&
+        rows * cols < (int64_t)1 << 42)
+        PVS_BY_TYPE(dtype, e = (flat_launch<TYPE, false>(nullptr, codes, scales, rows, cols, out, st)));
+    else if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(out, ldout, element_bytes(dtype)))
         PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 8, false>(nullptr, 0, codes, ldcodes, scales, rows,
                                                         cols, out, ldout, st)));
     else
@@ -491,7 +596,10 @@ extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const 
     count_launches(1);
     cudaError_t e = cudaSuccess;
     const int es = element_bytes(dtype);
-    if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(dy, lddy, es) &&
+    if (cols % 8 != 0 && flat_ok(dy, lddy, codes, ldcodes, cols, dx, lddx, es) &&
+        rows * cols < (int64_t)1 << 42)
+        PVS_BY_TYPE(dtype, e = (flat_launch<TYPE, true>(dy, codes, scales, rows, cols, dx, st)));
+    else if (cols % 8 == 0 && by_eight(codes, ldcodes, 1) && by_eight(dy, lddy, es) &&
         by_eight(dx, lddx, es))
         PVS_BY_TYPE(dtype, e = (load_launch<TYPE, 8, true>(dy, lddy, codes, ldcodes, scales, rows, cols,
                                                        dx, lddx, st)));

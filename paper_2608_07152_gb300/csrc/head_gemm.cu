@@ -757,6 +757,15 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, int per_b
                                                    : __half2float(__ushort_as_half((uint16_t)h));
                     }
                 }
+            } else if (a.dtype != PVS_F32 && col + 8 <= a.cols) {
+                uint32_t u[4];
+                load_eight_halves(static_cast<const uint16_t*>(a.src) + at, u);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t h = (u[k >> 1] >> (16 * (k & 1))) & 0xffffu;
+                    v[k] = a.dtype == PVS_BF16 ? __uint_as_float(h << 16)
+                                               : __half2float(__ushort_as_half((uint16_t)h));
+                }
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)

@@ -110,6 +110,21 @@ __device__ __forceinline__ void next_early() {
 }
 __device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Eight 16-bit elements from any element's address, in 4-byte loads: the words that hold
+// them, shifted by half a word where they start in the middle of one.  Reads up to one
+// element before them and one after, within the words of the first and the last.
+__device__ __forceinline__ void load_eight_halves(const uint16_t* p, uint32_t (&w)[4]) {
+    const bool odd = (reinterpret_cast<uintptr_t>(p) & 2u) != 0;
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p - (odd ? 1 : 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __ldg(q + i);
+    if (odd) {
+        const uint32_t last = __ldg(q + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], i < 3 ? w[i + 1] : last, 16);
+    }
+}
+
 template <typename... Params, typename... Given>
 cudaError_t launch_early(void (*kernel)(Params...), int64_t grid, int block, size_t smem,
                          cudaStream_t st, Given&&... given) {

@@ -346,6 +346,12 @@ struct Eight {
             }
             return;
         }
+        if constexpr (TYPE != PVS_F32) {
+            if (k + 8 <= cols) {
+                load_eight_halves(static_cast<const uint16_t*>(p) + at + k, w);
+                return;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = 0;
         if (k >= cols) return;
@@ -505,6 +511,10 @@ __global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* __restric
     wait_before();
     const int lane = threadIdx.x & 31, l = lane & 15, side = lane >> 4;
     const int at_code = 16 * (l & 3) + 4 * (l >> 2), at_scale = l >> (gs - 3);
+    // where rows are not aligned, a warp's 256 values go through shared memory, so that
+    // neighbours write neighbours
+    __shared__ float stage[WIDE ? 1 : 8][WIDE ? 1 : 256 + 8];
+    float* mine = stage[WIDE ? 0 : threadIdx.x >> 5];
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows;
          row += (int64_t)gridDim.x * 8) {
         for (int first = 0; first < blocks; first += 2 * kPackAhead) {
@@ -518,7 +528,8 @@ __global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* __restric
 #pragma unroll
             for (int i = 0; i < kPackAhead; ++i) {
                 const int k = (first + 2 * i + side) * 128 + l * 8;
-                if (k >= cols) continue;
+                if (WIDE && k >= cols) continue;
+                if (!WIDE && (first + 2 * i) * 128 >= cols) break;
                 const float s = __uint_as_float(unit[i] << 16);
                 // u under the exponent of 2^23 reads as 2^23 + u
                 float v[8];
@@ -532,8 +543,26 @@ __global__ void __launch_bounds__(256) wq_unpack_kernel(const uint8_t* __restric
                                             k2),
                                      s2),
                               v[j], v[j + 1]);
+                if constexpr (!WIDE) {
+                    // (every 32 values a word further: the eights of the lanes meet fewer conflicts)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = side * 128 + l * 8 + j;
+                        mine[at + (at >> 5)] = v[j];
+                    }
+                    __syncwarp();
+                    const int k0 = (first + 2 * i) * 128;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = j * 32 + lane;
+                        if (k0 + at < cols)
+                            store_y(out, dtype, row * ldo + k0 + at, mine[at + (at >> 5)]);
+                    }
+                    __syncwarp();
+                    continue;
+                }
                 const int64_t at = row * ldo + k;
-                if (WIDE && k + 8 <= cols) {
+                if (k + 8 <= cols) {
                     if (dtype == PVS_F32) {
                         float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
                         p[0] = make_float4(v[0], v[1], v[2], v[3]);

@@ -280,32 +280,35 @@ double unit_cost(int64_t chunks, bool sums) { return 1.3 * (double)chunks + (sum
 struct Division {
     int xsplits = 1, wsplits = 1, slots0 = 1;
 };
+// xleast, wleast: the fewest splits that float32 sums take (else 1).
 Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int npairs,
-                int64_t most_chunks, bool accumulate) {
+                int64_t xleast, int64_t wleast, bool accumulate) {
     Division best;
     double least = 1e300;
-    const double sum = 2.0 * 6 / slots;           // a split tile's store and its later read
-    for (int64_t wsplits = 1; wsplits <= 16 && wsplits <= k1; wsplits *= 2) {
-        if (wsplits > 1 && u1 * wsplits > 8 * slots) break;
-        if (k1 > most_chunks * wsplits && 2 * wsplits <= 16 && 2 * wsplits <= k1) continue;
+    // a split tile's store and its later read, and the launch that adds the splits
+    const double sum = 2.0 * 6 / slots, launch = 16;
+    for (int64_t wsplits = wleast; wsplits <= k1; wsplits *= 2) {
+        if (wsplits > wleast && u1 * wsplits > 8 * slots) break;
         const double w1 = unit_cost((k1 + wsplits - 1) / wsplits * npairs, wsplits > 1);
         const int64_t n1 = u1 * wsplits;
-        // (every split up to 8, then in steps of a quarter to an eighth)
-        for (int64_t xsplits = 1; xsplits <= k0 && (xsplits == 1 || u0 * xsplits <= 8 * slots);
+        // (every split up to 8, then in steps of an eighth)
+        for (int64_t xsplits = xleast;
+             xsplits <= k0 && (xsplits == xleast || u0 * xsplits <= 8 * slots);
              xsplits += std::max<int64_t>(1, xsplits / 8)) {
             const int64_t len = (k0 + xsplits - 1) / xsplits;
-            if (len > most_chunks && xsplits < k0 && u0 * (xsplits + 1) <= 8 * slots) continue;
             const double w0 = unit_cost(len * npairs, xsplits > 1 || accumulate);
             const int64_t n0 = u0 * xsplits;
             const int p = (int)(slots * (n0 * w0) / (n0 * w0 + n1 * w1) + 0.5);
-            for (int s0 = std::max(1, p - 1); s0 <= std::min(slots - 1, p + 1); ++s0) {
+            for (int s0 = std::min(std::max(1, p - 1), slots - 1); s0 <= std::min(slots - 1, p + 1);
+                 ++s0) {
                 const double t0 = (double)((n0 + s0 - 1) / s0) * w0;
                 const double t1 = (double)((n1 + slots - s0 - 1) / (slots - s0)) * w1;
                 // (dx alone, which a head trained against fixed items wants, takes the same
                 // splits over every slot: a quarter of its time counts too)
                 const double x_alone = (double)((n0 + slots - 1) / slots) * w0;
                 const double cost = std::max(t0, t1) + 0.25 * x_alone +
-                                    sum * ((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0));
+                                    sum * ((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0)) +
+                                    launch * ((xsplits > 1 || accumulate) + (wsplits > 1));
                 if (cost < least) {
                     least = cost;
                     best.xsplits = (int)xsplits;
@@ -366,12 +369,17 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         const int64_t nt = (a.dim + p.bnd - 1) / p.bnd;
         const int cta = ctas_for(std::max(T, first), dev);
         const int tile = kTileM * cta;
-        // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 64
-        // steps at most before the splits are added with rounding
-        const Division s = divide((T + tile - 1) / tile * nt, (first + kTileK - 1) / kTileK,
-                                  (first + tile - 1) / tile * nt, (T + kTileK - 1) / kTileK,
-                                  cta == 2 ? dev.pairs : dev.sms, a.dtype == PVS_F32 ? 6 : 1,
-                                  a.dtype == PVS_F32 ? 16 : INT64_MAX / 64, p.pieces > 1);
+        const int slots = cta == 2 ? dev.pairs : dev.sms, npairs = a.dtype == PVS_F32 ? 6 : 1;
+        const int64_t ux = (T + tile - 1) / tile * nt, kx = (first + kTileK - 1) / kTileK;
+        const int64_t uw = (first + tile - 1) / tile * nt, kw = (T + kTileK - 1) / kTileK;
+        // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 64 steps
+        // at most before the splits are added with rounding (as far as 2 GB of them go)
+        auto fewest = [&](int64_t chunks, int64_t rows) {
+            const int64_t room = ((int64_t)2 << 30) / std::max<int64_t>(1, rows * p.lds * 4);
+            return a.dtype == PVS_F32 ? std::max<int64_t>(1, std::min((chunks + 15) / 16, room)) : 1;
+        };
+        const Division s = divide(ux, kx, uw, kw, slots, npairs, fewest(kx, T), fewest(kw, first),
+                                  p.pieces > 1);
         p.xsplits = even_splits((first + kTileK - 1) / kTileK, s.xsplits);
         p.wsplits = even_splits((T + kTileK - 1) / kTileK, s.wsplits);
         p.slots0 = s.slots0;
