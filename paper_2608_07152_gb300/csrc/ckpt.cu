@@ -645,8 +645,8 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
         return PVS_ERR_INVALID;
     const pvs_status before = (pvs_status)take_status(dev);
     if (before != PVS_OK) return before;
+    SplitArgs s{};
     if (p.copy) {
-        SplitArgs s{};
         s.src = dy;
         s.ld = lddy;
         s.rows = rows;
@@ -657,11 +657,16 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
         s.ldd = p.lda;
         s.part_stride = rows * p.lda;
         s.parts = p.parts;
-        e = launch_split(s, st);
     }
-    if (e == cudaSuccess)
-        e = launch_split_codes(codes, ldcodes, p.scaled ? scales : nullptr, rows, cols, p.b, p.ldb,
-                               st);
+    CodesArgs c{};
+    c.codes = codes;
+    c.ldc = ldcodes;
+    c.rows = rows;
+    c.cols = cols;
+    c.scales = p.scaled ? scales : nullptr;
+    c.dst = p.b;
+    c.ldd = p.ldb;
+    e = launch_codes(c, s, st);
     if (e != cudaSuccess) return queued(e);
     Args g{};
     g.status = dev.status;

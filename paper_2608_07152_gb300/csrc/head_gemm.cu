@@ -722,14 +722,11 @@ __device__ __forceinline__ float load_as_float(const void* p, int dtype, int64_t
 
 // Eight consecutive elements a thread, in one load (two of float32) where rows are
 // aligned; n / pieces by a product as in sum_slots_kernel.
-__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, int per_block, uint64_t m,
-                                                    int wide) {
-    next_early();
-    wait_before();
-    if (a.only_if && *a.only_if == 0) return;
-    const int pieces = (a.cols + 7) / 8;
-    const int64_t step = (int64_t)gridDim.x * per_block;
-    for (int64_t row0 = (int64_t)blockIdx.x * per_block; row0 < a.rows; row0 += step) {
+__device__ __forceinline__ void split_rows(const SplitArgs& a, int64_t block, int64_t blocks) {
+    const int pieces = (a.cols + 7) / 8, per_block = a.per_block, wide = a.wide;
+    const uint64_t m = a.magic;
+    const int64_t step = blocks * per_block;
+    for (int64_t row0 = block * per_block; row0 < a.rows; row0 += step) {
         const uint32_t total = (uint32_t)(min((int64_t)per_block, a.rows - row0) * pieces);
         for (uint32_t i = threadIdx.x; i < total; i += 256) {
             const uint32_t r = (uint32_t)((i * m) >> 40);
@@ -794,101 +791,191 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, int per_b
     }
 }
 
-cudaError_t launch_split(const SplitArgs& a, cudaStream_t st) {
-    if (a.rows <= 0) return cudaSuccess;
-    const int pieces = (a.cols + 7) / 8;
-    const int per_block = std::max(1, 512 / pieces);
-    const int wide = (reinterpret_cast<uintptr_t>(a.src) & 15u) == 0 && a.ld % 8 == 0;
-    const int64_t blocks = (a.rows + per_block - 1) / per_block;
-    // (a conditional copy mostly does nothing: few blocks)
-    const int64_t most = a.only_if ? 152 * 4 : 1 << 20;
-    count_launches(1);
-    return launch_early(split_kernel, std::min(blocks, most), 256, 0, st, a, per_block,
-                        (1ull << 40) / pieces + 1, wide);
-}
-
-// A warp per row, which it reads twice (the second time from L1).
-__global__ void __launch_bounds__(256) split16_kernel(const Split16Args a, int wide) {
+__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a) {
     next_early();
     wait_before();
+    if (a.only_if && *a.only_if == 0) return;
+    split_rows(a, blockIdx.x, gridDim.x);
+}
+
+// How a split's blocks share its rows: set before its launch.
+int64_t plan_split(SplitArgs& a) {
+    const int pieces = (a.cols + 7) / 8;
+    a.per_block = std::max(1, 512 / pieces);
+    a.magic = (1ull << 40) / pieces + 1;
+    a.wide = (reinterpret_cast<uintptr_t>(a.src) & 15u) == 0 && a.ld % (a.dtype == PVS_F32 ? 4 : 8) == 0;
+    // (a conditional copy mostly does nothing: few blocks)
+    const int64_t most = a.only_if ? 152 * 4 : 1 << 20;
+    return std::min((a.rows + a.per_block - 1) / a.per_block, most);
+}
+
+cudaError_t launch_split(const SplitArgs& s, cudaStream_t st) {
+    if (s.rows <= 0) return cudaSuccess;
+    SplitArgs a = s;
+    const int64_t blocks = plan_split(a);
+    count_launches(1);
+    return launch_early(split_kernel, blocks, 256, 0, st, a);
+}
+
+// Eight float32 elements of a row from column k, zeros past it.
+__device__ __forceinline__ void load_eight_floats(const float* x, int k, int cols, bool wide,
+                                                  float (&v)[8]) {
+    if (wide && k + 8 <= cols) {
+        const float4 p = __ldg(reinterpret_cast<const float4*>(x + k));
+        const float4 q = __ldg(reinterpret_cast<const float4*>(x + k) + 1);
+        v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
+        v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = k + j < cols ? __ldg(x + k + j) : 0.0f;
+    }
+}
+__device__ __forceinline__ float finite_top(const float (&v)[8], float top) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float f = fabsf(v[j]);
+        if (f <= 3.402823466e38f) top = fmaxf(top, f);
+    }
+    return top;
+}
+__device__ __forceinline__ void store_parts(const Split16Args& a, int64_t at, float (&v)[8], float up) {
+    const SplitArgs& s = a.s;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float f0 = v[2 * j] * up, f1 = v[2 * j + 1] * up;
+        hi[j] = pack_f16(f0, f1);
+        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
+        // (nothing is left of an infinity or a NaN)
+        lo[j] = pack_f16(isfinite(f0) ? f0 - h.x : 0.0f, isfinite(f1) ? f1 - h.y : 0.0f);
+    }
+    *reinterpret_cast<uint4*>(a.dst16 + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(a.dst16 + a.part16_stride + at) =
+        make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if (!s.dst) return;
+    for (int part = 0; part < s.parts; ++part) {
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            h[j] = part + 1 < s.parts ? cut_bf16(v[2 * j], v[2 * j + 1])
+                                      : pack_bf16(v[2 * j], v[2 * j + 1]);
+        *reinterpret_cast<uint4*>(s.dst + part * s.part_stride + at) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+    }
+}
+
+// A warp per row: up to 1024 elements in registers, all loads in flight at once (read
+// twice, 200 rows over 100,003 items of 385 took 189 us in all); longer rows are read
+// twice, the second time from L1.
+__device__ __forceinline__ void split16_rows(const Split16Args& a, int64_t block, int64_t blocks) {
+    constexpr int kHeld = 4;
     const SplitArgs& s = a.s;
     const int lane = threadIdx.x & 31;
-    const float* src = static_cast<const float*>(s.src);
-    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < s.rows;
-         row += (int64_t)gridDim.x * 8) {
+    for (int64_t row = block * 8 + (threadIdx.x >> 5); row < s.rows; row += blocks * 8) {
         const bool zero = (s.zero_target && s.zero_target[row] == s.ignore_index) ||
                           (s.zero_bias && s.zero_bias[row] == -INFINITY);
-        const float* x = src + row * s.ld;
-        float top = 0.0f;
-        if (!zero) {
-            for (int k = lane; k < s.cols; k += 32) {
-                const float f = fabsf(__ldg(x + k));
-                if (f <= 3.402823466e38f) top = fmaxf(top, f);
-            }
+        const float* x = static_cast<const float*>(s.src) + row * s.ld;
+        const int cols = zero ? 0 : s.cols;       // (a zero row: nothing is read)
+        float v[kHeld][8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) load_eight_floats(x, lane * 8 + 256 * i, cols, s.wide, v[i]);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) top = finite_top(v[i], top);
+        for (int k = lane * 8 + 256 * kHeld; k < cols; k += 256) {
+            float w[8];
+            load_eight_floats(x, k, cols, s.wide, w);
+            top = finite_top(w, top);
         }
         top = warp_max(top);
         const int e = top > 0.0f ? min(13 - ilogbf(top), 126) : 0;
         const float up = exp2f((float)e);
         if (lane == 0) a.units[row] = exp2f((float)-e);
-        for (int k = lane * 8; k < s.cols; k += 256) {
-            float v[8];
-            if (wide && k + 8 <= s.cols && !zero) {
-                const float4 p = __ldg(reinterpret_cast<const float4*>(x + k));
-                const float4 q = __ldg(reinterpret_cast<const float4*>(x + k) + 1);
-                v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
-                v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = !zero && k + j < s.cols ? __ldg(x + k + j) : 0.0f;
-            }
-            const int64_t at = row * s.ldd + k;
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float f0 = v[2 * j] * up, f1 = v[2 * j + 1] * up;
-                const __half h0 = __float2half_rn(f0), h1 = __float2half_rn(f1);
-                hi[j] = (uint32_t)__half_as_ushort(h0) | ((uint32_t)__half_as_ushort(h1) << 16);
-                // (nothing is left of an infinity or a NaN)
-                lo[j] = pack_f16(isfinite(f0) ? f0 - __half2float(h0) : 0.0f,
-                                 isfinite(f1) ? f1 - __half2float(h1) : 0.0f);
-            }
-            *reinterpret_cast<uint4*>(a.dst16 + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(a.dst16 + a.part16_stride + at) =
-                make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            if (!s.dst) continue;
-            for (int part = 0; part < s.parts; ++part) {
-                uint32_t h[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    h[j] = part + 1 < s.parts ? cut_bf16(v[2 * j], v[2 * j + 1])
-                                              : pack_bf16(v[2 * j], v[2 * j + 1]);
-                *reinterpret_cast<uint4*>(s.dst + part * s.part_stride + at) =
-                    make_uint4(h[0], h[1], h[2], h[3]);
-            }
+        for (int i = 0; i < kHeld; ++i) {
+            const int k = lane * 8 + 256 * i;
+            if (k < s.cols) store_parts(a, row * s.ldd + k, v[i], up);
         }
-        __syncwarp();
+        for (int k = lane * 8 + 256 * kHeld; k < s.cols; k += 256) {
+            float w[8];
+            load_eight_floats(x, k, cols, s.wide, w);
+            store_parts(a, row * s.ldd + k, w, up);
+        }
     }
 }
 
-cudaError_t launch_split16(const Split16Args& a, cudaStream_t st) {
-    if (a.s.rows <= 0) return cudaSuccess;
-    const int wide = (reinterpret_cast<uintptr_t>(a.s.src) & 15u) == 0 && a.s.ld % 4 == 0;
+// The rows of the backward pass.
+__device__ __forceinline__ void prepare_row(const RowArgs& r, int64_t i) {
+    if (i == 0) *r.bad_masked = 0;
+    if (i >= r.rows) return;
+    const float4 st = r.stats[i];
+    const int64_t y = r.targets[i];
+    GradRow o{0.0f, 0.0f, 0.0f, -1};
+    if (y != r.ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
+        const float g = r.grad[i] * (r.up ? *r.up : 1.0f);
+        o.m = st.x;
+        if (y < 0 || y >= r.items) {
+            o.coef = o.hit = __int_as_float(0x7fffffff);
+        } else {
+            o.coef = g / st.y;
+            o.hit = g * st.z;
+            // (a masked target has no logit, and no gradient of its own)
+            if (st.w != -INFINITY) o.y = (int)y;
+        }
+    }
+    r.out[i] = o;
+}
+
+// What a pass does before its first product, in one launch: its copies, and the
+// backward pass's rows, each on blocks of its own.
+template <bool TWO>
+__global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
+    next_early();
+    wait_before();
+    int64_t b = blockIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (b < a.blocks[i]) {
+            if (TWO)
+                split16_rows(a.copy[i], b, a.blocks[i]);
+            else
+                split_rows(a.copy[i].s, b, a.blocks[i]);
+            return;
+        }
+        b -= a.blocks[i];
+    }
+    prepare_row(a.rows, b * 256 + threadIdx.x);
+}
+
+cudaError_t launch_prepare(PrepareArgs& a, cudaStream_t st) {
+    int64_t total = 0;
+    bool two = false;
+    for (int i = 0; i < 2; ++i) {
+        Split16Args& c = a.copy[i];
+        if (c.s.rows <= 0) {
+            a.blocks[i] = 0;
+            continue;
+        }
+        two = c.dst16 != nullptr;
+        a.blocks[i] = plan_split(c.s);
+        if (two) a.blocks[i] = std::min<int64_t>((c.s.rows + 7) / 8, 1 << 20);
+        total += a.blocks[i];
+    }
+    if (a.rows.out) total += (a.rows.rows + 255) / 256;
+    if (total == 0) return cudaSuccess;
+    if (total > 0x7fffffff) return cudaErrorInvalidValue;
     count_launches(1);
-    return launch_early(split16_kernel, std::min<int64_t>((a.s.rows + 7) / 8, 1 << 20), 256, 0, st, a,
-                        wide);
+    return launch_early(two ? prepare_kernel<true> : prepare_kernel<false>, total, 256, 0, st, a);
 }
 
 // Eight codes a thread, in one load where rows are aligned.
-__global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restrict__ codes,
-                                                          int64_t ldc,
-                                                          const float* __restrict__ scales,
-                                                          int64_t rows, int cols, int per_block,
-                                                          uint64_t m, int wide,
-                                                          uint16_t* __restrict__ dst, int64_t ldd) {
-    next_early();
-    wait_before();
-    const int pieces = (cols + 7) / 8;
-    const int64_t row0 = (int64_t)blockIdx.x * per_block;
+__device__ __forceinline__ void split_codes_rows(const CodesArgs& a, int64_t block) {
+    const int8_t* codes = a.codes;
+    const float* scales = a.scales;
+    uint16_t* dst = a.dst;
+    const int64_t ldc = a.ldc, ldd = a.ldd, rows = a.rows;
+    const int cols = a.cols, per_block = a.per_block, wide = a.wide, pieces = (cols + 7) / 8;
+    const uint64_t m = a.magic;
+    const int64_t row0 = block * per_block;
     const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
 #pragma unroll 2
     for (uint32_t i = threadIdx.x; i < total; i += 256) {
@@ -918,15 +1005,27 @@ __global__ void __launch_bounds__(256) split_codes_kernel(const int8_t* __restri
     }
 }
 
-cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows,
-                               int cols, uint16_t* dst, int64_t ldd, cudaStream_t st) {
-    if (rows <= 0) return cudaSuccess;
-    const int pieces = (cols + 7) / 8;
-    const int per_block = std::max(1, 512 / pieces);
-    const int wide = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 8 == 0;
+// The operands of a weight gradient from kept rows: codes, and dy where it is copied.
+__global__ void __launch_bounds__(256) codes_kernel(const CodesArgs c, const SplitArgs s,
+                                                    int64_t blocks) {
+    next_early();
+    wait_before();
+    if (blockIdx.x < blocks)
+        split_rows(s, blockIdx.x, blocks);
+    else
+        split_codes_rows(c, blockIdx.x - blocks);
+}
+
+cudaError_t launch_codes(CodesArgs c, SplitArgs s, cudaStream_t st) {
+    const int pieces = (c.cols + 7) / 8;
+    c.per_block = std::max(1, 512 / pieces);
+    c.magic = (1ull << 40) / pieces + 1;
+    c.wide = (reinterpret_cast<uintptr_t>(c.codes) & 7u) == 0 && c.ldc % 8 == 0;
+    const int64_t first = s.dst ? plan_split(s) : 0;
+    const int64_t total = first + (c.rows + c.per_block - 1) / c.per_block;
+    if (total > 0x7fffffff) return cudaErrorInvalidValue;
     count_launches(1);
-    return launch_early(split_codes_kernel, (rows + per_block - 1) / per_block, 256, 0, st, codes, ldc,
-                        scales, rows, cols, per_block, (1ull << 40) / pieces + 1, wide, dst, ldd);
+    return launch_early(codes_kernel, total, 256, 0, st, c, s, first);
 }
 
 // ---- host side ---------------------------------------------------------------------

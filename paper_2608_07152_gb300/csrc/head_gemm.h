@@ -209,6 +209,8 @@ struct SplitArgs {
     uint16_t* dst;
     int64_t ldd, part_stride;
     int parts, to_f16;
+    int per_block, wide;         // set by the launch: rows a block, aligned rows, and
+    uint64_t magic;              // n / pieces of a row as n magic / 2^40
 };
 cudaError_t launch_split(const SplitArgs& a, cudaStream_t st);
 
@@ -223,10 +225,40 @@ struct Split16Args {
     int64_t part16_stride;
     float* units;
 };
-cudaError_t launch_split16(const Split16Args& a, cudaStream_t st);
-// Codes as bf16 (exact), or times their rows' scales, rounded to bf16.
-cudaError_t launch_split_codes(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows,
-                               int cols, uint16_t* dst, int64_t ldd, cudaStream_t st);
+
+// A row of the backward pass from the forward pass's statistics.
+struct RowArgs {
+    const float4* stats;
+    const float* grad;
+    const int64_t* targets;
+    int64_t rows, items, ignore_index;
+    const float* up;             // f16: the power of two of every gradient, or null
+    GradRow* out;                // null: no rows
+    int* bad_masked;             // cleared
+};
+
+// Up to two copies (of 16-bit operands, or of float32 ones with both kinds of parts) and
+// the rows, in one launch.
+struct PrepareArgs {
+    Split16Args copy[2];         // s.rows 0: none; dst16 null: as launch_split
+    int64_t blocks[2];           // set by the launch
+    RowArgs rows;
+};
+cudaError_t launch_prepare(PrepareArgs& a, cudaStream_t st);
+
+// Int8 codes as bf16 (exact), or times their rows' scales, rounded to bf16; in the same
+// launch a copy, where s.dst is given.
+struct CodesArgs {
+    const int8_t* codes;
+    int64_t ldc, rows;
+    int cols;
+    const float* scales;
+    uint16_t* dst;
+    int64_t ldd;
+    int per_block, wide;         // set by the launch, as in SplitArgs
+    uint64_t magic;
+};
+cudaError_t launch_codes(CodesArgs c, SplitArgs s, cudaStream_t st);
 
 // A product's tiles; splits and everything else are the caller's.
 inline void set_tiles(Problem& p, int64_t m, int64_t n, int bn, int64_t k, int cta) {

@@ -197,38 +197,6 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
     up[1] = exp2f((float)-e);
 }
 
-struct RowArgs {
-    pvs_xent_args a;
-    const float4* stats;
-    const float* grad;
-    const float* up;             // or null
-    GradRow* out;
-    int* bad_masked;             // cleared
-};
-__global__ void __launch_bounds__(256) xent_rows_kernel(const RowArgs r) {
-    next_early();
-    wait_before();
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i == 0) *r.bad_masked = 0;
-    if (i >= r.a.rows) return;
-    const float4 st = r.stats[i];
-    const int64_t y = r.a.targets[i];
-    GradRow o{0.0f, 0.0f, 0.0f, -1};
-    if (y != r.a.ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
-        const float g = r.grad[i] * (r.up ? *r.up : 1.0f);
-        o.m = st.x;
-        if (y < 0 || y >= r.a.items) {
-            o.coef = o.hit = __int_as_float(0x7fffffff);
-        } else {
-            o.coef = g / st.y;
-            o.hit = g * st.z;
-            // (a masked target has no logit, and no gradient of its own)
-            if (st.w != -INFINITY) o.y = (int)y;
-        }
-    }
-    r.out[i] = o;
-}
-
 // ---- the plan of a call --------------------------------------------------------------
 // float32 operands: the logits' product takes them in two f16 parts with a power of two
 // for each row and item, which its epilogue undoes (three products, the fourth is below
@@ -429,7 +397,9 @@ SplitArgs split_of(const pvs_xent_args& a, const Plan& p) {
     return s;
 }
 
-cudaError_t copy_rows(const pvs_xent_args& a, const Plan& p, bool zero_ignored, cudaStream_t st) {
+// The copy of x (backward: without the rows that have no gradient, whatever they hold:
+// it must not meet G's zeros), and that of the items [v0, v0 + n) without masked ones.
+Split16Args rows_copy(const pvs_xent_args& a, const Plan& p, bool zero_ignored) {
     SplitArgs s = split_of(a, p);
     s.src = a.x;
     s.ld = a.ldx;
@@ -437,12 +407,9 @@ cudaError_t copy_rows(const pvs_xent_args& a, const Plan& p, bool zero_ignored, 
     s.dst = p.x;
     s.part_stride = a.rows * p.ldp;
     if (zero_ignored) s.zero_target = a.targets;
-    if (p.two) return launch_split16(Split16Args{s, p.x16, a.rows * p.ldp, p.xunit}, st);
-    return launch_split(s, st);
+    return Split16Args{s, p.x16, a.rows * p.ldp, p.xunit};
 }
-
-cudaError_t copy_items(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_t n,
-                       const int* only_if, cudaStream_t st) {
+Split16Args items_copy(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_t n) {
     SplitArgs s = split_of(a, p);
     s.src = static_cast<const uint8_t*>(a.w) + v0 * a.ldw * element_bytes(a.dtype);
     s.ld = a.ldw;
@@ -450,9 +417,7 @@ cudaError_t copy_items(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_
     s.dst = p.w;
     s.part_stride = p.piece * p.ldp;
     if (a.bias) s.zero_bias = a.bias + v0;
-    s.only_if = only_if;
-    if (p.two) return launch_split16(Split16Args{s, p.w16, p.piece * p.ldp, p.wunit}, st);
-    return launch_split(s, st);
+    return Split16Args{s, p.w16, p.piece * p.ldp, p.wunit};
 }
 
 Softmax softmax_of(const pvs_xent_args& a) {
@@ -468,7 +433,6 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
                     float* stats, cudaStream_t st) {
     cudaError_t e = cudaSuccess;
     const int64_t T = a.rows, V = a.items;
-    if (p.copy_x) e = copy_rows(a, p, false, st);
     Args g{};
     g.status = dev.status;
     g.sm = softmax_of(a);
@@ -476,7 +440,10 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     g.sm.targets = a.targets;
     for (int64_t v0 = 0; v0 < V && e == cudaSuccess; v0 += p.piece) {
         const int64_t n = std::min(p.piece, V - v0);
-        if (p.copy_w) e = copy_items(a, p, v0, n, nullptr, st);
+        PrepareArgs c{};
+        if (p.copy_x && v0 == 0) c.copy[0] = rows_copy(a, p, false);
+        if (p.copy_w) c.copy[1] = items_copy(a, p, v0, n);
+        e = launch_prepare(c, st);
         if (e != cudaSuccess) break;
         g.sm.part0 = (int)(v0 / p.piece * p.piece_tiles);
         e = logits(kStats, g, p, a, v0, n, dev, st);
@@ -504,20 +471,20 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         e = launch_early(xent_grad_scale_kernel, 1, 1024, 0, st, grad_loss, a.targets, a.ignore_index,
                          T, up);
     }
-    if (e != cudaSuccess) return e;
-    count_launches(1);
-    e = launch_early(xent_rows_kernel, (T + 255) / 256, 256, 0, st,
-                     RowArgs{a, reinterpret_cast<const float4*>(stats), grad_loss,
-                             p.f16 ? up : nullptr, p.row, bad_masked});
-    // x without the rows that have no gradient: what they hold must not meet G's zeros
-    if (e == cudaSuccess) e = copy_rows(a, p, true, st);
     const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
     const float* alpha = p.f16 ? undo : nullptr;
     for (int64_t v0 = 0, i = 0; v0 < V && e == cudaSuccess; v0 += p.piece, ++i) {
         const int64_t n = std::min(p.piece, V - v0);
         const Matrix direct{a.w, V, a.dim, a.ldw, 1, 0};
         const Matrix copied{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
-        if (p.copy_w) e = copy_items(a, p, v0, n, nullptr, st);
+        PrepareArgs c{};
+        if (i == 0) {
+            c.copy[0] = rows_copy(a, p, true);
+            c.rows = RowArgs{reinterpret_cast<const float4*>(stats), grad_loss, a.targets, T, V,
+                             a.ignore_index, p.f16 ? up : nullptr, p.row, bad_masked};
+        }
+        if (p.copy_w) c.copy[1] = items_copy(a, p, v0, n);
+        e = launch_prepare(c, st);
         if (e != cudaSuccess) break;
         Args g{};
         g.status = dev.status;
@@ -533,7 +500,11 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         if (alt) g.sm.bad_masked = bad_masked;
         e = logits(kGrad, g, p, a, v0, n, dev, st);
         // a masked item that holds NaN or infinities: dx takes w from a copy with zeros there
-        if (e == cudaSuccess && alt && dx) e = copy_items(a, p, v0, n, bad_masked, st);
+        if (e == cudaSuccess && alt && dx) {
+            SplitArgs s = items_copy(a, p, v0, n).s;
+            s.only_if = bad_masked;
+            e = launch_split(s, st);
+        }
         if (e != cudaSuccess) break;
         const Matrix gm{p.g, T, n, p.ldg, p.parts, T * p.ldg};
         g.nprob = 0;
