@@ -81,7 +81,7 @@ typedef struct pvs_xent_args {
     int64_t ignore_index;
     int32_t dim;              /* 1 .. 32767                                    */
     int32_t dtype;            /* pvs_dtype of x, w and their gradients         */
-    float scale;              /* a > 0, finite                                 */
+    float scale;              /* a > 0, a normal float32                       */
     int32_t reserved;         /* 0                                             */
 } pvs_xent_args;
 

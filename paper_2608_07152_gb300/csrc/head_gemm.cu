@@ -32,6 +32,7 @@
 
 #include "../../include/head.h"
 #include "alloc.h"
+#include "f32x2.cuh"
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
@@ -450,6 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             const int ncols = min(p.bn, p.n - n0);      // columns of D in the tile
             [[maybe_unused]] int64_t y = -1;
             [[maybe_unused]] float row_k2 = 0.0f;
+            [[maybe_unused]] uint32_t yt = ~0u, targets_in = 0;   // the target's column, chunks with one
             [[maybe_unused]] GradRow gr;
             if constexpr (EPI != kOut) {
                 // the tile's biases, and which of its columns are in the softmax
@@ -478,7 +480,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     y = gr.y < 0 ? -1 : (int64_t)gr.y - (sm.item0 + n0);
                 }
                 row_k2 = sm.row_unit && row < sm.rows ? sm.k2 * __ldg(sm.row_unit + row) : sm.k2;
-                __syncwarp();
+                yt = y >= 0 && y < kTileN ? (uint32_t)y : ~0u;
+                targets_in = __reduce_or_sync(0xffffffffu, yt < kTileN ? 1u << (yt >> 5) : 0u);
                 asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
                 if constexpr (EPI == kStats) {
                     // the tile before this one: all its shares are in shared memory
@@ -551,8 +554,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                             r[i] = __float_as_uint(__uint_as_float(r[i]) *
                                                    (row_k2 * sh.unit[b][cc * 32 + i]));
                     }
+                    // the logits are v f: where nothing but the scale is to be done, one FMA takes
+                    // it and the reference off together
+                    float f = sm.col_unit ? 1.0f : sm.k2;
                     if (sm.bias || mask) {
-                        const float f = sm.col_unit ? 1.0f : sm.k2;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const float l = fmaf(__uint_as_float(r[i]), f, sh.b2[b][cc * 32 + i]);
@@ -561,38 +566,60 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                             // (a masked item's l is -inf unless its product is not finite)
                             if (EPI == kGrad) bad |= out && !(l == -INFINITY);
                         }
+                        f = 1.0f;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            v[i] = sm.col_unit ? __uint_as_float(r[i]) : __uint_as_float(r[i]) * sm.k2;
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
                     }
-                    // the column of the row's target, as a bit
-                    const int64_t yr = y - cc * 32;
-                    const uint32_t here = yr >= 0 && yr < 32 ? 1u << (int)yr : 0u;
-                    const bool any_here = __any_sync(0xffffffffu, here != 0);
+                    // the column of the row's target, as a bit, where a row has one here
+                    const bool any_here = (targets_in >> cc) & 1u;
+                    const uint32_t here = (yt >> 5) == (uint32_t)cc ? 1u << (yt & 31u) : 0u;
+                    const uint64_t ff = f2_pack(f, f);
                     if constexpr (EPI == kStats) {
                         if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 v[i] = here & (1u << i) ? -INFINITY : v[i];
                         }
-                        float cm = v[0];
+                        float c0 = v[0], c1 = v[1];
 #pragma unroll
-                        for (int i = 1; i < 32; ++i) cm = fmaxf(cm, v[i]);
-                        const float nm = fmaxf(mx, cm);
+                        for (int i = 2; i < 32; i += 2) {
+                            c0 = fmaxf(c0, v[i]);
+                            c1 = fmaxf(c1, v[i + 1]);
+                        }
+                        const float nm = fmaxf(mx, fmaxf(c0, c1) * f);
                         const float ref = nm == -INFINITY ? 0.0f : nm;
-                        float part = 0.0f;
+                        const uint64_t off = f2_pack(-ref, -ref);
+                        uint64_t s0 = 0, s1 = 0;                 // pairs of zeros
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) part += ex2(v[i] - ref);
-                        sum = sum * ex2(mx - ref) + part;
+                        for (int i = 0; i < 32; i += 4) {
+                            float e0, e1, e2, e3;
+                            f2_unpack(f2_fma(f2_pack(v[i], v[i + 1]), ff, off), e0, e1);
+                            f2_unpack(f2_fma(f2_pack(v[i + 2], v[i + 3]), ff, off), e2, e3);
+                            s0 = f2_add(s0, f2_pack(ex2(e0), ex2(e1)));
+                            s1 = f2_add(s1, f2_pack(ex2(e2), ex2(e3)));
+                        }
+                        float p0, p1;
+                        f2_unpack(f2_add(s0, s1), p0, p1);
+                        sum = sum * ex2(mx - ref) + (p0 + p1);
                         mx = nm;
                     } else {
                         if (bad && row < sm.rows && sm.bad_masked)
                             *reinterpret_cast<volatile int*>(sm.bad_masked) = 1;
-                        const bool none = gr.coef == 0.0f && gr.hit == 0.0f;
+                        if (gr.coef == 0.0f && gr.hit == 0.0f) {
+                            // (whatever the row holds)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            v[i] = none ? 0.0f : ex2(v[i] - gr.m) * gr.coef;
+                            for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                        } else {
+                            const uint64_t off = f2_pack(-gr.m, -gr.m), by = f2_pack(gr.coef, gr.coef);
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                float e0, e1;
+                                f2_unpack(f2_fma(f2_pack(v[i], v[i + 1]), ff, off), e0, e1);
+                                f2_unpack(f2_mul(f2_pack(ex2(e0), ex2(e1)), by), v[i], v[i + 1]);
+                            }
+                        }
+                        __syncwarp();
                         if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)

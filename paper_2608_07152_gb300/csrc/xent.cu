@@ -232,7 +232,7 @@ bool aligned(const void* p, int64_t ld, int dtype) {
 bool valid(const pvs_xent_args* a) {
     if (!a || a->rows < 0 || a->rows > kMaxRows || a->items < 1 || a->items > kMaxRows ||
         a->dim < 1 || a->dim > kMaxDim || a->dtype < PVS_BF16 || a->dtype > PVS_F32 ||
-        a->reserved != 0 || !(a->scale > 0.0f) || !std::isfinite(a->scale) || a->ldx < a->dim ||
+        a->reserved != 0 || !(a->scale >= 0x1p-126f) || !std::isfinite(a->scale) || a->ldx < a->dim ||
         a->ldw < a->dim)
         return false;
     return a->w && (a->rows == 0 || (a->x && a->targets));
