@@ -204,10 +204,11 @@ __device__ __forceinline__ void codes_of(const float (&v)[N], float s, float r, 
 
 // TPR threads per row hold it in registers: read once, the maximum, the codes, the
 // activation.  N elements (8, or 1 where nothing is aligned) make a piece; a thread
-// holds NV pieces of 8 elements' worth.  Rows without gaps of any width are cut into
-// the aligned eights of the whole matrix: a row's first and last piece may hold
-// elements of its neighbours, which are left out.
-template <int TYPE, int N, int NV, int TPR>
+// holds NV pieces of 8 elements' worth.  FLAT: rows without gaps of any width are cut
+// into the aligned eights of the whole matrix: a row's first and last piece may hold
+// elements of its neighbours, which are left out (aligned rows took 107 us that way
+// where they take 74 without its checks).
+template <int TYPE, int N, int NV, int TPR, bool FLAT>
 __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict__ x, int64_t ldx,
                                                          int64_t rows, int cols, int act,
                                                          int8_t* __restrict__ codes, int64_t ldc,
@@ -220,20 +221,21 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
     const bool live = row < rows;
-    // (the three leading dimensions agree modulo 8 where N is 8)
-    const int before = N == 1 ? 0 : (int)(row * ldx & 7);
+    // (the three leading dimensions are the width then)
+    const int before = FLAT ? (int)(row * ldx & 7) : 0;
     const int pieces = (before + cols + N - 1) / N;
     float v[kPieces][N];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         const int j = i * TPR + lane, e = j * N - before;    // the piece's first element
-        if (live && j < pieces && e >= 0 && e + N <= cols) {
+        if (live && j < pieces && (!FLAT || (e >= 0 && e + N <= cols))) {
             load_elements<TYPE, N>(x, row * ldx + e, v[i]);
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 float one[1] = {0.0f};
-                if (live && e + k >= 0 && e + k < cols) load_elements<TYPE, 1>(x, row * ldx + e + k, one);
+                if (FLAT && live && e + k >= 0 && e + k < cols)
+                    load_elements<TYPE, 1>(x, row * ldx + e + k, one);
                 v[i][k] = one[0];
             }
         }
@@ -263,7 +265,7 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
     for (int i = 0; i < kPieces; ++i) {
         const int j = i * TPR + lane, e = j * N - before;
         if (j >= pieces) break;
-        const bool whole = N == 1 || (e >= 0 && e + N <= cols);
+        const bool whole = !FLAT || (e >= 0 && e + N <= cols);
         uint32_t c[N];
         if (finite) {
             codes_of<N>(v[i], s, r, fast, c);
@@ -411,28 +413,28 @@ bool by_eight(const void* p, int64_t ld, int elem) {
     return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(std::min(8 * elem, 16) - 1)) == 0 && ld % 8 == 0;
 }
 
-template <int TYPE, int N, int NV, int TPR>
+template <int TYPE, int N, int NV, int TPR, bool FLAT>
 cudaError_t store_launch(const void* x, int64_t ldx, int64_t rows, int cols, int act, int8_t* codes,
                   int64_t ldc, float* scales, void* y, int64_t ldy, cudaStream_t st) {
     constexpr int kRows = 256 / TPR;
-    return launch_early(ckpt_store_kernel<TYPE, N, NV, TPR>, (rows + kRows - 1) / kRows, 256, 0, st, x,
+    return launch_early(ckpt_store_kernel<TYPE, N, NV, TPR, FLAT>, (rows + kRows - 1) / kRows, 256, 0, st, x,
                         ldx, rows, cols, act, codes, ldc, scales, y, ldy);
 }
 
 // The narrowest layout that holds a row: a warp up to 2048 elements, else a block.
-template <int TYPE, int N, typename... A>
+template <int TYPE, int N, bool FLAT, typename... A>
 cudaError_t store_rows(int cols, A... a) {
     // (a row may reach into one piece more than its width makes)
-    const int nv = (cols + (N == 8 && cols % 8 != 0 ? 14 : 0) + 255) / 256;
-    if (nv <= 1) return store_launch<TYPE, N, 1, 32>(a...);
-    if (nv <= 2) return store_launch<TYPE, N, 2, 32>(a...);
-    if (nv <= 3) return store_launch<TYPE, N, 3, 32>(a...);
-    if (nv <= 4) return store_launch<TYPE, N, 4, 32>(a...);
-    if (nv <= 6) return store_launch<TYPE, N, 6, 32>(a...);
-    if (nv <= 8) return store_launch<TYPE, N, 8, 32>(a...);
-    if (nv <= 16) return store_launch<TYPE, N, 2, 256>(a...);
-    if (nv <= 32) return store_launch<TYPE, N, 4, 256>(a...);
-    return store_launch<TYPE, N, 16, 256>(a...);
+    const int nv = (cols + (FLAT ? 14 : 0) + 255) / 256;
+    if (nv <= 1) return store_launch<TYPE, N, 1, 32, FLAT>(a...);
+    if (nv <= 2) return store_launch<TYPE, N, 2, 32, FLAT>(a...);
+    if (nv <= 3) return store_launch<TYPE, N, 3, 32, FLAT>(a...);
+    if (nv <= 4) return store_launch<TYPE, N, 4, 32, FLAT>(a...);
+    if (nv <= 6) return store_launch<TYPE, N, 6, 32, FLAT>(a...);
+    if (nv <= 8) return store_launch<TYPE, N, 8, 32, FLAT>(a...);
+    if (nv <= 16) return store_launch<TYPE, N, 2, 256, FLAT>(a...);
+    if (nv <= 32) return store_launch<TYPE, N, 4, 256, FLAT>(a...);
+    return store_launch<TYPE, N, 16, 256, FLAT>(a...);
 }
 
 // Matrices without gaps that start aligned.
@@ -553,12 +555,15 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
                        by_eight(codes, dense ? 8 : ldcodes, 1) &&
                        (act == PVS_ACT_NONE || by_eight(y, dense ? 8 : ldy, es)) &&
                        cols <= 32767 - 8;
-    if (eight)
-        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 8>(cols, x, ldx, rows, cols, act, codes, ldcodes,
-                                                scales, y, ldy, st)));
+    if (eight && cols % 8 != 0)
+        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 8, true>(cols, x, ldx, rows, cols, act, codes,
+                                                          ldcodes, scales, y, ldy, st)));
+    else if (eight)
+        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 8, false>(cols, x, ldx, rows, cols, act, codes,
+                                                           ldcodes, scales, y, ldy, st)));
     else
-        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 1>(cols, x, ldx, rows, cols, act, codes, ldcodes,
-                                                scales, y, ldy, st)));
+        PVS_BY_TYPE(dtype, e = (store_rows<TYPE, 1, false>(cols, x, ldx, rows, cols, act, codes,
+                                                           ldcodes, scales, y, ldy, st)));
     return queued(e);
 }
 
