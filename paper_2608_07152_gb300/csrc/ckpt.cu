@@ -503,11 +503,9 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     const int64_t slots = tile_m > kTileM ? dev.pairs : dev.sms;
     const int64_t units = (int64_t)((out_cols + tile_m - 1) / tile_m) * ((cols + bn - 1) / bn);
     const int64_t kc = (rows + kTileK - 1) / kTileK;
-    // enough splits for every SM, none under 8 chunks
-    int64_t s = std::max<int64_t>(1, std::min<int64_t>(slots / std::min<int64_t>(units, slots), kc / 8));
-    // float32 sums: 128 steps at most before the splits are added with rounding
-    if (dtype == PVS_F32) s = std::max<int64_t>(s, (kc + 31) / 32);
-    p.splits = even_splits(kc, s);
+    // float32 sums: 128 steps in the tensor cores, which cut the sum to 24 bits each, at
+    // most before the splits are added with rounding
+    p.splits = best_splits(units, kc, (int)slots, p.parts, dtype == PVS_F32 ? (kc + 31) / 32 : 1);
     Carver c{static_cast<uint8_t*>(workspace)};
     if (p.copy) p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
     p.b = c.take<uint16_t>(rows * p.ldb);

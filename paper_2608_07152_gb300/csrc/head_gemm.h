@@ -280,6 +280,33 @@ inline int even_splits(int64_t kchunks, int64_t want) {
     return (int)((kchunks + len - 1) / len);
 }
 
+// What a unit of `chunks` chunks takes, in the time of a chunk's MMAs: 1.3 times its
+// chunks and 7 more (10 where it leaves float32 sums for splits), as dw's tiles of 1, 4 and
+// 16 chunks did (64, 256 and 1024 rows over a million items: 8, 10.5 and 27).
+inline double unit_cost(int64_t chunks, bool sums) { return 1.3 * (double)chunks + (sums ? 10 : 7); }
+// And for the whole launch: a split tile's store and its later read, and the launch
+// that adds the splits.
+inline double sums_cost(int64_t tiles, int slots) { return 12.0 * (double)tiles / slots; }
+constexpr double kSumsLaunch = 16;
+
+// The splits of k of a product with the launch to itself, u tiles of k chunks, npairs of
+// parts, no fewer than `fewest`.
+inline int best_splits(int64_t u, int64_t k, int slots, int npairs, int64_t fewest) {
+    double least = 1e300;
+    int64_t best = 1;
+    for (int64_t s = fewest; s <= k && (s == fewest || u * s <= 8 * slots);
+         s += s / 8 > 1 ? s / 8 : 1) {
+        const double cost = (double)((u * s + slots - 1) / slots) *
+                                unit_cost((k + s - 1) / s * npairs, s > 1) +
+                            (s > 1 ? sums_cost(u * s, slots) + kSumsLaunch : 0.0);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return even_splits(k, best);
+}
+
 // Scratch of one call, carved from the caller's workspace in 256-byte steps.
 struct Carver {
     uint8_t* base;

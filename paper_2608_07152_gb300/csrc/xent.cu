@@ -241,10 +241,8 @@ bool valid(const pvs_xent_args* a) {
 // How dx (u0 tiles, k0 chunks of k) and dw (u1, k1) share the `slots` CTAs or pairs
 // of one launch: each gets slots of its own, and its k is cut where that evens the
 // ends.  The cost of a choice, in the time of a chunk's MMAs (npairs of them a
-// chunk), is the longer side's rounds of units, and what the splits' sums move.  A
-// unit takes 1.3 times its chunks and 7 more (10 where it leaves float32 sums): what
-// dw's tiles took with 1, 4 and 16 chunks (64, 256 and 1024 rows: 8, 10.5 and 27).
-double unit_cost(int64_t chunks, bool sums) { return 1.3 * (double)chunks + (sums ? 10 : 7); }
+// chunk), is the longer side's rounds of units (unit_cost), and what the splits' sums
+// move.
 struct Division {
     int xsplits = 1, wsplits = 1, slots0 = 1;
 };
@@ -253,8 +251,6 @@ Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int n
                 int64_t xleast, int64_t wleast, bool accumulate) {
     Division best;
     double least = 1e300;
-    // a split tile's store and its later read, and the launch that adds the splits
-    const double sum = 2.0 * 6 / slots, launch = 16;
     for (int64_t wsplits = wleast; wsplits <= k1; wsplits *= 2) {
         if (wsplits > wleast && u1 * wsplits > 8 * slots) break;
         const double w1 = unit_cost((k1 + wsplits - 1) / wsplits * npairs, wsplits > 1);
@@ -275,8 +271,8 @@ Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int n
                 // splits over every slot: a quarter of its time counts too)
                 const double x_alone = (double)((n0 + slots - 1) / slots) * w0;
                 const double cost = std::max(t0, t1) + 0.25 * x_alone +
-                                    sum * ((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0)) +
-                                    launch * ((xsplits > 1 || accumulate) + (wsplits > 1));
+                                    sums_cost((xsplits > 1 ? n0 : 0) + (wsplits > 1 ? n1 : 0), slots) +
+                                    kSumsLaunch * ((xsplits > 1 || accumulate) + (wsplits > 1));
                 if (cost < least) {
                     least = cost;
                     best.xsplits = (int)xsplits;
