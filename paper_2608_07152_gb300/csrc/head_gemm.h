@@ -163,22 +163,6 @@ inline int tile_columns(int64_t n) {
     return (int)((w + 31) / 32 * 32);
 }
 
-// Columns per tile of n logits for `mtiles` tiles of rows on `slots` CTAs or pairs: where
-// the tiles make few rounds, narrower ones can end sooner (a tile costs its columns and
-// about 32 more).  777 rows over 20,011 items are 5 rounds of 256 columns, or 5 of 224.
-inline int logit_columns(int64_t n, int64_t mtiles, int slots) {
-    int best = kTileN;
-    int64_t least = INT64_MAX;
-    for (int bn = kTileN; bn >= 128; bn -= 32) {
-        const int64_t cost = (mtiles * ((n + bn - 1) / bn) + slots - 1) / slots * (bn + 32);
-        if (cost < least) {
-            least = cost;
-            best = bn;
-        }
-    }
-    return n >= best ? best : tile_columns(n);
-}
-
 // The part pairs of a product of operands in `pa` and `pb` parts, i and j of one pair
 // adding up to `levels` at most.
 void part_pairs(Args& a, int pa, int pb, int levels = 2);

@@ -307,9 +307,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     }
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
-    const int rows_cta = ctas_for(T, dev);
-    p.bnl = logit_columns(std::min(piece, V), (T + kTileM * rows_cta - 1) / (kTileM * rows_cta),
-                          rows_cta == 2 ? dev.pairs : dev.sms);
+    p.bnl = std::min(piece, V) >= kTileN ? kTileN : tile_columns(V);
     // (a piece's tiles of logits: their statistics are numbered on from piece to piece)
     p.piece_tiles = (piece + p.bnl - 1) / p.bnl;
     Carver c{static_cast<uint8_t*>(workspace)};
