@@ -20,6 +20,7 @@
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
+#include "xent_few.h"
 
 namespace pvs {
 namespace head {
@@ -216,6 +217,8 @@ struct Plan {
     int bnl = 0;                // columns per tile of the logits
     int bnd = 0;                // columns per tile of the gradients
     int xsplits = 1, wsplits = 1, slots0 = 0;
+    int few = 0;                // few float32 rows: those kernels' blocks
+    float* few_g = nullptr;
     // workspace
     uint16_t *x = nullptr, *w = nullptr, *g = nullptr;
     float2* part = nullptr;
@@ -285,6 +288,11 @@ Division divide(int64_t u0, int64_t k0, int64_t u1, int64_t k1, int slots, int n
     return best;
 }
 
+// Whether a call's rows are few enough for the kernels that take w as it is.
+bool few_rows(const pvs_xent_args& a) {
+    return a.dtype == PVS_F32 && a.dim <= kFewDim && a.rows <= kFewRows;
+}
+
 Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace) {
     Plan p;
     const int64_t T = a.rows, V = a.items;
@@ -293,6 +301,20 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     p.two = a.dtype == PVS_F32;
     p.ldp = copied_ld(a.dim);
     p.lds = round_up(a.dim, 8);
+    if (few_rows(a)) {
+        Carver c{static_cast<uint8_t*>(workspace)};
+        p.few = few_blocks(V, dev);
+        if (!backward) {
+            p.part = c.take<float2>(p.few * T);
+        } else {
+            p.row = c.take<GradRow>(T);
+            p.words = c.take<unsigned int>(64);
+            p.few_g = c.take<float>(V * few_rows_padded(T));
+            p.xslots = c.take<float>(p.few * T * p.lds);
+        }
+        p.bytes = c.used;
+        return p;
+    }
     p.copy_x = !aligned(a.x, a.ldx, a.dtype);
     p.copy_w = !aligned(a.w, a.ldw, a.dtype);
     int64_t piece = round_up(V, kTileN);
@@ -423,16 +445,39 @@ Softmax softmax_of(const pvs_xent_args& a) {
     return s;
 }
 
+FewArgs few_args(const pvs_xent_args& a) {
+    FewArgs f{};
+    f.x = static_cast<const float*>(a.x);
+    f.ldx = a.ldx;
+    f.rows = (int)a.rows;
+    f.w = static_cast<const float*>(a.w);
+    f.ldw = a.ldw;
+    f.items = a.items;
+    f.dim = a.dim;
+    f.k2 = a.scale * kLog2e;
+    f.bias = a.bias;
+    f.targets = a.targets;
+    f.ignore_index = a.ignore_index;
+    f.scale = a.scale;
+    return f;
+}
+
 cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, float* loss,
                     float* stats, cudaStream_t st) {
     cudaError_t e = cudaSuccess;
     const int64_t T = a.rows, V = a.items;
+    if (p.few) {
+        FewArgs f = few_args(a);
+        f.part = p.part;
+        f.part_rows = T;
+        e = launch_few_stats(f, p.few, st);
+    }
     Args g{};
     g.status = dev.status;
     g.sm = softmax_of(a);
     g.sm.part = p.part;
     g.sm.targets = a.targets;
-    for (int64_t v0 = 0; v0 < V && e == cudaSuccess; v0 += p.piece) {
+    for (int64_t v0 = 0; !p.few && v0 < V && e == cudaSuccess; v0 += p.piece) {
         const int64_t n = std::min(p.piece, V - v0);
         PrepareArgs c{};
         if (p.copy_x && v0 == 0) c.copy[0] = rows_copy(a, p, false);
@@ -444,8 +489,9 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     }
     if (e != cudaSuccess) return e;
     const int64_t last = V - (p.pieces - 1) * p.piece;
-    const JoinArgs j{p.part, (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl, a, a.scale * kLog2e,
-                     !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
+    const int64_t tiles = p.few ? p.few : (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl;
+    const JoinArgs j{p.part, tiles, a, a.scale * kLog2e,
+                     a.dtype != PVS_F32 && !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
                      reinterpret_cast<float4*>(stats)};
     count_launches(1);
     if (T >= 4 * dev.sms) return launch_early(xent_join_kernel<8>, (T + 7) / 8, 256, 0, st, j);
@@ -464,6 +510,25 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         count_launches(1);
         e = launch_early(xent_grad_scale_kernel, 1, 1024, 0, st, grad_loss, a.targets, a.ignore_index,
                          T, up);
+    }
+    if (p.few) {
+        PrepareArgs c{};
+        c.rows = RowArgs{reinterpret_cast<const float4*>(stats), grad_loss, a.targets, T, V,
+                         a.ignore_index, nullptr, p.row, bad_masked};
+        e = launch_prepare(c, st);
+        FewArgs f = few_args(a);
+        f.row = p.row;
+        f.g = p.few_g;
+        f.slots = dx ? p.xslots : nullptr;
+        f.slot_stride = T * p.lds;
+        f.ldslot = p.lds;
+        f.dw = static_cast<float*>(dw);
+        f.lddw = lddw;
+        if (e == cudaSuccess) e = launch_few_grads(f, p.few, st);
+        if (e == cudaSuccess && dx)
+            e = launch_sum_slots(p.xslots, p.few, T * p.lds, p.lds, T, a.dim, nullptr, a.scale, dx,
+                                 lddx, a.dtype, st);
+        return e;
     }
     const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
     const float* alpha = p.f16 ? undo : nullptr;
