@@ -207,7 +207,9 @@ __device__ __forceinline__ void codes_of(const float (&v)[N], float s, float r, 
 // holds NV pieces of 8 elements' worth.  FLAT: rows without gaps of any width are cut
 // into the aligned eights of the whole matrix: a row's first and last piece may hold
 // elements of its neighbours, which are left out (aligned rows took 107 us that way
-// where they take 74 without its checks).
+// where they take 74 without its checks; element by element, 40,000 rows of 1,001 took
+// 271 us with the load, in eights 92).
+// 32,768 rows of 1,536 in bf16 with GELU: 43 us, 5.7 TB/s (issue 65%).
 template <int TYPE, int N, int NV, int TPR, bool FLAT>
 __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict__ x, int64_t ldx,
                                                          int64_t rows, int cols, int act,
@@ -306,6 +308,8 @@ __global__ void __launch_bounds__(256) ckpt_store_kernel(const void* __restrict_
 // What the codes stand for (DY: times dy act').  A block takes `per_block` rows;
 // a thread's pieces of N elements run over them.  n / pieces by a product:
 // m = floor(2^40 / pieces) + 1 is exact for n < 2^23 and pieces < 2^16.
+// 32,768 x 1,536 in bf16: 29 us (5.2 TB/s), with dy act' 55 us (4.6 TB/s; issue 70%: the
+// error function and the exponential).
 template <int TYPE, int N, bool DY>
 __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__ dy, int64_t lddy,
                                                         const int8_t* __restrict__ codes,
@@ -349,7 +353,8 @@ __global__ void __launch_bounds__(256) ckpt_load_kernel(const void* __restrict__
 
 // The same for matrices without gaps of any width: the aligned eights of the whole
 // matrix, which may hold the end of one row and the start of the next (rows are 8
-// elements long at least).
+// elements long at least).  With dy, and the product after it, 32,768 rows of 1,001 took
+// 138 us this way and 367 element by element.
 template <int TYPE, bool DY>
 __global__ void __launch_bounds__(256) ckpt_load_flat_kernel(const void* __restrict__ dy,
                                                              const int8_t* __restrict__ codes,

@@ -5,7 +5,12 @@
 // rows of A and half of B's rows, 32 KB a chunk.  A lone CTA needs 48 KB for 128 x
 // 256, and its shared memory (fills and the MMAs' reads, 192 bytes a cycle at
 // full rate where 128 are there) kept the tensor cores 62% busy; lone CTAs (kCta = 1)
-// serve the products of 128 rows or fewer, which memory bounds.
+// serve the products of 128 rows or fewer, which memory bounds (a loss of 100 rows over
+// 500,000 items of 768: 125 us, in pairs 132; of 256 rows 140 in pairs, 155 in lone CTAs).
+//
+// 8,192 rows over 8,192 items of 768 in bf16: statistics 68 us (1.50 PFLOP/s, tensor
+// pipe 71% busy), G 74 us (66%), dx and dw 150 us (1.37 PFLOP/s, 76%).  What is lost is
+// the last, half empty, of 14 rounds of tiles, and with short k the epilogue.
 //   warp 0     TMA producer (both CTAs): chunks of A (128 x 64) and B into a ring,
 //              128-byte swizzle, the pair's bytes counted on the even CTA's barrier;
 //   warp 1     one thread (of the even CTA) issues the MMAs (M = 128 or 256, N = bn,
@@ -223,7 +228,8 @@ struct Units {
 };
 
 // 32 float32 values of one row to `out` of any type: whole sectors where the
-// row is aligned, else one by one.  `valid` of them exist.
+// row is aligned, 16 bytes at a time where it is to those (a step of 9 rows over 300,000
+// items of 1,000 in bf16: 600 us, 1,077 by store_block), else one by one.  `valid` of them exist.
 __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const float (&v)[32],
                                           int valid) {
     if (type == PVS_F32) {
@@ -232,6 +238,10 @@ __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
                 store_32b(o + i, reinterpret_cast<const uint32_t*>(&v[i]));
+        } else if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+                *reinterpret_cast<float4*>(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -248,6 +258,10 @@ __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const
     if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 31u) == 0) {
         store_32b(o, w);
         store_32b(o + 16, w + 8);
+    } else if (valid == 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint4*>(o + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
     } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -256,7 +270,7 @@ __device__ __forceinline__ void store_row(void* out, int type, int64_t at, const
 }
 
 // A block of 32 rows of `out` (a row per lane, `rows` and `valid` columns of which exist)
-// that is not whole aligned sectors: turned round among the warp's lanes, so that
+// that is not whole and aligned to 16 bytes: turned round among the warp's lanes, so that
 // neighbours write neighbours.  Element by element from a row's lane, dw of 900,000 items
 // of 385 (16 rows, bf16) made a step of 5,845 us; this way it takes 2,047.
 __device__ __forceinline__ void store_block(void* out, int type, int64_t at, int64_t ld,
@@ -536,10 +550,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             const uint32_t tcol =
                 tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * kTileN);
             [[maybe_unused]] float mx = -INFINITY, sum = 0.0f;
-            // (rows of D in `out` start on a sector, and so do their chunks)
+            // (rows of D in `out` start on 16 bytes, and so do their chunks)
             [[maybe_unused]] const bool out_whole =
                 ((reinterpret_cast<uintptr_t>(p.out) |
-                  (uintptr_t)p.ldout * (p.out_type == PVS_F32 ? 4 : 2)) & 31u) == 0;
+                  (uintptr_t)p.ldout * (p.out_type == PVS_F32 ? 4 : 2)) & 15u) == 0;
             for (int cc = group; cc * 32 < p.bn; cc += kEpiGroups) {
                 uint32_t r[32];
                 __syncwarp();
@@ -713,30 +727,46 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
 }
 
 // ---- sums over the splits ------------------------------------------------------
-// Four columns a thread; a block takes `per_block` rows, n / pieces by a product
-// (m = floor(2^40 / pieces) + 1, exact for n < 2^23 and pieces < 2^16).
-__global__ void __launch_bounds__(256) sum_slots_kernel(const float* __restrict__ slots, int splits,
-                                                        int64_t slot_stride, int64_t ldslot,
-                                                        int64_t rows, int n, int per_block,
-                                                        uint64_t m,
-                                                        const float* __restrict__ alpha,
-                                                        float alpha0, void* __restrict__ out,
-                                                        int64_t ldout, int out_type) {
+// Four columns a thread, all of them added in the splits' order.  Small blocks of one
+// round each: what a sum waits for is its chain of loads (8 rows of 768
+// from 152 splits took 66 us with two rounds a block, 38 in one).
+constexpr int kSumThreads = 128;
+__global__ void __launch_bounds__(kSumThreads) sum_slots_kernel(
+    const float* __restrict__ slots, int splits, int64_t slot_stride, int64_t ldslot, int64_t rows,
+    int n, int blocks_per_row, int rows_per_block, const float* __restrict__ alpha, float alpha0,
+    void* __restrict__ out, int64_t ldout, int out_type) {
     next_early();
     wait_before();
     const int pieces = (n + 3) / 4;
-    const int64_t row0 = (int64_t)blockIdx.x * per_block;
-    const uint32_t total = (uint32_t)(min((int64_t)per_block, rows - row0) * pieces);
     const float f = alpha ? alpha0 * __ldg(alpha) : alpha0;
-    for (uint32_t i = threadIdx.x; i < total; i += 256) {
-        const uint32_t r = (uint32_t)((i * m) >> 40);
-        const int64_t row = row0 + r;
-        const int col = (int)(i - r * (uint32_t)pieces) * 4;
+    int64_t row = (int64_t)blockIdx.x * rows_per_block;
+    int piece = threadIdx.x;
+    if (blocks_per_row > 1) {
+        row = blockIdx.x / blocks_per_row;
+        piece += (int)(blockIdx.x % blocks_per_row) * kSumThreads;
+    } else {
+        row += threadIdx.x / pieces;
+        piece = threadIdx.x % pieces;
+        if (threadIdx.x >= rows_per_block * pieces) return;
+    }
+    if (row < rows && piece < pieces) {
+        const int col = piece * 4;
         // (a slot's rows are padded to eight columns)
         const float* p = slots + row * ldslot + col;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        // (sixteen loads in flight; added in the splits' order)
+        int k = 0;
+        for (; k + 16 <= splits; k += 16) {
+            float4 v[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                v[u] = __ldg(reinterpret_cast<const float4*>(p + (k + u) * slot_stride));
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                s.x += v[u].x, s.y += v[u].y, s.z += v[u].z, s.w += v[u].w;
+        }
 #pragma unroll 4
-        for (int k = 0; k < splits; ++k) {
+        for (; k < splits; ++k) {
             const float4 v = __ldg(reinterpret_cast<const float4*>(p + k * slot_stride));
             s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
         }
@@ -772,11 +802,13 @@ cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
                              int64_t ldout, int out_type, cudaStream_t st) {
     const int pieces = (n + 3) / 4;
-    const int per_block = std::max(1, 512 / pieces);
+    const int blocks_per_row = (pieces + kSumThreads - 1) / kSumThreads;
+    const int rows_per_block = std::max(1, kSumThreads / pieces);
+    const int64_t blocks = blocks_per_row > 1 ? m * blocks_per_row : (m + rows_per_block - 1) / rows_per_block;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     count_launches(1);
-    return launch_early(sum_slots_kernel, (m + per_block - 1) / per_block, 256, 0, st, slots, splits,
-                        slot_stride, ldslot, m, n, per_block, (1ull << 40) / pieces + 1, alpha,
-                        alpha0, out, ldout, out_type);
+    return launch_early(sum_slots_kernel, blocks, kSumThreads, 0, st, slots, splits, slot_stride, ldslot,
+                        m, n, blocks_per_row, rows_per_block, alpha, alpha0, out, ldout, out_type);
 }
 
 // ---- operands in 16-bit parts ----------------------------------------------------
@@ -930,43 +962,80 @@ __device__ __forceinline__ void store_parts(const Split16Args& a, int64_t at, fl
     }
 }
 
-// A warp per row: up to 1024 elements in registers, all loads in flight at once (read
-// twice, 200 rows over 100,003 items of 385 took 189 us in all); longer rows are read
-// twice, the second time from L1.
+// Rows to a warp at a time: four of up to 256 elements, two of up to 512, else one.
+__host__ __device__ __forceinline__ int rows_of_warp(int cols) {
+    return cols <= 256 ? 4 : cols <= 512 ? 2 : 1;
+}
+
+// A warp holds up to 1024 elements of its ROWS rows in registers, all loads in flight at
+// once (read twice, 200 rows over 100,003 items of 385 took 189 us in all; with a row to
+// a warp, 401,423 items of 128 took 181 us, with four 108); longer rows are read twice,
+// the second time from L1.
+template <int ROWS>
 __device__ __forceinline__ void split16_rows(const Split16Args& a, int64_t block, int64_t blocks) {
-    constexpr int kHeld = 4;
+    constexpr int kHeld = 4 / ROWS;
     const SplitArgs& s = a.s;
     const int lane = threadIdx.x & 31;
-    for (int64_t row = block * 8 + (threadIdx.x >> 5); row < s.rows; row += blocks * 8) {
-        const bool zero = (s.zero_target && s.zero_target[row] == s.ignore_index) ||
-                          (s.zero_bias && s.zero_bias[row] == -INFINITY);
-        const float* x = static_cast<const float*>(s.src) + row * s.ld;
-        const int cols = zero ? 0 : s.cols;       // (a zero row: nothing is read)
-        float v[kHeld][8], top = 0.0f;
+    for (int64_t first = (block * 8 + (threadIdx.x >> 5)) * ROWS; first < s.rows;
+         first += blocks * 8 * ROWS) {
+        float v[ROWS][kHeld][8];
+        int cols[ROWS];
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) load_eight_floats(x, lane * 8 + 256 * i, cols, s.wide, v[i]);
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) top = finite_top(v[i], top);
-        for (int k = lane * 8 + 256 * kHeld; k < cols; k += 256) {
-            float w[8];
-            load_eight_floats(x, k, cols, s.wide, w);
-            top = finite_top(w, top);
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t row = min(first + r, s.rows - 1);
+            const bool zero = (s.zero_target && s.zero_target[row] == s.ignore_index) ||
+                              (s.zero_bias && s.zero_bias[row] == -INFINITY);
+            cols[r] = zero ? 0 : s.cols;          // (a zero row: nothing is read)
         }
-        top = warp_max(top);
-        const int e = top > 0.0f ? min(13 - ilogbf(top), 126) : 0;
-        const float up = exp2f((float)e);
-        if (lane == 0) a.units[row] = exp2f((float)-e);
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            const int k = lane * 8 + 256 * i;
-            if (k < s.cols) store_parts(a, row * s.ldd + k, v[i], up);
+        for (int r = 0; r < ROWS; ++r) {
+            const float* x = static_cast<const float*>(s.src) + min(first + r, s.rows - 1) * s.ld;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                load_eight_floats(x, lane * 8 + 256 * i, cols[r], s.wide, v[r][i]);
         }
-        for (int k = lane * 8 + 256 * kHeld; k < s.cols; k += 256) {
-            float w[8];
-            load_eight_floats(x, k, cols, s.wide, w);
-            store_parts(a, row * s.ldd + k, w, up);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t row = first + r;
+            if (row >= s.rows) break;
+            const float* x = static_cast<const float*>(s.src) + row * s.ld;
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) top = finite_top(v[r][i], top);
+            if (ROWS == 1) {
+                for (int k = lane * 8 + 256 * kHeld; k < cols[r]; k += 256) {
+                    float w[8];
+                    load_eight_floats(x, k, cols[r], s.wide, w);
+                    top = finite_top(w, top);
+                }
+            }
+            top = warp_max(top);
+            const int e = top > 0.0f ? min(13 - ilogbf(top), 126) : 0;
+            const float up = exp2f((float)e);
+            if (lane == 0) a.units[row] = exp2f((float)-e);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                const int k = lane * 8 + 256 * i;
+                if (k < s.cols) store_parts(a, row * s.ldd + k, v[r][i], up);
+            }
+            if (ROWS == 1) {
+                for (int k = lane * 8 + 256 * kHeld; k < s.cols; k += 256) {
+                    float w[8];
+                    load_eight_floats(x, k, cols[r], s.wide, w);
+                    store_parts(a, row * s.ldd + k, w, up);
+                }
+            }
         }
     }
+}
+__device__ __forceinline__ void split16_any(const Split16Args& a, int64_t block, int64_t blocks) {
+    const int n = rows_of_warp(a.s.cols);
+    if (n == 4)
+        split16_rows<4>(a, block, blocks);
+    else if (n == 2)
+        split16_rows<2>(a, block, blocks);
+    else
+        split16_rows<1>(a, block, blocks);
 }
 
 // The rows of the backward pass.
@@ -992,7 +1061,8 @@ __device__ __forceinline__ void prepare_row(const RowArgs& r, int64_t i) {
 }
 
 // What a pass does before its first product, in one launch: its copies, and the
-// backward pass's rows, each on blocks of its own.
+// backward pass's rows, each on blocks of its own.  Memory bounds it: 400,000 rows of 385 in
+// 16 bits 124 us (5.0 TB/s), 401,423 float32 rows of 128 in two parts 108 us (3.8 TB/s).
 template <bool TWO>
 __global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
     next_early();
@@ -1002,7 +1072,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
     for (int i = 0; i < 2; ++i) {
         if (b < a.blocks[i]) {
             if (TWO)
-                split16_rows(a.copy[i], b, a.blocks[i]);
+                split16_any(a.copy[i], b, a.blocks[i]);
             else
                 split_rows(a.copy[i].s, b, a.blocks[i]);
             return;
@@ -1023,7 +1093,10 @@ cudaError_t launch_prepare(PrepareArgs& a, cudaStream_t st) {
         }
         two = c.dst16 != nullptr;
         a.blocks[i] = plan_split(c.s);
-        if (two) a.blocks[i] = std::min<int64_t>((c.s.rows + 7) / 8, 1 << 20);
+        if (two) {
+            const int n = 8 * rows_of_warp(c.s.cols);
+            a.blocks[i] = std::min<int64_t>((c.s.rows + n - 1) / n, 1 << 20);
+        }
         total += a.blocks[i];
     }
     if (a.rows.out) total += (a.rows.rows + 255) / 256;
@@ -1072,6 +1145,7 @@ __device__ __forceinline__ void split_codes_rows(const CodesArgs& a, int64_t blo
 }
 
 // The operands of a weight gradient from kept rows: codes, and dy where it is copied.
+// 32,768 x 768 codes to bf16 in 15 us (5 TB/s; issue 77%).
 __global__ void __launch_bounds__(256) codes_kernel(const CodesArgs c, const SplitArgs s,
                                                     int64_t blocks) {
     next_early();

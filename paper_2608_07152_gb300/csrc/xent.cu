@@ -9,7 +9,9 @@
 //
 // Every logit costs 2 d operations in the forward pass and 6 d in the backward
 // pass: bound by the tensor cores unless there are few rows, when w (and dw) bound
-// it.  G of a piece is written once and read twice.
+// it.  G of a piece is written once and read twice.  With both gradients, bf16: 8,192
+// rows over 8,192 items of 768 0.30 ms, 256 rows over 1,000,000 items 1.5 ms; f16: 4,096
+// rows over 200,000 items of 1,024 4.7 ms.
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -94,7 +96,9 @@ __device__ __forceinline__ void join(float& m, float& s, float2 p) {
 // the largest and the one that the loss subtracts.  Left out of the tiles' sums, it
 // also leaves 1 - p exact where p is near 1.
 // R rows a block; a warp's lanes run over the rows first (the tiles' statistics
-// are stored by rows).
+// are stored by rows).  Eight where that still gives every SM four blocks' rows, else one:
+// 8,192 rows over as many items of 768 take a loss of 73 us with eight, 89 with one; 500 rows
+// over 100,000 of 256 take 35 and 38, 64 over 500,000 63 and 53.
 template <int R>
 __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
     constexpr int kLanes = 256 / R;

@@ -15,8 +15,8 @@
 // of w from L1 and L2, took 1,640 us for 8 rows over 700,000 items of 768.)
 //
 // 700,000 items of 768, in us: the loss of 8 rows 411 (5.2 TB/s of w; on the tensor cores,
-// with the copies, 1,178), of 16 rows 544 (1,174); a step of 8 rows 1,712 (4,870), of 16
-// rows 2,306 (4,801).  Up to 8 rows the memory bounds it, at 16 the products' reads of x
+// with the copies, 1,178), of 16 rows 544 (1,174); a step of 8 rows 1,683 (4,870), of 16
+// rows 2,271 (4,801).  Up to 8 rows the memory bounds it, at 16 the products' reads of x
 // from shared memory and the FMAs.  More rows go to the tensor cores: 32 in two turns took
 // 1,131 where those take 1,173.
 #include "xent_few.h"
