@@ -70,6 +70,7 @@ pvs_status pvs_head_status(void);
  * bf16 and f16 products are exact.  float32 operands enter the logits as pairs
  * of f16 with a power of two for each row and item, and the gradients as three
  * bf16 parts; what is left out of a product is about 2^-22 of it.
+ * Up to 16 float32 rows of dim <= 1024 are multiplied in float32 as they are.
  * ------------------------------------------------------------------------ */
 typedef struct pvs_xent_args {
     const void* x;            /* [rows x dim], leading dimension ldx           */
@@ -102,7 +103,8 @@ pvs_status pvs_xent_forward(const pvs_xent_args* args, float* loss, float* stats
  * computed again, a piece of the items at a time, and G = dloss/dl of the
  * piece is kept in the workspace, for bf16 rounded to bf16 (2^-8 of each
  * entry, what rounding dx and dw loses too), for f16 to f16 after a common
- * scaling to the largest |grad_loss|, for float32 as three bf16 parts. */
+ * scaling to the largest |grad_loss|, for float32 as three bf16 parts (up to
+ * 16 rows of dim <= 1024: in float32, of all items at once). */
 pvs_status pvs_xent_backward(const pvs_xent_args* args, const float* stats,
                              const float* grad_loss, void* dx, int64_t lddx, void* dw,
                              int64_t lddw, void* workspace, size_t workspace_bytes,
