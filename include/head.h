@@ -103,7 +103,8 @@ pvs_status pvs_xent_forward(const pvs_xent_args* args, float* loss, float* stats
  * computed again, a piece of the items at a time, and G = dloss/dl of the
  * piece is kept in the workspace, for bf16 rounded to bf16 (2^-8 of each
  * entry, what rounding dx and dw loses too), for f16 to f16 after a common
- * scaling to the largest |grad_loss|, for float32 as three bf16 parts (up to
+ * scaling to the largest |grad_loss|, both in two such parts for up to 128
+ * rows (nothing then shows of it), for float32 as three bf16 parts (up to
  * 16 rows of dim <= 1024: in float32, of all items at once). */
 pvs_status pvs_xent_backward(const pvs_xent_args* args, const float* stats,
                              const float* grad_loss, void* dx, int64_t lddx, void* dw,

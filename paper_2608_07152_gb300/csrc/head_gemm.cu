@@ -165,6 +165,15 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t ad, uint64_t bd, uint32
         tc::mma_bf16(d, ad, bd, idesc, acc);
 }
 
+// Two values rounded to f16, and what is left of them (nothing of what is not finite).
+__device__ __forceinline__ uint32_t cut_f16(float& x, float& y) {
+    const uint32_t h = pack_f16(x, y);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    x = isfinite(f.x) ? x - f.x : 0.0f;
+    y = isfinite(f.y) ? y - f.y : 0.0f;
+    return h;
+}
+
 // The units of one slot (a CTA, or a pair): those of one problem, `step` apart.  A unit
 // is a tile and a range of k; the next one is found by additions with carries (its
 // division by the tiles, in each of the three roles, cost a short unit as much as its
@@ -686,7 +695,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
 #pragma unroll
                                 for (int i = 0; i < 16; ++i)
                                     h[i] = part + 1 < sm.grad_parts
-                                               ? cut_bf16(v[2 * i], v[2 * i + 1])
+                                               ? (sm.grad_f16 ? cut_f16(v[2 * i], v[2 * i + 1])
+                                                              : cut_bf16(v[2 * i], v[2 * i + 1]))
                                            : sm.grad_f16 ? pack_f16(v[2 * i], v[2 * i + 1])
                                                          : pack_bf16(v[2 * i], v[2 * i + 1]);
                                 store_32b(o, h);

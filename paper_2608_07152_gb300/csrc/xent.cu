@@ -207,8 +207,14 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
 // for each row and item, which its epilogue undoes (three products, the fourth is below
 // 2^-22 of an element); the gradients' products, whose sums run over those rows and
 // items, in three bf16 parts (six products).
+// 16-bit operands: G in one part costs a gradient about what its own rounding does.  In one
+// tile of rows, where memory bounds the products, G has two parts: errors of dx and dw of
+// 10 rows over 866 items of 768 in bf16 2.7e-3 -> 1.65e-3, the result's own rounding.  A step
+// of 64 rows over 700,000 items of 768 takes 987 us so, 786 with one part; of 100 over 3,000 of
+// 256 62, 58.  In more rows the products would take twice as long.
 struct Plan {
     int parts = 1, f16 = 0;     // of the gradients' operands
+    int gparts = 1;             // of G
     bool two = false;           // the logits' operands are f16 pairs
     uint16_t *x16 = nullptr, *w16 = nullptr;
     float *xunit = nullptr, *wunit = nullptr;
@@ -302,6 +308,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     const int64_t T = a.rows, V = a.items;
     p.parts = parts_of(a.dtype);
     p.f16 = a.dtype == PVS_F16;
+    p.gparts = p.parts == 1 && T <= kTileM ? 2 : p.parts;
     p.two = a.dtype == PVS_F32;
     p.ldp = copied_ld(a.dim);
     p.lds = round_up(a.dim, 8);
@@ -328,7 +335,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         piece = std::min(piece, std::max<int64_t>(most, 4 * kTileN));
     }
     if (backward) {
-        const int64_t most = (int64_t)(kGradBytes / ((size_t)p.parts * T * 2)) / kTileN * kTileN;
+        const int64_t most = (int64_t)(kGradBytes / ((size_t)p.gparts * T * 2)) / kTileN * kTileN;
         piece = std::min(piece, std::max<int64_t>(most, 4 * kTileN));
     }
     p.piece = piece;
@@ -351,13 +358,13 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         p.row = c.take<GradRow>(T);
         p.words = c.take<unsigned int>(64);
         p.ldg = piece;
-        p.g = c.take<uint16_t>((int64_t)p.parts * T * p.ldg);
+        p.g = c.take<uint16_t>((int64_t)p.gparts * T * p.ldg);
         p.bnd = tile_columns(a.dim);
         const int64_t first = std::min(piece, V);
         const int64_t nt = (a.dim + p.bnd - 1) / p.bnd;
         const int cta = ctas_for(std::max(T, first), dev);
         const int tile = kTileM * cta;
-        const int slots = cta == 2 ? dev.pairs : dev.sms, npairs = a.dtype == PVS_F32 ? 6 : 1;
+        const int slots = cta == 2 ? dev.pairs : dev.sms, npairs = a.dtype == PVS_F32 ? 6 : p.gparts;
         const int64_t ux = (T + tile - 1) / tile * nt, kx = (first + kTileK - 1) / kTileK;
         const int64_t uw = (first + tile - 1) / tile * nt, kw = (T + kTileK - 1) / kTileK;
         // float32 sums: each step in the tensor cores cuts the sum to 24 bits, 64 steps
@@ -557,7 +564,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         g.sm.grad = p.g;
         g.sm.ldg = p.ldg;
         g.sm.grad_part = T * p.ldg;
-        g.sm.grad_parts = p.parts;
+        g.sm.grad_parts = p.gparts;
         g.sm.grad_f16 = p.f16;
         const bool alt = !p.copy_w && a.bias;
         if (alt) g.sm.bad_masked = bad_masked;
@@ -569,7 +576,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             e = launch_split(s, st);
         }
         if (e != cudaSuccess) break;
-        const Matrix gm{p.g, T, n, p.ldg, p.parts, T * p.ldg};
+        const Matrix gm{p.g, T, n, p.ldg, p.gparts, T * p.ldg};
         g.nprob = 0;
         g.f16 = p.f16;
         // dw's tiles have items for rows: pairs unless all of it is one CTA's tile
@@ -621,7 +628,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         }
         if (g.nprob == 0) break;
         if (n == std::min(p.piece, V)) g.slots0 = p.slots0;   // (the last piece: by its work)
-        part_pairs(g, p.parts, p.parts);
+        part_pairs(g, p.gparts, p.parts);
         e = launch_gemm(kOut, g, dev, st);
         if (e == cudaSuccess && qw && qw->to_slots)
             e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.lds, n, a.dim, alpha,
