@@ -1,4 +1,5 @@
-"""Softmax cross entropy of up to 16 float32 rows, which takes the items as they lie.
+"""Softmax cross entropy of few rows: up to 16 float32 rows, which take the items as they
+lie, and up to 128 of 16 bits, whose gradients are as exact as their own rounding.
 
 Against the same definition in binary64 and with the same bounds as the other row
 counts: a logit's float32 sum has d / 32 + 5 steps here, a sum over items one step for
@@ -10,7 +11,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pvs = pytest.importorskip("paper_2608_07152_gb300")
 
-from test_gpu_head_xent import F32, INF, check, close, make, reference, step  # noqa: E402
+from test_gpu_head_xent import (BF16, F16, F32, INF, TINY, UNIT, check, close, make,  # noqa: E402
+                                reference, step)
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +91,27 @@ def test_gradient_against_differences():
     tol = (tdx * u.abs()).sum() + (tdw * v.abs()).sum() + h * h * third * grad.abs().sum() + 1e-9
     assert (slope - along).abs() <= tol
     close(dx, reference(*case)[0][1], tdx)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("T,V,d", [(1, 616, 1024), (10, 866, 200), (128, 3000, 64)])
+def test_16_bit_gradients_show_their_own_rounding_only(T, V, d, dtype):
+    # G in two parts: cut to 8 bits, the rest rounded to 8 (bf16), 2^-15 of an entry; f16
+    # leaves less.  Each of the two products has its steps.  The rest as in the bounds
+    # of one part, without that part's rounding.
+    x, w, y, bias, grad, scale = make(T, V, d, dtype, masked=0.1)
+    _, dx, dw = step(x, w, y, bias, grad, scale)
+    (_, want_x, want_w), _ = reference(x, w, y, bias, grad, scale)
+    X, W = x.double(), torch.where((bias == -INF)[:, None], 0.0, w.double())
+    l = scale * (X @ W.T) + bias.double()
+    p = torch.softmax(l, dim=1)
+    G = (p - torch.nn.functional.one_hot(y, V)) * grad.double()[:, None]
+    finite = torch.where(torch.isfinite(l), l.abs(), torch.zeros_like(l))
+    e = ((d / 16 + 4) * 2.0 ** -23 * scale * (X.abs() @ W.abs().T) + 2.0 ** -22 * finite).amax(dim=1)
+    aG = G.abs() * (2.0 ** -15 + 2 * e + 2.0 ** -19)[:, None]
+    if dtype == F16:   # entries below the scaled f16's last bit
+        aG = aG + grad.abs().max().double() * 2.0 ** -37
+    unit = UNIT[dtype] * 1.001
+    for got, want, other, a, g in ((dx, want_x, W.abs(), aG, G.abs()), (dw, want_w, X.abs(), aG.T, G.abs().T)):
+        steps = 2 * (other.shape[0] / 16 + 8) * 2.0 ** -23
+        close(got, want, scale * (a @ other + steps * (g @ other)) + unit * want.abs() + TINY[dtype])
