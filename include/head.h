@@ -101,11 +101,10 @@ pvs_status pvs_xent_forward(const pvs_xent_args* args, float* loss, float* stats
  * dimension lddx) and dw [items x dim] (lddw), of the operands' type, each
  * rounded once from its float32 sum; either may be null.  The logits are
  * computed again, a piece of the items at a time, and G = dloss/dl of the
- * piece is kept in the workspace, for bf16 rounded to bf16 (2^-8 of each
- * entry, what rounding dx and dw loses too), for f16 to f16 after a common
- * scaling to the largest |grad_loss|, both in two such parts for up to 128
- * rows (nothing then shows of it), for float32 as three bf16 parts (up to
- * 16 rows of dim <= 1024: in float32, of all items at once). */
+ * piece is kept in the workspace: in two bf16 parts for bf16, in two f16 parts
+ * after a common scaling to the largest |grad_loss| for f16 (2^-15 of each entry is
+ * lost, next to nothing of what rounding dx and dw loses), for float32 in three bf16
+ * parts (up to 16 rows of dim <= 1024: in float32, of all items at once). */
 pvs_status pvs_xent_backward(const pvs_xent_args* args, const float* stats,
                              const float* grad_loss, void* dx, int64_t lddx, void* dw,
                              int64_t lddw, void* workspace, size_t workspace_bytes,

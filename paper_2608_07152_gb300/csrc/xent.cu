@@ -4,14 +4,14 @@
 //   forward    l = a x w^T + b, tile by tile; each tile's rows leave a maximum and
 //              a sum of 2^(l - max), which a second launch joins; no logit is kept
 //   backward   for each piece of the vocabulary: the logits again, and from them
-//              G = g (2^(l - m) / s - [j = y]) in 16 bits; then, in one launch,
+//              G = g (2^(l - m) / s - [j = y]) in 16-bit parts; then, in one launch,
 //              dx += G w and dw = G^T x
 //
-// Every logit costs 2 d operations in the forward pass and 6 d in the backward
+// Every logit costs 2 d operations in the forward pass and 10 d in the backward
 // pass: bound by the tensor cores unless there are few rows, when w (and dw) bound
-// it.  G of a piece is written once and read twice.  With both gradients, bf16: 8,192
-// rows over 8,192 items of 768 0.30 ms, 256 rows over 1,000,000 items 1.5 ms; f16: 4,096
-// rows over 200,000 items of 1,024 4.7 ms.
+// it.  G of a piece is written once and read twice, in two parts, each a product of its
+// own.  With both gradients, bf16: 8,192 rows over 8,192 items of 768 0.49 ms, 256 rows over
+// 1,000,000 items 2.2 ms; f16: 4,096 rows over 200,000 items of 1,024 7.2 ms.
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -207,11 +207,10 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
 // for each row and item, which its epilogue undoes (three products, the fourth is below
 // 2^-22 of an element); the gradients' products, whose sums run over those rows and
 // items, in three bf16 parts (six products).
-// 16-bit operands: G in one part costs a gradient about what its own rounding does.  In one
-// tile of rows, where memory bounds the products, G has two parts: errors of dx and dw of
-// 10 rows over 866 items of 768 in bf16 2.7e-3 -> 1.65e-3, the result's own rounding.  A step
-// of 64 rows over 700,000 items of 768 takes 987 us so, 786 with one part; of 100 over 3,000 of
-// 256 62, 58.  In more rows the products would take twice as long.
+// 16-bit operands: G has two parts, so that a gradient's error is the rounding of its
+// output (bf16 1.7e-3, f16 2.1e-4).  One part would lose as much again (bf16 2.3e-3 to 2.7e-3)
+// and take two thirds of the time: a step of 8,192 rows over 8,192 items of 768 485 us, 302 with
+// one part; of 256 over a million 2,230 and 1,520.
 struct Plan {
     int parts = 1, f16 = 0;     // of the gradients' operands
     int gparts = 1;             // of G
@@ -308,7 +307,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     const int64_t T = a.rows, V = a.items;
     p.parts = parts_of(a.dtype);
     p.f16 = a.dtype == PVS_F16;
-    p.gparts = p.parts == 1 && T <= kTileM ? 2 : p.parts;
+    p.gparts = std::max(2, p.parts);
     p.two = a.dtype == PVS_F32;
     p.ldp = copied_ld(a.dim);
     p.lds = round_up(a.dim, 8);
