@@ -139,8 +139,9 @@ pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const int8_t* cod
 
 /* Weight gradient of a linear layer y = x W^T whose input was kept:
  *     dw[n, k] = sum_r dy[r, n] s_r z[r, k],  dw [out_cols x cols] in dy's type.
- * The codes are exact operands; dy s_r is one bf16 for bf16 dy (2^-8 of each
- * term, what rounding dw loses too), two bf16 parts for f16, three for float32. */
+ * bf16: dy is an exact operand, and s_r z the other in two bf16 parts (2^-15 of a term
+ * is lost).  Else the codes are exact operands, and dy s_r is in two bf16 parts for f16,
+ * three for float32. */
 pvs_status pvs_ckpt_grad_workspace(int64_t rows, int32_t out_cols, int32_t cols, int32_t dtype,
                                    size_t* bytes);
 pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const int8_t* codes,

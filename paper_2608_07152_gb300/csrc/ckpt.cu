@@ -481,10 +481,12 @@ pvs_status queued(cudaError_t e = cudaSuccess) {
     return PVS_ERR_CUDA;
 }
 
-// bf16: dy is an operand as it lies, and the kept rows the other, each a bf16.  f16
-// and float32: dy s in two or three bf16 parts, and the codes as they are (exact).
+// bf16: dy is an operand as it lies, and the kept rows s z the other, in two bf16 parts:
+// what they lose is 2^-15 of an entry.  (In one part they lost about half of what rounding dw
+// does: 2.8e-3 against 2.3e-3 in all.)  f16 and float32: dy s in two or three bf16 parts, and
+// the codes as they are (exact).
 struct GradPlan {
-    int parts;
+    int parts, kept_parts;   // of dy and of the kept rows
     bool scaled;             // the kept rows are the operand, dy has no scale
     bool copy;               // dy is copied
     int64_t lda, ldb;
@@ -500,6 +502,7 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     p.scaled = dtype == PVS_BF16;
     p.copy = !p.scaled || !in_place;
     p.parts = dtype == PVS_BF16 ? 1 : dtype == PVS_F16 ? 2 : 3;
+    p.kept_parts = p.scaled ? 2 : 1;
     p.lda = copied_ld(out_cols);
     p.ldb = copied_ld(cols);
     p.ldslot = round_up(cols, 8);
@@ -510,10 +513,11 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     const int64_t kc = (rows + kTileK - 1) / kTileK;
     // float32 sums: 128 steps in the tensor cores, which cut the sum to 24 bits each, at
     // most before the splits are added with rounding
-    p.splits = best_splits(units, kc, (int)slots, p.parts, dtype == PVS_F32 ? (kc + 31) / 32 : 1);
+    p.splits = best_splits(units, kc, (int)slots, p.parts * p.kept_parts,
+                           dtype == PVS_F32 ? (kc + 31) / 32 : 1);
     Carver c{static_cast<uint8_t*>(workspace)};
     if (p.copy) p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
-    p.b = c.take<uint16_t>(rows * p.ldb);
+    p.b = c.take<uint16_t>((int64_t)p.kept_parts * rows * p.ldb);
     if (p.splits > 1) p.slots = c.take<float>((int64_t)p.splits * out_cols * p.ldslot);
     p.bytes = c.used;
     return p;
@@ -674,6 +678,8 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     c.scales = p.scaled ? scales : nullptr;
     c.dst = p.b;
     c.ldd = p.ldb;
+    c.part_stride = rows * p.ldb;
+    c.parts = p.kept_parts;
     e = launch_codes(c, s, st);
     if (e != cudaSuccess) return queued(e);
     Args g{};
@@ -686,7 +692,7 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     const Matrix a = p.copy ? Matrix{p.a, rows, out_cols, p.lda, p.parts, rows * p.lda}
                             : Matrix{dy, rows, out_cols, lddy, 1, 0};
     if (!operand_map(&q.a, a, true, 0) ||
-        !operand_map(&q.b, Matrix{p.b, rows, cols, p.ldb, 1, 0}, true, 0))
+        !operand_map(&q.b, Matrix{p.b, rows, cols, p.ldb, p.kept_parts, rows * p.ldb}, true, 0))
         return PVS_ERR_CUDA;
     q.a_mn = q.b_mn = 1;
     q.to_slots = p.splits > 1;
@@ -697,7 +703,7 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     q.ldout = lddw;
     q.out_type = dtype;
     q.alpha0 = 1.0f;
-    part_pairs(g, p.parts, 1);
+    part_pairs(g, p.parts, p.kept_parts);
     e = launch_gemm(kOut, g, dev, st);
     if (e == cudaSuccess && q.to_slots)
         e = launch_sum_slots(p.slots, p.splits, q.slot_stride, p.ldslot, out_cols, cols, nullptr,

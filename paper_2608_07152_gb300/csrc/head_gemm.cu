@@ -1148,9 +1148,15 @@ __device__ __forceinline__ void split_codes_rows(const CodesArgs& a, int64_t blo
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? v[k] * s : 0.0f;
-        *reinterpret_cast<uint4*>(dst + row * ldd + col) =
-            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
-                       pack_bf16(v[6], v[7]));
+        for (int part = 0; part < a.parts; ++part) {
+            uint32_t h[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                h[k] = part + 1 < a.parts ? cut_bf16(v[2 * k], v[2 * k + 1])
+                                          : pack_bf16(v[2 * k], v[2 * k + 1]);
+            *reinterpret_cast<uint4*>(dst + part * a.part_stride + row * ldd + col) =
+                make_uint4(h[0], h[1], h[2], h[3]);
+        }
     }
 }
 

@@ -230,15 +230,16 @@ struct PrepareArgs {
 };
 cudaError_t launch_prepare(PrepareArgs& a, cudaStream_t st);
 
-// Int8 codes as bf16 (exact), or times their rows' scales, rounded to bf16; in the same
-// launch a copy, where s.dst is given.
+// Int8 codes as bf16 (exact), or times their rows' scales in `parts` bf16 parts; in the
+// same launch a copy, where s.dst is given.
 struct CodesArgs {
     const int8_t* codes;
     int64_t ldc, rows;
     int cols;
     const float* scales;
     uint16_t* dst;
-    int64_t ldd;
+    int64_t ldd, part_stride;
+    int parts;
     int per_block, wide;         // set by the launch, as in SplitArgs
     uint64_t magic;
 };

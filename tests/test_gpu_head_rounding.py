@@ -10,6 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pvs = pytest.importorskip("paper_2608_07152_gb300")
 
+from test_gpu_head_ckpt import rows  # noqa: E402
 from test_gpu_head_xent import BF16, F16, TINY, UNIT, close, make, reference, step  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +35,15 @@ def test_16_bit_gradients_of_many_rows(T, V, d, dtype):
                                    (dw, want_w, aG.T, G.abs().T, X.abs())):
         steps = 2 * (other.shape[0] / 16 + 8) * 2.0 ** -23
         close(got, want, scale * (a @ other + steps * (g @ other)) + unit * want.abs() + TINY[dtype])
+
+
+@pytest.mark.parametrize("R,N,K", [(7, 9, 17), (64, 128, 256), (300, 130, 385), (1000, 72, 40)])
+def test_bf16_weight_gradients(R, N, K):
+    x, dy = rows(R, K, BF16, 4, spread=0.5), rows(R, N, BF16, 5, spread=0.5)
+    codes, scales, _ = pvs.pvs_ckpt_store(x)
+    dw = pvs.pvs_ckpt_grad_weight(dy, codes, scales)
+    kept = codes.double() * scales.double()[:, None]
+    want = dy.double().T @ kept
+    size = dy.double().abs().T @ kept.abs()
+    close(dw, want, (2.0 ** -15 + 2 * (R / 16 + 8) * 2.0 ** -23) * size
+          + UNIT[BF16] * 1.001 * want.abs() + TINY[BF16])
