@@ -625,8 +625,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                             const float l = fmaf(__uint_as_float(r[i]), f, sh.b2[b][cc * 32 + i]);
                             const bool out = (mask >> i) & 1u;
                             v[i] = out ? -INFINITY : l;
-                            // (a masked item's l is -inf unless its product is not finite)
-                            if (EPI == kGrad) bad |= out && !(l == -INFINITY);
+                            // a masked item that holds an infinity or a NaN has no finite
+                            // product with any row (its l does not tell: -inf for one of -inf)
+                            if (EPI == kGrad)
+                                bad |= out && !(fabsf(__uint_as_float(r[i])) <= 3.402823466e38f);
                         }
                         f = 1.0f;
                     } else {
