@@ -47,7 +47,8 @@ typedef enum pvs_dtype { PVS_BF16 = 0, PVS_F16 = 1, PVS_F32 = 2 } pvs_dtype;
 
 typedef enum pvs_act {
     PVS_ACT_NONE = 0,
-    PVS_ACT_GELU = 1          /* x Phi(x), Phi the normal distribution function */
+    PVS_ACT_GELU = 1          /* x Phi(x), Phi the normal distribution function; +inf
+                                 at +inf, NaN at -inf (-inf times 0) and at NaN */
 } pvs_act;
 
 /* PVS_OK, or the status of an operator whose device-side wait ran out on the

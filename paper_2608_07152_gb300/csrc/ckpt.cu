@@ -137,10 +137,13 @@ __device__ __forceinline__ uint64_t upper_tail(float x0, float x1, float& a0, fl
 // x Phi(x) = max(x, 0) - |x| (1 - Phi(|x|)): the negative side is the tail itself,
 // without a difference from 1.
 __device__ __forceinline__ void gelu2(float& x0, float& x1) {
-    float a0, a1, e0, e1;
+    float a0, a1, e0, e1, y0, y1;
     const uint64_t h = upper_tail(x0, x1, a0, a1, e0, e1);
-    // (-inf, whose tail is 0, gives NaN as the formula does; a NaN stays one through h)
-    f2_unpack(f2_fma(f2_pack(-a0, -a1), h, f2_pack(fmaxf(x0, 0.0f), fmaxf(x1, 0.0f))), x0, x1);
+    f2_unpack(f2_fma(f2_pack(-a0, -a1), h, f2_pack(fmaxf(x0, 0.0f), fmaxf(x1, 0.0f))), y0, y1);
+    // The tail is 0 at an infinity: -inf gives NaN as x Phi(x) does, and +inf has to stay
+    // what it is; a NaN stays one through h.
+    x0 = x0 == INFINITY ? x0 : y0;
+    x1 = x1 == INFINITY ? x1 : y1;
 }
 __device__ __forceinline__ void slope2(float x0, float x1, float& s0, float& s1) {
     float a0, a1, e0, e1, h0, h1;
