@@ -48,7 +48,9 @@ typedef enum pvs_dtype { PVS_BF16 = 0, PVS_F16 = 1, PVS_F32 = 2 } pvs_dtype;
 typedef enum pvs_act {
     PVS_ACT_NONE = 0,
     PVS_ACT_GELU = 1          /* x Phi(x), Phi the normal distribution function; +inf
-                                 at +inf, NaN at -inf (-inf times 0) and at NaN */
+                                 at +inf, NaN at -inf (-inf times 0) and at NaN.
+                                 Its Phi is off by at most 7.5e-8 for bf16 and f16,
+                                 in float32 by (x^2 + 6) 2^-23 of itself */
 } pvs_act;
 
 /* PVS_OK, or the status of an operator whose device-side wait ran out on the

@@ -3,15 +3,19 @@
 Bounds taken before any run.  16-bit gradients: G and kept rows enter their products in two
 16-bit parts, cut to the first and rounded to the second, which leaves 2^-15 of an
 entry (f16 less); a logit's error e is that of the other tests; each of the two
-products has its steps of 2^-23.
+products has its steps of 2^-23.  GELU in float32: x / sqrt(2) is off by 2^-23 of itself, which
+moves 1 - Phi by x^2 + 1 times that, erfcf by four last bits, a product by a half; the
+exponential's argument by x^2 / 4 times 2^-23, itself and its factors by four last bits.
 """
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
 pvs = pytest.importorskip("paper_2608_07152_gb300")
 
 from test_gpu_head_ckpt import rows  # noqa: E402
-from test_gpu_head_xent import BF16, F16, TINY, UNIT, close, make, reference, step  # noqa: E402
+from test_gpu_head_xent import BF16, F16, F32, TINY, UNIT, close, make, reference, step  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +51,20 @@ def test_bf16_weight_gradients(R, N, K):
     size = dy.double().abs().T @ kept.abs()
     close(dw, want, (2.0 ** -15 + 2 * (R / 16 + 8) * 2.0 ** -23) * size
           + UNIT[BF16] * 1.001 * want.abs() + TINY[BF16])
+
+
+@pytest.mark.parametrize("K", [1, 33, 64, 1001, 2100])
+def test_float32_gelu_keeps_its_digits(K):
+    x = torch.linspace(-13.0, 13.0, 5 * K, device="cuda").reshape(5, K)
+    codes, scales, y = pvs.pvs_ckpt_store(x, act=pvs.PVS_ACT_GELU)
+    X = x.double()
+    want = 0.5 * X * torch.erfc(-X / math.sqrt(2.0))
+    close(y, want, (X * X + 6) * 2.0 ** -23 * want.abs() + TINY[F32])
+    # the slope at what the codes stand for
+    X = (codes.float() * scales[:, None]).double()
+    dy = torch.linspace(1.0, 2.0, K, device="cuda").expand(5, K).contiguous()
+    dx = pvs.pvs_ckpt_act_backward(dy, codes, scales, pvs.PVS_ACT_GELU)
+    below = 0.5 * torch.erfc(-X / math.sqrt(2.0))
+    beside = X * torch.exp(-0.5 * X * X) / math.sqrt(2.0 * math.pi)
+    close(dx, dy.double() * (below + beside),
+          (X * X + 8) * 2.0 ** -23 * (below + beside.abs()) * dy.double() + TINY[F32])
