@@ -144,7 +144,9 @@ pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const int8_t* cod
  *     dw[n, k] = sum_r dy[r, n] s_r z[r, k],  dw [out_cols x cols] in dy's type.
  * bf16: dy is an exact operand, and s_r z the other in two bf16 parts (2^-15 of a term
  * is lost).  Else the codes are exact operands, and dy s_r is in two bf16 parts for f16,
- * three for float32. */
+ * three for float32.  Operands are laid out in the workspace a piece of the rows at a
+ * time: 1 GB of them, and 2 GB of float32 sums, or 4,096 rows and one dw in float32
+ * where that is more. */
 pvs_status pvs_ckpt_grad_workspace(int64_t rows, int32_t out_cols, int32_t cols, int32_t dtype,
                                    size_t* bytes);
 pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const int8_t* codes,

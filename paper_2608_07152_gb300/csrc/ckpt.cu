@@ -505,10 +505,14 @@ pvs_status queued(cudaError_t e = cudaSuccess) {
 // what they lose is 2^-15 of an entry.  (In one part they lost about half of what rounding dw
 // does: 2.8e-3 against 2.3e-3 in all.)  f16 and float32: dy s in two or three bf16 parts, and
 // the codes as they are (exact).
+// Rows go by in pieces whose copies take 1 GB (4,096 rows at least), each added to the sums of
+// the one before.
+constexpr int64_t kCopyBytes = (int64_t)1 << 30;
 struct GradPlan {
     int parts, kept_parts;   // of dy and of the kept rows
     bool scaled;             // the kept rows are the operand, dy has no scale
     bool copy;               // dy is copied
+    int64_t piece;           // rows at a time, a multiple of kTileK (or all)
     int64_t lda, ldb;
     int splits;
     uint16_t *a, *b;
@@ -526,19 +530,23 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     p.lda = copied_ld(out_cols);
     p.ldb = copied_ld(cols);
     p.ldslot = round_up(cols, 8);
+    // (the same pieces whether dy is copied or not: the workspace serves both)
+    const int64_t row_bytes = 2 * (p.parts * p.lda + p.kept_parts * p.ldb);
+    p.piece = std::min(rows, std::max<int64_t>(kCopyBytes / row_bytes, 4096) / kTileK * kTileK);
     const int bn = tile_columns(cols);
     const int tile_m = kTileM * ctas_for(out_cols, dev);
     const int64_t slots = tile_m > kTileM ? dev.pairs : dev.sms;
     const int64_t units = (int64_t)((out_cols + tile_m - 1) / tile_m) * ((cols + bn - 1) / bn);
-    const int64_t kc = (rows + kTileK - 1) / kTileK;
+    const int64_t kc = (p.piece + kTileK - 1) / kTileK;
     // float32 sums: 128 steps in the tensor cores, which cut the sum to 24 bits each, at
-    // most before the splits are added with rounding
+    // most before the splits are added with rounding (as far as 2 GB of them go)
+    const int64_t room = std::max<int64_t>(1, ((int64_t)2 << 30) / (out_cols * p.ldslot * 4));
     p.splits = best_splits(units, kc, (int)slots, p.parts * p.kept_parts,
-                           dtype == PVS_F32 ? (kc + 31) / 32 : 1);
+                           dtype == PVS_F32 ? std::min((kc + 31) / 32, room) : 1);
     Carver c{static_cast<uint8_t*>(workspace)};
-    if (p.copy) p.a = c.take<uint16_t>((int64_t)p.parts * rows * p.lda);
-    p.b = c.take<uint16_t>((int64_t)p.kept_parts * rows * p.ldb);
-    if (p.splits > 1) p.slots = c.take<float>((int64_t)p.splits * out_cols * p.ldslot);
+    if (p.copy) p.a = c.take<uint16_t>(p.parts * p.piece * p.lda);
+    p.b = c.take<uint16_t>(p.kept_parts * p.piece * p.ldb);
+    if (p.splits > 1 || p.piece < rows) p.slots = c.take<float>((int64_t)p.splits * out_cols * p.ldslot);
     p.bytes = c.used;
     return p;
 }
@@ -677,56 +685,61 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
         return PVS_ERR_INVALID;
     const pvs_status before = (pvs_status)take_status(dev);
     if (before != PVS_OK) return before;
-    SplitArgs s{};
-    if (p.copy) {
-        s.src = dy;
-        s.ld = lddy;
-        s.rows = rows;
-        s.cols = out_cols;
-        s.dtype = dtype;
-        s.row_scale = p.scaled ? nullptr : scales;
-        s.dst = p.a;
-        s.ldd = p.lda;
-        s.part_stride = rows * p.lda;
-        s.parts = p.parts;
+    for (int64_t r0 = 0; r0 < rows && e == cudaSuccess; r0 += p.piece) {
+        const int64_t n = std::min(p.piece, rows - r0);
+        const void* dy0 = static_cast<const uint8_t*>(dy) + r0 * lddy * (int64_t)es;
+        SplitArgs s{};
+        if (p.copy) {
+            s.src = dy0;
+            s.ld = lddy;
+            s.rows = n;
+            s.cols = out_cols;
+            s.dtype = dtype;
+            s.row_scale = p.scaled ? nullptr : scales + r0;
+            s.dst = p.a;
+            s.ldd = p.lda;
+            s.part_stride = n * p.lda;
+            s.parts = p.parts;
+        }
+        CodesArgs c{};
+        c.codes = codes + r0 * ldcodes;
+        c.ldc = ldcodes;
+        c.rows = n;
+        c.cols = cols;
+        c.scales = p.scaled ? scales + r0 : nullptr;
+        c.dst = p.b;
+        c.ldd = p.ldb;
+        c.part_stride = n * p.ldb;
+        c.parts = p.kept_parts;
+        e = launch_codes(c, s, st);
+        if (e != cudaSuccess) break;
+        Args g{};
+        g.status = dev.status;
+        g.nprob = 1;
+        Problem& q = g.p[0];
+        g.cta = ctas_for(out_cols, dev);
+        set_tiles(q, out_cols, cols, tile_columns(cols), n, g.cta);
+        q.splits = even_splits(q.kchunks, p.splits);
+        const Matrix a = p.copy ? Matrix{p.a, n, out_cols, p.lda, p.parts, n * p.lda}
+                                : Matrix{dy0, n, out_cols, lddy, 1, 0};
+        if (!operand_map(&q.a, a, true, 0) ||
+            !operand_map(&q.b, Matrix{p.b, n, cols, p.ldb, p.kept_parts, n * p.ldb}, true, 0))
+            return PVS_ERR_CUDA;
+        q.a_mn = q.b_mn = 1;
+        q.to_slots = p.slots != nullptr;
+        q.accumulate = r0 > 0;
+        q.slots = p.slots;
+        q.slot_stride = (int64_t)out_cols * p.ldslot;
+        q.ldslot = p.ldslot;
+        q.out = dw;
+        q.ldout = lddw;
+        q.out_type = dtype;
+        q.alpha0 = 1.0f;
+        part_pairs(g, p.parts, p.kept_parts);
+        e = launch_gemm(kOut, g, dev, st);
     }
-    CodesArgs c{};
-    c.codes = codes;
-    c.ldc = ldcodes;
-    c.rows = rows;
-    c.cols = cols;
-    c.scales = p.scaled ? scales : nullptr;
-    c.dst = p.b;
-    c.ldd = p.ldb;
-    c.part_stride = rows * p.ldb;
-    c.parts = p.kept_parts;
-    e = launch_codes(c, s, st);
-    if (e != cudaSuccess) return queued(e);
-    Args g{};
-    g.status = dev.status;
-    g.nprob = 1;
-    Problem& q = g.p[0];
-    g.cta = ctas_for(out_cols, dev);
-    set_tiles(q, out_cols, cols, tile_columns(cols), rows, g.cta);
-    q.splits = p.splits;
-    const Matrix a = p.copy ? Matrix{p.a, rows, out_cols, p.lda, p.parts, rows * p.lda}
-                            : Matrix{dy, rows, out_cols, lddy, 1, 0};
-    if (!operand_map(&q.a, a, true, 0) ||
-        !operand_map(&q.b, Matrix{p.b, rows, cols, p.ldb, p.kept_parts, rows * p.ldb}, true, 0))
-        return PVS_ERR_CUDA;
-    q.a_mn = q.b_mn = 1;
-    q.to_slots = p.splits > 1;
-    q.slots = p.slots;
-    q.slot_stride = (int64_t)out_cols * p.ldslot;
-    q.ldslot = p.ldslot;
-    q.out = dw;
-    q.ldout = lddw;
-    q.out_type = dtype;
-    q.alpha0 = 1.0f;
-    part_pairs(g, p.parts, p.kept_parts);
-    e = launch_gemm(kOut, g, dev, st);
-    if (e == cudaSuccess && q.to_slots)
-        e = launch_sum_slots(p.slots, p.splits, q.slot_stride, p.ldslot, out_cols, cols, nullptr,
-                             1.0f, dw, lddw, dtype, st);
+    if (e == cudaSuccess && p.slots)
+        e = launch_sum_slots(p.slots, p.splits, (int64_t)out_cols * p.ldslot, p.ldslot, out_cols, cols,
+                             nullptr, 1.0f, dw, lddw, dtype, st);
     return queued(e);
 }
