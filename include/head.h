@@ -90,7 +90,9 @@ typedef struct pvs_xent_args {
 } pvs_xent_args;
 
 /* Bytes of scratch for pvs_xent_forward (backward = 0) or pvs_xent_backward
- * (1) of these arguments. */
+ * (1) of these arguments.  Forward: copies of rows that are not 16-bit and aligned
+ * and of 1 GB of such items, and 8 bytes for each row and 256 items of a block of rows
+ * (1 GB, or 1,024 rows). */
 pvs_status pvs_xent_workspace(const pvs_xent_args* args, int32_t backward, size_t* bytes);
 
 /* loss [rows] and stats [rows x 4], both float32, stats 16-byte aligned.  A

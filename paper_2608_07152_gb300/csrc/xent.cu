@@ -2,7 +2,8 @@
 // the product of head_gemm.cu.
 //
 //   forward    l = a x w^T + b, tile by tile; each tile's rows leave a maximum and
-//              a sum of 2^(l - max), which a second launch joins; no logit is kept
+//              a sum of 2^(l - max), which a second launch joins; no logit is kept (of
+//              many rows and items, a block of the rows at a time)
 //   backward   for each piece of the vocabulary: the logits again, and from them
 //              G = g (2^(l - m) / s - [j = y]) in 16-bit parts; then, in one launch,
 //              dx += G w and dw = G^T x
@@ -35,6 +36,10 @@ constexpr double kLn2 = 0.6931471805599453;
 // over a million items took 2.5 ms in pieces of 32 K items, 1.6 ms in 256 K ones.
 constexpr size_t kGradBytes = (size_t)1 << 30;
 constexpr size_t kPartsBytes = (size_t)1 << 30;
+// The tiles' statistics of the forward pass, 8 bytes for each row and tile of items: the rows
+// go by in blocks whose statistics take this much, or of 1,024 (32 bytes an item then).
+constexpr int64_t kStatBytes = (int64_t)1 << 30;
+constexpr int64_t kStatRows = 1024;
 
 __device__ __forceinline__ float element(const void* p, int dtype, int64_t i) {
     if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
@@ -385,6 +390,29 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
     return p;
 }
 
+// Rows of a block of the forward pass.
+int64_t block_rows(const pvs_xent_args& a) {
+    const int64_t most = kStatBytes / (8 * ((a.items + kTileN - 1) / kTileN));
+    return std::min(a.rows, std::max(most / (2 * kTileM) * (2 * kTileM), kStatRows));
+}
+
+// The call for the rows [t0, t0 + n).
+pvs_xent_args rows_of(const pvs_xent_args& a, int64_t t0, int64_t n) {
+    pvs_xent_args b = a;
+    b.x = static_cast<const uint8_t*>(a.x) + t0 * a.ldx * element_bytes(a.dtype);
+    b.targets = a.targets + t0;
+    b.rows = n;
+    return b;
+}
+
+// What the forward pass wants: that of a whole block, or of the last.
+size_t forward_bytes(const pvs_xent_args& a, const Device& dev) {
+    const int64_t block = block_rows(a), last = a.rows - (a.rows - 1) / block * block;
+    if (block == a.rows) return plan_of(a, false, dev, nullptr).bytes;
+    return std::max(plan_of(rows_of(a, 0, block), false, dev, nullptr).bytes,
+                    plan_of(rows_of(a, a.rows - last, last), false, dev, nullptr).bytes);
+}
+
 // Logits of the piece [v0, v0 + n).
 cudaError_t logits(int epilogue, Args& g, const Plan& p, const pvs_xent_args& a, int64_t v0,
                    int64_t n, const Device& dev, cudaStream_t st) {
@@ -654,7 +682,7 @@ extern "C" pvs_status pvs_xent_workspace(const pvs_xent_args* a, int32_t backwar
         cudaGetLastError();
         return PVS_ERR_CUDA;
     }
-    *bytes = plan_of(*a, backward != 0, dev, nullptr).bytes;
+    *bytes = backward ? plan_of(*a, true, dev, nullptr).bytes : forward_bytes(*a, dev);
     return PVS_OK;
 }
 
@@ -679,10 +707,16 @@ extern "C" pvs_status pvs_xent_forward(const pvs_xent_args* a, float* loss, floa
     if (!loss || !stats || (reinterpret_cast<uintptr_t>(stats) & 15u)) return PVS_ERR_INVALID;
     Device dev;
     if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
-    const Plan p = plan_of(*a, false, dev, workspace);
-    const pvs_status s = begin(workspace, workspace_bytes, p.bytes, dev);
+    const pvs_status s = begin(workspace, workspace_bytes, forward_bytes(*a, dev), dev);
     if (s != PVS_OK) return s;
-    return ended(forward(*a, p, dev, loss, stats, static_cast<cudaStream_t>(cuda_stream)));
+    cudaError_t e = cudaSuccess;
+    const int64_t block = block_rows(*a);
+    for (int64_t t0 = 0; t0 < a->rows && e == cudaSuccess; t0 += block) {
+        const pvs_xent_args b = rows_of(*a, t0, std::min(block, a->rows - t0));
+        e = forward(b, plan_of(b, false, dev, workspace), dev, loss + t0, stats + 4 * t0,
+                    static_cast<cudaStream_t>(cuda_stream));
+    }
+    return ended(e);
 }
 
 extern "C" pvs_status pvs_xent_backward(const pvs_xent_args* a, const float* stats,

@@ -41,3 +41,39 @@ def test_weight_gradient_in_pieces_of_rows(dtype, strided):
         at = slice(i, i + (1 << 16))
         want += dy[at].double().T @ (codes[at].double() * scales[at].double()[:, None])
     close(dw, want, (OPERAND[dtype] + (R / 16 + 8) * 2.0 ** -23 + UNIT[dtype]) * want)
+
+
+def xent_args(rows, items, dim, dtype):
+    p = 1 << 20                    # a pointer that nothing reads
+    code = {BF16: pvs.PVS_BF16, F16: pvs.PVS_F16, F32: pvs.PVS_F32}[dtype]
+    return pvs.pvs_xent_args(p, p, p, None, rows, items, dim, dim, -100, dim, code, 1.0, 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("T,V", [(1 << 20, 1 << 20), (1 << 24, 100_000), (5000, 100_000_000)])
+def test_loss_scratch_is_bounded(T, V, dtype):
+    # statistics of a block of rows, and copies of a piece of the items
+    size = ctypes.c_size_t()
+    a = xent_args(T, V, 64, dtype)
+    assert pvs._lib.pvs_xent_workspace(ctypes.byref(a), 0, ctypes.byref(size)) == pvs.PVS_OK
+    assert size.value <= max(2 * GB, 32 * V + GB)
+
+
+@pytest.mark.parametrize("dtype,T,V", [(BF16, 200_003, 200_000), (F32, 180_000, 200_000), (F32, 171_530, 200_000)])
+def test_loss_in_blocks_of_rows(dtype, T, V):
+    # more than 1 GB of statistics; the last block of one call has a few rows
+    d, scale = 8, 3.0
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(T, d, generator=g, device="cuda").to(dtype)
+    w = torch.randn(V, d, generator=g, device="cuda").to(dtype)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    loss, stats = pvs.pvs_xent_forward(x, w, y, scale=scale)
+    assert torch.isfinite(loss).all() and torch.isfinite(stats).all()
+    for at in (slice(0, 40), slice(171_500, 171_530), slice(T - 40, T)):
+        l = scale * (x[at].double() @ w.double().T)
+        want = torch.logsumexp(l, dim=1) - l.gather(1, y[at][:, None])[:, 0]
+        e = (d / 16 + 4) * 2.0 ** -23 * scale * (x[at].double().abs() @ w.double().abs().T).amax(dim=1)
+        close(loss[at], want, 2 * e + 2.0 ** -21 * l.abs().amax(dim=1) + 2.0 ** -19)
+        # s 2^m is the sum of the exponentials
+        total = torch.log(stats[at, 1].double()) + stats[at, 0].double() * 0.6931471805599453
+        close(total, torch.logsumexp(l, dim=1), 2 * e + 2.0 ** -21 * l.abs().amax(dim=1) + 2.0 ** -19)
