@@ -109,7 +109,8 @@ pvs_status pvs_xent_forward(const pvs_xent_args* args, float* loss, float* stats
  * piece is kept in the workspace: in two bf16 parts for bf16, in two f16 parts
  * after a common scaling to the largest |grad_loss| for f16 (2^-15 of each entry is
  * lost, next to nothing of what rounding dx and dw loses), for float32 in three bf16
- * parts (up to 16 rows of dim <= 1024: in float32, of all items at once). */
+ * parts (up to 16 rows of dim <= 1024: in float32).  G takes 1 GB at most, or 1,024
+ * items' where that is more. */
 pvs_status pvs_xent_backward(const pvs_xent_args* args, const float* stats,
                              const float* grad_loss, void* dx, int64_t lddx, void* dw,
                              int64_t lddw, void* workspace, size_t workspace_bytes,

@@ -324,7 +324,8 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
         } else {
             p.row = c.take<GradRow>(T);
             p.words = c.take<unsigned int>(64);
-            p.few_g = c.take<float>(V * few_rows_padded(T));
+            p.piece = std::min(V, (int64_t)(kGradBytes / (4 * few_rows_padded(T))));
+            p.few_g = c.take<float>(p.piece * few_rows_padded(T));
             p.xslots = c.take<float>(p.few * T * p.lds);
         }
         p.bytes = c.used;
@@ -554,15 +555,22 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         c.rows = RowArgs{reinterpret_cast<const float4*>(stats), grad_loss, a.targets, T, V,
                          a.ignore_index, nullptr, p.row, bad_masked};
         e = launch_prepare(c, st);
-        FewArgs f = few_args(a);
-        f.row = p.row;
-        f.g = p.few_g;
-        f.slots = dx ? p.xslots : nullptr;
-        f.slot_stride = T * p.lds;
-        f.ldslot = p.lds;
-        f.dw = static_cast<float*>(dw);
-        f.lddw = lddw;
-        if (e == cudaSuccess) e = launch_few_grads(f, p.few, st);
+        for (int64_t v0 = 0; v0 < V && e == cudaSuccess; v0 += p.piece) {
+            FewArgs f = few_args(a);
+            f.w += v0 * a.ldw;
+            f.items = std::min(p.piece, V - v0);
+            f.item0 = v0;
+            if (a.bias) f.bias += v0;
+            f.row = p.row;
+            f.g = p.few_g;
+            f.slots = dx ? p.xslots : nullptr;
+            f.slot_stride = T * p.lds;
+            f.ldslot = p.lds;
+            f.accumulate = v0 > 0;
+            if (dw) f.dw = static_cast<float*>(dw) + v0 * lddw;
+            f.lddw = lddw;
+            e = launch_few_grads(f, p.few, st);
+        }
         if (e == cudaSuccess && dx)
             e = launch_sum_slots(p.xslots, p.few, T * p.lds, p.lds, T, a.dim, nullptr, a.scale, dx,
                                  lddx, a.dtype, st);

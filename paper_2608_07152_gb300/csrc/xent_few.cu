@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kStatThreads) few_softmax_kernel(const FewArgs
             const float bias = bias_of(a, j);
             float v = 0.0f;
             if (bias != -INFINITY && (gr.coef != 0.0f || gr.hit != 0.0f))
-                v = j == gr.y ? gr.hit : gr.coef * exp2f(fmaf(dots[q], a.k2, bias) - gr.m);
+                v = j + a.item0 == gr.y ? gr.hit : gr.coef * exp2f(fmaf(dots[q], a.k2, bias) - gr.m);
             if (j < a.items) a.g[j * R + lane % R] = v;
         }
     }
@@ -317,8 +317,10 @@ __global__ void __launch_bounds__(kMostThreads, 1) few_columns_kernel(const FewA
                     if (n > 0) v[c] += sum[t * a.dim + k];
                     if (n + 1 < groups)
                         sum[t * a.dim + k] = v[c];
-                    else
-                        a.slots[blockIdx.x * a.slot_stride + t * a.ldslot + k] = v[c];
+                    else {
+                        float* to = a.slots + blockIdx.x * a.slot_stride + t * a.ldslot + k;
+                        *to = a.accumulate ? *to + v[c] : v[c];
+                    }
                 }
             }
         }

@@ -13,11 +13,11 @@ struct FewArgs {
     const float* x;               // [rows, dim], rows <= kFewRows
     int64_t ldx;
     int rows;
-    const float* w;               // [items, dim]
-    int64_t ldw, items;
+    const float* w;               // [items, dim], of the whole vocabulary from item0 on
+    int64_t ldw, items, item0;
     int dim;
     float k2;                     // scale log2(e)
-    const float* bias;
+    const float* bias;            // of the same items, or null
     const int64_t* targets;
     int64_t ignore_index;
     // the forward pass: a block's (m, s) of row t at part[block * part_rows + t]
@@ -28,6 +28,7 @@ struct FewArgs {
     float* g;                     // [items][few_rows_padded(rows)]
     float* slots;                 // sums of dx, [block][rows, ldslot], or null
     int64_t slot_stride, ldslot;
+    bool accumulate;              // added to what slots hold
     float* dw;                    // or null
     int64_t lddw;
     float scale;

@@ -77,3 +77,45 @@ def test_loss_in_blocks_of_rows(dtype, T, V):
         # s 2^m is the sum of the exponentials
         total = torch.log(stats[at, 1].double()) + stats[at, 0].double() * 0.6931471805599453
         close(total, torch.logsumexp(l, dim=1), 2 * e + 2.0 ** -21 * l.abs().amax(dim=1) + 2.0 ** -19)
+
+
+@pytest.mark.parametrize("T,V", [(1, 500_000_000), (16, 100_000_000), (9, 2_000_000_000)])
+def test_gradient_scratch_of_few_rows_is_bounded(T, V):
+    size = ctypes.c_size_t()
+    a = xent_args(T, V, 64, F32)
+    assert pvs._lib.pvs_xent_workspace(ctypes.byref(a), 1, ctypes.byref(size)) == pvs.PVS_OK
+    assert size.value <= GB + GB // 4
+
+
+@pytest.mark.parametrize("T,V", [(5, 40_000_003), (12, 17_000_000)])
+def test_gradients_of_few_rows_in_pieces_of_the_items(T, V):
+    # more than 1 GB of G, for 8 and for 16 rows; a target and a share of every softmax in
+    # each piece, masked items too.  A thread adds about V / 2,400 items, 200 sums join them.
+    d, scale = 4, 2.0
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(T, d, generator=g, device="cuda")
+    w = torch.rand(V, d, generator=g, device="cuda")
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[0], y[1], y[2] = 0, V - 1, -100
+    bias = torch.randn(V, generator=g, device="cuda")
+    bias[::7] = -torch.inf
+    bias[y[y >= 0]] = 1.0
+    grad = torch.rand(T, generator=g, device="cuda") + 0.5
+    _, stats = pvs.pvs_xent_forward(x, w, y, bias=bias, scale=scale)
+    dx, dw = pvs.pvs_xent_backward(x, w, y, stats, grad, bias=bias, scale=scale)
+    W = w.double()
+    for t in range(T):
+        X = x[t].double()
+        l = scale * (W @ X) + bias.double()
+        G = torch.softmax(l, dim=0)
+        if t != 2:
+            G[y[t]] -= 1.0
+        G *= float(grad[t]) if t != 2 else 0.0
+        e = float(((d / 16 + 4) * 2.0 ** -23 * scale * (W @ X.abs())).max()) + 2.0 ** -22 * 30
+        rel = 2 * e + 2.0 ** -19 + (V / 2400 + 200) * 2.0 ** -23
+        close(dx[t], scale * (G @ W), rel * scale * (G.abs() @ W) + 2.0 ** -126)
+        if t == 0:
+            want, tol = torch.zeros_like(W), torch.zeros_like(W)
+        want += scale * G[:, None] * X
+        tol += scale * (2 * e + 2.0 ** -18) * G.abs()[:, None] * X.abs()
+    close(dw, want, tol + 2.0 ** -126)
