@@ -15,7 +15,8 @@
  * Conventions:
  *   - Every matrix is in DEVICE memory, row-major with a leading dimension
  *     `ld` in elements (>= its columns); element types are pvs_dtype, held
- *     as the native bf16, f16 or float32.  Sums are float32.
+ *     as the native bf16, f16 or float32.  Sums are float32.  A pointer is
+ *     aligned to its elements where nothing else is said.
  *   - Every call queues its work on `cuda_stream` (a cudaStream_t; NULL: the
  *     legacy default stream) of the current device and returns; nothing is
  *     allocated and nothing waited for, so calls can be captured into a CUDA
@@ -24,7 +25,7 @@
  *     operator wants for the same arguments (256-byte aligned device memory).
  *     It may be used again once the call's work is done.
  *   - A call returns PVS_ERR_INVALID for arguments that it can see to be
- *     wrong (sizes, null pointers, unknown types, too small a workspace)
+ *     wrong (sizes, null or misaligned pointers, unknown types, too small a workspace)
  *     and then queues nothing, PVS_ERR_CUDA where a CUDA call fails.  What
  *     only the device sees is said for each operator.  A device-side wait
  *     that runs out ends its kernel; the next call on that device, or

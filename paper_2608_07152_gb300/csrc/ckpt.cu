@@ -579,11 +579,13 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
         (act != PVS_ACT_NONE && act != PVS_ACT_GELU) || (act != PVS_ACT_NONE && ldy < cols))
         return PVS_ERR_INVALID;
     if (rows == 0) return PVS_OK;
-    if (!x || !codes || !scales || (act != PVS_ACT_NONE && !y)) return PVS_ERR_INVALID;
+    const int es = element_bytes(dtype);
+    if (!x || !codes || !scales || (act != PVS_ACT_NONE && (!y || !on_elements(y, es))) ||
+        !on_elements(x, es) || !on_elements(scales, 4))
+        return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
-    const int es = element_bytes(dtype);
     // eights: aligned rows, or matrices without gaps that start aligned
     const bool dense = ldx == cols && ldcodes == cols && (act == PVS_ACT_NONE || ldy == cols);
     const bool eight = (cols % 8 == 0 || dense) && by_eight(x, dense ? 8 : ldx, es) &&
@@ -607,7 +609,8 @@ extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const 
                                     int32_t dtype, void* cuda_stream) {
     if (!rows_ok(rows, cols, dtype) || ldcodes < cols || ldout < cols) return PVS_ERR_INVALID;
     if (rows == 0) return PVS_OK;
-    if (!codes || !scales || !out) return PVS_ERR_INVALID;
+    if (!codes || !scales || !out || !on_elements(scales, 4) || !on_elements(out, element_bytes(dtype)))
+        return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
@@ -631,11 +634,13 @@ extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const 
         act != PVS_ACT_GELU)
         return PVS_ERR_INVALID;
     if (rows == 0) return PVS_OK;
-    if (!dy || !codes || !scales || !dx) return PVS_ERR_INVALID;
+    const int es = element_bytes(dtype);
+    if (!dy || !codes || !scales || !dx || !on_elements(dy, es) || !on_elements(scales, 4) ||
+        !on_elements(dx, es))
+        return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
-    const int es = element_bytes(dtype);
     if (cols % 8 != 0 && flat_ok(dy, lddy, codes, ldcodes, cols, dx, lddx, es) &&
         rows * cols < (int64_t)1 << 42)
         PVS_BY_TYPE(dtype, e = (flat_launch<TYPE, true>(dy, codes, scales, rows, cols, dx, st)));
@@ -668,14 +673,15 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
                                            int64_t lddw, void* workspace, size_t workspace_bytes,
                                            void* cuda_stream) {
     if (!rows_ok(rows, cols, dtype) || out_cols < 1 || out_cols > kMaxDim || lddy < out_cols ||
-        ldcodes < cols || lddw < cols || !dw)
+        ldcodes < cols || lddw < cols || !dw || !on_elements(dw, element_bytes(dtype)))
         return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const size_t es = (size_t)element_bytes(dtype);
     if (rows == 0)
         return queued(cudaMemset2DAsync(dw, (size_t)lddw * es, 0, (size_t)cols * es,
                                         (size_t)out_cols, st));
-    if (!dy || !codes || !scales) return PVS_ERR_INVALID;
+    if (!dy || !codes || !scales || !on_elements(dy, (int)es) || !on_elements(scales, 4))
+        return PVS_ERR_INVALID;
     Device dev;
     cudaError_t e = device(&dev);
     if (e != cudaSuccess) return queued(e);

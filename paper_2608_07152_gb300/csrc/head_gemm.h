@@ -313,6 +313,10 @@ inline int64_t copied_ld(int64_t cols) { return round_up(cols, cols > 256 ? 64 :
 // Rows of any matrix here: coordinates of tiles past the end still fit an int.
 constexpr int64_t kMaxRows = 0x7fff0000;
 inline int element_bytes(int dtype) { return dtype == 2 ? 4 : 2; }
+// Whether a pointer is aligned to its elements (null is).
+inline bool on_elements(const void* p, int bytes) {
+    return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0;
+}
 inline int parts_of(int dtype) { return dtype == 2 ? 3 : 1; }
 
 }  // namespace head

@@ -637,7 +637,8 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
                                   void* cuda_stream) {
     if (!shape_ok(rows, cols, group, dtype) || ldw < cols) return PVS_ERR_INVALID;
     if (rows == 0) return PVS_OK;
-    if (!w || !codes || !scales || !codes_aligned(codes, scales)) return PVS_ERR_INVALID;
+    if (!w || !codes || !scales || !codes_aligned(codes, scales) || !on_elements(w, element_bytes(dtype)))
+        return PVS_ERR_INVALID;
     const int blocks = (cols + 127) / 128;
     const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -653,7 +654,9 @@ extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, in
                                     int32_t dtype, void* cuda_stream) {
     if (!shape_ok(rows, cols, group, dtype) || ldout < cols) return PVS_ERR_INVALID;
     if (rows == 0) return PVS_OK;
-    if (!out || !codes || !scales || !codes_aligned(codes, scales)) return PVS_ERR_INVALID;
+    if (!out || !codes || !scales || !codes_aligned(codes, scales) ||
+        !on_elements(out, element_bytes(dtype)))
+        return PVS_ERR_INVALID;
     const int blocks = (cols + 127) / 128;
     const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -671,7 +674,9 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
     if (!shape_ok(rows, cols, group, dtype) || batch < 0 || batch > 64 || ldx < cols || ldy < rows)
         return PVS_ERR_INVALID;
     if (rows == 0 || batch == 0) return PVS_OK;
-    if (!x || !y || !codes || !scales || !codes_aligned(codes, scales)) return PVS_ERR_INVALID;
+    if (!x || !y || !codes || !scales || !codes_aligned(codes, scales) ||
+        !on_elements(x, element_bytes(dtype)) || !on_elements(y, element_bytes(dtype)))
+        return PVS_ERR_INVALID;
     Device dev;
     cudaError_t e = device(&dev);
     if (e != cudaSuccess) return queued(e);

@@ -252,7 +252,9 @@ bool valid(const pvs_xent_args* a) {
         a->reserved != 0 || !(a->scale >= 0x1p-126f) || !std::isfinite(a->scale) || a->ldx < a->dim ||
         a->ldw < a->dim)
         return false;
-    return a->w && (a->rows == 0 || (a->x && a->targets));
+    const int es = element_bytes(a->dtype);
+    return a->w && (a->rows == 0 || (a->x && a->targets)) && on_elements(a->x, es) &&
+           on_elements(a->w, es) && on_elements(a->targets, 8) && on_elements(a->bias, 4);
 }
 
 // How dx (u0 tiles, k0 chunks of k) and dw (u1, k1) share the `slots` CTAs or pairs
@@ -712,7 +714,7 @@ extern "C" pvs_status pvs_xent_forward(const pvs_xent_args* a, float* loss, floa
                                        void* cuda_stream) {
     if (!valid(a)) return PVS_ERR_INVALID;
     if (a->rows == 0) return PVS_OK;
-    if (!loss || !stats || (reinterpret_cast<uintptr_t>(stats) & 15u)) return PVS_ERR_INVALID;
+    if (!loss || !stats || !on_elements(loss, 4) || !on_elements(stats, 16)) return PVS_ERR_INVALID;
     Device dev;
     if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
     const pvs_status s = begin(workspace, workspace_bytes, forward_bytes(*a, dev), dev);
@@ -731,7 +733,9 @@ extern "C" pvs_status pvs_xent_backward(const pvs_xent_args* a, const float* sta
                                         const float* grad_loss, void* dx, int64_t lddx, void* dw,
                                         int64_t lddw, void* workspace, size_t workspace_bytes,
                                         void* cuda_stream) {
-    if (!valid(a) || (dx && lddx < a->dim) || (dw && lddw < a->dim)) return PVS_ERR_INVALID;
+    if (!valid(a) || (dx && lddx < a->dim) || (dw && lddw < a->dim) ||
+        !on_elements(dx, element_bytes(a->dtype)) || !on_elements(dw, element_bytes(a->dtype)))
+        return PVS_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (a->rows == 0) {
         if (!dw) return PVS_OK;
@@ -739,7 +743,8 @@ extern "C" pvs_status pvs_xent_backward(const pvs_xent_args* a, const float* sta
         return ended(cudaMemset2DAsync(dw, (size_t)lddw * es, 0, (size_t)a->dim * es,
                                        (size_t)a->items, st));
     }
-    if (!stats || !grad_loss || (reinterpret_cast<uintptr_t>(stats) & 15u)) return PVS_ERR_INVALID;
+    if (!stats || !grad_loss || !on_elements(stats, 16) || !on_elements(grad_loss, 4))
+        return PVS_ERR_INVALID;
     Device dev;
     if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
     const Plan p = plan_of(*a, true, dev, workspace);
