@@ -58,6 +58,14 @@ typedef enum pvs_act {
  * current device since this was last asked (cleared by asking). */
 pvs_status pvs_head_status(void);
 
+/* Limit, in nanoseconds, of each wait of the tensor-core products that are
+ * queued from now on on the current device (default and maximum 2e9, i.e. 2 s).
+ * 0 makes every such wait give up at once unless what it waits for is already
+ * there, which lets tests reach PVS_ERR_TIMEOUT without a fault.  A product's
+ * waits for its own copies in flight always keep the 2 s limit.  A CUDA graph
+ * keeps the limit that it was captured with. */
+pvs_status pvs_head_set_wait_limit(int64_t ns);
+
 /* ---------------------------------------------------------------------------
  * Softmax cross entropy.  For T = rows rows x_t and V = items vectors w_j of
  * `dim` elements, a = scale and b = bias (zeros where null):

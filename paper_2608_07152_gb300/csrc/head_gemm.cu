@@ -69,7 +69,9 @@ struct Shared {
     uint64_t tfull[2];
     uint64_t tempty[2];
     uint32_t tmem_base;
-    int abort;
+    int abort;                           // of the pair: set in both its CTAs
+    uint32_t fills;                      // stages that this CTA has filled
+    uint32_t chunks, tiles;              // even CTA: chunks and tiles committed
     uint32_t masked[2][kTileN / 32];     // items of the tile outside the softmax
     alignas(16) float b2[2][kTileN];     // their biases, in powers of two
     alignas(16) float unit[2][kTileN];   // what their logits are in units of
@@ -85,9 +87,36 @@ static_assert(smem_bytes<1>() <= 227 * 1024 && smem_bytes<2>() <= 227 * 1024, "s
 __device__ __forceinline__ bool abort_set(Shared& sh) {
     return *reinterpret_cast<volatile int*>(&sh.abort) != 0;
 }
-__device__ __forceinline__ void raise_abort(Shared& sh, int* status) {
+template <int kCta>
+__device__ __forceinline__ void raise_abort(Shared& sh, int* status, int crank) {
     *reinterpret_cast<volatile int*>(&sh.abort) = 1;
+    if (kCta == 2)
+        asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(
+                         cluster_map(&sh.abort, crank ^ 1)),
+                     "r"(1)
+                     : "memory");
     *reinterpret_cast<volatile int*>(status) = PVS_ERR_TIMEOUT;
+}
+// A wait of the ring: most have nothing to wait for, and do not look at the limit.
+__device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
+    return mbar_test_wait(bar, parity) || (limit_ns != 0 && mbar_wait(bar, parity, limit_ns));
+}
+// A wait at a role's end, with the 2 s limit, given up in a millisecond where another role has
+// given up (what it waits for may then never come).
+template <int kCta>
+__device__ __forceinline__ void last_wait(uint64_t* bar, uint32_t parity, Shared& sh, int* status,
+                                          int crank) {
+    constexpr unsigned long long kTurn = 1000000;
+    for (unsigned long long t = 0; t < kWaitLimitNs; t += kTurn) {
+        if (abort_set(sh) || mbar_wait(bar, parity, kTurn)) return;
+    }
+    raise_abort<kCta>(sh, status, crank);
+}
+// A word of a pair's CTA.
+__device__ __forceinline__ uint32_t word_of(const uint32_t* p, int crank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_map(p, crank)) : "memory");
+    return v;
 }
 
 // M or N contiguous with 128-byte swizzle: 64 elements of m (128 bytes) by 8 of
@@ -325,6 +354,68 @@ __device__ __forceinline__ void write_stats(const float2 (&share)[kEpiGroups][kT
     sm.part[(int64_t)at * sm.rows + row] = make_float2(m, s);
 }
 
+// The copies of one fill of a stage, this CTA's share.
+struct Producer {
+    const Problem& p;
+    const CUtensorMap* b;
+    int nbox;                    // boxes of B, where N is its contiguous index
+    uint32_t bytes;              // of a stage, of both CTAs
+
+    __device__ __forceinline__ Producer(const Problem& p, bool alt, int kcta) : p(p) {
+        const int bhalf = p.bn / kcta;                  // rows of B that this CTA supplies
+        b = alt ? &p.b_alt : &p.b;
+        nbox = (bhalf + 63) / 64;
+        bytes = kcta * (kStageA + (uint32_t)(p.b_mn ? nbox * 64 : bhalf) * kTileK * 2u);
+    }
+    template <int kCta>
+    __device__ __forceinline__ void fill(uint8_t* stage, uint64_t* full, bool leader, int am, int ka,
+                                         int pa, int bn, int kb, int pb) const {
+        uint8_t* sb = stage + kStageA;
+        if (leader) mbar_arrive_expect_tx(full, bytes);
+        const uint32_t bar = kCta == 2 ? cluster_map(full, 0) : smem_u32(full);
+        if (p.a_mn) {
+            tma_load_3d<kCta>(stage, &p.a, am, ka, pa, bar);
+            tma_load_3d<kCta>(stage + kTileK * 128, &p.a, am + 64, ka, pa, bar);
+        } else {
+            tma_load_3d<kCta>(stage, &p.a, ka, am, pa, bar);
+        }
+        if (p.b_mn) {
+            for (int i = 0; i < nbox; ++i)
+                tma_load_3d<kCta>(sb + i * kTileK * 128, b, bn + 64 * i, kb, pb, bar);
+        } else {
+            tma_load_3d<kCta>(sb, b, kb, bn, pb, bar);
+        }
+    }
+};
+
+// After a wait that ran out: one thread of each CTA waits for what is still on its way to its
+// CTA, which must not end before.  Fills first: those that the other CTA of the pair has issued
+// and this one has not are issued here (the stage is free, or the other would not have filled
+// it; what is read does not matter), so that every `full` barrier completes.  Then the MMAs and
+// their commits.  With the 2 s limit; after one that runs out nothing more is waited for.
+template <int kCta>
+__device__ __noinline__ void settle(Shared& sh, uint8_t* stages, const Problem& p, int crank) {
+    using R = Ring<kCta>;
+    const Producer make(p, false, kCta);
+    const uint32_t mine = sh.fills;
+    const uint32_t fills = kCta == 2 ? max(mine, word_of(&sh.fills, crank ^ 1)) : mine;
+    for (uint32_t g = mine; g < fills; ++g) {
+        const int s = g % R::kStages;
+        make.fill<kCta>(stages + s * R::kStageBytes, &sh.full[s], crank == 0, p.a_mo, p.a_ko, 0, p.b_no,
+                        p.b_ko, 0);
+    }
+    const uint32_t chunks = kCta == 2 ? word_of(&sh.chunks, 0) : sh.chunks;
+    const uint32_t tiles = kCta == 2 ? word_of(&sh.tiles, 0) : sh.tiles;
+    bool in_time = true;
+    for (uint32_t s = 0; s < (uint32_t)R::kStages; ++s) {
+        if (in_time && crank == 0 && s < fills)
+            in_time = mbar_wait(&sh.full[s], ((fills - 1 - s) / R::kStages) & 1u);
+        if (in_time && s < chunks) in_time = mbar_wait(&sh.empty[s], ((chunks - 1 - s) / R::kStages) & 1u);
+    }
+    for (uint32_t b = 0; b < 2; ++b)
+        if (in_time && b < tiles) in_time = mbar_wait(&sh.tfull[b], ((tiles - 1 - b) / 2) & 1u);
+}
+
 template <int EPI, int kCta>
 __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ Args a) {
     using R = Ring<kCta>;
@@ -350,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             mbar_init(&sh.tempty[b], kCta * kEpiWarps);   // both CTAs' epilogue warps
         }
         sh.abort = 0;
+        sh.fills = sh.chunks = sh.tiles = 0;
         mbar_fence_init();
     }
     if (warp == 1) {
@@ -371,12 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         if (lane == 0) {
             uint32_t g = 0;
             const bool alt = p.alt_flag && *p.alt_flag;
-            const CUtensorMap* mb = alt ? &p.b_alt : &p.b;
-            const int bhalf = p.bn / kCta;              // rows of B that this CTA supplies
-            const int nbox = (bhalf + 63) / 64;
-            // the bytes of a stage, of both CTAs
-            const uint32_t bytes =
-                kCta * (kStageA + (uint32_t)(p.b_mn ? nbox * 64 : bhalf) * kTileK * 2u);
+            const int bhalf = p.bn / kCta;
+            const Producer make(p, alt, kCta);
             for (; w.left > 0 && !abort_set(sh); w.next()) {
                 const int am = p.a_mo + (w.mt * kCta + crank) * kTileM;
                 const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn + crank * bhalf;
@@ -385,37 +473,21 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     const int pa = a.pa[q], pb = a.pb[q];
                     for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
                         const int s = g % R::kStages;
-                        if (!mbar_wait(&sh.empty[s], ((g / R::kStages) & 1u) ^ 1u)) {
-                            raise_abort(sh, a.status);
+                        if (!ring_wait(&sh.empty[s], ((g / R::kStages) & 1u) ^ 1u, a.wait_ns)) {
+                            raise_abort<kCta>(sh, a.status, crank);
                             break;
                         }
-                        uint8_t* sa = stages + s * R::kStageBytes;
-                        uint8_t* sb = sa + kStageA;
-                        if (leader) mbar_arrive_expect_tx(&sh.full[s], bytes);
-                        const uint32_t bar =
-                            kCta == 2 ? cluster_map(&sh.full[s], 0) : smem_u32(&sh.full[s]);
-                        const int ka = p.a_ko + kc * kTileK, kb = bk + kc * kTileK;
-                        if (p.a_mn) {
-                            tma_load_3d<kCta>(sa, &p.a, am, ka, pa, bar);
-                            tma_load_3d<kCta>(sa + kTileK * 128, &p.a, am + 64, ka, pa, bar);
-                        } else {
-                            tma_load_3d<kCta>(sa, &p.a, ka, am, pa, bar);
-                        }
-                        if (p.b_mn) {
-                            for (int i = 0; i < nbox; ++i)
-                                tma_load_3d<kCta>(sb + i * kTileK * 128, mb, bnc + 64 * i, kb, pb,
-                                                  bar);
-                        } else {
-                            tma_load_3d<kCta>(sb, mb, kb, bnc, pb, bar);
-                        }
+                        make.fill<kCta>(stages + s * R::kStageBytes, &sh.full[s], leader, am,
+                                        p.a_ko + kc * kTileK, pa, bnc, bk + kc * kTileK, pb);
                     }
                 }
             }
+            sh.fills = g;
             // the MMAs have consumed the last fill of every stage used: no copy into
             // this CTA and no commit to its barriers is still in flight when it ends
             for (int s = 0; s < R::kStages && (uint32_t)s < g; ++s) {
                 const uint32_t last = g - 1 - ((g - 1 - s) % R::kStages);
-                if (!mbar_wait(&sh.empty[s], (last / R::kStages) & 1u)) raise_abort(sh, a.status);
+                last_wait<kCta>(&sh.empty[s], (last / R::kStages) & 1u, sh, a.status, crank);
             }
         }
     } else if (warp == 1) {
@@ -435,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             int it = 0;
             for (; w.left > 0 && !abort_set(sh); w.next(), ++it) {
                 const int b = it & 1;
-                if (!mbar_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u)) {
-                    raise_abort(sh, a.status);
+                if (!ring_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, a.wait_ns)) {
+                    raise_abort<kCta>(sh, a.status, crank);
                     break;
                 }
                 tc::fence_after_sync();
@@ -447,8 +519,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 const bool tail = w.k1 == p.kchunks && p.ktail < kTileK / 16;
                 for (int kc = 0; kc < chunks; ++kc, ++g) {
                     const int s = g % R::kStages;
-                    if (!mbar_wait(&sh.full[s], (g / R::kStages) & 1u)) {
-                        raise_abort(sh, a.status);
+                    if (!ring_wait(&sh.full[s], (g / R::kStages) & 1u, a.wait_ns)) {
+                        raise_abort<kCta>(sh, a.status, crank);
                         break;
                     }
                     tc::fence_after_sync();
@@ -479,11 +551,12 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 else
                     tc::commit(&sh.tfull[b]);
             }
+            sh.chunks = g;
+            sh.tiles = it;
             // TMEM is released after the last unit's MMAs
             if (it > 0) {
                 const int lb = (it - 1) & 1;
-                if (!mbar_wait(&sh.tfull[lb], (uint32_t)((it - 1) >> 1) & 1u))
-                    raise_abort(sh, a.status);
+                last_wait<kCta>(&sh.tfull[lb], (uint32_t)((it - 1) >> 1) & 1u, sh, a.status, crank);
             }
         }
     } else {
@@ -548,8 +621,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             // after a wait that ran out, the warps still meet at every barrier
             if (!dead) {
                 bool late = abort_set(sh);
-                if (!late && !mbar_wait(&sh.tfull[b], (uint32_t)(it >> 1) & 1u)) {
-                    raise_abort(sh, a.status);
+                if (!late && !ring_wait(&sh.tfull[b], (uint32_t)(it >> 1) & 1u, a.wait_ns)) {
+                    raise_abort<kCta>(sh, a.status, crank);
                     late = true;
                 }
                 dead = __any_sync(0xffffffffu, late);
@@ -729,6 +802,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     }
     __syncthreads();
     if (kCta == 2) cluster_barrier();   // no CTA leaves while its peer may still address it
+    if (abort_set(sh)) {
+        if (threadIdx.x == 0) settle<kCta>(sh, stages, p, crank);
+        __syncthreads();
+        if (kCta == 2) cluster_barrier();
+    }
     if (warp == 1) {
         tc::fence_after_sync();
         if (kCta == 2)
@@ -1261,6 +1339,7 @@ cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t s
         }
     }
     const void* fn = cta == 2 ? kernel_of<2>(epilogue) : kernel_of<1>(epilogue);
+    a.wait_ns = dev.wait_ns;
     cudaLaunchAttribute attr[2];
     const cudaLaunchConfig_t cfg = config(cta, used * cta, st, attr);
     cudaError_t e = raise_smem_limit(fn, cfg.dynamicSmemBytes);
@@ -1302,6 +1381,7 @@ cudaError_t device(Device* d) {
         *static_cast<volatile int*>(p) = 0;
         g.sms = sms;
         g.pairs = pairs;
+        g.wait_ns = kWaitLimitNs;
         g.status = p;
     }
     *d = g;
@@ -1316,14 +1396,32 @@ int take_status(const Device& d) {
     return s;
 }
 
+int ready(Device* d) {
+    if (device(d) != cudaSuccess) {
+        cudaGetLastError();
+        return PVS_ERR_CUDA;
+    }
+    return take_status(*d);
+}
+
 }  // namespace head
 }  // namespace pvs
 
 extern "C" pvs_status pvs_head_status(void) {
     pvs::head::Device d;
-    if (pvs::head::device(&d) != cudaSuccess) {
+    return (pvs_status)pvs::head::ready(&d);
+}
+
+extern "C" pvs_status pvs_head_set_wait_limit(int64_t ns) {
+    using namespace pvs::head;
+    if (ns < 0) return PVS_ERR_INVALID;
+    Device d;
+    int dev = 0;
+    if (device(&d) != cudaSuccess || cudaGetDevice(&dev) != cudaSuccess) {
         cudaGetLastError();
         return PVS_ERR_CUDA;
     }
-    return (pvs_status)pvs::head::take_status(d);
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    g_devices[dev].wait_ns = std::min<unsigned long long>((unsigned long long)ns, pvs::kWaitLimitNs);
+    return PVS_OK;
 }

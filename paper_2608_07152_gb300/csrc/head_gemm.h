@@ -98,6 +98,7 @@ struct Args {
     int slots0;                  // of two problems, the CTAs (pairs) of the first; 0: by work
     Softmax sm;
     int* status;
+    unsigned long long wait_ns;  // set by the launch: the limit of a wait
 };
 
 // A kernel of a call may be put on the SMs while the one before it ends: its setup then
@@ -142,14 +143,18 @@ cudaError_t launch_early(void (*kernel)(Params...), int64_t grid, int block, siz
 }
 #endif
 
-// The current device: its SMs, the CTA pairs that run at once on them, and the
-// status word that its kernels set (pinned host memory).
+// The current device: its SMs, the CTA pairs that run at once on them, the status word that
+// its kernels set (pinned host memory), and the limit of their waits.
 struct Device {
     int sms, pairs;
     int* status;
+    unsigned long long wait_ns;
 };
 cudaError_t device(Device* d);
 int take_status(const Device& d);
+// What a call that is about to queue work begins with: PVS_OK, or the pvs_status that it
+// returns instead.
+int ready(Device* d);
 
 // Tensor map of an operand: boxes of kTileK x box_rows (K contiguous) or
 // 64 x kTileK (M / N contiguous).

@@ -32,6 +32,7 @@ class pvs_xent_args(ctypes.Structure):
 
 _SIGNATURES = {
     "pvs_head_status": (_i32, []),
+    "pvs_head_set_wait_limit": (_i32, [_i64]),
     "pvs_xent_workspace": (_i32, [_P, _i32, _P]),
     "pvs_xent_forward": (_i32, [_P, _P, _P, _P, ctypes.c_size_t, _P]),
     "pvs_xent_backward": (_i32, [_P, _P, _P, _P, _i64, _P, _i64, _P, ctypes.c_size_t, _P]),
@@ -141,6 +142,12 @@ def pvs_head_status() -> int:
     """PVS_OK, or raises what an earlier operator of this module left on the
     current device (PVS_ERR_TIMEOUT); ask after a synchronisation."""
     return _check(_lib.pvs_head_status(), "pvs_head_status")
+
+
+def pvs_head_set_wait_limit(ns: int) -> None:
+    """Limit of the device-side waits of products queued from now on on the current
+    device (default and maximum 2e9; 0: a wait gives up unless it need not wait)."""
+    _check(_lib.pvs_head_set_wait_limit(int(ns)), "pvs_head_set_wait_limit")
 
 
 def _xent_args(x, w, targets, bias, scale, ignore_index):
