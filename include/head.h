@@ -28,9 +28,10 @@
  *     wrong (sizes, null or misaligned pointers, unknown types, too small a workspace)
  *     and then queues nothing, PVS_ERR_CUDA where a CUDA call fails.  What
  *     only the device sees is said for each operator.  A device-side wait
- *     that runs out ends its kernel; the next call on that device, or
- *     pvs_head_status, then returns PVS_ERR_TIMEOUT once: what was queued
- *     before it has no valid outputs.
+ *     that runs out ends its kernel; the next call on that device that has
+ *     work to queue, or pvs_head_status, then returns PVS_ERR_TIMEOUT once, and
+ *     queues nothing: what was queued before it has no valid outputs.  (The
+ *     status is the device's: whichever thread asks next has it.)
  */
 #ifndef PVS_HEAD_H_
 #define PVS_HEAD_H_

@@ -583,6 +583,9 @@ extern "C" pvs_status pvs_ckpt_store(const void* x, int64_t ldx, int64_t rows, i
     if (!x || !codes || !scales || (act != PVS_ACT_NONE && (!y || !on_elements(y, es))) ||
         !on_elements(x, es) || !on_elements(scales, 4))
         return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
@@ -611,6 +614,9 @@ extern "C" pvs_status pvs_ckpt_load(const int8_t* codes, int64_t ldcodes, const 
     if (rows == 0) return PVS_OK;
     if (!codes || !scales || !out || !on_elements(scales, 4) || !on_elements(out, element_bytes(dtype)))
         return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;
@@ -638,6 +644,9 @@ extern "C" pvs_status pvs_ckpt_act_backward(const void* dy, int64_t lddy, const 
     if (!dy || !codes || !scales || !dx || !on_elements(dy, es) || !on_elements(scales, 4) ||
         !on_elements(dx, es))
         return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     count_launches(1);
     cudaError_t e = cudaSuccess;

@@ -639,6 +639,9 @@ extern "C" pvs_status pvs_wq_pack(const void* w, int64_t ldw, int64_t rows, int3
     if (rows == 0) return PVS_OK;
     if (!w || !codes || !scales || !codes_aligned(codes, scales) || !on_elements(w, element_bytes(dtype)))
         return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     const int blocks = (cols + 127) / 128;
     const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -657,6 +660,9 @@ extern "C" pvs_status pvs_wq_unpack(const uint8_t* codes, const void* scales, in
     if (!out || !codes || !scales || !codes_aligned(codes, scales) ||
         !on_elements(out, element_bytes(dtype)))
         return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     const int blocks = (cols + 127) / 128;
     const unsigned grid = (unsigned)std::min<int64_t>((rows + 7) / 8, 1 << 20);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -678,9 +684,10 @@ extern "C" pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch,
         !on_elements(x, element_bytes(dtype)) || !on_elements(y, element_bytes(dtype)))
         return PVS_ERR_INVALID;
     Device dev;
-    cudaError_t e = device(&dev);
-    if (e != cudaSuccess) return queued(e);
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
     const int es = element_bytes(dtype);
+    cudaError_t e = cudaSuccess;
     WqArgs a{};
     a.ldx = ldx;
     a.dtype = dtype;

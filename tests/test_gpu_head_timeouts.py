@@ -87,3 +87,33 @@ def test_limits():
         assert torch.equal(pvs.pvs_xent_forward(x, w, y, scale=scale)[0], want)
     torch.cuda.synchronize()
     assert pvs.pvs_head_status() == pvs.PVS_OK
+
+
+def entry_points():
+    x, w, y, _, grad, scale = make(200, 900, 64, BF16)
+    _, stats = pvs.pvs_xent_forward(x, w, y, scale=scale)
+    codes, scales, _ = pvs.pvs_ckpt_store(x)
+    packed, units = pvs.pvs_wq_pack(w, 64)
+    return {
+        "xent_forward": lambda: pvs.pvs_xent_forward(x, w, y, scale=scale),
+        "xent_backward": lambda: pvs.pvs_xent_backward(x, w, y, stats, grad, scale=scale),
+        "ckpt_store": lambda: pvs.pvs_ckpt_store(x, act=pvs.PVS_ACT_GELU),
+        "ckpt_load": lambda: (pvs.pvs_ckpt_load(codes, scales, BF16),),
+        "ckpt_act_backward": lambda: (pvs.pvs_ckpt_act_backward(x, codes, scales),),
+        "ckpt_grad_weight": lambda: (pvs.pvs_ckpt_grad_weight(x, codes, scales),),
+        "wq_pack": lambda: pvs.pvs_wq_pack(w, 64),
+        "wq_unpack": lambda: (pvs.pvs_wq_unpack(packed, units, 64, 64, BF16),),
+        "wq_matvec": lambda: (pvs.pvs_wq_matvec(x[:3], packed, units, 64),),
+    }
+
+
+@pytest.mark.parametrize("name", ["xent_forward", "xent_backward", "ckpt_store", "ckpt_load", "ckpt_act_backward",
+                                  "ckpt_grad_weight", "wq_pack", "wq_unpack", "wq_matvec"])
+def test_the_next_call_of_any_kind_reports_it(name):
+    calls = entry_points()
+    want = calls[name]()
+    run_out(calls["xent_forward"])
+    assert raised(calls[name]) == pvs.PVS_ERR_TIMEOUT
+    assert pvs.pvs_head_status() == pvs.PVS_OK
+    for a, b in zip(calls[name](), want):
+        assert torch.equal(a, b)
