@@ -79,7 +79,9 @@ pvs_status pvs_head_set_wait_limit(int64_t ns);
  *     are the gradients that the row reaches.
  *   - no item in the softmax: every loss is 0, and no gradient.
  *   - the target itself masked: loss +inf, and no gradient through the target.
- * NaN and overflows elsewhere reach the outputs as in that formula.
+ * NaN and overflows elsewhere reach the outputs as in that formula, but that
+ * finite biases beyond 2.3e38 in size count as 2.36e38 (one of the lowest value at a
+ * target gives its own loss).
  * bf16 and f16 products are exact.  float32 operands enter the logits as pairs
  * of f16 with a power of two for each row and item, and the gradients as three
  * bf16 parts; what is left out of a product is about 2^-22 of it.

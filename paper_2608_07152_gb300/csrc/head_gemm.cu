@@ -8,9 +8,10 @@
 // serve the products of 128 rows or fewer, which memory bounds (a loss of 100 rows over
 // 500,000 items of 768: 125 us, in pairs 132; of 256 rows 140 in pairs, 155 in lone CTAs).
 //
-// 8,192 rows over 8,192 items of 768 in bf16: statistics 68 us (1.50 PFLOP/s, tensor
-// pipe 71% busy), G 74 us (66%), dx and dw 150 us (1.37 PFLOP/s, 76%).  What is lost is
-// the last, half empty, of 14 rounds of tiles, and with short k the epilogue.
+// 8,192 rows over 8,192 items of 768 in bf16: statistics 69 us (1.50 PFLOP/s, tensor
+// pipe 70% busy), G 111 us (43%: two parts of 134 MB are stored), dx and dw 287 us (two
+// products each, 1.44 PFLOP/s, 78%).  What is lost beside is the last, half empty, of 14 rounds of
+// tiles, and with short k the epilogue.
 //   warp 0     TMA producer (both CTAs): chunks of A (128 x 64) and B into a ring,
 //              128-byte swizzle, the pair's bytes counted on the even CTA's barrier;
 //   warp 1     one thread (of the even CTA) issues the MMAs (M = 128 or 256, N = bn,
@@ -909,7 +910,7 @@ __device__ __forceinline__ float load_as_float(const void* p, int dtype, int64_t
 }
 
 // Eight consecutive elements a thread, in one load (two of float32) where rows are
-// aligned; n / pieces by a product as in sum_slots_kernel.
+// aligned; n / pieces by a product: m = floor(2^40 / pieces) + 1 is exact for what a block has.
 __device__ __forceinline__ void split_rows(const SplitArgs& a, int64_t block, int64_t blocks) {
     const int pieces = (a.cols + 7) / 8, per_block = a.per_block, wide = a.wide;
     const uint64_t m = a.magic;
@@ -1241,7 +1242,7 @@ __device__ __forceinline__ void split_codes_rows(const CodesArgs& a, int64_t blo
 }
 
 // The operands of a weight gradient from kept rows: codes, and dy where it is copied.
-// 32,768 x 768 codes to bf16 in 15 us (5 TB/s; issue 77%).
+// 32,768 x 768 codes times their scales to two bf16 parts in 26 us (4.9 TB/s; issue 75%).
 __global__ void __launch_bounds__(256) codes_kernel(const CodesArgs c, const SplitArgs s,
                                                     int64_t blocks) {
     next_early();

@@ -6,7 +6,7 @@
 // contiguous), each in up to three parts that add up to it: the product then
 // runs over a list of part pairs.  What becomes of D is the kernel's choice:
 //   kStats   softmax statistics of D's rows, tile by tile (forward);
-//   kGrad    the softmax gradient of each entry, kept in 16 bits (backward);
+//   kGrad    the softmax gradient of each entry, kept in 16-bit parts (backward);
 //   kOut     D itself, split over k where that fills the GPU.
 #pragma once
 
@@ -73,7 +73,6 @@ struct Softmax {
     const float* row_unit;       // float32 operands: what D's rows and columns (the piece's
     const float* col_unit;       // items) are in units of; else null
     const float* bias;           // of the whole vocabulary, or null
-    int64_t items;               // bias entries
     int item0;                   // the piece's first item
     int rows;
     // kStats

@@ -11,9 +11,9 @@
 // k is split over the warps of a block where there are few rows of weights.
 //
 // 1,000,000 x 768 in groups of 128: one bf16 row 97 us (4.1 TB/s), four float32 rows
-// (12 columns) 113 us; issue 56%, about three instructions a code.  Fully memory-bound
-// it would be 58: deeper prefetch (112 us for the one row) and tiles run on into one another
-// (110) were slower.
+// (12 columns) 113 us; issue 56%, tensor pipe 38%, DRAM 45%: none of them full, latency bounds
+// it.  Fully memory-bound it would be 58: prefetch deeper in registers, which are at their cap
+// (112 us for the one row), and tiles run on into one another (110) were slower.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -32,7 +32,11 @@ namespace {
 constexpr int kWqThreads = 256;
 constexpr int kWqWarps = kWqThreads / 32;
 constexpr int kWqBlockBytes = 2048;      // x fragments of 128 of k and 8 columns
-constexpr int kWqSmem = 88 * 1024;       // of x fragments, at most (two blocks an SM)
+// Of x fragments, at most: two blocks an SM with one or two tiles of columns.  With four (36 KB
+// of sums beside) a second block fits up to 1,152 columns of weights; past 1,408 the fragments
+// are made again for every 128 rows: 8 float32 rows over 200,000 x 1,024 weights take 55 us, over
+// as many weights in rows of 1,280 76, of 2,048 104.
+constexpr int kWqSmem = 88 * 1024;
 
 __device__ __forceinline__ float load_x(const void* p, int dtype, int64_t i) {
     if (dtype == PVS_F32) return static_cast<const float*>(p)[i];

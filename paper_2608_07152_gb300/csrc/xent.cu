@@ -32,8 +32,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 // G of a piece, and copies of a piece of w, at most about: a piece costs two launches and
-// their uneven ends, and the sums of dx one pass over its splits.  A step of 256 rows
-// over a million items took 2.5 ms in pieces of 32 K items, 1.6 ms in 256 K ones.
+// their uneven ends, and the sums of dx one pass over its splits.  With G in one part a step of
+// 256 rows over a million items took 2.5 ms in pieces of 32 K items, 1.6 ms in 256 K ones.
 constexpr size_t kGradBytes = (size_t)1 << 30;
 constexpr size_t kPartsBytes = (size_t)1 << 30;
 // The tiles' statistics of the forward pass, 8 bytes for each row and tile of items: the rows
@@ -481,7 +481,6 @@ Softmax softmax_of(const pvs_xent_args& a) {
     Softmax s{};
     s.k2 = a.scale * kLog2e;
     s.bias = a.bias;
-    s.items = a.items;
     s.rows = (int)a.rows;
     return s;
 }

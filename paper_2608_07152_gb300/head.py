@@ -6,7 +6,9 @@ and products with 4-bit weights.  Operands are CUDA ``torch`` tensors of one
 device, whose rows may be strided; work is queued on torch's current stream of
 that device, outputs and scratch come from torch's allocator on that stream,
 and nothing waits for the GPU.  A tensor made on another stream is the caller's
-to order, as with torch's own operators.  A negative status raises ``PvsError``;
+to order, as with torch's own operators.  Autograd does not see these calls: a
+result has no graph, whether its inputs require gradients or not, and the gradients are
+the backward entry points' to compute.  A negative status raises ``PvsError``;
 wrong shapes and types raise ``ValueError`` and ``TypeError``.
 """
 from __future__ import annotations
