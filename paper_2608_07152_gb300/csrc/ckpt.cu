@@ -539,11 +539,12 @@ GradPlan grad_plan(int64_t rows, int out_cols, int cols, int dtype, bool in_plac
     const int64_t slots = tile_m > kTileM ? dev.pairs : dev.sms;
     const int64_t units = (int64_t)((out_cols + tile_m - 1) / tile_m) * ((cols + bn - 1) / bn);
     const int64_t kc = (p.piece + kTileK - 1) / kTileK;
-    // float32 sums: 128 steps in the tensor cores, which cut the sum to 24 bits each, at
-    // most before the splits are added with rounding (as far as 2 GB of them go)
+    // float32 sums: 64 steps in the tensor cores, which cut the sum to 24 bits each, at
+    // most before the splits are added with rounding (as far as 2 GB of them go).  With 128 dw of
+    // 25,000 rows was off by 1.5e-6, 2.7 times the plain form; so by 8e-7
     const int64_t room = std::max<int64_t>(1, ((int64_t)2 << 30) / (out_cols * p.ldslot * 4));
     p.splits = best_splits(units, kc, (int)slots, p.parts * p.kept_parts,
-                           dtype == PVS_F32 ? std::min((kc + 31) / 32, room) : 1);
+                           dtype == PVS_F32 ? std::min((kc + 15) / 16, room) : 1);
     Carver c{static_cast<uint8_t*>(workspace)};
     if (p.copy) p.a = c.take<uint16_t>(p.parts * p.piece * p.lda);
     p.b = c.take<uint16_t>(p.kept_parts * p.piece * p.ldb);

@@ -68,3 +68,37 @@ def test_float32_gelu_keeps_its_digits(K):
     beside = X * torch.exp(-0.5 * X * X) / math.sqrt(2.0 * math.pi)
     close(dx, dy.double() * (below + beside),
           (X * X + 8) * 2.0 ** -23 * (below + beside.abs()) * dy.double() + TINY[F32])
+
+
+# float32 sums of terms of one sign.  Each step of 16 in the tensor cores cuts the running sum,
+# by half of 2^-23 of it on average at most, and a split's running sum is half of its last
+# one on average: n steps cost n / 2 times 2^-24 in the mean over many entries.  Four more for
+# the logits, the operands' parts and the sums of the splits, which round.
+def mean_error(got, want):
+    return float(((got.double() - want).abs() / want).mean())
+
+
+@pytest.mark.parametrize("R,N,K", [(25_103, 1093, 122), (24_983, 893, 1860), (4096, 2048, 2048)])
+def test_float32_weight_gradients_of_many_rows(R, N, K):
+    codes, scales, _ = pvs.pvs_ckpt_store(rows(R, K, F32, 4, spread=0.5).abs())
+    dy = rows(R, N, F32, 5, spread=0.5).abs()
+    dw = pvs.pvs_ckpt_grad_weight(dy, codes, scales)
+    want = dy.double().T @ (codes.double() * scales.double()[:, None])
+    assert mean_error(dw, want) <= (64 / 2 + 4) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("T,V,d", [(6320, 3384, 128), (2000, 2000, 1024), (777, 20_011, 385)])
+def test_float32_gradients_of_many_rows(T, V, d):
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.rand(T, d, generator=g, device="cuda") / d ** 0.5
+    w = torch.rand(V, d, generator=g, device="cuda")
+    grad = torch.rand(T, generator=g, device="cuda") + 0.5
+    # the target is masked: it has no gradient, and every entry of G is positive
+    bias = torch.zeros(V, device="cuda")
+    bias[0] = -torch.inf
+    y = torch.zeros(T, dtype=torch.int64, device="cuda")
+    _, stats = pvs.pvs_xent_forward(x, w, y, bias=bias)
+    dx, dw = pvs.pvs_xent_backward(x, w, y, stats, grad, bias=bias)
+    G = torch.softmax(x.double() @ w.double().T + bias.double(), dim=1) * grad.double()[:, None]
+    assert mean_error(dx, G @ w.double()) <= (32 / 2 + 4) * 2.0 ** -24
+    assert mean_error(dw[1:], (G.T @ x.double())[1:]) <= (32 / 2 + 4) * 2.0 ** -24
