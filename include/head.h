@@ -15,8 +15,9 @@
  * Conventions:
  *   - Every matrix is in DEVICE memory, row-major with a leading dimension
  *     `ld` in elements (>= its columns); element types are pvs_dtype, held
- *     as the native bf16, f16 or float32.  Sums are float32.  A pointer is
- *     aligned to its elements where nothing else is said.
+ *     as the native bf16, f16 or float32.  Sums are float32; the tensor cores
+ *     cut the sum of each step of 16 terms to 24 bits, where float32 arithmetic
+ *     rounds.  A pointer is aligned to its elements where nothing else is said.
  *   - Every call queues its work on `cuda_stream` (a cudaStream_t; NULL: the
  *     legacy default stream) of the current device and returns; nothing is
  *     allocated and nothing waited for, so calls can be captured into a CUDA

@@ -504,7 +504,7 @@ pvs_status queued(cudaError_t e = cudaSuccess) {
 // bf16: dy is an operand as it lies, and the kept rows s z the other, in two bf16 parts:
 // what they lose is 2^-15 of an entry.  In one part they lost about half of what rounding dw
 // does (2.8e-3 against 2.3e-3 in all); dw of 768 -> 1,536 over 32,768 rows takes 128 us, 72 so
-// (f16 166, float32 249).  f16 and float32: dy s in two or three bf16 parts, and
+// (f16 166, float32 274).  f16 and float32: dy s in two or three bf16 parts, and
 // the codes as they are (exact).
 // Rows go by in pieces whose copies take 1 GB (4,096 rows at least), each added to the sums of
 // the one before.
