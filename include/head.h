@@ -200,6 +200,30 @@ pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch, const uint8_
                          const void* scales, int64_t rows, int32_t cols, int32_t group,
                          int32_t dtype, void* y, int64_t ldy, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Rows of a table by their ids, for the tokens or items that a head is fed with:
+ *     y_t = scale w[ids[t]]                          [rows x dim], in w's type
+ * and the table's gradient
+ *     dw_v = scale sum_{t: ids[t] = v} dy_t          [items x dim], in dy's type
+ * for a row of the table that no id names, zeros.  Each output is rounded once; a
+ * sum is float32, of whole stretches of the order of t, and the same in every call.
+ *   - ids[t] == ignore_index: a row of zeros, and no gradient, whatever dy_t holds.
+ *   - any other id outside [0, items): a row of NaN, and no gradient.
+ * 0 <= rows <= 2^31 - 2^16, 1 <= items <= 2^31 - 2^16, 1 <= dim <= 32767; scale finite.
+ * Outputs may not overlap inputs.
+ * ------------------------------------------------------------------------ */
+pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t items, int32_t dim, int32_t dtype,
+                             const int64_t* ids, int64_t rows, float scale, int64_t ignore_index,
+                             void* y, int64_t ldy, void* cuda_stream);
+
+/* Scratch of the gradient: 16 bytes an id at most, 4 KB for every 2,048 of more than 4,096
+ * ids, and two float32 rows for every 32 ids. */
+pvs_status pvs_embed_workspace(int64_t rows, int64_t items, int32_t dim, size_t* bytes);
+pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int64_t* ids, int64_t rows,
+                              int64_t items, int32_t dim, int32_t dtype, float scale,
+                              int64_t ignore_index, void* dw, int64_t lddw, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,668 @@
+// Rows of a table looked up by their ids, scaled, and the table's gradient (head.h).
+//
+//   forward    y_t = s w[id_t]
+//   backward   dw_v = s sum_{t: id_t = v} dy_t, a float32 sum in the order of t
+//
+// Both are bound by memory.  The backward pass sorts (id, t) first, so that a row's sum runs
+// over neighbours, nothing is added by atomics and the result depends on nothing but the
+// call: up to kSmall ids in one block's shared memory, more by a stable radix sort of 10 bits
+// a pass.  Then a warp takes 32 sorted entries by 256 columns, eight rows' loads in flight, and
+// writes the rows whose entries all lie among them; sums of rows that run on over several
+// such pieces are kept in float32 and joined by a second launch.  Rows without an entry are
+// found by search in the sorted ids and filled with zeros by other blocks of the first: no
+// row of dw is written twice.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/head.h"
+#include "head_gemm.h"
+#include "kernels.h"
+#include "pvs_common.cuh"
+
+namespace pvs {
+namespace head {
+namespace {
+
+constexpr int kEmbedThreads = 256;
+constexpr int kEmbedWarps = kEmbedThreads / 32;
+constexpr int kSmall = 4096;         // ids that one block sorts
+constexpr int kDigitBits = 10;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kKeysPerThread = 8;
+constexpr int kSortTile = kEmbedThreads * kKeysPerThread;
+constexpr int kPiece = 32;           // sorted entries to a warp
+constexpr int kSlab = 256;           // and columns
+constexpr int kZeroRows = 32;        // rows that a warp searches at once
+
+__device__ __forceinline__ float widen(const void* p, int dtype, int64_t i) {
+    if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
+    if (dtype == PVS_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+    return __half2float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ uint16_t narrow(float v, int dtype) {
+    if (dtype == PVS_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    return __half_as_ushort(__float2half_rn(v));
+}
+__device__ __forceinline__ void put(void* p, int dtype, int64_t i, float v) {
+    if (dtype == PVS_F32)
+        static_cast<float*>(p)[i] = v;
+    else
+        static_cast<uint16_t*>(p)[i] = narrow(v, dtype);
+}
+__device__ __forceinline__ void widen_two(uint32_t u, int dtype, float& lo, float& hi) {
+    if (dtype == PVS_BF16) {
+        lo = __uint_as_float(u << 16);
+        hi = __uint_as_float(u & 0xffff0000u);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+__device__ __forceinline__ uint32_t narrow_two(float lo, float hi, int dtype) {
+    return (uint32_t)narrow(lo, dtype) | (uint32_t)narrow(hi, dtype) << 16;
+}
+
+// Eight elements of a row, a lane's share of 256: neighbours (WIDE: the row is aligned to 16
+// bytes and holds whole eights) or 32 apart.  Nothing is read past the row.
+template <bool WIDE>
+__device__ __forceinline__ void load_share(const void* p, int dtype, int64_t row, int col0, int dim,
+                                           float (&v)[8]) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (WIDE) {
+        const int c = col0 + 8 * lane;
+        if (c >= dim) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        } else if (dtype == PVS_F32) {
+            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
+            const float4 a = __ldg(q), b = __ldg(q + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+            v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a =
+                __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c));
+            widen_two(a.x, dtype, v[0], v[1]);
+            widen_two(a.y, dtype, v[2], v[3]);
+            widen_two(a.z, dtype, v[4], v[5]);
+            widen_two(a.w, dtype, v[6], v[7]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = col0 + lane + 32 * i;
+            v[i] = c < dim ? widen(p, dtype, row + c) : 0.0f;
+        }
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_share(void* p, int dtype, int64_t row, int col0, int dim,
+                                            const float (&v)[8]) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (WIDE) {
+        const int c = col0 + 8 * lane;
+        if (c >= dim) return;
+        if (dtype == PVS_F32) {
+            float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + row + c);
+            q[0] = make_float4(v[0], v[1], v[2], v[3]);
+            q[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + row + c) =
+                make_uint4(narrow_two(v[0], v[1], dtype), narrow_two(v[2], v[3], dtype),
+                           narrow_two(v[4], v[5], dtype), narrow_two(v[6], v[7], dtype));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = col0 + lane + 32 * i;
+            if (c < dim) put(p, dtype, row + c, v[i]);
+        }
+    }
+}
+
+// ---- lookup ------------------------------------------------------------------------
+struct LookupArgs {
+    const void* w;
+    int64_t ldw, items;
+    const int64_t* ids;
+    int64_t rows, ignore_index;
+    int dim, dtype;
+    float scale;
+    void* y;
+    int64_t ldy;
+    int slabs;
+};
+
+// A warp takes 256 columns of a row.
+template <bool WIDE>
+__global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const LookupArgs a) {
+    next_early();
+    wait_before();
+    const int64_t units = a.rows * a.slabs, step = (int64_t)gridDim.x * kEmbedWarps;
+    for (int64_t u = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); u < units; u += step) {
+        const int64_t row = u / a.slabs;
+        const int col0 = (int)(u - row * a.slabs) * kSlab;
+        const int64_t id = __ldg(a.ids + row);
+        float v[8];
+        if (id == a.ignore_index || id < 0 || id >= a.items) {
+            const float f = id == a.ignore_index ? 0.0f : __int_as_float(0x7fffffff);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = f;
+        } else {
+            load_share<WIDE>(a.w, a.dtype, id * a.ldw, col0, a.dim, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+        }
+        store_share<WIDE>(a.y, a.dtype, row * a.ldy, col0, a.dim, v);
+    }
+}
+
+// ---- sorting -----------------------------------------------------------------------
+// An id as a key: `items`, past every row, for what has no row.
+__device__ __forceinline__ uint32_t key_of(int64_t id, int64_t ignore_index, int64_t items) {
+    return id == ignore_index || id < 0 || id >= items ? (uint32_t)items : (uint32_t)id;
+}
+
+// Up to kSmall ids in one block: (key, position) as one number, a bitonic network over the next
+// power of two.
+__global__ void __launch_bounds__(1024) embed_sort_small_kernel(const int64_t* __restrict__ ids, int n,
+                                                                int padded, int64_t ignore_index,
+                                                                int64_t items, uint32_t* keys,
+                                                                uint32_t* places) {
+    __shared__ unsigned long long s[kSmall];
+    next_early();
+    wait_before();
+    for (int i = threadIdx.x; i < padded; i += blockDim.x)
+        s[i] = i < n ? (unsigned long long)key_of(ids[i], ignore_index, items) << 32 | (uint32_t)i
+                     : ~0ull;
+    for (int k = 2; k <= padded; k <<= 1) {
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            __syncthreads();
+            for (int t = threadIdx.x; t < padded / 2; t += blockDim.x) {
+                const int i = (t / j) * 2 * j + t % j, l = i + j;
+                const unsigned long long x = s[i], y = s[l];
+                if ((x > y) == ((i & k) == 0)) {
+                    s[i] = y;
+                    s[l] = x;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        keys[i] = (uint32_t)(s[i] >> 32);
+        places[i] = (uint32_t)s[i];
+    }
+}
+
+struct SortArgs {
+    const int64_t* ids;              // of the first pass, else null
+    int64_t ignore_index, items;
+    const uint32_t *keys, *places;   // of the passes after it
+    uint32_t *keys_out, *places_out;
+    int64_t n;
+    int shift, digits;               // this pass's digit
+    int64_t tiles;
+    uint32_t* counts;                // [digits][tiles]
+    uint32_t* totals;                // [digits]
+};
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
+    return a.ids ? key_of(a.ids[i], a.ignore_index, a.items) : a.keys[i];
+}
+__device__ __forceinline__ int digit_of(const SortArgs& a, uint32_t key) {
+    return (int)(key >> a.shift) & (a.digits - 1);
+}
+
+// How often each digit comes in each tile.
+__global__ void __launch_bounds__(kEmbedThreads) embed_count_kernel(const SortArgs a) {
+    __shared__ uint32_t count[kDigits];
+    for (int d = threadIdx.x; d < a.digits; d += kEmbedThreads) count[d] = 0;
+    next_early();
+    wait_before();
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * kSortTile;
+#pragma unroll
+    for (int r = 0; r < kKeysPerThread; ++r) {
+        const int64_t i = base + r * kEmbedThreads + threadIdx.x;
+        if (i < a.n) atomicAdd(&count[digit_of(a, sort_key(a, i))], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < a.digits; d += kEmbedThreads)
+        a.counts[d * a.tiles + blockIdx.x] = count[d];
+}
+
+__device__ __forceinline__ uint32_t inclusive_sum(uint32_t v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+
+// A digit's counts to what comes before each tile; a warp to a digit.
+__global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const SortArgs a) {
+    next_early();
+    wait_before();
+    const int d = blockIdx.x * kEmbedWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (d >= a.digits) return;
+    uint32_t before = 0;
+    for (int64_t t0 = 0; t0 < a.tiles; t0 += 32) {
+        const int64_t t = t0 + lane;
+        const uint32_t v = t < a.tiles ? a.counts[d * a.tiles + t] : 0u;
+        const uint32_t s = inclusive_sum(v);
+        if (t < a.tiles) a.counts[d * a.tiles + t] = before + s - v;
+        before += __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (lane == 0) a.totals[d] = before;
+}
+
+// A tile's entries to their places.  A warp ranks its 256 neighbours in order, 32 at a time:
+// equal digits among them by a match, those before by the warp's own counts.
+__global__ void __launch_bounds__(kEmbedThreads) embed_place_kernel(const SortArgs a) {
+    __shared__ uint16_t count[kEmbedWarps][kDigits];
+    __shared__ uint32_t first[kDigits];
+    __shared__ uint32_t sums[kEmbedWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < kEmbedWarps * a.digits; i += kEmbedThreads)
+        count[i / a.digits][i % a.digits] = 0;
+    next_early();
+    wait_before();
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * kSortTile + warp * 32 * kKeysPerThread;
+    uint32_t key[kKeysPerThread], place[kKeysPerThread], rank[kKeysPerThread];
+#pragma unroll
+    for (int r = 0; r < kKeysPerThread; ++r) {
+        const int64_t i = base + 32 * r + lane;
+        key[r] = i < a.n ? sort_key(a, i) : 0u;
+        place[r] = i < a.n ? (a.ids ? (uint32_t)i : a.places[i]) : 0u;
+    }
+#pragma unroll
+    for (int r = 0; r < kKeysPerThread; ++r) {
+        const bool in = base + 32 * r + lane < a.n;
+        const int d = in ? digit_of(a, key[r]) : kDigits;
+        const uint32_t peers = __match_any_sync(0xffffffffu, d);
+        const uint32_t before = in ? count[warp][d] : 0u;
+        rank[r] = before + __popc(peers & ((1u << lane) - 1u));
+        __syncwarp();
+        if (in && lane == 31 - __clz(peers)) count[warp][d] = (uint16_t)(before + __popc(peers));
+        __syncwarp();
+    }
+    // where each digit starts among all: a scan of the totals, four to a thread
+    const int per = kDigits / kEmbedThreads;
+    uint32_t mine[per], sum = 0;
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+        const int d = threadIdx.x * per + k;
+        mine[k] = sum;
+        if (d < a.digits) sum += a.totals[d];
+    }
+    const uint32_t incl = inclusive_sum(sum);
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    uint32_t start = incl - sum;
+    for (int w = 0; w < warp; ++w) start += sums[w];
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+        const int d = threadIdx.x * per + k;
+        if (d < a.digits) {
+            first[d] = start + mine[k] + a.counts[d * a.tiles + blockIdx.x];
+            uint32_t before = 0;
+            for (int w = 0; w < kEmbedWarps; ++w) {
+                const uint32_t c = count[w][d];
+                count[w][d] = (uint16_t)before;
+                before += c;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kKeysPerThread; ++r) {
+        if (base + 32 * r + lane >= a.n) continue;
+        const int d = digit_of(a, key[r]);
+        const uint32_t to = first[d] + count[warp][d] + rank[r];
+        a.keys_out[to] = key[r];
+        a.places_out[to] = place[r];
+    }
+}
+
+// ---- sums --------------------------------------------------------------------------
+struct SumArgs {
+    const void* dy;
+    int64_t lddy;
+    const uint32_t *keys, *places;
+    int64_t n, items;
+    int dim, dtype, slabs;
+    float scale;
+    void* dw;
+    int64_t lddw;
+    float* part;                     // [piece][2][ldp]: of a run from before, and one that goes on
+    int64_t ldp;
+    int64_t pieces, sum_blocks;
+};
+
+// The first of the sorted keys that is v or more.
+__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t v) {
+    int64_t lo = 0;
+    while (n > 0) {
+        const int64_t half = n >> 1;
+        if (__ldg(keys + lo + half) < v) {
+            lo += half + 1;
+            n -= half + 1;
+        } else {
+            n = half;
+        }
+    }
+    return lo;
+}
+
+template <bool WIDE>
+__device__ void zero_rows(const SumArgs& a, int64_t first) {
+    const int lane = threadIdx.x & 31;
+    const int64_t v = first + lane;
+    bool empty = false;
+    if (v < a.items) {
+        const int64_t at = lower_bound(a.keys, a.n, (uint32_t)v);
+        empty = at >= a.n || __ldg(a.keys + at) != (uint32_t)v;
+    }
+    const float zeros[8] = {};
+    for (uint32_t rows = __ballot_sync(0xffffffffu, empty); rows != 0; rows &= rows - 1) {
+        const int64_t row = first + __ffs(rows) - 1;
+        for (int c = 0; c < a.dim; c += kSlab)
+            store_share<WIDE>(a.dw, a.dtype, row * a.lddw, c, a.dim, zeros);
+    }
+}
+
+template <bool WIDE>
+__global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs a) {
+    next_early();
+    wait_before();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x >= a.sum_blocks) {
+        const int64_t step = ((int64_t)gridDim.x - a.sum_blocks) * kEmbedWarps * kZeroRows;
+        for (int64_t v = (((int64_t)blockIdx.x - a.sum_blocks) * kEmbedWarps + warp) * kZeroRows;
+             v < a.items; v += step)
+            zero_rows<WIDE>(a, v);
+        return;
+    }
+    const int64_t u = (int64_t)blockIdx.x * kEmbedWarps + warp;
+    const int64_t piece = u / a.slabs;
+    if (piece >= a.pieces) return;
+    const int col0 = (int)(u - piece * a.slabs) * kSlab;
+    const int64_t base = piece * kPiece;
+    const uint32_t none = (uint32_t)a.items;
+    const uint32_t key = base + lane < a.n ? __ldg(a.keys + base + lane) : none;
+    const uint32_t place = base + lane < a.n ? __ldg(a.places + base + lane) : 0u;
+    const uint32_t before = base > 0 ? __ldg(a.keys + base - 1) : none;
+    const uint32_t after = base + kPiece < a.n ? __ldg(a.keys + base + kPiece) : none;
+    // entries without a row come last
+    const int count = __popc(__ballot_sync(0xffffffffu, key != none));
+    float acc[8] = {};
+    bool from_before = count > 0 && __shfl_sync(0xffffffffu, key, 0) == before;
+    constexpr int kFlight = 8;
+    for (int i0 = 0; i0 < count; i0 += kFlight) {
+        float v[kFlight][8];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const uint32_t p = __shfl_sync(0xffffffffu, place, (i0 + i) & 31);
+            if (i0 + i < count) load_share<WIDE>(a.dy, a.dtype, (int64_t)p * a.lddy, col0, a.dim, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (i0 + i >= count) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
+            const uint32_t here = __shfl_sync(0xffffffffu, key, i0 + i);
+            const uint32_t next =
+                i0 + i + 1 < kPiece ? __shfl_sync(0xffffffffu, key, (i0 + i + 1) & 31) : after;
+            const bool goes_on = next == here;
+            if (goes_on && i0 + i + 1 < kPiece) continue;
+            if (!from_before && !goes_on) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] *= a.scale;
+                store_share<WIDE>(a.dw, a.dtype, (int64_t)here * a.lddw, col0, a.dim, acc);
+            } else {
+                float* to = a.part + (2 * piece + (from_before ? 0 : 1)) * a.ldp;
+                store_share<WIDE>(to, PVS_F32, 0, col0, a.dim, acc);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
+            from_before = false;
+        }
+    }
+}
+
+// A run that goes on past the piece that it starts in: its pieces' sums, 32 warps over them in
+// turn and their sums in the warps' order.
+constexpr int kJoinThreads = 1024;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinCols = 128;
+__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs a, int slabs) {
+    __shared__ float4 sh[kJoinWarps][32];
+    next_early();
+    wait_before();
+    const int64_t step = gridDim.x / slabs;
+    const int col = (int)(blockIdx.x % slabs) * kJoinCols + 4 * (threadIdx.x & 31);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int64_t piece = blockIdx.x / slabs; piece + 1 < a.pieces; piece += step) {
+        const int64_t end = (piece + 1) * kPiece;
+        const uint32_t key = __ldg(a.keys + end - 1);
+        // (every thread of the block sees the same)
+        if (key == (uint32_t)a.items || __ldg(a.keys + end) != key) continue;
+        const bool all_piece = __ldg(a.keys + piece * kPiece) == key;
+        if (all_piece && piece > 0 && __ldg(a.keys + piece * kPiece - 1) == key) continue;
+        const int64_t last = (lower_bound(a.keys + end, a.n - end, key + 1) + end - 1) / kPiece;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (col < a.ldp) {
+#pragma unroll 4
+            for (int64_t q = piece + warp; q <= last; q += kJoinWarps) {
+                const float4 v = *reinterpret_cast<const float4*>(
+                    a.part + (2 * q + (q == piece ? 1 : 0)) * a.ldp + col);
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+        }
+        sh[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0) {
+            const int used = (int)min((int64_t)kJoinWarps, last - piece + 1);
+            for (int w = 1; w < used; ++w) {
+                const float4 v = sh[w][lane];
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+            const float f[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < a.dim) put(a.dw, a.dtype, (int64_t)key * a.lddw + col + k, f[k] * a.scale);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- the plan of a call --------------------------------------------------------------
+struct EmbedPlan {
+    int passes = 0, bits = 0;
+    int64_t tiles = 0, pieces = 0, ldp = 0;
+    uint32_t *keys[2] = {}, *places[2] = {}, *counts = nullptr, *totals = nullptr;
+    float* part = nullptr;
+    size_t bytes = 0;
+};
+
+EmbedPlan embed_plan(int64_t n, int64_t items, int dim, void* workspace) {
+    EmbedPlan p;
+    Carver c{static_cast<uint8_t*>(workspace)};
+    p.keys[0] = c.take<uint32_t>(n);
+    p.places[0] = c.take<uint32_t>(n);
+    if (n > kSmall) {
+        int width = 1;
+        while (items >> width) ++width;                // of the largest key, `items`
+        p.passes = (width + kDigitBits - 1) / kDigitBits;
+        p.bits = (width + p.passes - 1) / p.passes;
+        p.tiles = (n + kSortTile - 1) / kSortTile;
+        if (p.passes > 1) {
+            p.keys[1] = c.take<uint32_t>(n);
+            p.places[1] = c.take<uint32_t>(n);
+        }
+        p.counts = c.take<uint32_t>(p.tiles << p.bits);
+        p.totals = c.take<uint32_t>((int64_t)1 << p.bits);
+    }
+    p.pieces = (n + kPiece - 1) / kPiece;
+    p.ldp = round_up(dim, 8);
+    if (p.pieces > 1) p.part = c.take<float>(p.pieces * 2 * p.ldp);
+    p.bytes = c.used;
+    return p;
+}
+
+bool embed_shape(int64_t rows, int64_t items, int32_t dim, int32_t dtype) {
+    return rows >= 0 && rows <= kMaxRows && items >= 1 && items <= kMaxRows && dim >= 1 && dim <= 32767 &&
+           dtype >= PVS_BF16 && dtype <= PVS_F32;
+}
+bool on_16(const void* p, int64_t ld, int dtype) {
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % (dtype == PVS_F32 ? 4 : 8) == 0;
+}
+pvs_status embed_ended(cudaError_t e) {
+    if (e == cudaSuccess) return PVS_OK;
+    cudaGetLastError();
+    return PVS_ERR_CUDA;
+}
+
+// The sorted entries' place in the plan's buffers.
+cudaError_t sort_ids(const int64_t* ids, int64_t n, int64_t items, int64_t ignore_index,
+                     const EmbedPlan& p, int* where, cudaStream_t st) {
+    *where = 0;
+    if (p.passes == 0) {
+        int padded = 2;
+        while (padded < n) padded *= 2;
+        count_launches(1);
+        return launch_early(embed_sort_small_kernel, 1, std::min(1024, std::max(32, padded / 2)), 0, st,
+                            ids, (int)n, padded, ignore_index, items, p.keys[0], p.places[0]);
+    }
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < p.passes && e == cudaSuccess; ++i) {
+        // the last pass ends in the first buffers
+        const int to = (p.passes - 1 - i) & 1;
+        SortArgs s{};
+        s.ids = i == 0 ? ids : nullptr;
+        s.ignore_index = ignore_index;
+        s.items = items;
+        s.keys = p.keys[to ^ 1];
+        s.places = p.places[to ^ 1];
+        s.keys_out = p.keys[to];
+        s.places_out = p.places[to];
+        s.n = n;
+        s.shift = i * p.bits;
+        s.digits = 1 << p.bits;
+        s.tiles = p.tiles;
+        s.counts = p.counts;
+        s.totals = p.totals;
+        count_launches(3);
+        e = launch_early(embed_count_kernel, p.tiles, kEmbedThreads, 0, st, s);
+        if (e == cudaSuccess)
+            e = launch_early(embed_scan_kernel, (s.digits + kEmbedWarps - 1) / kEmbedWarps, kEmbedThreads,
+                             0, st, s);
+        if (e == cudaSuccess) e = launch_early(embed_place_kernel, p.tiles, kEmbedThreads, 0, st, s);
+    }
+    return e;
+}
+
+}  // namespace
+}  // namespace head
+}  // namespace pvs
+
+using namespace pvs;
+using namespace pvs::head;
+
+extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t items, int32_t dim,
+                                        int32_t dtype, const int64_t* ids, int64_t rows, float scale,
+                                        int64_t ignore_index, void* y, int64_t ldy, void* cuda_stream) {
+    if (!embed_shape(rows, items, dim, dtype) || ldw < dim || ldy < dim || !std::isfinite(scale))
+        return PVS_ERR_INVALID;
+    if (rows == 0) return PVS_OK;
+    const int es = element_bytes(dtype);
+    if (!w || !ids || !y || !on_elements(w, es) || !on_elements(y, es) || !on_elements(ids, 8))
+        return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
+    LookupArgs a{};
+    a.w = w;
+    a.ldw = ldw;
+    a.items = items;
+    a.ids = ids;
+    a.rows = rows;
+    a.ignore_index = ignore_index;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.scale = scale;
+    a.y = y;
+    a.ldy = ldy;
+    a.slabs = (dim + kSlab - 1) / kSlab;
+    const bool wide = dim % 8 == 0 && on_16(w, ldw, dtype) && on_16(y, ldy, dtype);
+    const int64_t blocks = (rows * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
+    count_launches(1);
+    return embed_ended(launch_early(wide ? embed_forward_kernel<true> : embed_forward_kernel<false>,
+                                    std::min<int64_t>(blocks, 1 << 24), kEmbedThreads, 0,
+                                    static_cast<cudaStream_t>(cuda_stream), a));
+}
+
+extern "C" pvs_status pvs_embed_workspace(int64_t rows, int64_t items, int32_t dim, size_t* bytes) {
+    if (!bytes || !embed_shape(rows, items, dim, PVS_F32)) return PVS_ERR_INVALID;
+    *bytes = rows == 0 ? 0 : embed_plan(rows, items, dim, nullptr).bytes;
+    return PVS_OK;
+}
+
+extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int64_t* ids, int64_t rows,
+                                         int64_t items, int32_t dim, int32_t dtype, float scale,
+                                         int64_t ignore_index, void* dw, int64_t lddw, void* workspace,
+                                         size_t workspace_bytes, void* cuda_stream) {
+    if (!embed_shape(rows, items, dim, dtype) || lddy < dim || lddw < dim || !std::isfinite(scale))
+        return PVS_ERR_INVALID;
+    const int es = element_bytes(dtype);
+    if (!dw || !on_elements(dw, es)) return PVS_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (rows > 0 && (!dy || !ids || !on_elements(dy, es) || !on_elements(ids, 8))) return PVS_ERR_INVALID;
+    const EmbedPlan p = rows > 0 ? embed_plan(rows, items, dim, workspace) : EmbedPlan{};
+    if (workspace_bytes < p.bytes ||
+        (p.bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))))
+        return PVS_ERR_INVALID;
+    Device dev;
+    const pvs_status before = (pvs_status)ready(&dev);
+    if (before != PVS_OK) return before;
+    if (rows == 0)
+        return embed_ended(cudaMemset2DAsync(dw, (size_t)lddw * es, 0, (size_t)dim * es, (size_t)items, st));
+    int where = 0;
+    cudaError_t e = sort_ids(ids, rows, items, ignore_index, p, &where, st);
+    if (e != cudaSuccess) return embed_ended(e);
+    SumArgs a{};
+    a.dy = dy;
+    a.lddy = lddy;
+    a.keys = p.keys[where];
+    a.places = p.places[where];
+    a.n = rows;
+    a.items = items;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.slabs = (dim + kSlab - 1) / kSlab;
+    a.scale = scale;
+    a.dw = dw;
+    a.lddw = lddw;
+    a.part = p.part;
+    a.ldp = p.ldp;
+    a.pieces = p.pieces;
+    a.sum_blocks = (p.pieces * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
+    const int64_t zero = std::min<int64_t>((items + kEmbedWarps * kZeroRows - 1) / (kEmbedWarps * kZeroRows),
+                                           (int64_t)1 << 16);
+    const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
+    if (a.sum_blocks + zero > 0x7fffffff) return PVS_ERR_INVALID;
+    count_launches(1);
+    e = launch_early(wide ? embed_sum_kernel<true> : embed_sum_kernel<false>, a.sum_blocks + zero,
+                     kEmbedThreads, 0, st, a);
+    if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
+    const int slabs = (int)((p.ldp + kJoinCols - 1) / kJoinCols);
+    const int64_t owners = std::min<int64_t>(p.pieces - 1, std::max(1, 8 * dev.sms / slabs));
+    count_launches(1);
+    return embed_ended(launch_early(embed_join_kernel, owners * slabs, kJoinThreads, 0, st, a, slabs));
+}

@@ -48,6 +48,11 @@ _SIGNATURES = {
     "pvs_wq_pack": (_i32, [_P, _i64, _i64, _i32, _i32, _i32, _P, _P, _P]),
     "pvs_wq_unpack": (_i32, [_P, _P, _i64, _i32, _i32, _P, _i64, _i32, _P]),
     "pvs_wq_matvec": (_i32, [_P, _i64, _i32, _P, _P, _i64, _i32, _i32, _i32, _P, _i64, _P]),
+    "pvs_embed_forward": (_i32, [_P, _i64, _i64, _i32, _i32, _P, _i64, ctypes.c_float, _i64, _P,
+                                 _i64, _P]),
+    "pvs_embed_workspace": (_i32, [_i64, _i64, _i32, _P]),
+    "pvs_embed_backward": (_i32, [_P, _i64, _P, _i64, _i64, _i32, _i32, ctypes.c_float, _i64, _P,
+                                  _i64, _P, ctypes.c_size_t, _P]),
 }
 EXPORTED = tuple(_SIGNATURES)
 
@@ -390,3 +395,56 @@ def pvs_wq_matvec(x, codes, scales, group: int):
     _check(_lib.pvs_wq_matvec(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), n, k, int(group), dt,
                               _ptr(y), n, _stream(device)), "pvs_wq_matvec")
     return y
+
+
+def _finite(scale: float) -> float:
+    if not abs(scale) < float("inf"):
+        raise ValueError("scale must be finite")
+    return float(scale)
+
+
+def pvs_embed_forward(w, ids, scale: float = 1.0, ignore_index: int = -100):
+    """Rows of the table w [V, d] by their ids, int64 [T], times `scale`: [T, d] in w's
+    type.  ``ignore_index`` gives a row of zeros, another id outside the table NaN."""
+    device = _on_gpu(w, ids)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_embed_forward(w, ids, scale, ignore_index)
+    w, ldw = _matrix(w, "w")
+    dt = _dtype_code(w.dtype)
+    items, dim = w.shape
+    if items < 1:
+        raise ValueError("w must have a row at least")
+    ids = _vector(ids, "ids", ids.shape[0] if ids.dim() == 1 else -1, torch.int64)
+    if ids.shape[0] > _MAX_ROWS:
+        raise ValueError(f"more than {_MAX_ROWS} ids")
+    y = torch.empty(ids.shape[0], dim, dtype=w.dtype, device=device)
+    _check(_lib.pvs_embed_forward(_ptr(w), ldw, items, dim, dt, _ptr(ids), ids.shape[0],
+                                  _finite(scale), int(ignore_index), _ptr(y), dim, _stream(device)),
+           "pvs_embed_forward")
+    return y
+
+
+def pvs_embed_backward(dy, ids, items: int, scale: float = 1.0, ignore_index: int = -100):
+    """The gradient [items, d] of a table from the gradient dy [T, d] of the rows that
+    ``pvs_embed_forward`` took from it, in dy's type."""
+    device = _on_gpu(dy, ids)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_embed_backward(dy, ids, items, scale, ignore_index)
+    dy, lddy = _matrix(dy, "dy")
+    dt = _dtype_code(dy.dtype)
+    rows, dim = dy.shape
+    ids = _vector(ids, "ids", rows, torch.int64)
+    items = int(items)
+    if items < 1 or items > _MAX_ROWS:
+        raise ValueError(f"items must be in [1, {_MAX_ROWS}]")
+    scale = _finite(scale)
+    dw = torch.empty(items, dim, dtype=dy.dtype, device=device)
+    n = ctypes.c_size_t()
+    _check(_lib.pvs_embed_workspace(rows, items, dim, ctypes.byref(n)), "pvs_embed_workspace")
+    ws = _workspace(n.value, device)
+    _check(_lib.pvs_embed_backward(_ptr(dy), lddy, _ptr(ids), rows, items, dim, dt, scale,
+                                   int(ignore_index), _ptr(dw), dim, _ptr(ws), n.value,
+                                   _stream(device)), "pvs_embed_backward")
+    return dw
