@@ -130,6 +130,49 @@ pvs_status pvs_xent_backward(const pvs_xent_args* args, const float* stats,
                              void* cuda_stream);
 
 /* ---------------------------------------------------------------------------
+ * Distillation: a row's target is a teacher's distribution over the items of its list (its
+ * `top` best, say).  With l_tj as above, slots k of ids i_tk and teacher logits z_tk, and
+ * c = teacher_scale:
+ *     p_tk   = exp(c z_tk) / sum_k exp(c z_tk)
+ *     loss_t = sum_k p_tk (ln p_tk - l_{t, i_tk} + ln(sum_j exp(l_tj)))
+ * the divergence of the student's softmax over all items from the teacher's over the list;
+ * dloss_t / dl_tj = softmax(l_t)_j - sum_{k: i_tk = j} p_tk.
+ *   - a slot whose id is ignore_index, whose c z_tk is -inf, or whose item's bias is -inf (an
+ *     item that was deleted after the list was made) is not in the list: the others share its part.
+ *   - no slot in the list: loss 0 and no gradient, whatever the row holds.
+ *   - any other id outside [0, items): the loss is NaN, and so are the gradients that the row
+ *     reaches.
+ *   - an id that a list has twice: its slots' shares add up.
+ * Biases, overflows and types are as in the softmax cross entropy.
+ * ------------------------------------------------------------------------ */
+typedef struct pvs_distill_args {
+    pvs_xent_args student;    /* targets are not used; ignore_index is that of ids   */
+    const int64_t* ids;       /* [rows x top] without gaps                           */
+    const void* logits;       /* [rows x top] without gaps                           */
+    int32_t top;              /* 1 .. 1024                                           */
+    int32_t teacher_dtype;    /* pvs_dtype of logits                                 */
+    float teacher_scale;      /* c > 0, a normal float32                             */
+    int32_t reserved;         /* 0                                                   */
+} pvs_distill_args;
+
+/* Bytes of scratch of the two calls, as pvs_xent_workspace; forward, 6 more for each slot and 2
+ * for each row and 256 items of a block of rows; backward, 8 more for each row. */
+pvs_status pvs_distill_workspace(const pvs_distill_args* args, int32_t backward, size_t* bytes);
+
+/* loss [rows], stats [rows x 4] (16-byte aligned) and hits [rows x top], all float32.  stats
+ * and hits are for the backward pass: a row's m and s with sum_j exp(l_tj) = s 2^m, 0 and
+ * -inf; and dloss_t / dl of each slot's item, 2 for a slot that is not in the list. */
+pvs_status pvs_distill_forward(const pvs_distill_args* args, float* loss, float* stats, float* hits,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The gradients of sum_t grad_loss[t] loss_t, as pvs_xent_backward's; logits and teacher_scale
+ * are not used (teacher_scale is checked). */
+pvs_status pvs_distill_backward(const pvs_distill_args* args, const float* stats, const float* hits,
+                                const float* grad_loss, void* dx, int64_t lddx, void* dw,
+                                int64_t lddw, void* workspace, size_t workspace_bytes,
+                                void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
  * Rows kept in 8 bits.  Row r of x [rows x cols] is kept as Sec. 2.3.1 keeps
  * a vector, its scale to within a last bit: s_r = RN(max|x| RN(1 / 127)) (1 for a
  * zero row, the smallest positive float32 where that underflows), z =

@@ -34,6 +34,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <climits>
 #include <mutex>
 
 #include "../../include/head.h"
@@ -569,6 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         const Softmax& sm = a.sm;
         const uint32_t tempty_at[2] = {kCta == 2 ? cluster_map(&sh.tempty[0], 0) : 0u,
                                        kCta == 2 ? cluster_map(&sh.tempty[1], 0) : 0u};
+        constexpr bool kAnyStats = EPI == kStats || EPI == kTopStats;
         int it = 0;
         [[maybe_unused]] int part_at = 0, row_before = 0;
         bool dead = false;
@@ -581,6 +583,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
             [[maybe_unused]] float row_k2 = 0.0f;
             [[maybe_unused]] uint32_t yt = ~0u, targets_in = 0;   // the target's column, chunks with one
             [[maybe_unused]] GradRow gr;
+            [[maybe_unused]] int listed = INT_MAX, list_left = 0;   // the row's next listed item
+            [[maybe_unused]] const int* list = nullptr;
             if constexpr (EPI != kOut) {
                 // the tile's biases, and which of its columns are in the softmax
                 const int item = sm.item0 + n0 + et;
@@ -597,7 +601,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     if (sm.col_unit) sh.unit[b][et] = et < ncols ? __ldg(sm.col_unit + n0 + et) : 0.0f;
                     if (lane == 0) sh.masked[b][et >> 5] = mask;
                 }
-                if constexpr (EPI == kStats) {
+                if constexpr (EPI == kTopStats) {
+                    if (row < sm.rows) {
+                        const int at = __ldg(sm.list_first + (int64_t)(sm.part0 + w.nt) * sm.rows + row);
+                        list = sm.list + (int64_t)row * sm.top + at;
+                        list_left = sm.top - at;
+                        if (list_left > 0) listed = __ldg(list);
+                    }
+                } else if constexpr (EPI == kStats) {
                     if (row < sm.rows) y = __ldg(sm.targets + row) - (sm.item0 + n0);
                 } else {
                     gr = GradRow{0.0f, 0.0f, 0.0f, -1};
@@ -611,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 yt = y >= 0 && y < kTileN ? (uint32_t)y : ~0u;
                 targets_in = __reduce_or_sync(0xffffffffu, yt < kTileN ? 1u << (yt >> 5) : 0u);
                 asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
-                if constexpr (EPI == kStats) {
+                if constexpr (kAnyStats) {
                     // the tile before this one: all its shares are in shared memory
                     if (it > 0 && group == 0)
                         write_stats(sh.rowstat[b ^ 1], sm, part_at, row_before, row_in_tile);
@@ -710,10 +721,21 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                         for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
                     }
                     // the column of the row's target, as a bit, where a row has one here
-                    const bool any_here = (targets_in >> cc) & 1u;
-                    const uint32_t here = (yt >> 5) == (uint32_t)cc ? 1u << (yt & 31u) : 0u;
+                    bool any_here = (targets_in >> cc) & 1u;
+                    uint32_t here = (yt >> 5) == (uint32_t)cc ? 1u << (yt & 31u) : 0u;
+                    if constexpr (EPI == kTopStats) {
+                        // those of the listed items (past the other warps' chunks)
+                        const int first = sm.item0 + n0 + cc * 32;
+                        auto advance = [&] { listed = --list_left > 0 ? __ldg(++list) : INT_MAX; };
+                        while (listed < first) advance();
+                        while (listed - first < 32) {
+                            here |= 1u << (listed - first);
+                            advance();
+                        }
+                        any_here = __any_sync(0xffffffffu, here != 0);
+                    }
                     const uint64_t ff = f2_pack(f, f);
-                    if constexpr (EPI == kStats) {
+                    if constexpr (kAnyStats) {
                         if (any_here) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
@@ -783,7 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     }
                 }
             }
-            if constexpr (EPI == kStats)
+            if constexpr (kAnyStats)
                 sh.rowstat[b][group][row_in_tile] = make_float2(mx, sum);
             tc::fence_before_sync();
             __syncwarp();
@@ -794,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                     mbar_arrive(&sh.tempty[b]);
             }
         }
-        if constexpr (EPI == kStats) {
+        if constexpr (kAnyStats) {
             __syncwarp();
             asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
             if (it > 0 && group == 0)
@@ -1290,9 +1312,10 @@ namespace {
 
 template <int kCta>
 const void* kernel_of(int epilogue) {
-    return epilogue == kStats  ? (const void*)head_gemm_kernel<kStats, kCta>
-           : epilogue == kGrad ? (const void*)head_gemm_kernel<kGrad, kCta>
-                               : (const void*)head_gemm_kernel<kOut, kCta>;
+    return epilogue == kStats      ? (const void*)head_gemm_kernel<kStats, kCta>
+           : epilogue == kTopStats ? (const void*)head_gemm_kernel<kTopStats, kCta>
+           : epilogue == kGrad     ? (const void*)head_gemm_kernel<kGrad, kCta>
+                                   : (const void*)head_gemm_kernel<kOut, kCta>;
 }
 
 cudaLaunchConfig_t config(int cta, int grid, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {

@@ -6,6 +6,7 @@
 // contiguous), each in up to three parts that add up to it: the product then
 // runs over a list of part pairs.  What becomes of D is the kernel's choice:
 //   kStats   softmax statistics of D's rows, tile by tile (forward);
+//   kTopStats  the same without the items of a list that each row has;
 //   kGrad    the softmax gradient of each entry, kept in 16-bit parts (backward);
 //   kOut     D itself, split over k where that fills the GPU.
 #pragma once
@@ -24,7 +25,7 @@ constexpr int kTileK = 64;      // 128 bytes: one swizzle row
 constexpr int kMaxParts = 3;
 constexpr int kMaxPairs = 6;
 
-enum Epilogue { kStats = 0, kGrad = 1, kOut = 2 };
+enum Epilogue { kStats = 0, kGrad = 1, kOut = 2, kTopStats = 3 };
 
 // An operand in memory: `parts` matrices [rows x cols] of 16-bit elements,
 // leading dimension ld, part_stride elements apart.  Base 16-byte aligned, ld and
@@ -79,6 +80,11 @@ struct Softmax {
     float2* part;                // [tile of columns][rows]
     int part0;                   // the piece's first tile
     const int64_t* targets;      // a row's own target is left out of its statistics
+    // kTopStats: so are the items of its list, ascending, `top` of them ([rows][top], those
+    // that are none INT_MAX at the end); a tile's begin at list_first [tile of columns][rows]
+    const int* list;
+    const uint16_t* list_first;
+    int top;
     // kGrad
     const GradRow* row;
     uint16_t* grad;              // [parts][rows][ldg]

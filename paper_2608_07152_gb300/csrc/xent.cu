@@ -20,6 +20,7 @@
 #include <cuda_fp16.h>
 
 #include "../../include/head.h"
+#include "distill.h"
 #include "head_gemm.h"
 #include "kernels.h"
 #include "pvs_common.cuh"
@@ -239,6 +240,10 @@ struct Plan {
     GradRow* row = nullptr;
     unsigned int* words = nullptr;   // [0] up, [1] its inverse, [2] bad masked
     float *xslots = nullptr, *wslots = nullptr;
+    // distillation: the rows' lists, and which rows have one
+    int* list = nullptr;
+    uint16_t *list_slot = nullptr, *list_first = nullptr;
+    int64_t* flags = nullptr;
     size_t bytes = 0;
 };
 
@@ -309,7 +314,19 @@ bool few_rows(const pvs_xent_args& a) {
     return a.dtype == PVS_F32 && a.dim <= kFewDim && a.rows <= kFewRows;
 }
 
-Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace) {
+// The lists of a distillation's rows (top 0: there are none).
+void plan_lists(Plan& p, const pvs_xent_args& a, bool backward, int top, Carver& c) {
+    if (top == 0) return;
+    if (backward) {
+        p.flags = c.take<int64_t>(a.rows);
+    } else {
+        p.list = c.take<int>(a.rows * top);
+        p.list_slot = c.take<uint16_t>(a.rows * top);
+        if (!p.few) p.list_first = c.take<uint16_t>(p.pieces * p.piece_tiles * a.rows);
+    }
+}
+
+Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace, int top = 0) {
     Plan p;
     const int64_t T = a.rows, V = a.items;
     p.parts = parts_of(a.dtype);
@@ -330,6 +347,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
             p.few_g = c.take<float>(p.piece * few_rows_padded(T));
             p.xslots = c.take<float>(p.few * T * p.lds);
         }
+        plan_lists(p, a, backward, top, c);
         p.bytes = c.used;
         return p;
     }
@@ -391,6 +409,7 @@ Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* wor
             p.xslots = c.take<float>((int64_t)p.xsplits * T * p.lds);
         if (p.wsplits > 1) p.wslots = c.take<float>((int64_t)p.wsplits * first * p.lds);
     }
+    plan_lists(p, a, backward, top, c);
     p.bytes = c.used;
     return p;
 }
@@ -405,17 +424,17 @@ int64_t block_rows(const pvs_xent_args& a) {
 pvs_xent_args rows_of(const pvs_xent_args& a, int64_t t0, int64_t n) {
     pvs_xent_args b = a;
     b.x = static_cast<const uint8_t*>(a.x) + t0 * a.ldx * element_bytes(a.dtype);
-    b.targets = a.targets + t0;
+    if (a.targets) b.targets = a.targets + t0;
     b.rows = n;
     return b;
 }
 
 // What the forward pass wants: that of a whole block, or of the last.
-size_t forward_bytes(const pvs_xent_args& a, const Device& dev) {
+size_t forward_bytes(const pvs_xent_args& a, const Device& dev, int top = 0) {
     const int64_t block = block_rows(a), last = a.rows - (a.rows - 1) / block * block;
-    if (block == a.rows) return plan_of(a, false, dev, nullptr).bytes;
-    return std::max(plan_of(rows_of(a, 0, block), false, dev, nullptr).bytes,
-                    plan_of(rows_of(a, a.rows - last, last), false, dev, nullptr).bytes);
+    if (block == a.rows) return plan_of(a, false, dev, nullptr, top).bytes;
+    return std::max(plan_of(rows_of(a, 0, block), false, dev, nullptr, top).bytes,
+                    plan_of(rows_of(a, a.rows - last, last), false, dev, nullptr, top).bytes);
 }
 
 // Logits of the piece [v0, v0 + n).
@@ -504,10 +523,18 @@ FewArgs few_args(const pvs_xent_args& a) {
     return f;
 }
 
+// `top`: the rows' lists in place of targets, and what is kept of them in `hits`.
 cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, float* loss,
-                    float* stats, cudaStream_t st) {
+                    float* stats, cudaStream_t st, const TopRows* top = nullptr, float* hits = nullptr) {
     cudaError_t e = cudaSuccess;
     const int64_t T = a.rows, V = a.items;
+    const int64_t last = V - (p.pieces - 1) * p.piece;
+    const int64_t tiles = p.few ? p.few : (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl;
+    if (top) {
+        TopLists l{*top, p.list, p.list_slot, p.list_first, p.few ? 0 : tiles, p.piece_tiles, p.piece, p.bnl};
+        e = launch_top_lists(l, st);
+        if (e != cudaSuccess) return e;
+    }
     if (p.few) {
         FewArgs f = few_args(a);
         f.part = p.part;
@@ -519,6 +546,11 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     g.sm = softmax_of(a);
     g.sm.part = p.part;
     g.sm.targets = a.targets;
+    if (top) {
+        g.sm.list = p.list;
+        g.sm.list_first = p.list_first;
+        g.sm.top = top->top;
+    }
     for (int64_t v0 = 0; !p.few && v0 < V && e == cudaSuccess; v0 += p.piece) {
         const int64_t n = std::min(p.piece, V - v0);
         PrepareArgs c{};
@@ -527,22 +559,51 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
         e = launch_prepare(c, st);
         if (e != cudaSuccess) break;
         g.sm.part0 = (int)(v0 / p.piece * p.piece_tiles);
-        e = logits(kStats, g, p, a, v0, n, dev, st);
+        e = logits(top ? kTopStats : kStats, g, p, a, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
-    const int64_t last = V - (p.pieces - 1) * p.piece;
-    const int64_t tiles = p.few ? p.few : (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl;
-    const JoinArgs j{p.part, tiles, a, a.scale * kLog2e,
-                     a.dtype != PVS_F32 && !p.copy_x && !p.copy_w && a.dim % 8 == 0, loss,
-                     reinterpret_cast<float4*>(stats)};
+    const bool wide = a.dtype != PVS_F32 && !p.copy_x && !p.copy_w && a.dim % 8 == 0;
+    if (top) {
+        const TopJoin j{*top, p.list, p.list_slot, p.part, tiles, !p.few, wide, a.scale * kLog2e, loss,
+                        reinterpret_cast<float4*>(stats), hits};
+        return launch_top_join(j, dev, st);
+    }
+    const JoinArgs j{p.part, tiles, a, a.scale * kLog2e, wide, loss, reinterpret_cast<float4*>(stats)};
     count_launches(1);
     if (T >= 4 * dev.sms) return launch_early(xent_join_kernel<8>, (T + 7) / 8, 256, 0, st, j);
     return launch_early(xent_join_kernel<1>, T, 256, 0, st, j);
 }
 
+// The listed entries of G of the items [v0, v0 + n).
+struct TopGrad {
+    const int64_t* ids;
+    const float* hits;
+    int top;
+};
+TopScatter scatter_of(const TopGrad& t, const Plan& p, const pvs_xent_args& a, const float* grad_loss,
+                      int64_t v0, int64_t n) {
+    TopScatter s{};
+    s.ids = t.ids;
+    s.hits = t.hits;
+    s.grad = grad_loss;
+    s.up = p.f16 ? reinterpret_cast<const float*>(p.words) : nullptr;
+    s.rows = a.rows;
+    s.v0 = v0;
+    s.n = n;
+    s.top = t.top;
+    s.g = p.g;
+    s.ldg = p.ldg;
+    s.g_part = a.rows * p.ldg;
+    s.parts = p.gparts;
+    s.f16 = p.f16;
+    s.few = p.few_g;
+    s.few_rows = few_rows_padded(a.rows);
+    return s;
+}
+
 cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, const float* stats,
                      const float* grad_loss, void* dx, int64_t lddx, void* dw, int64_t lddw,
-                     cudaStream_t st) {
+                     cudaStream_t st, const TopGrad* top = nullptr) {
     const int64_t T = a.rows, V = a.items;
     float* up = reinterpret_cast<float*>(p.words);
     const float* undo = up + 1;
@@ -572,7 +633,10 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             f.accumulate = v0 > 0;
             if (dw) f.dw = static_cast<float*>(dw) + v0 * lddw;
             f.lddw = lddw;
-            e = launch_few_grads(f, p.few, st);
+            e = launch_few_softmax(f, p.few, st);
+            if (e == cudaSuccess && top)
+                e = launch_top_scatter(scatter_of(*top, p, a, grad_loss, v0, f.items), st);
+            if (e == cudaSuccess) e = launch_few_columns(f, p.few, st);
         }
         if (e == cudaSuccess && dx)
             e = launch_sum_slots(p.xslots, p.few, T * p.lds, p.lds, T, a.dim, nullptr, a.scale, dx,
@@ -607,6 +671,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         const bool alt = !p.copy_w && a.bias;
         if (alt) g.sm.bad_masked = bad_masked;
         e = logits(kGrad, g, p, a, v0, n, dev, st);
+        if (e == cudaSuccess && top) e = launch_top_scatter(scatter_of(*top, p, a, grad_loss, v0, n), st);
         // a masked item that holds NaN or infinities: dx takes w from a copy with zeros there
         if (e == cudaSuccess && alt && dx) {
             SplitArgs s = items_copy(a, p, v0, n).s;
@@ -753,4 +818,85 @@ extern "C" pvs_status pvs_xent_backward(const pvs_xent_args* a, const float* sta
     if (s != PVS_OK) return s;
     if (!dx && !dw) return PVS_OK;
     return ended(backward(*a, p, dev, stats, grad_loss, dx, lddx, dw, lddw, st));
+}
+
+// ---- distillation --------------------------------------------------------------------
+// The student as the cross entropy takes it, without targets of its own.
+static bool valid_distill(const pvs_distill_args* a, pvs_xent_args* s) {
+    if (!a || a->top < 1 || a->top > kMaxTop || a->teacher_dtype < PVS_BF16 || a->teacher_dtype > PVS_F32 ||
+        !(a->teacher_scale >= 0x1p-126f) || !std::isfinite(a->teacher_scale) || a->reserved != 0)
+        return false;
+    *s = a->student;
+    s->targets = a->ids;                     // (for the checks of the rows' pointers)
+    if (!valid(s) || (s->rows > 0 && !a->ids)) return false;
+    s->targets = nullptr;
+    return true;
+}
+
+extern "C" pvs_status pvs_distill_workspace(const pvs_distill_args* a, int32_t backward, size_t* bytes) {
+    pvs_xent_args s;
+    if (!bytes || !valid_distill(a, &s)) return PVS_ERR_INVALID;
+    *bytes = 0;
+    if (s.rows == 0) return PVS_OK;
+    Device dev;
+    if (device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return PVS_ERR_CUDA;
+    }
+    *bytes = backward ? plan_of(s, true, dev, nullptr, a->top).bytes : forward_bytes(s, dev, a->top);
+    return PVS_OK;
+}
+
+extern "C" pvs_status pvs_distill_forward(const pvs_distill_args* a, float* loss, float* stats, float* hits,
+                                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    pvs_xent_args s;
+    if (!valid_distill(a, &s)) return PVS_ERR_INVALID;
+    if (s.rows == 0) return PVS_OK;
+    const int es = element_bytes(a->teacher_dtype);
+    if (!a->logits || !on_elements(a->logits, es) || !loss || !stats || !hits || !on_elements(loss, 4) ||
+        !on_elements(stats, 16) || !on_elements(hits, 4))
+        return PVS_ERR_INVALID;
+    Device dev;
+    if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
+    const pvs_status before = begin(workspace, workspace_bytes, forward_bytes(s, dev, a->top), dev);
+    if (before != PVS_OK) return before;
+    cudaError_t e = cudaSuccess;
+    const int64_t block = block_rows(s);
+    for (int64_t t0 = 0; t0 < s.rows && e == cudaSuccess; t0 += block) {
+        TopRows r{rows_of(s, t0, std::min(block, s.rows - t0)), a->ids + t0 * a->top,
+                  static_cast<const uint8_t*>(a->logits) + t0 * a->top * es, a->top, a->teacher_dtype,
+                  a->teacher_scale};
+        e = forward(r.a, plan_of(r.a, false, dev, workspace, a->top), dev, loss + t0, stats + 4 * t0,
+                    static_cast<cudaStream_t>(cuda_stream), &r, hits + t0 * a->top);
+    }
+    return ended(e);
+}
+
+extern "C" pvs_status pvs_distill_backward(const pvs_distill_args* a, const float* stats, const float* hits,
+                                           const float* grad_loss, void* dx, int64_t lddx, void* dw,
+                                           int64_t lddw, void* workspace, size_t workspace_bytes,
+                                           void* cuda_stream) {
+    pvs_xent_args s;
+    if (!valid_distill(a, &s) || (dx && lddx < s.dim) || (dw && lddw < s.dim) ||
+        !on_elements(dx, element_bytes(s.dtype)) || !on_elements(dw, element_bytes(s.dtype)))
+        return PVS_ERR_INVALID;
+    if (s.rows == 0)
+        return pvs_xent_backward(&s, nullptr, nullptr, dx, lddx, dw, lddw, nullptr, 0, cuda_stream);
+    if (!stats || !hits || !grad_loss || !on_elements(stats, 16) || !on_elements(hits, 4) ||
+        !on_elements(grad_loss, 4))
+        return PVS_ERR_INVALID;
+    Device dev;
+    if (device(&dev) != cudaSuccess) return ended(cudaErrorUnknown);
+    const Plan p = plan_of(s, true, dev, workspace, a->top);
+    const pvs_status before = begin(workspace, workspace_bytes, p.bytes, dev);
+    if (before != PVS_OK) return before;
+    if (!dx && !dw) return PVS_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    // rows without a list take the part of ignored ones
+    cudaError_t e = launch_top_flags(reinterpret_cast<const float4*>(stats), s.rows, p.flags, st);
+    s.targets = p.flags;
+    s.ignore_index = -1;
+    const TopGrad top{a->ids, hits, a->top};
+    if (e == cudaSuccess) e = backward(s, p, dev, stats, grad_loss, dx, lddx, dw, lddw, st, &top);
+    return ended(e);
 }

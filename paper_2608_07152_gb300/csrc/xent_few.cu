@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kStatThreads) few_stats_kernel(const FewArgs a
     fill_rows(a, xs, R, false);
     __syncthreads();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane % R;
-    const int64_t y = t < a.rows ? a.targets[t] : -1;
+    const int64_t y = t < a.rows && a.targets ? a.targets[t] : -1;
     float m = -INFINITY, s = 0.0f;
     for (int64_t item = ((int64_t)blockIdx.x * kWarps + warp) * I; item < a.items;
          item += (int64_t)gridDim.x * kWarps * I) {
@@ -360,14 +360,15 @@ cudaError_t launch_few_stats(const FewArgs& a, int blocks, cudaStream_t st) {
                                     16, blocks, kStatThreads, st);
 }
 
-cudaError_t launch_few_grads(const FewArgs& a, int blocks, cudaStream_t st) {
+cudaError_t launch_few_softmax(const FewArgs& a, int blocks, cudaStream_t st) {
     const bool v = by_fours(a);
-    const cudaError_t e =
-        a.rows <= 8 ? few_launch(v ? few_softmax_kernel<8, 4, true> : few_softmax_kernel<8, 4, false>, a, 8,
-                                 blocks, kStatThreads, st)
-                    : few_launch(v ? few_softmax_kernel<16, 4, true> : few_softmax_kernel<16, 4, false>, a,
-                                 16, blocks, kStatThreads, st);
-    if (e != cudaSuccess) return e;
+    return a.rows <= 8 ? few_launch(v ? few_softmax_kernel<8, 4, true> : few_softmax_kernel<8, 4, false>, a, 8,
+                                    blocks, kStatThreads, st)
+                       : few_launch(v ? few_softmax_kernel<16, 4, true> : few_softmax_kernel<16, 4, false>, a,
+                                    16, blocks, kStatThreads, st);
+}
+
+cudaError_t launch_few_columns(const FewArgs& a, int blocks, cudaStream_t st) {
     const int width = (a.dim + 63) / 64 * 32;
     const int threads = kMostThreads / width * width;
     return a.rows <= 8 ? few_launch(few_columns_kernel<8, 8>, a, 8, blocks, threads, st, width)

@@ -18,7 +18,7 @@ struct FewArgs {
     int dim;
     float k2;                     // scale log2(e)
     const float* bias;            // of the same items, or null
-    const int64_t* targets;
+    const int64_t* targets;       // forward: left out of their rows' statistics (null: none)
     int64_t ignore_index;
     // the forward pass: a block's (m, s) of row t at part[block * part_rows + t]
     float2* part;
@@ -39,7 +39,9 @@ int few_blocks(int64_t items, const Device& dev);
 // The rows that a launch works on.
 int few_rows_padded(int64_t rows);
 cudaError_t launch_few_stats(const FewArgs& a, int blocks, cudaStream_t st);
-cudaError_t launch_few_grads(const FewArgs& a, int blocks, cudaStream_t st);
+// The backward pass in two launches: G, then the gradients from it.
+cudaError_t launch_few_softmax(const FewArgs& a, int blocks, cudaStream_t st);
+cudaError_t launch_few_columns(const FewArgs& a, int blocks, cudaStream_t st);
 
 }  // namespace head
 }  // namespace pvs

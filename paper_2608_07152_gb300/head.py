@@ -32,12 +32,20 @@ class pvs_xent_args(ctypes.Structure):
                 ("dim", _i32), ("dtype", _i32), ("scale", ctypes.c_float), ("reserved", _i32)]
 
 
+class pvs_distill_args(ctypes.Structure):
+    _fields_ = [("student", pvs_xent_args), ("ids", _P), ("logits", _P), ("top", _i32),
+                ("teacher_dtype", _i32), ("teacher_scale", ctypes.c_float), ("reserved", _i32)]
+
+
 _SIGNATURES = {
     "pvs_head_status": (_i32, []),
     "pvs_head_set_wait_limit": (_i32, [_i64]),
     "pvs_xent_workspace": (_i32, [_P, _i32, _P]),
     "pvs_xent_forward": (_i32, [_P, _P, _P, _P, ctypes.c_size_t, _P]),
     "pvs_xent_backward": (_i32, [_P, _P, _P, _P, _i64, _P, _i64, _P, ctypes.c_size_t, _P]),
+    "pvs_distill_workspace": (_i32, [_P, _i32, _P]),
+    "pvs_distill_forward": (_i32, [_P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "pvs_distill_backward": (_i32, [_P, _P, _P, _P, _P, _i64, _P, _i64, _P, ctypes.c_size_t, _P]),
     "pvs_ckpt_store": (_i32, [_P, _i64, _i64, _i32, _i32, _i32, _P, _i64, _P, _P, _i64, _P]),
     "pvs_ckpt_load": (_i32, [_P, _i64, _P, _i64, _i32, _P, _i64, _i32, _P]),
     "pvs_ckpt_act_backward": (_i32, [_P, _i64, _P, _i64, _P, _i64, _i32, _i32, _i32, _P, _i64,
@@ -225,6 +233,100 @@ def pvs_xent_backward(x, w, targets, stats, grad_loss, bias=None, scale: float =
     _check(_lib.pvs_xent_backward(ctypes.byref(a), _ptr(stats), _ptr(grad_loss), _ptr(dx),
                                   a.dim, _ptr(dw), a.dim, _ptr(ws), n.value, _stream(device)),
            "pvs_xent_backward")
+    return dx, dw
+
+
+_MAX_TOP = 1024
+
+
+def _list(x, name: str, rows: int):
+    if x.dim() != 2 or x.shape[0] != rows or not 1 <= x.shape[1] <= _MAX_TOP:
+        raise ValueError(f"{name} must be [{rows}, K], K in [1, {_MAX_TOP}]")
+    return x.contiguous()
+
+
+def _distill_args(x, w, ids, logits, bias, scale, teacher_scale, ignore_index):
+    device = _on_gpu(x, w, ids, logits, bias)
+    x, ldx = _matrix(x, "x")
+    w, ldw = _matrix(w, "w", x.dtype)
+    if x.shape[1] != w.shape[1]:
+        raise ValueError(f"x has {x.shape[1]} columns, w {w.shape[1]}")
+    if w.shape[0] < 1:
+        raise ValueError("w must have a row at least")
+    for name, v in (("scale", scale), ("teacher_scale", teacher_scale)):
+        if not (0.0 < v < float("inf")):
+            raise ValueError(f"{name} must be positive and finite")
+    ids = _list(ids, "ids", x.shape[0])
+    if ids.dtype != torch.int64:
+        raise TypeError("ids must be torch.int64")
+    teacher = PVS_F32
+    if logits is not None:
+        teacher = _dtype_code(logits.dtype)
+        logits = _list(logits, "logits", x.shape[0])
+        if logits.shape != ids.shape:
+            raise ValueError("logits and ids must have one shape")
+    if bias is not None:
+        bias = _vector(bias, "bias", w.shape[0], torch.float32)
+    s = pvs_xent_args(x.data_ptr(), w.data_ptr(), None, _ptr(bias), x.shape[0], w.shape[0], ldx, ldw,
+                      int(ignore_index), x.shape[1], _dtype_code(x.dtype), float(scale), 0)
+    a = pvs_distill_args(s, ids.data_ptr(), _ptr(logits), ids.shape[1], teacher, float(teacher_scale), 0)
+    return a, device, (x, w, ids, logits, bias)
+
+
+def pvs_distill_forward(x, w, ids, logits, bias=None, scale: float = 1.0,
+                        teacher_scale: float = 1.0, ignore_index: int = -100):
+    """Distillation of a teacher's logits [T, K] of the items ids, int64 [T, K], into the softmax
+    of the rows of x [T, d] over all items w [V, d] (logits ``scale * x @ w.T + bias``, bias
+    float32 [V] or None): the divergence of that softmax from ``softmax(teacher_scale *
+    logits)`` over each row's list.  A slot of ``ignore_index``, or of an item whose bias is -inf,
+    is not in the list; a row without a list has no loss.  Returns (loss float32 [T], stats
+    float32 [T, 4], hits float32 [T, K]); the backward pass takes the last two.  x and w are
+    both bfloat16, float16 or float32, logits any of them."""
+    if logits is None:
+        raise TypeError("logits must be a tensor")
+    a, device, keep = _distill_args(x, w, ids, logits, bias, scale, teacher_scale, ignore_index)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_distill_forward(x, w, ids, logits, bias, scale, teacher_scale, ignore_index)
+    rows = a.student.rows
+    loss = torch.empty(rows, dtype=torch.float32, device=device)
+    stats = torch.empty(rows, 4, dtype=torch.float32, device=device)
+    hits = torch.empty(rows, a.top, dtype=torch.float32, device=device)
+    n = ctypes.c_size_t()
+    _check(_lib.pvs_distill_workspace(ctypes.byref(a), 0, ctypes.byref(n)), "pvs_distill_workspace")
+    ws = _workspace(n.value, device)
+    _check(_lib.pvs_distill_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(hits), _ptr(ws),
+                                    n.value, _stream(device)), "pvs_distill_forward")
+    return loss, stats, hits
+
+
+def pvs_distill_backward(x, w, ids, stats, hits, grad_loss, bias=None, scale: float = 1.0,
+                         ignore_index: int = -100, need_x: bool = True, need_w: bool = True):
+    """The gradients (dx, dw) of ``(grad_loss * loss).sum()`` of ``pvs_distill_forward``,
+    grad_loss float32 [T], from its stats and hits; None for one that is not needed."""
+    a, device, keep = _distill_args(x, w, ids, None, bias, scale, 1.0, ignore_index)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_distill_backward(x, w, ids, stats, hits, grad_loss, bias, scale, ignore_index,
+                                        need_x, need_w)
+    _on_gpu(x, stats, hits, grad_loss)
+    s = a.student
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (s.rows, 4):
+        raise ValueError("stats must be the forward pass's float32 [T, 4]")
+    if hits.dtype != torch.float32 or tuple(hits.shape) != (s.rows, a.top):
+        raise ValueError("hits must be the forward pass's float32 [T, K]")
+    stats, hits = stats.contiguous(), hits.contiguous()
+    if stats.data_ptr() % 16:
+        stats = stats.clone()
+    grad_loss = _vector(grad_loss, "grad_loss", s.rows, torch.float32)
+    dx = torch.empty(s.rows, s.dim, dtype=x.dtype, device=device) if need_x else None
+    dw = torch.empty(s.items, s.dim, dtype=x.dtype, device=device) if need_w else None
+    n = ctypes.c_size_t()
+    _check(_lib.pvs_distill_workspace(ctypes.byref(a), 1, ctypes.byref(n)), "pvs_distill_workspace")
+    ws = _workspace(n.value, device)
+    _check(_lib.pvs_distill_backward(ctypes.byref(a), _ptr(stats), _ptr(hits), _ptr(grad_loss),
+                                     _ptr(dx), s.dim, _ptr(dw), s.dim, _ptr(ws), n.value,
+                                     _stream(device)), "pvs_distill_backward")
     return dx, dw
 
 

@@ -63,3 +63,59 @@ def test_gradient_workspace(rows):
         pieces = (rows + 31) // 32
         tiles = (rows + 2047) // 2048
         assert 8 * rows <= n.value <= 16 * rows + 8 * pieces * padded + 4096 * (tiles + 1) + 7 * 256
+
+
+def distill(student=None, **kw):
+    s = dict(x=P, w=P, targets=None, bias=None, rows=4, items=9, ldx=16, ldw=16, ignore_index=-100, dim=16,
+             dtype=pvs.PVS_BF16, scale=1.0, reserved=0)
+    s.update(student or {})
+    a = dict(ids=P, logits=P, top=5, teacher_dtype=pvs.PVS_F32, teacher_scale=1.0, reserved=0)
+    a.update(kw)
+    return pvs.pvs_distill_args(pvs.pvs_xent_args(*s.values()), *a.values())
+
+
+@pytest.mark.parametrize("bad", [
+    dict(top=0), dict(top=1025), dict(teacher_dtype=3), dict(teacher_dtype=-1), dict(teacher_scale=0.0),
+    dict(teacher_scale=float("nan")), dict(teacher_scale=float("inf")), dict(reserved=1), dict(ids=None),
+    dict(ids=P + 4), dict(student=dict(rows=-1)), dict(student=dict(items=0)), dict(student=dict(scale=-1.0)),
+    dict(student=dict(ldx=15)), dict(student=dict(x=None)), dict(student=dict(w=P + 1)), dict(student=dict(reserved=1)),
+    dict(student=dict(bias=P + 2))])
+def test_distill_refusals(bad):
+    a = distill(**bad)
+    n = ctypes.c_size_t()
+    assert L.pvs_distill_workspace(ctypes.byref(a), 0, ctypes.byref(n)) == BAD
+    assert L.pvs_distill_forward(ctypes.byref(a), P, P, P, P, 0, None) == BAD
+    assert L.pvs_distill_backward(ctypes.byref(a), P, P, P, P, 16, P, 16, P, 0, None) == BAD
+
+
+def test_distill_pointers():
+    n = ctypes.c_size_t()
+    a = distill()
+    assert L.pvs_distill_workspace(None, 0, ctypes.byref(n)) == BAD
+    assert L.pvs_distill_workspace(ctypes.byref(a), 0, None) == BAD
+    for bad in ((None, P, P), (P, None, P), (P, P, None), (P + 2, P, P), (P, P + 8, P), (P, P, P + 2)):
+        assert L.pvs_distill_forward(ctypes.byref(a), *bad, P, 0, None) == BAD
+    for a2 in (distill(logits=None), distill(logits=P + 2)):
+        assert L.pvs_distill_forward(ctypes.byref(a2), P, P, P, P, 0, None) == BAD
+    for bad in ((None, P, P, P, 16, P, 16), (P, None, P, P, 16, P, 16), (P, P, None, P, 16, P, 16),
+                (P + 8, P, P, P, 16, P, 16), (P, P + 2, P, P, 16, P, 16), (P, P, P, P + 1, 16, P, 16),
+                (P, P, P, P, 15, P, 16), (P, P, P, P, 16, P, 15), (P, P, P, P, 16, P + 1, 16)):
+        assert L.pvs_distill_backward(ctypes.byref(a), *bad, P, 0, None) == BAD
+    none = distill(student=dict(rows=0, x=None), ids=None, logits=None)
+    assert L.pvs_distill_forward(ctypes.byref(none), None, None, None, None, 0, None) == pvs.PVS_OK
+    assert L.pvs_distill_backward(ctypes.byref(none), None, None, None, P, 16, None, 16, None, 0, None) == pvs.PVS_OK
+
+
+def test_distill_layout(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = [f for f, _ in pvs.pvs_distill_args._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text("#include <stdio.h>\n#include <stddef.h>\n#include \"head.h\"\nint main(void) {\n"
+                   + 'printf("%zu\\n", sizeof(pvs_distill_args));\n'
+                   + "".join(f'printf("%zu\\n", offsetof(pvs_distill_args, {n}));\n' for n in names) + "return 0; }\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(pvs.pvs_distill_args)] + [getattr(pvs.pvs_distill_args, n).offset for n in names]
