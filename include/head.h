@@ -244,6 +244,45 @@ pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch, const uint8_
                          int32_t dtype, void* y, int64_t ldy, void* cuda_stream);
 
 /* ---------------------------------------------------------------------------
+ * Microscaled 4-bit rows, for products of any number of rows on the tensor cores.  An element
+ * is kept as one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign (e2m1), in units of a scale that
+ * `group` neighbours of a row share; columns are padded with zeros to kp, a multiple of 128:
+ *   group 32   scale 2^(floor(log2 max|x|) - 2), clipped to 2^-127 from below (zero groups too),
+ *              as its exponent with bias 127; 255 (NaN) for a group that holds a NaN or an
+ *              infinity, with codes 0.
+ *   group 16   each row has a power of two r = 2^(floor(log2 max|x_row|) - 10), 2^-126 at least (1
+ *              for a zero row; NaN, with scales and codes 0, for a row that holds a NaN or an
+ *              infinity), and a group the scale s = RN_e4m3(RN(max|x| RN(1 / 6)) / r), in units of r.
+ * An element is the nearest of those values to x / scale, of two the one with an even code,
+ * 6 beyond 6; 0 where the scale is 0.
+ * codes: uint8 [rows x kp / 2] without gaps, 16-byte aligned; the lower half of a byte comes first,
+ * bit 3 of a half is the sign.
+ * scales: uint8, 16-byte aligned, as the tensor cores take them: blocks of 512 bytes
+ * [ceil(rows / 128)][kp / (4 group)], each the four scales of 4 group columns of 128 rows, those
+ * of row 32 i + j from byte 16 j + 4 i; zeros for rows that are not there.
+ * row_scales: float32 [rows] for group 16; not used for 32.
+ * 0 <= rows <= 2^31 - 2^16, 1 <= cols <= 32767.
+ * ------------------------------------------------------------------------ */
+pvs_status pvs_mx_pack(const void* x, int64_t ldx, int64_t rows, int32_t cols, int32_t dtype,
+                       int32_t group, uint8_t* codes, uint8_t* scales, float* row_scales,
+                       void* cuda_stream);
+
+/* out [rows x cols] = what codes stand for, in out's type. */
+pvs_status pvs_mx_unpack(const uint8_t* codes, const uint8_t* scales, const float* row_scales,
+                         int64_t rows, int32_t cols, int32_t group, void* out, int64_t ldout,
+                         int32_t dtype, void* cuda_stream);
+
+/* y [batch x rows] in x's type = x [batch x cols], put into the weights' format as pvs_mx_pack
+ * does, times the transposed weights [rows x cols]: products of codes are exact, sums float32,
+ * y rounded once from them (group 16: from the sum times both row scales).  Scratch: x in that
+ * format, and float32 sums of a few units of y where k is split. */
+pvs_status pvs_mx_workspace(int64_t batch, int64_t rows, int32_t cols, int32_t group, size_t* bytes);
+pvs_status pvs_mx_matmul(const void* x, int64_t ldx, int64_t batch, const uint8_t* codes,
+                         const uint8_t* scales, const float* row_scales, int64_t rows, int32_t cols,
+                         int32_t group, int32_t dtype, void* y, int64_t ldy, void* workspace,
+                         size_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------
  * Rows of a table by their ids, for the tokens or items that a head is fed with:
  *     y_t = scale w[ids[t]]                          [rows x dim], in w's type
  * and the table's gradient

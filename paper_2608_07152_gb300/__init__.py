@@ -876,5 +876,5 @@ from .head import (  # noqa: E402,F401
     PVS_ACT_GELU, PVS_ACT_NONE, PVS_BF16, PVS_F16, PVS_F32, pvs_ckpt_act_backward,
     pvs_ckpt_grad_weight, pvs_ckpt_load, pvs_ckpt_store, pvs_distill_args,
     pvs_distill_backward, pvs_distill_forward, pvs_embed_backward, pvs_embed_forward,
-    pvs_head_set_wait_limit, pvs_head_status,
+    pvs_head_set_wait_limit, pvs_head_status, pvs_mx_matmul, pvs_mx_pack, pvs_mx_unpack,
     pvs_wq_matvec, pvs_wq_pack, pvs_wq_unpack, pvs_xent_args, pvs_xent_backward, pvs_xent_forward)

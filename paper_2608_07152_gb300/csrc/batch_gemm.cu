@@ -504,6 +504,18 @@ bool tensor_map_3d(CUtensorMap* m, CUtensorMapDataType type, int elem, const voi
            CUDA_SUCCESS;
 }
 
+bool tensor_map_blocks(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box) {
+    const EncodeTiledFn fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {128, cols, rows};
+    const cuuint64_t strides[2] = {512, cols * 512};
+    const cuuint32_t boxes[3] = {128, box, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, boxes, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 // bf16 matrix [rows][cols] (row stride cols), box = [64 cols x box_rows], 128B swizzle.

@@ -130,6 +130,71 @@ __device__ __forceinline__ void mma_f16_pair_ts(uint32_t d_tmem, uint32_t a_tmem
         : "memory");
 }
 
+// ---- block-scaled 4-bit MMA (K = 64) ---------------------------------------------
+// Instruction descriptor, kind::mxf4 and kind::mxf4nvf4: A = B = e2m1 (bits [7,10) = 1, [10,12) = 1),
+// both K-major, N >> 3 in bits [17,23), scale type in bit 23 (0: ue4m3, 1: ue8m0), M >> 7 in bits
+// [27,29); which byte of its 32-bit cells the scales of an MMA start at: B's in bits [4,6), A's
+// in bits [29,31); K = 64 (bit 31 = 0).
+__host__ __device__ constexpr uint32_t idesc_e2m1_f32(int M, int N, bool ue8m0, int byte) {
+    return ((uint32_t)byte << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) |
+           ((ue8m0 ? 1u : 0u) << 23) | ((uint32_t)(M >> 7) << 27) | ((uint32_t)byte << 29);
+}
+
+// D (+)= (A scales) (B scales)^T: scales of every 16 elements (ue4m3, four a row and MMA) or of
+// every 32 (ue8m0, two); a_scale and b_scale are TMEM addresses.  Row 32 i + j of an operand has
+// its scales in lane j of column i, the same in each quarter of the lanes.
+template <int kCta, bool kSixteen>
+__device__ __forceinline__ void mma_e2m1(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                         uint32_t a_scale, uint32_t b_scale, uint32_t accumulate) {
+    if constexpr (kCta == 1 && kSixteen)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X "
+            "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+            "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+    else if constexpr (kCta == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X "
+            "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+            "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+    else if constexpr (kSixteen)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X "
+            "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+            "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X "
+            "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+            "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+            : "memory");
+}
+
+// 32 rows of 16 bytes in shared memory, one after another, to four TMEM columns of 32 lanes,
+// repeated in each quarter of the lanes.  Of a CTA pair, issued by the even CTA: each CTA's TMEM
+// from its own shared memory at the same offset.
+__device__ __forceinline__ uint64_t smem_desc_rows16(uint32_t smem_addr) {
+    return (uint64_t)((smem_addr >> 4) & 0x3fffu) | (uint64_t)(128u >> 4) << 16 |
+           (uint64_t)(128u >> 4) << 32 | (uint64_t)1 << 46;
+}
+template <int kCta>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (kCta == 1)
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 // The mbarrier at the offset of `bar` in both CTAs of the pair gets one
 // arrival when every tcgen05 operation this thread issued has completed.
 __device__ __forceinline__ void commit_pair(uint64_t* bar) {

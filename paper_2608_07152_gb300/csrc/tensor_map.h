@@ -18,4 +18,8 @@ bool tensor_map_3d(CUtensorMap* m, CUtensorMapDataType type, int elem, const voi
                    uint64_t parts, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t part_stride,
                    uint32_t box_cols, uint32_t box_rows);
 
+// Blocks of 512 bytes [rows][cols] without gaps, boxes of `box` neighbours in a row, no swizzle,
+// blocks past the matrix read as zeros.
+bool tensor_map_blocks(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box);
+
 }  // namespace pvs

@@ -56,6 +56,11 @@ _SIGNATURES = {
     "pvs_wq_pack": (_i32, [_P, _i64, _i64, _i32, _i32, _i32, _P, _P, _P]),
     "pvs_wq_unpack": (_i32, [_P, _P, _i64, _i32, _i32, _P, _i64, _i32, _P]),
     "pvs_wq_matvec": (_i32, [_P, _i64, _i32, _P, _P, _i64, _i32, _i32, _i32, _P, _i64, _P]),
+    "pvs_mx_pack": (_i32, [_P, _i64, _i64, _i32, _i32, _i32, _P, _P, _P, _P]),
+    "pvs_mx_unpack": (_i32, [_P, _P, _P, _i64, _i32, _i32, _P, _i64, _i32, _P]),
+    "pvs_mx_workspace": (_i32, [_i64, _i64, _i32, _i32, _P]),
+    "pvs_mx_matmul": (_i32, [_P, _i64, _i64, _P, _P, _P, _i64, _i32, _i32, _i32, _P, _i64, _P,
+                             ctypes.c_size_t, _P]),
     "pvs_embed_forward": (_i32, [_P, _i64, _i64, _i32, _i32, _P, _i64, ctypes.c_float, _i64, _P,
                                  _i64, _P]),
     "pvs_embed_workspace": (_i32, [_i64, _i64, _i32, _P]),
@@ -550,3 +555,97 @@ def pvs_embed_backward(dy, ids, items: int, scale: float = 1.0, ignore_index: in
                                    int(ignore_index), _ptr(dw), dim, _ptr(ws), n.value,
                                    _stream(device)), "pvs_embed_backward")
     return dw
+
+
+def _mx_group(group: int) -> int:
+    if group not in (16, 32):
+        raise ValueError("group must be 16 or 32")
+    return int(group)
+
+
+def _mx_rows(codes, scales, row_scales, group: int):
+    """Packed rows that the kernels can read, and their padded columns."""
+    group = _mx_group(group)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise TypeError("codes and scales must be uint8")
+    if codes.dim() != 2 or codes.shape[1] % 64 != 0 or codes.shape[1] == 0:
+        raise ValueError("codes must be [N, padded K / 2], padded K a multiple of 128")
+    n, kp = codes.shape[0], codes.shape[1] * 2
+    if tuple(scales.shape) != ((n + 127) // 128, kp // (4 * group), 512):
+        raise ValueError("scales must be [ceil(N / 128), padded K / (4 group), 512]")
+    codes, scales = codes.contiguous(), scales.contiguous()
+    # a view can start anywhere; the kernels copy 16 bytes at once
+    if codes.data_ptr() % 16:
+        codes = codes.clone()
+    if scales.data_ptr() % 16:
+        scales = scales.clone()
+    if group == 16:
+        if row_scales is None:
+            raise ValueError("groups of 16 have row scales")
+        row_scales = _vector(row_scales, "row_scales", n, torch.float32)
+    elif row_scales is not None:
+        raise ValueError("groups of 32 have no row scales")
+    return codes, scales, row_scales, kp
+
+
+def pvs_mx_pack(x, group: int):
+    """Rows [N, K] in microscaled 4-bit floating point with a scale for every `group` (16 or 32)
+    of a row: (codes uint8 [N, Kp / 2], scales uint8 [ceil(N / 128), Kp / (4 group), 512],
+    row_scales float32 [N], None for groups of 32), Kp = K padded to a multiple of 128."""
+    device = _on_gpu(x)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_mx_pack(x, group)
+    group = _mx_group(group)
+    x, ldx = _matrix(x, "x")
+    dt = _dtype_code(x.dtype)
+    n, k = x.shape
+    kp = _wq_padded(k)
+    codes = torch.empty(n, kp // 2, dtype=torch.uint8, device=device)
+    scales = torch.empty((n + 127) // 128, kp // (4 * group), 512, dtype=torch.uint8, device=device)
+    rows = torch.empty(n, dtype=torch.float32, device=device) if group == 16 else None
+    _check(_lib.pvs_mx_pack(_ptr(x), ldx, n, k, dt, group, _ptr(codes), _ptr(scales), _ptr(rows),
+                            _stream(device)), "pvs_mx_pack")
+    return codes, scales, rows
+
+
+def pvs_mx_unpack(codes, scales, row_scales, group: int, cols: int, dtype):
+    """The rows [N, cols] that packed ones stand for, as a tensor of `dtype`."""
+    device = _on_gpu(codes, scales, row_scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_mx_unpack(codes, scales, row_scales, group, cols, dtype)
+    codes, scales, row_scales, kp = _mx_rows(codes, scales, row_scales, group)
+    dt = _dtype_code(dtype)
+    if cols < 1 or cols > _MAX_DIM or _wq_padded(cols) != kp:
+        raise ValueError(f"cols = {cols} does not pad to {kp}")
+    n = codes.shape[0]
+    out = torch.empty(n, cols, dtype=dtype, device=device)
+    _check(_lib.pvs_mx_unpack(_ptr(codes), _ptr(scales), _ptr(row_scales), n, cols, group, _ptr(out), cols,
+                              dt, _stream(device)), "pvs_mx_unpack")
+    return out
+
+
+def pvs_mx_matmul(x, codes, scales, row_scales, group: int):
+    """``x @ weights.T`` [B, N] in x's type, for any number of rows x [B, K] and weights packed by
+    ``pvs_mx_pack``; x is put into the same format first, so that both operands have 4 bits."""
+    device = _on_gpu(x, codes, scales, row_scales)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return pvs_mx_matmul(x, codes, scales, row_scales, group)
+    codes, scales, row_scales, kp = _mx_rows(codes, scales, row_scales, group)
+    x, ldx = _matrix(x, "x")
+    dt = _dtype_code(x.dtype)
+    b, k = x.shape
+    if _wq_padded(k) != kp:
+        raise ValueError(f"x has {k} columns, the packed weights {kp} after padding")
+    n = codes.shape[0]
+    if n > _MAX_ROWS:
+        raise ValueError(f"the weights have more than {_MAX_ROWS} rows")
+    y = torch.empty(b, n, dtype=x.dtype, device=device)
+    size = ctypes.c_size_t()
+    _check(_lib.pvs_mx_workspace(b, n, k, group, ctypes.byref(size)), "pvs_mx_workspace")
+    ws = _workspace(size.value, device)
+    _check(_lib.pvs_mx_matmul(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), _ptr(row_scales), n, k, group, dt,
+                              _ptr(y), n, _ptr(ws), size.value, _stream(device)), "pvs_mx_matmul")
+    return y

@@ -119,3 +119,58 @@ def test_distill_layout(tmp_path):
     subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
     got = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     assert got == [ctypes.sizeof(pvs.pvs_distill_args)] + [getattr(pvs.pvs_distill_args, n).offset for n in names]
+
+
+def pack(**kw):
+    a = dict(x=P, ldx=300, rows=4, cols=300, dtype=0, group=16, codes=P, scales=P, row_scales=P, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return L.pvs_mx_pack(*a.values())
+
+
+def unpack(**kw):
+    a = dict(codes=P, scales=P, row_scales=P, rows=4, cols=300, group=16, out=P, ldout=300, dtype=0, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return L.pvs_mx_unpack(*a.values())
+
+
+def product(**kw):
+    a = dict(x=P, ldx=300, batch=3, codes=P, scales=P, row_scales=P, rows=4, cols=300, group=16, dtype=0, y=P, ldy=4,
+             ws=P, bytes=1 << 30, stream=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return L.pvs_mx_matmul(*a.values())
+
+
+OPERAND = [dict(codes=None), dict(codes=P + 8), dict(scales=None), dict(scales=P + 8), dict(row_scales=None),
+           dict(row_scales=P + 2), dict(group=8), dict(group=64), dict(rows=-1), dict(rows=1 << 31), dict(cols=0),
+           dict(dtype=3), dict(dtype=-1)]
+
+
+@pytest.mark.parametrize("bad", OPERAND + [dict(x=None), dict(x=P + 1), dict(ldx=299), dict(cols=32768, ldx=40000)])
+def test_mx_pack_refusals(bad):
+    assert pack(**bad) == BAD
+
+
+@pytest.mark.parametrize("bad", OPERAND + [dict(out=None), dict(out=P + 1), dict(ldout=299), dict(cols=32768, ldout=40000)])
+def test_mx_unpack_refusals(bad):
+    assert unpack(**bad) == BAD
+
+
+@pytest.mark.parametrize("bad", OPERAND + [dict(x=None), dict(x=P + 1), dict(y=None), dict(y=P + 1), dict(ldx=299),
+                                           dict(ldy=3), dict(batch=-1), dict(batch=1 << 31),
+                                           dict(cols=32768, ldx=40000)])
+def test_mx_matmul_refusals(bad):
+    assert product(**bad) == BAD
+
+
+def test_mx_of_nothing():
+    assert pack(rows=0, x=None, codes=None, scales=None, row_scales=None) == pvs.PVS_OK
+    assert unpack(rows=0, out=None, codes=None, scales=None, row_scales=None) == pvs.PVS_OK
+    assert product(batch=0, x=None, y=None, codes=None, scales=None, row_scales=None, ws=None) == pvs.PVS_OK
+    assert product(rows=0, ldy=0, codes=None, scales=None, row_scales=None, ws=None) == pvs.PVS_OK
+    n = ctypes.c_size_t(3)
+    assert L.pvs_mx_workspace(0, 5, 128, 16, ctypes.byref(n)) == pvs.PVS_OK and n.value == 0
+    assert L.pvs_mx_workspace(5, 5, 128, 16, None) == BAD
+    assert L.pvs_mx_workspace(5, 5, 128, 8, ctypes.byref(n)) == BAD
