@@ -12,8 +12,8 @@
 //   warp 0     TMA producer: chunks of 256 of k, 128 bytes a row (128-byte swizzle), and their
 //              blocks of scales;
 //   warp 1     one thread copies a chunk's scales from shared memory to TMEM and issues its four
-//              MMAs.  Two sets of TMEM columns hold scales, and a set is written again when
-//              the MMAs of the chunk before last are complete;
+//              MMAs.  Four sets of TMEM columns hold scales, and a set is written again when
+//              the MMAs that read it are complete;
 //   warps 2-9  epilogue: each takes every other 32 columns of its quarter of the lanes into
 //              registers, hands the accumulator back, and stores.
 // Many rows of x go to CTA pairs (cta_group::2, 256 x 256 tiles): each CTA holds 128 rows of
@@ -40,8 +40,9 @@ constexpr int kMxEpiWarps = 8;
 constexpr int kMxThreads = (2 + kMxEpiWarps) * 32;
 constexpr int kMxPart = 128 * 128;       // bytes of 128 rows' codes of a chunk
 constexpr uint32_t kMxTmem = 512;
-constexpr uint32_t kScaleCol = 256;      // two sets of scales behind the accumulators
-constexpr uint32_t kScaleSet = 64;       // A's 16 columns, B's 32
+constexpr uint32_t kScaleCol = 256;      // sets of scales behind the accumulators
+constexpr uint32_t kScaleSet = 64;       // columns of a set: A's 16, B's 32
+constexpr uint32_t kScaleSets = 4;       // (fewer than a ring has stages)
 
 struct MxArgs {
     CUtensorMap a, b, sa, sb;
@@ -50,8 +51,6 @@ struct MxArgs {
     int mtiles, ntiles, splits, units, m_fast;
     int steps;                           // of 64 of k
     int kchunks, klength;                // chunks in all, and in a split
-    int blocks;                          // of scales in a chunk, for 128 rows
-    int bblocks;                         // 128-row blocks of B's scales in a tile
     int accs;                            // accumulators
     int stages;
     uint32_t b_bytes, stage_bytes;
@@ -74,9 +73,21 @@ struct MxShared {
     int abort;                           // of the pair: set in both its CTAs
     uint32_t fills;                      // stages that this CTA has filled
     uint32_t chunks, tiles;              // even CTA: chunks and tiles committed
+    alignas(16) float row_b[kMxEpiWarps][32];
 };
 
 constexpr size_t kMxSmem = 227 * 1024;
+
+// A place in the ring of stages, and the parity of its turn.
+struct Turn {
+    uint32_t stage = 0, parity = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++stage == (uint32_t)stages) {
+            stage = 0;
+            parity ^= 1u;
+        }
+    }
+};
 
 // A unit: a tile over a range of chunks.
 struct MxUnit {
@@ -95,7 +106,7 @@ struct MxUnit {
 template <int kCta>
 __device__ __forceinline__ int columns_of(const MxArgs& a, int nt) {
     const int left = min(a.bn, a.n - nt * a.bn);
-    return (left + 16 * kCta - 1) / (16 * kCta) * (16 * kCta);
+    return (left + 16 * kCta - 1) & ~(16 * kCta - 1);
 }
 
 __device__ __forceinline__ bool mx_aborted(MxShared& sh) {
@@ -113,6 +124,10 @@ __device__ __forceinline__ void mx_abort(MxShared& sh, int* status, int crank) {
 }
 __device__ __forceinline__ bool mx_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
     return mbar_test_wait(bar, parity) || (limit_ns != 0 && mbar_wait(bar, parity, limit_ns));
+}
+// The same by a whole warp, so that what follows is uniform.
+__device__ __forceinline__ bool mx_warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
+    return __all_sync(0xffffffffu, mx_wait(bar, parity, limit_ns));
 }
 // A wait at a role's end, with the 2 s limit, given up in a millisecond where another role has
 // given up (what it waits for may then never come).
@@ -149,19 +164,18 @@ __device__ __forceinline__ void mx_load(void* dst, const void* tmap, int x, int 
 
 // This CTA's copies of one fill of a stage: 128 rows of A, its share of B's rows, the scales of
 // both (of all of B's rows in each CTA of a pair).
-template <int kCta>
-__device__ __forceinline__ void mx_fill(const MxArgs& a, uint8_t* stage, uint64_t* full, int crank, int mt,
-                                        int nt, int kc) {
+template <int kCta, bool kSixteen>
+__device__ __forceinline__ void mx_fill(const MxArgs& a, uint8_t* stage, uint64_t* full, int crank, int am,
+                                        int bm, int bs, int kc) {
+    constexpr int kBlocks = kSixteen ? 4 : 2;
     if (crank == 0) mbar_arrive_expect_tx(full, (uint32_t)kCta * a.stage_bytes);
     const uint32_t bar = kCta == 2 ? cluster_map(full, 0) : smem_u32(full);
-    const int am = (mt * kCta + crank) * 128, b0 = nt * a.bn;
-    const uint32_t part = (uint32_t)a.blocks * 512;
     mx_load<kCta>(stage, &a.a, kc * 128, am, 0, bar);
-    mx_load<kCta>(stage + kMxPart, &a.b, kc * 128, b0 + crank * (columns_of<kCta>(a, nt) / 2), 0, bar);
+    mx_load<kCta>(stage + kMxPart, &a.b, kc * 128, bm, 0, bar);
     uint8_t* s = stage + kMxPart + a.b_bytes;
-    mx_load<kCta>(s, &a.sa, 0, kc * a.blocks, am / 128, bar);
-    for (int i = 0; i < a.bblocks; ++i)
-        mx_load<kCta>(s + (1 + i) * part, &a.sb, 0, kc * a.blocks, b0 / 128 + i, bar);
+    mx_load<kCta>(s, &a.sa, 0, kc * kBlocks, am / 128, bar);
+    mx_load<kCta>(s + kBlocks * 512, &a.sb, 0, kc * kBlocks, bs, bar);
+    if constexpr (kCta == 2) mx_load<kCta>(s + 2 * kBlocks * 512, &a.sb, 0, kc * kBlocks, bs + 1, bar);
 }
 
 // After a wait that ran out: one thread of each CTA waits for what is still on its way to its
@@ -169,14 +183,14 @@ __device__ __forceinline__ void mx_fill(const MxArgs& a, uint8_t* stage, uint64_
 // and this one has not are issued here (the stage is free, or the other would not have filled
 // it; what is read does not matter), so that every `full` barrier completes.  Then the MMAs and
 // their commits.  With the 2 s limit; after one that runs out nothing more is waited for.
-template <int kCta>
+template <int kCta, bool kSixteen>
 __device__ __noinline__ void mx_settle(const MxArgs& a, MxShared& sh, uint8_t* stages, int crank) {
     const uint32_t n = (uint32_t)a.stages;
     const uint32_t mine = sh.fills;
     const uint32_t fills = kCta == 2 ? max(mine, mx_word_of(&sh.fills, crank ^ 1)) : mine;
     for (uint32_t g = mine; g < fills; ++g) {
         const uint32_t s = g % n;
-        mx_fill<kCta>(a, stages + s * a.stage_bytes, &sh.full[s], crank, 0, 0, 0);
+        mx_fill<kCta, kSixteen>(a, stages + s * a.stage_bytes, &sh.full[s], crank, 0, 0, 0, 0);
     }
     const uint32_t chunks = kCta == 2 ? mx_word_of(&sh.chunks, 0) : sh.chunks;
     const uint32_t tiles = kCta == 2 ? mx_word_of(&sh.tiles, 0) : sh.tiles;
@@ -190,13 +204,25 @@ __device__ __noinline__ void mx_settle(const MxArgs& a, MxShared& sh, uint8_t* s
         if (in_time && b < tiles) in_time = mbar_wait(&sh.tfull[b], ((tiles - 1 - b) / accs) & 1u);
 }
 
-__device__ __forceinline__ void mx_put(void* p, int dtype, int64_t i, float v) {
-    if (dtype == PVS_F32)
-        static_cast<float*>(p)[i] = v;
-    else if (dtype == PVS_BF16)
-        static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+// A lane's column of up to 32 rows of y, ld apart (neighbouring lanes: neighbours).
+template <typename T>
+__device__ __forceinline__ T mx_round(uint32_t u) {
+    const float v = __uint_as_float(u);
+    if constexpr (sizeof(T) == 4)
+        return v;
     else
-        static_cast<__half*>(p)[i] = __float2half_rn(v);
+        return T(v);
+}
+template <typename T>
+__device__ __forceinline__ void mx_store(T* p, int64_t ld, const uint32_t (&r)[32], int count) {
+    if (count >= 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) p[j * ld] = mx_round<T>(r[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < count) p[j * ld] = mx_round<T>(r[j]);
+    }
 }
 
 template <int kCta, bool kSixteen>
@@ -207,7 +233,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     const uint32_t raw = smem_u32(mx_smem);
     uint8_t* stages = mx_smem + (((raw + 1023u) & ~1023u) - raw);
     MxShared& sh = *reinterpret_cast<MxShared*>(stages + (size_t)a.stages * a.stage_bytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int crank = kCta == 2 ? (int)cluster_ctarank() : 0;
     const int slot = blockIdx.x / kCta, nslots = gridDim.x / kCta;
 
@@ -234,102 +260,128 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     __syncthreads();
     if (kCta == 2) cluster_barrier();
     tc::fence_after_sync();
-    const uint32_t tmem = sh.tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);
     next_early();
     wait_before();
 
+    // The producer's and the issuer's loops are run by whole warps, one lane of which issues: their
+    // addresses and descriptors then stay in uniform registers, where the instructions want them
+    // (by lone lanes, which move each operand there, a chunk took 1,000 cycles where its MMAs take
+    // 512).
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            uint32_t g = 0;
-            for (int u = slot; u < a.units && !mx_aborted(sh); u += nslots) {
-                const MxUnit w(a, u);
-                for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
-                    const uint32_t s = g % a.stages;
-                    if (!mx_wait(&sh.empty[s], ((g / a.stages) & 1u) ^ 1u, a.wait_ns)) {
-                        mx_abort<kCta>(sh, a.status, crank);
-                        break;
-                    }
-                    mx_fill<kCta>(a, stages + s * a.stage_bytes, &sh.full[s], crank, w.mt, w.nt, kc);
-                }
+        const bool one = tc::elect_one();
+        uint32_t g = 0;
+        Turn at;
+        bool go = true;
+        for (int u = slot; go && u < a.units; u += nslots) {
+            const MxUnit w(a, u);
+            const int am = (w.mt * kCta + crank) * 128, bs = w.nt * a.bn / 128;
+            const int bm = w.nt * a.bn + crank * (columns_of<kCta>(a, w.nt) / 2);
+            if (__any_sync(0xffffffffu, mx_aborted(sh))) break;
+            for (int kc = w.k0; kc < w.k1; ++kc, ++g, at.next(a.stages)) {
+                go = mx_warp_wait(&sh.empty[at.stage], at.parity ^ 1u, a.wait_ns);
+                if (!go) break;
+                if (one)
+                    mx_fill<kCta, kSixteen>(a, stages + at.stage * a.stage_bytes, &sh.full[at.stage], crank,
+                                            am, bm, bs, kc);
             }
+        }
+        if (one) {
+            if (!go) mx_abort<kCta>(sh, a.status, crank);
             sh.fills = g;
             // the MMAs have consumed the last fill of every stage used: no copy into
             // this CTA and no commit to its barriers is still in flight when it ends
             for (uint32_t s = 0; s < (uint32_t)a.stages && s < g; ++s)
                 mx_last_wait<kCta>(&sh.empty[s], ((g - 1 - s) / a.stages) & 1u, sh, a.status, crank);
         }
+        __syncwarp();
     } else if (warp == 1) {
         // ---------------- MMA issuer (the even CTA of a pair) ----------------
-        if (lane == 0 && crank == 0) {
+        if (crank == 0) {
+            const bool one = tc::elect_one();
+            // descriptors: their upper halves do not change, the address is in the lower ones
             const uint32_t s0 = smem_u32(stages);
-            const uint64_t a0 = tc::smem_desc_sw128_kmajor(s0);
-            const uint64_t b0 = tc::smem_desc_sw128_kmajor(s0 + kMxPart);
-            const uint64_t c0 = tc::smem_desc_rows16(s0 + kMxPart + a.b_bytes);
+            const uint64_t codes0 = tc::smem_desc_sw128_kmajor(s0), rows0 = tc::smem_desc_rows16(s0);
+            const uint32_t codes_hi = (uint32_t)(codes0 >> 32), rows_hi = (uint32_t)(rows0 >> 32);
+            const uint32_t b_off = kMxPart >> 4, s_off = (kMxPart + a.b_bytes) >> 4;
+            const uint32_t stage16 = a.stage_bytes >> 4;
+            auto codes_at = [&](uint32_t lo) { return (uint64_t)codes_hi << 32 | lo; };
+            auto rows_at = [&](uint32_t lo) { return (uint64_t)rows_hi << 32 | lo; };
+            constexpr int kBlocks = kSixteen ? 4 : 2;      // of scales for 128 rows
             uint32_t g = 0;
             int it = 0;
-            for (int u = slot; u < a.units && !mx_aborted(sh); u += nslots, ++it) {
+            Turn at, before;
+            bool go = true;
+            for (int u = slot; u < a.units; u += nslots, ++it) {
                 const MxUnit w(a, u);
-                const int b = it % a.accs;
-                if (!mx_wait(&sh.tempty[b], ((uint32_t)(it / a.accs) & 1u) ^ 1u, a.wait_ns)) {
-                    mx_abort<kCta>(sh, a.status, crank);
-                    break;
-                }
+                const int b = a.accs == 2 ? it & 1 : 0;
+                const uint32_t turns = (uint32_t)(a.accs == 2 ? it >> 1 : it);
+                if (__any_sync(0xffffffffu, mx_aborted(sh))) break;
+                go = mx_warp_wait(&sh.tempty[b], (turns & 1u) ^ 1u, a.wait_ns);
+                if (!go) break;
                 tc::fence_after_sync();
                 const uint32_t d = tmem + (uint32_t)(b * 128);
                 const int columns = columns_of<kCta>(a, w.nt);
                 const uint32_t first = tc::idesc_e2m1_f32(128 * kCta, columns, !kSixteen, 0);
                 const uint32_t second = tc::idesc_e2m1_f32(128 * kCta, columns, !kSixteen, 2);
-                uint32_t acc = 0;
-                for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
-                    const uint32_t s = g % a.stages;
-                    if (!mx_wait(&sh.full[s], (g / a.stages) & 1u, a.wait_ns)) {
-                        mx_abort<kCta>(sh, a.status, crank);
-                        break;
-                    }
-                    // the MMAs of the chunk before last have read this set of scales
-                    if (g >= 2) {
-                        const uint32_t h = g - 2;
-                        if (!mx_wait(&sh.empty[h % a.stages], (h / a.stages) & 1u, a.wait_ns)) {
-                            mx_abort<kCta>(sh, a.status, crank);
-                            break;
-                        }
+                for (int kc = w.k0; kc < w.k1; ++kc, ++g, at.next(a.stages)) {
+                    go = mx_warp_wait(&sh.full[at.stage], at.parity, a.wait_ns);
+                    if (!go) break;
+                    // the MMAs that read this set of scales before are complete
+                    if (g >= kScaleSets) {
+                        go = mx_warp_wait(&sh.empty[before.stage], before.parity, a.wait_ns);
+                        if (!go) break;
+                        before.next(a.stages);
                     }
                     tc::fence_after_sync();
-                    const uint64_t off = (uint64_t)(s * a.stage_bytes) >> 4;
-                    const uint64_t ad = a0 + off, bd = b0 + off, cd = c0 + off;
+                    const uint32_t al = (uint32_t)codes0 + at.stage * stage16, bl = al + b_off;
+                    const uint32_t cl = (uint32_t)rows0 + at.stage * stage16 + s_off;
+                    const uint32_t sa = tmem + kScaleCol + g % kScaleSets * kScaleSet, sb = sa + 16;
+                    // (the last chunk of k may be half a one)
                     const int steps = min(4, a.steps - 4 * kc);
-                    const int blocks = kSixteen ? steps : (steps + 1) / 2;
-                    const uint32_t sa = tmem + kScaleCol + (g & 1u) * kScaleSet, sb = sa + 16;
-                    for (int i = 0; i < blocks; ++i) {
-                        tc::copy_scales<kCta>(sa + 4 * i, cd + 32 * i);
-                        for (int j = 0; j < a.bblocks; ++j)
-                            tc::copy_scales<kCta>(sb + 8 * i + 4 * j, cd + 32 * (a.blocks * (1 + j) + i));
+                    if (one) {
+#pragma unroll
+                        for (int i = 0; i < kBlocks; ++i) {
+                            tc::copy_scales<kCta>(sa + 4 * i, rows_at(cl + 32 * i));
+                            tc::copy_scales<kCta>(sb + 8 * i, rows_at(cl + 32 * (kBlocks + i)));
+                            if constexpr (kCta == 2)
+                                tc::copy_scales<kCta>(sb + 8 * i + 4, rows_at(cl + 32 * (2 * kBlocks + i)));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (i >= steps) break;
+                            const uint32_t c = kSixteen ? i : i / 2;
+                            tc::mma_e2m1<kCta, kSixteen>(d, codes_at(al + 2 * i), codes_at(bl + 2 * i),
+                                                         !kSixteen && (i & 1) ? second : first, sa + 4 * c,
+                                                         sb + 8 * c, i > 0 || kc > w.k0 ? 1u : 0u);
+                        }
+                        if (kCta == 2)
+                            tc::commit_pair(&sh.empty[at.stage]);
+                        else
+                            tc::commit(&sh.empty[at.stage]);
                     }
-                    for (int i = 0; i < steps; ++i) {
-                        const uint32_t c = kSixteen ? i : i / 2;
-                        tc::mma_e2m1<kCta, kSixteen>(d, ad + 2 * i, bd + 2 * i,
-                                                     !kSixteen && (i & 1) ? second : first, sa + 4 * c,
-                                                     sb + 8 * c, acc);
-                        acc = 1;
-                    }
-                    if (kCta == 2)
-                        tc::commit_pair(&sh.empty[s]);
-                    else
-                        tc::commit(&sh.empty[s]);
+                    __syncwarp();
                 }
-                if (mx_aborted(sh)) break;
-                if (kCta == 2)
-                    tc::commit_pair(&sh.tfull[b]);
-                else
-                    tc::commit(&sh.tfull[b]);
+                if (!go) break;
+                if (one) {
+                    if (kCta == 2)
+                        tc::commit_pair(&sh.tfull[b]);
+                    else
+                        tc::commit(&sh.tfull[b]);
+                }
+                __syncwarp();
             }
-            sh.chunks = g;
-            sh.tiles = it;
-            // TMEM is released after the last unit's MMAs
-            if (it > 0)
-                mx_last_wait<kCta>(&sh.tfull[(it - 1) % a.accs], (uint32_t)((it - 1) / a.accs) & 1u, sh,
-                                   a.status, crank);
+            if (one) {
+                if (!go) mx_abort<kCta>(sh, a.status, crank);
+                sh.chunks = g;
+                sh.tiles = it;
+                // TMEM is released after the last unit's MMAs
+                if (it > 0)
+                    mx_last_wait<kCta>(&sh.tfull[(it - 1) % a.accs], (uint32_t)((it - 1) / a.accs) & 1u, sh,
+                                       a.status, crank);
+            }
+            __syncwarp();
         }
     } else {
         // ---------------- epilogue ----------------
@@ -369,29 +421,38 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                     mbar_arrive(&sh.tempty[b]);
             }
             const int row = (w.mt * kCta + crank) * 128 + quarter * 32 + lane;
-            if (row >= a.m) continue;
-            const float ra = kSixteen ? __ldg(a.row_a + row) : 1.0f;
+            const float ra = kSixteen && row < a.m ? __ldg(a.row_a + row) : 1.0f;
+            float* rb = sh.row_b[warp - 2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int c0 = (2 * i + group) * 32;
-                if (c0 >= ncols) break;
+                const int c0 = (2 * i + group) * 32, count = ncols - c0;
+                if (count <= 0) break;
+                if (kSixteen) {
+                    __syncwarp();
+                    rb[lane] = lane < count ? __ldg(a.row_b + n0 + c0 + lane) : 0.0f;
+                    __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    if (c0 + j >= ncols) break;
-                    float v = __uint_as_float(r[i][j]);
-                    if (kSixteen) v = v * ra * __ldg(a.row_b + n0 + c0 + j);
-                    if (a.splits > 1)
-                        a.slots[w.split * a.slot_stride + (int64_t)(n0 + c0 + j) * a.ldslot + row] = v;
-                    else
-                        mx_put(a.y, a.dtype, (int64_t)(n0 + c0 + j) * a.ldy + row, v);
+                    for (int j = 0; j < 32; ++j)
+                        r[i][j] = __float_as_uint(__uint_as_float(r[i][j]) * ra * rb[j]);
                 }
+                if (row >= a.m) continue;
+                if (a.splits > 1)
+                    mx_store(a.slots + w.split * a.slot_stride + (int64_t)(n0 + c0) * a.ldslot + row,
+                             a.ldslot, r[i], count);
+                else if (a.dtype == PVS_F32)
+                    mx_store(static_cast<float*>(a.y) + (int64_t)(n0 + c0) * a.ldy + row, a.ldy, r[i], count);
+                else if (a.dtype == PVS_BF16)
+                    mx_store(static_cast<__nv_bfloat16*>(a.y) + (int64_t)(n0 + c0) * a.ldy + row, a.ldy, r[i],
+                             count);
+                else
+                    mx_store(static_cast<__half*>(a.y) + (int64_t)(n0 + c0) * a.ldy + row, a.ldy, r[i], count);
             }
         }
     }
     __syncthreads();
     if (kCta == 2) cluster_barrier();   // no CTA leaves while its peer may still address it
     if (mx_aborted(sh)) {
-        if (threadIdx.x == 0) mx_settle<kCta>(a, sh, stages, crank);
+        if (threadIdx.x == 0) mx_settle<kCta, kSixteen>(a, sh, stages, crank);
         __syncthreads();
         if (kCta == 2) cluster_barrier();
     }
@@ -455,12 +516,10 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     a.steps = kp / 64;
     a.kchunks = (kp + kMxK - 1) / kMxK;
     a.klength = (a.kchunks + p.splits - 1) / p.splits;
-    a.blocks = kMxK / (4 * group);
-    a.bblocks = p.bn > 128 ? 2 : 1;
+    const int blocks = kMxK / (4 * group);   // of scales in a chunk, for 128 rows
     a.accs = p.bn > 128 ? 1 : 2;
     a.b_bytes = (uint32_t)(p.bn / p.cta * 128);
-    a.stage_bytes = kMxPart + a.b_bytes + (uint32_t)((1 + a.bblocks) * a.blocks * 512);
-    a.stage_bytes = (a.stage_bytes + 1023u) / 1024u * 1024u;
+    a.stage_bytes = kMxPart + a.b_bytes + (uint32_t)((1 + p.cta) * blocks * 512);
     a.stages = std::min<int>(kMxStages, (int)((kMxSmem - 2048) / a.stage_bytes));
     const int64_t mtiles = (rows + 128 * p.cta - 1) / (128 * p.cta), ntiles = (batch + p.bn - 1) / p.bn;
     if (mtiles * ntiles * p.splits > 1 << 30) return cudaErrorInvalidValue;
@@ -483,8 +542,8 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     if (!tensor_map_3d(&a.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, codes, 1, rows, ld, ld, ld * rows, 128, 128) ||
         !tensor_map_3d(&a.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.codes, 1, batch, ld, ld, ld * batch, 128,
                        (uint32_t)(p.bn / p.cta)) ||
-        !tensor_map_blocks(&a.sa, scales, (rows + 127) / 128, sblocks, (uint32_t)a.blocks) ||
-        !tensor_map_blocks(&a.sb, p.scales, (batch + 127) / 128, sblocks, (uint32_t)a.blocks))
+        !tensor_map_blocks(&a.sa, scales, (rows + 127) / 128, sblocks, (uint32_t)blocks) ||
+        !tensor_map_blocks(&a.sb, p.scales, (batch + 127) / 128, sblocks, (uint32_t)blocks))
         return cudaErrorInvalidValue;
     const void* fn = mx_kernel(p.cta, group == 16);
     cudaError_t e = raise_smem_limit(fn, kMxSmem);
