@@ -1,9 +1,8 @@
 // Rows in microscaled 4-bit floating point (head.h): packing and unpacking.
 //
-// Bound by memory: a row is read once (groups of 16: its largest element first; up to 1,024
-// elements of it stay in registers) and leaves half a byte an element and a byte a group.  A
-// warp takes a row, a lane eight neighbours at a time, so that a group of 16 is two lanes and
-// one of 32 four.
+// A row is read once (groups of 16: its largest element first; up to 4,096 elements of it stay in
+// the registers of one or four warps) and leaves half a byte an element and a byte a group.  A lane
+// takes eight neighbours, so that a group of 16 is two lanes and one of 32 four.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -23,56 +22,72 @@ constexpr int kPackThreads = 256;
 constexpr int kPackWarps = kPackThreads / 32;
 constexpr int kHeld = 4;             // steps of 256 elements that stay in registers
 
-__device__ __forceinline__ float mx_element(const void* p, int dtype, int64_t i) {
-    if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
-    if (dtype == PVS_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return __half2float(static_cast<const __half*>(p)[i]);
-}
+// Eight neighbours of a row as they lie: four words of 16-bit elements, or eight float32.
+template <int DT>
+struct Eight {
+    uint32_t u[DT == PVS_F32 ? 8 : 4];
 
-// Eight elements of a row from column c, zeros past it.
-template <bool WIDE>
-__device__ __forceinline__ void load_eight(const void* x, int dtype, int64_t row, int c, int cols,
-                                           float (&v)[8]) {
-    uint32_t u[4];
-    if (WIDE && c + 8 <= cols && dtype == PVS_F32) {
-        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(x) + row + c);
-        const float4 a = __ldg(q), b = __ldg(q + 1);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-        v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        return;
-    }
-    if (c + 8 > cols || dtype == PVS_F32) {
+    // From column c of the row at element `row`, zeros past it.
+    template <bool WIDE>
+    __device__ __forceinline__ void load(const void* x, int64_t row, int c, int cols) {
+        if constexpr (DT == PVS_F32) {
+            const float* p = static_cast<const float*>(x) + row + c;
+            if (WIDE && c + 8 <= cols) {
+                const uint4* q = reinterpret_cast<const uint4*>(p);
+                const uint4 f = __ldg(q), g = __ldg(q + 1);
+                u[0] = f.x, u[1] = f.y, u[2] = f.z, u[3] = f.w;
+                u[4] = g.x, u[5] = g.y, u[6] = g.z, u[7] = g.w;
+            } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? mx_element(x, dtype, row + c + i) : 0.0f;
-        return;
-    }
-    const uint16_t* p = static_cast<const uint16_t*>(x) + row + c;
-    if (WIDE) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-        u[0] = a.x, u[1] = a.y, u[2] = a.z, u[3] = a.w;
-    } else {
-        load_eight_halves(p, u);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (dtype == PVS_BF16) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+                for (int i = 0; i < 8; ++i) u[i] = c + i < cols ? __float_as_uint(__ldg(p + i)) : 0u;
+            }
         } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
+            const uint16_t* p = static_cast<const uint16_t*>(x) + row + c;
+            if (c + 8 > cols) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    u[i] = (c + 2 * i < cols ? (uint32_t)__ldg(p + 2 * i) : 0u) |
+                           (c + 2 * i + 1 < cols ? (uint32_t)__ldg(p + 2 * i + 1) : 0u) << 16;
+            } else if (WIDE) {
+                const uint4 f = __ldg(reinterpret_cast<const uint4*>(p));
+                u[0] = f.x, u[1] = f.y, u[2] = f.z, u[3] = f.w;
+            } else {
+                load_eight_halves(p, u);
+            }
         }
     }
-}
-
-// The largest magnitude's bits; an infinity's or more where one is not finite.
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
-    uint32_t t = 0;
+    // The largest magnitude's bits as a float32; an infinity's or more where one is not finite.
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (DT == PVS_F32) {
+            uint32_t t = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(v[i]) & 0x7fffffffu);
-    return t;
-}
+            for (int i = 0; i < 8; ++i) t = max(t, u[i] & 0x7fffffffu);
+            return t;
+        } else {
+            const uint32_t m = 0x7fff7fffu;
+            const uint32_t t = __vmaxu2(__vmaxu2(u[0] & m, u[1] & m), __vmaxu2(u[2] & m, u[3] & m));
+            const uint32_t h = max(t >> 16, t & 0xffffu);
+            if (DT == PVS_BF16) return h << 16;
+            return __float_as_uint(__half2float(__ushort_as_half((uint16_t)h)));
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == PVS_F32) {
+                v[2 * i] = __uint_as_float(u[2 * i]);
+                v[2 * i + 1] = __uint_as_float(u[2 * i + 1]);
+            } else if constexpr (DT == PVS_BF16) {
+                v[2 * i] = __uint_as_float(u[i] << 16);
+                v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
+            }
+        }
+    }
+};
 
 // Eight values in units of their scale to e2m1, ties to the even code, beyond 6 to 6.
 __device__ __forceinline__ uint32_t e2m1_of(const float (&q)[8]) {
@@ -91,114 +106,148 @@ __device__ __forceinline__ uint32_t e2m1_of(const float (&q)[8]) {
 struct PackArgs {
     const void* x;
     int64_t ldx, rows, padded_rows;
-    int cols, dtype, kp;
+    int cols, kp;
     uint8_t* codes;
     uint8_t* scales;
     float* row_scales;               // groups of 16
 };
 
-// The four bytes of a block's four groups of kLanes lanes, in the first of its lanes.
-template <int kLanes>
-__device__ __forceinline__ uint32_t four_of(uint32_t byte) {
-    const int first = (threadIdx.x & 31) & ~(4 * kLanes - 1);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w |= __shfl_sync(0xffffffffu, byte, first + i * kLanes) << (8 * i);
-    return w;
+// x / s by a product with 1 / s, as far as its code goes: off by 2^-22 of itself at most.  A
+// border between codes has three bits and its product with s seven; an element of 16-bit type has
+// 11 at most, so that a quotient is a border or 2^-11 away from it: rounded to 16 bits, it is on
+// its side.  A float32 one may be nearer: there the border's product decides, exactly.
+template <int DT>
+__device__ __forceinline__ float quotient(float x, float s, float over) {
+    const float q = x * over;
+    const uint32_t u = (__float_as_uint(q) + 0x40u) & ~0x7fu;
+    if (DT != PVS_F32) return __uint_as_float(u);
+    if ((u & 0x1fffffu) != 0) return q;
+    const float left = fmaf(-__uint_as_float(u), s, x);
+    const bool more = (left > 0.0f) == (x > 0.0f);
+    return __uint_as_float(left == 0.0f ? u : more ? u + 1u : u - 1u);
+}
+__device__ __forceinline__ float about_inverse(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
 }
 
-template <bool kSixteen, bool WIDE>
-__global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a) {
+// A lane's eight elements from column c, and the scales of the groups that they are in.
+template <bool kSixteen, int DT>
+__device__ __forceinline__ void pack_eight(const PackArgs& a, const Eight<DT>& in, int64_t row, int c,
+                                           uint8_t* to, float row_up, bool bad_row) {
     constexpr int kLanes = kSixteen ? 2 : 4;           // of a group
+    uint32_t top = in.top();
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    uint32_t byte, word;
+    float w[8];
+    in.values(w);
+    if (!kSixteen) {
+        // 2^(floor(log2 top) - 2), its exponent with bias 127: multiplying is exact
+        byte = (uint32_t)max((int)(top >> 23) - 2, 0);
+        const float up = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] *= up;
+        word = e2m1_of(w);
+        if (top >= 0x7f800000u) byte = 255, word = 0;
+    } else {
+        const __nv_fp8_storage_t s8 =
+            __nv_cvt_float_to_fp8(__uint_as_float(top) * (1.0f / 6.0f) * row_up, __NV_SATFINITE, __NV_E4M3);
+        byte = s8;
+        const float s = __half2float(__half(__nv_cvt_fp8_to_halfraw(s8, __NV_E4M3)));
+        const float over = about_inverse(s);
+        // (x row_up is exact but for what is far below a code)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = quotient<DT>(w[k] * row_up, s, over);
+        word = e2m1_of(w);
+        if (bad_row || byte == 0) word = 0;
+        if (bad_row) byte = 0;
+    }
+    if (c >= a.kp) return;
+    *reinterpret_cast<uint32_t*>(a.codes + row * (a.kp / 2) + c / 2) = word;
+    if ((threadIdx.x & (kLanes - 1)) == 0) to[c / (32 * kLanes) * 512 + c / (8 * kLanes) % 4] = (uint8_t)byte;
+}
+
+// A block takes kPackWarps / kWarps rows at a time, kWarps warps to a row, each 1,024 columns in
+// registers (again from memory where a row is longer than all of them hold).
+template <bool kSixteen, int DT, bool WIDE, int kWarps>
+__global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a) {
+    constexpr int kRows = kPackWarps / kWarps, kCols = 256 * kHeld;
+    __shared__ uint32_t tops[kPackWarps];
     next_early();
     wait_before();
-    const int lane = threadIdx.x & 31;
-    const int blocks = a.kp / (kLanes * 32);
-    for (int64_t row = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); row < a.padded_rows;
-         row += (int64_t)gridDim.x * kPackWarps) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_row = warp % kWarps;
+    const int blocks = a.kp / (kSixteen ? 64 : 128);
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.padded_rows; row0 += (int64_t)gridDim.x * kRows) {
+        const int64_t row = row0 + warp / kWarps;
+        const bool here = row < a.rows;
         uint8_t* to = a.scales + row / 128 * blocks * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
-        if (row >= a.rows) {
-            for (int b = lane; b < blocks; b += 32) *reinterpret_cast<uint32_t*>(to + (int64_t)b * 512) = 0;
-            continue;
-        }
         const int64_t at = row * a.ldx;
-        float v[kHeld][8];
+        Eight<DT> v[kHeld];
 #pragma unroll
         for (int i = 0; i < kHeld; ++i)
-            load_eight<WIDE>(a.x, a.dtype, at, 256 * i + 8 * lane, a.cols, v[i]);
+            v[i].template load<WIDE>(a.x, at, in_row * kCols + 256 * i + 8 * lane, here ? a.cols : 0);
         float row_up = 1.0f;                           // 1 / the row's scale
         bool bad_row = false;
         if (kSixteen) {
             uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) top = max(top, top_bits(v[i]));
-            for (int c = 256 * kHeld; c < a.cols; c += 256) {
-                float w[8];
-                load_eight<WIDE>(a.x, a.dtype, at, c + 8 * lane, a.cols, w);
-                top = max(top, top_bits(w));
+            for (int i = 0; i < kHeld; ++i) top = max(top, v[i].top());
+            for (int c0 = (in_row + kWarps) * kCols; here && c0 < a.cols; c0 += kWarps * kCols) {
+                for (int c = c0; c < min(c0 + kCols, a.cols); c += 256) {
+                    Eight<DT> w;
+                    w.template load<WIDE>(a.x, at, c + 8 * lane, a.cols);
+                    top = max(top, w.top());
+                }
             }
             top = __reduce_max_sync(0xffffffffu, top);
+            if (kWarps > 1) {
+                if (lane == 0) tops[warp] = top;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) top = max(top, tops[warp / kWarps * kWarps + i]);
+                __syncthreads();
+            }
             bad_row = top >= 0x7f800000u;
             // 2^(floor(log2 top) - 10): the scales of groups then reach 171 to 352 of 448
             const int e = top == 0 ? 127 : max((int)(top >> 23) - 10, 1);
             row_up = __uint_as_float((uint32_t)(254 - e) << 23);
-            if (lane == 0)
+            if (lane == 0 && in_row == 0 && here)
                 a.row_scales[row] = bad_row ? __int_as_float(0x7fffffff) : __uint_as_float((uint32_t)e << 23);
         }
-#pragma unroll 1
-        for (int c = 0; c < a.kp; c += 256) {
-            float w[8];
-            if (c < 256 * kHeld) {
+        if (!here) {
+            if (row < a.padded_rows)
+                for (int b = in_row * 32 + lane; b < blocks; b += kWarps * 32)
+                    *reinterpret_cast<uint32_t*>(to + (int64_t)b * 512) = 0;
+            continue;
+        }
 #pragma unroll
-                for (int i = 0; i < kHeld; ++i)
-                    if (c == 256 * i) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) w[k] = v[i][k];
-                    }
-            } else {
-                load_eight<WIDE>(a.x, a.dtype, at, c + 8 * lane, a.cols, w);
+        for (int i = 0; i < kHeld; ++i) {
+            const int c = in_row * kCols + 256 * i;
+            if (c < a.kp) pack_eight<kSixteen, DT>(a, v[i], row, c + 8 * lane, to, row_up, bad_row);
+        }
+        for (int c0 = (in_row + kWarps) * kCols; c0 < a.kp; c0 += kWarps * kCols) {
+            for (int c = c0; c < min(c0 + kCols, a.kp); c += 256) {
+                Eight<DT> w;
+                w.template load<WIDE>(a.x, at, c + 8 * lane, a.cols);
+                pack_eight<kSixteen, DT>(a, w, row, c + 8 * lane, to, row_up, bad_row);
             }
-            uint32_t top = top_bits(w);
-#pragma unroll
-            for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            uint32_t byte, word;
-            if (!kSixteen) {
-                // 2^(floor(log2 top) - 2), its exponent with bias 127: multiplying is exact
-                byte = (uint32_t)max((int)(top >> 23) - 2, 0);
-                const float up = __uint_as_float((254u - byte) << 23);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] *= up;
-                word = e2m1_of(w);
-                if (top >= 0x7f800000u) byte = 255, word = 0;
-            } else {
-                const __nv_fp8_storage_t s8 =
-                    __nv_cvt_float_to_fp8(__uint_as_float(top) * (1.0f / 6.0f) * row_up, __NV_SATFINITE, __NV_E4M3);
-                byte = s8;
-                const float s = __half2float(__half(__nv_cvt_fp8_to_halfraw(s8, __NV_E4M3)));
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float x = w[k] * row_up;     // (exact but for what is far below a code)
-                    float q = x / s;
-                    // a quotient that was rounded to a border between codes (three bits, zeros
-                    // behind them) goes a last bit towards what the division left over
-                    const float left = fmaf(-q, s, x);
-                    const uint32_t u = __float_as_uint(q);
-                    if (left != 0.0f && q != 0.0f && (u & 0x1fffffu) == 0)
-                        q = __uint_as_float((left > 0.0f) == (q > 0.0f) ? u + 1u : u - 1u);
-                    w[k] = q;
-                }
-                word = e2m1_of(w);
-                if (bad_row || byte == 0) word = 0;
-                if (bad_row) byte = 0;
-            }
-            if (c + 8 * lane < a.kp)
-                *reinterpret_cast<uint32_t*>(a.codes + row * (a.kp / 2) + (c + 8 * lane) / 2) = word;
-            const uint32_t four = four_of<kLanes>(byte);
-            const int b = (c + 8 * lane) / (32 * kLanes);
-            if ((lane & (4 * kLanes - 1)) == 0 && b < blocks)
-                *reinterpret_cast<uint32_t*>(to + (int64_t)b * 512) = four;
         }
     }
+}
+
+using PackKernel = void (*)(const PackArgs);
+template <bool kSixteen, int DT>
+PackKernel pack_of(bool wide, int warps) {
+    return warps == 1 ? (wide ? mx_pack_kernel<kSixteen, DT, true, 1> : mx_pack_kernel<kSixteen, DT, false, 1>)
+                      : (wide ? mx_pack_kernel<kSixteen, DT, true, 4> : mx_pack_kernel<kSixteen, DT, false, 4>);
+}
+template <bool kSixteen>
+PackKernel pack_of(int dtype, bool wide, int warps) {
+    return dtype == PVS_F32   ? pack_of<kSixteen, PVS_F32>(wide, warps)
+           : dtype == PVS_F16 ? pack_of<kSixteen, PVS_F16>(wide, warps)
+                              : pack_of<kSixteen, PVS_BF16>(wide, warps);
 }
 
 // What codes stand for, eight a thread.
@@ -282,13 +331,14 @@ pvs_status mx_queued(cudaError_t e) {
 
 cudaError_t launch_mx_pack(const void* x, int64_t ldx, int64_t rows, int cols, int dtype, int group,
                            uint8_t* codes, uint8_t* scales, float* row_scales, cudaStream_t st) {
-    const PackArgs a{x, ldx, rows, round_up(rows, 128), cols, dtype, mx_padded(cols), codes, scales, row_scales};
-    const int64_t grid = std::min<int64_t>((a.padded_rows + kPackWarps - 1) / kPackWarps, 1 << 20);
+    const PackArgs a{x, ldx, rows, round_up(rows, 128), cols, mx_padded(cols), codes, scales, row_scales};
+    const int warps = a.kp > 256 * kHeld ? 4 : 1;
+    const int64_t per_block = kPackWarps / warps;
+    const int64_t grid = std::min<int64_t>((a.padded_rows + per_block - 1) / per_block, 1 << 20);
     const bool w = mx_wide(x, ldx, dtype);
     count_launches(1);
-    return launch_early(group == 16 ? (w ? mx_pack_kernel<true, true> : mx_pack_kernel<true, false>)
-                                    : (w ? mx_pack_kernel<false, true> : mx_pack_kernel<false, false>),
-                        grid, kPackThreads, 0, st, a);
+    return launch_early(group == 16 ? pack_of<true>(dtype, w, warps) : pack_of<false>(dtype, w, warps), grid,
+                        kPackThreads, 0, st, a);
 }
 
 }  // namespace head
