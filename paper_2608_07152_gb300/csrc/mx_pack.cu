@@ -174,7 +174,8 @@ __device__ __forceinline__ void pack_eight(const PackArgs& a, const Eight<DT>& i
 template <bool kSixteen, int DT, bool WIDE, int kWarps>
 __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a) {
     constexpr int kRows = kPackWarps / kWarps, kCols = 256 * kHeld;
-    __shared__ uint32_t tops[kPackWarps];
+    __shared__ uint32_t tops[2][kPackWarps];
+    [[maybe_unused]] int turn = 0;
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_row = warp % kWarps;
@@ -203,11 +204,13 @@ __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a)
             }
             top = __reduce_max_sync(0xffffffffu, top);
             if (kWarps > 1) {
-                if (lane == 0) tops[warp] = top;
-                __syncthreads();
+                // (a barrier of the row's warps; the next row's tops go to the other half)
+                uint32_t* t = tops[turn & 1] + warp / kWarps * kWarps;
+                if (lane == 0) t[in_row] = top;
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / kWarps), "n"(kWarps * 32) : "memory");
 #pragma unroll
-                for (int i = 0; i < kWarps; ++i) top = max(top, tops[warp / kWarps * kWarps + i]);
-                __syncthreads();
+                for (int i = 0; i < kWarps; ++i) top = max(top, t[i]);
+                ++turn;
             }
             bad_row = top >= 0x7f800000u;
             // 2^(floor(log2 top) - 10): the scales of groups then reach 171 to 352 of 448
@@ -250,7 +253,24 @@ PackKernel pack_of(int dtype, bool wide, int warps) {
                               : pack_of<kSixteen, PVS_BF16>(wide, warps);
 }
 
-// What codes stand for, eight a thread.
+// A code's value: 0, 1/2, 1, 3/2, 2, 3, 4, 6, and bit 3 the sign.
+__device__ __forceinline__ float value_of(uint32_t n) {
+    const uint32_t e = n >> 1 & 3u, m = n & 1u;
+    const uint32_t f = e == 0 ? m * 0x3f000000u : (126u + e) << 23 | m << 22;
+    return __uint_as_float(f | (n & 8u) << 28);
+}
+template <bool kSixteen>
+__device__ __forceinline__ float unit_of(uint32_t byte, float row_scale) {
+    if (kSixteen)
+        return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * row_scale;
+    return byte == 255 ? __int_as_float(0x7fffffff) : byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+}
+__device__ __forceinline__ uint16_t mx_narrow(float v, int dtype) {
+    return dtype == PVS_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+}
+
+// What codes stand for: eight a thread where rows of `out` are aligned, else one, so that
+// neighbours write neighbours.
 template <bool kSixteen, bool WIDE>
 __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* __restrict__ codes,
                                                                  const uint8_t* __restrict__ scales,
@@ -260,33 +280,45 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
     next_early();
     wait_before();
     constexpr int kGroup = kSixteen ? 16 : 32;
-    const int pieces = (cols + 7) / 8, blocks = kp / (4 * kGroup);
+    const int blocks = kp / (4 * kGroup);
+    auto scale_at = [&](int64_t row, int c) {
+        return __ldg(scales + (row / 128 * blocks + c / (4 * kGroup)) * 512 + (row & 31) * 16 +
+                     ((row >> 5) & 3) * 4 + c / kGroup % 4);
+    };
+    if (!WIDE) {
+        for (int64_t row = (int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5); row < rows;
+             row += (int64_t)gridDim.x * kPackWarps) {
+            const float rs = kSixteen ? __ldg(row_scales + row) : 1.0f;
+#pragma unroll 4
+            for (int c = threadIdx.x & 31; c < cols; c += 32) {
+                const uint32_t n = __ldg(codes + row * (kp / 2) + c / 2) >> (4 * (c & 1)) & 15u;
+                const float v = value_of(n) * unit_of<kSixteen>(scale_at(row, c), rs);
+                if (dtype == PVS_F32)
+                    static_cast<float*>(out)[row * ldout + c] = v;
+                else
+                    static_cast<uint16_t*>(out)[row * ldout + c] = mx_narrow(v, dtype);
+            }
+        }
+        return;
+    }
+    const int pieces = (cols + 7) / 8;
     const int64_t total = rows * pieces, step = (int64_t)gridDim.x * kPackThreads;
     for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < total; i += step) {
         const int64_t row = i / pieces;
         const int c = (int)(i - row * pieces) * 8;
         const uint32_t word = __ldg(reinterpret_cast<const uint32_t*>(codes + row * (kp / 2) + c / 2));
-        const uint8_t byte = __ldg(scales + (row / 128 * blocks + c / (4 * kGroup)) * 512 + (row & 31) * 16 +
-                                   ((row >> 5) & 3) * 4 + c / kGroup % 4);
-        float unit;
-        if (kSixteen)
-            unit = __half2float(__half(__nv_cvt_fp8_to_halfraw(byte, __NV_E4M3))) * __ldg(row_scales + row);
-        else
-            unit = byte == 255 ? __int_as_float(0x7fffffff)
-                   : byte == 0 ? 0x1p-127f : __uint_as_float((uint32_t)byte << 23);
+        const float unit = unit_of<kSixteen>(scale_at(row, c), kSixteen ? __ldg(row_scales + row) : 1.0f);
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t n = word >> (4 * k) & 15u;
-            // 0, 1/2, 1, 3/2, 2, 3, 4, 6
-            const uint32_t e = n >> 1 & 3u, m = n & 1u;
-            const float f = e == 0 ? 0.5f * (float)m : __uint_as_float((126u + e) << 23 | m << 22);
-            v[k] = (n & 8u ? -f : f) * unit;
-        }
+        for (int k = 0; k < 8; ++k) v[k] = value_of(word >> (4 * k) & 15u) * unit;
         const int64_t at = row * ldout + c;
         if (dtype == PVS_F32) {
             float* o = static_cast<float*>(out) + at;
-            if (WIDE && c + 8 <= cols) {
+            if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(o) & 31u) == 0) {
+                asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o), "f"(v[0]), "f"(v[1]),
+                             "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                             : "memory");
+            } else if (c + 8 <= cols) {
                 *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
                 *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
             } else {
@@ -295,20 +327,17 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
                     if (c + k < cols) o[k] = v[k];
             }
         } else {
-            uint16_t h[8];
+            uint32_t h[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                h[k] = dtype == PVS_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[k]))
-                                         : __half_as_ushort(__float2half_rn(v[k]));
+            for (int k = 0; k < 4; ++k)
+                h[k] = mx_narrow(v[2 * k], dtype) | (uint32_t)mx_narrow(v[2 * k + 1], dtype) << 16;
             uint16_t* o = static_cast<uint16_t*>(out) + at;
-            if (WIDE && c + 8 <= cols) {
-                *reinterpret_cast<uint4*>(o) =
-                    make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16,
-                               h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+            if (c + 8 <= cols) {
+                *reinterpret_cast<uint4*>(o) = make_uint4(h[0], h[1], h[2], h[3]);
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (c + k < cols) o[k] = h[k];
+                    if (c + k < cols) o[k] = (uint16_t)(h[k >> 1] >> (16 * (k & 1)));
             }
         }
     }
@@ -371,9 +400,10 @@ extern "C" pvs_status pvs_mx_unpack(const uint8_t* codes, const uint8_t* scales,
     Device dev;
     const pvs_status before = (pvs_status)ready(&dev);
     if (before != PVS_OK) return before;
-    const int64_t pieces = rows * ((cols + 7) / 8);
-    const int64_t grid = std::min<int64_t>((pieces + kPackThreads - 1) / kPackThreads, 1 << 20);
     const bool w = mx_wide(out, ldout, dtype);
+    const int64_t blocks = w ? (rows * ((cols + 7) / 8) + kPackThreads - 1) / kPackThreads
+                             : (rows + kPackWarps - 1) / kPackWarps;
+    const int64_t grid = std::min<int64_t>(blocks, 1 << 20);
     count_launches(1);
     return mx_queued(launch_early(
         group == 16 ? (w ? mx_unpack_kernel<true, true> : mx_unpack_kernel<true, false>)
