@@ -155,7 +155,7 @@ typedef struct pvs_distill_args {
     int32_t reserved;         /* 0                                                   */
 } pvs_distill_args;
 
-/* Bytes of scratch of the two calls, as pvs_xent_workspace; forward, 6 more for each slot and 2
+/* Bytes of scratch of the two calls, as pvs_xent_workspace; forward, 10 more for each slot and 2
  * for each row and 256 items of a block of rows; backward, 8 more for each row. */
 pvs_status pvs_distill_workspace(const pvs_distill_args* args, int32_t backward, size_t* bytes);
 
@@ -298,8 +298,8 @@ pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t items, int32_t 
                              const int64_t* ids, int64_t rows, float scale, int64_t ignore_index,
                              void* y, int64_t ldy, void* cuda_stream);
 
-/* Scratch of the gradient: 16 bytes an id at most, 4 KB for every 2,048 of more than 4,096
- * ids, and two float32 rows for every 32 ids. */
+/* Scratch of the gradient: 16 bytes an id at most, 4 KB for every 1,024 of more than 4,096
+ * ids, and two float32 rows and 4 bytes for every 32 ids. */
 pvs_status pvs_embed_workspace(int64_t rows, int64_t items, int32_t dim, size_t* bytes);
 pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int64_t* ids, int64_t rows,
                               int64_t items, int32_t dim, int32_t dtype, float scale,

@@ -3,10 +3,10 @@
 //   p_k  = exp(c z_k) / sum_i exp(c z_i)           over the slots of a row's list
 //   loss = sum_k p_k (ln p_k - l_k + lse),  G_j = g (q_j - sum_{k: id_k = j} p_k)
 //
-//   forward    lists, each row's ids in ascending order; the product, whose epilogue leaves
-//              the listed items out of the tiles' statistics; and the join, which adds them
-//              with logits that are float32 products of their own (the tensor cores cut each
-//              step's sum, and the teacher's items have the largest logits)
+//   forward    lists, each row's ids in ascending order; their logits, float32 products of
+//              their own (the tensor cores cut each step's sum, and the teacher's items have
+//              the largest logits); the product over all items, whose epilogue leaves the
+//              listed ones out of the tiles' statistics; and the join, which adds them
 //   backward   the product writes G = g q; the listed entries, of which there are few, are
 //              written over it with what the forward pass kept, so that q_j - p_j is taken
 //              once and from one pair of numbers
@@ -45,17 +45,18 @@ __device__ __forceinline__ float teacher_logit(const TopRows& r, int64_t at, int
 }
 
 // ---- lists ---------------------------------------------------------------------------
-// A bitonic network of (id, slot) over the next power of two, padded / 2 threads to a row.
-__global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int padded, int rows_here) {
+// A bitonic network of (id, slot) over the next power of two, 2^bits; a block takes whole rows.
+__global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int bits, int rows_bits) {
     __shared__ unsigned long long keys[kMaxTop];
     next_early();
     wait_before();
     const TopRows& r = a.r;
-    const int64_t row0 = (int64_t)blockIdx.x * rows_here;
-    const int total = rows_here * padded;
+    const int padded = 1 << bits, rows_here = 1 << rows_bits;
+    const int64_t row0 = (int64_t)blockIdx.x << rows_bits;
+    const int total = 1 << (bits + rows_bits);
     for (int i = threadIdx.x; i < total; i += blockDim.x) {
-        const int64_t row = row0 + i / padded;
-        const int k = i % padded;
+        const int64_t row = row0 + (i >> bits);
+        const int k = i & (padded - 1);
         unsigned long long key = (unsigned long long)INT_MAX << 32 | 0xffffffffu;
         if (row < r.a.rows && k < r.top) {
             const int64_t id = r.ids[row * r.top + k];
@@ -65,13 +66,13 @@ __global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int pa
         }
         keys[i] = key;
     }
-    for (int k = 2; k <= padded; k <<= 1) {
-        for (int j = k >> 1; j > 0; j >>= 1) {
+    for (int k = 1; k <= bits; ++k) {
+        for (int j = k - 1; j >= 0; --j) {
             __syncthreads();
             for (int t = threadIdx.x; t < total / 2; t += blockDim.x) {
-                const int i = (t / j) * 2 * j + t % j, l = i + j;
+                const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1)), l = i + (1 << j);
                 const unsigned long long x = keys[i], y = keys[l];
-                if ((x > y) == ((i % padded & k) == 0)) {
+                if ((x > y) == ((i & (padded - 1) & (1 << k)) == 0)) {
                     keys[i] = y;
                     keys[l] = x;
                 }
@@ -80,29 +81,106 @@ __global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int pa
     }
     __syncthreads();
     for (int i = threadIdx.x; i < total; i += blockDim.x) {
-        const int64_t row = row0 + i / padded;
-        const int k = i % padded;
+        const int64_t row = row0 + (i >> bits);
+        const int k = i & (padded - 1);
         if (row < r.a.rows && k < r.top) {
             a.list[row * r.top + k] = (int)(keys[i] >> 32);
             a.slot[row * r.top + k] = (uint16_t)keys[i];
         }
     }
-    for (int64_t i = threadIdx.x; i < a.tiles * rows_here; i += blockDim.x) {
-        const int in = (int)(i % rows_here);
-        const int64_t q = i / rows_here, row = row0 + in;
-        if (row >= r.a.rows) continue;
-        const int64_t start = q / a.piece_tiles * a.piece + q % a.piece_tiles * a.tile;
+    // where each tile of items begins in each row's list: the row first, so that neighbours write
+    // neighbours
+    const int in = threadIdx.x & (rows_here - 1);
+    const int64_t row = row0 + in;
+    if (row >= r.a.rows) return;
+    const unsigned long long* mine = keys + (in << bits);
+    uint16_t* out = a.first + row;
+    for (int q = threadIdx.x >> rows_bits; q < a.tiles; q += blockDim.x >> rows_bits) {
+        const int piece = q / a.piece_tiles;
+        const int64_t start = piece * a.piece + (int64_t)(q - piece * a.piece_tiles) * a.tile;
+        const unsigned long long from = (unsigned long long)start << 32;
         int lo = 0;
         for (int n = r.top; n > 0;) {
             const int half = n >> 1;
-            if ((int64_t)(keys[in * padded + lo + half] >> 32) < start) {
-                lo += half + 1;
-                n -= half + 1;
-            } else {
-                n = half;
+            const bool right = mine[lo + half] < from;
+            lo = right ? lo + half + 1 : lo;
+            n = right ? n - half - 1 : half;
+        }
+        out[q * r.a.rows] = (uint16_t)lo;
+    }
+}
+
+// ---- logits of the listed items ----------------------------------------------------------
+constexpr int kDots = 4;                 // of a warp at once, their loads in flight together
+
+__device__ __forceinline__ void add_pairs(int dtype, uint32_t u, uint32_t v, float& lo, float& hi) {
+    if (dtype == PVS_BF16) {
+        lo = fmaf(__uint_as_float(u << 16), __uint_as_float(v << 16), lo);
+        hi = fmaf(__uint_as_float(u & 0xffff0000u), __uint_as_float(v & 0xffff0000u), hi);
+    } else {
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u));
+        const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&v));
+        lo = fmaf(p.x, q.x, lo);
+        hi = fmaf(p.y, q.y, hi);
+    }
+}
+
+// Bound by the rows of w, `top` for each row of x.
+template <bool WIDE>
+__global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
+    next_early();
+    wait_before();
+    const pvs_xent_args& a = j.r.a;
+    const int lane = threadIdx.x & 31, top = j.r.top, quads = (top + kDots - 1) / kDots;
+    const int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t row = u / quads;
+    if (row >= a.rows) return;
+    const int k0 = (int)(u - row * quads) * kDots;
+    int id[kDots];
+#pragma unroll
+    for (int i = 0; i < kDots; ++i) {
+        id[i] = k0 + i < top ? __ldg(j.list + row * top + k0 + i) : INT_MAX;
+    }
+    if (id[0] == INT_MAX) return;        // (and so are those behind it)
+    float lo[kDots] = {}, hi[kDots] = {};
+    if (WIDE) {
+        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.ldx);
+        const uint4* w[kDots];
+#pragma unroll
+        for (int i = 0; i < kDots; ++i)
+            w[i] = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.w) +
+                                                  (int64_t)(id[i] == INT_MAX ? id[0] : id[i]) * a.ldw);
+#pragma unroll 2
+        for (int k = lane; k < a.dim / 8; k += 32) {
+            uint4 v[kDots];
+#pragma unroll
+            for (int i = 0; i < kDots; ++i) v[i] = __ldg(w[i] + k);
+            const uint4 p = __ldg(x + k);
+#pragma unroll
+            for (int i = 0; i < kDots; ++i) {
+                add_pairs(a.dtype, p.x, v[i].x, lo[i], hi[i]);
+                add_pairs(a.dtype, p.y, v[i].y, lo[i], hi[i]);
+                add_pairs(a.dtype, p.z, v[i].z, lo[i], hi[i]);
+                add_pairs(a.dtype, p.w, v[i].w, lo[i], hi[i]);
             }
         }
-        a.first[q * r.a.rows + row] = (uint16_t)lo;
+    } else {
+#pragma unroll 4
+        for (int k = lane; k < a.dim; k += 32) {
+            const float x = element(a.x, a.dtype, row * a.ldx + k);
+#pragma unroll
+            for (int i = 0; i < kDots; ++i)
+                lo[i] = fmaf(x, element(a.w, a.dtype, (int64_t)(id[i] == INT_MAX ? id[0] : id[i]) * a.ldw + k),
+                             lo[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kDots; ++i) {
+        const float dot = warp_sum(lo[i] + hi[i]);
+        if (lane != i || id[i] == INT_MAX) continue;
+        float b = a.bias ? a.bias[id[i]] : 0.0f;
+        if (isfinite(b)) b = fminf(fmaxf(b * kLog2e, -3.402823466e38f), 3.402823466e38f);
+        j.dots[row * top + k0 + i] = fmaf(dot, j.k2, b);
     }
 }
 
@@ -113,38 +191,7 @@ __device__ __forceinline__ void join(float& m, float& s, float2 p) {
     m = nm;
 }
 
-// A lane's part of <x_row, w_y>.
-__device__ __forceinline__ float dot_part(const TopJoin& j, int64_t row, int64_t y) {
-    const pvs_xent_args& a = j.r.a;
-    float lo = 0.0f, hi = 0.0f;
-    if (!j.wide) {
-#pragma unroll 4
-        for (int k = threadIdx.x & 31; k < a.dim; k += 32)
-            lo = fmaf(element(a.x, a.dtype, row * a.ldx + k), element(a.w, a.dtype, y * a.ldw + k), lo);
-        return lo;
-    }
-    const uint4* x = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.ldx);
-    const uint4* w = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.w) + y * a.ldw);
-    auto add = [&](uint32_t u, uint32_t v) {
-        if (a.dtype == PVS_BF16) {
-            lo = fmaf(__uint_as_float(u << 16), __uint_as_float(v << 16), lo);
-            hi = fmaf(__uint_as_float(u & 0xffff0000u), __uint_as_float(v & 0xffff0000u), hi);
-        } else {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u));
-            const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&v));
-            lo = fmaf(p.x, q.x, lo);
-            hi = fmaf(p.y, q.y, hi);
-        }
-    };
-#pragma unroll 4
-    for (int k = threadIdx.x & 31; k < a.dim / 8; k += 32) {
-        const uint4 u = __ldg(x + k), v = __ldg(w + k);
-        add(u.x, v.x), add(u.y, v.y), add(u.z, v.z), add(u.w, v.w);
-    }
-    return lo + hi;
-}
-
-// R rows a block of eight warps, which share the products; then a warp to a row.
+// R rows a block of eight warps: their tiles' statistics together, then a warp to a row.
 template <int R>
 __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
     constexpr int kLanes = 256 / R;
@@ -155,57 +202,35 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
     const TopRows& r = j.r;
     const pvs_xent_args& a = r.a;
     const int top = r.top;
-    float* ts = top_smem;                        // logits of the listed items, in powers of two
-    float* ps = top_smem + R * top;              // their shares of the teacher's distribution
-    int* ids = reinterpret_cast<int*>(ps + R * top);
     const int64_t row0 = (int64_t)blockIdx.x * R;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     {
-        const int c = threadIdx.x % R, lane = threadIdx.x / R;
+        const int c = threadIdx.x % R, l = threadIdx.x / R;
         float m = -INFINITY, s = 0.0f;
         if (row0 + c < a.rows) {
 #pragma unroll 4
-            for (int64_t i = lane; i < j.n; i += kLanes) join(m, s, j.part[i * a.rows + row0 + c]);
+            for (int64_t i = l; i < j.n; i += kLanes) join(m, s, j.part[i * a.rows + row0 + c]);
         }
-        sh[lane][c] = make_float2(m, s);
-    }
-    for (int i = threadIdx.x; i < R * top; i += 256)
-        ids[i] = row0 + i / top < a.rows ? j.list[row0 * top + i] : INT_MAX;
-    __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = warp; i < R * top; i += 8) {
-        if (ids[i] == INT_MAX) continue;         // (the same for the warp)
-        float dot = 0.0f;
-        if (i % top == 0 || ids[i - 1] != ids[i]) {
-            dot = warp_sum(dot_part(j, row0 + i / top, ids[i]));
-            if (lane == 0) {
-                float b = a.bias ? a.bias[ids[i]] : 0.0f;
-                if (isfinite(b)) b = fminf(fmaxf(b * kLog2e, -3.402823466e38f), 3.402823466e38f);
-                ts[i] = fmaf(dot, j.k2, b);
+        sh[l][c] = make_float2(m, s);
+        // joined in a fixed order
+        for (int w = kLanes / 2; w > 0; w >>= 1) {
+            __syncthreads();
+            if (l < w) {
+                join(m, s, sh[l + w][c]);
+                sh[l][c] = make_float2(m, s);
             }
         }
-    }
-    // the tiles' statistics of a row, joined in a fixed order
-    for (int w = kLanes / 2; w > 0; w >>= 1) {
-        const int c = threadIdx.x % R, l = threadIdx.x / R;
-        float2 v{};
-        if (l < w) {
-            v = sh[l][c];
-            join(v.x, v.y, sh[l + w][c]);
-        }
-        __syncthreads();
-        if (l < w) sh[l][c] = v;
         __syncthreads();
     }
-    __syncthreads();
     for (int c = warp; c < R; c += 8) {
         const int64_t row = row0 + c;
         if (row >= a.rows) continue;
-        const int* id = ids + c * top;
-        float* t = ts + c * top;
-        float* p = ps + c * top;
+        float* t = top_smem + 3 * c * top;           // logits of the listed items, in powers of two
+        float* p = t + top;                          // the teacher's, then their shares
+        int* id = reinterpret_cast<int*>(p + top);
         float m = sh[0][c].x, s = sh[0][c].y;
         float* hits = j.hits + row * top;
-        // the teacher's distribution; ids that are no items, and slots that are not in the list
+        // ids that are no items, and slots that are not in the list
         float zmax = -INFINITY, zsum = 0.0f;
         bool bad = false;
         int n = 0;
@@ -214,17 +239,23 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
             const int64_t raw = r.ids[row * top + slot];
             const float z = teacher_logit(r, row * top + slot, raw);
             p[k] = z;
+            id[k] = j.list[row * top + k];
             if (z == -INFINITY) {
                 hits[slot] = kNoHit;
                 continue;
             }
-            if (raw < 0 || raw >= a.items) bad = true;
+            if (id[k] == INT_MAX) {
+                bad = true;
+            } else {
+                t[k] = j.dots[row * top + k];
+            }
             zmax = fmaxf(zmax, z);
             ++n;
         }
         n = __reduce_add_sync(0xffffffffu, n);
         bad = __any_sync(0xffffffffu, bad);
         zmax = warp_max(zmax);
+        __syncwarp();
         const float nan = __int_as_float(0x7fffffff);
         if (n == 0 || bad) {
             if (lane == 0) {
@@ -237,13 +268,15 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
             continue;
         }
         // (the listed items come first: n of them)
-        for (int k = lane; k < n; k += 32) zsum += expf(p[k] - zmax);
+        float tm = m;
+        for (int k = lane; k < n; k += 32) {
+            const float e = expf(p[k] - zmax);
+            zsum += e;
+            if (k == 0 || id[k - 1] != id[k]) tm = fmaxf(tm, t[k]);
+        }
         zsum = warp_sum(zsum);
         const float log_sum = logf(zsum);
         if (j.apart) {
-            float tm = m;
-            for (int k = lane; k < n; k += 32)
-                if (k == 0 || id[k - 1] != id[k]) tm = fmaxf(tm, t[k]);
             tm = warp_max(tm);
             const float ref = tm == -INFINITY ? 0.0f : tm;
             float ssum = 0.0f;
@@ -253,7 +286,6 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
             s = s * exp2f(m - ref) + ssum;
             m = tm;
         }
-        __syncwarp();
         const float log_s = logf(s);
         float loss = 0.0f;
         for (int k = lane; k < n; k += 32) {
@@ -261,10 +293,13 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
             int first = k, last = k;
             while (first > 0 && id[first - 1] == id[k]) --first;
             while (last + 1 < n && id[last + 1] == id[k]) ++last;
-            float share = 0.0f;
-            for (int i = first; i <= last; ++i) share += expf(p[i] - zmax) / zsum;
-            const float d = t[first] - m;
             const float pk = expf(p[k] - zmax) / zsum;
+            float share = pk;
+            if (first < last) {
+                share = 0.0f;
+                for (int i = first; i <= last; ++i) share += expf(p[i] - zmax) / zsum;
+            }
+            const float d = t[first] - m;
             if (pk > 0.0f || pk != pk)
                 loss += pk * ((p[k] - zmax) - log_sum - fmaf(d, kLn2, -log_s));
             hits[j.slot[row * top + k]] = exp2f(d) / s - share;
@@ -333,12 +368,21 @@ cudaError_t join_launch(const TopJoin& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_top_lists(const TopLists& a, cudaStream_t st) {
-    int padded = 2;
-    while (padded < a.r.top) padded *= 2;
-    const int rows_here = std::max(1, 512 / padded);
+    int bits = 1;
+    while (1 << bits < a.r.top) ++bits;
+    // as many rows a block as 256 threads sort, but a block for every SM first
+    int rows_bits = 0;
+    while (rows_bits < 5 && bits + rows_bits < 9 && a.r.a.rows >> (rows_bits + 1) >= 256) ++rows_bits;
+    const int64_t blocks = ((a.r.a.rows - 1) >> rows_bits) + 1;
     count_launches(1);
-    return launch_early(top_lists_kernel, (a.r.a.rows + rows_here - 1) / rows_here,
-                        std::max(256, padded / 2), 0, st, a, padded, rows_here);
+    return launch_early(top_lists_kernel, blocks, bits == 10 ? 512 : 256, 0, st, a, bits, rows_bits);
+}
+
+cudaError_t launch_top_dots(const TopDots& a, cudaStream_t st) {
+    const int64_t warps = a.r.a.rows * ((a.r.top + kDots - 1) / kDots);
+    if (warps > (int64_t)8 * 0x7fffffff) return cudaErrorInvalidValue;
+    count_launches(1);
+    return launch_early(a.wide ? top_dots_kernel<true> : top_dots_kernel<false>, (warps + 7) / 8, 256, 0, st, a);
 }
 
 cudaError_t launch_top_join(const TopJoin& a, const Device& dev, cudaStream_t st) {

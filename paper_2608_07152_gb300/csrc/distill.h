@@ -27,10 +27,21 @@ struct TopLists {
     int* list;                           // [rows][top]
     uint16_t* slot;                      // [rows][top]
     uint16_t* first;                     // [tiles][rows]
-    int64_t tiles, piece_tiles, piece;   // tile q starts at item q / piece_tiles * piece + ...
+    int tiles, piece_tiles;              // tile q starts at item q / piece_tiles * piece + ...
+    int64_t piece;
     int tile;                            // ... q % piece_tiles * tile
 };
 cudaError_t launch_top_lists(const TopLists& a, cudaStream_t st);
+
+// The student's logits of the listed items, in powers of two: float32 products.
+struct TopDots {
+    TopRows r;
+    const int* list;
+    float k2;
+    bool wide;                           // 16-bit rows of whole, aligned eights
+    float* dots;                         // [rows][top]
+};
+cudaError_t launch_top_dots(const TopDots& a, cudaStream_t st);
 
 // A row's loss and what the backward pass wants, from its tiles' statistics: of every item, or
 // (apart) of those that are not listed.
@@ -38,10 +49,10 @@ struct TopJoin {
     TopRows r;
     const int* list;
     const uint16_t* slot;
+    const float* dots;
     const float2* part;                  // [n][rows]
     int64_t n;
-    bool apart, wide;
-    float k2;
+    bool apart;
     float* loss;
     float4* stats;
     float* hits;                         // [rows][top]

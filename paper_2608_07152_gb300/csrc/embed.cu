@@ -7,8 +7,8 @@
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
 // call: up to kSmall ids in one block's shared memory, more by a stable radix sort of 10 bits
 // a pass.  Then a warp takes 32 sorted entries by 256 columns, eight rows' loads in flight, and
-// writes the rows whose entries all lie among them; sums of rows that run on over several
-// such pieces are kept in float32 and joined by a second launch.  Rows without an entry are
+// writes the rows whose entries start among them; of rows with more than kLong entries the
+// pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
 // found by search in the sorted ids and filled with zeros by other blocks of the first: no
 // row of dw is written twice.
 #include <cuda_bf16.h>
@@ -31,10 +31,11 @@ constexpr int kEmbedWarps = kEmbedThreads / 32;
 constexpr int kSmall = 4096;         // ids that one block sorts
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kKeysPerThread = 8;
+constexpr int kKeysPerThread = 4;
 constexpr int kSortTile = kEmbedThreads * kKeysPerThread;
 constexpr int kPiece = 32;           // sorted entries to a warp
 constexpr int kSlab = 256;           // and columns
+constexpr int kLong = 64;            // entries of a run that one warp adds, at most
 constexpr int kZeroRows = 32;        // rows that a warp searches at once
 
 __device__ __forceinline__ float widen(const void* p, int dtype, int64_t i) {
@@ -171,10 +172,11 @@ __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t ignore_index, int
 __global__ void __launch_bounds__(1024) embed_sort_small_kernel(const int64_t* __restrict__ ids, int n,
                                                                 int padded, int64_t ignore_index,
                                                                 int64_t items, uint32_t* keys,
-                                                                uint32_t* places) {
+                                                                uint32_t* places, uint32_t* longs) {
     __shared__ unsigned long long s[kSmall];
     next_early();
     wait_before();
+    if (threadIdx.x == 0) *longs = 0;
     for (int i = threadIdx.x; i < padded; i += blockDim.x)
         s[i] = i < n ? (unsigned long long)key_of(ids[i], ignore_index, items) << 32 | (uint32_t)i
                      : ~0ull;
@@ -208,6 +210,7 @@ struct SortArgs {
     int64_t tiles;
     uint32_t* counts;                // [digits][tiles]
     uint32_t* totals;                // [digits]
+    uint32_t* longs;                 // of the sums: cleared
 };
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
     return a.ids ? key_of(a.ids[i], a.ignore_index, a.items) : a.keys[i];
@@ -222,6 +225,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_count_kernel(const SortAr
     for (int d = threadIdx.x; d < a.digits; d += kEmbedThreads) count[d] = 0;
     next_early();
     wait_before();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.longs = 0;
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kSortTile;
 #pragma unroll
@@ -340,9 +344,10 @@ struct SumArgs {
     float scale;
     void* dw;
     int64_t lddw;
-    float* part;                     // [piece][2][ldp]: of a run from before, and one that goes on
+    float* part;                     // [piece][2][ldp]: of a long run from before, and one that starts
     int64_t ldp;
     int64_t pieces, sum_blocks;
+    uint32_t* longs;                 // [0] how many pieces a long run starts in, then which
 };
 
 // The first of the sorted keys that is v or more.
@@ -377,106 +382,164 @@ __device__ void zero_rows(const SumArgs& a, int64_t first) {
     }
 }
 
+// A warp's sums over 32 columns of entries that lie in windows of 32 lanes.
+template <bool WIDE>
+struct Sum {
+    const SumArgs& a;
+    int col0;
+    float acc[8];
+
+    __device__ __forceinline__ Sum(const SumArgs& a, int col0) : a(a), col0(col0) { clear(); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
+    }
+    __device__ __forceinline__ void row(uint32_t key) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] *= a.scale;
+        store_share<WIDE>(a.dw, a.dtype, (int64_t)key * a.lddw, col0, a.dim, acc);
+        clear();
+    }
+    __device__ __forceinline__ void piece(int64_t slot) {
+        store_share<WIDE>(a.part + slot * a.ldp, PVS_F32, 0, col0, a.dim, acc);
+        clear();
+    }
+};
+constexpr int kFlight = 8;           // rows whose loads are under way at once
+
 template <bool WIDE>
 __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs a) {
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (blockIdx.x >= a.sum_blocks) {
-        const int64_t step = ((int64_t)gridDim.x - a.sum_blocks) * kEmbedWarps * kZeroRows;
-        for (int64_t v = (((int64_t)blockIdx.x - a.sum_blocks) * kEmbedWarps + warp) * kZeroRows;
-             v < a.items; v += step)
+    // blocks that sum and blocks that write zeros take turns, so that reads and writes overlap
+    const int64_t b = blockIdx.x, blocks = gridDim.x;
+    const int64_t sums_before = b * a.sum_blocks / blocks;
+    if ((b + 1) * a.sum_blocks / blocks == sums_before) {
+        const int64_t step = (blocks - a.sum_blocks) * kEmbedWarps * kZeroRows;
+        for (int64_t v = ((b - sums_before) * kEmbedWarps + warp) * kZeroRows; v < a.items; v += step)
             zero_rows<WIDE>(a, v);
         return;
     }
-    const int64_t u = (int64_t)blockIdx.x * kEmbedWarps + warp;
+    const int64_t u = sums_before * kEmbedWarps + warp;
     const int64_t piece = u / a.slabs;
     if (piece >= a.pieces) return;
     const int col0 = (int)(u - piece * a.slabs) * kSlab;
     const int64_t base = piece * kPiece;
     const uint32_t none = (uint32_t)a.items;
-    const uint32_t key = base + lane < a.n ? __ldg(a.keys + base + lane) : none;
-    const uint32_t place = base + lane < a.n ? __ldg(a.places + base + lane) : 0u;
-    const uint32_t before = base > 0 ? __ldg(a.keys + base - 1) : none;
-    const uint32_t after = base + kPiece < a.n ? __ldg(a.keys + base + kPiece) : none;
+    // five windows of 32 keys, this piece's in the middle: a run of equal keys is long when it
+    // has more than kLong entries, which every piece that it meets sees alike
+    uint32_t k[5], place[3];
+#pragma unroll
+    for (int w = 0; w < 5; ++w) {
+        const int64_t i = base + 32 * (w - 2) + lane;
+        k[w] = i >= 0 && i < a.n ? __ldg(a.keys + i) : none;
+        if (w >= 2) place[w - 2] = i < a.n ? __ldg(a.places + i) : 0u;
+    }
     // entries without a row come last
-    const int count = __popc(__ballot_sync(0xffffffffu, key != none));
-    float acc[8] = {};
-    bool from_before = count > 0 && __shfl_sync(0xffffffffu, key, 0) == before;
-    constexpr int kFlight = 8;
-    for (int i0 = 0; i0 < count; i0 += kFlight) {
+    const int count = __popc(__ballot_sync(0xffffffffu, k[2] != none));
+    if (count == 0) return;
+    const uint32_t head = __shfl_sync(0xffffffffu, k[2], 0);
+    const uint32_t tail = __shfl_sync(0xffffffffu, k[2], count - 1);
+    // how far the first entry's run reaches back (64 at most), and the last one's start and end
+    const uint32_t b1 = ~__ballot_sync(0xffffffffu, k[1] == head), b0 = ~__ballot_sync(0xffffffffu, k[0] == head);
+    const int back = base == 0 ? 0 : b1 ? __clz(b1) : 32 + (b0 ? __clz(b0) : 32);
+    const uint32_t same_head = ~__ballot_sync(0xffffffffu, k[2] == head);
+    const int head_in = same_head ? __ffs(same_head) - 1 : 32;            // of its entries, here
+    const uint32_t same_tail = __ballot_sync(0xffffffffu, k[2] == tail);
+    const int tail_at = __ffs(same_tail) - 1;
+    const uint32_t a3 = ~__ballot_sync(0xffffffffu, k[3] == tail), a4 = ~__ballot_sync(0xffffffffu, k[4] == tail);
+    const int after = count < kPiece ? 0 : a3 ? __ffs(a3) - 1 : 32 + (a4 ? __ffs(a4) - 1 : 32);
+    const bool one_run = head_in == 32;
+    int first = 0, last = count;                 // entries that this warp adds
+    bool head_part = false, tail_part = false;   // as parts of long runs
+    if (back > 0) {
+        const int length = back + (one_run ? 32 + after : head_in);
+        head_part = back >= kLong || length > kLong;
+        if (!head_part) first = head_in;         // the piece that it starts in has it
+    }
+    if (after > 0 && !(one_run && back > 0)) {
+        tail_part = 32 - tail_at + after > kLong;
+        if (!tail_part) last = 32 + after;
+        if (tail_part && lane == 0 && col0 == 0) a.longs[1 + atomicAdd(a.longs, 1u)] = (uint32_t)piece;
+    }
+    Sum<WIDE> sum(a, col0);
+    for (int i0 = first; i0 < last; i0 += kFlight) {
         float v[kFlight][8];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            const uint32_t p = __shfl_sync(0xffffffffu, place, (i0 + i) & 31);
-            if (i0 + i < count) load_share<WIDE>(a.dy, a.dtype, (int64_t)p * a.lddy, col0, a.dim, v[i]);
+            const int at = i0 + i;
+            const uint32_t p0 = __shfl_sync(0xffffffffu, place[0], at & 31);
+            const uint32_t p1 = __shfl_sync(0xffffffffu, place[1], at & 31);
+            const uint32_t p2 = __shfl_sync(0xffffffffu, place[2], at & 31);
+            const uint32_t p = at < 32 ? p0 : at < 64 ? p1 : p2;
+            if (at < last) load_share<WIDE>(a.dy, a.dtype, (int64_t)p * a.lddy, col0, a.dim, v[i]);
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (i0 + i >= count) break;
+            const int at = i0 + i;
+            if (at >= last) break;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
-            const uint32_t here = __shfl_sync(0xffffffffu, key, i0 + i);
-            const uint32_t next =
-                i0 + i + 1 < kPiece ? __shfl_sync(0xffffffffu, key, (i0 + i + 1) & 31) : after;
-            const bool goes_on = next == here;
-            if (goes_on && i0 + i + 1 < kPiece) continue;
-            if (!from_before && !goes_on) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k] *= a.scale;
-                store_share<WIDE>(a.dw, a.dtype, (int64_t)here * a.lddw, col0, a.dim, acc);
-            } else {
-                float* to = a.part + (2 * piece + (from_before ? 0 : 1)) * a.ldp;
-                store_share<WIDE>(to, PVS_F32, 0, col0, a.dim, acc);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
-            from_before = false;
+            for (int c = 0; c < 8; ++c) sum.acc[c] += v[i][c];
+            if (at + 1 == last) break;
+            // (past the piece it is all one run)
+            const uint32_t here = __shfl_sync(0xffffffffu, k[2], at & 31);
+            const uint32_t next = __shfl_sync(0xffffffffu, k[2], (at + 1) & 31);
+            if (at + 1 >= 32 || here == next) continue;
+            if (head_part && at < head_in)
+                sum.piece(2 * piece);
+            else
+                sum.row(here);
         }
     }
+    if (first >= last) return;
+    if (head_part && (one_run || last <= head_in))
+        sum.piece(2 * piece);
+    else if (tail_part)
+        sum.piece(2 * piece + 1);
+    else
+        sum.row(tail);
 }
 
-// A run that goes on past the piece that it starts in: its pieces' sums, 32 warps over them in
-// turn and their sums in the warps' order.
+// The long runs: their pieces' sums, by 16 groups of threads a stretch of the pieces each, and
+// the groups' sums in their order.
 constexpr int kJoinThreads = 1024;
-constexpr int kJoinWarps = kJoinThreads / 32;
-constexpr int kJoinCols = 128;
+constexpr int kJoinLanes = 64;       // of four columns
+constexpr int kJoinGroups = kJoinThreads / kJoinLanes;
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs a, int slabs) {
-    __shared__ float4 sh[kJoinWarps][32];
+    __shared__ float4 sh[kJoinGroups][kJoinLanes];
     next_early();
     wait_before();
-    const int64_t step = gridDim.x / slabs;
-    const int col = (int)(blockIdx.x % slabs) * kJoinCols + 4 * (threadIdx.x & 31);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int64_t piece = blockIdx.x / slabs; piece + 1 < a.pieces; piece += step) {
+    const int64_t total = (int64_t)a.longs[0] * slabs;
+    const int group = threadIdx.x / kJoinLanes, lane = threadIdx.x % kJoinLanes;
+    for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
+        const int64_t piece = a.longs[1 + u / slabs];
+        const int col = (int)(u % slabs) * 4 * kJoinLanes + 4 * lane;
         const int64_t end = (piece + 1) * kPiece;
         const uint32_t key = __ldg(a.keys + end - 1);
-        // (every thread of the block sees the same)
-        if (key == (uint32_t)a.items || __ldg(a.keys + end) != key) continue;
-        const bool all_piece = __ldg(a.keys + piece * kPiece) == key;
-        if (all_piece && piece > 0 && __ldg(a.keys + piece * kPiece - 1) == key) continue;
         const int64_t last = (lower_bound(a.keys + end, a.n - end, key + 1) + end - 1) / kPiece;
+        const int64_t each = (last - piece + kJoinGroups) / kJoinGroups;
+        const int64_t q0 = piece + group * each, q1 = min(q0 + each, last + 1);
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (col < a.ldp) {
-#pragma unroll 4
-            for (int64_t q = piece + warp; q <= last; q += kJoinWarps) {
-                const float4 v = *reinterpret_cast<const float4*>(
-                    a.part + (2 * q + (q == piece ? 1 : 0)) * a.ldp + col);
+#pragma unroll 8
+            for (int64_t q = q0; q < q1; ++q) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(
+                    a.part + (2 * q + (q == piece ? 1 : 0)) * a.ldp + col));
                 s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
             }
         }
-        sh[warp][lane] = s;
+        sh[group][lane] = s;
         __syncthreads();
-        if (warp == 0) {
-            const int used = (int)min((int64_t)kJoinWarps, last - piece + 1);
-            for (int w = 1; w < used; ++w) {
-                const float4 v = sh[w][lane];
+        if (group == 0) {
+            for (int g = 1; g < kJoinGroups && piece + g * each <= last; ++g) {
+                const float4 v = sh[g][lane];
                 s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
             }
             const float f[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (col + k < a.dim) put(a.dw, a.dtype, (int64_t)key * a.lddw + col + k, f[k] * a.scale);
+            for (int c = 0; c < 4; ++c)
+                if (col + c < a.dim) put(a.dw, a.dtype, (int64_t)key * a.lddw + col + c, f[c] * a.scale);
         }
         __syncthreads();
     }
@@ -486,7 +549,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs 
 struct EmbedPlan {
     int passes = 0, bits = 0;
     int64_t tiles = 0, pieces = 0, ldp = 0;
-    uint32_t *keys[2] = {}, *places[2] = {}, *counts = nullptr, *totals = nullptr;
+    uint32_t *keys[2] = {}, *places[2] = {}, *counts = nullptr, *totals = nullptr, *longs = nullptr;
     float* part = nullptr;
     size_t bytes = 0;
 };
@@ -511,6 +574,7 @@ EmbedPlan embed_plan(int64_t n, int64_t items, int dim, void* workspace) {
     }
     p.pieces = (n + kPiece - 1) / kPiece;
     p.ldp = round_up(dim, 8);
+    p.longs = c.take<uint32_t>(1 + p.pieces);
     if (p.pieces > 1) p.part = c.take<float>(p.pieces * 2 * p.ldp);
     p.bytes = c.used;
     return p;
@@ -538,7 +602,7 @@ cudaError_t sort_ids(const int64_t* ids, int64_t n, int64_t items, int64_t ignor
         while (padded < n) padded *= 2;
         count_launches(1);
         return launch_early(embed_sort_small_kernel, 1, std::min(1024, std::max(32, padded / 2)), 0, st,
-                            ids, (int)n, padded, ignore_index, items, p.keys[0], p.places[0]);
+                            ids, (int)n, padded, ignore_index, items, p.keys[0], p.places[0], p.longs);
     }
     cudaError_t e = cudaSuccess;
     for (int i = 0; i < p.passes && e == cudaSuccess; ++i) {
@@ -558,6 +622,7 @@ cudaError_t sort_ids(const int64_t* ids, int64_t n, int64_t items, int64_t ignor
         s.tiles = p.tiles;
         s.counts = p.counts;
         s.totals = p.totals;
+        s.longs = p.longs;
         count_launches(3);
         e = launch_early(embed_count_kernel, p.tiles, kEmbedThreads, 0, st, s);
         if (e == cudaSuccess)
@@ -652,6 +717,7 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     a.part = p.part;
     a.ldp = p.ldp;
     a.pieces = p.pieces;
+    a.longs = p.longs;
     a.sum_blocks = (p.pieces * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
     const int64_t zero = std::min<int64_t>((items + kEmbedWarps * kZeroRows - 1) / (kEmbedWarps * kZeroRows),
                                            (int64_t)1 << 16);
@@ -661,8 +727,9 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     e = launch_early(wide ? embed_sum_kernel<true> : embed_sum_kernel<false>, a.sum_blocks + zero,
                      kEmbedThreads, 0, st, a);
     if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
-    const int slabs = (int)((p.ldp + kJoinCols - 1) / kJoinCols);
-    const int64_t owners = std::min<int64_t>(p.pieces - 1, std::max(1, 8 * dev.sms / slabs));
+    if (rows <= kLong) return PVS_OK;            // (no run is long)
+    const int slabs = (int)((p.ldp + 4 * kJoinLanes - 1) / (4 * kJoinLanes));
+    const int64_t most = std::min<int64_t>(rows / kLong * slabs, 2 * dev.sms);
     count_launches(1);
-    return embed_ended(launch_early(embed_join_kernel, owners * slabs, kJoinThreads, 0, st, a, slabs));
+    return embed_ended(launch_early(embed_join_kernel, most, kJoinThreads, 0, st, a, slabs));
 }

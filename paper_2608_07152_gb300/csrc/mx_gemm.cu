@@ -24,6 +24,7 @@
 #include <algorithm>
 
 #include "../../include/head.h"
+#include "f32x2.cuh"
 #include "kernels.h"
 #include "mx.h"
 #include "pvs_common.cuh"
@@ -57,7 +58,7 @@ struct MxArgs {
     const float *row_a, *row_b;          // row scales, or null
     void* y;
     int64_t ldy;
-    int dtype;
+    int dtype, by_pairs;                 // y in 16 bits, its rows on 4 bytes
     float* slots;                        // splits: float32 sums [split][n][ldslot]
     int64_t slot_stride, ldslot;
     int* status;
@@ -212,6 +213,26 @@ __device__ __forceinline__ T mx_round(uint32_t u) {
         return v;
     else
         return T(v);
+}
+__device__ __forceinline__ uint32_t mx_two(uint32_t lo, uint32_t hi, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t mx_two(uint32_t lo, uint32_t hi, __half) {
+    const __half2 v = __floats2half2_rn(__uint_as_float(lo), __uint_as_float(hi));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// 32 whole rows of 32 neighbours of 16 bits, on 4 bytes: even lanes store the pairs of even rows,
+// odd ones those of odd rows.
+template <typename T>
+__device__ __forceinline__ void mx_store_pairs(T* p, int64_t ld, const uint32_t (&r)[32]) {
+    const bool odd = threadIdx.x & 1u;
+    if (odd) p += ld - 1;
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? r[j] : r[j + 1], 1);
+        *reinterpret_cast<uint32_t*>(p + j * ld) = mx_two(odd ? got : r[j], odd ? r[j + 1] : got, T());
+    }
 }
 template <typename T>
 __device__ __forceinline__ void mx_store(T* p, int64_t ld, const uint32_t (&r)[32], int count) {
@@ -423,6 +444,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const int row = (w.mt * kCta + crank) * 128 + quarter * 32 + lane;
             const float ra = kSixteen && row < a.m ? __ldg(a.row_a + row) : 1.0f;
             float* rb = sh.row_b[warp - 2];
+            const bool pairs = a.by_pairs && row - lane + 32 <= a.m;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c0 = (2 * i + group) * 32, count = ncols - c0;
@@ -431,9 +453,24 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                     __syncwarp();
                     rb[lane] = lane < count ? __ldg(a.row_b + n0 + c0 + lane) : 0.0f;
                     __syncwarp();
+                    const uint64_t by = f2_pack(ra, ra);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        r[i][j] = __float_as_uint(__uint_as_float(r[i][j]) * ra * rb[j]);
+                    for (int j = 0; j < 32; j += 4) {
+                        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(rb + j);
+                        float v0, v1, v2, v3;
+                        f2_unpack(f2_mul(f2_mul(f2_pack(__uint_as_float(r[i][j]), __uint_as_float(r[i][j + 1])), by), f.x), v0, v1);
+                        f2_unpack(f2_mul(f2_mul(f2_pack(__uint_as_float(r[i][j + 2]), __uint_as_float(r[i][j + 3])), by), f.y), v2, v3);
+                        r[i][j] = __float_as_uint(v0), r[i][j + 1] = __float_as_uint(v1);
+                        r[i][j + 2] = __float_as_uint(v2), r[i][j + 3] = __float_as_uint(v3);
+                    }
+                }
+                if (pairs && count >= 32) {
+                    if (a.dtype == PVS_BF16)
+                        mx_store_pairs(static_cast<__nv_bfloat16*>(a.y) + (int64_t)(n0 + c0) * a.ldy + row, a.ldy,
+                                       r[i]);
+                    else
+                        mx_store_pairs(static_cast<__half*>(a.y) + (int64_t)(n0 + c0) * a.ldy + row, a.ldy, r[i]);
+                    continue;
                 }
                 if (row >= a.m) continue;
                 if (a.splits > 1)
@@ -533,6 +570,7 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     a.y = y;
     a.ldy = ldy;
     a.dtype = dtype;
+    a.by_pairs = dtype != PVS_F32 && p.splits == 1 && ldy % 2 == 0 && on_elements(y, 4);
     a.slots = p.slots;
     a.slot_stride = batch * p.ldslot;
     a.ldslot = p.ldslot;

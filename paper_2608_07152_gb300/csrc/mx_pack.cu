@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "../../include/head.h"
+#include "f32x2.cuh"
 #include "kernels.h"
 #include "mx.h"
 #include "pvs_common.cuh"
@@ -112,17 +113,16 @@ struct PackArgs {
     float* row_scales;               // groups of 16
 };
 
-// x / s by a product with 1 / s, as far as its code goes: off by 2^-22 of itself at most.  A
-// border between codes has three bits and its product with s seven; an element of 16-bit type has
-// 11 at most, so that a quotient is a border or 2^-11 away from it: rounded to 16 bits, it is on
-// its side.  A float32 one may be nearer: there the border's product decides, exactly.
+// What x / unit is, as far as its code goes, from q = x times about 1 / unit, off by 2^-22 of itself at
+// most.  A border between codes has three bits and its product with a unit seven; an element of
+// 16-bit type has 11 at most, so that a quotient is a border or 2^-11 away from it: rounded to 16
+// bits, it is on its side.  A float32 one may be nearer: there the border's product decides, exactly.
 template <int DT>
-__device__ __forceinline__ float quotient(float x, float s, float over) {
-    const float q = x * over;
+__device__ __forceinline__ float quotient(float q, float x, float unit) {
     const uint32_t u = (__float_as_uint(q) + 0x40u) & ~0x7fu;
     if (DT != PVS_F32) return __uint_as_float(u);
     if ((u & 0x1fffffu) != 0) return q;
-    const float left = fmaf(-__uint_as_float(u), s, x);
+    const float left = fmaf(-__uint_as_float(u), unit, x);
     const bool more = (left > 0.0f) == (x > 0.0f);
     return __uint_as_float(left == 0.0f ? u : more ? u + 1u : u - 1u);
 }
@@ -131,11 +131,22 @@ __device__ __forceinline__ float about_inverse(float s) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     return r;
 }
+__device__ __forceinline__ void times(float (&w)[8], float f) {
+    const uint64_t ff = f2_pack(f, f);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) f2_unpack(f2_mul(f2_pack(w[k], w[k + 1]), ff), w[k], w[k + 1]);
+}
 
-// A lane's eight elements from column c, and the scales of the groups that they are in.
+// A row of groups of 16: its scale r and 1 / r.
+struct RowScale {
+    float r, up;
+    bool bad;
+};
+
+// A lane's eight elements to `code`, and the scale of the group that they are in to `scale`.
 template <bool kSixteen, int DT>
-__device__ __forceinline__ void pack_eight(const PackArgs& a, const Eight<DT>& in, int64_t row, int c,
-                                           uint8_t* to, float row_up, bool bad_row) {
+__device__ __forceinline__ void pack_eight(const Eight<DT>& in, bool here, uint32_t* code, uint8_t* scale,
+                                           const RowScale& row) {
     constexpr int kLanes = kSixteen ? 2 : 4;           // of a group
     uint32_t top = in.top();
 #pragma unroll
@@ -146,27 +157,34 @@ __device__ __forceinline__ void pack_eight(const PackArgs& a, const Eight<DT>& i
     if (!kSixteen) {
         // 2^(floor(log2 top) - 2), its exponent with bias 127: multiplying is exact
         byte = (uint32_t)max((int)(top >> 23) - 2, 0);
-        const float up = __uint_as_float((254u - byte) << 23);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] *= up;
+        times(w, __uint_as_float((254u - byte) << 23));
         word = e2m1_of(w);
         if (top >= 0x7f800000u) byte = 255, word = 0;
     } else {
         const __nv_fp8_storage_t s8 =
-            __nv_cvt_float_to_fp8(__uint_as_float(top) * (1.0f / 6.0f) * row_up, __NV_SATFINITE, __NV_E4M3);
+            __nv_cvt_float_to_fp8(__uint_as_float(top) * (1.0f / 6.0f) * row.up, __NV_SATFINITE, __NV_E4M3);
         byte = s8;
         const float s = __half2float(__half(__nv_cvt_fp8_to_halfraw(s8, __NV_E4M3)));
-        const float over = about_inverse(s);
-        // (x row_up is exact but for what is far below a code)
+        float unit = s * row.r, up = about_inverse(s) * row.up;
+        if (row.up > 0x1p100f) {
+            // (a row so small that 1 / unit may be no float32)
+            times(w, row.up);
+            unit = s;
+            up = about_inverse(s);
+        }
+        float q[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = quotient<DT>(w[k] * row_up, s, over);
-        word = e2m1_of(w);
-        if (bad_row || byte == 0) word = 0;
-        if (bad_row) byte = 0;
+        for (int k = 0; k < 8; ++k) q[k] = w[k];
+        times(q, up);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[k] = quotient<DT>(q[k], w[k], unit);
+        word = e2m1_of(q);
+        if (row.bad || byte == 0) word = 0;
+        if (row.bad) byte = 0;
     }
-    if (c >= a.kp) return;
-    *reinterpret_cast<uint32_t*>(a.codes + row * (a.kp / 2) + c / 2) = word;
-    if ((threadIdx.x & (kLanes - 1)) == 0) to[c / (32 * kLanes) * 512 + c / (8 * kLanes) % 4] = (uint8_t)byte;
+    if (!here) return;
+    *code = word;
+    if ((threadIdx.x & (kLanes - 1)) == 0) *scale = (uint8_t)byte;
 }
 
 // A block takes kPackWarps / kWarps rows at a time, kWarps warps to a row, each 1,024 columns in
@@ -184,13 +202,16 @@ __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a)
         const int64_t row = row0 + warp / kWarps;
         const bool here = row < a.rows;
         uint8_t* to = a.scales + row / 128 * blocks * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+        // a lane's codes and scale of a step of 256 columns; a step on, 32 words and kStep bytes
+        constexpr int kGroups = kSixteen ? 16 : 8, kStep = kGroups * 128, kLanes = 32 / kGroups;
+        uint32_t* code = reinterpret_cast<uint32_t*>(a.codes + row * (a.kp / 2)) + lane;
+        uint8_t* scale = to + lane / kLanes / 4 * 512 + lane / kLanes % 4;
         const int64_t at = row * a.ldx;
         Eight<DT> v[kHeld];
 #pragma unroll
         for (int i = 0; i < kHeld; ++i)
             v[i].template load<WIDE>(a.x, at, in_row * kCols + 256 * i + 8 * lane, here ? a.cols : 0);
-        float row_up = 1.0f;                           // 1 / the row's scale
-        bool bad_row = false;
+        RowScale rs{1.0f, 1.0f, false};
         if (kSixteen) {
             uint32_t top = 0;
 #pragma unroll
@@ -212,12 +233,13 @@ __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a)
                 for (int i = 0; i < kWarps; ++i) top = max(top, t[i]);
                 ++turn;
             }
-            bad_row = top >= 0x7f800000u;
+            rs.bad = top >= 0x7f800000u;
             // 2^(floor(log2 top) - 10): the scales of groups then reach 171 to 352 of 448
             const int e = top == 0 ? 127 : max((int)(top >> 23) - 10, 1);
-            row_up = __uint_as_float((uint32_t)(254 - e) << 23);
+            rs.r = __uint_as_float((uint32_t)e << 23);
+            rs.up = __uint_as_float((uint32_t)(254 - e) << 23);
             if (lane == 0 && in_row == 0 && here)
-                a.row_scales[row] = bad_row ? __int_as_float(0x7fffffff) : __uint_as_float((uint32_t)e << 23);
+                a.row_scales[row] = rs.bad ? __int_as_float(0x7fffffff) : rs.r;
         }
         if (!here) {
             if (row < a.padded_rows)
@@ -227,14 +249,15 @@ __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a)
         }
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
-            const int c = in_row * kCols + 256 * i;
-            if (c < a.kp) pack_eight<kSixteen, DT>(a, v[i], row, c + 8 * lane, to, row_up, bad_row);
+            const int n = in_row * kHeld + i;
+            if (256 * n < a.kp)
+                pack_eight<kSixteen, DT>(v[i], 256 * n + 8 * lane < a.kp, code + 32 * n, scale + kStep * n, rs);
         }
-        for (int c0 = (in_row + kWarps) * kCols; c0 < a.kp; c0 += kWarps * kCols) {
-            for (int c = c0; c < min(c0 + kCols, a.kp); c += 256) {
+        for (int n0 = (in_row + kWarps) * kHeld; 256 * n0 < a.kp; n0 += kWarps * kHeld) {
+            for (int n = n0; n < n0 + kHeld && 256 * n < a.kp; ++n) {
                 Eight<DT> w;
-                w.template load<WIDE>(a.x, at, c + 8 * lane, a.cols);
-                pack_eight<kSixteen, DT>(a, w, row, c + 8 * lane, to, row_up, bad_row);
+                w.template load<WIDE>(a.x, at, 256 * n + 8 * lane, a.cols);
+                pack_eight<kSixteen, DT>(w, 256 * n + 8 * lane < a.kp, code + 32 * n, scale + kStep * n, rs);
             }
         }
     }

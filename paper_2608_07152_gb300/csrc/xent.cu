@@ -243,6 +243,7 @@ struct Plan {
     // distillation: the rows' lists, and which rows have one
     int* list = nullptr;
     uint16_t *list_slot = nullptr, *list_first = nullptr;
+    float* list_dots = nullptr;
     int64_t* flags = nullptr;
     size_t bytes = 0;
 };
@@ -322,6 +323,7 @@ void plan_lists(Plan& p, const pvs_xent_args& a, bool backward, int top, Carver&
     } else {
         p.list = c.take<int>(a.rows * top);
         p.list_slot = c.take<uint16_t>(a.rows * top);
+        p.list_dots = c.take<float>(a.rows * top);
         if (!p.few) p.list_first = c.take<uint16_t>(p.pieces * p.piece_tiles * a.rows);
     }
 }
@@ -530,9 +532,13 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     const int64_t T = a.rows, V = a.items;
     const int64_t last = V - (p.pieces - 1) * p.piece;
     const int64_t tiles = p.few ? p.few : (p.pieces - 1) * p.piece_tiles + (last + p.bnl - 1) / p.bnl;
+    const bool wide = a.dtype != PVS_F32 && !p.copy_x && !p.copy_w && a.dim % 8 == 0;
     if (top) {
-        TopLists l{*top, p.list, p.list_slot, p.list_first, p.few ? 0 : tiles, p.piece_tiles, p.piece, p.bnl};
+        const TopLists l{*top, p.list, p.list_slot, p.list_first, p.few ? 0 : (int)tiles, (int)p.piece_tiles,
+                         p.piece, p.bnl};
         e = launch_top_lists(l, st);
+        const TopDots d{*top, p.list, a.scale * kLog2e, wide, p.list_dots};
+        if (e == cudaSuccess) e = launch_top_dots(d, st);
         if (e != cudaSuccess) return e;
     }
     if (p.few) {
@@ -562,9 +568,8 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
         e = logits(top ? kTopStats : kStats, g, p, a, v0, n, dev, st);
     }
     if (e != cudaSuccess) return e;
-    const bool wide = a.dtype != PVS_F32 && !p.copy_x && !p.copy_w && a.dim % 8 == 0;
     if (top) {
-        const TopJoin j{*top, p.list, p.list_slot, p.part, tiles, !p.few, wide, a.scale * kLog2e, loss,
+        const TopJoin j{*top, p.list, p.list_slot, p.list_dots, p.part, tiles, !p.few, loss,
                         reinterpret_cast<float4*>(stats), hits};
         return launch_top_join(j, dev, st);
     }
