@@ -1,7 +1,7 @@
 // Rows in microscaled 4-bit floating point (head.h): packing and unpacking.
 //
 // A row is read once (groups of 16: its largest element first; up to 4,096 elements of it stay in
-// the registers of one or four warps) and leaves half a byte an element and a byte a group.  A lane
+// the registers of one to four warps) and leaves half a byte an element and a byte a group.  A lane
 // takes eight neighbours, so that a group of 16 is two lanes and one of 32 four.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -113,14 +113,21 @@ struct PackArgs {
     float* row_scales;               // groups of 16
 };
 
-// What x / unit is, as far as its code goes, from q = x times about 1 / unit, off by 2^-22 of itself at
-// most.  A border between codes has three bits and its product with a unit seven; an element of
-// 16-bit type has 11 at most, so that a quotient is a border or 2^-11 away from it: rounded to 16
-// bits, it is on its side.  A float32 one may be nearer: there the border's product decides, exactly.
-template <int DT>
-__device__ __forceinline__ float quotient(float q, float x, float unit) {
+// The code of x / unit from q = x times about 1 / unit, off by 2^-22 of itself at most.  A border
+// between codes (1/4 to 5) has three bits and its product with a unit seven.  An element of 16-bit
+// type has 11 at most: x is a border's product, or an 11th bit of that product away from it,
+// which is 2^-13 or more in q.  So q to a multiple of 2^-13 is the border, or on its side of it:
+// one FMA and one addition, two elements an instruction.  A float32 may be nearer: there the
+// border's product decides, exactly.
+__device__ __forceinline__ void by_grid(float (&w)[8], float up) {
+    constexpr float kGrid = 1536.0f;                   // 3/2 2^10: float32 steps of 2^-13 around it
+    const uint64_t f = f2_pack(up, up), plus = f2_pack(kGrid, kGrid), minus = f2_pack(-kGrid, -kGrid);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2)
+        f2_unpack(f2_add(f2_fma(f2_pack(w[k], w[k + 1]), f, plus), minus), w[k], w[k + 1]);
+}
+__device__ __forceinline__ float beside_border(float q, float x, float unit) {
     const uint32_t u = (__float_as_uint(q) + 0x40u) & ~0x7fu;
-    if (DT != PVS_F32) return __uint_as_float(u);
     if ((u & 0x1fffffu) != 0) return q;
     const float left = fmaf(-__uint_as_float(u), unit, x);
     const bool more = (left > 0.0f) == (x > 0.0f);
@@ -172,13 +179,18 @@ __device__ __forceinline__ void pack_eight(const Eight<DT>& in, bool here, uint3
             unit = s;
             up = about_inverse(s);
         }
-        float q[8];
+        if (DT != PVS_F32) {
+            by_grid(w, up);
+            word = e2m1_of(w);
+        } else {
+            float q[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) q[k] = w[k];
-        times(q, up);
+            for (int k = 0; k < 8; ++k) q[k] = w[k];
+            times(q, up);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) q[k] = quotient<DT>(q[k], w[k], unit);
-        word = e2m1_of(q);
+            for (int k = 0; k < 8; ++k) q[k] = beside_border(q[k], w[k], unit);
+            word = e2m1_of(q);
+        }
         if (row.bad || byte == 0) word = 0;
         if (row.bad) byte = 0;
     }
@@ -187,10 +199,15 @@ __device__ __forceinline__ void pack_eight(const Eight<DT>& in, bool here, uint3
     if ((threadIdx.x & (kLanes - 1)) == 0) *scale = (uint8_t)byte;
 }
 
+// Blocks to an SM, which set how many loads are in flight: 16,384 rows of 4,096 in bf16, in groups
+// of 16, took 55 us with the registers that the compiler takes by itself, 36 with four blocks, 42
+// with six; in groups of 32 30, 30 and 28.
+constexpr int pack_blocks(bool sixteen, int dtype) { return dtype == PVS_F32 ? 3 : sixteen ? 4 : 6; }
+
 // A block takes kPackWarps / kWarps rows at a time, kWarps warps to a row, each 1,024 columns in
 // registers (again from memory where a row is longer than all of them hold).
 template <bool kSixteen, int DT, bool WIDE, int kWarps>
-__global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a) {
+__global__ void __launch_bounds__(kPackThreads, pack_blocks(kSixteen, DT)) mx_pack_kernel(const PackArgs a) {
     constexpr int kRows = kPackWarps / kWarps, kCols = 256 * kHeld;
     __shared__ uint32_t tops[2][kPackWarps];
     [[maybe_unused]] int turn = 0;
@@ -266,8 +283,9 @@ __global__ void __launch_bounds__(kPackThreads) mx_pack_kernel(const PackArgs a)
 using PackKernel = void (*)(const PackArgs);
 template <bool kSixteen, int DT>
 PackKernel pack_of(bool wide, int warps) {
-    return warps == 1 ? (wide ? mx_pack_kernel<kSixteen, DT, true, 1> : mx_pack_kernel<kSixteen, DT, false, 1>)
-                      : (wide ? mx_pack_kernel<kSixteen, DT, true, 4> : mx_pack_kernel<kSixteen, DT, false, 4>);
+    return warps == 1   ? (wide ? mx_pack_kernel<kSixteen, DT, true, 1> : mx_pack_kernel<kSixteen, DT, false, 1>)
+           : warps == 2 ? (wide ? mx_pack_kernel<kSixteen, DT, true, 2> : mx_pack_kernel<kSixteen, DT, false, 2>)
+                        : (wide ? mx_pack_kernel<kSixteen, DT, true, 4> : mx_pack_kernel<kSixteen, DT, false, 4>);
 }
 template <bool kSixteen>
 PackKernel pack_of(int dtype, bool wide, int warps) {
@@ -384,7 +402,7 @@ pvs_status mx_queued(cudaError_t e) {
 cudaError_t launch_mx_pack(const void* x, int64_t ldx, int64_t rows, int cols, int dtype, int group,
                            uint8_t* codes, uint8_t* scales, float* row_scales, cudaStream_t st) {
     const PackArgs a{x, ldx, rows, round_up(rows, 128), cols, mx_padded(cols), codes, scales, row_scales};
-    const int warps = a.kp > 256 * kHeld ? 4 : 1;
+    const int warps = a.kp > 512 * kHeld ? 4 : a.kp > 256 * kHeld ? 2 : 1;
     const int64_t per_block = kPackWarps / warps;
     const int64_t grid = std::min<int64_t>((a.padded_rows + per_block - 1) / per_block, 1 << 20);
     const bool w = mx_wide(x, ldx, dtype);
