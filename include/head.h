@@ -298,8 +298,8 @@ pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t items, int32_t 
                              const int64_t* ids, int64_t rows, float scale, int64_t ignore_index,
                              void* y, int64_t ldy, void* cuda_stream);
 
-/* Scratch of the gradient: 16 bytes an id at most, 4 KB for every 1,024 of more than 4,096
- * ids, and two float32 rows and 4 bytes for every 32 ids. */
+/* Scratch of the gradient: 16 bytes an id at most, 4 KB for every 1,024 of more than 8,192
+ * ids, and two float32 rows and 4 bytes for every 32 ids (for every 8 of few). */
 pvs_status pvs_embed_workspace(int64_t rows, int64_t items, int32_t dim, size_t* bytes);
 pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int64_t* ids, int64_t rows,
                               int64_t items, int32_t dim, int32_t dtype, float scale,

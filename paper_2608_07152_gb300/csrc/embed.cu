@@ -5,8 +5,7 @@
 //
 // Both are bound by memory.  The backward pass sorts (id, t) first, so that a row's sum runs
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
-// call: up to kSmall ids in one block's shared memory, more by a stable radix sort of 10 bits
-// a pass.  Then a warp takes 32 sorted entries by 256 columns, eight rows' loads in flight, and
+// call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and
 // writes the rows whose entries start among them; of rows with more than kLong entries the
 // pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
 // found by search in the sorted ids and filled with zeros by other blocks of the first: no
@@ -28,14 +27,13 @@ namespace {
 
 constexpr int kEmbedThreads = 256;
 constexpr int kEmbedWarps = kEmbedThreads / 32;
-constexpr int kSmall = 4096;         // ids that one block sorts
+constexpr int kSmall = 8192;         // ids that one block sorts
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kKeysPerThread = 4;
 constexpr int kSortTile = kEmbedThreads * kKeysPerThread;
-constexpr int kPiece = 32;           // sorted entries to a warp
-constexpr int kSlab = 256;           // and columns
-constexpr int kLong = 64;            // entries of a run that one warp adds, at most
+constexpr int kSlab = 256;           // columns to a warp
+constexpr int kLong = 32;            // entries of a run that one warp adds, at most
 constexpr int kZeroRows = 32;        // rows that a warp searches at once
 
 __device__ __forceinline__ float widen(const void* p, int dtype, int64_t i) {
@@ -68,37 +66,46 @@ __device__ __forceinline__ uint32_t narrow_two(float lo, float hi, int dtype) {
 }
 
 // Eight elements of a row, a lane's share of 256: neighbours (WIDE: the row is aligned to 16
-// bytes and holds whole eights) or 32 apart.  Nothing is read past the row.
-template <bool WIDE>
-__device__ __forceinline__ void load_share(const void* p, int dtype, int64_t row, int col0, int dim,
-                                           float (&v)[8]) {
-    const int lane = threadIdx.x & 31;
-    if constexpr (WIDE) {
-        const int c = col0 + 8 * lane;
-        if (c >= dim) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        } else if (dtype == PVS_F32) {
-            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
-            const float4 a = __ldg(q), b = __ldg(q + 1);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-            v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// bytes and holds whole eights; as they lie, four words of 16-bit ones) or 32 apart.  Nothing is
+// read past the row.
+template <bool WIDE, bool F32>
+struct Share {
+    uint32_t u[WIDE && !F32 ? 4 : 8];
+
+    __device__ __forceinline__ void load(const void* p, int dtype, int64_t row, int col0, int dim) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (WIDE) {
+            const int c = col0 + 8 * lane;
+            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (F32) {
+                const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + row + c);
+                const uint4 f = c < dim ? __ldg(q) : none, g = c < dim ? __ldg(q + 1) : none;
+                u[0] = f.x, u[1] = f.y, u[2] = f.z, u[3] = f.w;
+                u[4] = g.x, u[5] = g.y, u[6] = g.z, u[7] = g.w;
+            } else {
+                const uint4 f =
+                    c < dim ? __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c))
+                            : none;
+                u[0] = f.x, u[1] = f.y, u[2] = f.z, u[3] = f.w;
+            }
         } else {
-            const uint4 a =
-                __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + row + c));
-            widen_two(a.x, dtype, v[0], v[1]);
-            widen_two(a.y, dtype, v[2], v[3]);
-            widen_two(a.z, dtype, v[4], v[5]);
-            widen_two(a.w, dtype, v[6], v[7]);
-        }
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = col0 + lane + 32 * i;
-            v[i] = c < dim ? widen(p, dtype, row + c) : 0.0f;
+            for (int i = 0; i < 8; ++i) {
+                const int c = col0 + lane + 32 * i;
+                u[i] = c < dim ? __float_as_uint(widen(p, F32 ? PVS_F32 : dtype, row + c)) : 0u;
+            }
         }
     }
-}
+    __device__ __forceinline__ void values(int dtype, float (&v)[8]) const {
+        if constexpr (WIDE && !F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) widen_two(u[i], dtype, v[2 * i], v[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+        }
+    }
+};
 template <bool WIDE>
 __device__ __forceinline__ void store_share(void* p, int dtype, int64_t row, int col0, int dim,
                                             const float (&v)[8]) {
@@ -137,27 +144,40 @@ struct LookupArgs {
     int slabs;
 };
 
-// A warp takes 256 columns of a row.
-template <bool WIDE>
+// A warp takes 256 columns of kLookups rows, their loads in flight together.
+constexpr int kLookups = 4;
+template <bool WIDE, bool F32>
 __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const LookupArgs a) {
     next_early();
     wait_before();
-    const int64_t units = a.rows * a.slabs, step = (int64_t)gridDim.x * kEmbedWarps;
+    const int64_t units = (a.rows + kLookups - 1) / kLookups * a.slabs;
+    const int64_t step = (int64_t)gridDim.x * kEmbedWarps;
     for (int64_t u = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); u < units; u += step) {
-        const int64_t row = u / a.slabs;
-        const int col0 = (int)(u - row * a.slabs) * kSlab;
-        const int64_t id = __ldg(a.ids + row);
-        float v[8];
-        if (id == a.ignore_index || id < 0 || id >= a.items) {
-            const float f = id == a.ignore_index ? 0.0f : __int_as_float(0x7fffffff);
+        const int64_t row0 = u / a.slabs * kLookups;
+        const int col0 = (int)(u % a.slabs) * kSlab;
+        int64_t id[kLookups];
+        Share<WIDE, F32> in[kLookups];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = f;
-        } else {
-            load_share<WIDE>(a.w, a.dtype, id * a.ldw, col0, a.dim, v);
+        for (int i = 0; i < kLookups; ++i) id[i] = row0 + i < a.rows ? __ldg(a.ids + row0 + i) : a.ignore_index;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+        for (int i = 0; i < kLookups; ++i)
+            if (id[i] != a.ignore_index && id[i] >= 0 && id[i] < a.items)
+                in[i].load(a.w, a.dtype, id[i] * a.ldw, col0, a.dim);
+#pragma unroll
+        for (int i = 0; i < kLookups; ++i) {
+            if (row0 + i >= a.rows) break;
+            float v[8];
+            if (id[i] == a.ignore_index || id[i] < 0 || id[i] >= a.items) {
+                const float f = id[i] == a.ignore_index ? 0.0f : __int_as_float(0x7fffffff);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = f;
+            } else {
+                in[i].values(a.dtype, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= a.scale;
+            }
+            store_share<WIDE>(a.y, a.dtype, (row0 + i) * a.ldy, col0, a.dim, v);
         }
-        store_share<WIDE>(a.y, a.dtype, row * a.ldy, col0, a.dim, v);
     }
 }
 
@@ -167,36 +187,98 @@ __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t ignore_index, int
     return id == ignore_index || id < 0 || id >= items ? (uint32_t)items : (uint32_t)id;
 }
 
-// Up to kSmall ids in one block: (key, position) as one number, a bitonic network over the next
-// power of two.
-__global__ void __launch_bounds__(1024) embed_sort_small_kernel(const int64_t* __restrict__ ids, int n,
-                                                                int padded, int64_t ignore_index,
-                                                                int64_t items, uint32_t* keys,
-                                                                uint32_t* places, uint32_t* longs) {
-    __shared__ unsigned long long s[kSmall];
+__device__ __forceinline__ uint32_t inclusive_sum(uint32_t v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+
+// Up to kSmall ids in one block, eight bits a pass.  A warp ranks its neighbours in order, 32 at a
+// time: equal digits among them by a match, those before by the warp's own counts.
+constexpr int kBlockThreads = 1024;
+constexpr int kBlockWarps = kBlockThreads / 32;
+constexpr int kBlockKeys = kSmall / kBlockThreads;
+constexpr int kBlockDigits = 256;
+__global__ void __launch_bounds__(kBlockThreads) embed_sort_block_kernel(const int64_t* __restrict__ ids, int n,
+                                                                         int bits, int64_t ignore_index,
+                                                                         int64_t items, uint32_t* keys,
+                                                                         uint32_t* places, uint32_t* longs) {
+    extern __shared__ uint2 sorted[];
+    __shared__ uint16_t count[kBlockWarps][kBlockDigits];
+    __shared__ uint32_t first[kBlockDigits];
+    __shared__ uint32_t sums[kBlockDigits / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     next_early();
     wait_before();
     if (threadIdx.x == 0) *longs = 0;
-    for (int i = threadIdx.x; i < padded; i += blockDim.x)
-        s[i] = i < n ? (unsigned long long)key_of(ids[i], ignore_index, items) << 32 | (uint32_t)i
-                     : ~0ull;
-    for (int k = 2; k <= padded; k <<= 1) {
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
-            for (int t = threadIdx.x; t < padded / 2; t += blockDim.x) {
-                const int i = (t / j) * 2 * j + t % j, l = i + j;
-                const unsigned long long x = s[i], y = s[l];
-                if ((x > y) == ((i & k) == 0)) {
-                    s[i] = y;
-                    s[l] = x;
-                }
+    const int rounds = (n + kBlockThreads - 1) / kBlockThreads;
+    const int base = warp * 32 * rounds + lane;
+    uint2 entry[kBlockKeys];
+    uint32_t rank[kBlockKeys];
+#pragma unroll
+    for (int r = 0; r < kBlockKeys; ++r) {
+        const int i = base + 32 * r;
+        if (r < rounds && i < n) entry[r] = make_uint2(key_of(ids[i], ignore_index, items), (uint32_t)i);
+    }
+    for (int shift = 0; shift < bits; shift += 8) {
+        for (int i = threadIdx.x; i < kBlockWarps * kBlockDigits / 2; i += kBlockThreads)
+            reinterpret_cast<uint32_t*>(&count[0][0])[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kBlockKeys; ++r) {
+            if (r >= rounds) break;
+            const bool in = base + 32 * r < n;
+            const int d = in ? (int)(entry[r].x >> shift & 255u) : kBlockDigits;
+            const uint32_t peers = __match_any_sync(0xffffffffu, d);
+            const uint32_t before = in ? count[warp][d] : 0u;
+            rank[r] = before + __popc(peers & ((1u << lane) - 1u));
+            __syncwarp();
+            if (in && lane == 31 - __clz(peers)) count[warp][d] = (uint16_t)(before + __popc(peers));
+            __syncwarp();
+        }
+        __syncthreads();
+        uint32_t total = 0;
+        if (threadIdx.x < kBlockDigits) {
+#pragma unroll 8
+            for (int w = 0; w < kBlockWarps; ++w) {
+                const uint32_t c = count[w][threadIdx.x];
+                count[w][threadIdx.x] = (uint16_t)total;
+                total += c;
+            }
+            const uint32_t incl = inclusive_sum(total);
+            if (lane == 31) sums[warp] = incl;
+            first[threadIdx.x] = incl - total;
+        }
+        __syncthreads();
+        if (threadIdx.x < kBlockDigits) {
+            uint32_t start = 0;
+            for (int w = 0; w < warp; ++w) start += sums[w];
+            first[threadIdx.x] += start;
+        }
+        __syncthreads();
+        const bool last = shift + 8 >= bits;
+#pragma unroll
+        for (int r = 0; r < kBlockKeys; ++r) {
+            if (r >= rounds || base + 32 * r >= n) break;
+            const int d = (int)(entry[r].x >> shift & 255u);
+            const uint32_t to = first[d] + count[warp][d] + rank[r];
+            if (last) {
+                keys[to] = entry[r].x;
+                places[to] = entry[r].y;
+            } else {
+                sorted[to] = entry[r];
             }
         }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        keys[i] = (uint32_t)(s[i] >> 32);
-        places[i] = (uint32_t)s[i];
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kBlockKeys; ++r)
+            if (r < rounds && base + 32 * r < n) entry[r] = sorted[base + 32 * r];
+        // (the counts are cleared after this, and a barrier comes before the next entries)
     }
 }
 
@@ -236,16 +318,6 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_count_kernel(const SortAr
     __syncthreads();
     for (int d = threadIdx.x; d < a.digits; d += kEmbedThreads)
         a.counts[d * a.tiles + blockIdx.x] = count[d];
-}
-
-__device__ __forceinline__ uint32_t inclusive_sum(uint32_t v) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
-    }
-    return v;
 }
 
 // A digit's counts to what comes before each tile; a warp to a digit.
@@ -407,8 +479,9 @@ struct Sum {
 };
 constexpr int kFlight = 8;           // rows whose loads are under way at once
 
-template <bool WIDE>
-__global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs a) {
+// kPiece sorted entries to a warp, and 256 columns.
+template <bool WIDE, bool F32, int kPiece>
+__global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -427,65 +500,68 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs 
     const int col0 = (int)(u - piece * a.slabs) * kSlab;
     const int64_t base = piece * kPiece;
     const uint32_t none = (uint32_t)a.items;
-    // five windows of 32 keys, this piece's in the middle: a run of equal keys is long when it
-    // has more than kLong entries, which every piece that it meets sees alike
-    uint32_t k[5], place[3];
+    // three windows of 32 keys, the middle one from this piece's first: a run of equal keys is long
+    // when it has more than kLong = 32 entries, which every piece that it meets sees alike
+    uint32_t k[3], place[2];
 #pragma unroll
-    for (int w = 0; w < 5; ++w) {
-        const int64_t i = base + 32 * (w - 2) + lane;
+    for (int w = 0; w < 3; ++w) {
+        const int64_t i = base + 32 * (w - 1) + lane;
         k[w] = i >= 0 && i < a.n ? __ldg(a.keys + i) : none;
-        if (w >= 2) place[w - 2] = i < a.n ? __ldg(a.places + i) : 0u;
+        if (w >= 1) place[w - 1] = i < a.n ? __ldg(a.places + i) : 0u;
     }
     // entries without a row come last
-    const int count = __popc(__ballot_sync(0xffffffffu, k[2] != none));
+    constexpr uint32_t kHere = kPiece == 32 ? 0xffffffffu : (1u << (kPiece & 31)) - 1u;
+    const int count = __popc(__ballot_sync(0xffffffffu, k[1] != none) & kHere);
     if (count == 0) return;
-    const uint32_t head = __shfl_sync(0xffffffffu, k[2], 0);
-    const uint32_t tail = __shfl_sync(0xffffffffu, k[2], count - 1);
-    // how far the first entry's run reaches back (64 at most), and the last one's start and end
-    const uint32_t b1 = ~__ballot_sync(0xffffffffu, k[1] == head), b0 = ~__ballot_sync(0xffffffffu, k[0] == head);
-    const int back = base == 0 ? 0 : b1 ? __clz(b1) : 32 + (b0 ? __clz(b0) : 32);
-    const uint32_t same_head = ~__ballot_sync(0xffffffffu, k[2] == head);
-    const int head_in = same_head ? __ffs(same_head) - 1 : 32;            // of its entries, here
-    const uint32_t same_tail = __ballot_sync(0xffffffffu, k[2] == tail);
-    const int tail_at = __ffs(same_tail) - 1;
-    const uint32_t a3 = ~__ballot_sync(0xffffffffu, k[3] == tail), a4 = ~__ballot_sync(0xffffffffu, k[4] == tail);
-    const int after = count < kPiece ? 0 : a3 ? __ffs(a3) - 1 : 32 + (a4 ? __ffs(a4) - 1 : 32);
-    const bool one_run = head_in == 32;
+    const uint32_t head = __shfl_sync(0xffffffffu, k[1], 0);
+    const uint32_t tail = __shfl_sync(0xffffffffu, k[1], count - 1);
+    // how far the first entry's run reaches back, and in; where the last one's starts, and how far
+    // it goes past the piece (32 at most)
+    const int back = base == 0 ? 0 : __clz(~__ballot_sync(0xffffffffu, k[0] == head));
+    const int head_in = min(kPiece, __clz(__brev(~__ballot_sync(0xffffffffu, k[1] == head))));
+    const uint32_t same = __ballot_sync(0xffffffffu, k[1] == tail);
+    const uint32_t same_next = __ballot_sync(0xffffffffu, k[2] == tail);
+    const int tail_at = __ffs(same) - 1;
+    int after = 0;
+    if (count == kPiece) {
+        const uint64_t differ = ~(((uint64_t)same_next << 32 | same) >> kPiece);
+        after = min(kLong, __ffsll((long long)differ) - 1);
+    }
+    const bool one_run = head_in == kPiece;
     int first = 0, last = count;                 // entries that this warp adds
     bool head_part = false, tail_part = false;   // as parts of long runs
     if (back > 0) {
-        const int length = back + (one_run ? 32 + after : head_in);
-        head_part = back >= kLong || length > kLong;
+        head_part = back + (one_run ? kPiece + after : head_in) > kLong;
         if (!head_part) first = head_in;         // the piece that it starts in has it
     }
     if (after > 0 && !(one_run && back > 0)) {
-        tail_part = 32 - tail_at + after > kLong;
-        if (!tail_part) last = 32 + after;
+        tail_part = kPiece - tail_at + after > kLong;
+        if (!tail_part) last = kPiece + after;
         if (tail_part && lane == 0 && col0 == 0) a.longs[1 + atomicAdd(a.longs, 1u)] = (uint32_t)piece;
     }
     Sum<WIDE> sum(a, col0);
     for (int i0 = first; i0 < last; i0 += kFlight) {
-        float v[kFlight][8];
+        Share<WIDE, F32> in[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int at = i0 + i;
             const uint32_t p0 = __shfl_sync(0xffffffffu, place[0], at & 31);
             const uint32_t p1 = __shfl_sync(0xffffffffu, place[1], at & 31);
-            const uint32_t p2 = __shfl_sync(0xffffffffu, place[2], at & 31);
-            const uint32_t p = at < 32 ? p0 : at < 64 ? p1 : p2;
-            if (at < last) load_share<WIDE>(a.dy, a.dtype, (int64_t)p * a.lddy, col0, a.dim, v[i]);
+            if (at < last) in[i].load(a.dy, a.dtype, (int64_t)(at < 32 ? p0 : p1) * a.lddy, col0, a.dim);
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int at = i0 + i;
             if (at >= last) break;
+            float v[8];
+            in[i].values(a.dtype, v);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) sum.acc[c] += v[i][c];
+            for (int c = 0; c < 8; ++c) sum.acc[c] += v[c];
             if (at + 1 == last) break;
             // (past the piece it is all one run)
-            const uint32_t here = __shfl_sync(0xffffffffu, k[2], at & 31);
-            const uint32_t next = __shfl_sync(0xffffffffu, k[2], (at + 1) & 31);
-            if (at + 1 >= 32 || here == next) continue;
+            const uint32_t here = __shfl_sync(0xffffffffu, k[1], at & 31);
+            const uint32_t next = __shfl_sync(0xffffffffu, k[1], (at + 1) & 31);
+            if (at + 1 >= kPiece || here == next) continue;
             if (head_part && at < head_in)
                 sum.piece(2 * piece);
             else
@@ -493,7 +569,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs 
         }
     }
     if (first >= last) return;
-    if (head_part && (one_run || last <= head_in))
+    if (head_part && last <= head_in)
         sum.piece(2 * piece);
     else if (tail_part)
         sum.piece(2 * piece + 1);
@@ -506,7 +582,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumArgs 
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinLanes = 64;       // of four columns
 constexpr int kJoinGroups = kJoinThreads / kJoinLanes;
-__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs a, int slabs) {
+__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs a, int slabs, int piece_keys) {
     __shared__ float4 sh[kJoinGroups][kJoinLanes];
     next_early();
     wait_before();
@@ -515,9 +591,13 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs 
     for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
         const int64_t piece = a.longs[1 + u / slabs];
         const int col = (int)(u % slabs) * 4 * kJoinLanes + 4 * lane;
-        const int64_t end = (piece + 1) * kPiece;
-        const uint32_t key = __ldg(a.keys + end - 1);
-        const int64_t last = (lower_bound(a.keys + end, a.n - end, key + 1) + end - 1) / kPiece;
+        const uint32_t key = __ldg(a.keys + (piece + 1) * piece_keys - 1);
+        // the pieces that start with its key follow one another
+        int64_t last = piece;
+        for (int found = kJoinThreads; found == kJoinThreads; last += found) {
+            const int64_t at = (last + 1 + threadIdx.x) * piece_keys;
+            found = __syncthreads_count(at < a.n && __ldg(a.keys + min(at, a.n - 1)) == key);
+        }
         const int64_t each = (last - piece + kJoinGroups) / kJoinGroups;
         const int64_t q0 = piece + group * each, q1 = min(q0 + each, last + 1);
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -547,6 +627,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs 
 
 // ---- the plan of a call --------------------------------------------------------------
 struct EmbedPlan {
+    int piece = 0;                   // sorted entries to a warp: 32, or 8 where those leave SMs idle
     int passes = 0, bits = 0;
     int64_t tiles = 0, pieces = 0, ldp = 0;
     uint32_t *keys[2] = {}, *places[2] = {}, *counts = nullptr, *totals = nullptr, *longs = nullptr;
@@ -554,14 +635,19 @@ struct EmbedPlan {
     size_t bytes = 0;
 };
 
+// (pieces of 32 by 256 columns that give each of 152 SMs eight warps: 5,000 rows of 385 took a
+// sum of 44 us in them)
+constexpr int64_t kFewUnits = 32 * 8 * 152;
+
 EmbedPlan embed_plan(int64_t n, int64_t items, int dim, void* workspace) {
     EmbedPlan p;
     Carver c{static_cast<uint8_t*>(workspace)};
     p.keys[0] = c.take<uint32_t>(n);
     p.places[0] = c.take<uint32_t>(n);
+    int width = 1;
+    while (items >> width) ++width;                    // of the largest key, `items`
+    p.bits = width;
     if (n > kSmall) {
-        int width = 1;
-        while (items >> width) ++width;                // of the largest key, `items`
         p.passes = (width + kDigitBits - 1) / kDigitBits;
         p.bits = (width + p.passes - 1) / p.passes;
         p.tiles = (n + kSortTile - 1) / kSortTile;
@@ -572,7 +658,8 @@ EmbedPlan embed_plan(int64_t n, int64_t items, int dim, void* workspace) {
         p.counts = c.take<uint32_t>(p.tiles << p.bits);
         p.totals = c.take<uint32_t>((int64_t)1 << p.bits);
     }
-    p.pieces = (n + kPiece - 1) / kPiece;
+    p.piece = n * ((dim + kSlab - 1) / kSlab) < kFewUnits ? 8 : 32;
+    p.pieces = (n + p.piece - 1) / p.piece;
     p.ldp = round_up(dim, 8);
     p.longs = c.take<uint32_t>(1 + p.pieces);
     if (p.pieces > 1) p.part = c.take<float>(p.pieces * 2 * p.ldp);
@@ -593,16 +680,25 @@ pvs_status embed_ended(cudaError_t e) {
     return PVS_ERR_CUDA;
 }
 
+using SumKernel = void (*)(const SumArgs);
+SumKernel sum_kernel(bool wide, bool f32, int piece) {
+    if (piece == 8)
+        return wide ? (f32 ? embed_sum_kernel<true, true, 8> : embed_sum_kernel<true, false, 8>)
+                    : (f32 ? embed_sum_kernel<false, true, 8> : embed_sum_kernel<false, false, 8>);
+    return wide ? (f32 ? embed_sum_kernel<true, true, 32> : embed_sum_kernel<true, false, 32>)
+                : (f32 ? embed_sum_kernel<false, true, 32> : embed_sum_kernel<false, false, 32>);
+}
+
 // The sorted entries' place in the plan's buffers.
 cudaError_t sort_ids(const int64_t* ids, int64_t n, int64_t items, int64_t ignore_index,
                      const EmbedPlan& p, int* where, cudaStream_t st) {
     *where = 0;
     if (p.passes == 0) {
-        int padded = 2;
-        while (padded < n) padded *= 2;
+        const cudaError_t e = raise_smem_limit((const void*)embed_sort_block_kernel, kSmall * 8);
+        if (e != cudaSuccess) return e;
         count_launches(1);
-        return launch_early(embed_sort_small_kernel, 1, std::min(1024, std::max(32, padded / 2)), 0, st,
-                            ids, (int)n, padded, ignore_index, items, p.keys[0], p.places[0], p.longs);
+        return launch_early(embed_sort_block_kernel, 1, kBlockThreads, (size_t)n * 8, st, ids, (int)n, p.bits,
+                            ignore_index, items, p.keys[0], p.places[0], p.longs);
     }
     cudaError_t e = cudaSuccess;
     for (int i = 0; i < p.passes && e == cudaSuccess; ++i) {
@@ -666,9 +762,13 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     a.ldy = ldy;
     a.slabs = (dim + kSlab - 1) / kSlab;
     const bool wide = dim % 8 == 0 && on_16(w, ldw, dtype) && on_16(y, ldy, dtype);
-    const int64_t blocks = (rows * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
+    const int64_t units = (rows + kLookups - 1) / kLookups * a.slabs;
+    const int64_t blocks = (units + kEmbedWarps - 1) / kEmbedWarps;
     count_launches(1);
-    return embed_ended(launch_early(wide ? embed_forward_kernel<true> : embed_forward_kernel<false>,
+    return embed_ended(launch_early(dtype == PVS_F32 ? (wide ? embed_forward_kernel<true, true>
+                                                             : embed_forward_kernel<false, true>)
+                                                     : (wide ? embed_forward_kernel<true, false>
+                                                             : embed_forward_kernel<false, false>),
                                     std::min<int64_t>(blocks, 1 << 24), kEmbedThreads, 0,
                                     static_cast<cudaStream_t>(cuda_stream), a));
 }
@@ -724,12 +824,11 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
     if (a.sum_blocks + zero > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
-    e = launch_early(wide ? embed_sum_kernel<true> : embed_sum_kernel<false>, a.sum_blocks + zero,
-                     kEmbedThreads, 0, st, a);
+    e = launch_early(sum_kernel(wide, dtype == PVS_F32, p.piece), a.sum_blocks + zero, kEmbedThreads, 0, st, a);
     if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
     if (rows <= kLong) return PVS_OK;            // (no run is long)
     const int slabs = (int)((p.ldp + 4 * kJoinLanes - 1) / (4 * kJoinLanes));
     const int64_t most = std::min<int64_t>(rows / kLong * slabs, 2 * dev.sms);
     count_launches(1);
-    return embed_ended(launch_early(embed_join_kernel, most, kJoinThreads, 0, st, a, slabs));
+    return embed_ended(launch_early(embed_join_kernel, most, kJoinThreads, 0, st, a, slabs, p.piece));
 }

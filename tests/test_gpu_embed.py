@@ -69,7 +69,7 @@ def check_gradient(dy, ids, V, scale, **kw):
 
 
 SHAPES = [(1, 1, 1), (1, 50_000, 768), (31, 2, 7), (32, 77, 8), (33, 77, 264), (64, 5, 256), (65, 1023, 100),
-          (1000, 1024, 385), (4096, 1025, 72), (4097, 1025, 72), (6000, 1 << 20, 24), (10_000, 600, 33),
+          (1000, 1024, 385), (4096, 1025, 72), (4097, 1025, 72), (8192, 300, 72), (8193, 70_000, 264), (6000, 1 << 20, 24), (10_000, 600, 33),
           (70_000, 50_000, 16), (300, 100, 2056), (200, 9, 32_767)]
 
 
@@ -85,12 +85,25 @@ def test_lookup_and_gradient(n, V, d, dtype):
         check_gradient(dy, ids, V, 27.7)
 
 
-@pytest.mark.parametrize("n", [1, 32, 33, 64, 95, 2500, 9000])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 31, 32, 33, 34, 64, 65, 95, 2500, 9000, 40_000])
 @pytest.mark.parametrize("how", ["same", "none", "down", "few"])
 def test_runs_of_one_id(n, how):
     dy = torch.randn(n, 40, generator=generator(2), device="cuda")
     for dtype, V in ((F32, 5), (BF16, 3000)):
         check_gradient(dy.to(dtype), some_ids(n, V, how), V, -0.5)
+
+
+@pytest.mark.parametrize("n", [3000, 41_000])
+@pytest.mark.parametrize("seed", range(3))
+def test_runs_of_every_length(n, seed):
+    # runs of 1 to 100 entries, so that they start, cross and end everywhere in the pieces
+    g = generator(100 + seed)
+    lengths = torch.randint(1, 101, (n // 40,), generator=g, device="cuda")
+    ids = torch.repeat_interleave(torch.arange(lengths.numel(), device="cuda") * 2, lengths)[:n]
+    dy = torch.randn(ids.numel(), 24, generator=g, device="cuda")
+    V = 2 * lengths.numel()
+    check_gradient(dy, ids, V, 1.0)
+    check_gradient(dy.to(BF16), ids[torch.randperm(ids.numel(), generator=g, device="cuda")], V, 1.0)
 
 
 def test_long_run_amid_others():

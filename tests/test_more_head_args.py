@@ -53,14 +53,15 @@ def test_lookup_of_nothing():
     assert L.pvs_embed_workspace(4, 0, 16, ctypes.byref(n)) == BAD
 
 
-@pytest.mark.parametrize("rows", [1, 32, 33, 4096, 4097, 100_000, 1 << 30])
+@pytest.mark.parametrize("rows", [1, 32, 33, 8192, 8193, 100_000, 1 << 30])
 def test_gradient_workspace(rows):
     # the documented most; each of eight parts may be rounded up to 256 bytes, and totals take 4 KB
     for items, dim in ((1, 1), (1000, 385), (1 << 20, 4096), ((1 << 31) - (1 << 16), 32767)):
         n = ctypes.c_size_t()
         assert L.pvs_embed_workspace(rows, items, dim, ctypes.byref(n)) == pvs.PVS_OK
         padded = (dim + 7) // 8 * 8
-        pieces = (rows + 31) // 32
+        piece = 8 if rows * ((dim + 255) // 256) < 38_912 else 32
+        pieces = (rows + piece - 1) // piece
         tiles = (rows + 1023) // 1024
         assert 8 * rows <= n.value <= 16 * rows + pieces * (8 * padded + 4) + 4096 * (tiles + 1) + 8 * 256
 
