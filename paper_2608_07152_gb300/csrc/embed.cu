@@ -36,11 +36,6 @@ constexpr int kSlab = 256;           // columns to a warp
 constexpr int kLong = 32;            // entries of a run that one warp adds, at most
 constexpr int kZeroRows = 32;        // rows that a warp searches at once
 
-__device__ __forceinline__ float widen(const void* p, int dtype, int64_t i) {
-    if (dtype == PVS_F32) return static_cast<const float*>(p)[i];
-    if (dtype == PVS_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return __half2float(static_cast<const __half*>(p)[i]);
-}
 __device__ __forceinline__ uint16_t narrow(float v, int dtype) {
     if (dtype == PVS_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
     return __half_as_ushort(__float2half_rn(v));
@@ -72,7 +67,7 @@ template <bool WIDE, bool F32>
 struct Share {
     uint32_t u[WIDE && !F32 ? 4 : 8];
 
-    __device__ __forceinline__ void load(const void* p, int dtype, int64_t row, int col0, int dim) {
+    __device__ __forceinline__ void load(const void* p, int64_t row, int col0, int dim) {
         const int lane = threadIdx.x & 31;
         if constexpr (WIDE) {
             const int c = col0 + 8 * lane;
@@ -92,7 +87,10 @@ struct Share {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = col0 + lane + 32 * i;
-                u[i] = c < dim ? __float_as_uint(widen(p, F32 ? PVS_F32 : dtype, row + c)) : 0u;
+                if constexpr (F32)
+                    u[i] = c < dim ? __float_as_uint(__ldg(static_cast<const float*>(p) + row + c)) : 0u;
+                else
+                    u[i] = c < dim ? (uint32_t)__ldg(static_cast<const uint16_t*>(p) + row + c) : 0u;
             }
         }
     }
@@ -101,8 +99,14 @@ struct Share {
 #pragma unroll
             for (int i = 0; i < 4; ++i) widen_two(u[i], dtype, v[2 * i], v[2 * i + 1]);
         } else {
+            // (a bf16 is the upper half of a float32)
+            if (!F32 && dtype == PVS_F16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+                for (int i = 0; i < 8; ++i) v[i] = __half2float(__ushort_as_half((uint16_t)u[i]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(F32 ? u[i] : u[i] << 16);
+            }
         }
     }
 };
@@ -123,10 +127,18 @@ __device__ __forceinline__ void store_share(void* p, int dtype, int64_t row, int
                            narrow_two(v[4], v[5], dtype), narrow_two(v[6], v[7], dtype));
         }
     } else {
+        if (dtype == PVS_F32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = col0 + lane + 32 * i;
-            if (c < dim) put(p, dtype, row + c, v[i]);
+            for (int i = 0; i < 8; ++i) {
+                const int c = col0 + lane + 32 * i;
+                if (c < dim) static_cast<float*>(p)[row + c] = v[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = col0 + lane + 32 * i;
+                if (c < dim) static_cast<uint16_t*>(p)[row + c] = narrow(v[i], dtype);
+            }
         }
     }
 }
@@ -144,40 +156,46 @@ struct LookupArgs {
     int slabs;
 };
 
-// A warp takes 256 columns of kLookups rows, their loads in flight together.
+// A warp takes kLookups neighbouring pieces of 256 columns of y, their loads in flight together.
 constexpr int kLookups = 4;
 template <bool WIDE, bool F32>
 __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const LookupArgs a) {
     next_early();
     wait_before();
-    const int64_t units = (a.rows + kLookups - 1) / kLookups * a.slabs;
-    const int64_t step = (int64_t)gridDim.x * kEmbedWarps;
-    for (int64_t u = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); u < units; u += step) {
-        const int64_t row0 = u / a.slabs * kLookups;
-        const int col0 = (int)(u % a.slabs) * kSlab;
-        int64_t id[kLookups];
-        Share<WIDE, F32> in[kLookups];
+    const int64_t pieces = a.rows * a.slabs;
+    const int64_t p0 = ((int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5)) * kLookups;
+    if (p0 >= pieces) return;
+    int64_t row[kLookups], id[kLookups];
+    int col0[kLookups];
+    Share<WIDE, F32> in[kLookups];
+    row[0] = p0 / a.slabs;
+    col0[0] = (int)(p0 - row[0] * a.slabs) * kSlab;
 #pragma unroll
-        for (int i = 0; i < kLookups; ++i) id[i] = row0 + i < a.rows ? __ldg(a.ids + row0 + i) : a.ignore_index;
+    for (int i = 1; i < kLookups; ++i) {
+        const bool next = col0[i - 1] + kSlab >= a.dim;
+        row[i] = row[i - 1] + (next ? 1 : 0);
+        col0[i] = next ? 0 : col0[i - 1] + kSlab;
+    }
 #pragma unroll
-        for (int i = 0; i < kLookups; ++i)
-            if (id[i] != a.ignore_index && id[i] >= 0 && id[i] < a.items)
-                in[i].load(a.w, a.dtype, id[i] * a.ldw, col0, a.dim);
+    for (int i = 0; i < kLookups; ++i) id[i] = row[i] < a.rows ? __ldg(a.ids + row[i]) : a.ignore_index;
 #pragma unroll
-        for (int i = 0; i < kLookups; ++i) {
-            if (row0 + i >= a.rows) break;
-            float v[8];
-            if (id[i] == a.ignore_index || id[i] < 0 || id[i] >= a.items) {
-                const float f = id[i] == a.ignore_index ? 0.0f : __int_as_float(0x7fffffff);
+    for (int i = 0; i < kLookups; ++i)
+        if (id[i] != a.ignore_index && id[i] >= 0 && id[i] < a.items)
+            in[i].load(a.w, id[i] * a.ldw, col0[i], a.dim);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = f;
-            } else {
-                in[i].values(a.dtype, v);
+    for (int i = 0; i < kLookups; ++i) {
+        if (row[i] >= a.rows) break;
+        float v[8];
+        if (id[i] == a.ignore_index || id[i] < 0 || id[i] >= a.items) {
+            const float f = id[i] == a.ignore_index ? 0.0f : __int_as_float(0x7fffffff);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= a.scale;
-            }
-            store_share<WIDE>(a.y, a.dtype, (row0 + i) * a.ldy, col0, a.dim, v);
+            for (int k = 0; k < 8; ++k) v[k] = f;
+        } else {
+            in[i].values(a.dtype, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= a.scale;
         }
+        store_share<WIDE>(a.y, a.dtype, row[i] * a.ldy, col0[i], a.dim, v);
     }
 }
 
@@ -547,7 +565,7 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum
             const int at = i0 + i;
             const uint32_t p0 = __shfl_sync(0xffffffffu, place[0], at & 31);
             const uint32_t p1 = __shfl_sync(0xffffffffu, place[1], at & 31);
-            if (at < last) in[i].load(a.dy, a.dtype, (int64_t)(at < 32 ? p0 : p1) * a.lddy, col0, a.dim);
+            if (at < last) in[i].load(a.dy, (int64_t)(at < 32 ? p0 : p1) * a.lddy, col0, a.dim);
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
@@ -762,14 +780,14 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     a.ldy = ldy;
     a.slabs = (dim + kSlab - 1) / kSlab;
     const bool wide = dim % 8 == 0 && on_16(w, ldw, dtype) && on_16(y, ldy, dtype);
-    const int64_t units = (rows + kLookups - 1) / kLookups * a.slabs;
-    const int64_t blocks = (units + kEmbedWarps - 1) / kEmbedWarps;
+    const int64_t blocks = (rows * a.slabs + kEmbedWarps * kLookups - 1) / (kEmbedWarps * kLookups);
+    if (blocks > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
     return embed_ended(launch_early(dtype == PVS_F32 ? (wide ? embed_forward_kernel<true, true>
                                                              : embed_forward_kernel<false, true>)
                                                      : (wide ? embed_forward_kernel<true, false>
                                                              : embed_forward_kernel<false, false>),
-                                    std::min<int64_t>(blocks, 1 << 24), kEmbedThreads, 0,
+                                    blocks, kEmbedThreads, 0,
                                     static_cast<cudaStream_t>(cuda_stream), a));
 }
 
