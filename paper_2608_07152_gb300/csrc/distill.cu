@@ -125,8 +125,21 @@ __device__ __forceinline__ void add_pairs(int dtype, uint32_t u, uint32_t v, flo
     }
 }
 
-// Bound by the rows of w, `top` for each row of x.
-template <bool WIDE>
+// Elements as they lie, so that no load waits for another's type.
+template <int KIND>
+__device__ __forceinline__ uint32_t raw_element(const void* p, int64_t i) {
+    if constexpr (KIND == 2) return __float_as_uint(__ldg(static_cast<const float*>(p) + i));
+    return __ldg(static_cast<const uint16_t*>(p) + i);
+}
+template <int KIND>
+__device__ __forceinline__ float raw_value(uint32_t u, int dtype) {
+    if constexpr (KIND == 2) return __uint_as_float(u);
+    return dtype == PVS_BF16 ? __uint_as_float(u << 16) : __half2float(__ushort_as_half((uint16_t)u));
+}
+
+// Bound by the rows of w, `top` for each row of x.  KIND 0: 16-bit rows of whole, aligned eights;
+// 1: other 16-bit rows; 2: float32.
+template <int KIND>
 __global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
     next_early();
     wait_before();
@@ -143,7 +156,7 @@ __global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
     }
     if (id[0] == INT_MAX) return;        // (and so are those behind it)
     float lo[kDots] = {}, hi[kDots] = {};
-    if (WIDE) {
+    if constexpr (KIND == 0) {
         const uint4* x = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.ldx);
         const uint4* w[kDots];
 #pragma unroll
@@ -165,13 +178,18 @@ __global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
             }
         }
     } else {
+        int64_t w[kDots];
+#pragma unroll
+        for (int i = 0; i < kDots; ++i) w[i] = (int64_t)(id[i] == INT_MAX ? id[0] : id[i]) * a.ldw;
 #pragma unroll 4
         for (int k = lane; k < a.dim; k += 32) {
-            const float x = element(a.x, a.dtype, row * a.ldx + k);
+            const uint32_t x = raw_element<KIND>(a.x, row * a.ldx + k);
+            uint32_t v[kDots];
+#pragma unroll
+            for (int i = 0; i < kDots; ++i) v[i] = raw_element<KIND>(a.w, w[i] + k);
 #pragma unroll
             for (int i = 0; i < kDots; ++i)
-                lo[i] = fmaf(x, element(a.w, a.dtype, (int64_t)(id[i] == INT_MAX ? id[0] : id[i]) * a.ldw + k),
-                             lo[i]);
+                lo[i] = fmaf(raw_value<KIND>(x, a.dtype), raw_value<KIND>(v[i], a.dtype), lo[i]);
         }
     }
 #pragma unroll
@@ -382,7 +400,8 @@ cudaError_t launch_top_dots(const TopDots& a, cudaStream_t st) {
     const int64_t warps = a.r.a.rows * ((a.r.top + kDots - 1) / kDots);
     if (warps > (int64_t)8 * 0x7fffffff) return cudaErrorInvalidValue;
     count_launches(1);
-    return launch_early(a.wide ? top_dots_kernel<true> : top_dots_kernel<false>, (warps + 7) / 8, 256, 0, st, a);
+    return launch_early(a.r.a.dtype == PVS_F32 ? top_dots_kernel<2> : a.wide ? top_dots_kernel<0> : top_dots_kernel<1>,
+                        (warps + 7) / 8, 256, 0, st, a);
 }
 
 cudaError_t launch_top_join(const TopJoin& a, const Device& dev, cudaStream_t st) {

@@ -595,9 +595,9 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum
         sum.row(tail);
 }
 
-// The long runs: their pieces' sums, by 16 groups of threads a stretch of the pieces each, and
+// The long runs: their pieces' sums, by eight groups of threads a stretch of the pieces each, and
 // the groups' sums in their order.
-constexpr int kJoinThreads = 1024;
+constexpr int kJoinThreads = 512;
 constexpr int kJoinLanes = 64;       // of four columns
 constexpr int kJoinGroups = kJoinThreads / kJoinLanes;
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const SumArgs a, int slabs, int piece_keys) {
@@ -846,7 +846,7 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
     if (rows <= kLong) return PVS_OK;            // (no run is long)
     const int slabs = (int)((p.ldp + 4 * kJoinLanes - 1) / (4 * kJoinLanes));
-    const int64_t most = std::min<int64_t>(rows / kLong * slabs, 2 * dev.sms);
+    const int64_t most = std::min<int64_t>(rows / kLong * slabs, 4 * dev.sms);
     count_launches(1);
     return embed_ended(launch_early(embed_join_kernel, most, kJoinThreads, 0, st, a, slabs, p.piece));
 }
