@@ -74,7 +74,7 @@ struct MxShared {
     int abort;                           // of the pair: set in both its CTAs
     uint32_t fills;                      // stages that this CTA has filled
     uint32_t chunks, tiles;              // even CTA: chunks and tiles committed
-    alignas(16) float row_b[kMxEpiWarps][32];
+    alignas(16) float row_b[kMxEpiWarps][4][32];   // a tile's scales of rows of x, by warp
 };
 
 constexpr size_t kMxSmem = 227 * 1024;
@@ -414,6 +414,20 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         for (int u = slot; u < a.units; u += nslots, ++it) {
             const MxUnit w(a, u);
             const int b = it % a.accs;
+            const int n0 = w.nt * a.bn, ncols = min(a.bn, a.n - n0);
+            const int row = (w.mt * kCta + crank) * 128 + quarter * 32 + lane;
+            float ra = 1.0f;
+            if (kSixteen) {
+                // (before the wait, under which the loads are done)
+                if (row < a.m) ra = __ldg(a.row_a + row);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = (2 * i + group) * 32 + lane;
+                    sh.row_b[warp - 2][i][lane] = c < ncols ? __ldg(a.row_b + n0 + c) : 0.0f;
+                }
+                __syncwarp();
+            }
             if (!dead) {
                 bool late = mx_aborted(sh);
                 if (!late && !mx_wait(&sh.tfull[b], (uint32_t)(it / a.accs) & 1u, a.wait_ns)) {
@@ -425,7 +439,6 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             if (dead) continue;
             tc::fence_after_sync();
             const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * 128);
-            const int n0 = w.nt * a.bn, ncols = min(a.bn, a.n - n0);
             uint32_t r[4][32];
             __syncwarp();
 #pragma unroll
@@ -441,18 +454,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 else
                     mbar_arrive(&sh.tempty[b]);
             }
-            const int row = (w.mt * kCta + crank) * 128 + quarter * 32 + lane;
-            const float ra = kSixteen && row < a.m ? __ldg(a.row_a + row) : 1.0f;
-            float* rb = sh.row_b[warp - 2];
             const bool pairs = a.by_pairs && row - lane + 32 <= a.m;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c0 = (2 * i + group) * 32, count = ncols - c0;
                 if (count <= 0) break;
                 if (kSixteen) {
-                    __syncwarp();
-                    rb[lane] = lane < count ? __ldg(a.row_b + n0 + c0 + lane) : 0.0f;
-                    __syncwarp();
+                    const float* rb = sh.row_b[warp - 2][i];
                     const uint64_t by = f2_pack(ra, ra);
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
@@ -557,7 +565,7 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     a.accs = p.bn > 128 ? 1 : 2;
     a.b_bytes = (uint32_t)(p.bn / p.cta * 128);
     a.stage_bytes = kMxPart + a.b_bytes + (uint32_t)((1 + p.cta) * blocks * 512);
-    a.stages = std::min<int>(kMxStages, (int)((kMxSmem - 2048) / a.stage_bytes));
+    a.stages = std::min<int>(kMxStages, (int)((kMxSmem - 1024 - sizeof(MxShared)) / a.stage_bytes));
     const int64_t mtiles = (rows + 128 * p.cta - 1) / (128 * p.cta), ntiles = (batch + p.bn - 1) / p.bn;
     if (mtiles * ntiles * p.splits > 1 << 30) return cudaErrorInvalidValue;
     a.mtiles = (int)mtiles;
