@@ -5,8 +5,8 @@
 //
 // Both are bound by memory.  The backward pass sorts (id, t) first, so that a row's sum runs
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
-// call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and
-// writes the rows whose entries start among them; of rows with more than kLong entries the
+// call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes
+// 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and writes the rows whose entries start among them; of rows with more than kLong entries the
 // pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
 // found by search in the sorted ids and filled with zeros by other blocks of the first: no
 // row of dw is written twice.
@@ -840,7 +840,6 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     const int64_t zero = std::min<int64_t>((items + kEmbedWarps * kZeroRows - 1) / (kEmbedWarps * kZeroRows),
                                            (int64_t)1 << 16);
     const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
-    if (a.sum_blocks + zero > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
     e = launch_early(sum_kernel(wide, dtype == PVS_F32, p.piece), a.sum_blocks + zero, kEmbedThreads, 0, st, a);
     if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
