@@ -6,8 +6,8 @@
 // Both are bound by memory.  The backward pass sorts (id, t) first, so that a row's sum runs
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
 // call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes
-// 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and writes the rows whose entries start among them; of rows with more than kLong entries the
-// pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
+// 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and writes the rows
+// whose entries start among them; of rows with more than kLong entries the pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
 // found by search in the sorted ids and filled with zeros by other blocks of the first: no
 // row of dw is written twice.
 #include <cuda_bf16.h>
@@ -57,14 +57,20 @@ __device__ __forceinline__ void widen_two(uint32_t u, int dtype, float& lo, floa
     }
 }
 __device__ __forceinline__ uint32_t narrow_two(float lo, float hi, int dtype) {
-    return (uint32_t)narrow(lo, dtype) | (uint32_t)narrow(hi, dtype) << 16;
+    if (dtype == PVS_BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 
 // Eight elements of a row, a lane's share of 256: neighbours (WIDE: the row is aligned to 16
 // bytes and holds whole eights; as they lie, four words of 16-bit ones) or 32 apart.  Nothing is
 // read past the row.
-template <bool WIDE, bool F32>
+template <bool WIDE, int DT>
 struct Share {
+    static constexpr bool F32 = DT == PVS_F32;
     uint32_t u[WIDE && !F32 ? 4 : 8];
 
     __device__ __forceinline__ void load(const void* p, int64_t row, int col0, int dim) {
@@ -94,13 +100,13 @@ struct Share {
             }
         }
     }
-    __device__ __forceinline__ void values(int dtype, float (&v)[8]) const {
+    __device__ __forceinline__ void values(float (&v)[8]) const {
         if constexpr (WIDE && !F32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) widen_two(u[i], dtype, v[2 * i], v[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) widen_two(u[i], DT, v[2 * i], v[2 * i + 1]);
         } else {
             // (a bf16 is the upper half of a float32)
-            if (!F32 && dtype == PVS_F16) {
+            if (DT == PVS_F16) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = __half2float(__ushort_as_half((uint16_t)u[i]));
             } else {
@@ -158,7 +164,7 @@ struct LookupArgs {
 
 // A warp takes kLookups neighbouring pieces of 256 columns of y, their loads in flight together.
 constexpr int kLookups = 4;
-template <bool WIDE, bool F32>
+template <bool WIDE, int DT>
 __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const LookupArgs a) {
     next_early();
     wait_before();
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const Look
     if (p0 >= pieces) return;
     int64_t row[kLookups], id[kLookups];
     int col0[kLookups];
-    Share<WIDE, F32> in[kLookups];
+    Share<WIDE, DT> in[kLookups];
     row[0] = p0 / a.slabs;
     col0[0] = (int)(p0 - row[0] * a.slabs) * kSlab;
 #pragma unroll
@@ -191,11 +197,11 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const Look
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = f;
         } else {
-            in[i].values(a.dtype, v);
+            in[i].values(v);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= a.scale;
         }
-        store_share<WIDE>(a.y, a.dtype, row[i] * a.ldy, col0[i], a.dim, v);
+        store_share<WIDE>(a.y, DT, row[i] * a.ldy, col0[i], a.dim, v);
     }
 }
 
@@ -455,7 +461,7 @@ __device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t n, 
     return lo;
 }
 
-template <bool WIDE>
+template <bool WIDE, int DT>
 __device__ void zero_rows(const SumArgs& a, int64_t first) {
     const int lane = threadIdx.x & 31;
     const int64_t v = first + lane;
@@ -468,12 +474,12 @@ __device__ void zero_rows(const SumArgs& a, int64_t first) {
     for (uint32_t rows = __ballot_sync(0xffffffffu, empty); rows != 0; rows &= rows - 1) {
         const int64_t row = first + __ffs(rows) - 1;
         for (int c = 0; c < a.dim; c += kSlab)
-            store_share<WIDE>(a.dw, a.dtype, row * a.lddw, c, a.dim, zeros);
+            store_share<WIDE>(a.dw, DT, row * a.lddw, c, a.dim, zeros);
     }
 }
 
 // A warp's sums over 32 columns of entries that lie in windows of 32 lanes.
-template <bool WIDE>
+template <bool WIDE, int DT>
 struct Sum {
     const SumArgs& a;
     int col0;
@@ -487,7 +493,7 @@ struct Sum {
     __device__ __forceinline__ void row(uint32_t key) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[k] *= a.scale;
-        store_share<WIDE>(a.dw, a.dtype, (int64_t)key * a.lddw, col0, a.dim, acc);
+        store_share<WIDE>(a.dw, DT, (int64_t)key * a.lddw, col0, a.dim, acc);
         clear();
     }
     __device__ __forceinline__ void piece(int64_t slot) {
@@ -498,8 +504,8 @@ struct Sum {
 constexpr int kFlight = 8;           // rows whose loads are under way at once
 
 // kPiece sorted entries to a warp, and 256 columns.
-template <bool WIDE, bool F32, int kPiece>
-__global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
+template <bool WIDE, int DT, int kPiece>
+__global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -509,7 +515,7 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum
     if ((b + 1) * a.sum_blocks / blocks == sums_before) {
         const int64_t step = (blocks - a.sum_blocks) * kEmbedWarps * kZeroRows;
         for (int64_t v = ((b - sums_before) * kEmbedWarps + warp) * kZeroRows; v < a.items; v += step)
-            zero_rows<WIDE>(a, v);
+            zero_rows<WIDE, DT>(a, v);
         return;
     }
     const int64_t u = sums_before * kEmbedWarps + warp;
@@ -557,9 +563,9 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum
         if (!tail_part) last = kPiece + after;
         if (tail_part && lane == 0 && col0 == 0) a.longs[1 + atomicAdd(a.longs, 1u)] = (uint32_t)piece;
     }
-    Sum<WIDE> sum(a, col0);
+    Sum<WIDE, DT> sum(a, col0);
     for (int i0 = first; i0 < last; i0 += kFlight) {
-        Share<WIDE, F32> in[kFlight];
+        Share<WIDE, DT> in[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int at = i0 + i;
@@ -572,7 +578,7 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && !F32 ? 3 : 2) embed_sum
             const int at = i0 + i;
             if (at >= last) break;
             float v[8];
-            in[i].values(a.dtype, v);
+            in[i].values(v);
 #pragma unroll
             for (int c = 0; c < 8; ++c) sum.acc[c] += v[c];
             if (at + 1 == last) break;
@@ -698,13 +704,16 @@ pvs_status embed_ended(cudaError_t e) {
     return PVS_ERR_CUDA;
 }
 
+using LookupKernel = void (*)(const LookupArgs);
 using SumKernel = void (*)(const SumArgs);
-SumKernel sum_kernel(bool wide, bool f32, int piece) {
-    if (piece == 8)
-        return wide ? (f32 ? embed_sum_kernel<true, true, 8> : embed_sum_kernel<true, false, 8>)
-                    : (f32 ? embed_sum_kernel<false, true, 8> : embed_sum_kernel<false, false, 8>);
-    return wide ? (f32 ? embed_sum_kernel<true, true, 32> : embed_sum_kernel<true, false, 32>)
-                : (f32 ? embed_sum_kernel<false, true, 32> : embed_sum_kernel<false, false, 32>);
+template <int DT>
+LookupKernel lookup_kernel(bool wide) {
+    return wide ? embed_forward_kernel<true, DT> : embed_forward_kernel<false, DT>;
+}
+template <int DT>
+SumKernel sum_kernel(bool wide, int piece) {
+    if (piece == 8) return wide ? embed_sum_kernel<true, DT, 8> : embed_sum_kernel<false, DT, 8>;
+    return wide ? embed_sum_kernel<true, DT, 32> : embed_sum_kernel<false, DT, 32>;
 }
 
 // The sorted entries' place in the plan's buffers.
@@ -783,10 +792,9 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     const int64_t blocks = (rows * a.slabs + kEmbedWarps * kLookups - 1) / (kEmbedWarps * kLookups);
     if (blocks > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
-    return embed_ended(launch_early(dtype == PVS_F32 ? (wide ? embed_forward_kernel<true, true>
-                                                             : embed_forward_kernel<false, true>)
-                                                     : (wide ? embed_forward_kernel<true, false>
-                                                             : embed_forward_kernel<false, false>),
+    return embed_ended(launch_early(dtype == PVS_F32   ? lookup_kernel<PVS_F32>(wide)
+                                    : dtype == PVS_F16 ? lookup_kernel<PVS_F16>(wide)
+                                                       : lookup_kernel<PVS_BF16>(wide),
                                     blocks, kEmbedThreads, 0,
                                     static_cast<cudaStream_t>(cuda_stream), a));
 }
@@ -841,7 +849,10 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
                                            (int64_t)1 << 16);
     const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
     count_launches(1);
-    e = launch_early(sum_kernel(wide, dtype == PVS_F32, p.piece), a.sum_blocks + zero, kEmbedThreads, 0, st, a);
+    e = launch_early(dtype == PVS_F32   ? sum_kernel<PVS_F32>(wide, p.piece)
+                     : dtype == PVS_F16 ? sum_kernel<PVS_F16>(wide, p.piece)
+                                        : sum_kernel<PVS_BF16>(wide, p.piece),
+                     a.sum_blocks + zero, kEmbedThreads, 0, st, a);
     if (e != cudaSuccess || p.pieces < 2) return embed_ended(e);
     if (rows <= kLong) return PVS_OK;            // (no run is long)
     const int slabs = (int)((p.ldp + 4 * kJoinLanes - 1) / (4 * kJoinLanes));

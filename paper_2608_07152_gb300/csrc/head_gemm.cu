@@ -103,6 +103,10 @@ __device__ __forceinline__ void raise_abort(Shared& sh, int* status, int crank) 
 __device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
     return mbar_test_wait(bar, parity) || (limit_ns != 0 && mbar_wait(bar, parity, limit_ns));
 }
+// The same by a whole warp, so that what follows is uniform.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
+    return __all_sync(0xffffffffu, ring_wait(bar, parity, limit_ns));
+}
 // A wait at a role's end, with the 2 s limit, given up in a millisecond where another role has
 // given up (what it waits for may then never come).
 template <int kCta>
@@ -427,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t* stages = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
     Shared& sh = *reinterpret_cast<Shared*>(stages + R::kStages * R::kStageBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int crank = kCta == 2 ? (int)cluster_ctarank() : 0;
     const bool leader = crank == 0;
     Units w(a, blockIdx.x / kCta, gridDim.x / kCta);
@@ -456,34 +460,39 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
     __syncthreads();
     if (kCta == 2) cluster_barrier();   // both CTAs' barriers and TMEM are ready
     tc::fence_after_sync();
-    const uint32_t tmem = sh.tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);
     next_early();
     wait_before();
 
+    // The producer's and the issuer's loops are run by whole warps, one lane of which issues: their
+    // addresses and descriptors then stay in uniform registers, where the instructions want them.
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            uint32_t g = 0;
-            const bool alt = p.alt_flag && *p.alt_flag;
-            const int bhalf = p.bn / kCta;
-            const Producer make(p, alt, kCta);
-            for (; w.left > 0 && !abort_set(sh); w.next()) {
-                const int am = p.a_mo + (w.mt * kCta + crank) * kTileM;
-                const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn + crank * bhalf;
-                const int bk = alt ? p.alt_ko : p.b_ko;
-                for (int q = 0; q < a.npairs && !abort_set(sh); ++q) {
-                    const int pa = a.pa[q], pb = a.pb[q];
-                    for (int kc = w.k0; kc < w.k1; ++kc, ++g) {
-                        const int s = g % R::kStages;
-                        if (!ring_wait(&sh.empty[s], ((g / R::kStages) & 1u) ^ 1u, a.wait_ns)) {
-                            raise_abort<kCta>(sh, a.status, crank);
-                            break;
-                        }
-                        make.fill<kCta>(stages + s * R::kStageBytes, &sh.full[s], leader, am,
+        const bool one = tc::elect_one();
+        uint32_t g = 0;
+        Turn at;
+        bool go = true;
+        const bool alt = p.alt_flag && *p.alt_flag;
+        const int bhalf = p.bn / kCta;
+        const Producer make(p, alt, kCta);
+        for (; go && w.left > 0; w.next()) {
+            if (__any_sync(0xffffffffu, abort_set(sh))) break;
+            const int am = p.a_mo + (w.mt * kCta + crank) * kTileM;
+            const int bnc = (alt ? p.alt_no : p.b_no) + w.nt * p.bn + crank * bhalf;
+            const int bk = alt ? p.alt_ko : p.b_ko;
+            for (int q = 0; go && q < a.npairs; ++q) {
+                const int pa = a.pa[q], pb = a.pb[q];
+                for (int kc = w.k0; kc < w.k1; ++kc, ++g, at.next(R::kStages)) {
+                    go = warp_wait(&sh.empty[at.stage], at.parity ^ 1u, a.wait_ns);
+                    if (!go) break;
+                    if (one)
+                        make.fill<kCta>(stages + at.stage * R::kStageBytes, &sh.full[at.stage], leader, am,
                                         p.a_ko + kc * kTileK, pa, bnc, bk + kc * kTileK, pb);
-                    }
                 }
             }
+        }
+        if (one) {
+            if (!go) raise_abort<kCta>(sh, a.status, crank);
             sh.fills = g;
             // the MMAs have consumed the last fill of every stage used: no copy into
             // this CTA and no commit to its barriers is still in flight when it ends
@@ -492,74 +501,80 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
                 last_wait<kCta>(&sh.empty[s], (last / R::kStages) & 1u, sh, a.status, crank);
             }
         }
+        __syncwarp();
     } else if (warp == 1) {
         // ---------------- MMA issuer (the even CTA of a pair) ----------------
-        if (lane == 0 && leader) {
+        if (leader) {
+            const bool one = tc::elect_one();
             const uint32_t idesc = (a.f16 ? tc::idesc_f16_f32(kTileM * kCta, p.bn)
                                           : tc::idesc_bf16_f32(kTileM * kCta, p.bn)) |
                                    ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16);
             // the first stage's descriptors, and their steps of 16 of k (32 bytes, or two
-            // atoms): one thread issues every MMA, and has 128 cycles for each
+            // atoms): the upper halves do not change, the address is in the lower ones
             const uint32_t s0 = smem_u32(stages);
             const uint64_t a0 = p.a_mn ? smem_desc_sw128_mn(s0) : tc::smem_desc_sw128_kmajor(s0);
             const uint64_t b0 = p.b_mn ? smem_desc_sw128_mn(s0 + kStageA)
                                        : tc::smem_desc_sw128_kmajor(s0 + kStageA);
-            const uint64_t astep = p.a_mn ? 128 : 2, bstep = p.b_mn ? 128 : 2;
+            const uint32_t a_hi = (uint32_t)(a0 >> 32), b_hi = (uint32_t)(b0 >> 32);
+            auto desc = [](uint32_t hi, uint32_t lo) { return (uint64_t)hi << 32 | lo; };
+            const uint32_t astep = p.a_mn ? 128 : 2, bstep = p.b_mn ? 128 : 2;
             uint32_t g = 0;
             int it = 0;
-            for (; w.left > 0 && !abort_set(sh); w.next(), ++it) {
+            Turn at;
+            bool go = true;
+            for (; w.left > 0; w.next(), ++it) {
                 const int b = it & 1;
-                if (!ring_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, a.wait_ns)) {
-                    raise_abort<kCta>(sh, a.status, crank);
-                    break;
-                }
+                if (__any_sync(0xffffffffu, abort_set(sh))) break;
+                go = warp_wait(&sh.tempty[b], ((uint32_t)(it >> 1) & 1u) ^ 1u, a.wait_ns);
+                if (!go) break;
                 tc::fence_after_sync();
                 const uint32_t d = tmem + (uint32_t)(b * kTileN);
-                uint32_t acc = 0;
                 const int chunks = a.npairs * (w.k1 - w.k0);
                 int in_k = w.k0;
                 const bool tail = w.k1 == p.kchunks && p.ktail < kTileK / 16;
-                for (int kc = 0; kc < chunks; ++kc, ++g) {
-                    const int s = g % R::kStages;
-                    if (!ring_wait(&sh.full[s], (g / R::kStages) & 1u, a.wait_ns)) {
-                        raise_abort<kCta>(sh, a.status, crank);
-                        break;
-                    }
+                for (int kc = 0; kc < chunks; ++kc, ++g, at.next(R::kStages)) {
+                    go = warp_wait(&sh.full[at.stage], at.parity, a.wait_ns);
+                    if (!go) break;
                     tc::fence_after_sync();
-                    const uint32_t off = (uint32_t)(s * R::kStageBytes) >> 4;
-                    uint64_t ad = a0 + off, bd = b0 + off;
+                    const uint32_t off = at.stage * (uint32_t)(R::kStageBytes >> 4);
+                    const uint32_t al = (uint32_t)a0 + off, bl = (uint32_t)b0 + off;
                     if (++in_k == w.k1) in_k = w.k0;
-                    if (tail && in_k == w.k0) {
-                        // the last chunk's steps past k multiply zeros: left out
-                        for (int k = 0; k < p.ktail; ++k, ad += astep, bd += bstep) {
-                            mma<kCta>(d, ad, bd, idesc, acc);
-                            acc = 1;
-                        }
-                    } else {
+                    // the last chunk's steps past k multiply zeros: left out
+                    const int steps = tail && in_k == w.k0 ? p.ktail : kTileK / 16;
+                    if (one) {
 #pragma unroll
-                        for (int k = 0; k < kTileK / 16; ++k, ad += astep, bd += bstep) {
-                            mma<kCta>(d, ad, bd, idesc, acc);
-                            acc = 1;
+                        for (int k = 0; k < kTileK / 16; ++k) {
+                            if (k >= steps) break;
+                            mma<kCta>(d, desc(a_hi, al + k * astep), desc(b_hi, bl + k * bstep), idesc,
+                                      k > 0 || kc > 0 ? 1u : 0u);
                         }
+                        if (kCta == 2)
+                            tc::commit_pair(&sh.empty[at.stage]);   // the stage is free in both CTAs
+                        else
+                            tc::commit(&sh.empty[at.stage]);
                     }
-                    if (kCta == 2)
-                        tc::commit_pair(&sh.empty[s]);   // the stage is free in both CTAs
-                    else
-                        tc::commit(&sh.empty[s]);
+                    __syncwarp();
                 }
-                if (abort_set(sh)) break;
-                if (kCta == 2)
-                    tc::commit_pair(&sh.tfull[b]);
-                else
-                    tc::commit(&sh.tfull[b]);
+                if (!go) break;
+                if (one) {
+                    if (kCta == 2)
+                        tc::commit_pair(&sh.tfull[b]);
+                    else
+                        tc::commit(&sh.tfull[b]);
+                }
+                __syncwarp();
             }
-            sh.chunks = g;
-            sh.tiles = it;
-            // TMEM is released after the last unit's MMAs
-            if (it > 0) {
-                const int lb = (it - 1) & 1;
-                last_wait<kCta>(&sh.tfull[lb], (uint32_t)((it - 1) >> 1) & 1u, sh, a.status, crank);
+            if (one) {
+                if (!go) raise_abort<kCta>(sh, a.status, crank);
+                sh.chunks = g;
+                sh.tiles = it;
+                // TMEM is released after the last unit's MMAs
+                if (it > 0) {
+                    const int lb = (it - 1) & 1;
+                    last_wait<kCta>(&sh.tfull[lb], (uint32_t)((it - 1) >> 1) & 1u, sh, a.status, crank);
+                }
             }
+            __syncwarp();
         }
     } else {
         // ---------------- epilogue ----------------

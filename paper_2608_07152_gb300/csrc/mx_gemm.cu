@@ -79,17 +79,6 @@ struct MxShared {
 
 constexpr size_t kMxSmem = 227 * 1024;
 
-// A place in the ring of stages, and the parity of its turn.
-struct Turn {
-    uint32_t stage = 0, parity = 0;
-    __device__ __forceinline__ void next(int stages) {
-        if (++stage == (uint32_t)stages) {
-            stage = 0;
-            parity ^= 1u;
-        }
-    }
-};
-
 // A unit: a tile over a range of chunks.
 struct MxUnit {
     int mt, nt, split, k0, k1;

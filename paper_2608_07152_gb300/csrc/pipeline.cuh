@@ -75,6 +75,17 @@ __device__ inline bool mbar_wait(uint64_t* bar, uint32_t parity,
     }
 }
 
+// A place in the ring of stages, and the parity of its turn.
+struct Turn {
+    uint32_t stage = 0, parity = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++stage == (uint32_t)stages) {
+            stage = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
 // ---- thread-block clusters ----------------------------------------------------
 __device__ inline uint32_t cluster_ctarank() {
     uint32_t r;
