@@ -162,10 +162,13 @@ struct LookupArgs {
     int slabs;
 };
 
-// A warp takes kLookups neighbouring pieces of 256 columns of y, their loads in flight together.
-constexpr int kLookups = 4;
+// A warp takes neighbouring pieces of 256 columns of y, their loads in flight together: four of
+// aligned rows, one of others (whose eight loads a lane are single elements: 200,000 rows of 385 in
+// float32 took 110 us with four).
+__host__ __device__ constexpr int lookups(bool wide) { return wide ? 4 : 1; }
 template <bool WIDE, int DT>
 __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const LookupArgs a) {
+    constexpr int kLookups = lookups(WIDE);
     next_early();
     wait_before();
     const int64_t pieces = a.rows * a.slabs;
@@ -184,10 +187,12 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const Look
     }
 #pragma unroll
     for (int i = 0; i < kLookups; ++i) id[i] = row[i] < a.rows ? __ldg(a.ids + row[i]) : a.ignore_index;
+    // (no branches, so that all loads are under way at once: the table's first row for no row)
 #pragma unroll
-    for (int i = 0; i < kLookups; ++i)
-        if (id[i] != a.ignore_index && id[i] >= 0 && id[i] < a.items)
-            in[i].load(a.w, id[i] * a.ldw, col0[i], a.dim);
+    for (int i = 0; i < kLookups; ++i) {
+        const bool there = id[i] != a.ignore_index && id[i] >= 0 && id[i] < a.items;
+        in[i].load(a.w, there ? id[i] * a.ldw : 0, col0[i], a.dim);
+    }
 #pragma unroll
     for (int i = 0; i < kLookups; ++i) {
         if (row[i] >= a.rows) break;
@@ -789,7 +794,8 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     a.ldy = ldy;
     a.slabs = (dim + kSlab - 1) / kSlab;
     const bool wide = dim % 8 == 0 && on_16(w, ldw, dtype) && on_16(y, ldy, dtype);
-    const int64_t blocks = (rows * a.slabs + kEmbedWarps * kLookups - 1) / (kEmbedWarps * kLookups);
+    const int64_t per_block = kEmbedWarps * lookups(wide);
+    const int64_t blocks = (rows * a.slabs + per_block - 1) / per_block;
     if (blocks > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
     return embed_ended(launch_early(dtype == PVS_F32   ? lookup_kernel<PVS_F32>(wide)
