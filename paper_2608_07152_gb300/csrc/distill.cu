@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
     const pvs_xent_args& a = j.r.a;
     const int lane = threadIdx.x & 31, top = j.r.top, quads = (top + kDots - 1) / kDots;
     const int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t row = u / quads;
+    const int64_t row = quotient_of(u, quads);
     if (row >= a.rows) return;
     const int k0 = (int)(u - row * quads) * kDots;
     int id[kDots];
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(256) top_scatter_kernel(const TopScatter a) {
     const int64_t id = a.ids[i] - a.v0;
     const float hit = a.hits[i];
     if (id < 0 || id >= a.n || hit == kNoHit) return;
-    const int64_t row = i / a.top;
+    const int64_t row = quotient_of(i, a.top);
     float v = a.grad[row] * (a.up ? *a.up : 1.0f) * hit;
     if (a.few) {
         a.few[id * a.few_rows + row] = v;

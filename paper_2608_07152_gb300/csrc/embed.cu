@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const Look
     int64_t row[kLookups], id[kLookups];
     int col0[kLookups];
     Share<WIDE, DT> in[kLookups];
-    row[0] = p0 / a.slabs;
+    row[0] = quotient_of(p0, a.slabs);
     col0[0] = (int)(p0 - row[0] * a.slabs) * kSlab;
 #pragma unroll
     for (int i = 1; i < kLookups; ++i) {
@@ -514,17 +514,20 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) 
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // blocks that sum and blocks that write zeros take turns, so that reads and writes overlap
-    const int64_t b = blockIdx.x, blocks = gridDim.x;
-    const int64_t sums_before = b * a.sum_blocks / blocks;
-    if ((b + 1) * a.sum_blocks / blocks == sums_before) {
-        const int64_t step = (blocks - a.sum_blocks) * kEmbedWarps * kZeroRows;
-        for (int64_t v = ((b - sums_before) * kEmbedWarps + warp) * kZeroRows; v < a.items; v += step)
+    // blocks that sum and blocks that write zeros take turns, so that reads and writes overlap, as
+    // long as there are both
+    const int64_t b = blockIdx.x, zero_blocks = gridDim.x - a.sum_blocks;
+    const int64_t turns = min(a.sum_blocks, zero_blocks);
+    const bool sums = b < 2 * turns ? (b & 1) == 0 : a.sum_blocks > turns;
+    const int64_t of_kind = b < 2 * turns ? b >> 1 : b - turns;
+    if (!sums) {
+        const int64_t step = zero_blocks * kEmbedWarps * kZeroRows;
+        for (int64_t v = (of_kind * kEmbedWarps + warp) * kZeroRows; v < a.items; v += step)
             zero_rows<WIDE, DT>(a, v);
         return;
     }
-    const int64_t u = sums_before * kEmbedWarps + warp;
-    const int64_t piece = u / a.slabs;
+    const int64_t u = of_kind * kEmbedWarps + warp;
+    const int64_t piece = quotient_of(u, a.slabs);
     if (piece >= a.pieces) return;
     const int col0 = (int)(u - piece * a.slabs) * kSlab;
     const int64_t base = piece * kPiece;

@@ -5,6 +5,7 @@
 // takes eight neighbours, so that a group of 16 is two lanes and one of 32 four.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cuda_fp4.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -201,8 +202,8 @@ __device__ __forceinline__ void pack_eight(const Eight<DT>& in, bool here, uint3
 
 // Blocks to an SM, which set how many loads are in flight: 16,384 rows of 4,096 in bf16, in groups
 // of 16, took 55 us with the registers that the compiler takes by itself, 36 with four blocks, 42
-// with six; in groups of 32 30, 30 and 28.
-constexpr int pack_blocks(bool sixteen, int dtype) { return dtype == PVS_F32 ? 3 : sixteen ? 4 : 6; }
+// with six; in groups of 32 30, 30 and 28; in float32 and groups of 16 72 with two, 51 with four.
+constexpr int pack_blocks(bool sixteen, int dtype) { return dtype == PVS_F32 || sixteen ? 4 : 6; }
 
 // A block takes kPackWarps / kWarps rows at a time, kWarps warps to a row, each 1,024 columns in
 // registers (again from memory where a row is longer than all of them hold).
@@ -312,6 +313,7 @@ __device__ __forceinline__ uint16_t mx_narrow(float v, int dtype) {
 
 // What codes stand for: eight a thread where rows of `out` are aligned, else one, so that
 // neighbours write neighbours.
+constexpr int kUnpack = 4;
 template <bool kSixteen, bool WIDE>
 __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* __restrict__ codes,
                                                                  const uint8_t* __restrict__ scales,
@@ -342,16 +344,30 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
         }
         return;
     }
-    const int pieces = (cols + 7) / 8;
-    const int64_t total = rows * pieces, step = (int64_t)gridDim.x * kPackThreads;
-    for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < total; i += step) {
-        const int64_t row = i / pieces;
-        const int c = (int)(i - row * pieces) * 8;
+    // a warp takes neighbouring pieces of 256 columns
+    const int lane = threadIdx.x & 31, slabs = (cols + 255) / 256;
+    const int64_t total = rows * slabs, p0 = ((int64_t)blockIdx.x * kPackWarps + (threadIdx.x >> 5)) * kUnpack;
+    int64_t row = quotient_of(p0, slabs);
+    int c = (int)(p0 - row * slabs) * 256 + 8 * lane;
+#pragma unroll
+    for (int i = 0; i < kUnpack; ++i, c += 256) {
+        if (p0 + i >= total) return;
+        if (c - 8 * lane >= cols) {
+            ++row;
+            c = 8 * lane;
+        }
+        if (c >= cols) continue;
         const uint32_t word = __ldg(reinterpret_cast<const uint32_t*>(codes + row * (kp / 2) + c / 2));
         const float unit = unit_of<kSixteen>(scale_at(row, c), kSixteen ? __ldg(row_scales + row) : 1.0f);
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = value_of(word >> (4 * k) & 15u) * unit;
+        for (int k = 0; k < 4; ++k) {
+            const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(word >> (8 * k)), __NV_E2M1);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            v[2 * k] = f.x;
+            v[2 * k + 1] = f.y;
+        }
+        times(v, unit);
         const int64_t at = row * ldout + c;
         if (dtype == PVS_F32) {
             float* o = static_cast<float*>(out) + at;
@@ -442,13 +458,13 @@ extern "C" pvs_status pvs_mx_unpack(const uint8_t* codes, const uint8_t* scales,
     const pvs_status before = (pvs_status)ready(&dev);
     if (before != PVS_OK) return before;
     const bool w = mx_wide(out, ldout, dtype);
-    const int64_t blocks = w ? (rows * ((cols + 7) / 8) + kPackThreads - 1) / kPackThreads
-                             : (rows + kPackWarps - 1) / kPackWarps;
-    const int64_t grid = std::min<int64_t>(blocks, 1 << 20);
+    const int64_t per_block = kPackWarps * (w ? kUnpack : 1);
+    const int64_t blocks = (rows * (w ? (cols + 255) / 256 : 1) + per_block - 1) / per_block;
+    if (blocks > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
     return mx_queued(launch_early(
         group == 16 ? (w ? mx_unpack_kernel<true, true> : mx_unpack_kernel<true, false>)
                     : (w ? mx_unpack_kernel<false, true> : mx_unpack_kernel<false, false>),
-        grid, kPackThreads, 0, static_cast<cudaStream_t>(cuda_stream), codes, scales, row_scales, rows, cols,
+        blocks, kPackThreads, 0, static_cast<cudaStream_t>(cuda_stream), codes, scales, row_scales, rows, cols,
         mx_padded(cols), out, ldout, dtype));
 }
