@@ -4,12 +4,16 @@
  *
  * The index of pvs.h holds vectors that a learned head makes of an encoder's
  * hidden rows.  These operators train such a head against the items of a
- * collection and serve it for single queries:
+ * collection and serve it for single queries and for many:
  *   - softmax cross entropy of rows over the items (a large vocabulary), in
  *     pieces of the vocabulary, without keeping the logits, and its gradients;
  *   - rows kept in 8 bits between the forward and the backward pass, by the
  *     per-vector quantizer of Sec. 2.3.1, and the backward steps that read them;
- *   - products of a few rows with weights kept in 4 bits, with group scales.
+ *   - distillation: the same softmax against a teacher's distribution over a list of
+ *     items of each row, and its gradients;
+ *   - rows of a table by their ids, scaled, and the table's gradient;
+ *   - products of a few rows with weights kept in 4 bits, with group scales, and of any
+ *     number of rows with both operands in microscaled 4-bit floating point.
  * The paper has no counterpart to them.
  *
  * Conventions:

@@ -10,6 +10,11 @@
 // whose entries start among them; of rows with more than kLong entries the pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
 // found by search in the sorted ids and filled with zeros by other blocks of the first: no
 // row of dw is written twice.
+//
+// 131,072 ids after Zipf's law in 200,000 rows of 1,024, bf16 (36,000 rows of them named), in us: lookup 66
+// (5.1 TB/s of 342 MB; issue 64%), sorting 33 in six launches, sums and zeros 114 (6.0 TB/s of 678
+// MB), long runs 15.  (All runs that cross a piece joined by the second launch: it took 300.)
+// 5,000 in 10,007 of 385, float32: lookup 7, sorting 15, sums 19, long runs 8: latency.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

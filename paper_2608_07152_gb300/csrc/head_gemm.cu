@@ -8,13 +8,14 @@
 // serve the products of 128 rows or fewer, which memory bounds (a loss of 100 rows over
 // 500,000 items of 768: 125 us, in pairs 132; of 256 rows 140 in pairs, 155 in lone CTAs).
 //
-// 8,192 rows over 8,192 items of 768 in bf16: statistics 69 us (1.50 PFLOP/s, tensor
-// pipe 70% busy), G 111 us (43%: two parts of 134 MB are stored), dx and dw 287 us (two
-// products each, 1.44 PFLOP/s, 78%).  What is lost beside is the last, half empty, of 14 rounds of
-// tiles, and with short k the epilogue.
+// 8,192 rows over 8,192 items of 768 in bf16: statistics 56 us (1.84 PFLOP/s, tensor
+// pipe 87% busy), G 98 us (49%: two parts of 134 MB are stored), dx and dw 241 us (two
+// products each, 1.71 PFLOP/s, 96%).  What is lost beside is the last, half empty, of 14 rounds of
+// tiles.  (With lone lanes that issued, and moved each operand to where the instructions
+// take it: 69, 117 and 287 us, 70%, 43% and 78%.)
 //   warp 0     TMA producer (both CTAs): chunks of A (128 x 64) and B into a ring,
 //              128-byte swizzle, the pair's bytes counted on the even CTA's barrier;
-//   warp 1     one thread (of the even CTA) issues the MMAs (M = 128 or 256, N = bn,
+//   warp 1     (of the even CTA) issues the MMAs (M = 128 or 256, N = bn,
 //              K = 16, four to a chunk) into one of two TMEM accumulators;
 //   warps 2-9  epilogue (both CTAs): a TMEM lane (a row of D) per thread; the two
 //              warps that share a lane quarter take every other chunk of 32 columns.

@@ -282,7 +282,9 @@ inline int even_splits(int64_t kchunks, int64_t want) {
 
 // What a unit of `chunks` chunks takes, in the time of a chunk's MMAs: 1.3 times its
 // chunks and 7 more (10 where it leaves float32 sums for splits), as dw's tiles of 1, 4 and
-// 16 chunks did (64, 256 and 1024 rows over a million items: 8, 10.5 and 27).
+// 16 chunks did (64, 256 and 1024 rows over a million items: 8, 10.5 and 27) while lone lanes
+// issued the MMAs.  With 1.05 or 1.15 in 1.3's place, nearer to a chunk now, the plans of twelve
+// steps of all types took the same times to 2%.
 inline double unit_cost(int64_t chunks, bool sums) { return 1.3 * (double)chunks + (sums ? 10 : 7); }
 // And for the whole launch: a split tile's store and its later read, and the launch
 // that adds the splits.

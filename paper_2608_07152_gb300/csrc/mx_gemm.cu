@@ -17,7 +17,15 @@
 //   warps 2-9  epilogue: each takes every other 32 columns of its quarter of the lanes into
 //              registers, hands the accumulator back, and stores.
 // Many rows of x go to CTA pairs (cta_group::2, 256 x 256 tiles): each CTA holds 128 rows of
-// weights and half of the tile's rows of x, and the scales of all of them.
+// weights and half of the tile's rows of x, and the scales of all of them.  Their accumulator is
+// one (two and the scales are more than TMEM): it is handed back when its columns are in
+// registers, before they are stored.
+//
+// 16,384 rows by 4,096 x 4,096 in bf16, groups of 16: 94 us (5.8 PFLOP/s, tensor pipe 67%), of 32 86 (6.3,
+// 72%), with 8,192 of k 157 and 146 (7.5, 85%): about 490 cycles a chunk, and beside the mainloop some
+// 4,000 a tile for the stores that it does not hide.  32 rows by 1,000,000 x 768, groups of 32: 73 us,
+// 6.4 TB/s.  (With lone lanes that issue, a chunk took 1,000 cycles; with a branch at each store
+// the first took 440 us.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -11,8 +11,11 @@
 // Every logit costs 2 d operations in the forward pass and 10 d in the backward
 // pass: bound by the tensor cores unless there are few rows, when w (and dw) bound
 // it.  G of a piece is written once and read twice, in two parts, each a product of its
-// own.  With both gradients, bf16: 8,192 rows over 8,192 items of 768 0.49 ms, 256 rows over
-// 1,000,000 items 2.2 ms; f16: 4,096 rows over 200,000 items of 1,024 7.2 ms.
+// own.  With both gradients, bf16: 8,192 rows over 8,192 items of 768 0.43 ms, 256 rows over
+// 1,000,000 items 2.0 ms; f16: 4,096 rows over 200,000 items of 1,024 6.5 ms.
+//
+// Distillation (at the end) is the same with a list of items and shares in each row's target's
+// place; distill.cu has what it adds.
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -215,7 +218,8 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
 // items, in three bf16 parts (six products).
 // 16-bit operands: G has two parts, so that a gradient's error is the rounding of its
 // output (bf16 1.7e-3, f16 2.1e-4).  One part would lose as much again (bf16 2.3e-3 to 2.7e-3)
-// and take two thirds of the time: a step of 8,192 rows over 8,192 items of 768 485 us, 302 with
+// and take two thirds of the time (both measured with the slower issue that head_gemm.cu tells
+// of): a step of 8,192 rows over 8,192 items of 768 485 us, 302 with
 // one part; of 256 over a million 2,230 and 1,520.
 struct Plan {
     int parts = 1, f16 = 0;     // of the gradients' operands

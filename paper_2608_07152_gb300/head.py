@@ -1,8 +1,9 @@
 """Training and serving of the head that makes an index's vectors.
 
-The binding of ``include/head.h``: softmax cross entropy over a collection's items
-and its gradients, rows kept in 8 bits with the backward steps that read them,
-and products with 4-bit weights.  Operands are CUDA ``torch`` tensors of one
+The binding of ``include/head.h``: softmax cross entropy over a collection's items and
+distillation from a teacher's lists of them, with their gradients, table lookups and the
+table's gradient, rows kept in 8 bits with the backward steps that read them, and
+products with 4-bit weights and of microscaled 4-bit rows.  Operands are CUDA ``torch`` tensors of one
 device, whose rows may be strided; work is queued on torch's current stream of
 that device, outputs and scratch come from torch's allocator on that stream,
 and nothing waits for the GPU.  A tensor made on another stream is the caller's
