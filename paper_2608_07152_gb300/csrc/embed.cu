@@ -39,7 +39,6 @@ constexpr int kKeysPerThread = 4;
 constexpr int kSortTile = kEmbedThreads * kKeysPerThread;
 constexpr int kSlab = 256;           // columns to a warp
 constexpr int kLong = 32;            // entries of a run that one warp adds, at most
-constexpr int kZeroRows = 32;        // rows that a warp searches at once
 
 __device__ __forceinline__ uint16_t narrow(float v, int dtype) {
     if (dtype == PVS_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
@@ -453,6 +452,8 @@ struct SumArgs {
     float* part;                     // [piece][2][ldp]: of a long run from before, and one that starts
     int64_t ldp;
     int64_t pieces, sum_blocks;
+    int zero_rows;                   // table rows to a warp, a multiple of 32
+    int lane_bits;                   // lanes to a row of zeros: 2^this
     uint32_t* longs;                 // [0] how many pieces a long run starts in, then which
 };
 
@@ -471,20 +472,54 @@ __device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t n, 
     return lo;
 }
 
+// Zeros to those of `rows` (a bit each) of the 32 table rows from v0 that are set: as many rows at
+// once as the warp's lanes hold.
+template <bool WIDE, int DT>
+__device__ __forceinline__ void put_zeros(const SumArgs& a, int64_t v0, uint32_t rows) {
+    constexpr int kStep = WIDE ? 8 : 1;                    // elements a lane
+    const int lane = threadIdx.x & 31, shift = a.lane_bits;
+    const int in = lane >> shift, first = (lane & ((1 << shift) - 1)) * kStep, step = kStep << shift;
+    for (int r = in; r < 32; r += 32 >> shift) {
+        if (!(rows >> r & 1u)) continue;
+        const int64_t at = (v0 + r) * a.lddw;
+        for (int c = first; c < a.dim; c += step) {
+            if constexpr (!WIDE) {
+                if constexpr (DT == PVS_F32)
+                    static_cast<float*>(a.dw)[at + c] = 0.0f;
+                else
+                    static_cast<uint16_t*>(a.dw)[at + c] = 0;
+            } else if constexpr (DT == PVS_F32) {
+                float4* q = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at + c);
+                q[0] = q[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            } else {
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.dw) + at + c) = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+    }
+}
+
+// The rows without an entry of a.zero_rows table rows, 32 at a time.  The lanes search for the
+// groups' first entries at once; a group of few entries shows its rows in one load, one of many is
+// searched row by row.
 template <bool WIDE, int DT>
 __device__ void zero_rows(const SumArgs& a, int64_t first) {
     const int lane = threadIdx.x & 31;
-    const int64_t v = first + lane;
-    bool empty = false;
-    if (v < a.items) {
-        const int64_t at = lower_bound(a.keys, a.n, (uint32_t)v);
-        empty = at >= a.n || __ldg(a.keys + at) != (uint32_t)v;
-    }
-    const float zeros[8] = {};
-    for (uint32_t rows = __ballot_sync(0xffffffffu, empty); rows != 0; rows &= rows - 1) {
-        const int64_t row = first + __ffs(rows) - 1;
-        for (int c = 0; c < a.dim; c += kSlab)
-            store_share<WIDE>(a.dw, DT, row * a.lddw, c, a.dim, zeros);
+    const int64_t end = min(first + a.zero_rows, a.items);
+    const int64_t bound = lower_bound(a.keys, a.n, (uint32_t)min(first + 32 * lane, end));
+    for (int g = 0; first + 32 * g < end; ++g) {
+        const int64_t v0 = first + 32 * g;
+        const int64_t lo = __shfl_sync(0xffffffffu, bound, g), hi = __shfl_sync(0xffffffffu, bound, g + 1);
+        uint32_t used;
+        if (hi - lo <= 32) {
+            const bool in = lo + lane < hi;
+            used = __reduce_or_sync(0xffffffffu, in ? 1u << (__ldg(a.keys + lo + lane) - (uint32_t)v0) : 0u);
+        } else {
+            const uint32_t row = (uint32_t)v0 + lane;
+            const int64_t at = lo + lower_bound(a.keys + lo, hi - lo, row);
+            used = __ballot_sync(0xffffffffu, at < hi && __ldg(a.keys + at) == row);
+        }
+        const int here = (int)min((int64_t)32, end - v0);
+        put_zeros<WIDE, DT>(a, v0, ~used & (here == 32 ? 0xffffffffu : (1u << here) - 1u));
     }
 }
 
@@ -526,8 +561,8 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) 
     const bool sums = b < 2 * turns ? (b & 1) == 0 : a.sum_blocks > turns;
     const int64_t of_kind = b < 2 * turns ? b >> 1 : b - turns;
     if (!sums) {
-        const int64_t step = zero_blocks * kEmbedWarps * kZeroRows;
-        for (int64_t v = (of_kind * kEmbedWarps + warp) * kZeroRows; v < a.items; v += step)
+        const int64_t step = zero_blocks * kEmbedWarps * a.zero_rows;
+        for (int64_t v = (of_kind * kEmbedWarps + warp) * a.zero_rows; v < a.items; v += step)
             zero_rows<WIDE, DT>(a, v);
         return;
     }
@@ -859,9 +894,12 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     a.pieces = p.pieces;
     a.longs = p.longs;
     a.sum_blocks = (p.pieces * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
-    const int64_t zero = std::min<int64_t>((items + kEmbedWarps * kZeroRows - 1) / (kEmbedWarps * kZeroRows),
-                                           (int64_t)1 << 16);
     const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
+    // 32 to 256 rows a warp, so that there are warps for every SM
+    a.zero_rows = 32 * (int)std::min<int64_t>(8, std::max<int64_t>(1, items / (32 * 16 * (int64_t)dev.sms)));
+    while (a.lane_bits < 5 && (wide ? 8 : 1) << a.lane_bits < dim) ++a.lane_bits;
+    const int64_t zero = std::min<int64_t>((items + kEmbedWarps * a.zero_rows - 1) / (kEmbedWarps * a.zero_rows),
+                                           (int64_t)1 << 20);
     count_launches(1);
     e = launch_early(dtype == PVS_F32   ? sum_kernel<PVS_F32>(wide, p.piece)
                      : dtype == PVS_F16 ? sum_kernel<PVS_F16>(wide, p.piece)
