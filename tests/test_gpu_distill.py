@@ -232,6 +232,42 @@ def test_masked_items_may_hold_anything(T, dtype):
         close(a, b, t)
 
 
+@pytest.mark.parametrize("T", [5, 50])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_biases_of_the_lowest_value(T, dtype):
+    # a mask by the type's lowest value: those items have no share, and lists without them keep their loss
+    case = make(T, 300, 64, 6, dtype)
+    case["bias"] = torch.zeros(300, device="cuda")
+    case["bias"][200:] = torch.finfo(F32).min
+    case["ids"] %= 200
+    got = step(**case)
+    hidden = dict(case, bias=case["bias"].clone())
+    hidden["bias"][200:] = -INF
+    for a, b, t in zip(got, *reference(**hidden)):
+        close(a, b, t)
+
+
+@pytest.mark.parametrize("limit_first", [True, False])
+def test_a_wait_that_runs_out(limit_first):
+    case = make(300, 20_000, 512, 8, BF16)
+    want = step(**case)
+    loss, stats, hits = pvs.pvs_distill_forward(case["x"], case["w"], case["ids"], case["z"], scale=case["scale"],
+                                                teacher_scale=case["c"])
+    torch.cuda.synchronize()
+    pvs.pvs_head_set_wait_limit(0)
+    try:
+        if limit_first:
+            pvs.pvs_distill_forward(case["x"], case["w"], case["ids"], case["z"])
+        else:
+            pvs.pvs_distill_backward(case["x"], case["w"], case["ids"], stats, hits, case["grad"])
+        torch.cuda.synchronize()
+        with pytest.raises(pvs.PvsError):
+            pvs.pvs_head_status()
+    finally:
+        pvs.pvs_head_set_wait_limit(2_000_000_000)
+    assert all(torch.equal(a, b) for a, b in zip(want, step(**case)))
+
+
 def test_nan_and_infinite_teacher():
     case = make(40, 300, 32, 5, BF16)
     case["z"][2, 1] = float("nan")
