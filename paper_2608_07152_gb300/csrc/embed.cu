@@ -523,7 +523,7 @@ __device__ void zero_rows(const SumArgs& a, int64_t first) {
     }
 }
 
-// A warp's sums over 32 columns of entries that lie in windows of 32 lanes.
+// A lane's sums over eight of a warp's 256 columns, and where they go.
 template <bool WIDE, int DT>
 struct Sum {
     const SumArgs& a;
