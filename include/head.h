@@ -160,7 +160,7 @@ typedef struct pvs_distill_args {
 } pvs_distill_args;
 
 /* Bytes of scratch of the two calls, as pvs_xent_workspace; forward, 10 more for each slot and 2
- * for each row and 256 items of a block of rows; backward, 8 more for each row. */
+ * for each row and 256 items of a block of rows. */
 pvs_status pvs_distill_workspace(const pvs_distill_args* args, int32_t backward, size_t* bytes);
 
 /* loss [rows], stats [rows x 4] (16-byte aligned) and hits [rows x top], all float32.  stats

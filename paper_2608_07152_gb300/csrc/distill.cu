@@ -3,7 +3,8 @@
 //   p_k  = exp(c z_k) / sum_i exp(c z_i)           over the slots of a row's list
 //   loss = sum_k p_k (ln p_k - l_k + lse),  G_j = g (q_j - sum_{k: id_k = j} p_k)
 //
-//   forward    lists, each row's ids in ascending order; their logits, float32 products of
+//   forward    lists, each row's ids in ascending order; their logits (of few rows in the
+//              same launch), float32 products of
 //              their own (the tensor cores cut each step's sum, and the teacher's items have
 //              the largest logits); the product over all items, whose epilogue leaves the
 //              listed ones out of the tiles' statistics; and the join, which adds them
@@ -14,7 +15,7 @@
 // Beside the products this costs `top` scattered rows of w a row forward, and `top` sectors of
 // each part of G backward.  4,096 rows over 8,192 items of 768 in bf16, lists of 64, in us: lists 13,
 // their logits 47 (403 MB of rows, out of the L2: 8.5 TB/s), the product 38 (as without lists), join 12;
-// flags, rows and copy 12, G 54, listed entries 11, both gradients 137.  2,048 over 200,000 of 1,024
+// rows and copy 8, G 54, listed entries 11, both gradients 137.  2,048 over 200,000 of 1,024
 // in f16, lists of 128: 24, 64 (537 MB), 490, 20; backward 2,700.  (Logits within the joining launch,
 // 32 rows of w in flight an SM, took it to 100 and 294.)
 #include <cuda_bf16.h>
@@ -48,72 +49,6 @@ __device__ __forceinline__ float teacher_logit(const TopRows& r, int64_t at, int
     return element(r.logits, r.dtype, at) * r.teacher_scale;
 }
 
-// ---- lists ---------------------------------------------------------------------------
-// A bitonic network of (id, slot) over the next power of two, 2^bits; a block takes whole rows.
-__global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int bits, int rows_bits) {
-    __shared__ unsigned long long keys[kMaxTop];
-    next_early();
-    wait_before();
-    const TopRows& r = a.r;
-    const int padded = 1 << bits, rows_here = 1 << rows_bits;
-    const int64_t row0 = (int64_t)blockIdx.x << rows_bits;
-    const int total = 1 << (bits + rows_bits);
-    for (int i = threadIdx.x; i < total; i += blockDim.x) {
-        const int64_t row = row0 + (i >> bits);
-        const int k = i & (padded - 1);
-        unsigned long long key = (unsigned long long)INT_MAX << 32 | 0xffffffffu;
-        if (row < r.a.rows && k < r.top) {
-            const int64_t id = r.ids[row * r.top + k];
-            key = (unsigned long long)INT_MAX << 32 | (uint32_t)k;
-            if (id >= 0 && id < r.a.items && teacher_logit(r, row * r.top + k, id) != -INFINITY)
-                key = (unsigned long long)id << 32 | (uint32_t)k;
-        }
-        keys[i] = key;
-    }
-    for (int k = 1; k <= bits; ++k) {
-        for (int j = k - 1; j >= 0; --j) {
-            __syncthreads();
-            for (int t = threadIdx.x; t < total / 2; t += blockDim.x) {
-                const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1)), l = i + (1 << j);
-                const unsigned long long x = keys[i], y = keys[l];
-                if ((x > y) == ((i & (padded - 1) & (1 << k)) == 0)) {
-                    keys[i] = y;
-                    keys[l] = x;
-                }
-            }
-        }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < total; i += blockDim.x) {
-        const int64_t row = row0 + (i >> bits);
-        const int k = i & (padded - 1);
-        if (row < r.a.rows && k < r.top) {
-            a.list[row * r.top + k] = (int)(keys[i] >> 32);
-            a.slot[row * r.top + k] = (uint16_t)keys[i];
-        }
-    }
-    // where each tile of items begins in each row's list: the row first, so that neighbours write
-    // neighbours
-    const int in = threadIdx.x & (rows_here - 1);
-    const int64_t row = row0 + in;
-    if (row >= r.a.rows) return;
-    const unsigned long long* mine = keys + (in << bits);
-    uint16_t* out = a.first + row;
-    for (int q = threadIdx.x >> rows_bits; q < a.tiles; q += blockDim.x >> rows_bits) {
-        const int piece = q / a.piece_tiles;
-        const int64_t start = piece * a.piece + (int64_t)(q - piece * a.piece_tiles) * a.tile;
-        const unsigned long long from = (unsigned long long)start << 32;
-        int lo = 0;
-        for (int n = r.top; n > 0;) {
-            const int half = n >> 1;
-            const bool right = mine[lo + half] < from;
-            lo = right ? lo + half + 1 : lo;
-            n = right ? n - half - 1 : half;
-        }
-        out[q * r.a.rows] = (uint16_t)lo;
-    }
-}
-
 // ---- logits of the listed items ----------------------------------------------------------
 constexpr int kDots = 4;                 // of a warp at once, their loads in flight together
 
@@ -141,23 +76,12 @@ __device__ __forceinline__ float raw_value(uint32_t u, int dtype) {
     return dtype == PVS_BF16 ? __uint_as_float(u << 16) : __half2float(__ushort_as_half((uint16_t)u));
 }
 
-// Bound by the rows of w, `top` for each row of x.  KIND 0: 16-bit rows of whole, aligned eights;
-// 1: other 16-bit rows; 2: float32.
+// A warp's: the logits of entries k0 .. k0 + 3 of a row's list.  KIND 0: 16-bit rows of whole, aligned
+// eights; 1: other 16-bit rows; 2: float32.
 template <int KIND>
-__global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
-    next_early();
-    wait_before();
+__device__ __forceinline__ void top_dots(const TopDots& j, int64_t row, int k0, const int (&id)[kDots]) {
     const pvs_xent_args& a = j.r.a;
-    const int lane = threadIdx.x & 31, top = j.r.top, quads = (top + kDots - 1) / kDots;
-    const int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t row = quotient_of(u, quads);
-    if (row >= a.rows) return;
-    const int k0 = (int)(u - row * quads) * kDots;
-    int id[kDots];
-#pragma unroll
-    for (int i = 0; i < kDots; ++i) {
-        id[i] = k0 + i < top ? __ldg(j.list + row * top + k0 + i) : INT_MAX;
-    }
+    const int lane = threadIdx.x & 31, top = j.r.top;
     if (id[0] == INT_MAX) return;        // (and so are those behind it)
     float lo[kDots] = {}, hi[kDots] = {};
     if constexpr (KIND == 0) {
@@ -203,6 +127,99 @@ __global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
         float b = a.bias ? a.bias[id[i]] : 0.0f;
         if (isfinite(b)) b = fminf(fmaxf(b * kLog2e, -3.402823466e38f), 3.402823466e38f);
         j.dots[row * top + k0 + i] = fmaf(dot, j.k2, b);
+    }
+}
+
+// Bound by the rows of w, `top` for each row of x.
+template <int KIND>
+__global__ void __launch_bounds__(256) top_dots_kernel(const TopDots j) {
+    next_early();
+    wait_before();
+    const int top = j.r.top, quads = (top + kDots - 1) / kDots;
+    const int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t row = quotient_of(u, quads);
+    if (row >= j.r.a.rows) return;
+    const int k0 = (int)(u - row * quads) * kDots;
+    int id[kDots];
+#pragma unroll
+    for (int i = 0; i < kDots; ++i) id[i] = k0 + i < top ? __ldg(j.list + row * top + k0 + i) : INT_MAX;
+    top_dots<KIND>(j, row, k0, id);
+}
+
+// ---- lists ---------------------------------------------------------------------------
+// A bitonic network of (id, slot) over the next power of two, 2^bits; a block takes whole rows, and
+// with a KIND (one row a block then) its logits too.
+template <int KIND>
+__global__ void __launch_bounds__(512) top_lists_kernel(const TopLists a, int bits, int rows_bits,
+                                                        const TopDots dots) {
+    __shared__ unsigned long long keys[kMaxTop];
+    next_early();
+    wait_before();
+    const TopRows& r = a.r;
+    const int padded = 1 << bits, rows_here = 1 << rows_bits;
+    const int64_t row0 = (int64_t)blockIdx.x << rows_bits;
+    const int total = 1 << (bits + rows_bits);
+    for (int i = threadIdx.x; i < total; i += blockDim.x) {
+        const int64_t row = row0 + (i >> bits);
+        const int k = i & (padded - 1);
+        unsigned long long key = (unsigned long long)INT_MAX << 32 | 0xffffffffu;
+        if (row < r.a.rows && k < r.top) {
+            const int64_t id = r.ids[row * r.top + k];
+            key = (unsigned long long)INT_MAX << 32 | (uint32_t)k;
+            if (id >= 0 && id < r.a.items && teacher_logit(r, row * r.top + k, id) != -INFINITY)
+                key = (unsigned long long)id << 32 | (uint32_t)k;
+        }
+        keys[i] = key;
+    }
+    for (int k = 1; k <= bits; ++k) {
+        for (int j = k - 1; j >= 0; --j) {
+            __syncthreads();
+            for (int t = threadIdx.x; t < total / 2; t += blockDim.x) {
+                const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1)), l = i + (1 << j);
+                const unsigned long long x = keys[i], y = keys[l];
+                if ((x > y) == ((i & (padded - 1) & (1 << k)) == 0)) {
+                    keys[i] = y;
+                    keys[l] = x;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < total; i += blockDim.x) {
+        const int64_t row = row0 + (i >> bits);
+        const int k = i & (padded - 1);
+        if (row < r.a.rows && k < r.top) {
+            a.list[row * r.top + k] = (int)(keys[i] >> 32);
+            a.slot[row * r.top + k] = (uint16_t)keys[i];
+        }
+    }
+    if constexpr (KIND >= 0) {
+        for (int k0 = (threadIdx.x >> 5) * kDots; k0 < r.top; k0 += (blockDim.x >> 5) * kDots) {
+            int id[kDots];
+#pragma unroll
+            for (int i = 0; i < kDots; ++i) id[i] = k0 + i < r.top ? (int)(keys[k0 + i] >> 32) : INT_MAX;
+            top_dots<KIND>(dots, row0, k0, id);
+        }
+    }
+    // where each tile of items begins in each row's list: the row first, so that neighbours write
+    // neighbours
+    const int in = threadIdx.x & (rows_here - 1);
+    const int64_t row = row0 + in;
+    if (row >= r.a.rows) return;
+    const unsigned long long* mine = keys + (in << bits);
+    uint16_t* out = a.first + row;
+    for (int q = threadIdx.x >> rows_bits; q < a.tiles; q += blockDim.x >> rows_bits) {
+        const int piece = q / a.piece_tiles;
+        const int64_t start = piece * a.piece + (int64_t)(q - piece * a.piece_tiles) * a.tile;
+        const unsigned long long from = (unsigned long long)start << 32;
+        int lo = 0;
+        for (int n = r.top; n > 0;) {
+            const int half = n >> 1;
+            const bool right = mine[lo + half] < from;
+            lo = right ? lo + half + 1 : lo;
+            n = right ? n - half - 1 : half;
+        }
+        out[q * r.a.rows] = (uint16_t)lo;
     }
 }
 
@@ -335,16 +352,6 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
 }
 
 // ---- backward --------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) top_flags_kernel(const float4* __restrict__ stats, int64_t rows,
-                                                        int64_t* __restrict__ flags) {
-    next_early();
-    wait_before();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows) return;
-    const float4 s = stats[i];
-    flags[i] = s.x == -INFINITY && s.y == 0.0f ? -1 : 0;
-}
-
 __global__ void __launch_bounds__(256) top_scatter_kernel(const TopScatter a) {
     next_early();
     wait_before();
@@ -389,34 +396,36 @@ cudaError_t join_launch(const TopJoin& a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_top_lists(const TopLists& a, cudaStream_t st) {
+cudaError_t launch_top_lists(const TopLists& a, const TopDots& dots, cudaStream_t st) {
     int bits = 1;
     while (1 << bits < a.r.top) ++bits;
     // as many rows a block as 256 threads sort, but a block for every SM first
     int rows_bits = 0;
     while (rows_bits < 5 && bits + rows_bits < 9 && a.r.a.rows >> (rows_bits + 1) >= 256) ++rows_bits;
     const int64_t blocks = ((a.r.a.rows - 1) >> rows_bits) + 1;
+    const int threads = bits == 10 ? 512 : 256;
+    const int kind = a.r.a.dtype == PVS_F32 ? 2 : dots.wide ? 0 : 1;
+    // a short list's logits in the same launch, where that has a block for each row anyway (four
+    // entries a warp at once, and four times at most)
+    const bool together = rows_bits == 0 && a.r.top <= 16 * kDots * 2;
     count_launches(1);
-    return launch_early(top_lists_kernel, blocks, bits == 10 ? 512 : 256, 0, st, a, bits, rows_bits);
-}
-
-cudaError_t launch_top_dots(const TopDots& a, cudaStream_t st) {
+    cudaError_t e = launch_early(!together   ? top_lists_kernel<-1>
+                                 : kind == 0 ? top_lists_kernel<0>
+                                 : kind == 1 ? top_lists_kernel<1>
+                                             : top_lists_kernel<2>,
+                                 blocks, threads, 0, st, a, bits, rows_bits, dots);
+    if (e != cudaSuccess || together) return e;
     const int64_t warps = a.r.a.rows * ((a.r.top + kDots - 1) / kDots);
     if (warps > (int64_t)8 * 0x7fffffff) return cudaErrorInvalidValue;
     count_launches(1);
-    return launch_early(a.r.a.dtype == PVS_F32 ? top_dots_kernel<2> : a.wide ? top_dots_kernel<0> : top_dots_kernel<1>,
-                        (warps + 7) / 8, 256, 0, st, a);
+    return launch_early(kind == 0 ? top_dots_kernel<0> : kind == 1 ? top_dots_kernel<1> : top_dots_kernel<2>,
+                        (warps + 7) / 8, 256, 0, st, dots);
 }
 
 cudaError_t launch_top_join(const TopJoin& a, const Device& dev, cudaStream_t st) {
     // eight rows' statistics share their sectors, where that leaves every SM some blocks
     if (a.r.a.rows >= 4 * dev.sms) return join_launch<8>(a, st);
     return join_launch<1>(a, st);
-}
-
-cudaError_t launch_top_flags(const float4* stats, int64_t rows, int64_t* flags, cudaStream_t st) {
-    count_launches(1);
-    return launch_early(top_flags_kernel, (rows + 255) / 256, 256, 0, st, stats, rows, flags);
 }
 
 cudaError_t launch_top_scatter(const TopScatter& a, cudaStream_t st) {

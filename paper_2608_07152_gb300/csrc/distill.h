@@ -31,7 +31,6 @@ struct TopLists {
     int64_t piece;
     int tile;                            // ... q % piece_tiles * tile
 };
-cudaError_t launch_top_lists(const TopLists& a, cudaStream_t st);
 
 // The student's logits of the listed items, in powers of two: float32 products.
 struct TopDots {
@@ -41,7 +40,8 @@ struct TopDots {
     bool wide;                           // 16-bit rows of whole, aligned eights
     float* dots;                         // [rows][top]
 };
-cudaError_t launch_top_dots(const TopDots& a, cudaStream_t st);
+// Both, in one launch or two.
+cudaError_t launch_top_lists(const TopLists& a, const TopDots& dots, cudaStream_t st);
 
 // A row's loss and what the backward pass wants, from its tiles' statistics: of every item, or
 // (apart) of those that are not listed.
@@ -58,9 +58,6 @@ struct TopJoin {
     float* hits;                         // [rows][top]
 };
 cudaError_t launch_top_join(const TopJoin& a, const Device& dev, cudaStream_t st);
-
-// 0 for a row that has a list, -1 for one that has not, as targets.
-cudaError_t launch_top_flags(const float4* stats, int64_t rows, int64_t* flags, cudaStream_t st);
 
 // G of the listed items of a piece, over what the product wrote there.
 struct TopScatter {

@@ -1015,7 +1015,7 @@ __device__ __forceinline__ void split_rows(const SplitArgs& a, int64_t block, in
             const uint32_t r = (uint32_t)((i * m) >> 40);
             const int64_t row = row0 + r;
             const int col = (int)(i - r * (uint32_t)pieces) * 8;
-            const bool zero = (a.zero_target && a.zero_target[row] == a.ignore_index) ||
+            const bool zero = ignored_row(a.zero_target, a.ignore_index, a.zero_stats, row) ||
                               (a.zero_bias && a.zero_bias[row] == -INFINITY);
             const int64_t at = row * a.ld + col;
             float v[8];
@@ -1168,7 +1168,7 @@ __device__ __forceinline__ void split16_rows(const Split16Args& a, int64_t block
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const int64_t row = min(first + r, s.rows - 1);
-            const bool zero = (s.zero_target && s.zero_target[row] == s.ignore_index) ||
+            const bool zero = ignored_row(s.zero_target, s.ignore_index, s.zero_stats, row) ||
                               (s.zero_bias && s.zero_bias[row] == -INFINITY);
             cols[r] = zero ? 0 : s.cols;          // (a zero row: nothing is read)
         }
@@ -1228,9 +1228,10 @@ __device__ __forceinline__ void prepare_row(const RowArgs& r, int64_t i) {
     if (i == 0) *r.bad_masked = 0;
     if (i >= r.rows) return;
     const float4 st = r.stats[i];
-    const int64_t y = r.targets[i];
+    // (a row that has a list: its logits' entries are not the product's to write)
+    const int64_t y = r.targets ? r.targets[i] : 0;
     GradRow o{0.0f, 0.0f, 0.0f, -1};
-    if (y != r.ignore_index && !(st.x == -INFINITY && st.y == 0.0f)) {
+    if (!(r.targets && y == r.ignore_index) && !(st.x == -INFINITY && st.y == 0.0f)) {
         const float g = r.grad[i] * (r.up ? *r.up : 1.0f);
         o.m = st.x;
         if (y < 0 || y >= r.items) {

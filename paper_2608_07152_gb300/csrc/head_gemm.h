@@ -121,6 +121,16 @@ __device__ __forceinline__ int64_t quotient_of(int64_t n, int d) {
     return n <= 0xffffffffll ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
+// Whether a row has no gradient, whatever it holds: by its target, or (there are none: rows have
+// lists) by its statistics.
+__device__ __forceinline__ bool ignored_row(const int64_t* targets, int64_t ignore_index, const float4* stats,
+                                            int64_t row) {
+    if (targets) return targets[row] == ignore_index;
+    if (!stats) return false;
+    const float4 s = stats[row];
+    return s.x == -INFINITY && s.y == 0.0f;
+}
+
 // Eight 16-bit elements from any element's address, in 4-byte loads: the words that hold
 // them, shifted by half a word where they start in the middle of one.  Reads up to one
 // element before them and one after, within the words of the first and the last.
@@ -203,6 +213,7 @@ struct SplitArgs {
     const float* row_scale;
     const int64_t* zero_target;
     int64_t ignore_index;
+    const float4* zero_stats;    // without zero_target: of the forward pass
     const float* zero_bias;
     const int* only_if;
     uint16_t* dst;
@@ -229,7 +240,7 @@ struct Split16Args {
 struct RowArgs {
     const float4* stats;
     const float* grad;
-    const int64_t* targets;
+    const int64_t* targets;      // null: rows have lists
     int64_t rows, items, ignore_index;
     const float* up;             // f16: the power of two of every gradient, or null
     GradRow* out;                // null: no rows

@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs j) {
 // inverse.  One block: a row's weight is 12 bytes of the thousands that it costs.
 __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __restrict__ grad,
                                                                const int64_t* __restrict__ targets,
+                                                               const float4* __restrict__ stats,
                                                                int64_t ignore_index, int64_t rows,
                                                                float* up) {
     next_early();
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(1024) xent_grad_scale_kernel(const float* __re
     float v = 0.0f;
     for (int64_t i = threadIdx.x; i < rows; i += 1024) {
         const float g = fabsf(grad[i]);
-        if (targets[i] != ignore_index && isfinite(g)) v = fmaxf(v, g);
+        if (!ignored_row(targets, ignore_index, stats, i) && isfinite(g)) v = fmaxf(v, g);
     }
     v = warp_max(v);
     if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = v;
@@ -244,11 +245,10 @@ struct Plan {
     GradRow* row = nullptr;
     unsigned int* words = nullptr;   // [0] up, [1] its inverse, [2] bad masked
     float *xslots = nullptr, *wslots = nullptr;
-    // distillation: the rows' lists, and which rows have one
+    // distillation: the rows' lists
     int* list = nullptr;
     uint16_t *list_slot = nullptr, *list_first = nullptr;
     float* list_dots = nullptr;
-    int64_t* flags = nullptr;
     size_t bytes = 0;
 };
 
@@ -321,15 +321,11 @@ bool few_rows(const pvs_xent_args& a) {
 
 // The lists of a distillation's rows (top 0: there are none).
 void plan_lists(Plan& p, const pvs_xent_args& a, bool backward, int top, Carver& c) {
-    if (top == 0) return;
-    if (backward) {
-        p.flags = c.take<int64_t>(a.rows);
-    } else {
-        p.list = c.take<int>(a.rows * top);
-        p.list_slot = c.take<uint16_t>(a.rows * top);
-        p.list_dots = c.take<float>(a.rows * top);
-        if (!p.few) p.list_first = c.take<uint16_t>(p.pieces * p.piece_tiles * a.rows);
-    }
+    if (top == 0 || backward) return;
+    p.list = c.take<int>(a.rows * top);
+    p.list_slot = c.take<uint16_t>(a.rows * top);
+    p.list_dots = c.take<float>(a.rows * top);
+    if (!p.few) p.list_first = c.take<uint16_t>(p.pieces * p.piece_tiles * a.rows);
 }
 
 Plan plan_of(const pvs_xent_args& a, bool backward, const Device& dev, void* workspace, int top = 0) {
@@ -483,14 +479,17 @@ SplitArgs split_of(const pvs_xent_args& a, const Plan& p) {
 
 // The copy of x (backward: without the rows that have no gradient, whatever they hold:
 // it must not meet G's zeros), and that of the items [v0, v0 + n) without masked ones.
-Split16Args rows_copy(const pvs_xent_args& a, const Plan& p, bool zero_ignored) {
+Split16Args rows_copy(const pvs_xent_args& a, const Plan& p, bool zero_ignored, const float* stats = nullptr) {
     SplitArgs s = split_of(a, p);
     s.src = a.x;
     s.ld = a.ldx;
     s.rows = a.rows;
     s.dst = p.x;
     s.part_stride = a.rows * p.ldp;
-    if (zero_ignored) s.zero_target = a.targets;
+    if (zero_ignored) {
+        s.zero_target = a.targets;
+        s.zero_stats = reinterpret_cast<const float4*>(stats);
+    }
     return Split16Args{s, p.x16, a.rows * p.ldp, p.xunit};
 }
 Split16Args items_copy(const pvs_xent_args& a, const Plan& p, int64_t v0, int64_t n) {
@@ -540,9 +539,8 @@ cudaError_t forward(const pvs_xent_args& a, const Plan& p, const Device& dev, fl
     if (top) {
         const TopLists l{*top, p.list, p.list_slot, p.list_first, p.few ? 0 : (int)tiles, (int)p.piece_tiles,
                          p.piece, p.bnl};
-        e = launch_top_lists(l, st);
         const TopDots d{*top, p.list, a.scale * kLog2e, wide, p.list_dots};
-        if (e == cudaSuccess) e = launch_top_dots(d, st);
+        e = launch_top_lists(l, d, st);
         if (e != cudaSuccess) return e;
     }
     if (p.few) {
@@ -620,8 +618,8 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
     cudaError_t e = cudaSuccess;
     if (p.f16) {
         count_launches(1);
-        e = launch_early(xent_grad_scale_kernel, 1, 1024, 0, st, grad_loss, a.targets, a.ignore_index,
-                         T, up);
+        e = launch_early(xent_grad_scale_kernel, 1, 1024, 0, st, grad_loss, a.targets,
+                         reinterpret_cast<const float4*>(stats), a.ignore_index, T, up);
     }
     if (p.few) {
         PrepareArgs c{};
@@ -635,6 +633,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
             f.item0 = v0;
             if (a.bias) f.bias += v0;
             f.row = p.row;
+            f.stats = reinterpret_cast<const float4*>(stats);
             f.g = p.few_g;
             f.slots = dx ? p.xslots : nullptr;
             f.slot_stride = T * p.lds;
@@ -660,7 +659,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         const Matrix copied{p.w, n, a.dim, p.ldp, p.parts, p.piece * p.ldp};
         PrepareArgs c{};
         if (i == 0) {
-            c.copy[0] = rows_copy(a, p, true);
+            c.copy[0] = rows_copy(a, p, true, stats);
             c.rows = RowArgs{reinterpret_cast<const float4*>(stats), grad_loss, a.targets, T, V,
                              a.ignore_index, p.f16 ? up : nullptr, p.row, bad_masked};
         }
@@ -901,11 +900,6 @@ extern "C" pvs_status pvs_distill_backward(const pvs_distill_args* a, const floa
     if (before != PVS_OK) return before;
     if (!dx && !dw) return PVS_OK;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    // rows without a list take the part of ignored ones
-    cudaError_t e = launch_top_flags(reinterpret_cast<const float4*>(stats), s.rows, p.flags, st);
-    s.targets = p.flags;
-    s.ignore_index = -1;
     const TopGrad top{a->ids, hits, a->top};
-    if (e == cudaSuccess) e = backward(s, p, dev, stats, grad_loss, dx, lddx, dw, lddw, st, &top);
-    return ended(e);
+    return ended(backward(s, p, dev, stats, grad_loss, dx, lddx, dw, lddw, st, &top));
 }

@@ -60,7 +60,7 @@ __device__ __forceinline__ void fill_rows(const FewArgs& a, float* xs, int r, bo
     for (int i = threadIdx.x; i < r * dp; i += blockDim.x) {
         const int t = i / dp, k = i - t * dp;
         float v = 0.0f;
-        if (t < a.rows && k < a.dim && !(zero_ignored && a.targets[t] == a.ignore_index))
+        if (t < a.rows && k < a.dim && !(zero_ignored && ignored_row(a.targets, a.ignore_index, a.stats, t)))
             v = a.x[t * a.ldx + k];
         xs[i] = v;
     }
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kMostThreads, 1) few_columns_kernel(const FewA
     uint64_t x[R], dx[R];
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-        const bool row = t < a.rows && a.targets[t] != a.ignore_index;
+        const bool row = t < a.rows && !ignored_row(a.targets, a.ignore_index, a.stats, t);
         const float* p = a.x + t * a.ldx;
         x[t] = f2_pack(row && in0 ? p[k0] : 0.0f, row && in1 ? p[k1] : 0.0f);
         dx[t] = f2_pack(0.0f, 0.0f);

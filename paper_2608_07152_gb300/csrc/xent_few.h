@@ -25,6 +25,7 @@ struct FewArgs {
     int64_t part_rows;
     // the backward pass
     const GradRow* row;
+    const float4* stats;          // of the forward pass, for rows without targets
     float* g;                     // [items][few_rows_padded(rows)]
     float* slots;                 // sums of dx, [block][rows, ldslot], or null
     int64_t slot_stride, ldslot;

@@ -146,6 +146,12 @@ def test_several_pieces_of_the_vocabulary(dtype):
     check(make(8192, 33_001, 24, 40, dtype, masked=0.1, empty=0.1))
 
 
+@pytest.mark.parametrize("T", [3, 40])
+def test_several_pieces_of_copied_items(T):
+    # float32 items are copied 1 GB at a time: three pieces of the forward pass (few rows: one)
+    check(make(T, 400_000, 1000, 24, F32, masked=0.05, empty=0.1))
+
+
 def test_several_blocks_of_rows():
     # 8 bytes of statistics for each row and 256 items: two blocks of the forward pass
     case = make(2100, 16_900_000, 8, 5, BF16, empty=0.1)
