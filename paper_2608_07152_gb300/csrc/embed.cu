@@ -14,7 +14,7 @@
 // 131,072 ids after Zipf's law in 200,000 rows of 1,024, bf16 (36,000 rows of them named), in us: lookup 66
 // (5.1 TB/s of 342 MB; issue 64%), sorting 33 in six launches, sums and zeros 114 (6.0 TB/s of 678
 // MB), long runs 15.  (All runs that cross a piece joined by the second launch: it took 300.)
-// 5,000 in 10,007 of 385, float32: lookup 7, sorting 15, sums 19, long runs 8: latency.
+// 5,000 in 10,007 of 385, float32: the gradient 30 in a graph (sorting 10, sums 13, long runs 6), latency.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -453,6 +453,7 @@ struct SumArgs {
     int64_t ldp;
     int64_t pieces, sum_blocks;
     int zero_rows;                   // table rows to a warp, a multiple of 32
+    int zero_bits;                   // 2^this warps share them, 0 to 3
     int lane_bits;                   // lanes to a row of zeros: 2^this
     uint32_t* longs;                 // [0] how many pieces a long run starts in, then which
 };
@@ -482,17 +483,24 @@ __device__ __forceinline__ void put_zeros(const SumArgs& a, int64_t v0, uint32_t
     for (int r = in; r < 32; r += 32 >> shift) {
         if (!(rows >> r & 1u)) continue;
         const int64_t at = (v0 + r) * a.lddw;
-        for (int c = first; c < a.dim; c += step) {
-            if constexpr (!WIDE) {
-                if constexpr (DT == PVS_F32)
+        if constexpr (!WIDE && DT != PVS_F32) {
+            // words of two elements, and an element before or after them
+            uint16_t* p = static_cast<uint16_t*>(a.dw) + at;
+            const int head = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1u), words = (a.dim - head) / 2;
+            uint32_t* q = reinterpret_cast<uint32_t*>(p + head);
+            for (int c = first; c < words; c += step) q[c] = 0;
+            if (first == 0 && head) p[0] = 0;
+            if (first == 0 && (a.dim - head) % 2) p[a.dim - 1] = 0;
+        } else {
+            for (int c = first; c < a.dim; c += step) {
+                if constexpr (!WIDE) {
                     static_cast<float*>(a.dw)[at + c] = 0.0f;
-                else
-                    static_cast<uint16_t*>(a.dw)[at + c] = 0;
-            } else if constexpr (DT == PVS_F32) {
-                float4* q = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at + c);
-                q[0] = q[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            } else {
-                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.dw) + at + c) = make_uint4(0u, 0u, 0u, 0u);
+                } else if constexpr (DT == PVS_F32) {
+                    float4* q = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at + c);
+                    q[0] = q[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                } else {
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.dw) + at + c) = make_uint4(0u, 0u, 0u, 0u);
+                }
             }
         }
     }
@@ -502,7 +510,7 @@ __device__ __forceinline__ void put_zeros(const SumArgs& a, int64_t v0, uint32_t
 // groups' first entries at once; a group of few entries shows its rows in one load, one of many is
 // searched row by row.
 template <bool WIDE, int DT>
-__device__ void zero_rows(const SumArgs& a, int64_t first) {
+__device__ void zero_rows(const SumArgs& a, int64_t first, uint32_t mine) {
     const int lane = threadIdx.x & 31;
     const int64_t end = min(first + a.zero_rows, a.items);
     const int64_t bound = lower_bound(a.keys, a.n, (uint32_t)min(first + 32 * lane, end));
@@ -519,7 +527,7 @@ __device__ void zero_rows(const SumArgs& a, int64_t first) {
             used = __ballot_sync(0xffffffffu, at < hi && __ldg(a.keys + at) == row);
         }
         const int here = (int)min((int64_t)32, end - v0);
-        put_zeros<WIDE, DT>(a, v0, ~used & (here == 32 ? 0xffffffffu : (1u << here) - 1u));
+        put_zeros<WIDE, DT>(a, v0, mine & ~used & (here == 32 ? 0xffffffffu : (1u << here) - 1u));
     }
 }
 
@@ -546,11 +554,9 @@ struct Sum {
         clear();
     }
 };
-constexpr int kFlight = 8;           // rows whose loads are under way at once
-
 // kPiece sorted entries to a warp, and 256 columns.
 template <bool WIDE, int DT, int kPiece>
-__global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
+__global__ void __launch_bounds__(kEmbedThreads, kPiece == 8 ? 1 : WIDE && DT != PVS_F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -561,9 +567,14 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) 
     const bool sums = b < 2 * turns ? (b & 1) == 0 : a.sum_blocks > turns;
     const int64_t of_kind = b < 2 * turns ? b >> 1 : b - turns;
     if (!sums) {
-        const int64_t step = zero_blocks * kEmbedWarps * a.zero_rows;
-        for (int64_t v = (of_kind * kEmbedWarps + warp) * a.zero_rows; v < a.items; v += step)
-            zero_rows<WIDE, DT>(a, v);
+        // (2^zero_bits warps share the rows of a group)
+        const int64_t w = of_kind * kEmbedWarps + warp, step = (zero_blocks * kEmbedWarps >> a.zero_bits) * a.zero_rows;
+        const uint32_t mine = (a.zero_bits == 0   ? 0xffffffffu
+                               : a.zero_bits == 1 ? 0x55555555u
+                               : a.zero_bits == 2 ? 0x11111111u
+                                                  : 0x01010101u)
+                              << (w & ((1 << a.zero_bits) - 1));
+        for (int64_t v = (w >> a.zero_bits) * a.zero_rows; v < a.items; v += step) zero_rows<WIDE, DT>(a, v, mine);
         return;
     }
     const int64_t u = of_kind * kEmbedWarps + warp;
@@ -582,6 +593,7 @@ __global__ void __launch_bounds__(kEmbedThreads, WIDE && DT != PVS_F32 ? 3 : 2) 
         if (w >= 1) place[w - 1] = i < a.n ? __ldg(a.places + i) : 0u;
     }
     // entries without a row come last
+    constexpr int kFlight = kPiece == 8 ? 16 : 8;    // rows whose loads are under way at once
     constexpr uint32_t kHere = kPiece == 32 ? 0xffffffffu : (1u << (kPiece & 31)) - 1u;
     const int count = __popc(__ballot_sync(0xffffffffu, k[1] != none) & kHere);
     if (count == 0) return;
@@ -895,11 +907,13 @@ extern "C" pvs_status pvs_embed_backward(const void* dy, int64_t lddy, const int
     a.longs = p.longs;
     a.sum_blocks = (p.pieces * a.slabs + kEmbedWarps - 1) / kEmbedWarps;
     const bool wide = dim % 8 == 0 && on_16(dy, lddy, dtype) && on_16(dw, lddw, dtype);
-    // 32 to 256 rows a warp, so that there are warps for every SM
-    a.zero_rows = 32 * (int)std::min<int64_t>(8, std::max<int64_t>(1, items / (32 * 16 * (int64_t)dev.sms)));
+    // 32 to 256 rows a warp, or up to eight warps to 32 rows, so that there are warps for every SM
+    const int64_t groups = (items + 31) / 32, enough = 16ll * dev.sms;
+    a.zero_rows = 32 * (int)std::min<int64_t>(8, std::max<int64_t>(1, groups / enough));
+    while (a.zero_bits < 3 && groups << (a.zero_bits + 1) <= enough) ++a.zero_bits;
     while (a.lane_bits < 5 && (wide ? 8 : 1) << a.lane_bits < dim) ++a.lane_bits;
-    const int64_t zero = std::min<int64_t>((items + kEmbedWarps * a.zero_rows - 1) / (kEmbedWarps * a.zero_rows),
-                                           (int64_t)1 << 20);
+    const int64_t units = ((items + a.zero_rows - 1) / a.zero_rows) << a.zero_bits;
+    const int64_t zero = std::min<int64_t>((units + kEmbedWarps - 1) / kEmbedWarps, (int64_t)1 << 20);
     count_launches(1);
     e = launch_early(dtype == PVS_F32   ? sum_kernel<PVS_F32>(wide, p.piece)
                      : dtype == PVS_F16 ? sum_kernel<PVS_F16>(wide, p.piece)

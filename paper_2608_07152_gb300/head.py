@@ -15,6 +15,7 @@ wrong shapes and types raise ``ValueError`` and ``TypeError``.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 PVS_BF16 = 0
 PVS_F16 = 1
@@ -251,6 +252,32 @@ def _list(x, name: str, rows: int):
     return x.contiguous()
 
 
+# What an operator wants of scratch follows from a call's sizes and alignments alone, and asking for it
+# costs a small call a tenth of its time: the last few thousand answers are kept.
+def _asked(name: str, *args) -> int:
+    n = ctypes.c_size_t()
+    _check(getattr(_lib, name)(*args, ctypes.byref(n)), name)
+    return n.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _distill_bytes(device: int, backward: int, x_fits: bool, w_fits: bool, bias: bool, rows: int, items: int,
+                   ldx: int, ldw: int, dim: int, dtype: int, top: int) -> int:
+    at = 1 << 20              # a pointer that nothing reads, and one that is on its elements alone
+    off = at + (4 if dtype == PVS_F32 else 2)
+    s = pvs_xent_args(at if x_fits else off, at if w_fits else off, None, at if bias else None, rows, items,
+                      ldx, ldw, 0, dim, dtype, 1.0, 0)
+    a = pvs_distill_args(s, at, None, top, PVS_F32, 1.0, 0)
+    return _asked("pvs_distill_workspace", ctypes.byref(a), backward)
+
+
+def _distill_scratch(a, device: int, backward: int):
+    s = a.student
+    n = _distill_bytes(device, backward, s.x % 16 == 0 if s.x else True, s.w % 16 == 0, bool(s.bias), s.rows,
+                       s.items, s.ldx, s.ldw, s.dim, s.dtype, a.top)
+    return _workspace(n, device), n
+
+
 def _distill_args(x, w, ids, logits, bias, scale, teacher_scale, ignore_index):
     device = _on_gpu(x, w, ids, logits, bias)
     x, ldx = _matrix(x, "x")
@@ -298,11 +325,9 @@ def pvs_distill_forward(x, w, ids, logits, bias=None, scale: float = 1.0,
     loss = torch.empty(rows, dtype=torch.float32, device=device)
     stats = torch.empty(rows, 4, dtype=torch.float32, device=device)
     hits = torch.empty(rows, a.top, dtype=torch.float32, device=device)
-    n = ctypes.c_size_t()
-    _check(_lib.pvs_distill_workspace(ctypes.byref(a), 0, ctypes.byref(n)), "pvs_distill_workspace")
-    ws = _workspace(n.value, device)
-    _check(_lib.pvs_distill_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(hits), _ptr(ws),
-                                    n.value, _stream(device)), "pvs_distill_forward")
+    ws, n = _distill_scratch(a, device, 0)
+    _check(_lib.pvs_distill_forward(ctypes.byref(a), _ptr(loss), _ptr(stats), _ptr(hits), _ptr(ws), n,
+                                    _stream(device)), "pvs_distill_forward")
     return loss, stats, hits
 
 
@@ -327,12 +352,10 @@ def pvs_distill_backward(x, w, ids, stats, hits, grad_loss, bias=None, scale: fl
     grad_loss = _vector(grad_loss, "grad_loss", s.rows, torch.float32)
     dx = torch.empty(s.rows, s.dim, dtype=x.dtype, device=device) if need_x else None
     dw = torch.empty(s.items, s.dim, dtype=x.dtype, device=device) if need_w else None
-    n = ctypes.c_size_t()
-    _check(_lib.pvs_distill_workspace(ctypes.byref(a), 1, ctypes.byref(n)), "pvs_distill_workspace")
-    ws = _workspace(n.value, device)
+    ws, n = _distill_scratch(a, device, 1)
     _check(_lib.pvs_distill_backward(ctypes.byref(a), _ptr(stats), _ptr(hits), _ptr(grad_loss),
-                                     _ptr(dx), s.dim, _ptr(dw), s.dim, _ptr(ws), n.value,
-                                     _stream(device)), "pvs_distill_backward")
+                                     _ptr(dx), s.dim, _ptr(dw), s.dim, _ptr(ws), n, _stream(device)),
+           "pvs_distill_backward")
     return dx, dw
 
 
@@ -533,6 +556,11 @@ def pvs_embed_forward(w, ids, scale: float = 1.0, ignore_index: int = -100):
     return y
 
 
+@functools.lru_cache(maxsize=4096)
+def _embed_bytes(rows: int, items: int, dim: int) -> int:
+    return _asked("pvs_embed_workspace", rows, items, dim)
+
+
 def pvs_embed_backward(dy, ids, items: int, scale: float = 1.0, ignore_index: int = -100):
     """The gradient [items, d] of a table from the gradient dy [T, d] of the rows that
     ``pvs_embed_forward`` took from it, in dy's type."""
@@ -549,12 +577,11 @@ def pvs_embed_backward(dy, ids, items: int, scale: float = 1.0, ignore_index: in
         raise ValueError(f"items must be in [1, {_MAX_ROWS}]")
     scale = _finite(scale)
     dw = torch.empty(items, dim, dtype=dy.dtype, device=device)
-    n = ctypes.c_size_t()
-    _check(_lib.pvs_embed_workspace(rows, items, dim, ctypes.byref(n)), "pvs_embed_workspace")
-    ws = _workspace(n.value, device)
+    n = _embed_bytes(rows, items, dim)
+    ws = _workspace(n, device)
     _check(_lib.pvs_embed_backward(_ptr(dy), lddy, _ptr(ids), rows, items, dim, dt, scale,
-                                   int(ignore_index), _ptr(dw), dim, _ptr(ws), n.value,
-                                   _stream(device)), "pvs_embed_backward")
+                                   int(ignore_index), _ptr(dw), dim, _ptr(ws), n, _stream(device)),
+           "pvs_embed_backward")
     return dw
 
 
@@ -627,6 +654,11 @@ def pvs_mx_unpack(codes, scales, row_scales, group: int, cols: int, dtype):
     return out
 
 
+@functools.lru_cache(maxsize=4096)
+def _mx_bytes(device: int, batch: int, rows: int, cols: int, group: int) -> int:
+    return _asked("pvs_mx_workspace", batch, rows, cols, group)
+
+
 def pvs_mx_matmul(x, codes, scales, row_scales, group: int):
     """``x @ weights.T`` [B, N] in x's type, for any number of rows x [B, K] and weights packed by
     ``pvs_mx_pack``; x is put into the same format first, so that both operands have 4 bits."""
@@ -644,9 +676,8 @@ def pvs_mx_matmul(x, codes, scales, row_scales, group: int):
     if n > _MAX_ROWS:
         raise ValueError(f"the weights have more than {_MAX_ROWS} rows")
     y = torch.empty(b, n, dtype=x.dtype, device=device)
-    size = ctypes.c_size_t()
-    _check(_lib.pvs_mx_workspace(b, n, k, group, ctypes.byref(size)), "pvs_mx_workspace")
-    ws = _workspace(size.value, device)
+    size = _mx_bytes(device, b, n, k, group)
+    ws = _workspace(size, device)
     _check(_lib.pvs_mx_matmul(_ptr(x), ldx, b, _ptr(codes), _ptr(scales), _ptr(row_scales), n, k, group, dt,
-                              _ptr(y), n, _ptr(ws), size.value, _stream(device)), "pvs_mx_matmul")
+                              _ptr(y), n, _ptr(ws), size, _stream(device)), "pvs_mx_matmul")
     return y
