@@ -164,6 +164,7 @@ struct LookupArgs {
     void* y;
     int64_t ldy;
     int slabs;
+    int lane_bits;                   // 2^this lanes to a row: 5, or fewer where that is all of it
 };
 
 // A warp takes neighbouring pieces of 256 columns of y, their loads in flight together: four of
@@ -175,19 +176,29 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_forward_kernel(const Look
     constexpr int kLookups = lookups(WIDE);
     next_early();
     wait_before();
-    const int64_t pieces = a.rows * a.slabs;
     const int64_t p0 = ((int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5)) * kLookups;
-    if (p0 >= pieces) return;
     int64_t row[kLookups], id[kLookups];
     int col0[kLookups];
     Share<WIDE, DT> in[kLookups];
-    row[0] = quotient_of(p0, a.slabs);
-    col0[0] = (int)(p0 - row[0] * a.slabs) * kSlab;
+    if (WIDE && a.lane_bits < 5) {
+        // narrow rows: several of them side by side
+        const int lane = threadIdx.x & 31, rows = 32 >> a.lane_bits;
+        if (p0 * rows >= a.rows) return;
 #pragma unroll
-    for (int i = 1; i < kLookups; ++i) {
-        const bool next = col0[i - 1] + kSlab >= a.dim;
-        row[i] = row[i - 1] + (next ? 1 : 0);
-        col0[i] = next ? 0 : col0[i - 1] + kSlab;
+        for (int i = 0; i < kLookups; ++i) {
+            row[i] = (p0 + i) * rows + (lane >> a.lane_bits);
+            col0[i] = -8 * (lane >> a.lane_bits << a.lane_bits);
+        }
+    } else {
+        if (p0 >= a.rows * a.slabs) return;
+        row[0] = quotient_of(p0, a.slabs);
+        col0[0] = (int)(p0 - row[0] * a.slabs) * kSlab;
+#pragma unroll
+        for (int i = 1; i < kLookups; ++i) {
+            const bool next = col0[i - 1] + kSlab >= a.dim;
+            row[i] = row[i - 1] + (next ? 1 : 0);
+            col0[i] = next ? 0 : col0[i - 1] + kSlab;
+        }
     }
 #pragma unroll
     for (int i = 0; i < kLookups; ++i) id[i] = row[i] < a.rows ? __ldg(a.ids + row[i]) : a.ignore_index;
@@ -849,7 +860,9 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     a.ldy = ldy;
     a.slabs = (dim + kSlab - 1) / kSlab;
     const bool wide = dim % 8 == 0 && on_16(w, ldw, dtype) && on_16(y, ldy, dtype);
-    const int64_t per_block = kEmbedWarps * lookups(wide);
+    a.lane_bits = 5;
+    while (wide && a.lane_bits > 0 && 8 << (a.lane_bits - 1) >= dim) --a.lane_bits;
+    const int64_t per_block = (int64_t)kEmbedWarps * lookups(wide) * (32 >> a.lane_bits);
     const int64_t blocks = (rows * a.slabs + per_block - 1) / per_block;
     if (blocks > 0x7fffffff) return PVS_ERR_INVALID;
     count_launches(1);
