@@ -565,9 +565,15 @@ struct Sum {
         clear();
     }
 };
-// kPiece sorted entries to a warp, and 256 columns.
+
+// kPiece sorted entries to a warp, and 256 columns.  Blocks to an SM: as many as the rows in flight
+// leave registers for; small calls (pieces of eight) have few blocks and twice the rows in flight.
+constexpr int sum_blocks_of(bool wide, int dtype, int piece) {
+    return piece == 8 ? 1 : wide && dtype != PVS_F32 ? 3 : 2;
+}
 template <bool WIDE, int DT, int kPiece>
-__global__ void __launch_bounds__(kEmbedThreads, kPiece == 8 ? 1 : WIDE && DT != PVS_F32 ? 3 : 2) embed_sum_kernel(const SumArgs a) {
+__global__ void __launch_bounds__(kEmbedThreads, sum_blocks_of(WIDE, DT, kPiece))
+    embed_sum_kernel(const SumArgs a) {
     next_early();
     wait_before();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -579,7 +585,8 @@ __global__ void __launch_bounds__(kEmbedThreads, kPiece == 8 ? 1 : WIDE && DT !=
     const int64_t of_kind = b < 2 * turns ? b >> 1 : b - turns;
     if (!sums) {
         // (2^zero_bits warps share the rows of a group)
-        const int64_t w = of_kind * kEmbedWarps + warp, step = (zero_blocks * kEmbedWarps >> a.zero_bits) * a.zero_rows;
+        const int64_t w = of_kind * kEmbedWarps + warp;
+        const int64_t step = (zero_blocks * kEmbedWarps >> a.zero_bits) * a.zero_rows;
         const uint32_t mine = (a.zero_bits == 0   ? 0xffffffffu
                                : a.zero_bits == 1 ? 0x55555555u
                                : a.zero_bits == 2 ? 0x11111111u
