@@ -7,9 +7,10 @@
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
 // call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes
 // 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and writes the rows
-// whose entries start among them; of rows with more than kLong entries the pieces' sums are kept in float32 and joined by a second launch.  Rows without an entry are
-// found by search in the sorted ids and filled with zeros by other blocks of the first: no
-// row of dw is written twice.
+// whose entries start among them; of rows with more than kLong entries the pieces' sums are
+// kept in float32 and joined by a second launch.  Rows without an entry are found by search in
+// the sorted ids and filled with zeros by other blocks of the first: no row of dw is written
+// twice.
 //
 // 131,072 ids after Zipf's law in 200,000 rows of 1,024, bf16 (36,000 rows of them named), in us: lookup 66
 // (5.1 TB/s of 342 MB; issue 64%), sorting 33 in six launches, sums and zeros 114 (6.0 TB/s of 678

@@ -462,9 +462,12 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
                         const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(rb + j);
+                        auto two = [&](int k) {
+                            return f2_mul(f2_pack(__uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1])), by);
+                        };
                         float v0, v1, v2, v3;
-                        f2_unpack(f2_mul(f2_mul(f2_pack(__uint_as_float(r[i][j]), __uint_as_float(r[i][j + 1])), by), f.x), v0, v1);
-                        f2_unpack(f2_mul(f2_mul(f2_pack(__uint_as_float(r[i][j + 2]), __uint_as_float(r[i][j + 3])), by), f.y), v2, v3);
+                        f2_unpack(f2_mul(two(j), f.x), v0, v1);
+                        f2_unpack(f2_mul(two(j + 2), f.y), v2, v3);
                         r[i][j] = __float_as_uint(v0), r[i][j + 1] = __float_as_uint(v1);
                         r[i][j + 2] = __float_as_uint(v2), r[i][j + 3] = __float_as_uint(v3);
                     }
