@@ -278,8 +278,10 @@ pvs_status pvs_mx_unpack(const uint8_t* codes, const uint8_t* scales, const floa
 
 /* y [batch x rows] in x's type = x [batch x cols], put into the weights' format as pvs_mx_pack
  * does, times the transposed weights [rows x cols]: products of codes are exact, sums float32,
- * y rounded once from them (group 16: from the sum times both row scales).  Scratch: x in that
- * format, and float32 sums of a few units of y where k is split. */
+ * y rounded once from them (group 16: from the sum times both row scales, right wherever that is a
+ * float32; group 32: its scales are in the sums, which are infinite or NaN where one leaves
+ * float32's range on its way).  Scratch: x in that format, and float32 sums of a few units of y
+ * where k is split. */
 pvs_status pvs_mx_workspace(int64_t batch, int64_t rows, int32_t cols, int32_t group, size_t* bytes);
 pvs_status pvs_mx_matmul(const void* x, int64_t ldx, int64_t batch, const uint8_t* codes,
                          const uint8_t* scales, const float* row_scales, int64_t rows, int32_t cols,

@@ -881,7 +881,8 @@ constexpr int kSumThreads = 128;
 __global__ void __launch_bounds__(kSumThreads) sum_slots_kernel(
     const float* __restrict__ slots, int splits, int64_t slot_stride, int64_t ldslot, int64_t rows,
     int n, int blocks_per_row, int rows_per_block, const float* __restrict__ alpha, float alpha0,
-    void* __restrict__ out, int64_t ldout, int out_type) {
+    void* __restrict__ out, int64_t ldout, int out_type, const float* __restrict__ row_scales,
+    const float* __restrict__ col_scales) {
     next_early();
     wait_before();
     const int pieces = (n + 3) / 4;
@@ -918,6 +919,14 @@ __global__ void __launch_bounds__(kSumThreads) sum_slots_kernel(
             s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
         }
         s.x *= f, s.y *= f, s.z *= f, s.w *= f;
+        if (col_scales) {
+            const float r = __ldg(row_scales + row);
+            const float* c = col_scales + col;
+            s.x = times_scales(s.x, r, __ldg(c));
+            if (col + 1 < n) s.y = times_scales(s.y, r, __ldg(c + 1));
+            if (col + 2 < n) s.z = times_scales(s.z, r, __ldg(c + 2));
+            if (col + 3 < n) s.w = times_scales(s.w, r, __ldg(c + 3));
+        }
         const int64_t at = row * ldout + col;
         if (out_type == PVS_F32) {
             float* o = static_cast<float*>(out) + at;
@@ -950,7 +959,8 @@ __global__ void __launch_bounds__(kSumThreads) sum_slots_kernel(
 constexpr int kSumFlight = 32;
 __global__ void __launch_bounds__(kSumThreads) sum_columns_kernel(
     const float* __restrict__ slots, int splits, int64_t slot_stride, int64_t ldslot, int n, int blocks_per_row,
-    const float* __restrict__ alpha, float alpha0, void* __restrict__ out, int64_t ldout, int out_type) {
+    const float* __restrict__ alpha, float alpha0, void* __restrict__ out, int64_t ldout, int out_type,
+    const float* __restrict__ row_scales, const float* __restrict__ col_scales) {
     next_early();
     wait_before();
     const float f = alpha ? alpha0 * __ldg(alpha) : alpha0;
@@ -970,6 +980,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_columns_kernel(
 #pragma unroll 8
     for (; k < splits; ++k) s += __ldg(p + k * slot_stride);
     s *= f;
+    if (col_scales) s = times_scales(s, __ldg(row_scales + row), __ldg(col_scales + col));
     if (out_type == PVS_F32)
         static_cast<float*>(out)[row * ldout + col] = s;
     else
@@ -979,21 +990,23 @@ __global__ void __launch_bounds__(kSumThreads) sum_columns_kernel(
 
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
-                             int64_t ldout, int out_type, cudaStream_t st) {
+                             int64_t ldout, int out_type, cudaStream_t st, const float* row_scales,
+                             const float* col_scales) {
     const int pieces = (n + 3) / 4;
     count_launches(1);
     // (152 SMs of eight such blocks)
     if (splits >= 16 && m * pieces < 152 * 8 * kSumThreads) {
         const int per_row = (n + kSumThreads - 1) / kSumThreads;
         return launch_early(sum_columns_kernel, m * per_row, kSumThreads, 0, st, slots, splits, slot_stride, ldslot,
-                            n, per_row, alpha, alpha0, out, ldout, out_type);
+                            n, per_row, alpha, alpha0, out, ldout, out_type, row_scales, col_scales);
     }
     const int blocks_per_row = (pieces + kSumThreads - 1) / kSumThreads;
     const int rows_per_block = std::max(1, kSumThreads / pieces);
     const int64_t blocks = blocks_per_row > 1 ? m * blocks_per_row : (m + rows_per_block - 1) / rows_per_block;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     return launch_early(sum_slots_kernel, blocks, kSumThreads, 0, st, slots, splits, slot_stride, ldslot,
-                        m, n, blocks_per_row, rows_per_block, alpha, alpha0, out, ldout, out_type);
+                        m, n, blocks_per_row, rows_per_block, alpha, alpha0, out, ldout, out_type, row_scales,
+                        col_scales);
 }
 
 // ---- operands in 16-bit parts ----------------------------------------------------

@@ -121,6 +121,17 @@ __device__ __forceinline__ int64_t quotient_of(int64_t n, int d) {
     return n <= 0xffffffffll ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
+// v a b where one scale alone may take v out of float32's normal range although the product is in it:
+// by both scales' product where they are on both sides of 1 (it is between them), else by the larger
+// first (on its way to 0 or infinity, v is there by both or still normal).  Powers of two are exact
+// to multiply by, so that the product is rounded once.
+__device__ __forceinline__ float times_scales(float v, float a, float b) {
+    const bool first = fabsf(a) >= fabsf(b);
+    const float most = first ? a : b, least = first ? b : a;
+    if (fabsf(most) >= 1.0f && fabsf(least) < 1.0f) return v * (most * least);
+    return v * most * least;
+}
+
 // Whether a row has no gradient, whatever it holds: by its target, or (there are none: rows have
 // lists) by its statistics.
 __device__ __forceinline__ bool ignored_row(const int64_t* targets, int64_t ignore_index, const float4* stats,
@@ -197,10 +208,11 @@ cudaError_t launch_gemm(int epilogue, Args& a, const Device& dev, cudaStream_t s
 // Pairs where there are more rows than one CTA takes.
 inline int ctas_for(int64_t m, const Device& dev) { return m > kTileM && dev.pairs > 0 ? 2 : 1; }
 
-// out = alpha sum_s slots[s], rounded once.
+// out = alpha sum_s slots[s], rounded once; with scales of its rows and columns, that times both.
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
-                             int64_t ldout, int out_type, cudaStream_t st);
+                             int64_t ldout, int out_type, cudaStream_t st,
+                             const float* row_scales = nullptr, const float* col_scales = nullptr);
 
 // src [rows x cols] of `dtype` to `parts` 16-bit matrices [rows x ldd] (f16 where
 // to_f16, else bf16), rows that `zero_target` ignores (or whose zero_bias is

@@ -219,6 +219,14 @@ __device__ __forceinline__ uint32_t mx_two(uint32_t lo, uint32_t hi, __half) {
     const __half2 v = __floats2half2_rn(__uint_as_float(lo), __uint_as_float(hi));
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+// Whether the product of a sum and one of the warp's scales may leave float32's normal range, so that
+// the order of its products with both scales matters.  A sum is below 2^38 (32,767 products of
+// codes of 6 at most and scales of 448), and no less than 2^-20 where it is not zero (codes are
+// whole halves, scales whole 2^-9): 2^-106 to 2^89 keep the product from 2^-126 to 2^128.  Scales
+// of rows that hold anything from 2^-95 to 2^98 are in there.
+__device__ __forceinline__ bool mx_apart(float ra) {
+    return __any_sync(0xffffffffu, !(fabsf(ra) >= 0x1p-106f && fabsf(ra) <= 0x1p89f));
+}
 // 32 whole rows of 32 neighbours of 16 bits, on 4 bytes: even lanes store the pairs of even rows,
 // odd ones those of odd rows.
 template <typename T>
@@ -414,9 +422,11 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const int n0 = w.nt * a.bn, ncols = min(a.bn, a.n - n0);
             const int row = (w.mt * kCta + crank) * 128 + quarter * 32 + lane;
             float ra = 1.0f;
-            if (kSixteen) {
+            bool apart = false;
+            if (kSixteen && a.splits == 1) {
                 // (before the wait, under which the loads are done)
                 if (row < a.m) ra = __ldg(a.row_a + row);
+                apart = mx_apart(ra);
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -456,7 +466,12 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             for (int i = 0; i < 4; ++i) {
                 const int c0 = (2 * i + group) * 32, count = ncols - c0;
                 if (count <= 0) break;
-                if (kSixteen) {
+                if (kSixteen && apart) {
+                    const float* rb = sh.row_b[warp - 2][i];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        r[i][j] = __float_as_uint(times_scales(__uint_as_float(r[i][j]), ra, rb[j]));
+                } else if (kSixteen && a.splits == 1) {
                     const float* rb = sh.row_b[warp - 2][i];
                     const uint64_t by = f2_pack(ra, ra);
 #pragma unroll
@@ -614,7 +629,7 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     e = cudaLaunchKernelExC(&cfg, fn, args);
     if (e == cudaSuccess && p.splits > 1)
         e = launch_sum_slots(p.slots, p.splits, a.slot_stride, p.ldslot, batch, (int)rows, nullptr, 1.0f, y, ldy,
-                             dtype, st);
+                             dtype, st, p.rows, group == 16 ? row_scales : nullptr);
     return e;
 }
 
