@@ -325,6 +325,8 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
             s = s * exp2f(m - ref) + ssum;
             m = tm;
         }
+        // (every logit is -inf: no softmax, and not the mark of a row without a list)
+        if (m == -INFINITY) s = nan;
         const float log_s = logf(s);
         float loss = 0.0f;
         for (int k = lane; k < n; k += 32) {
