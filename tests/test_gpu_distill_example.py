@@ -127,3 +127,31 @@ def test_calls_from_two_streams_at_once(example):
     for out in got:
         for a, b in zip(out, want):
             assert torch.equal(a, b)
+
+
+def test_vectors_of_the_packed_layer(example):
+    # serving: the rows' sums and the product of what both packed operands stand for, in binary64
+    head = example.Head(200, 128, 64, seed=8)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    tokens = torch.randint(0, 200, (300, 6), generator=g, device="cuda")
+    tokens[torch.rand(300, 6, generator=g, device="cuda") < 0.2] = example.EMPTY
+    tokens[:, 0] = torch.arange(300, device="cuda") % 200
+    rows = head.table.double()[tokens.clamp(min=0)] * (tokens != example.EMPTY)[..., None]
+    x = head.pooled(tokens)
+    # six float32 products and their sum
+    assert ((x.double() - rows.sum(dim=1) * 6 ** -0.5).abs() <= 6 * 2.0 ** -23 * rows.abs().sum(dim=1)).all()
+    packed = pvs.pvs_mx_pack(head.w, example.GROUP)
+
+    def stands_for(p):
+        return pvs.pvs_mx_unpack(*p, example.GROUP, 128, torch.float32).double()
+
+    want = stands_for(pvs.pvs_mx_pack(x, example.GROUP)) @ stands_for(packed).T
+    want = want / want.norm(dim=1, keepdim=True)
+    got = head.vectors(tokens, packed)
+    # (128 / 64 + 8) 2^-23 of sums of magnitudes, which are about 0.64 128^1/2 = 7.2 times as large as the
+    # sums: 72 2^-23, and some 2^-22 for the norm
+    assert float((got.double() - want).norm(dim=1).max()) <= 2.0 ** -16
+    # against the float32 layer: a code is off by a fifth of its element at most (from 5/2), by about a
+    # tenth in the mean, in both operands and alike in no direction: 0.15 of a vector, a third of the bound
+    exact = head.vectors(tokens).double()
+    assert float((got.double() - exact).norm(dim=1).max()) <= 0.5

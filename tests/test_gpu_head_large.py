@@ -87,3 +87,44 @@ def test_microscaled_rows(table, group):
     x = table[:5].clone()
     y = pvs.pvs_mx_matmul(x, codes, scales, rows, group)
     assert torch.equal(y[:, V - 300:], pvs.pvs_mx_matmul(x, *few, group))
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_distillation_gradients_over_all_items(table, T):
+    # both gradients, of items on both sides of the offset, against binary64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = (torch.randn(T, D, generator=g, device="cuda") / D ** 0.5).to(BF16)
+    ids = torch.cat([torch.randint(0, 1000, (T, 4), generator=g, device="cuda"),
+                     torch.randint(V - 1000, V, (T, 4), generator=g, device="cuda")], dim=1)
+    z = torch.randn(T, 8, generator=g, device="cuda")
+    grad = torch.rand(T, generator=g, device="cuda") + 0.5
+    _, stats, hits = pvs.pvs_distill_forward(x, table, ids, z)
+    dx, dw = pvs.pvs_distill_backward(x, table, ids, stats, hits, grad)
+    pieces = [(i, min(i + (1 << 18), V)) for i in range(0, V, 1 << 18)]
+    X, p, gr = x.double(), torch.softmax(z.double(), dim=1), grad.double()[:, None]
+    lse = torch.logsumexp(torch.stack([torch.logsumexp(X @ table[a:b].double().T, dim=1) for a, b in pieces]), dim=0)
+    # an entry of G: a logit's steps of 16 and its rounding in a share of q, 2^-20 of p and its
+    # exponent's rounding, and 2^-15 for the two parts; a sum: its steps of 16, cut to 24 bits
+    e = (D / 16 + 4) * 2.0 ** -23 * 8.0 * float(X.norm(dim=1).max()) * D ** 0.5 + 2.0 ** -19
+    t = 2.0 ** -20 + 2.0 ** -22 * 8.0 + 2.0 ** -15
+    want, size, off = (torch.zeros(T, D, dtype=torch.float64, device="cuda") for _ in range(3))
+    rows = torch.cat([torch.arange(40, device="cuda"), torch.arange(2_097_130, 2_097_170, device="cuda"),
+                      torch.arange(V - 40, V, device="cuda"), ids[0], ids[T - 1]])
+    for a, b in pieces:
+        W = table[a:b].double()
+        q = torch.exp(X @ W.T - lse[:, None]) * gr
+        here = (ids >= a) & (ids < b)
+        P = torch.zeros_like(q).scatter_add_(1, (ids - a).clamp(0, b - a - 1), torch.where(here, p, 0.0) * gr)
+        want += (q - P) @ W
+        size += (q + P) @ W.abs()
+        off += ((2 * e + 2.0 ** -15) * q + t * P) @ W.abs()
+        j = rows[(rows >= a) & (rows < b)]
+        if len(j):
+            G = (q - P)[:, j - a].T
+            to = G @ X
+            slack = (((2 * e + 2.0 ** -15) * q + t * P)[:, j - a].T + (T / 16 + 8) * 2.0 ** -23 * G.abs()) @ X.abs()
+            assert ((dw[j].double() - to).abs() <= slack + 2.0 ** -8 * to.abs() + 2.0 ** -126).all()
+    tol = off + (V / 16 + 8) * 2.0 ** -23 * size + 2.0 ** -8 * want.abs()
+    assert ((dx.double() - want).abs() <= tol).all()
+    # (the bound is far below the gradients: items that were not read would show)
+    assert float(tol.norm()) < 0.1 * float(want.norm())
