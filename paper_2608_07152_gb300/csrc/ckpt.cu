@@ -757,6 +757,6 @@ extern "C" pvs_status pvs_ckpt_grad_weight(const void* dy, int64_t lddy, const i
     }
     if (e == cudaSuccess && p.slots)
         e = launch_sum_slots(p.slots, p.splits, (int64_t)out_cols * p.ldslot, p.ldslot, out_cols, cols,
-                             nullptr, 1.0f, dw, lddw, dtype, st);
+                             nullptr, 1.0f, dw, lddw, dtype, dev, st);
     return queued(e);
 }

@@ -175,8 +175,7 @@ __device__ __forceinline__ void load_32b(const void* p, uint32_t* v) {
 // A lane's 64 bytes of its row, rows `ld` elements apart: neighbouring lanes turn two rows' sectors
 // round, so that a store writes 64 bytes of 16 rows, not 32 of 32 (G of 8,192 rows over 8,192
 // items took 117 us that way; without any store 73).  `rows` of the warp's 32 exist.
-template <typename T>
-__device__ __forceinline__ void store_two_rows(T* o, int64_t ld, const uint32_t (&h)[16], int rows) {
+__device__ __forceinline__ void store_two_rows(uint16_t* o, int64_t ld, const uint32_t (&h)[16], int rows) {
     const int lane = threadIdx.x & 31;
     const bool odd = lane & 1;
     uint32_t even_row[8], odd_row[8];
@@ -186,7 +185,7 @@ __device__ __forceinline__ void store_two_rows(T* o, int64_t ld, const uint32_t 
         even_row[i] = odd ? got : h[i];
         odd_row[i] = odd ? h[8 + i] : got;
     }
-    T* p = o - (odd ? ld : 0) + (odd ? 32 / sizeof(T) : 0);
+    uint16_t* p = o - (odd ? ld : 0) + (odd ? 16 : 0);
     if ((lane & ~1) < rows) store_32b(p, even_row);
     if ((lane | 1) < rows) store_32b(p + ld, odd_row);
 }
@@ -990,12 +989,12 @@ __global__ void __launch_bounds__(kSumThreads) sum_columns_kernel(
 
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
-                             int64_t ldout, int out_type, cudaStream_t st, const float* row_scales,
-                             const float* col_scales) {
+                             int64_t ldout, int out_type, const Device& dev, cudaStream_t st,
+                             const float* row_scales, const float* col_scales) {
     const int pieces = (n + 3) / 4;
     count_launches(1);
-    // (152 SMs of eight such blocks)
-    if (splits >= 16 && m * pieces < 152 * 8 * kSumThreads) {
+    // (less than eight such blocks an SM)
+    if (splits >= 16 && m * pieces < (int64_t)dev.sms * 8 * kSumThreads) {
         const int per_row = (n + kSumThreads - 1) / kSumThreads;
         return launch_early(sum_columns_kernel, m * per_row, kSumThreads, 0, st, slots, splits, slot_stride, ldslot,
                             n, per_row, alpha, alpha0, out, ldout, out_type, row_scales, col_scales);

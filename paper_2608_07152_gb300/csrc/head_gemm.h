@@ -211,7 +211,7 @@ inline int ctas_for(int64_t m, const Device& dev) { return m > kTileM && dev.pai
 // out = alpha sum_s slots[s], rounded once; with scales of its rows and columns, that times both.
 cudaError_t launch_sum_slots(const float* slots, int splits, int64_t slot_stride, int64_t ldslot,
                              int64_t m, int n, const float* alpha, float alpha0, void* out,
-                             int64_t ldout, int out_type, cudaStream_t st,
+                             int64_t ldout, int out_type, const Device& dev, cudaStream_t st,
                              const float* row_scales = nullptr, const float* col_scales = nullptr);
 
 // src [rows x cols] of `dtype` to `parts` 16-bit matrices [rows x ldd] (f16 where

@@ -629,7 +629,7 @@ cudaError_t mx_product(const MxPlan& p, int64_t batch, const uint8_t* codes, con
     e = cudaLaunchKernelExC(&cfg, fn, args);
     if (e == cudaSuccess && p.splits > 1)
         e = launch_sum_slots(p.slots, p.splits, a.slot_stride, p.ldslot, batch, (int)rows, nullptr, 1.0f, y, ldy,
-                             dtype, st, p.rows, group == 16 ? row_scales : nullptr);
+                             dtype, dev, st, p.rows, group == 16 ? row_scales : nullptr);
     return e;
 }
 

@@ -648,7 +648,7 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         }
         if (e == cudaSuccess && dx)
             e = launch_sum_slots(p.xslots, p.few, T * p.lds, p.lds, T, a.dim, nullptr, a.scale, dx,
-                                 lddx, a.dtype, st);
+                                 lddx, a.dtype, dev, st);
         return e;
     }
     const Matrix x{p.x, T, a.dim, p.ldp, p.parts, T * p.ldp};
@@ -743,11 +743,11 @@ cudaError_t backward(const pvs_xent_args& a, const Plan& p, const Device& dev, c
         e = launch_gemm(kOut, g, dev, st);
         if (e == cudaSuccess && qw && qw->to_slots)
             e = launch_sum_slots(p.wslots, qw->splits, qw->slot_stride, p.lds, n, a.dim, alpha,
-                                 a.scale, qw->out, lddw, a.dtype, st);
+                                 a.scale, qw->out, lddw, a.dtype, dev, st);
     }
     if (e == cudaSuccess && dx && p.xslots)
         e = launch_sum_slots(p.xslots, p.xsplits, T * p.lds, p.lds, T, a.dim, alpha, a.scale, dx,
-                             lddx, a.dtype, st);
+                             lddx, a.dtype, dev, st);
     return e;
 }
 
