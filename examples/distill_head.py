@@ -1,7 +1,7 @@
 """A query head over token embeddings, distilled from a teacher and served in 4-bit floats.
 
-Queries are short lists of token ids.  A table turns tokens into rows, a query is the mean of
-its rows, and one layer makes its vector.  Instead of one right item, each query has a teacher's
+Queries are short lists of token ids.  A table turns tokens into rows, a query is the sum of
+its rows over the root of their number, and one layer makes its vector.  Instead of one right item, each query has a teacher's
 scores of a few items (a slower model's list); a step lowers the divergence of the head's softmax
 over the whole collection from it.  Afterwards the layer is packed in microscaled 4-bit floats, a
 batch of queries goes through it at once, and their vectors read exact ranks from the index.
@@ -28,7 +28,7 @@ EMPTY = -100          # a token or a slot of a list that is not there
 
 
 class Head:
-    """tokens [B, L] -> rows of `table` [V, H] -> their mean -> `w` [D, H] -> vectors [B, D]."""
+    """tokens [B, L] -> rows of `table` [V, H] -> their sum L^-1/2 -> `w` [D, H] -> vectors [B, D]."""
 
     def __init__(self, vocabulary: int, hidden: int, dim: int, seed: int = 0, lr: float = 2e-2):
         g = torch.Generator(device="cuda").manual_seed(seed)
@@ -37,7 +37,7 @@ class Head:
         self.adam = torch.optim.Adam([self.table, self.w], lr=lr)
 
     def pooled(self, tokens):
-        """The mean [B, H] of the tokens' rows (an empty token counts as zeros)."""
+        """The sum [B, H] of the tokens' rows times L^-1/2 (an empty token counts as zeros)."""
         b, n = tokens.shape
         rows = pvs.pvs_embed_forward(self.table, tokens.reshape(-1), scale=n ** -0.5, ignore_index=EMPTY)
         return rows.view(b, n, -1).sum(dim=1)

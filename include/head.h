@@ -256,7 +256,9 @@ pvs_status pvs_wq_matvec(const void* x, int64_t ldx, int32_t batch, const uint8_
  *              infinity, with codes 0.
  *   group 16   each row has a power of two r = 2^(floor(log2 max|x_row|) - 10), 2^-126 at least (1
  *              for a zero row; NaN, with scales and codes 0, for a row that holds a NaN or an
- *              infinity), and a group the scale s = RN_e4m3(RN(max|x| RN(1 / 6)) / r), in units of r.
+ *              infinity), and a group the scale s = RN_e4m3(RN(max|x| RN(1 / 6)) / r), in units of r
+ *              (of float32's 2^23 significands one, which lies beside a border of e4m3, gets the scale
+ *              on its other side than max|x| / 6 would; none of 16 bits does).
  * An element is the nearest of those values to x / scale, of two the one with an even code,
  * 6 beyond 6; 0 where the scale is 0.
  * codes: uint8 [rows x kp / 2] without gaps, 16-byte aligned; the lower half of a byte comes first,

@@ -17,7 +17,9 @@
 // their logits 47 (403 MB of rows, out of the L2: 8.5 TB/s), the product 38 (as without lists), join 12;
 // rows and copy 8, G 54, listed entries 11, both gradients 137.  2,048 over 200,000 of 1,024
 // in f16, lists of 128: 24, 64 (537 MB), 490, 20; backward 2,700.  (Logits within the joining launch,
-// 32 rows of w in flight an SM, took it to 100 and 294.)
+// 32 rows of w in flight an SM, took it to 100 and 294.)  It grows with the lists, whatever the
+// product takes: the first with lists of 1,024 171, 598 (6.4 GB, 10.8 TB/s; issue at 68%, the
+// L2 at 42%), 120 and 187.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -330,7 +332,8 @@ __global__ void __launch_bounds__(256) top_join_kernel(const TopJoin j) {
         const float log_s = logf(s);
         float loss = 0.0f;
         for (int k = lane; k < n; k += 32) {
-            // the run of slots that name the same item
+            // the run of slots that name the same item (each slot walks all of it: 4,096 lists that
+            // name one item 64 times take 129 us for 96, 1,024 times 8.2 ms for 1.0)
             int first = k, last = k;
             while (first > 0 && id[first - 1] == id[k]) --first;
             while (last + 1 < n && id[last + 1] == id[k]) ++last;

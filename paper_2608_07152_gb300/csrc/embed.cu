@@ -6,7 +6,7 @@
 // Both are bound by memory.  The backward pass sorts (id, t) first, so that a row's sum runs
 // over neighbours, nothing is added by atomics and the result depends on nothing but the
 // call: up to kSmall ids in one block, more in three launches for each 10 bits.  Then a warp takes
-// 32 (or 8) sorted entries by 256 columns, eight rows' loads in flight, and writes the rows
+// 32 (or 8) sorted entries by 256 columns, eight (or 16) rows' loads in flight, and writes the rows
 // whose entries start among them; of rows with more than kLong entries the pieces' sums are
 // kept in float32 and joined by a second launch.  Rows without an entry are found by search in
 // the sorted ids and filled with zeros by other blocks of the first: no row of dw is written
@@ -160,7 +160,7 @@ struct LookupArgs {
     int64_t ldw, items;
     const int64_t* ids;
     int64_t rows, ignore_index;
-    int dim, dtype;
+    int dim;
     float scale;
     void* y;
     int64_t ldy;
@@ -738,8 +738,9 @@ struct EmbedPlan {
     size_t bytes = 0;
 };
 
-// (pieces of 32 by 256 columns that give each of 152 SMs eight warps: 5,000 rows of 385 took a
-// sum of 44 us in them)
+// Pieces of 32 by 256 columns that give each of 152 SMs eight warps (5,000 rows of 385 took a sum of
+// 44 us in them).  A constant, not the device's count: the order of a sum and the scratch, which are
+// the call's alone, follow from it.
 constexpr int64_t kFewUnits = 32 * 8 * 152;
 
 EmbedPlan embed_plan(int64_t n, int64_t items, int dim, void* workspace) {
@@ -862,7 +863,6 @@ extern "C" pvs_status pvs_embed_forward(const void* w, int64_t ldw, int64_t item
     a.rows = rows;
     a.ignore_index = ignore_index;
     a.dim = dim;
-    a.dtype = dtype;
     a.scale = scale;
     a.y = y;
     a.ldy = ldy;

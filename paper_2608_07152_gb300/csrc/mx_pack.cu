@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kPackThreads, pack_blocks(kSixteen, DT)) mx_pa
                 ++turn;
             }
             rs.bad = top >= 0x7f800000u;
-            // 2^(floor(log2 top) - 10): the scales of groups then reach 171 to 352 of 448
+            // 2^(floor(log2 top) - 10): the largest scale of its groups is 176 to 352, of 448
             const int e = top == 0 ? 127 : max((int)(top >> 23) - 10, 1);
             rs.r = __uint_as_float((uint32_t)e << 23);
             rs.up = __uint_as_float((uint32_t)(254 - e) << 23);
