@@ -305,9 +305,8 @@ __device__ __forceinline__ float value_of(uint32_t n) {
     return __uint_as_float(f | (n & 8u) << 28);
 }
 template <bool kSixteen>
-__device__ __forceinline__ float unit_of(uint32_t byte, float row_scale) {
-    if (kSixteen)
-        return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * row_scale;
+__device__ __forceinline__ float unit_of(uint32_t byte) {
+    if (kSixteen) return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
     return byte == 255 ? __int_as_float(0x7fffffff) : byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
 }
 __device__ __forceinline__ uint16_t mx_narrow(float v, int dtype) {
@@ -315,7 +314,9 @@ __device__ __forceinline__ uint16_t mx_narrow(float v, int dtype) {
 }
 
 // What codes stand for: eight a thread where rows of `out` are aligned, else one, so that
-// neighbours write neighbours.
+// neighbours write neighbours.  A code's value times its group's scale is exact, so that the product
+// with the row's is the only one that rounds (both scales together may be infinite, or no whole
+// number of the smallest float32).
 constexpr int kUnpack = 4;
 template <bool kSixteen, bool WIDE>
 __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* __restrict__ codes,
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
 #pragma unroll 4
             for (int c = threadIdx.x & 31; c < cols; c += 32) {
                 const uint32_t n = __ldg(codes + row * (kp / 2) + c / 2) >> (4 * (c & 1)) & 15u;
-                const float v = value_of(n) * unit_of<kSixteen>(scale_at(row, c), rs);
+                const float v = value_of(n) * unit_of<kSixteen>(scale_at(row, c)) * rs;
                 if (dtype == PVS_F32)
                     static_cast<float*>(out)[row * ldout + c] = v;
                 else
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
         }
         if (c >= cols) continue;
         const uint32_t word = __ldg(reinterpret_cast<const uint32_t*>(codes + row * (kp / 2) + c / 2));
-        const float unit = unit_of<kSixteen>(scale_at(row, c), kSixteen ? __ldg(row_scales + row) : 1.0f);
+        const float unit = unit_of<kSixteen>(scale_at(row, c)), rs = kSixteen ? __ldg(row_scales + row) : 1.0f;
         float v[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -371,6 +372,7 @@ __global__ void __launch_bounds__(kPackThreads) mx_unpack_kernel(const uint8_t* 
             v[2 * k + 1] = f.y;
         }
         times(v, unit);
+        if (kSixteen) times(v, rs);
         const int64_t at = row * ldout + c;
         if (dtype == PVS_F32) {
             float* o = static_cast<float*>(out) + at;

@@ -1,4 +1,4 @@
-"""Products of microscaled rows whose sizes are far apart, against the format's definition in binary64.
+"""Products and rows of microscaled codes whose sizes are far apart, against the definition in binary64.
 
 An output is rounded once, from a sum of exact products of codes and group scales times the row
 scales: it has to be right wherever it is a float32, whatever either row scale does to the sum
@@ -106,3 +106,22 @@ def test_f16_outputs_of_large_weights(b):
     check(x, (codes, scales, torch.ldexp(rows, torch.tensor(-2, device="cuda"))), 16)
     # (2^110 and the rows' own 2^-14 to 2^-24: every output is infinite, or nothing)
     check(x, (codes, scales, torch.ldexp(rows, torch.tensor(110, device="cuda"))), 16)
+
+
+@pytest.mark.parametrize("k", [128, 385])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_unpacked_rows_of_callers_scales(k, dtype):
+    # a code's value times its group's scale is exact: one product, rounded to float32, and its rounding
+    x = rows_of(200, k, F32, 7, [0])
+    x[:, 32:48] = 0.0                        # (a group of zeros, and codes of zero beside large ones)
+    x[:, 50] *= 2.0 ** 12
+    codes, scales, rows = pvs.pvs_mx_pack(x, 16)
+    units = stands_for((codes, scales, torch.ones_like(rows)), 16, k)
+    r = torch.ldexp(rows, torch.tensor([-140, -126, -100, 0, 100, 119, 126], device="cuda")[torch.arange(200, device="cuda") % 7])
+    r[3] = 3.4e38
+    r[11] = -1.3 * 2.0 ** -145
+    want = (units * r.double()[:, None]).float().to(dtype)
+    got = pvs.pvs_mx_unpack(codes, scales, r, 16, k, dtype)
+    # (some of those scales are infinite: codes of zero are NaN there, and nowhere else)
+    bad = torch.isinf(r)[:, None] & (units == 0.0)
+    assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], want[~bad])
