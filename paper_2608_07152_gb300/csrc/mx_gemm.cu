@@ -223,7 +223,8 @@ __device__ __forceinline__ uint32_t mx_two(uint32_t lo, uint32_t hi, __half) {
 // the order of its products with both scales matters.  A sum is below 2^38 (32,767 products of
 // codes of 6 at most and scales of 448), and no less than 2^-20 where it is not zero (codes are
 // whole halves, scales whole 2^-9): 2^-106 to 2^89 keep the product from 2^-126 to 2^128.  Scales
-// of rows that hold anything from 2^-95 to 2^98 are in there.
+// of rows whose largest element is 2^-95 to 2^98 are in there.  (Scales in either order cost the products
+// with them alone: 16,384 rows by 4,096 with 4,096 and 1,024 of k take 139 and 90 us, for 129 and 61.)
 __device__ __forceinline__ bool mx_apart(float ra) {
     return __any_sync(0xffffffffu, !(fabsf(ra) >= 0x1p-106f && fabsf(ra) <= 0x1p89f));
 }
